@@ -395,6 +395,94 @@ sdm_status sdm_test_recur_wait_timeout(const sdm_shape* shape, const int32_t* id
                                        void* workspace, size_t workspace_bytes, int64_t wait_cycles,
                                        sdm_stream_t stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Gated delta rule on a dense state (Sec. 2, Eq. gdn-update): the recurrence whose d_k x d_v state
+ * SDM replaces by slots.  For every sequence b, value head h and token t, with S [d_k, d_v]:
+ *   S~ = alpha_t S;  e_t = v_t - S~^T k_t;  S = S~ + beta_t k_t e_t^T;  y_t = scale S^T q_t.
+ * The state is float32 whatever the storage dtype: it is summed over every token of a sequence,
+ * across calls.  q and k have H_k heads, each shared by H / H_k consecutive value heads.
+ * ------------------------------------------------------------------------------------------ */
+enum { SDM_HEAD_MAJOR = 0,    /* q, k: [B, H_k, T, d_k]; v, y: [B, H, T, d_v] (as sdm_forward) */
+       SDM_TOKEN_MAJOR = 1 }; /* q, k: [B, T, H_k, d_k]; v, y: [B, T, H, d_v] (as sdm_linear writes them) */
+
+typedef struct {
+    int32_t B, H, H_k, T;     /* sequences, value heads, key heads (H a multiple of H_k), tokens */
+    int32_t d_k, d_v;         /* d_k <= 256; d_k and d_v times the element size multiples of 16 bytes */
+    int32_t dtype;            /* sdm_dtype of q, k, v, alpha, beta, y and of their gradients */
+    int32_t layout;           /* SDM_HEAD_MAJOR or SDM_TOKEN_MAJOR, of q, k, v, y and their gradients */
+    float scale;              /* of the read */
+} sdm_gdn_shape;
+
+/* Bytes of workspace of sdm_gdn_forward / sdm_gdn_backward (0 if none is needed; 0 with
+ * sdm_last_error set for an invalid shape). */
+size_t sdm_gdn_workspace_bytes(const sdm_gdn_shape* shape);
+size_t sdm_gdn_backward_workspace_bytes(const sdm_gdn_shape* shape);
+
+/* The recurrence over T tokens.  alpha, beta: [B, H, T] (as sdm_gates writes them); state:
+ * [B, H, d_k, d_v] float32, updated in place; y written.  lengths: NULL, or [B] int32 on the
+ * device: sequence b has lengths[b] tokens, and what q, k, v, alpha and beta hold past them is
+ * never used (it may be NaN); y is zero there and the state stays.  A length outside [0, T] is
+ * clamped and sets bit 0 of the device status word.  With T = 0 nothing is done.  bf16 calls with
+ * d_k <= 128 take a chunked form on the tensor cores from 64 tokens up (chunks of 64 tokens;
+ * operands split into bf16 parts wherever the state depends on them); others go token by token
+ * in fp32. */
+sdm_status sdm_gdn_forward(const sdm_gdn_shape* shape, const void* q, const void* k, const void* v,
+                           const void* alpha, const void* beta, const int32_t* lengths, float* state,
+                           void* y, void* workspace, size_t workspace_bytes, sdm_stream_t stream);
+
+/* One token of B sequences (shape->T must be 1) on a cache of n_slots states [n_slots, H, d_k, d_v]
+ * float32, updated in place.  slots: NULL (sequence b has row b; n_slots >= B), or [B] int32 on the
+ * device, the row of each sequence, no two the same; a negative slot skips its sequence (y = 0);
+ * one that is not below n_slots is skipped too and sets bit 0 of the device status word. */
+sdm_status sdm_gdn_step(const sdm_gdn_shape* shape, const void* q, const void* k, const void* v,
+                        const void* alpha, const void* beta, const int32_t* slots, int32_t n_slots,
+                        float* state, void* y, sdm_stream_t stream);
+
+/* Gradients of L = sum <dy, y> + <dstate, S_T> (dstate: [B, H, d_k, d_v] float32, or NULL) for the
+ * call of sdm_gdn_forward that started from state0 [B, H, d_k, d_v] float32 (not changed).  The
+ * forward is recomputed; nothing of it has to be kept.  dq, dk, dv, dalpha, dbeta: layout and dtype
+ * of what they are the gradients of, written (zero past the lengths; dq and dk summed over the value
+ * heads that share a key head); dstate0: [B, H, d_k, d_v] float32, or NULL.  Gates may be 0.  Same
+ * results on every call. */
+sdm_status sdm_gdn_backward(const sdm_gdn_shape* shape, const void* q, const void* k, const void* v,
+                            const void* alpha, const void* beta, const int32_t* lengths,
+                            const float* state0, const void* dy, const float* dstate, void* dq, void* dk,
+                            void* dv, void* dalpha, void* dbeta, float* dstate0, void* workspace,
+                            size_t workspace_bytes, sdm_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Linear layer on the tensor cores (bf16 storage, float32 accumulation), the projections before
+ * and after the recurrences:
+ *   z = x W^T + bias;  out = residual + act(z),   x: [M, K], W: [N, K], out: [M, N], row-major.
+ * ------------------------------------------------------------------------------------------ */
+enum { SDM_ACT_NONE = 0, SDM_ACT_RELU = 1, SDM_ACT_SILU = 2, SDM_ACT_GELU = 3 /* with erf */ };
+
+typedef struct {
+    int64_t M;                /* rows, at most 2^24 - 256 */
+    int32_t N, K;             /* multiples of 8 */
+    int32_t act;              /* SDM_ACT_* */
+} sdm_linear_shape;
+
+/* Bytes of workspace (0: none needed; 0 with sdm_last_error set for an invalid shape). */
+size_t sdm_linear_workspace_bytes(const sdm_linear_shape* shape);
+size_t sdm_linear_backward_workspace_bytes(const sdm_linear_shape* shape);
+
+/* bias: [N] float32 or NULL; residual: [M, N] bf16 or NULL (may be out itself, not overlap it
+ * otherwise); pre: NULL, or [M, N] bf16 that receives z rounded, for the backward.  16-byte aligned
+ * buffers; out and pre overlap nothing else. */
+sdm_status sdm_linear(const sdm_linear_shape* shape, const void* x, const void* W, const float* bias,
+                      const void* residual, void* out, void* pre, void* workspace, size_t workspace_bytes,
+                      sdm_stream_t stream);
+
+/* Gradients for dout [M, N] bf16, with dz = dout act'(pre) rounded to bf16 as an operand of
+ * dx = dz W [M, K] and dW = dz^T x [N, K] (bf16), and dbias = column sums of the unrounded dz
+ * [N] float32.  pre: what sdm_linear stored (may be NULL with SDM_ACT_NONE).  relu's slope at 0 is 0.  Any of dx, dW,
+ * dbias may be NULL (not computed).  The residual's gradient is dout.  With M = 0, dW and dbias are
+ * zero.  Same results on every call. */
+sdm_status sdm_linear_backward(const sdm_linear_shape* shape, const void* x, const void* W, const void* pre,
+                               const void* dout, void* dx, void* dW, float* dbias, void* workspace,
+                               size_t workspace_bytes, sdm_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

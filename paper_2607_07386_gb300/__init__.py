@@ -12,4 +12,6 @@ from ._binding import (  # noqa: F401
     materialize, touched_words, access_stats, access_stats_workspace_bytes, gates, norm_gate, gates_tensor_cores, head_mix,
     undo_log_bytes, recur_undo, recur_backward, undo_code_bytes, undo_quantize, recur_backward_q, recur_chunkwise, recur_plan, test_recur_wait_timeout,
     RECUR_PLAN_FIELDS, test_scores,
+    GdnShape, LinearShape, gdn_workspace_bytes, gdn_backward_workspace_bytes, gdn_forward, gdn_step, gdn_backward,
+    linear_workspace_bytes, linear_backward_workspace_bytes, linear, linear_backward,
 )

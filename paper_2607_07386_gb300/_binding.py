@@ -39,6 +39,37 @@ class SdmShape(ctypes.Structure):
         return SdmShape(**vals)
 
 
+LAYOUTS = {"head_major": 0, "token_major": 1}
+ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+
+
+class GdnShape(ctypes.Structure):
+    """sdm_gdn_shape: the dense gated delta rule."""
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("H_k", ctypes.c_int32), ("T", ctypes.c_int32),
+                ("d_k", ctypes.c_int32), ("d_v", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+    @classmethod
+    def make(cls, B, H, T, d_k, d_v, H_k=None, dtype="bf16", layout="head_major", scale=1.0) -> "GdnShape":
+        dt = {"f32": DTYPE_F32, "bf16": DTYPE_BF16}[dtype] if isinstance(dtype, str) else int(dtype)
+        lo = LAYOUTS[layout] if isinstance(layout, str) else int(layout)
+        return cls(B, H, H if H_k is None else H_k, T, d_k, d_v, dt, lo, scale)
+
+    def replace(self, **kw) -> "GdnShape":
+        vals = {f: getattr(self, f) for f, _ in self._fields_}
+        vals.update(kw)
+        return GdnShape(**vals)
+
+
+class LinearShape(ctypes.Structure):
+    """sdm_linear_shape: x [M, K], W [N, K], out [M, N]."""
+    _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int32), ("K", ctypes.c_int32), ("act", ctypes.c_int32)]
+
+    @classmethod
+    def make(cls, M, N, K, act="none") -> "LinearShape":
+        return cls(M, N, K, ACTS[act] if isinstance(act, str) else int(act))
+
+
 _lib = None
 _lock = threading.Lock()
 _VP, _SZ, _I32P = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p
@@ -118,6 +149,18 @@ def lib():
             L.sdm_test_recur_wait_timeout.argtypes = [_SHP, _I32P, _VP, _I32P, _VP, _VP, _VP, _VP, _VP, _VP, _VP,
                                                       _SZ, ctypes.c_int64, _VP]
             L.sdm_test_recur_wait_timeout.restype = ctypes.c_int
+            _GSP, _LSP = ctypes.POINTER(GdnShape), ctypes.POINTER(LinearShape)
+            for f, shp in (("sdm_gdn_workspace_bytes", _GSP), ("sdm_gdn_backward_workspace_bytes", _GSP),
+                           ("sdm_linear_workspace_bytes", _LSP), ("sdm_linear_backward_workspace_bytes", _LSP)):
+                getattr(L, f).restype = ctypes.c_size_t
+                getattr(L, f).argtypes = [shp]
+            L.sdm_gdn_forward.argtypes = [_GSP] + [_VP] * 9 + [_SZ, _VP]
+            L.sdm_gdn_step.argtypes = [_GSP] + [_VP] * 6 + [ctypes.c_int32, _VP, _VP, _VP]
+            L.sdm_gdn_backward.argtypes = [_GSP] + [_VP] * 16 + [_SZ, _VP]
+            L.sdm_linear.argtypes = [_LSP] + [_VP] * 7 + [_SZ, _VP]
+            L.sdm_linear_backward.argtypes = [_LSP] + [_VP] * 8 + [_SZ, _VP]
+            for f in ("sdm_gdn_forward", "sdm_gdn_step", "sdm_gdn_backward", "sdm_linear", "sdm_linear_backward"):
+                getattr(L, f).restype = ctypes.c_int
             for f in ("sdm_init_memory", "sdm_forward", "sdm_decode_step", "sdm_address", "sdm_recur",
                       "sdm_device_status"):
                 getattr(L, f).restype = ctypes.c_int
@@ -395,3 +438,69 @@ def device_stats(stream=None) -> dict:
     arr = (ctypes.c_uint32 * n)()
     _check(lib().sdm_device_stats(arr, n, _stream(stream)))
     return {name: int(arr[i]) for i, name in enumerate(STAT_NAMES)}
+
+
+def _size(fn, shape) -> int:
+    """A workspace size that may be 0: an invalid shape is told by the library's message."""
+    n = fn(ctypes.byref(shape))
+    if n == 0 and last_error():
+        raise SdmError(1, last_error())
+    return n
+
+
+def gdn_workspace_bytes(shape: GdnShape) -> int:
+    return _size(lib().sdm_gdn_workspace_bytes, shape)
+
+
+def gdn_backward_workspace_bytes(shape: GdnShape) -> int:
+    return _size(lib().sdm_gdn_backward_workspace_bytes, shape)
+
+
+def gdn_forward(shape: GdnShape, q, k, v, alpha, beta, state, y, workspace=None, lengths=None, stream=None,
+                workspace_nbytes=None):
+    """sdm_gdn_forward: the dense gated delta rule over T tokens; state (float32) is updated in place."""
+    nb = workspace_nbytes if workspace_nbytes is not None else (_nbytes(workspace) or 0)
+    _check(lib().sdm_gdn_forward(ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(alpha), _ptr(beta), _ptr(lengths),
+                                 _ptr(state), _ptr(y), _ptr(workspace), nb, _stream(stream)))
+
+
+def gdn_step(shape: GdnShape, q, k, v, alpha, beta, state, y, slots=None, n_slots=None, stream=None):
+    """sdm_gdn_step: one token of B sequences on a cache of states [n_slots, H, d_k, d_v] (n_slots: by default
+    the rows of `state`), slots: the row of each sequence (a negative one skips it)."""
+    n = n_slots if n_slots is not None else (state.shape[0] if hasattr(state, "shape") else shape.B)
+    _check(lib().sdm_gdn_step(ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(alpha), _ptr(beta), _ptr(slots),
+                              int(n), _ptr(state), _ptr(y), _stream(stream)))
+
+
+def gdn_backward(shape: GdnShape, q, k, v, alpha, beta, state0, dy, dstate, dq, dk, dv, dalpha, dbeta, dstate0,
+                 workspace, lengths=None, stream=None, workspace_nbytes=None):
+    """sdm_gdn_backward: gradients of the call of gdn_forward that started from state0 (dstate and dstate0,
+    the gradients of the last and the first state, may be None)."""
+    nb = workspace_nbytes if workspace_nbytes is not None else (_nbytes(workspace) or 0)
+    _check(lib().sdm_gdn_backward(ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(alpha), _ptr(beta),
+                                  _ptr(lengths), _ptr(state0), _ptr(dy), _ptr(dstate), _ptr(dq), _ptr(dk), _ptr(dv),
+                                  _ptr(dalpha), _ptr(dbeta), _ptr(dstate0), _ptr(workspace), nb, _stream(stream)))
+
+
+def linear_workspace_bytes(shape: LinearShape) -> int:
+    return _size(lib().sdm_linear_workspace_bytes, shape)
+
+
+def linear_backward_workspace_bytes(shape: LinearShape) -> int:
+    return _size(lib().sdm_linear_backward_workspace_bytes, shape)
+
+
+def linear(shape: LinearShape, x, W, out, bias=None, residual=None, pre=None, workspace=None, stream=None,
+           workspace_nbytes=None):
+    """sdm_linear: out = residual + act(x W^T + bias); pre receives x W^T + bias for the backward."""
+    nb = workspace_nbytes if workspace_nbytes is not None else (_nbytes(workspace) or 0)
+    _check(lib().sdm_linear(ctypes.byref(shape), _ptr(x), _ptr(W), _ptr(bias), _ptr(residual), _ptr(out), _ptr(pre),
+                            _ptr(workspace), nb, _stream(stream)))
+
+
+def linear_backward(shape: LinearShape, x, W, pre, dout, dx, dW, dbias, workspace=None, stream=None,
+                    workspace_nbytes=None):
+    """sdm_linear_backward: dx, dW (bf16) and dbias (float32) for dout; each of the three may be None."""
+    nb = workspace_nbytes if workspace_nbytes is not None else (_nbytes(workspace) or 0)
+    _check(lib().sdm_linear_backward(ctypes.byref(shape), _ptr(x), _ptr(W), _ptr(pre), _ptr(dout), _ptr(dx), _ptr(dW),
+                                     _ptr(dbias), _ptr(workspace), nb, _stream(stream)))

@@ -1,0 +1,98 @@
+// Gated delta rule (dense state) and linear layer: what the C ABI hands to the kernels.
+#pragma once
+#include "sdm_internal.h"
+
+namespace sdm {
+
+// Tokens per chunk of the saved states: the fp32 kernels and the tensor-core kernels.
+constexpr int GDN_C32 = 32;
+constexpr int GDN_C64 = 64;
+
+struct GdnArgs {
+    const void* q; const void* k;         // [B, Hk, T, dk] or [B, T, Hk, dk]
+    const void* v;                        // [B, H, T, dv]  or [B, T, H, dv]
+    const void* alpha; const void* beta;  // [B, H, T]
+    const int32_t* lengths;               // [B] or nullptr (every sequence has T tokens)
+    int B, H, Hk, T, dk, dv;
+    int token_major;
+    float scale;
+    int* err;                             // device status word
+};
+
+// Element offset of token 0 and the distance between tokens of one (sequence, head).
+__host__ __device__ __forceinline__ int64_t gdn_base(int token_major, int b, int h, int heads, int T, int d) {
+    return token_major ? (static_cast<int64_t>(b) * T * heads + h) * d
+                       : (static_cast<int64_t>(b) * heads + h) * T * static_cast<int64_t>(d);
+}
+__host__ __device__ __forceinline__ int64_t gdn_stride(int token_major, int heads, int d) {
+    return token_major ? static_cast<int64_t>(heads) * d : d;
+}
+
+// Tokens of sequence b; a length outside [0, T] is clamped and recorded in the status word.
+__device__ __forceinline__ int gdn_length(const GdnArgs& a, int b) {
+    if (a.lengths == nullptr) return a.T;
+    const int n = __ldg(a.lengths + b);
+    if (n < 0 || n > a.T) {
+        if (threadIdx.x == 0) flag_error(a.err, ERR_BAD_INDEX);
+        return n < 0 ? 0 : a.T;
+    }
+    return n;
+}
+
+// ---- token recurrence (k_gdn_recur.cu) ----
+struct GdnRecur {
+    GdnArgs a;
+    float* state;             // forward: [slots, H, dk, dv], updated in place (nullptr: see state_in)
+    const float* state_in;    // forward with saved states: the initial state (left as it is);
+                              // reverse: dL/dS_T or nullptr (zero)
+    const int32_t* slots;     // [B] row of `state` of each sequence, or nullptr (row b)
+    int n_slots;
+    void* y;                  // forward: y; reverse: dv
+    const void* dy;           // reverse
+    float* marks;             // saved states [B, H, ceil(T / 32), dk, dv]: forward, at the start of every
+                              // chunk; reverse, the gradient of the state at the end of every chunk
+    float* rows;              // forward with saved states: e [B, H, T, dv]; reverse: d
+    float* state_out;         // reverse: dL/dS_0 or nullptr
+};
+// mode 0: forward; 1: forward with saved states and e, no y; 2: reverse.
+cudaError_t launch_gdn_recur(int dtype, int mode, const GdnRecur& r, cudaStream_t stream);
+
+// ---- gradients of q, k and the gates from the saved states (k_gdn_grads.cu), chunks of 32 ----
+struct GdnGrads {
+    GdnArgs a;
+    const void* dy;
+    const float* S; const float* dE;      // [B, H, nc, dk, dv]
+    const float* e; const float* d;       // [B, H, T, dv]
+    void* dq; void* dk; void* dalpha; void* dbeta;
+};
+cudaError_t launch_gdn_grads(int dtype, const GdnGrads& g, cudaStream_t stream);
+
+// ---- linear layer (k_linear.cu): bf16 matrices, row-major ----
+// out [M, N] = residual + act(x W^T + bias); pre (optional) receives x W^T + bias.
+struct LinearOut {
+    const float* bias;                    // [N] or nullptr
+    const void* residual;                 // [M, N] bf16 or nullptr
+    void* pre;                            // [M, N] bf16 or nullptr
+    void* out;                            // [M, N] bf16
+    int act;
+};
+// How a product is cut: 128 x bn tiles, `splits` ranges of the contraction (each a multiple of 64)
+// whose fp32 shares are joined by a second kernel.
+struct LinearPlan {
+    int bn, splits;
+};
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K);
+size_t linear_split_bytes(int64_t M, int64_t N, int64_t K);
+bool linear_skinny(int64_t M);
+// D[m, n] = sum_k A(m, k) B(n, k).  A is [M, K] (a_mn = false) or [K, M] in memory; B alike.
+cudaError_t launch_linear(const void* A, bool a_mn, const void* B, bool b_mn, int64_t M, int64_t N, int64_t K,
+                          const LinearOut& o, float* split_ws, int* err, cudaStream_t stream);
+cudaError_t launch_linear_skinny(const void* x, const void* W, int M, int N, int K, const LinearOut& o,
+                                 cudaStream_t stream);
+// dp = dout act'(pre) (dp == nullptr: not written) and dbias = column sums of it (nullptr: not
+// taken); part: linear_dact_bytes(M, N) of scratch for the column sums.
+size_t linear_dact_bytes(int64_t M, int64_t N);
+cudaError_t launch_linear_dact(const void* dout, const void* pre, int act, int64_t M, int N, void* dp, float* dbias,
+                               float* part, cudaStream_t stream);
+
+}  // namespace sdm

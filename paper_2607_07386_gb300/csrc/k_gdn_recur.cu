@@ -1,0 +1,332 @@
+// Gated delta rule, token by token, in fp32 (every dtype, d_k <= 256, any d_v).
+//
+//   forward, per token:   S~ = alpha S;  e = v - S~^T k;  S = S~ + beta k e^T;  y = scale S^T q
+//   reverse, per token:   D += scale q dy^T;  d = D^T k;  dv = beta d;  D = alpha (D - beta k d^T)
+//
+// Columns of the state never meet, so a warp owns 16 of them for the whole call and keeps its
+// [d_k, 16] slice in registers: lane = 4 g + c holds columns 4c..4c+3 of the rows whose quad index
+// is g modulo 8.  A quad of rows of k (or q) is one 8- or 16-byte shared-memory read that the four
+// lanes of a group share, and the eight groups read neighbouring quads, so the reads are free of
+// bank conflicts; rows are paired in the packed fp32x2 units.  The dot products over d_k end in
+// three butterfly steps over the groups.  Blocks of TB tokens of q, k and v come through a
+// double-buffered cp.async ring shared by the warps of the CTA.
+//
+// One token (T = 1) is bound by the state's two trips through HBM: every thread has its whole
+// slice of loads in flight at once.  Long calls are bound by the instructions of the chain.
+#include "gdn_internal.h"
+
+namespace sdm {
+
+namespace {
+
+constexpr int TB = 16;          // tokens per staged block; divides the chunk lengths
+constexpr int MAX_WARPS = 8;
+
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<unsigned long long&>(d))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)),
+          "l"(reinterpret_cast<unsigned long long&>(c)));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<unsigned long long&>(d))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+    return d;
+}
+
+__device__ __forceinline__ void cp16(void* dst, const void* src, bool on) {
+    const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(dst));
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(s), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
+
+// Four consecutive storage elements of shared memory as two fp32 pairs.
+template <class D> __device__ __forceinline__ void quad(const typename D::T* p, float2& a, float2& b);
+template <> __device__ __forceinline__ void quad<F32>(const float* p, float2& a, float2& b) {
+    const float4 f = *reinterpret_cast<const float4*>(p);
+    a = make_float2(f.x, f.y);
+    b = make_float2(f.z, f.w);
+}
+template <> __device__ __forceinline__ void quad<BF16>(const __nv_bfloat16* p, float2& a, float2& b) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    a = make_float2(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u));
+    b = make_float2(__uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
+}
+template <class D> __device__ __forceinline__ void put4(typename D::T* p, const float (&f)[4]);
+template <> __device__ __forceinline__ void put4<F32>(float* p, const float (&f)[4]) {
+    *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+}
+template <> __device__ __forceinline__ void put4<BF16>(__nv_bfloat16* p, const float (&f)[4]) {
+    __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
+}
+
+// Sum of four columns over the eight row groups, in every lane.
+__device__ __forceinline__ void sum_groups(float (&f)[4]) {
+#pragma unroll
+    for (int m = 4; m < 32; m <<= 1) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) f[c] += __shfl_xor_sync(0xffffffffu, f[c], m);
+    }
+}
+
+template <class D, int Q>
+struct Smem {
+    typename D::T k[2][TB][32 * Q];
+    typename D::T q[2][TB][32 * Q];
+    typename D::T v[2][TB][16 * MAX_WARPS];     // v, or dy in reverse
+    float a[2][TB], b[2][TB];
+};
+
+// MODE 0: forward; 1: forward with saved states; 2: reverse.  Grid (column blocks, H, B).
+template <class D, int Q, int MODE>
+__global__ void __launch_bounds__(32 * MAX_WARPS) k_gdn_recur(const GdnRecur r) {
+    using T = typename D::T;
+    extern __shared__ __align__(16) unsigned char raw[];
+    Smem<D, Q>& sm = *reinterpret_cast<Smem<D, Q>*>(raw);
+    const GdnArgs& a = r.a;
+    const int b = blockIdx.z, h = blockIdx.y, hk = h / (a.H / a.Hk);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c4 = (lane & 3) * 4;
+    const int cols = static_cast<int>(blockDim.x >> 5) * 16;     // columns of this CTA
+    const int col0 = blockIdx.x * cols, col = col0 + warp * 16 + c4;
+    const bool live = col < a.dv;                                // d_v is a multiple of 4
+    const int len = gdn_length(a, b);
+    const int64_t chain = static_cast<int64_t>(b) * a.H + h;
+    const int64_t vb = gdn_base(a.token_major, b, h, a.H, a.T, a.dv), vs = gdn_stride(a.token_major, a.H, a.dv);
+    const int64_t kb = gdn_base(a.token_major, b, hk, a.Hk, a.T, a.dk), ks = gdn_stride(a.token_major, a.Hk, a.dk);
+    T* y = static_cast<T*>(r.y);
+
+    // where this chain's state lives
+    int64_t row = b;
+    bool skip = false;
+    if (MODE == 0 && r.slots != nullptr) {
+        row = __ldg(r.slots + b);
+        skip = row < 0 || row >= r.n_slots;
+        if (row >= r.n_slots && threadIdx.x == 0) flag_error(a.err, ERR_BAD_INDEX);
+    }
+    const int64_t per = static_cast<int64_t>(a.dk) * a.dv;
+    const int64_t soff = (row * a.H + h) * per;
+
+    const int n = skip ? 0 : len;
+    if (MODE != 1 && live && g == 0) {                            // tokens past the length
+        const float z[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int t = n; t < a.T; ++t) put4<D>(y + vb + t * vs + col, z);
+    }
+    if (skip) return;
+
+    float2 S[2 * Q][4];      // [row pair][column]: rows 4 (8 i + g) + 2 p, + 1 for pair 2 i + p
+    {
+        const float* src = MODE == 0 ? r.state + soff : (r.state_in ? r.state_in + chain * per : nullptr);
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            float4 f[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int rw = 4 * (8 * i + g) + j;
+                f[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (src != nullptr && live && rw < a.dk)
+                    f[j] = __ldcs(reinterpret_cast<const float4*>(src + static_cast<int64_t>(rw) * a.dv + col));
+            }
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                S[2 * i + p][0] = make_float2(f[2 * p].x, f[2 * p + 1].x);
+                S[2 * i + p][1] = make_float2(f[2 * p].y, f[2 * p + 1].y);
+                S[2 * i + p][2] = make_float2(f[2 * p].z, f[2 * p + 1].z);
+                S[2 * i + p][3] = make_float2(f[2 * p].w, f[2 * p + 1].w);
+            }
+        }
+    }
+    auto save = [&](float* dst) {
+        if (!live) return;
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int rw = 4 * (8 * i + g) + j, p = 2 * i + (j >> 1);
+                if (rw < a.dk) {
+                    const bool o = j & 1;
+                    __stcs(reinterpret_cast<float4*>(dst + static_cast<int64_t>(rw) * a.dv + col),
+                           make_float4(o ? S[p][0].y : S[p][0].x, o ? S[p][1].y : S[p][1].x,
+                                       o ? S[p][2].y : S[p][2].x, o ? S[p][3].y : S[p][3].x));
+                }
+            }
+        }
+    };
+
+    const int nblk = (n + TB - 1) / TB;
+    const T* kp = static_cast<const T*>(a.k) + kb;
+    const T* qp = static_cast<const T*>(a.q) + kb;
+    const T* vp = static_cast<const T*>(MODE == 2 ? r.dy : a.v) + vb;
+    auto stage = [&](int blk, int buf) {
+        const int t0 = blk * TB;
+        constexpr int KV = 32 * Q / D::E;                        // 16-byte pieces of a key row
+        for (int i = threadIdx.x; i < TB * KV; i += blockDim.x) {
+            const int t = i / KV, x = (i % KV) * D::E;
+            const bool on = t0 + t < n && x < a.dk;              // d_k is a multiple of a piece
+            const int64_t o = on ? (t0 + t) * ks + x : 0;
+            cp16(&sm.k[buf][t][x], kp + o, on);
+            if (MODE != 1) cp16(&sm.q[buf][t][x], qp + o, on);
+        }
+        const int VV = cols / D::E;
+        for (int i = threadIdx.x; i < TB * VV; i += blockDim.x) {
+            const int t = i / VV, x = (i % VV) * D::E;
+            const bool on = t0 + t < n && col0 + x < a.dv;
+            cp16(&sm.v[buf][t][x], vp + (on ? (t0 + t) * vs + col0 + x : 0), on);
+        }
+        cp_commit();
+        if (threadIdx.x < TB) {
+            const int t = t0 + threadIdx.x;
+            sm.a[buf][threadIdx.x] = t < n ? load_elem<D>(a.alpha, chain * a.T + t) : 1.f;
+            sm.b[buf][threadIdx.x] = t < n ? load_elem<D>(a.beta, chain * a.T + t) : 0.f;
+        }
+    };
+    const int nc = (a.T + GDN_C32 - 1) / GDN_C32;
+    auto block_of = [&](int i) { return MODE == 2 ? nblk - 1 - i : i; };
+    if (nblk > 0) stage(block_of(0), 0);
+    for (int i = 0; i < nblk; ++i) {
+        const int buf = i & 1, blk = block_of(i), t0 = blk * TB;
+        cp_wait<0>();
+        __syncthreads();                                         // block i is in; block i - 1 is done with
+        if (i + 1 < nblk) stage(block_of(i + 1), buf ^ 1);
+        const int cnt = n - t0 < TB ? n - t0 : TB;
+        if (MODE == 1 && t0 % GDN_C32 == 0) save(r.marks + (chain * nc + t0 / GDN_C32) * per);
+        if (MODE == 2 && (t0 + cnt == n || (t0 + TB) % GDN_C32 == 0))
+            save(r.marks + (chain * nc + t0 / GDN_C32) * per);
+#pragma unroll 1
+        for (int u = 0; u < cnt; ++u) {
+            const int j = MODE == 2 ? cnt - 1 - u : u, t = t0 + j;
+            const float al = sm.a[buf][j], be = sm.b[buf][j];
+            float2 va, vb2;
+            quad<D>(&sm.v[buf][j][warp * 16 + c4], va, vb2);
+            const float x[4] = {va.x, va.y, vb2.x, vb2.y};
+            float2 k2[2 * Q];
+#pragma unroll
+            for (int p = 0; p < Q; ++p) quad<D>(&sm.k[buf][j][4 * (8 * p + g)], k2[2 * p], k2[2 * p + 1]);
+            float2 acc[4];
+            float s[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) acc[c] = make_float2(0.f, 0.f);
+            if (MODE == 2) {
+                float2 xs[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) xs[c] = make_float2(a.scale * x[c], a.scale * x[c]);
+#pragma unroll
+                for (int p = 0; p < Q; ++p) {
+                    float2 q2[2];
+                    quad<D>(&sm.q[buf][j][4 * (8 * p + g)], q2[0], q2[1]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        S[2 * p][c] = fma2(q2[0], xs[c], S[2 * p][c]);
+                        S[2 * p + 1][c] = fma2(q2[1], xs[c], S[2 * p + 1][c]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < 2 * Q; ++p) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[c] = fma2(k2[p], S[p][c], acc[c]);
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[c] = acc[c].x + acc[c].y;
+            sum_groups(s);
+            const float2 al2 = make_float2(al, al);
+            if (MODE == 2) {
+                float o[4];
+                float2 w[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    o[c] = be * s[c];
+                    w[c] = make_float2(-al * o[c], -al * o[c]);
+                }
+#pragma unroll
+                for (int p = 0; p < 2 * Q; ++p) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) S[p][c] = fma2(k2[p], w[c], mul2(al2, S[p][c]));
+                }
+                if (live && g == 0) {
+                    put4<D>(y + vb + t * vs + col, o);
+                    put4<F32>(r.rows + (chain * a.T + t) * a.dv + col, s);
+                }
+            } else {
+                float2 w[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    s[c] = x[c] - al * s[c];                     // e
+                    w[c] = make_float2(be * s[c], be * s[c]);
+                }
+                if (MODE == 1 && live && g == 0) put4<F32>(r.rows + (chain * a.T + t) * a.dv + col, s);
+#pragma unroll
+                for (int p = 0; p < 2 * Q; ++p) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) S[p][c] = fma2(k2[p], w[c], mul2(al2, S[p][c]));
+                }
+                if (MODE == 0) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[c] = make_float2(0.f, 0.f);
+#pragma unroll
+                    for (int p = 0; p < Q; ++p) {
+                        float2 q2[2];
+                        quad<D>(&sm.q[buf][j][4 * (8 * p + g)], q2[0], q2[1]);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            acc[c] = fma2(q2[0], S[2 * p][c], acc[c]);
+                            acc[c] = fma2(q2[1], S[2 * p + 1][c], acc[c]);
+                        }
+                    }
+                    float o[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) o[c] = acc[c].x + acc[c].y;
+                    sum_groups(o);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) o[c] *= a.scale;
+                    if (live && g == 0) put4<D>(y + vb + t * vs + col, o);
+                }
+            }
+        }
+    }
+    if (MODE == 0 && n > 0) save(r.state + soff);
+    if (MODE == 2 && r.state_out != nullptr) save(r.state_out + chain * per);
+}
+
+template <class D, int Q>
+cudaError_t launch_mode(int mode, const GdnRecur& r, dim3 grid, int threads, cudaStream_t stream) {
+    const size_t smem = sizeof(Smem<D, Q>);
+    auto go = [&](auto kern) {
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+        if (e != cudaSuccess) return e;
+        kern<<<grid, threads, smem, stream>>>(r);
+        return cudaGetLastError();
+    };
+    if (mode == 0) return go(k_gdn_recur<D, Q, 0>);
+    if (mode == 1) return go(k_gdn_recur<D, Q, 1>);
+    return go(k_gdn_recur<D, Q, 2>);
+}
+
+template <class D>
+cudaError_t launch_rows(int mode, const GdnRecur& r, dim3 grid, int threads, cudaStream_t stream) {
+    if (r.a.dk <= 32) return launch_mode<D, 1>(mode, r, grid, threads, stream);
+    if (r.a.dk <= 64) return launch_mode<D, 2>(mode, r, grid, threads, stream);
+    if (r.a.dk <= 128) return launch_mode<D, 4>(mode, r, grid, threads, stream);
+    return launch_mode<D, 8>(mode, r, grid, threads, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_gdn_recur(int dtype, int mode, const GdnRecur& r, cudaStream_t stream) {
+    const GdnArgs& a = r.a;
+    // The warps of a CTA share the staged keys; few chains are spread over more, smaller CTAs so
+    // that every SM has one.
+    const int warps = (a.dv + 15) / 16;
+    int per = warps < MAX_WARPS ? warps : MAX_WARPS;
+    while (per > 1 && static_cast<int64_t>(a.B) * a.H * ((warps + per - 1) / per) < 152) per = (per + 1) / 2;
+    const dim3 grid((warps + per - 1) / per, a.H, a.B);
+    return dtype == SDM_F32 ? launch_rows<F32>(mode, r, grid, 32 * per, stream)
+                            : launch_rows<BF16>(mode, r, grid, 32 * per, stream);
+}
+
+}  // namespace sdm

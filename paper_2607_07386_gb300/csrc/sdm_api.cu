@@ -902,6 +902,8 @@ sdm_status api_error(sdm_status st, const char* msg) { return fail(st, "%s", msg
 
 sdm_status api_ok() { return ok(); }
 
+sdm_status api_status_word(int** out) { return status_word(out); }
+
 // The argument checks of sdm_recur without its workspace; fills `r` (including the status
 // word) and sets *empty when B H T == 0 (nothing to launch).
 sdm_status recur_args(const char* who, const sdm_shape* s, const int32_t* idx_w, const float* w_w,

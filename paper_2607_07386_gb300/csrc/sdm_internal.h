@@ -162,6 +162,7 @@ cudaError_t launch_materialize(const void* M0, const uint32_t* touched, void* me
 // in other translation units (sdm_api.cu).
 sdm_status api_error(sdm_status st, const char* msg);
 sdm_status api_ok();
+sdm_status api_status_word(int** out);     // device status word of the current device
 sdm_status recur_args(const char* who, const sdm_shape* s, const int32_t* idx_w, const float* w_w,
                       const int32_t* idx_r, const float* w_r, const void* v, const void* alpha, const void* beta,
                       void* mem, void* y, RecArgs* r, bool* empty);
