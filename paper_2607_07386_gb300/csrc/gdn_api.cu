@@ -85,6 +85,8 @@ sdm_status gdn_check(const sdm_gdn_shape* s) {
     if (s->d_k < 1 || s->d_v < 1) return fail(SDM_ERR_INVALID_ARG, "d_k and d_v must be >= 1 (got %d, %d)", s->d_k, s->d_v);
     if (s->d_k > 256) return fail(SDM_ERR_UNSUPPORTED, "d_k > 256 is not supported (d_k=%d)", s->d_k);
     if (s->d_v > (1 << 20)) return fail(SDM_ERR_UNSUPPORTED, "d_v too large (%d)", s->d_v);
+    if (static_cast<int64_t>(s->B) * s->H * ((static_cast<int64_t>(s->T) + 63) / 64) > INT_MAX / 256)
+        return fail(SDM_ERR_UNSUPPORTED, "B * H * T / 64 must be at most 2^23 (got %d, %d, %d)", s->B, s->H, s->T);
     const size_t es = esize(s->dtype);
     if (s->d_k * es % 16 != 0 || s->d_v * es % 16 != 0)
         return fail(SDM_ERR_UNSUPPORTED, "d_k and d_v times the element size must be multiples of 16 bytes (d_k=%d, d_v=%d)", s->d_k, s->d_v);
@@ -110,6 +112,19 @@ sdm::GdnArgs gdn_args(const sdm_gdn_shape* s, const void* q, const void* k, cons
     a.scale = s->scale;
     a.err = err;
     return a;
+}
+
+// Factors of the chunked form.
+struct FwdLayout {
+    size_t mat, gates, total;
+};
+FwdLayout fwd_layout(const sdm_gdn_shape* s) {
+    FwdLayout L{};
+    if (!sdm::gdn_chunk_supported(s->dtype, s->d_k, s->T)) return L;
+    const int64_t chunks = static_cast<int64_t>(s->B) * s->H * ((s->T + sdm::GDN_C64 - 1) / sdm::GDN_C64);
+    L.gates = align256(sdm::gdn_factor_mat_bytes(chunks));
+    L.total = L.gates + align256(sdm::gdn_factor_gate_bytes(chunks));
+    return L;
 }
 
 // Saved states and rows of the fp32 backward.
@@ -166,7 +181,7 @@ extern "C" {
 size_t sdm_gdn_workspace_bytes(const sdm_gdn_shape* s) {
     if (gdn_check(s) != SDM_OK) return 0;
     sdm::api_ok();
-    return 0;
+    return fwd_layout(s).total;
 }
 
 size_t sdm_gdn_backward_workspace_bytes(const sdm_gdn_shape* s) {
@@ -181,7 +196,8 @@ sdm_status sdm_gdn_forward(const sdm_gdn_shape* s, const void* q, const void* k,
     SDM_TRY(gdn_check(s));
     const GdnSizes z = gdn_sizes(s);
     if (static_cast<size_t>(s->B) * s->H * s->T == 0) return sdm::api_ok();
-    const size_t need = sdm_gdn_workspace_bytes(s);
+    const FwdLayout L = fwd_layout(s);
+    const size_t need = L.total;
     const Buf bufs[] = {{"q", q, z.qk, 16, false, false}, {"k", k, z.qk, 16, false, false}, {"v", v, z.v, 16, false, false},
                         {"alpha", alpha, z.gate, z.es, false, false}, {"beta", beta, z.gate, z.es, false, false},
                         {"lengths", lengths, static_cast<size_t>(s->B) * 4, 4, true, false},
@@ -191,8 +207,17 @@ sdm_status sdm_gdn_forward(const sdm_gdn_shape* s, const void* q, const void* k,
     SDM_TRY(check_ws("sdm_gdn_forward", workspace, workspace_bytes, need));
     int* err = nullptr;
     SDM_TRY(sdm::api_status_word(&err));
+    const sdm::GdnArgs a = gdn_args(s, q, k, v, alpha, beta, lengths, err);
+    if (L.total > 0) {
+        cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+        char* ws = static_cast<char*>(workspace);
+        const sdm::GdnFactors f{ws + L.mat, reinterpret_cast<float*>(ws + L.gates)};
+        cudaError_t e = sdm::launch_gdn_factors(a, f, st);
+        if (e == cudaSuccess) e = sdm::launch_gdn_scan(sdm::GdnScan{a, state, y}, f, st);
+        return done(e, "sdm_gdn_forward");
+    }
     sdm::GdnRecur r{};
-    r.a = gdn_args(s, q, k, v, alpha, beta, lengths, err);
+    r.a = a;
     r.state = state;
     r.n_slots = s->B;
     r.y = y;

@@ -67,6 +67,24 @@ struct GdnGrads {
 };
 cudaError_t launch_gdn_grads(int dtype, const GdnGrads& g, cudaStream_t stream);
 
+// ---- chunked form on the tensor cores (k_gdn_chunk.cu): bf16, d_k <= 128, chunks of 64 ----
+// What the chunks' own products are, per (sequence, head, chunk): three bf16 matrices [64][64] (the
+// inverse's upper and lower parts, the masked read products) and three rows of 64 floats.
+struct GdnFactors {
+    void* mat;                // [B, H, nc, 3, 64, 64] bf16
+    float* gates;             // [B, H, nc, 3, 64]: prod_{l <= i} alpha_l, beta_i, prod_{l > i} alpha_l
+};
+size_t gdn_factor_mat_bytes(int64_t chunks);
+size_t gdn_factor_gate_bytes(int64_t chunks);
+bool gdn_chunk_supported(int dtype, int dk, int T);
+cudaError_t launch_gdn_factors(const GdnArgs& a, const GdnFactors& f, cudaStream_t stream);
+struct GdnScan {
+    GdnArgs a;
+    float* state;             // [B, H, dk, dv], updated in place
+    void* y;
+};
+cudaError_t launch_gdn_scan(const GdnScan& s, const GdnFactors& f, cudaStream_t stream);
+
 // ---- linear layer (k_linear.cu): bf16 matrices, row-major ----
 // out [M, N] = residual + act(x W^T + bias); pre (optional) receives x W^T + bias.
 struct LinearOut {

@@ -60,18 +60,6 @@ bool make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int 
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Operand stored with its rows contiguous ([k][row], 64-row atoms of 64 k x 128 bytes): groups of
-// 8 k 1024 bytes apart, the next 64 rows one atom (8192 bytes) further.
-__device__ __forceinline__ uint64_t mn_desc(uint32_t addr) {
-    uint64_t d = 0;
-    d |= static_cast<uint64_t>((addr >> 4) & 0x3FFF);
-    d |= static_cast<uint64_t>(8192 >> 4) << 16;
-    d |= static_cast<uint64_t>(1024 >> 4) << 32;
-    d |= static_cast<uint64_t>(1) << 46;
-    d |= static_cast<uint64_t>(2) << 61;
-    return d;
-}
-
 __device__ __forceinline__ float act_fwd(float z, int act) {
     if (act == SDM_ACT_RELU) return z > 0.f ? z : 0.f;
     if (act == SDM_ACT_SILU) return z / (1.f + __expf(-z));
@@ -182,7 +170,7 @@ __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtens
         // the copies in flight land before the CTA may end
         for (uint32_t j = it > S ? it - S : 0; j < it; ++j) mbar_wait(full + 8 * (j % S), (j / S) & 1);
     } else if (tid == 32) {                            // MMAs
-        const uint32_t idesc = mma_idesc(BN) | (AMN ? 1u << 15 : 0u) | (BMN ? 1u << 16 : 0u);
+        const uint32_t idesc = mma_idesc(BN) | (AMN ? MN_A : 0u) | (BMN ? MN_B : 0u);
         uint32_t it = 0, n = 0;
         for (int w = blockIdx.x; w < items && ok; w += gridDim.x, ++n) {
             const int sp = w % g.splits;
@@ -197,8 +185,8 @@ __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtens
                 const uint32_t a = ring + s * STAGE, b = a + BM * 128;
 #pragma unroll
                 for (int kk = 0; kk < BK / 16; ++kk)
-                    mma_bf16(acc, AMN ? mn_desc(a + kk * 2048) : sw128_desc(a + kk * 32),
-                             BMN ? mn_desc(b + kk * 2048) : sw128_desc(b + kk * 32), idesc, (kb != k0 || kk != 0) ? 1u : 0u);
+                    mma_bf16(acc, AMN ? sw128_mn_desc(a + kk * 2048, 8192) : sw128_desc(a + kk * 32),
+                             BMN ? sw128_mn_desc(b + kk * 2048, 8192) : sw128_desc(b + kk * 32), idesc, (kb != k0 || kk != 0) ? 1u : 0u);
                 mma_commit(empty + 8 * s);
             }
             if (ok) mma_commit(afull + 8 * (n & 1));
