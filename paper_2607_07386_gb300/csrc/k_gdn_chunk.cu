@@ -9,15 +9,14 @@
 // never quotients or exponentials of sums, so a gate of zero is exact.
 //
 // Precision: the state and every sum are fp32.  k and q are exact operands.  What the state depends on
-// and is not a bf16 number (S itself, Z, the two stages of w) enters the MMAs as bf16 parts, upper and
-// lower (16 significant bits, products of two lower parts left out, about 1e-6); y alone takes P rounded
-// to bf16 once, as y is.
+// and is not a bf16 number enters the MMAs as bf16 parts: S, Z - I and beta (v - g K S) as two (16
+// significant bits; products of two lower parts are left out), h w, whose rounding the state would
+// keep, as three.  Z's unit diagonal is taken in fp32.  y alone takes P rounded to bf16 once, as y is.
 #include "gdn_internal.h"
 #include "tc_common.cuh"
 
 #include <cuda.h>
 #include <cudaTypedefs.h>
-#include <type_traits>
 
 namespace sdm {
 
@@ -67,21 +66,48 @@ bool mat_map(CUtensorMap* m, const void* base, int64_t mats) {
 
 // ------------------------------------------------------------------------------------------
 // Factors of a chunk: one CTA of 128 threads.  One MMA chain gives [K; Q] K^T (128 x 64); thread r
-// takes row r of it (k_i.k_j for r < 64, q_i.k_j above) and multiplies it by G along the row.  The
-// inverse is a column per thread, eliminated left to right in registers: 2016 fused multiply-adds
-// whose factors are shared-memory broadcasts.
+// takes row r of it (k_i.k_j for r < 64, q_i.k_j above) and multiplies it by G along the row.
+//
+// Z is inverted in fp32 by blocks of 16: the diagonal blocks by a column per thread in registers, then
+// the block diagonals below in order, Z_ij = -Z_ii (sum_k L_ik Z_kj), each product spread over the CTA
+// (a thread takes four rows of a column; the left operand is a broadcast).  Eliminating whole columns of
+// 64 in registers is 2016 unrolled instructions, whose fetching took 11,600 of a CTA's 20,000 cycles.
 // ------------------------------------------------------------------------------------------
 constexpr int FT = 128;
 constexpr int LP = C + 4;
+constexpr int BL = 16, NB = C / BL;
 struct FactorSmem {
-    float Lt[C][LP];                          // L transposed; then the inverse's two bf16 parts
-    float al[C], be[C];
+    float L[C][LP];
+    float al[C], be[C], g[C], h[C];
     unsigned long long bar[2];
     uint32_t tmem;
     int dead;
 };
+// The K and Q tiles make room for Z and the products once the MMAs have read them.
+struct FactorLate {
+    float Z[C][LP];
+    float X[C][BL + 4];
+};
 template <int DK>
-constexpr size_t factor_smem() { return 1024 + 128 * 2 * DK + sizeof(FactorSmem); }
+struct FactorSize {
+    static constexpr size_t TILE = 128 * 2 * DK > sizeof(FactorLate) ? 128 * 2 * DK : (sizeof(FactorLate) + 15) / 16 * 16;
+    static constexpr size_t BYTES = 1024 + TILE + sizeof(FactorSmem);
+};
+
+// One block product: dst = sign * sum over nk blocks of A[ar + .., ac + 16 k + ..] B[br + 16 k + .., bc + ..];
+// 64 threads, thread u: column u % 16, rows 4 (u / 16) .. + 3.
+__device__ __forceinline__ void block_mul(const float* A, int lda, const float* B, int ldb, int nk, float (&acc)[4], int u) {
+    const int c = u & 15, r = (u >> 4) * 4;
+    acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+    for (int k = 0; k < nk * BL; k += 4) {
+        const float b0 = B[k * ldb + c], b1 = B[(k + 1) * ldb + c], b2 = B[(k + 2) * ldb + c], b3 = B[(k + 3) * ldb + c];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float4 x = *reinterpret_cast<const float4*>(A + (r + e) * lda + k);
+            acc[e] = fmaf(x.x, b0, fmaf(x.y, b1, fmaf(x.z, b2, fmaf(x.w, b3, acc[e]))));
+        }
+    }
+}
 
 template <int DK>
 __global__ void __launch_bounds__(FT) k_gdn_factors(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tq,
@@ -89,7 +115,8 @@ __global__ void __launch_bounds__(FT) k_gdn_factors(const __grid_constant__ CUte
     extern __shared__ unsigned char raw[];
     const uint32_t base = smem_u32(raw);
     const uint32_t tile = (base + 1023u) & ~1023u;        // per 64 values of d_k: 64 rows of K, 64 of Q
-    FactorSmem& sm = *reinterpret_cast<FactorSmem*>(raw + (tile - base) + 128 * 2 * DK);
+    FactorSmem& sm = *reinterpret_cast<FactorSmem*>(raw + (tile - base) + FactorSize<DK>::TILE);
+    FactorLate& lt = *reinterpret_cast<FactorLate*>(raw + (tile - base));
     const int tid = threadIdx.x, warp = tid >> 5;
     const int b = blockIdx.z, h = blockIdx.y, ch = blockIdx.x, t0 = ch * C;
     const int hk = h / (a.H / a.Hk);
@@ -105,37 +132,42 @@ __global__ void __launch_bounds__(FT) k_gdn_factors(const __grid_constant__ CUte
         mbar_init(done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         fence_async();
-    }
-    if (warp == 0) tmem_alloc(smem_u32(&sm.tmem), 64);
-    if (tid < C) {
-        sm.al[tid] = tid < n ? load_elem<BF16>(a.alpha, chain * a.T + t0 + tid) : 1.f;
-        sm.be[tid] = tid < n ? load_elem<BF16>(a.beta, chain * a.T + t0 + tid) : 0.f;
-    }
-    tc_before_sync();
-    __syncthreads();
-    tc_after_sync();
-    const uint32_t tmem = sm.tmem;
-    if (tid == 0) {
         mbar_expect_tx(bar, 128 * 2 * DK);
 #pragma unroll
         for (int x = 0; x < DK / 64; ++x) {
             tma_load_4d(tile + x * 16384, &tk, 64 * x, t0, hk, b, bar);
             tma_load_4d(tile + x * 16384 + 8192, &tq, 64 * x, t0, hk, b, bar);
         }
+    }
+    if (warp == 1) tmem_alloc(smem_u32(&sm.tmem), 64);
+    if (tid >= C) {
+        const int t = tid - C;
+        sm.al[t] = t < n ? load_elem<BF16>(a.alpha, chain * a.T + t0 + t) : 1.f;
+        sm.be[t] = t < n ? load_elem<BF16>(a.beta, chain * a.T + t0 + t) : 0.f;
+    }
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    const uint32_t tmem = sm.tmem;
+    if (warp == 0) {
         mbar_wait_or_dead(bar, 0, &sm.dead);
+        __syncwarp();
         tc_after_sync();
         const uint32_t idesc = mma_idesc(64);
+        const uint64_t d0 = sw128_desc(tile);
+        if (elect_one()) {
 #pragma unroll
-        for (int kk = 0; kk < DK / 16; ++kk) {
-            const uint32_t at = tile + (kk / 4) * 16384 + (kk % 4) * 32;
-            mma_bf16(tmem, sw128_desc(at), sw128_desc(at), idesc, kk != 0);
+            for (int kk = 0; kk < DK / 16; ++kk) {
+                const uint64_t at = d0 + (kk / 4) * 1024 + (kk % 4) * 2;
+                mma_bf16(tmem, at, at, idesc, kk != 0);
+            }
+            mma_commit(done);
         }
-        mma_commit(done);
+        __syncwarp();
     }
     // row i of the decay products, from the diagonal to the left: G_ii = 1, G_i,j-1 = G_ij alpha_j
     const int i = tid & 63;
     const bool isk = tid < C;
-    __syncwarp();
     mbar_wait_or_dead(done, 0, &sm.dead);
     __syncwarp();
     tc_after_sync();
@@ -154,14 +186,13 @@ __global__ void __launch_bounds__(FT) k_gdn_factors(const __grid_constant__ CUte
     for (int j = C - 1; j >= 0; --j) {
         const bool in = row_on && (isk ? j < i : j <= i);
         x[j] = in ? G * (isk ? be * x[j] : x[j]) : 0.f;
-        if (isk && i == C - 1) f.gates[cid * 3 * C + 2 * C + j] = G;          // h_j
+        if (tid == 2 * C - 1) sm.h[j] = G;                                    // row 63: prod_{l > j}
         if (j <= i) G *= sm.al[j];
     }
     if (isk) {
-        f.gates[cid * 3 * C + i] = G;                                         // g_i: all factors up to i
-        f.gates[cid * 3 * C + C + i] = be;
+        sm.g[i] = G;                                                          // all factors up to i
 #pragma unroll
-        for (int j = 0; j < C; ++j) sm.Lt[j][i] = x[j];
+        for (int j = 0; j < C; j += 4) *reinterpret_cast<float4*>(&sm.L[i][j]) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
     } else {
         uint4* dst = reinterpret_cast<uint4*>(static_cast<char*>(f.mat) + (cid * 3 + 2) * MAT + i * C * 2);
 #pragma unroll
@@ -173,47 +204,65 @@ __global__ void __launch_bounds__(FT) k_gdn_factors(const __grid_constant__ CUte
         }
     }
     __syncthreads();
-    if (isk) {
-        const int c = tid;
-#pragma unroll
-        for (int j = 0; j < C; ++j) x[j] = j == c ? 1.f : 0.f;
-        // columns 32.. start at row 32: what is above is zero
-        auto eliminate = [&](auto from, auto to) {
-#pragma unroll
-            for (int j = decltype(from)::value; j < decltype(to)::value; ++j) {
-#pragma unroll
-                for (int q = (j + 1) / 4; q < C / 4; ++q) {
-                    const float4 l = *reinterpret_cast<const float4*>(&sm.Lt[j][4 * q]);
-                    if (4 * q > j) x[4 * q] = fmaf(-l.x, x[j], x[4 * q]);
-                    if (4 * q + 1 > j) x[4 * q + 1] = fmaf(-l.y, x[j], x[4 * q + 1]);
-                    if (4 * q + 2 > j) x[4 * q + 2] = fmaf(-l.z, x[j], x[4 * q + 2]);
-                    x[4 * q + 3] = fmaf(-l.w, x[j], x[4 * q + 3]);
-                }
-            }
-        };
-        if (warp == 0) eliminate(std::integral_constant<int, 0>{}, std::integral_constant<int, 32>{});
-        eliminate(std::integral_constant<int, 32>{}, std::integral_constant<int, C - 1>{});
+    if (tid < C) {
+        f.gates[cid * 3 * C + tid] = sm.g[tid];
+        f.gates[cid * 3 * C + C + tid] = sm.be[tid];
+    } else {
+        f.gates[cid * 3 * C + C + tid] = sm.h[tid - C];
     }
-    __syncthreads();
-    uint32_t* z = reinterpret_cast<uint32_t*>(&sm.Lt[0][0]);                  // [64][65] words: upper | lower << 16
-    if (isk) {
+    if (isk) {                                                                // diagonal block tid / 16, column tid % 16
+        const int o = tid & ~15, c = tid & 15;
+        float z[BL];
 #pragma unroll
-        for (int j = 0; j < C; ++j) {
-            const __nv_bfloat16 hi = __float2bfloat16_rn(x[j]);
-            const __nv_bfloat16 lo = __float2bfloat16_rn(x[j] - __bfloat162float(hi));
-            z[j * (C + 1) + tid] = static_cast<uint32_t>(__bfloat16_as_ushort(hi)) | (static_cast<uint32_t>(__bfloat16_as_ushort(lo)) << 16);
+        for (int j = 0; j < BL; ++j) z[j] = j == c ? 1.f : 0.f;
+#pragma unroll
+        for (int j = 1; j < BL; ++j) {
+            float4 l[4];
+#pragma unroll
+            for (int q = 0; q < (j + 3) / 4; ++q) l[q] = *reinterpret_cast<const float4*>(&sm.L[o + j][o + 4 * q]);
+#pragma unroll
+            for (int k = 0; k < j; ++k) {
+                const float lk = (k & 3) == 0 ? l[k / 4].x : (k & 3) == 1 ? l[k / 4].y : (k & 3) == 2 ? l[k / 4].z : l[k / 4].w;
+                z[j] = fmaf(-lk, z[k], z[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < BL; ++j) lt.Z[o + j][o + c] = z[j];
+    } else {                                                                  // above the diagonal
+        for (int p = tid - C; p < C * C / 4; p += C) {
+            const int r = p / (C / 4), c = (p % (C / 4)) * 4;
+            if (c / BL > r / BL) *reinterpret_cast<float4*>(&lt.Z[r][c]) = make_float4(0.f, 0.f, 0.f, 0.f);
         }
     }
     __syncthreads();
-    for (int p = tid; p < C * C / 8; p += FT) {
-        const int r = p / (C / 8), c = (p % (C / 8)) * 8;
-        uint32_t w[8], hi[4], lo[4];
+    for (int d = 1; d < NB; ++d) {                                            // blocks (j + d, j)
+        for (int j = tid / 64; j < NB - d; j += 2) {
+            float acc[4];
+            block_mul(&sm.L[(j + d) * BL][j * BL], LP, &lt.Z[j * BL][j * BL], LP, d, acc, tid & 63);
+            const int c = tid & 15, r = ((tid & 63) >> 4) * 4;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = z[r * (C + 1) + c + e];
+            for (int e = 0; e < 4; ++e) lt.X[j * BL + r + e][c] = acc[e];
+        }
+        __syncthreads();
+        for (int j = tid / 64; j < NB - d; j += 2) {
+            float acc[4];
+            block_mul(&lt.Z[(j + d) * BL][(j + d) * BL], LP, &lt.X[j * BL][0], BL + 4, 1, acc, tid & 63);
+            const int c = tid & 15, r = ((tid & 63) >> 4) * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) lt.Z[(j + d) * BL + r + e][j * BL + c] = -acc[e];
+        }
+        __syncthreads();
+    }
+    for (int p = tid; p < C * C / 8; p += FT) {                               // Z - I as upper and lower parts
+        const int r = p / (C / 8), c = (p % (C / 8)) * 8;
+        float v[8];
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c + e == r ? 0.f : lt.Z[r][c + e];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            hi[e] = (w[2 * e] & 0xffffu) | (w[2 * e + 1] << 16);
-            lo[e] = (w[2 * e] >> 16) | (w[2 * e + 1] & 0xffff0000u);
+            hi[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
+            lo[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
         }
         char* dst = static_cast<char*>(f.mat) + cid * 3 * MAT + p * 16;
         *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
@@ -222,7 +271,7 @@ __global__ void __launch_bounds__(FT) k_gdn_factors(const __grid_constant__ CUte
     if (tid == 0 && sm.dead) flag_error(a.err, ERR_TIMEOUT);
     tc_before_sync();
     __syncthreads();
-    if (warp == 0) tmem_free(tmem, 64);
+    if (warp == 1) tmem_free(tmem, 64);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -232,21 +281,26 @@ __global__ void __launch_bounds__(FT) k_gdn_factors(const __grid_constant__ CUte
 // K S, along the tokens for the update).  Per chunk:
 //   1  U = S^T K^T, then S^T Q^T                      (MMA; the second runs under step 2)
 //   2  R = beta (v - g U)                             (registers, bf16 parts to TMEM)
-//   3  w = R Z^T                                      (MMA; g Q S is taken out meanwhile)
-//   4  w, h w                                         (registers, bf16 parts to TMEM)
+//   3  R (Z - I)^T                                    (MMA; g Q S is taken out meanwhile)
+//   4  w = R + .., h w                                (registers, bf16 parts to TMEM)
 //   5  h w K, then w P^T                              (MMA)
 //   6  S = g_63 S + ..                                (registers, bf16 parts to TMEM)
-// and the output of a chunk is added up and stored under step 1 of the next.  Two warps share a lane
-// quarter: in steps 2 and 4 each takes 32 tokens, in step 6 half of d_k.
+// and the output of a chunk is added up under step 1 of the next, in the place of its v, and stored by
+// TMA.  Warps 0-7 compute: two share a lane quarter; in steps 2 and 4 each takes 32 tokens, in step 6
+// half of d_k.  Warp 8 issues the MMAs, warp 9 the copies; warps 10 and 11 only complete the warpgroup
+// that gives its registers to the others.
 //
-// The chain of six stages is what bounds it: the tensor pipe is busy for about a third of a chunk.
+// The chain of six stages is what bounds it, then the tensor pipe (2432 cycles of MMAs per chunk at d_k =
+// 128).
 // ------------------------------------------------------------------------------------------
 constexpr int SW = 8;                          // compute warps
-constexpr int ST = 32 * SW;
-constexpr int NS = 2;                          // bf16 parts of a split operand
-// TMEM columns
-constexpr uint32_t X_COL = 0, Y_COL = 128, S_COL = 192, R_COL = S_COL + 64 * NS, W_COL = R_COL + 32 * NS, T_COLS = 512;
-static_assert(W_COL + 32 * NS <= T_COLS, "TMEM columns");
+constexpr int ST = 32 * (SW + 4);
+constexpr int SCAN_REGS = 232, IDLE_REGS = 40;   // after the split of the launch's 168 per thread
+constexpr int NS = 2;                          // bf16 parts of S, of R and of w as the factor of P
+constexpr int NH = 3;                          // bf16 parts of h w
+// TMEM columns: X: steps 1, 3, 5; Y: w P^T; S; R, then w.  h w lies where S is, which steps 2 to 6 do not read.
+constexpr uint32_t X_COL = 0, Y_COL = 128, S_COL = 192, R_COL = S_COL + 128, T_COLS = 512;
+static_assert(R_COL + 32 * NS <= T_COLS && 32 * NH <= 128 && 64 * NS <= 128, "TMEM columns");
 
 template <int DK>
 struct ScanTile {
@@ -255,44 +309,62 @@ struct ScanTile {
     static constexpr int STAGES = 3;
 };
 struct ScanCtl {
-    unsigned long long full[3], step[5];
+    unsigned long long full[3];               // a stage's tile is in
+    unsigned long long step[5];               // MMAs: U; Q S; R (Z - I); h w K; w P
+    unsigned long long go[4];                 // operands in TMEM: S; R; w; y in shared memory
     uint32_t tmem;
     int dead;
 };
 template <int DK>
 constexpr size_t scan_smem() { return 1024 + ScanTile<DK>::BYTES * ScanTile<DK>::STAGES + sizeof(ScanCtl); }
 
-// 32 values as bf16 parts, 16 packed columns each, `stride` columns apart.
+// 32 values as `parts` bf16 parts, 16 packed columns each, `stride` columns apart.
+template <int PARTS>
 __device__ __forceinline__ void put_parts(uint32_t taddr, uint32_t stride, float (&v)[32]) {
 #pragma unroll
-    for (int p = 0; p < NS; ++p) {
+    for (int p = 0; p < PARTS; ++p) {
         uint32_t u[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) u[j] = split2(v[2 * j], v[2 * j + 1], v[2 * j], v[2 * j + 1]);
         tmem_st16(taddr + p * stride, u);
     }
 }
+// A warp's share of an operand is in TMEM (or shared memory): tells the issuing warp.
+__device__ __forceinline__ void announce(uint32_t bar, int lane) {
+    tc_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+}
+__device__ __forceinline__ void await(uint32_t bar, uint32_t parity, volatile int* dead) {
+    mbar_wait_or_dead(bar, parity, dead);
+    __syncwarp();
+    tc_after_sync();
+}
+// Element (row, x) of a tile of 64-value, 128-byte rows, swizzled as TMA leaves it.
+__device__ __forceinline__ uint32_t sw128_at(int row, int x) { return row * 128 + ((x * 2) ^ ((row & 7) << 4)); }
 
 template <int DK>
 __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tq,
-                                                    const __grid_constant__ CUtensorMap tv, const __grid_constant__ CUtensorMap tm,
-                                                    const GdnScan r, const GdnFactors f, int nc) {
+                                                    const __grid_constant__ CUtensorMap tv, const __grid_constant__ CUtensorMap ty,
+                                                    const __grid_constant__ CUtensorMap tm, const GdnScan r, const GdnFactors f, int nc) {
     using L = ScanTile<DK>;
     extern __shared__ unsigned char raw[];
     const GdnArgs& a = r.a;
     const uint32_t base = smem_u32(raw);
     const uint32_t ring = (base + 1023u) & ~1023u;
-    ScanCtl& ctl = *reinterpret_cast<ScanCtl*>(raw + (ring - base) + L::BYTES * L::STAGES);
+    unsigned char* const ringp = raw + (ring - base);
+    ScanCtl& ctl = *reinterpret_cast<ScanCtl*>(ringp + L::BYTES * L::STAGES);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int b = blockIdx.z, h = blockIdx.y, col0 = blockIdx.x * 128, hk = h / (a.H / a.Hk);
     const int len = gdn_length(a, b);
     const int64_t chain = static_cast<int64_t>(b) * a.H + h;
     const int chunks = (len + C - 1) / C;
-    const uint32_t full = smem_u32(&ctl.full[0]), step = smem_u32(&ctl.step[0]);
+    const uint32_t full = smem_u32(&ctl.full[0]), step = smem_u32(&ctl.step[0]), go = smem_u32(&ctl.go[0]);
     if (tid == 0) {
         ctl.dead = 0;
         for (int s = 0; s < L::STAGES; ++s) mbar_init(full + 8 * s, 1);
         for (int s = 0; s < 5; ++s) mbar_init(step + 8 * s, 1);
+        for (int s = 0; s < 4; ++s) mbar_init(go + 8 * s, SW);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         fence_async();
     }
@@ -302,35 +374,102 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
     tc_after_sync();
     const uint32_t tmem = ctl.tmem;
     volatile int* dead = &ctl.dead;
+    constexpr int SB = DK / 2;                               // TMEM columns of a part of S
 
-    // chunk tiles, by thread 32; a stage is filled again once step 5 of its last chunk is through
-    auto load = [&](int c) {
-        const uint32_t t = ring + (c % L::STAGES) * L::BYTES, bar = full + 8 * (c % L::STAGES);
-        const int64_t cid = chain * nc + c;
-        mbar_expect_tx(bar, L::LOAD);
+    if (warp >= SW) {
+        regs_dec<IDLE_REGS>();
+        if (warp == SW) {                                    // MMAs
+            const uint32_t id64 = mma_idesc(64), idk = mma_idesc(DK) | MN_B;
+            for (int c = 0; c < chunks; ++c) {
+                const uint32_t t = ring + (c % L::STAGES) * L::BYTES, ph = c & 1;
+                const uint64_t dk = sw128_desc(t + L::KQ), dq = sw128_desc(t + L::KQ + 8192), dm = sw128_desc(t + L::M),
+                               dkt = sw128_mn_desc(t + L::KQ, 16384);
+                await(full + 8 * (c % L::STAGES), (c / L::STAGES) & 1, dead);
+                await(go, ph, dead);
+                if (elect_one()) {                           // step 1
 #pragma unroll
-        for (int x = 0; x < DK / 64; ++x) {
-            tma_load_4d(t + L::KQ + x * 16384, &tk, 64 * x, c * C, hk, b, bar);
-            tma_load_4d(t + L::KQ + x * 16384 + 8192, &tq, 64 * x, c * C, hk, b, bar);
+                    for (int p = 0; p < NS; ++p)
+#pragma unroll
+                        for (int kk = 0; kk < DK / 16; ++kk)
+                            mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * SB + kk * 8, dk + (kk / 4) * 1024 + (kk % 4) * 2, id64, (p | kk) != 0);
+                    mma_commit(step);
+#pragma unroll
+                    for (int p = 0; p < NS; ++p)
+#pragma unroll
+                        for (int kk = 0; kk < DK / 16; ++kk)
+                            mma_bf16_ta(tmem + X_COL + 64, tmem + S_COL + p * SB + kk * 8, dq + (kk / 4) * 1024 + (kk % 4) * 2, id64, (p | kk) != 0);
+                    mma_commit(step + 8);
+                }
+                __syncwarp();
+                await(go + 8, ph, dead);
+                if (elect_one()) {                           // step 3: (upper, upper), (upper, lower), (lower, upper)
+#pragma unroll
+                    for (int m = 0; m < 3; ++m)
+#pragma unroll
+                        for (int kk = 0; kk < C / 16; ++kk)
+                            mma_bf16_ta(tmem + X_COL, tmem + R_COL + (m == 2 ? 32 : 0) + kk * 8, dm + (m == 1 ? MAT / 16 : 0) + kk * 2, id64, (m | kk) != 0);
+                    mma_commit(step + 16);
+                }
+                __syncwarp();
+                await(go + 16, ph, dead);
+                if (elect_one()) {                           // step 5
+#pragma unroll
+                    for (int p = 0; p < NH; ++p)
+#pragma unroll
+                        for (int kk = 0; kk < C / 16; ++kk)
+                            mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * 32 + kk * 8, dkt + kk * 128, idk, (p | kk) != 0);
+                    mma_commit(step + 24);
+#pragma unroll
+                    for (int p = 0; p < NS; ++p)
+#pragma unroll
+                        for (int kk = 0; kk < C / 16; ++kk)
+                            mma_bf16_ta(tmem + Y_COL, tmem + R_COL + p * 32 + kk * 8, dm + 2 * MAT / 16 + kk * 2, id64, (p | kk) != 0);
+                    mma_commit(step + 32);
+                }
+                __syncwarp();
+            }
+        } else if (warp == SW + 1 && lane == 0) {            // copies
+            auto load = [&](int c) {
+                const uint32_t t = ring + (c % L::STAGES) * L::BYTES, bar = full + 8 * (c % L::STAGES);
+                const int64_t cid = chain * nc + c;
+                mbar_expect_tx(bar, L::LOAD);
+#pragma unroll
+                for (int x = 0; x < DK / 64; ++x) {
+                    tma_load_4d(t + L::KQ + x * 16384, &tk, 64 * x, c * C, hk, b, bar);
+                    tma_load_4d(t + L::KQ + x * 16384 + 8192, &tq, 64 * x, c * C, hk, b, bar);
+                }
+                tma_load_4d(t + L::V, &tv, col0, c * C, h, b, bar);
+                tma_load_4d(t + L::V + 8192, &tv, col0 + 64, c * C, h, b, bar);
+#pragma unroll
+                for (int m = 0; m < 3; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * 3 + m) * C), bar);
+                bulk_load(t + L::G, f.gates + cid * 3 * C, GATES, bar);
+            };
+            int loaded = 0;
+            for (; loaded < chunks && loaded < L::STAGES; ++loaded) load(loaded);
+            for (int c = 0; c < chunks; ++c) {
+                mbar_wait_or_dead(go + 24, c & 1, dead);     // y of chunk c lies where its v was
+                if (*dead) break;
+                const uint32_t t = ring + (c % L::STAGES) * L::BYTES + L::V;
+                tma_store_4d(&ty, t, col0, c * C, h, b);
+                if (col0 + 64 < a.dv) tma_store_4d(&ty, t + 8192, col0 + 64, c * C, h, b);
+                bulk_commit();
+                if (loaded < chunks) {
+                    bulk_wait_read();
+                    load(loaded++);
+                }
+            }
+            bulk_wait();
+            if (*dead)                                       // the copies in flight land before the CTA ends
+                for (int j = loaded > L::STAGES ? loaded - L::STAGES : 0; j < loaded; ++j) mbar_wait(full + 8 * (j % L::STAGES), (j / L::STAGES) & 1);
         }
-        tma_load_4d(t + L::V, &tv, col0, c * C, h, b, bar);
-        tma_load_4d(t + L::V + 8192, &tv, col0 + 64, c * C, h, b, bar);
-#pragma unroll
-        for (int m = 0; m < 3; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * 3 + m) * C), bar);
-        bulk_load(t + L::G, f.gates + cid * 3 * C, GATES, bar);
-    };
-    int loaded = 0;                                          // (thread 32) chunks whose copies were started
-    if (tid == 32)
-        for (; loaded < chunks && loaded < L::STAGES; ++loaded) load(loaded);
-    {
+    } else {
+        regs_inc<SCAN_REGS>();
         const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane, col = col0 + row;
         const bool live = col < a.dv;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         const int64_t per = static_cast<int64_t>(a.dk) * a.dv;
         float* st = r.state + chain * per + col;
-        __nv_bfloat16* y = static_cast<__nv_bfloat16*>(r.y) + gdn_base(a.token_major, b, h, a.H, a.T, a.dv) + col;
-        const int64_t ys = gdn_stride(a.token_major, a.H, a.dv);
-        constexpr int RD = DK / 2, SB = DK / 2;              // rows of d_k per warp; TMEM columns of a part of S
+        constexpr int RD = DK / 2;                           // rows of d_k per warp
         float S[RD];
         if (chunks > 0) {
 #pragma unroll
@@ -339,140 +478,89 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 S[x] = live && rw < a.dk ? __ldcs(st + static_cast<int64_t>(rw) * a.dv) : 0.f;
             }
         }
-        auto put_state = [&]() {
+        auto put_state = [&](int next) {                     // S before chunk `next`
 #pragma unroll
             for (int x = 0; x < RD; x += 32) {
                 float v[32];
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = S[x + j];
-                put_parts(lanes + S_COL + (half * RD + x) / 2, SB, v);
+                put_parts<NS>(lanes + S_COL + (half * RD + x) / 2, SB, v);
             }
             tmem_st_wait();
-        };
-        const uint32_t id64 = mma_idesc(64), idk = mma_idesc(DK) | MN_B;
-        float out[32];                                       // g Q S of this warp's 32 tokens
-        auto finish = [&](int c) {                           // y of chunk c, once step 5 is through
-            mbar_wait_or_dead(step + 24, c & 1, dead);
-            __syncwarp();
-            tc_after_sync();
-            float v[32];
-            tmem_ld32(lanes + Y_COL + 32 * half, v);
-            const int t0 = c * C + 32 * half;
-            if (live) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (t0 + j < len) y[(t0 + j) * ys] = __float2bfloat16_rn(a.scale * (out[j] + v[j]));
-            }
-        };
-        if (chunks > 0) put_state();
-        for (int c = 0; c < chunks; ++c) {
-            const int s = c % L::STAGES;
-            const uint32_t t = ring + s * L::BYTES, ph = c & 1;
-            const unsigned char* tile = raw + (t - base);
-            const float* gate = reinterpret_cast<const float*>(tile + L::G);
-            mbar_wait_or_dead(full + 8 * s, (c / L::STAGES) & 1, dead);
-            const int n = len - c * C;                       // live tokens (64 or more: all)
-            if (n < C) {                                     // K rows past the length: zeros, whatever was there
+            if (next < chunks && len - next * C < C) {       // K rows past the length: zeros, whatever was there
+                const int n = len - next * C, s = next % L::STAGES;
+                mbar_wait_or_dead(full + 8 * s, (next / L::STAGES) & 1, dead);
                 for (int p = tid; p < (C - n) * DK / 8; p += 32 * SW) {
                     const int rw = n + p / (DK / 8), x = p % (DK / 8);
-                    *reinterpret_cast<uint4*>(raw + (t - base) + (x / 8) * 16384 + rw * 128 + (x % 8) * 16) = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4*>(ringp + s * L::BYTES + L::KQ + (x / 8) * 16384 + rw * 128 + (x % 8) * 16) = make_uint4(0, 0, 0, 0);
                 }
                 fence_async();
             }
-            tc_before_sync();
-            __syncthreads();
-            if (tid == 0) {                                  // step 1
-                tc_after_sync();
+            announce(go, lane);
+        };
+        const uint32_t vat = L::V + (row / 64) * 8192;
+        float out[32];                                       // g Q S of this warp's 32 tokens
+        auto finish = [&](int c) {                           // y of chunk c, once step 5 is through
+            await(step + 32, c & 1, dead);
+            float v[32];
+            tmem_ld32(lanes + Y_COL + 32 * half, v);
+            unsigned char* vt = ringp + (c % L::STAGES) * L::BYTES + vat;
+            const int n = len - c * C;
 #pragma unroll
-                for (int p = 0; p < NS; ++p)
-#pragma unroll
-                    for (int kk = 0; kk < DK / 16; ++kk)
-                        mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * SB + kk * 8, sw128_desc(t + (kk / 4) * 16384 + (kk % 4) * 32), id64, (p | kk) != 0);
-                mma_commit(step);
-#pragma unroll
-                for (int p = 0; p < NS; ++p)
-#pragma unroll
-                    for (int kk = 0; kk < DK / 16; ++kk)
-                        mma_bf16_ta(tmem + X_COL + 64, tmem + S_COL + p * SB + kk * 8, sw128_desc(t + 8192 + (kk / 4) * 16384 + (kk % 4) * 32), id64, (p | kk) != 0);
-                mma_commit(step + 32);
+            for (int j = 0; j < 32; ++j) {
+                const int i = 32 * half + j;
+                *reinterpret_cast<__nv_bfloat16*>(vt + sw128_at(i, row % 64)) = __float2bfloat16_rn(i < n ? a.scale * (out[j] + v[j]) : 0.f);
             }
-            __syncwarp();
-            if (c > 0) {
-                finish(c - 1);
-                if (tid == 32 && loaded < chunks && !*dead) load(loaded++);
-                __syncwarp();
-            }
-            mbar_wait_or_dead(step, ph, dead);
-            __syncwarp();
-            tc_after_sync();
+            fence_async();
+            announce(go + 24, lane);
+        };
+        if (chunks > 0) put_state(0);
+        for (int c = 0; c < chunks; ++c) {
+            const int s = c % L::STAGES;
+            const uint32_t ph = c & 1;
+            const unsigned char* tile = ringp + s * L::BYTES;
+            const float* gate = reinterpret_cast<const float*>(tile + L::G);
+            const int n = len - c * C;                       // live tokens (64 or more: all)
+            if (c > 0) finish(c - 1);
+            mbar_wait_or_dead(full + 8 * s, (c / L::STAGES) & 1, dead);
+            await(step, ph, dead);
+            float u[32];
             {                                                // step 2
-                float u[32];
                 tmem_ld32(lanes + X_COL + 32 * half, u);
-                const unsigned char* vt = tile + L::V + (row / 64) * 8192;
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
                     const int i = 32 * half + j;
-                    const unsigned short raw16 = *reinterpret_cast<const unsigned short*>(vt + i * 128 + (((row % 64) * 2) ^ ((i & 7) << 4)));
+                    const unsigned short raw16 = *reinterpret_cast<const unsigned short*>(tile + vat + sw128_at(i, row % 64));
                     const float v = __uint_as_float(static_cast<uint32_t>(raw16) << 16);
                     u[j] = i < n ? gate[C + i] * (v - gate[i] * u[j]) : 0.f;
                 }
-                put_parts(lanes + R_COL + 16 * half, 32, u);
+                float w[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) w[j] = u[j];
+                put_parts<NS>(lanes + R_COL + 16 * half, 32, w);
                 tmem_st_wait();
+                announce(go + 8, lane);
             }
-            tc_before_sync();
-            __syncthreads();
-            if (tid == 0) {                                  // step 3
-                tc_after_sync();
-#pragma unroll
-                for (int m = 0; m < 3; ++m) {                // parts (upper, upper), (upper, lower), (lower, upper)
-                    const uint32_t ra = tmem + R_COL + (m == 2 ? 32 : 0), zb = t + L::M + (m == 1 ? MAT : 0);
-#pragma unroll
-                    for (int kk = 0; kk < C / 16; ++kk)
-                        mma_bf16_ta(tmem + X_COL, ra + kk * 8, sw128_desc(zb + kk * 32), id64, (m | kk) != 0);
-                }
-                mma_commit(step + 8);
-            }
-            __syncwarp();
-            mbar_wait_or_dead(step + 32, ph, dead);
-            __syncwarp();
-            tc_after_sync();
+            await(step + 8, ph, dead);
             tmem_ld32(lanes + X_COL + 64 + 32 * half, out);
 #pragma unroll
             for (int j = 0; j < 32; ++j) out[j] *= gate[32 * half + j];
-            mbar_wait_or_dead(step + 8, ph, dead);
-            __syncwarp();
-            tc_after_sync();
+            await(step + 16, ph, dead);
             {                                                // step 4
-                float w[32], hw[32];
+                float w[32];
                 tmem_ld32(lanes + X_COL + 32 * half, w);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) hw[j] = w[j] * gate[2 * C + 32 * half + j];
-                put_parts(lanes + R_COL + 16 * half, 32, hw);
-                put_parts(lanes + W_COL + 16 * half, 32, w);
+                for (int j = 0; j < 32; ++j) {
+                    w[j] += u[j];
+                    u[j] = w[j] * gate[2 * C + 32 * half + j];
+                }
+                put_parts<NH>(lanes + S_COL + 16 * half, 32, u);
+                put_parts<NS>(lanes + R_COL + 16 * half, 32, w);
                 tmem_st_wait();
             }
             const float g63 = gate[C - 1];
-            tc_before_sync();
-            __syncthreads();
-            if (tid == 0) {                                  // step 5
-                tc_after_sync();
-#pragma unroll
-                for (int p = 0; p < NS; ++p)
-#pragma unroll
-                    for (int kk = 0; kk < C / 16; ++kk)
-                        mma_bf16_ta(tmem + X_COL, tmem + R_COL + p * 32 + kk * 8, sw128_mn_desc(t + kk * 2048, 16384), idk, (p | kk) != 0);
-                mma_commit(step + 16);
-#pragma unroll
-                for (int p = 0; p < 2; ++p)
-#pragma unroll
-                    for (int kk = 0; kk < C / 16; ++kk)
-                        mma_bf16_ta(tmem + Y_COL, tmem + W_COL + p * 32 + kk * 8, sw128_desc(t + L::M + 2 * MAT + kk * 32), id64, (p | kk) != 0);
-                mma_commit(step + 24);
-            }
-            __syncwarp();
-            mbar_wait_or_dead(step + 16, ph, dead);
-            __syncwarp();
-            tc_after_sync();
+            announce(go + 16, lane);
+            await(step + 24, ph, dead);
 #pragma unroll
             for (int x = 0; x < RD; x += 32) {               // step 6
                 float v[32];
@@ -480,7 +568,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
 #pragma unroll
                 for (int j = 0; j < 32; ++j) S[x + j] = fmaf(g63, S[x + j], v[j]);
             }
-            put_state();
+            if (c + 1 < chunks) put_state(c + 1);
         }
         if (chunks > 0) {
             finish(chunks - 1);
@@ -492,11 +580,12 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 }
             }
         }
-        if (live)
-            for (int t = len + half; t < a.T; t += 2) y[t * ys] = __float2bfloat16_rn(0.f);
+        if (live) {                                          // chunks past the length
+            __nv_bfloat16* y = static_cast<__nv_bfloat16*>(r.y) + gdn_base(a.token_major, b, h, a.H, a.T, a.dv) + col;
+            const int64_t ys = gdn_stride(a.token_major, a.H, a.dv);
+            for (int t = chunks * C + half; t < a.T; t += 2) y[t * ys] = __float2bfloat16_rn(0.f);
+        }
     }
-    if (tid == 32 && *dead)                                  // the copies in flight land before the CTA ends
-        for (int j = loaded > L::STAGES ? loaded - L::STAGES : 0; j < loaded; ++j) mbar_wait(full + 8 * (j % L::STAGES), (j / L::STAGES) & 1);
     tc_before_sync();
     __syncthreads();
     if (tid == 0 && ctl.dead) flag_error(a.err, ERR_TIMEOUT);
@@ -505,7 +594,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
 
 template <int DK>
 cudaError_t factors(const CUtensorMap& tk, const CUtensorMap& tq, const GdnArgs& a, const GdnFactors& f, cudaStream_t stream) {
-    constexpr size_t smem = factor_smem<DK>();
+    constexpr size_t smem = FactorSize<DK>::BYTES;
     cudaError_t e = cudaFuncSetAttribute(k_gdn_factors<DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
     k_gdn_factors<DK><<<dim3((a.T + C - 1) / C, a.H, a.B), FT, smem, stream>>>(tk, tq, a, f);
@@ -513,12 +602,17 @@ cudaError_t factors(const CUtensorMap& tk, const CUtensorMap& tq, const GdnArgs&
 }
 
 template <int DK>
-cudaError_t scan(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap& tv, const CUtensorMap& tm, const GdnScan& s,
+cudaError_t scan(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap& tv, const CUtensorMap& ty, const CUtensorMap& tm, const GdnScan& s,
                  const GdnFactors& f, cudaStream_t stream) {
     constexpr size_t smem = scan_smem<DK>();
-    cudaError_t e = cudaFuncSetAttribute(k_gdn_scan<DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    // the compute warpgroups' registers come out of what the CTA is launched with
+    cudaFuncAttributes at;
+    cudaError_t e = cudaFuncGetAttributes(&at, k_gdn_scan<DK>);
     if (e != cudaSuccess) return e;
-    k_gdn_scan<DK><<<dim3((s.a.dv + 127) / 128, s.a.H, s.a.B), ST, smem, stream>>>(tk, tq, tv, tm, s, f, (s.a.T + C - 1) / C);
+    if (at.numRegs * ST < 32 * (SW * SCAN_REGS + 4 * IDLE_REGS)) return cudaErrorInvalidConfiguration;
+    e = cudaFuncSetAttribute(k_gdn_scan<DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) return e;
+    k_gdn_scan<DK><<<dim3((s.a.dv + 127) / 128, s.a.H, s.a.B), ST, smem, stream>>>(tk, tq, tv, ty, tm, s, f, (s.a.T + C - 1) / C);
     return cudaGetLastError();
 }
 
@@ -540,11 +634,11 @@ cudaError_t launch_gdn_factors(const GdnArgs& a, const GdnFactors& f, cudaStream
 cudaError_t launch_gdn_scan(const GdnScan& s, const GdnFactors& f, cudaStream_t stream) {
     const GdnArgs& a = s.a;
     const int64_t chunks = static_cast<int64_t>(a.B) * a.H * ((a.T + C - 1) / C);
-    CUtensorMap tk, tq, tv, tm;
+    CUtensorMap tk, tq, tv, ty, tm;
     if (!token_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk) || !token_map(&tq, a.q, a.token_major, a.B, a.Hk, a.T, a.dk) ||
-        !token_map(&tv, a.v, a.token_major, a.B, a.H, a.T, a.dv) || !mat_map(&tm, f.mat, chunks * 3))
+        !token_map(&tv, a.v, a.token_major, a.B, a.H, a.T, a.dv) || !token_map(&ty, s.y, a.token_major, a.B, a.H, a.T, a.dv) || !mat_map(&tm, f.mat, chunks * 3))
         return cudaErrorInvalidValue;
-    return a.dk <= 64 ? scan<64>(tk, tq, tv, tm, s, f, stream) : scan<128>(tk, tq, tv, tm, s, f, stream);
+    return a.dk <= 64 ? scan<64>(tk, tq, tv, ty, tm, s, f, stream) : scan<128>(tk, tq, tv, ty, tm, s, f, stream);
 }
 
 }  // namespace sdm
