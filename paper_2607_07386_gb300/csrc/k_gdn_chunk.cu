@@ -77,14 +77,14 @@ constexpr int FT = 128;
 constexpr int LP = C + 4;
 constexpr int BL = 16, NB = C / BL;
 struct FactorSmem {
-    float L[C][LP];
     float al[C], be[C], g[C], h[C];
     unsigned long long bar[2];
     uint32_t tmem;
     int dead;
 };
-// The K and Q tiles make room for Z and the products once the MMAs have read them.
+// The K and Q tiles make room for these once the MMAs have read them.
 struct FactorLate {
+    float L[C][LP];
     float Z[C][LP];
     float X[C][BL + 4];
 };
@@ -110,7 +110,7 @@ __device__ __forceinline__ void block_mul(const float* A, int lda, const float* 
 }
 
 template <int DK>
-__global__ void __launch_bounds__(FT) k_gdn_factors(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tq,
+__global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tq,
                                                     const GdnArgs a, const GdnFactors f) {
     extern __shared__ unsigned char raw[];
     const uint32_t base = smem_u32(raw);
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(FT) k_gdn_factors(const __grid_constant__ CUte
     if (isk) {
         sm.g[i] = G;                                                          // all factors up to i
 #pragma unroll
-        for (int j = 0; j < C; j += 4) *reinterpret_cast<float4*>(&sm.L[i][j]) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+        for (int j = 0; j < C; j += 4) *reinterpret_cast<float4*>(&lt.L[i][j]) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
     } else {
         uint4* dst = reinterpret_cast<uint4*>(static_cast<char*>(f.mat) + (cid * 3 + 2) * MAT + i * C * 2);
 #pragma unroll
@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(FT) k_gdn_factors(const __grid_constant__ CUte
         for (int j = 1; j < BL; ++j) {
             float4 l[4];
 #pragma unroll
-            for (int q = 0; q < (j + 3) / 4; ++q) l[q] = *reinterpret_cast<const float4*>(&sm.L[o + j][o + 4 * q]);
+            for (int q = 0; q < (j + 3) / 4; ++q) l[q] = *reinterpret_cast<const float4*>(&lt.L[o + j][o + 4 * q]);
 #pragma unroll
             for (int k = 0; k < j; ++k) {
                 const float lk = (k & 3) == 0 ? l[k / 4].x : (k & 3) == 1 ? l[k / 4].y : (k & 3) == 2 ? l[k / 4].z : l[k / 4].w;
@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(FT) k_gdn_factors(const __grid_constant__ CUte
     for (int d = 1; d < NB; ++d) {                                            // blocks (j + d, j)
         for (int j = tid / 64; j < NB - d; j += 2) {
             float acc[4];
-            block_mul(&sm.L[(j + d) * BL][j * BL], LP, &lt.Z[j * BL][j * BL], LP, d, acc, tid & 63);
+            block_mul(&lt.L[(j + d) * BL][j * BL], LP, &lt.Z[j * BL][j * BL], LP, d, acc, tid & 63);
             const int c = tid & 15, r = ((tid & 63) >> 4) * 4;
 #pragma unroll
             for (int e = 0; e < 4; ++e) lt.X[j * BL + r + e][c] = acc[e];
@@ -285,17 +285,17 @@ __global__ void __launch_bounds__(FT) k_gdn_factors(const __grid_constant__ CUte
 //   4  w = R + .., h w                                (registers, bf16 parts to TMEM)
 //   5  h w K, then w P^T                              (MMA)
 //   6  S = g_63 S + ..                                (registers, bf16 parts to TMEM)
-// and the output of a chunk is added up under step 1 of the next, in the place of its v, and stored by
-// TMA.  Warps 0-7 compute: two share a lane quarter; in steps 2 and 4 each takes 32 tokens, in step 6
-// half of d_k.  Warp 8 issues the MMAs, warp 9 the copies; warps 10 and 11 only complete the warpgroup
-// that gives its registers to the others.
+// Warps 0-7 compute: two share a lane quarter; in steps 2 and 4 each takes 32 tokens, in step 6 half of
+// d_k.  Warps 8-11 add up the outputs of a chunk beside that, in the place of its v, for TMA to store.
+// Warp 12 issues the MMAs, warp 13 the copies.
 //
 // The chain of six stages is what bounds it, then the tensor pipe (2432 cycles of MMAs per chunk at d_k =
 // 128).
 // ------------------------------------------------------------------------------------------
 constexpr int SW = 8;                          // compute warps
-constexpr int ST = 32 * (SW + 4);
-constexpr int SCAN_REGS = 232, IDLE_REGS = 40;   // after the split of the launch's 168 per thread
+constexpr int OW = 4;                          // output warps
+constexpr int ST = 32 * (SW + OW + 4);
+constexpr int SCAN_REGS = 184, OUT_REGS = 104, IDLE_REGS = 40;   // the split of the launch's 128 per thread
 constexpr int NS = 2;                          // bf16 parts of S, of R and of w as the factor of P
 constexpr int NH = 3;                          // bf16 parts of h w
 // TMEM columns: X: steps 1, 3, 5; Y: w P^T; S; R, then w.  h w lies where S is, which steps 2 to 6 do not read.
@@ -308,29 +308,41 @@ struct ScanTile {
     static constexpr uint32_t LOAD = G + GATES;
     static constexpr int STAGES = 3;
 };
+// Barriers.  Completed by MMAs or copies: a stage's tile; U; Q S; R (Z - I); h w K; w P.  Completed by warps:
+// operands in TMEM, Q S taken out, y in shared memory.
+enum { B_FULL = 0, B_U = 3, B_QS, B_RZ, B_HK, B_WP, B_S, B_R, B_H, B_W, B_TAKEN, B_Y, B_COUNT };
 struct ScanCtl {
-    unsigned long long full[3];               // a stage's tile is in
-    unsigned long long step[5];               // MMAs: U; Q S; R (Z - I); h w K; w P
-    unsigned long long go[4];                 // operands in TMEM: S; R; w; y in shared memory
+    unsigned long long bar[B_COUNT];
     uint32_t tmem;
     int dead;
 };
 template <int DK>
 constexpr size_t scan_smem() { return 1024 + ScanTile<DK>::BYTES * ScanTile<DK>::STAGES + sizeof(ScanCtl); }
 
-// 32 values as `parts` bf16 parts, 16 packed columns each, `stride` columns apart.
-template <int PARTS>
-__device__ __forceinline__ void put_parts(uint32_t taddr, uint32_t stride, float (&v)[32]) {
+// The next bf16 part of 32 values into 16 packed columns; the values keep what its rounding left.
+__device__ __forceinline__ void put_part(uint32_t taddr, float (&v)[32]) {
+    uint32_t u[16];
 #pragma unroll
-    for (int p = 0; p < PARTS; ++p) {
-        uint32_t u[16];
+    for (int j = 0; j < 16; ++j) u[j] = split2(v[2 * j], v[2 * j + 1], v[2 * j], v[2 * j + 1]);
+    tmem_st16(taddr, u);
+}
+__device__ __forceinline__ void put_last(uint32_t taddr, const float (&v)[32]) {
+    uint32_t u[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) u[j] = split2(v[2 * j], v[2 * j + 1], v[2 * j], v[2 * j + 1]);
-        tmem_st16(taddr + p * stride, u);
+    for (int j = 0; j < 16; ++j) u[j] = pack2(v[2 * j], v[2 * j + 1]);
+    tmem_st16(taddr, u);
+}
+// 32 neighbouring floats of shared memory (16-byte aligned, the same for the whole warp).
+__device__ __forceinline__ void get32(const float* p, float (&v)[32]) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        const float4 f = *reinterpret_cast<const float4*>(p + 4 * q);
+        v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
     }
 }
-// A warp's share of an operand is in TMEM (or shared memory): tells the issuing warp.
+// A warp's share of an operand is in TMEM: tells the issuing warp.
 __device__ __forceinline__ void announce(uint32_t bar, int lane) {
+    tmem_st_wait();
     tc_before_sync();
     __syncwarp();
     if (lane == 0) mbar_arrive(bar);
@@ -359,12 +371,11 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
     const int len = gdn_length(a, b);
     const int64_t chain = static_cast<int64_t>(b) * a.H + h;
     const int chunks = (len + C - 1) / C;
-    const uint32_t full = smem_u32(&ctl.full[0]), step = smem_u32(&ctl.step[0]), go = smem_u32(&ctl.go[0]);
+    const uint32_t bars = smem_u32(&ctl.bar[0]);
+    auto bar = [&](int i) { return bars + 8 * i; };
     if (tid == 0) {
         ctl.dead = 0;
-        for (int s = 0; s < L::STAGES; ++s) mbar_init(full + 8 * s, 1);
-        for (int s = 0; s < 5; ++s) mbar_init(step + 8 * s, 1);
-        for (int s = 0; s < 4; ++s) mbar_init(go + 8 * s, SW);
+        for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), i < B_S ? 1 : i == B_TAKEN || i == B_Y ? OW : SW);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         fence_async();
     }
@@ -376,78 +387,83 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
     volatile int* dead = &ctl.dead;
     constexpr int SB = DK / 2;                               // TMEM columns of a part of S
 
-    if (warp >= SW) {
+    if (warp >= SW + OW) {
         regs_dec<IDLE_REGS>();
-        if (warp == SW) {                                    // MMAs
+        if (warp == SW + OW) {                               // MMAs
             const uint32_t id64 = mma_idesc(64), idk = mma_idesc(DK) | MN_B;
             for (int c = 0; c < chunks; ++c) {
                 const uint32_t t = ring + (c % L::STAGES) * L::BYTES, ph = c & 1;
                 const uint64_t dk = sw128_desc(t + L::KQ), dq = sw128_desc(t + L::KQ + 8192), dm = sw128_desc(t + L::M),
                                dkt = sw128_mn_desc(t + L::KQ, 16384);
-                await(full + 8 * (c % L::STAGES), (c / L::STAGES) & 1, dead);
-                await(go, ph, dead);
+                await(bar(B_FULL + c % L::STAGES), (c / L::STAGES) & 1, dead);
+                await(bar(B_S), ph, dead);
                 if (elect_one()) {                           // step 1
 #pragma unroll
                     for (int p = 0; p < NS; ++p)
 #pragma unroll
                         for (int kk = 0; kk < DK / 16; ++kk)
                             mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * SB + kk * 8, dk + (kk / 4) * 1024 + (kk % 4) * 2, id64, (p | kk) != 0);
-                    mma_commit(step);
+                    mma_commit(bar(B_U));
 #pragma unroll
                     for (int p = 0; p < NS; ++p)
 #pragma unroll
                         for (int kk = 0; kk < DK / 16; ++kk)
                             mma_bf16_ta(tmem + X_COL + 64, tmem + S_COL + p * SB + kk * 8, dq + (kk / 4) * 1024 + (kk % 4) * 2, id64, (p | kk) != 0);
-                    mma_commit(step + 8);
+                    mma_commit(bar(B_QS));
                 }
                 __syncwarp();
-                await(go + 8, ph, dead);
+                await(bar(B_R), ph, dead);
                 if (elect_one()) {                           // step 3: (upper, upper), (upper, lower), (lower, upper)
 #pragma unroll
                     for (int m = 0; m < 3; ++m)
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
                             mma_bf16_ta(tmem + X_COL, tmem + R_COL + (m == 2 ? 32 : 0) + kk * 8, dm + (m == 1 ? MAT / 16 : 0) + kk * 2, id64, (m | kk) != 0);
-                    mma_commit(step + 16);
+                    mma_commit(bar(B_RZ));
                 }
                 __syncwarp();
-                await(go + 16, ph, dead);
+                await(bar(B_TAKEN), ph, dead);
+                await(bar(B_H), ph, dead);
                 if (elect_one()) {                           // step 5
 #pragma unroll
                     for (int p = 0; p < NH; ++p)
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
                             mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * 32 + kk * 8, dkt + kk * 128, idk, (p | kk) != 0);
-                    mma_commit(step + 24);
+                    mma_commit(bar(B_HK));
+                }
+                __syncwarp();
+                await(bar(B_W), ph, dead);
+                if (elect_one()) {
 #pragma unroll
                     for (int p = 0; p < NS; ++p)
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
-                            mma_bf16_ta(tmem + Y_COL, tmem + R_COL + p * 32 + kk * 8, dm + 2 * MAT / 16 + kk * 2, id64, (p | kk) != 0);
-                    mma_commit(step + 32);
+                            mma_bf16_ta(tmem + Y_COL, tmem + R_COL + p * 32 + kk * 8, dm + 2 * (MAT / 16) + kk * 2, id64, (p | kk) != 0);
+                    mma_commit(bar(B_WP));
                 }
                 __syncwarp();
             }
-        } else if (warp == SW + 1 && lane == 0) {            // copies
+        } else if (warp == SW + OW + 1 && lane == 0) {       // copies
             auto load = [&](int c) {
-                const uint32_t t = ring + (c % L::STAGES) * L::BYTES, bar = full + 8 * (c % L::STAGES);
+                const uint32_t t = ring + (c % L::STAGES) * L::BYTES, fb = bar(B_FULL + c % L::STAGES);
                 const int64_t cid = chain * nc + c;
-                mbar_expect_tx(bar, L::LOAD);
+                mbar_expect_tx(fb, L::LOAD);
 #pragma unroll
                 for (int x = 0; x < DK / 64; ++x) {
-                    tma_load_4d(t + L::KQ + x * 16384, &tk, 64 * x, c * C, hk, b, bar);
-                    tma_load_4d(t + L::KQ + x * 16384 + 8192, &tq, 64 * x, c * C, hk, b, bar);
+                    tma_load_4d(t + L::KQ + x * 16384, &tk, 64 * x, c * C, hk, b, fb);
+                    tma_load_4d(t + L::KQ + x * 16384 + 8192, &tq, 64 * x, c * C, hk, b, fb);
                 }
-                tma_load_4d(t + L::V, &tv, col0, c * C, h, b, bar);
-                tma_load_4d(t + L::V + 8192, &tv, col0 + 64, c * C, h, b, bar);
+                tma_load_4d(t + L::V, &tv, col0, c * C, h, b, fb);
+                tma_load_4d(t + L::V + 8192, &tv, col0 + 64, c * C, h, b, fb);
 #pragma unroll
-                for (int m = 0; m < 3; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * 3 + m) * C), bar);
-                bulk_load(t + L::G, f.gates + cid * 3 * C, GATES, bar);
+                for (int m = 0; m < 3; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * 3 + m) * C), fb);
+                bulk_load(t + L::G, f.gates + cid * 3 * C, GATES, fb);
             };
             int loaded = 0;
             for (; loaded < chunks && loaded < L::STAGES; ++loaded) load(loaded);
             for (int c = 0; c < chunks; ++c) {
-                mbar_wait_or_dead(go + 24, c & 1, dead);     // y of chunk c lies where its v was
+                mbar_wait_or_dead(bar(B_Y), c & 1, dead);    // y of chunk c lies where its v was
                 if (*dead) break;
                 const uint32_t t = ring + (c % L::STAGES) * L::BYTES + L::V;
                 tma_store_4d(&ty, t, col0, c * C, h, b);
@@ -460,16 +476,65 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
             }
             bulk_wait();
             if (*dead)                                       // the copies in flight land before the CTA ends
-                for (int j = loaded > L::STAGES ? loaded - L::STAGES : 0; j < loaded; ++j) mbar_wait(full + 8 * (j % L::STAGES), (j / L::STAGES) & 1);
+                for (int j = loaded > L::STAGES ? loaded - L::STAGES : 0; j < loaded; ++j)
+                    mbar_wait(bar(B_FULL + j % L::STAGES), (j / L::STAGES) & 1);
+        }
+    } else if (warp >= SW) {                                 // outputs: column `row`, all tokens
+        regs_dec<OUT_REGS>();
+        const int quad = warp & 3, row = quad * 32 + lane;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+        for (int c = 0; c < chunks; ++c) {
+            const uint32_t ph = c & 1;
+            unsigned char* tile = ringp + (c % L::STAGES) * L::BYTES;
+            const float* gate = reinterpret_cast<const float*>(tile + L::G);
+            unsigned char* vt = tile + L::V + (row / 64) * 8192;
+            const int n = len - c * C;
+            mbar_wait_or_dead(bar(B_FULL + c % L::STAGES), (c / L::STAGES) & 1, dead);
+            await(bar(B_QS), ph, dead);
+            float out[C];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float v[32];
+                tmem_ld32(lanes + X_COL + 64 + 32 * e, v);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) out[32 * e + j] = v[j];
+            }
+            announce(bar(B_TAKEN), lane);
+#pragma unroll
+            for (int j = 0; j < C; j += 4) {
+                const float4 g = *reinterpret_cast<const float4*>(gate + j);
+                out[j] *= g.x; out[j + 1] *= g.y; out[j + 2] *= g.z; out[j + 3] *= g.w;
+            }
+            await(bar(B_WP), ph, dead);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float v[32];
+                tmem_ld32(lanes + Y_COL + 32 * e, v);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    const int i = 32 * e + j;
+                    *reinterpret_cast<__nv_bfloat16*>(vt + sw128_at(i, row % 64)) =
+                        __float2bfloat16_rn(i < n ? a.scale * (out[i] + v[j]) : 0.f);
+                }
+            }
+            fence_async();
+            announce(bar(B_Y), lane);
+        }
+        const int col = col0 + row;                          // chunks past the length
+        if (col < a.dv) {
+            __nv_bfloat16* y = static_cast<__nv_bfloat16*>(r.y) + gdn_base(a.token_major, b, h, a.H, a.T, a.dv) + col;
+            const int64_t ys = gdn_stride(a.token_major, a.H, a.dv);
+            for (int t = chunks * C; t < a.T; ++t) y[t * ys] = __float2bfloat16_rn(0.f);
         }
     } else {
         regs_inc<SCAN_REGS>();
         const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane, col = col0 + row;
+        const int i0 = 32 * half;                            // this warp's tokens of a chunk
         const bool live = col < a.dv;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         const int64_t per = static_cast<int64_t>(a.dk) * a.dv;
         float* st = r.state + chain * per + col;
-        constexpr int RD = DK / 2;                           // rows of d_k per warp
+        constexpr int RD = DK / 2;                           // rows of d_k of a warp
         float S[RD];
         if (chunks > 0) {
 #pragma unroll
@@ -484,36 +549,22 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 float v[32];
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = S[x + j];
-                put_parts<NS>(lanes + S_COL + (half * RD + x) / 2, SB, v);
+                put_part(lanes + S_COL + (half * RD + x) / 2, v);
+                put_last(lanes + S_COL + SB + (half * RD + x) / 2, v);
             }
-            tmem_st_wait();
-            if (next < chunks && len - next * C < C) {       // K rows past the length: zeros, whatever was there
+            if (len - next * C < C) {                        // K rows past the length: zeros, whatever was there
                 const int n = len - next * C, s = next % L::STAGES;
-                mbar_wait_or_dead(full + 8 * s, (next / L::STAGES) & 1, dead);
+                mbar_wait_or_dead(bar(B_FULL + s), (next / L::STAGES) & 1, dead);
                 for (int p = tid; p < (C - n) * DK / 8; p += 32 * SW) {
                     const int rw = n + p / (DK / 8), x = p % (DK / 8);
                     *reinterpret_cast<uint4*>(ringp + s * L::BYTES + L::KQ + (x / 8) * 16384 + rw * 128 + (x % 8) * 16) = make_uint4(0, 0, 0, 0);
                 }
                 fence_async();
+                __syncwarp();
             }
-            announce(go, lane);
+            announce(bar(B_S), lane);
         };
         const uint32_t vat = L::V + (row / 64) * 8192;
-        float out[32];                                       // g Q S of this warp's 32 tokens
-        auto finish = [&](int c) {                           // y of chunk c, once step 5 is through
-            await(step + 32, c & 1, dead);
-            float v[32];
-            tmem_ld32(lanes + Y_COL + 32 * half, v);
-            unsigned char* vt = ringp + (c % L::STAGES) * L::BYTES + vat;
-            const int n = len - c * C;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                const int i = 32 * half + j;
-                *reinterpret_cast<__nv_bfloat16*>(vt + sw128_at(i, row % 64)) = __float2bfloat16_rn(i < n ? a.scale * (out[j] + v[j]) : 0.f);
-            }
-            fence_async();
-            announce(go + 24, lane);
-        };
         if (chunks > 0) put_state(0);
         for (int c = 0; c < chunks; ++c) {
             const int s = c % L::STAGES;
@@ -521,69 +572,66 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
             const unsigned char* tile = ringp + s * L::BYTES;
             const float* gate = reinterpret_cast<const float*>(tile + L::G);
             const int n = len - c * C;                       // live tokens (64 or more: all)
-            if (c > 0) finish(c - 1);
-            mbar_wait_or_dead(full + 8 * s, (c / L::STAGES) & 1, dead);
-            await(step, ph, dead);
-            float u[32];
-            {                                                // step 2
-                tmem_ld32(lanes + X_COL + 32 * half, u);
+            mbar_wait_or_dead(bar(B_FULL + s), (c / L::STAGES) & 1, dead);
+            float u[32], w[32];
+            uint32_t v[16];                                  // this column's v, two tokens in a word
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const int i = 32 * half + j;
-                    const unsigned short raw16 = *reinterpret_cast<const unsigned short*>(tile + vat + sw128_at(i, row % 64));
-                    const float v = __uint_as_float(static_cast<uint32_t>(raw16) << 16);
-                    u[j] = i < n ? gate[C + i] * (v - gate[i] * u[j]) : 0.f;
-                }
-                float w[32];
+            for (int j = 0; j < 16; ++j)
+                v[j] = *reinterpret_cast<const unsigned short*>(tile + vat + sw128_at(i0 + 2 * j, row % 64)) |
+                       (static_cast<uint32_t>(*reinterpret_cast<const unsigned short*>(tile + vat + sw128_at(i0 + 2 * j + 1, row % 64))) << 16);
+            await(bar(B_U), ph, dead);
+            tmem_ld32(lanes + X_COL + i0, u);                // step 2
 #pragma unroll
-                for (int j = 0; j < 32; ++j) w[j] = u[j];
-                put_parts<NS>(lanes + R_COL + 16 * half, 32, w);
-                tmem_st_wait();
-                announce(go + 8, lane);
+            for (int j = 0; j < 32; j += 4) {
+                const float4 g = *reinterpret_cast<const float4*>(gate + i0 + j), be = *reinterpret_cast<const float4*>(gate + C + i0 + j);
+                u[j] = be.x * (__uint_as_float(v[j / 2] << 16) - g.x * u[j]);
+                u[j + 1] = be.y * (__uint_as_float(v[j / 2] & 0xffff0000u) - g.y * u[j + 1]);
+                u[j + 2] = be.z * (__uint_as_float(v[j / 2 + 1] << 16) - g.z * u[j + 2]);
+                u[j + 3] = be.w * (__uint_as_float(v[j / 2 + 1] & 0xffff0000u) - g.w * u[j + 3]);
             }
-            await(step + 8, ph, dead);
-            tmem_ld32(lanes + X_COL + 64 + 32 * half, out);
+            if (n < C) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) out[j] *= gate[32 * half + j];
-            await(step + 16, ph, dead);
-            {                                                // step 4
-                float w[32];
-                tmem_ld32(lanes + X_COL + 32 * half, w);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    w[j] += u[j];
-                    u[j] = w[j] * gate[2 * C + 32 * half + j];
-                }
-                put_parts<NH>(lanes + S_COL + 16 * half, 32, u);
-                put_parts<NS>(lanes + R_COL + 16 * half, 32, w);
-                tmem_st_wait();
+                for (int j = 0; j < 32; ++j) u[j] = i0 + j < n ? u[j] : 0.f;
             }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) w[j] = u[j];
+            put_part(lanes + R_COL + i0 / 2, w);
+            put_last(lanes + R_COL + 32 + i0 / 2, w);
+            announce(bar(B_R), lane);
+            float hh[32];
+            get32(gate + 2 * C + i0, hh);
             const float g63 = gate[C - 1];
-            announce(go + 16, lane);
-            await(step + 24, ph, dead);
+            await(bar(B_QS), ph, dead);                      // S is read: h w may lie there
+            await(bar(B_RZ), ph, dead);
+            tmem_ld32(lanes + X_COL + i0, w);                // step 4
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                w[j] += u[j];
+                u[j] = w[j] * hh[j];
+            }
+            put_part(lanes + S_COL + i0 / 2, u);
+            put_part(lanes + S_COL + 32 + i0 / 2, u);
+            put_last(lanes + S_COL + 64 + i0 / 2, u);
+            announce(bar(B_H), lane);
+            put_part(lanes + R_COL + i0 / 2, w);
+            put_last(lanes + R_COL + 32 + i0 / 2, w);
+            announce(bar(B_W), lane);
+            await(bar(B_HK), ph, dead);
 #pragma unroll
             for (int x = 0; x < RD; x += 32) {               // step 6
-                float v[32];
-                tmem_ld32(lanes + X_COL + half * RD + x, v);
+                float d[32];
+                tmem_ld32(lanes + X_COL + half * RD + x, d);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) S[x + j] = fmaf(g63, S[x + j], v[j]);
+                for (int j = 0; j < 32; ++j) S[x + j] = fmaf(g63, S[x + j], d[j]);
             }
             if (c + 1 < chunks) put_state(c + 1);
         }
-        if (chunks > 0) {
-            finish(chunks - 1);
-            if (live) {
+        if (chunks > 0 && live) {
 #pragma unroll
-                for (int x = 0; x < RD; ++x) {
-                    const int rw = half * RD + x;
-                    if (rw < a.dk) __stcs(st + static_cast<int64_t>(rw) * a.dv, S[x]);
-                }
+            for (int x = 0; x < RD; ++x) {
+                const int rw = half * RD + x;
+                if (rw < a.dk) __stcs(st + static_cast<int64_t>(rw) * a.dv, S[x]);
             }
-        }
-        if (live) {                                          // chunks past the length
-            __nv_bfloat16* y = static_cast<__nv_bfloat16*>(r.y) + gdn_base(a.token_major, b, h, a.H, a.T, a.dv) + col;
-            const int64_t ys = gdn_stride(a.token_major, a.H, a.dv);
-            for (int t = chunks * C + half; t < a.T; t += 2) y[t * ys] = __float2bfloat16_rn(0.f);
         }
     }
     tc_before_sync();
@@ -609,7 +657,7 @@ cudaError_t scan(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap
     cudaFuncAttributes at;
     cudaError_t e = cudaFuncGetAttributes(&at, k_gdn_scan<DK>);
     if (e != cudaSuccess) return e;
-    if (at.numRegs * ST < 32 * (SW * SCAN_REGS + 4 * IDLE_REGS)) return cudaErrorInvalidConfiguration;
+    if (at.numRegs * ST < 32 * (SW * SCAN_REGS + OW * OUT_REGS + 4 * IDLE_REGS)) return cudaErrorInvalidConfiguration;
     e = cudaFuncSetAttribute(k_gdn_scan<DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
     k_gdn_scan<DK><<<dim3((s.a.dv + 127) / 128, s.a.H, s.a.B), ST, smem, stream>>>(tk, tq, tv, ty, tm, s, f, (s.a.T + C - 1) / C);
