@@ -69,24 +69,28 @@ bool mat_map(CUtensorMap* m, const void* base, int64_t mats) {
 // takes row r of it (k_i.k_j for r < 64, q_i.k_j above) and multiplies it by G along the row.
 //
 // Z is inverted in fp32 by blocks of 16: the diagonal blocks by a column per thread in registers, then
-// the block diagonals below in order, Z_ij = -Z_ii (sum_k L_ik Z_kj), each product spread over the CTA
-// (a thread takes four rows of a column; the left operand is a broadcast).  Eliminating whole columns of
-// 64 in registers is 2016 unrolled instructions, whose fetching took 11,600 of a CTA's 20,000 cycles.
+// the block diagonals below in order, Z_ij = -Z_ii (sum_k L_ik Z_kj), a warp per 16 x 16 product, a lane per
+// 4 x 2 outputs (one 16-byte and one 8-byte shared-memory read per 8 multiply-adds; L and the diagonal
+// blocks lie transposed for that).  Shared-memory reads bound the kernel: with 4 x 1 outputs per thread they
+// kept the pipe 80% busy.  Eliminating whole columns of 64 in registers was slower still: 2016 unrolled
+// instructions, whose fetching took 11,600 of a CTA's 20,000 cycles.
 // ------------------------------------------------------------------------------------------
 constexpr int FT = 128;
 constexpr int LP = C + 4;
 constexpr int BL = 16, NB = C / BL;
 struct FactorSmem {
-    float al[C], be[C], g[C], h[C];
+    uint4 al[C / 8];                          // alpha, bf16
+    float be[C];
     unsigned long long bar[2];
     uint32_t tmem;
     int dead;
 };
 // The K and Q tiles make room for these once the MMAs have read them.
 struct FactorLate {
-    float L[C][LP];
-    float Z[C][LP];
-    float X[C][BL + 4];
+    float Lt[C][C];                           // L transposed
+    float Z[C][LP];                           // below and on the diagonal
+    float Zt[C][BL];                          // diagonal blocks transposed: [16 block + column][row]
+    float X[NB][BL][BL + 4];
 };
 template <int DK>
 struct FactorSize {
@@ -94,18 +98,25 @@ struct FactorSize {
     static constexpr size_t BYTES = 1024 + TILE + sizeof(FactorSmem);
 };
 
-// One block product: dst = sign * sum over nk blocks of A[ar + .., ac + 16 k + ..] B[br + 16 k + .., bc + ..];
-// 64 threads, thread u: column u % 16, rows 4 (u / 16) .. + 3.
-__device__ __forceinline__ void block_mul(const float* A, int lda, const float* B, int ldb, int nk, float (&acc)[4], int u) {
-    const int c = u & 15, r = (u >> 4) * 4;
-    acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
-    for (int k = 0; k < nk * BL; k += 4) {
-        const float b0 = B[k * ldb + c], b1 = B[(k + 1) * ldb + c], b2 = B[(k + 2) * ldb + c], b3 = B[(k + 3) * ldb + c];
+// acc[r][c] = sum_k At[k][4 (lane / 8) + r] B[k][2 (lane % 8) + c] over 16 k, B the sum of `terms` blocks.
+__device__ __forceinline__ void block_mul(const float* At, int lda, const float* B, int ldb, int terms, int term, float (&acc)[4][2], int lane) {
+    const float* ap = At + 4 * (lane >> 3);
+    const float* bp = B + 2 * (lane & 7);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float4 x = *reinterpret_cast<const float4*>(A + (r + e) * lda + k);
-            acc[e] = fmaf(x.x, b0, fmaf(x.y, b1, fmaf(x.z, b2, fmaf(x.w, b3, acc[e]))));
+    for (int r = 0; r < 4; ++r) acc[r][0] = acc[r][1] = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < BL; ++k) {
+        const float4 a = *reinterpret_cast<const float4*>(ap + k * lda);
+        float2 b = *reinterpret_cast<const float2*>(bp + k * ldb);
+        for (int t = 1; t < terms; ++t) {
+            const float2 o = *reinterpret_cast<const float2*>(bp + t * term + k * ldb);
+            b.x += o.x;
+            b.y += o.y;
         }
+        acc[0][0] = fmaf(a.x, b.x, acc[0][0]); acc[0][1] = fmaf(a.x, b.y, acc[0][1]);
+        acc[1][0] = fmaf(a.y, b.x, acc[1][0]); acc[1][1] = fmaf(a.y, b.y, acc[1][1]);
+        acc[2][0] = fmaf(a.z, b.x, acc[2][0]); acc[2][1] = fmaf(a.z, b.y, acc[2][1]);
+        acc[3][0] = fmaf(a.w, b.x, acc[3][0]); acc[3][1] = fmaf(a.w, b.y, acc[3][1]);
     }
 }
 
@@ -142,13 +153,22 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
     if (warp == 1) tmem_alloc(smem_u32(&sm.tmem), 64);
     if (tid >= C) {
         const int t = tid - C;
-        sm.al[t] = t < n ? load_elem<BF16>(a.alpha, chain * a.T + t0 + t) : 1.f;
+        reinterpret_cast<unsigned short*>(sm.al)[t] = t < n ? __ldg(static_cast<const unsigned short*>(a.alpha) + chain * a.T + t0 + t) : 0x3f80;
         sm.be[t] = t < n ? load_elem<BF16>(a.beta, chain * a.T + t0 + t) : 0.f;
     }
     tc_before_sync();
     __syncthreads();
     tc_after_sync();
     const uint32_t tmem = sm.tmem;
+    if (n < C) {                                          // rows past the length: zeros, whatever was there
+        mbar_wait_or_dead(bar, 0, &sm.dead);
+        for (int p = tid; p < (C - n) * DK / 4; p += FT) {
+            const int half = p % 2, rw = n + (p / 2) / (DK / 8), x = (p / 2) % (DK / 8);
+            *reinterpret_cast<uint4*>(raw + (tile - base) + (x / 8) * 16384 + half * 8192 + rw * 128 + (x % 8) * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_async();
+        __syncthreads();
+    }
     if (warp == 0) {
         mbar_wait_or_dead(bar, 0, &sm.dead);
         __syncwarp();
@@ -164,92 +184,110 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
             mma_commit(done);
         }
         __syncwarp();
+    } else if (warp == 1) {                               // prefix and suffix products of the gates, two tokens a lane
+        const int l = tid & 31;
+        const uint32_t w = reinterpret_cast<const uint32_t*>(sm.al)[l];
+        const float a0 = __uint_as_float(w << 16), a1 = __uint_as_float(w & 0xffff0000u);
+        float p = a0 * a1, q = p;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const float u = __shfl_up_sync(0xffffffffu, p, o), v = __shfl_down_sync(0xffffffffu, q, o);
+            if (l >= o) p *= u;
+            if (l + o < 32) q *= v;
+        }
+        const float before = __shfl_up_sync(0xffffffffu, p, 1), after = __shfl_down_sync(0xffffffffu, q, 1);
+        float* const gates = f.gates + cid * 3 * C;
+        const float h1 = l < 31 ? after : 1.f;
+        *reinterpret_cast<float2*>(gates + 2 * l) = make_float2(l > 0 ? before * a0 : a0, p);
+        *reinterpret_cast<float2*>(gates + C + 2 * l) = make_float2(sm.be[2 * l], sm.be[2 * l + 1]);
+        *reinterpret_cast<float2*>(gates + 2 * C + 2 * l) = make_float2(a1 * h1, h1);
     }
-    // row i of the decay products, from the diagonal to the left: G_ii = 1, G_i,j-1 = G_ij alpha_j
+    // row i of the decay products, from the diagonal to the left: G_ii = 1, G_i,j-1 = G_ij alpha_j (times
+    // beta_i where the row is one of L, whose diagonal is not used)
     const int i = tid & 63;
     const bool isk = tid < C;
     mbar_wait_or_dead(done, 0, &sm.dead);
     __syncwarp();
     tc_after_sync();
-    float x[C];
+    const float G0 = isk ? sm.be[i] : 1.f;
+    float G = 0.f;
+    uint4* const P = reinterpret_cast<uint4*>(static_cast<char*>(f.mat) + (cid * 3 + 2) * MAT + i * C * 2);
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        float v[32];
-        tmem_ld32(tmem + (static_cast<uint32_t>(warp * 32) << 16) + 32 * c, v);
+    for (int half = 1; half >= 0; --half) {               // columns 32.. , then 0..; rows 0-31 have none of the first
+        if (half == 1 && (warp & 1) == 0) {
+            if (!isk) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) x[32 * c + j] = v[j];
-    }
-    const bool row_on = i < n;
-    float G = 1.f;
-    const float be = sm.be[i];
+                for (int j = 4; j < 8; ++j) P[j] = make_uint4(0, 0, 0, 0);
+            }
+            continue;
+        }
+        float x[32];
+        tmem_ld32(tmem + (static_cast<uint32_t>(warp * 32) << 16) + 32 * half, x);
 #pragma unroll
-    for (int j = C - 1; j >= 0; --j) {
-        const bool in = row_on && (isk ? j < i : j <= i);
-        x[j] = in ? G * (isk ? be * x[j] : x[j]) : 0.f;
-        if (tid == 2 * C - 1) sm.h[j] = G;                                    // row 63: prod_{l > j}
-        if (j <= i) G *= sm.al[j];
-    }
-    if (isk) {
-        sm.g[i] = G;                                                          // all factors up to i
+        for (int q = 3; q >= 0; --q) {
+            const uint4 w = sm.al[4 * half + q];
+            const uint32_t al[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int j = 0; j < C; j += 4) *reinterpret_cast<float4*>(&lt.L[i][j]) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
-    } else {
-        uint4* dst = reinterpret_cast<uint4*>(static_cast<char*>(f.mat) + (cid * 3 + 2) * MAT + i * C * 2);
+            for (int e = 7; e >= 0; --e) {
+                const int j = 32 * half + 8 * q + e;
+                G = j == i ? G0 : G;
+                x[8 * q + e] *= G;
+                G *= __uint_as_float(e & 1 ? al[e / 2] & 0xffff0000u : al[e / 2] << 16);
+            }
+        }
+        if (isk) {
 #pragma unroll
-        for (int j = 0; j < C / 8; ++j) {
-            float v[8];
+            for (int j = 0; j < 32; ++j) lt.Lt[32 * half + j][i] = x[j];
+        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = x[8 * j + e];
-            dst[j] = pack16<BF16>(v);
+            for (int j = 0; j < 4; ++j) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = 32 * half + 8 * j + e <= i ? x[8 * j + e] : 0.f;
+                P[4 * half + j] = pack16<BF16>(v);
+            }
         }
     }
     __syncthreads();
-    if (tid < C) {
-        f.gates[cid * 3 * C + tid] = sm.g[tid];
-        f.gates[cid * 3 * C + C + tid] = sm.be[tid];
-    } else {
-        f.gates[cid * 3 * C + C + tid] = sm.h[tid - C];
-    }
     if (isk) {                                                                // diagonal block tid / 16, column tid % 16
         const int o = tid & ~15, c = tid & 15;
         float z[BL];
 #pragma unroll
         for (int j = 0; j < BL; ++j) z[j] = j == c ? 1.f : 0.f;
 #pragma unroll
-        for (int j = 1; j < BL; ++j) {
-            float4 l[4];
+        for (int k = 0; k < BL - 1; ++k) {
 #pragma unroll
-            for (int q = 0; q < (j + 3) / 4; ++q) l[q] = *reinterpret_cast<const float4*>(&lt.L[o + j][o + 4 * q]);
-#pragma unroll
-            for (int k = 0; k < j; ++k) {
-                const float lk = (k & 3) == 0 ? l[k / 4].x : (k & 3) == 1 ? l[k / 4].y : (k & 3) == 2 ? l[k / 4].z : l[k / 4].w;
-                z[j] = fmaf(-lk, z[k], z[j]);
+            for (int q = (k + 1) / 4; q < BL / 4; ++q) {
+                const float4 l = *reinterpret_cast<const float4*>(&lt.Lt[o + k][o + 4 * q]);
+                if (4 * q > k) z[4 * q] = fmaf(-l.x, z[k], z[4 * q]);
+                if (4 * q + 1 > k) z[4 * q + 1] = fmaf(-l.y, z[k], z[4 * q + 1]);
+                if (4 * q + 2 > k) z[4 * q + 2] = fmaf(-l.z, z[k], z[4 * q + 2]);
+                z[4 * q + 3] = fmaf(-l.w, z[k], z[4 * q + 3]);
             }
         }
 #pragma unroll
         for (int j = 0; j < BL; ++j) lt.Z[o + j][o + c] = z[j];
-    } else {                                                                  // above the diagonal
-        for (int p = tid - C; p < C * C / 4; p += C) {
-            const int r = p / (C / 4), c = (p % (C / 4)) * 4;
-            if (c / BL > r / BL) *reinterpret_cast<float4*>(&lt.Z[r][c]) = make_float4(0.f, 0.f, 0.f, 0.f);
-        }
+#pragma unroll
+        for (int j = 0; j < BL; j += 4) *reinterpret_cast<float4*>(&lt.Zt[tid][j]) = make_float4(z[j], z[j + 1], z[j + 2], z[j + 3]);
     }
     __syncthreads();
-    for (int d = 1; d < NB; ++d) {                                            // blocks (j + d, j)
-        for (int j = tid / 64; j < NB - d; j += 2) {
-            float acc[4];
-            block_mul(&lt.L[(j + d) * BL][j * BL], LP, &lt.Z[j * BL][j * BL], LP, d, acc, tid & 63);
-            const int c = tid & 15, r = ((tid & 63) >> 4) * 4;
+    const int lane = tid & 31, br = 4 * (lane >> 3), bc = 2 * (lane & 7);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) lt.X[j * BL + r + e][c] = acc[e];
+    for (int d = 1; d < NB; ++d) {                                            // blocks (j + d, j)
+        if (warp < (NB - d) * d) {                                            // warp: block j = warp / d, its term k = j + warp % d
+            const int j = warp / d, k = j + warp % d;
+            float acc[4][2];
+            block_mul(&lt.Lt[k * BL][(j + d) * BL], C, &lt.Z[k * BL][j * BL], LP, 1, 0, acc, lane);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) *reinterpret_cast<float2*>(&lt.X[warp][br + r][bc]) = make_float2(acc[r][0], acc[r][1]);
         }
         __syncthreads();
-        for (int j = tid / 64; j < NB - d; j += 2) {
-            float acc[4];
-            block_mul(&lt.Z[(j + d) * BL][(j + d) * BL], LP, &lt.X[j * BL][0], BL + 4, 1, acc, tid & 63);
-            const int c = tid & 15, r = ((tid & 63) >> 4) * 4;
+        if (warp < NB - d) {
+            float acc[4][2];
+            block_mul(&lt.Zt[(warp + d) * BL][0], BL, &lt.X[warp * d][0][0], BL + 4, d, BL * (BL + 4), acc, lane);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) lt.Z[(j + d) * BL + r + e][j * BL + c] = -acc[e];
+            for (int r = 0; r < 4; ++r)
+                *reinterpret_cast<float2*>(&lt.Z[(warp + d) * BL + br + r][warp * BL + bc]) = make_float2(-acc[r][0], -acc[r][1]);
         }
         __syncthreads();
     }
@@ -258,7 +296,7 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
         float v[8];
         uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c + e == r ? 0.f : lt.Z[r][c + e];
+        for (int e = 0; e < 8; ++e) v[e] = c + e < r ? lt.Z[r][c + e] : 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             hi[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
