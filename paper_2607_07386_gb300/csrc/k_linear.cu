@@ -27,7 +27,7 @@ namespace {
 using namespace tc;
 
 constexpr int BM = 128, BK = 64;
-constexpr int EPI_WARPS = 4;
+constexpr int EPI_WARPS = 8;                // two per TMEM lane quarter, each half of the tile's columns
 constexpr int LT = 64 + 32 * EPI_WARPS;       // producer, MMA issuer, epilogue
 constexpr int SMS = 152;
 
@@ -62,14 +62,14 @@ bool make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int 
 
 __device__ __forceinline__ float act_fwd(float z, int act) {
     if (act == SDM_ACT_RELU) return z > 0.f ? z : 0.f;
-    if (act == SDM_ACT_SILU) return z / (1.f + __expf(-z));
+    if (act == SDM_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));     // a few float32 ulps, rounded to bf16 below
     if (act == SDM_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
     return z;
 }
 __device__ __forceinline__ float act_slope(float z, int act) {
     if (act == SDM_ACT_RELU) return z > 0.f ? 1.f : 0.f;
     if (act == SDM_ACT_SILU) {
-        const float p = 1.f / (1.f + expf(-z));
+        const float p = __fdividef(1.f, 1.f + __expf(-z));
         return p * (1.f + z * (1.f - p));
     }
     if (act == SDM_ACT_GELU)
@@ -77,8 +77,13 @@ __device__ __forceinline__ float act_slope(float z, int act) {
     return 1.f;
 }
 
+// Eight values of the residual; it may be the output buffer (read by the thread that overwrites it), so
+// not through the read-only path.
+__device__ __forceinline__ uint4 residual8(const LinearOut& o, int64_t at) {
+    return *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(o.residual) + at);
+}
 // Epilogue of eight neighbouring columns of one row: bias, pre-activation, activation, residual.
-__device__ __forceinline__ void finish8(float (&v)[8], const LinearOut& o, int64_t at, int n) {
+__device__ __forceinline__ void finish8(float (&v)[8], const LinearOut& o, int64_t at, int n, const uint4& res) {
     if (o.bias != nullptr) {
         const float4 b0 = __ldg(reinterpret_cast<const float4*>(o.bias + n)), b1 = __ldg(reinterpret_cast<const float4*>(o.bias + n) + 1);
         v[0] += b0.x; v[1] += b0.y; v[2] += b0.z; v[3] += b0.w;
@@ -90,10 +95,8 @@ __device__ __forceinline__ void finish8(float (&v)[8], const LinearOut& o, int64
         for (int i = 0; i < 8; ++i) v[i] = act_fwd(v[i], o.act);
     }
     if (o.residual != nullptr) {
-        // the residual may be the output buffer: read by the thread that overwrites it, so not through
-        // the read-only path
         float r[8];
-        unpack16<BF16>(*reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(o.residual) + at), r);
+        unpack16<BF16>(res, r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += r[i];
     }
@@ -192,29 +195,42 @@ __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtens
             if (ok) mma_commit(afull + 8 * (n & 1));
         }
     } else if (warp >= 2) {                            // epilogue: TMEM lanes of this warp's quadrant
-        const int quad = warp & 3, lane = tid & 31;
+        const int quad = warp & 3, part_of = (warp - 2) >> 2, lane = tid & 31;
         uint32_t n = 0;
         for (int w = blockIdx.x; w < items && ok; w += gridDim.x, ++n) {
             const int sp = w % g.splits, tile = w / g.splits;
             const int n0 = (tile % g.ntn) * BN;
             const int64_t row = static_cast<int64_t>(tile / g.ntn) * BM + quad * 32 + lane;
+            constexpr int BLOCKS = BN / 64;                // blocks of 32 columns of this warp
+            const int c0 = part_of * (BN / 2);
+            const uint32_t src = tmem + (n & 1) * BN + c0 + (static_cast<uint32_t>(quad * 32) << 16);
+            const bool res = o.residual != nullptr && part == nullptr && row < g.M;
+            uint4 r[2][4];                                 // the residual, one block ahead
+            auto fetch = [&](int cb, uint4 (&to)[4]) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int col = n0 + c0 + cb * 32 + q * 8;
+                    to[q] = res && col < g.N ? residual8(o, row * g.N + col) : make_uint4(0, 0, 0, 0);
+                }
+            };
+            fetch(0, r[0]);
             ok = __all_sync(0xffffffffu, mbar_wait(afull + 8 * (n & 1), (n >> 1) & 1));
             if (!ok) break;
-            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-            const uint32_t src = tmem + (n & 1) * BN + (static_cast<uint32_t>(quad * 32) << 16);
-#pragma unroll 1
-            for (int cb = 0; cb < BN / 32; ++cb) {
+            tc_after_sync();
+#pragma unroll
+            for (int cb = 0; cb < BLOCKS; ++cb) {
+                if (cb + 1 < BLOCKS) fetch(cb + 1, r[(cb + 1) & 1]);
                 float v[32];
                 tmem_ld32(src + cb * 32, v);
-                if (cb == BN / 32 - 1) {
-                    asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+                if (cb == BLOCKS - 1) {
+                    tc_before_sync();
                     mbar_arrive(aempty + 8 * (n & 1));
                 }
                 if (row < g.M) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const int col = n0 + cb * 32 + q * 8;
-                        if (col < g.N) {               // N is a multiple of 8
+                        const int col = n0 + c0 + cb * 32 + q * 8;
+                        if (col < g.N) {                   // N is a multiple of 8
                             float f[8];
 #pragma unroll
                             for (int e = 0; e < 8; ++e) f[e] = v[q * 8 + e];
@@ -224,7 +240,7 @@ __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtens
                                 dst[0] = make_float4(f[0], f[1], f[2], f[3]);
                                 dst[1] = make_float4(f[4], f[5], f[6], f[7]);
                             } else {
-                                finish8(f, o, at, col);
+                                finish8(f, o, at, col, r[cb & 1][q]);
                             }
                         }
                     }
@@ -249,7 +265,8 @@ __global__ void __launch_bounds__(256) k_linear_join(const float* __restrict__ p
         v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
         v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
     }
-    finish8(v, o, i, static_cast<int>(i % N));
+    const uint4 r = o.residual != nullptr ? residual8(o, i) : make_uint4(0, 0, 0, 0);
+    finish8(v, o, i, static_cast<int>(i % N), r);
 }
 
 // Up to MR rows of x: a warp owns two rows of W (output columns), its lanes take 16-byte pieces of
@@ -330,22 +347,33 @@ __global__ void __launch_bounds__(256) k_linear_dact(const __nv_bfloat16* __rest
     const int64_t r0 = static_cast<int64_t>(blockIdx.y) * DA_ROWS;
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (col < N) {
-#pragma unroll 2
-        for (int j = 0; j < DA_ROWS / 32; ++j) {
-            const int64_t row = r0 + j * 32 + y;
-            if (row >= M) break;
-            const int64_t at = row * N + col;
-            float d[8];
-            unpack16<BF16>(__ldg(reinterpret_cast<const uint4*>(dout + at)), d);
-            if (act != SDM_ACT_NONE) {
-                float z[8];
-                unpack16<BF16>(__ldg(reinterpret_cast<const uint4*>(pre + at)), z);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d[e] *= act_slope(z[e], act);
+        for (int jj = 0; jj < DA_ROWS / 32; jj += 4) {
+            uint4 du[4], zu[4];                            // four rows of loads in flight
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t row = r0 + (jj + j) * 32 + y;
+                du[j] = zu[j] = make_uint4(0, 0, 0, 0);
+                if (row < M) {
+                    du[j] = __ldcs(reinterpret_cast<const uint4*>(dout + row * N + col));
+                    if (act != SDM_ACT_NONE) zu[j] = __ldcs(reinterpret_cast<const uint4*>(pre + row * N + col));
+                }
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] += d[e];
-            if (dp != nullptr) *reinterpret_cast<uint4*>(dp + at) = pack16<BF16>(d);
+            for (int j = 0; j < 4; ++j) {
+                const int64_t row = r0 + (jj + j) * 32 + y;
+                if (row >= M) break;
+                float d[8], z[8];
+                unpack16<BF16>(du[j], d);
+                if (act != SDM_ACT_NONE) {
+                    unpack16<BF16>(zu[j], z);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) d[e] *= act_slope(z[e], act);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] += d[e];
+                if (dp != nullptr) *reinterpret_cast<uint4*>(dp + row * N + col) = pack16<BF16>(d);
+            }
         }
     }
     if (part == nullptr) return;
