@@ -189,15 +189,30 @@ def _ptr(x):
         return x
     if not x.is_contiguous():
         raise ValueError("tensors passed to libsdm must be contiguous")
-    if x.device.type != "cuda":
+    if not x.is_cuda:
         raise ValueError("tensors passed to libsdm must live on a CUDA device")
     return x.data_ptr()
 
 
+_raw_stream = None
+
+
+def _raw_stream_function():
+    """The current stream's handle: torch's own accessor where it has one (no Stream object is made)."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    torch.cuda.current_stream()                 # initialises CUDA, or raises
+    if raw is None:
+        return lambda: torch.cuda.current_stream().cuda_stream
+    return lambda: raw(torch.cuda.current_device())
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        global _raw_stream
+        if _raw_stream is None:
+            _raw_stream = _raw_stream_function()
+        return _raw_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

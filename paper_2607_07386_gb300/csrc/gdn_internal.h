@@ -2,6 +2,8 @@
 #pragma once
 #include "sdm_internal.h"
 
+#include <atomic>
+
 namespace sdm {
 
 // Tokens per chunk of the saved states: the fp32 kernels and the tensor-core kernels.
@@ -37,6 +39,21 @@ __device__ __forceinline__ int gdn_length(const GdnArgs& a, int b) {
         return n < 0 ? 0 : a.T;
     }
     return n;
+}
+
+// Dynamic shared memory above 48 KB has to be allowed once per kernel and device; the call costs about
+// as much as a launch, so it is not repeated.
+template <class K>
+inline cudaError_t allow_smem(K kernel, size_t bytes, std::atomic<unsigned long long>& seen) {
+    if (bytes <= 48 * 1024) return cudaSuccess;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+    if (bit & seen.load(std::memory_order_acquire)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    if (e == cudaSuccess) seen.fetch_or(bit, std::memory_order_release);
+    return e;
 }
 
 // ---- token recurrence (k_gdn_recur.cu) ----

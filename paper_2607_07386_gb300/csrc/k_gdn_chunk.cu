@@ -681,7 +681,8 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
 template <int DK>
 cudaError_t factors(const CUtensorMap& tk, const CUtensorMap& tq, const GdnArgs& a, const GdnFactors& f, cudaStream_t stream) {
     constexpr size_t smem = FactorSize<DK>::BYTES;
-    cudaError_t e = cudaFuncSetAttribute(k_gdn_factors<DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    static std::atomic<unsigned long long> seen;
+    cudaError_t e = allow_smem(k_gdn_factors<DK>, smem, seen);
     if (e != cudaSuccess) return e;
     k_gdn_factors<DK><<<dim3((a.T + C - 1) / C, a.H, a.B), FT, smem, stream>>>(tk, tq, a, f);
     return cudaGetLastError();
@@ -692,11 +693,13 @@ cudaError_t scan(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap
                  const GdnFactors& f, cudaStream_t stream) {
     constexpr size_t smem = scan_smem<DK>();
     // the compute warpgroups' registers come out of what the CTA is launched with
-    cudaFuncAttributes at;
-    cudaError_t e = cudaFuncGetAttributes(&at, k_gdn_scan<DK>);
-    if (e != cudaSuccess) return e;
-    if (at.numRegs * ST < 32 * (SW * SCAN_REGS + OW * OUT_REGS + 4 * IDLE_REGS)) return cudaErrorInvalidConfiguration;
-    e = cudaFuncSetAttribute(k_gdn_scan<DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    static const int regs = [] {
+        cudaFuncAttributes at;
+        return cudaFuncGetAttributes(&at, k_gdn_scan<DK>) == cudaSuccess ? at.numRegs : 0;
+    }();
+    if (regs * ST < 32 * (SW * SCAN_REGS + OW * OUT_REGS + 4 * IDLE_REGS)) return cudaErrorInvalidConfiguration;
+    static std::atomic<unsigned long long> seen;
+    cudaError_t e = allow_smem(k_gdn_scan<DK>, smem, seen);
     if (e != cudaSuccess) return e;
     k_gdn_scan<DK><<<dim3((s.a.dv + 127) / 128, s.a.H, s.a.B), ST, smem, stream>>>(tk, tq, tv, ty, tm, s, f, (s.a.T + C - 1) / C);
     return cudaGetLastError();

@@ -267,7 +267,8 @@ __global__ void __launch_bounds__(NT) k_gdn_grads(const GdnGrads r) {
 template <class D, int DKP>
 cudaError_t launch_one(const GdnGrads& g, cudaStream_t stream) {
     const size_t smem = sizeof(Smem<DKP>);
-    cudaError_t e = cudaFuncSetAttribute(k_gdn_grads<D, DKP>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    static std::atomic<unsigned long long> seen;
+    cudaError_t e = allow_smem(k_gdn_grads<D, DKP>, smem, seen);
     if (e != cudaSuccess) return e;
     const dim3 grid((g.a.T + C - 1) / C, g.a.Hk, g.a.B);
     k_gdn_grads<D, DKP><<<grid, NT, smem, stream>>>(g);

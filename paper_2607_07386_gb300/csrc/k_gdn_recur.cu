@@ -186,6 +186,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS) k_gdn_recur(const GdnRecur r) 
         }
     };
     const int nc = (a.T + GDN_C32 - 1) / GDN_C32;
+    constexpr int UN = Q <= 2 ? 4 : 2;
     auto block_of = [&](int i) { return MODE == 2 ? nblk - 1 - i : i; };
     if (nblk > 0) stage(block_of(0), 0);
     for (int i = 0; i < nblk; ++i) {
@@ -197,9 +198,8 @@ __global__ void __launch_bounds__(32 * MAX_WARPS) k_gdn_recur(const GdnRecur r) 
         if (MODE == 1 && t0 % GDN_C32 == 0) save(r.marks + (chain * nc + t0 / GDN_C32) * per);
         if (MODE == 2 && (t0 + cnt == n || (t0 + TB) % GDN_C32 == 0))
             save(r.marks + (chain * nc + t0 / GDN_C32) * per);
-#pragma unroll 1
-        for (int u = 0; u < cnt; ++u) {
-            const int j = MODE == 2 ? cnt - 1 - u : u, t = t0 + j;
+        auto token = [&](int j) {
+            const int t = t0 + j;
             const float al = sm.a[buf][j], be = sm.b[buf][j];
             float2 va, vb2;
             quad<D>(&sm.v[buf][j][warp * 16 + c4], va, vb2);
@@ -287,6 +287,14 @@ __global__ void __launch_bounds__(32 * MAX_WARPS) k_gdn_recur(const GdnRecur r) 
                     if (live && g == 0) put4<D>(y + vb + t * vs + col, o);
                 }
             }
+        };
+        // whole blocks unrolled, so that the next tokens' reads and this one's output leave the chain
+        if (cnt == TB) {
+#pragma unroll UN
+            for (int u = 0; u < TB; ++u) token(MODE == 2 ? TB - 1 - u : u);
+        } else {
+#pragma unroll 1
+            for (int u = 0; u < cnt; ++u) token(MODE == 2 ? cnt - 1 - u : u);
         }
     }
     if (MODE == 0 && n > 0) save(r.state + soff);
@@ -296,8 +304,9 @@ __global__ void __launch_bounds__(32 * MAX_WARPS) k_gdn_recur(const GdnRecur r) 
 template <class D, int Q>
 cudaError_t launch_mode(int mode, const GdnRecur& r, dim3 grid, int threads, cudaStream_t stream) {
     const size_t smem = sizeof(Smem<D, Q>);
+    static std::atomic<unsigned long long> seen[3];
     auto go = [&](auto kern) {
-        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+        cudaError_t e = allow_smem(kern, smem, seen[mode]);
         if (e != cudaSuccess) return e;
         kern<<<grid, threads, smem, stream>>>(r);
         return cudaGetLastError();
@@ -322,7 +331,9 @@ cudaError_t launch_gdn_recur(int dtype, int mode, const GdnRecur& r, cudaStream_
     // The warps of a CTA share the staged keys; few chains are spread over more, smaller CTAs so
     // that every SM has one.
     const int warps = (a.dv + 15) / 16;
-    int per = warps < MAX_WARPS ? warps : MAX_WARPS;
+    // One token is all loads and stores: small CTAs, many to an SM, keep both going.
+    const int most = a.T == 1 ? 2 : MAX_WARPS;
+    int per = warps < most ? warps : most;
     while (per > 1 && static_cast<int64_t>(a.B) * a.H * ((warps + per - 1) / per) < 152) per = (per + 1) / 2;
     const dim3 grid((warps + per - 1) / per, a.H, a.B);
     return dtype == SDM_F32 ? launch_rows<F32>(mode, r, grid, 32 * per, stream)

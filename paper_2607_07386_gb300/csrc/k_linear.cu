@@ -405,7 +405,8 @@ template <int BN, bool AMN, bool BMN>
 cudaError_t launch_tiles(const CUtensorMap& ta, const CUtensorMap& tb, const LinearGeom& g, const LinearOut& o, float* part,
                          int* err, cudaStream_t stream) {
     constexpr uint32_t smem = smem_bytes(BN);
-    cudaError_t e = cudaFuncSetAttribute(k_linear<BN, AMN, BMN>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    static std::atomic<unsigned long long> seen;
+    cudaError_t e = allow_smem(k_linear<BN, AMN, BMN>, smem, seen);
     if (e != cudaSuccess) return e;
     const int64_t items = static_cast<int64_t>(g.ntm) * g.ntn * g.splits;
     k_linear<BN, AMN, BMN><<<static_cast<unsigned>(items < SMS ? items : SMS), LT, smem, stream>>>(ta, tb, g, o, part, err);
@@ -472,9 +473,10 @@ cudaError_t launch_linear(const void* A, bool a_mn, const void* B, bool b_mn, in
 
 cudaError_t launch_linear_skinny(const void* x, const void* W, int M, int N, int K, const LinearOut& o, cudaStream_t stream) {
     const unsigned grid = static_cast<unsigned>((N + 15) / 16);
+    static std::atomic<unsigned long long> seen;                // only the widest form needs more than 48 KB
     auto go = [&](auto kern, int mr) {
         const size_t smem = static_cast<size_t>(mr) * SKINNY_KT * 2;
-        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+        cudaError_t e = allow_smem(kern, smem, seen);
         if (e != cudaSuccess) return e;
         kern<<<grid, 256, smem, stream>>>(static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(W), M, N, K, o);
         return cudaGetLastError();
