@@ -62,7 +62,7 @@ struct GdnRecur {
     float* state;             // forward: [slots, H, dk, dv], updated in place (nullptr: see state_in)
     const float* state_in;    // forward with saved states: the initial state (left as it is);
                               // reverse: dL/dS_T or nullptr (zero)
-    const int32_t* slots;     // [B] row of `state` of each sequence, or nullptr (row b)
+    const int32_t* slots;     // T = 1: [B] row of `state` of each sequence, or nullptr (row b)
     int n_slots;
     void* y;                  // forward: y; reverse: dv
     const void* dy;           // reverse

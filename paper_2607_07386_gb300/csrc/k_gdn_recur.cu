@@ -11,8 +11,8 @@
 // three butterfly steps over the groups.  Blocks of TB tokens of q, k and v come through a
 // double-buffered cp.async ring shared by the warps of the CTA.
 //
-// One token (T = 1) is bound by the state's two trips through HBM: every thread has its whole
-// slice of loads in flight at once.  Long calls are bound by the instructions of the chain.
+// Long calls are bound by the instructions of the chain.  A single token has a kernel of its own,
+// k_gdn_step, below.
 #include "gdn_internal.h"
 
 namespace sdm {
@@ -101,23 +101,14 @@ __global__ void __launch_bounds__(32 * MAX_WARPS) k_gdn_recur(const GdnRecur r) 
     const int64_t kb = gdn_base(a.token_major, b, hk, a.Hk, a.T, a.dk), ks = gdn_stride(a.token_major, a.Hk, a.dk);
     T* y = static_cast<T*>(r.y);
 
-    // where this chain's state lives
-    int64_t row = b;
-    bool skip = false;
-    if (MODE == 0 && r.slots != nullptr) {
-        row = __ldg(r.slots + b);
-        skip = row < 0 || row >= r.n_slots;
-        if (row >= r.n_slots && threadIdx.x == 0) flag_error(a.err, ERR_BAD_INDEX);
-    }
     const int64_t per = static_cast<int64_t>(a.dk) * a.dv;
-    const int64_t soff = (row * a.H + h) * per;
+    const int64_t soff = chain * per;
 
-    const int n = skip ? 0 : len;
+    const int n = len;
     if (MODE != 1 && live && g == 0) {                            // tokens past the length
         const float z[4] = {0.f, 0.f, 0.f, 0.f};
         for (int t = n; t < a.T; ++t) put4<D>(y + vb + t * vs + col, z);
     }
-    if (skip) return;
 
     float2 S[2 * Q][4];      // [row pair][column]: rows 4 (8 i + g) + 2 p, + 1 for pair 2 i + p
     {
@@ -301,6 +292,100 @@ __global__ void __launch_bounds__(32 * MAX_WARPS) k_gdn_recur(const GdnRecur r) 
     if (MODE == 2 && r.state_out != nullptr) save(r.state_out + chain * per);
 }
 
+// One token: the state's two trips through HBM are all that counts.  A CTA takes 32 columns of one state,
+// a warp 32 rows of them, a lane 8 rows x 4 columns (a warp's load is four whole 128-byte row pieces), all
+// in flight before anything is waited for but the slot.  Sums over d_k: two butterfly steps, then the warps'
+// shares through shared memory.  At B = 256, H = 16, d_k = d_v = 128 the kernel above, with its staging and
+// 1,420 instructions a warp, took 145 us for 541 MB.
+template <class D>
+__device__ __forceinline__ void load8(const void* base, int64_t at, int left, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; i += D::E) {
+        const uint4 u = left > i ? __ldg(reinterpret_cast<const uint4*>(static_cast<const typename D::T*>(base) + at + i)) : make_uint4(0, 0, 0, 0);
+        unpack16<D>(u, f + i);
+    }
+}
+template <class D> __device__ __forceinline__ void load4(const void* base, int64_t at, float (&f)[4]);
+template <> __device__ __forceinline__ void load4<F32>(const void* base, int64_t at, float (&f)[4]) {
+    const float4 u = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(base) + at));
+    f[0] = u.x; f[1] = u.y; f[2] = u.z; f[3] = u.w;
+}
+template <> __device__ __forceinline__ void load4<BF16>(const void* base, int64_t at, float (&f)[4]) {
+    const uint2 u = __ldg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(base) + at));
+    f[0] = __uint_as_float(u.x << 16); f[1] = __uint_as_float(u.x & 0xffff0000u);
+    f[2] = __uint_as_float(u.y << 16); f[3] = __uint_as_float(u.y & 0xffff0000u);
+}
+
+// Sum over the rows of the CTA of four columns per lane; `sh`: [warps][32 columns].
+__device__ __forceinline__ void sum_rows(float (&f)[4], float (*sh)[32], int warp, int warps, int lane) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        f[c] += __shfl_xor_sync(0xffffffffu, f[c], 8);
+        f[c] += __shfl_xor_sync(0xffffffffu, f[c], 16);
+    }
+    if (warps == 1) return;
+    float4* const at = reinterpret_cast<float4*>(&sh[0][4 * (lane & 7)]);
+    if (lane < 8) at[warp * 8] = make_float4(f[0], f[1], f[2], f[3]);
+    __syncthreads();
+    f[0] = f[1] = f[2] = f[3] = 0.f;
+    for (int w = 0; w < warps; ++w) {
+        const float4 o = at[w * 8];
+        f[0] += o.x; f[1] += o.y; f[2] += o.z; f[3] += o.w;
+    }
+}
+
+template <class D>
+__global__ void __launch_bounds__(256) k_gdn_step(const GdnRecur r) {
+    __shared__ __align__(16) float sh[2][8][32];
+    const GdnArgs& a = r.a;
+    const int b = blockIdx.z, h = blockIdx.y, hk = h / (a.H / a.Hk);
+    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+    const int row0 = 32 * warp + 8 * (lane >> 3), col = 32 * blockIdx.x + 4 * (lane & 7);
+    const bool live = col < a.dv;                                // d_v is a multiple of 4
+    int64_t slot = b;
+    bool skip = gdn_length(a, b) == 0;
+    if (r.slots != nullptr) {
+        slot = __ldg(r.slots + b);
+        if (slot >= r.n_slots && threadIdx.x == 0) flag_error(a.err, ERR_BAD_INDEX);
+        skip = skip || slot < 0 || slot >= r.n_slots;
+    }
+    // with one token the two layouts are the same
+    const int64_t chain = static_cast<int64_t>(b) * a.H + h, kb = (static_cast<int64_t>(b) * a.Hk + hk) * a.dk;
+    float* const st = r.state + (slot * a.H + h) * a.dk * a.dv + col;
+    const int left = a.dk - row0;                                // rows of this lane: 8, 4 or none of d_k's end
+    float4 S[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        S[i] = !skip && live && i < left ? __ldcs(reinterpret_cast<const float4*>(st + static_cast<int64_t>(row0 + i) * a.dv)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    float k[8], q[8], v[4] = {0.f, 0.f, 0.f, 0.f};
+    load8<D>(a.k, kb + row0, left, k);
+    load8<D>(a.q, kb + row0, left, q);
+    if (live) load4<D>(a.v, chain * a.dv + col, v);
+    const float al = load_elem<D>(a.alpha, chain), be = load_elem<D>(a.beta, chain);
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        s[0] = fmaf(k[i], S[i].x, s[0]); s[1] = fmaf(k[i], S[i].y, s[1]);
+        s[2] = fmaf(k[i], S[i].z, s[2]); s[3] = fmaf(k[i], S[i].w, s[3]);
+    }
+    sum_rows(s, sh[0], warp, warps, lane);
+    float w[4], o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) w[c] = be * (v[c] - al * s[c]);  // beta e
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        S[i].x = fmaf(k[i], w[0], al * S[i].x); S[i].y = fmaf(k[i], w[1], al * S[i].y);
+        S[i].z = fmaf(k[i], w[2], al * S[i].z); S[i].w = fmaf(k[i], w[3], al * S[i].w);
+        if (!skip && live && i < left) __stcs(reinterpret_cast<float4*>(st + static_cast<int64_t>(row0 + i) * a.dv), S[i]);
+        o[0] = fmaf(q[i], S[i].x, o[0]); o[1] = fmaf(q[i], S[i].y, o[1]);
+        o[2] = fmaf(q[i], S[i].z, o[2]); o[3] = fmaf(q[i], S[i].w, o[3]);
+    }
+    sum_rows(o, sh[1], warp, warps, lane);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] = skip ? 0.f : a.scale * o[c];
+    if (warp == 0 && lane < 8 && live) put4<D>(static_cast<typename D::T*>(r.y) + chain * a.dv + col, o);
+}
+
 template <class D, int Q>
 cudaError_t launch_mode(int mode, const GdnRecur& r, dim3 grid, int threads, cudaStream_t stream) {
     const size_t smem = sizeof(Smem<D, Q>);
@@ -328,12 +413,17 @@ cudaError_t launch_rows(int mode, const GdnRecur& r, dim3 grid, int threads, cud
 
 cudaError_t launch_gdn_recur(int dtype, int mode, const GdnRecur& r, cudaStream_t stream) {
     const GdnArgs& a = r.a;
+    if (mode == 0 && a.T == 1) {
+        const dim3 grid((a.dv + 31) / 32, a.H, a.B);
+        const int threads = 32 * ((a.dk + 31) / 32);
+        if (dtype == SDM_F32) k_gdn_step<F32><<<grid, threads, 0, stream>>>(r);
+        else k_gdn_step<BF16><<<grid, threads, 0, stream>>>(r);
+        return cudaGetLastError();
+    }
     // The warps of a CTA share the staged keys; few chains are spread over more, smaller CTAs so
     // that every SM has one.
     const int warps = (a.dv + 15) / 16;
-    // One token is all loads and stores: small CTAs, many to an SM, keep both going.
-    const int most = a.T == 1 ? 2 : MAX_WARPS;
-    int per = warps < most ? warps : most;
+    int per = warps < MAX_WARPS ? warps : MAX_WARPS;
     while (per > 1 && static_cast<int64_t>(a.B) * a.H * ((warps + per - 1) / per) < 152) per = (per + 1) / 2;
     const dim3 grid((warps + per - 1) / per, a.H, a.B);
     return dtype == SDM_F32 ? launch_rows<F32>(mode, r, grid, 32 * per, stream)

@@ -270,8 +270,9 @@ __global__ void __launch_bounds__(256) k_linear_join(const float* __restrict__ p
 }
 
 // Up to MR rows of x: a warp owns two rows of W (output columns), its lanes take 16-byte pieces of
-// the contraction.  x is staged in shared memory, KT columns at a time.
-constexpr int SKINNY_KT = 2048;
+// the contraction, eight of them in flight, the first before x is staged in shared memory (KT columns at a
+// time).
+constexpr int SKINNY_KT = 2048, SKINNY_U = 4;
 template <int MR>
 __global__ void __launch_bounds__(256) k_linear_skinny(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ W,
                                                        int M, int N, int K, const LinearOut o) {
@@ -279,9 +280,20 @@ __global__ void __launch_bounds__(256) k_linear_skinny(const __nv_bfloat16* __re
     __nv_bfloat16* xs = reinterpret_cast<__nv_bfloat16*>(raw);          // [MR][KT]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int n0 = (blockIdx.x * 8 + warp) * 2;
+    const bool live = n0 < N;                               // N is even
+    const __nv_bfloat16* const w0 = W + static_cast<int64_t>(live ? n0 : 0) * K;
     float acc[2][MR];
 #pragma unroll
     for (int m = 0; m < MR; ++m) acc[0][m] = acc[1][m] = 0.f;
+    uint4 wv[SKINNY_U][2];
+    auto fetch = [&](int c) {                               // columns c + 256 u of W
+#pragma unroll
+        for (int u = 0; u < SKINNY_U; ++u)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                wv[u][j] = live && c + 256 * u < K ? __ldcs(reinterpret_cast<const uint4*>(w0 + static_cast<int64_t>(j) * K + c + 256 * u)) : make_uint4(0, 0, 0, 0);
+    };
+    fetch(lane * 8);
     for (int k0 = 0; k0 < K; k0 += SKINNY_KT) {
         const int kt = K - k0 < SKINNY_KT ? K - k0 : SKINNY_KT;
         __syncthreads();
@@ -291,21 +303,24 @@ __global__ void __launch_bounds__(256) k_linear_skinny(const __nv_bfloat16* __re
                 m < M ? __ldg(reinterpret_cast<const uint4*>(x + static_cast<int64_t>(m) * K + k0 + c)) : make_uint4(0, 0, 0, 0);
         }
         __syncthreads();
-        if (n0 < N) {                                   // N is even
-#pragma unroll 2
-            for (int c = lane * 8; c < kt; c += 256) {
-                float w[2][8];
+        for (int c = lane * 8; c < kt; c += 256 * SKINNY_U) {
+            float w[SKINNY_U][2][8];
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    unpack16<BF16>(__ldcs(reinterpret_cast<const uint4*>(W + static_cast<int64_t>(n0 + j) * K + k0 + c)), w[j]);
+            for (int u = 0; u < SKINNY_U; ++u)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) unpack16<BF16>(wv[u][j], w[u][j]);
+            fetch(k0 + c + 256 * SKINNY_U);
+#pragma unroll
+            for (int u = 0; u < SKINNY_U; ++u) {
+                if (c + 256 * u >= kt) break;
 #pragma unroll
                 for (int m = 0; m < MR; ++m) {
                     float f[8];
-                    unpack16<BF16>(*reinterpret_cast<const uint4*>(xs + m * SKINNY_KT + c), f);
+                    unpack16<BF16>(*reinterpret_cast<const uint4*>(xs + m * SKINNY_KT + c + 256 * u), f);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        acc[0][m] = fmaf(f[e], w[0][e], acc[0][m]);
-                        acc[1][m] = fmaf(f[e], w[1][e], acc[1][m]);
+                        acc[0][m] = fmaf(f[e], w[u][0][e], acc[0][m]);
+                        acc[1][m] = fmaf(f[e], w[u][1][e], acc[1][m]);
                     }
                 }
             }
@@ -319,7 +334,7 @@ __global__ void __launch_bounds__(256) k_linear_skinny(const __nv_bfloat16* __re
             acc[1][m] += __shfl_xor_sync(0xffffffffu, acc[1][m], s);
         }
     }
-    if (n0 >= N) return;
+    if (!live) return;
 #pragma unroll
     for (int m = 0; m < MR; ++m) {
         if (m < M && lane < 2) {
