@@ -122,7 +122,7 @@ FwdLayout fwd_layout(const sdm_gdn_shape* s) {
     FwdLayout L{};
     if (!sdm::gdn_chunk_supported(s->dtype, s->d_k, s->T)) return L;
     const int64_t chunks = static_cast<int64_t>(s->B) * s->H * ((s->T + sdm::GDN_C64 - 1) / sdm::GDN_C64);
-    L.gates = align256(sdm::gdn_factor_mat_bytes(chunks));
+    L.gates = align256(sdm::gdn_factor_mat_bytes(chunks, 3));
     L.total = L.gates + align256(sdm::gdn_factor_gate_bytes(chunks));
     return L;
 }
@@ -211,9 +211,9 @@ sdm_status sdm_gdn_forward(const sdm_gdn_shape* s, const void* q, const void* k,
     if (L.total > 0) {
         cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
         char* ws = static_cast<char*>(workspace);
-        const sdm::GdnFactors f{ws + L.mat, reinterpret_cast<float*>(ws + L.gates)};
+        const sdm::GdnFactors f{ws + L.mat, 3, reinterpret_cast<float*>(ws + L.gates)};
         cudaError_t e = sdm::launch_gdn_factors(a, f, st);
-        if (e == cudaSuccess) e = sdm::launch_gdn_scan(sdm::GdnScan{a, state, y}, f, st);
+        if (e == cudaSuccess) e = sdm::launch_gdn_scan(sdm::GdnScan{a, state, y, nullptr, nullptr, nullptr}, f, st);
         return done(e, "sdm_gdn_forward");
     }
     sdm::GdnRecur r{};

@@ -85,13 +85,14 @@ struct GdnGrads {
 cudaError_t launch_gdn_grads(int dtype, const GdnGrads& g, cudaStream_t stream);
 
 // ---- chunked form on the tensor cores (k_gdn_chunk.cu): bf16, d_k <= 128, chunks of 64 ----
-// What the chunks' own products are, per (sequence, head, chunk): three bf16 matrices [64][64] (the
-// inverse's upper and lower parts, the masked read products) and three rows of 64 floats.
+// What the chunks' own products are, per (sequence, head, chunk): three or four bf16 matrices [64][64]
+// (N as upper and lower parts, P and, for the backward, P's lower part) and three rows of 64 floats.
 struct GdnFactors {
-    void* mat;                // [B, H, nc, 3, 64, 64] bf16
+    void* mat;                // [B, H, nc, mats, 64, 64] bf16
+    int mats;
     float* gates;             // [B, H, nc, 3, 64]: prod_{l <= i} alpha_l, beta_i, prod_{l > i} alpha_l
 };
-size_t gdn_factor_mat_bytes(int64_t chunks);
+size_t gdn_factor_mat_bytes(int64_t chunks, int mats);
 size_t gdn_factor_gate_bytes(int64_t chunks);
 bool gdn_chunk_supported(int dtype, int dk, int T);
 cudaError_t launch_gdn_factors(const GdnArgs& a, const GdnFactors& f, cudaStream_t stream);
@@ -99,6 +100,10 @@ struct GdnScan {
     GdnArgs a;
     float* state;             // [B, H, dk, dv], updated in place
     void* y;
+    const float* state_in;    // with keep_S: the first state, left as it is
+    void* keep_S;             // [B, H, nc, dv', dk'] bf16: the states before the chunks, transposed, or nullptr
+                              // (dv': d_v rounded up to 128, dk': d_k to 64 or 128)
+    void* keep_e;             // [B, H, nc, 2, dv', 64] bf16: e as upper and lower parts, transposed
 };
 cudaError_t launch_gdn_scan(const GdnScan& s, const GdnFactors& f, cudaStream_t stream);
 

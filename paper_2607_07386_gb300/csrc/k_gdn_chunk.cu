@@ -2,76 +2,35 @@
 //
 // With the decay products of a chunk, G_ij = prod_{j < l <= i} alpha_l, g_i = prod_{l <= i} alpha_l and
 // h_j = prod_{l > j} alpha_l, and the state S before it,
-//   L_ij = beta_i G_ij k_i.k_j (j < i),  Z = (I + L)^-1,  P_ij = G_ij q_i.k_j (j <= i),
-//   w = Z (beta (v - g K S)),   y = scale (g Q S + P w),   S' = h_0.. : g_63 S + K^T (h w).
-// k_gdn_factors computes Z, P and the gate products of every chunk at once; k_gdn_scan then walks the
+//   B_ij = G_ij k_i.k_j (j < i),  P_ij = G_ij q_i.k_j (j <= i),  r = v - g K S,
+//   e = (I + B beta)^-1 r = r + N (beta r),  N = -(I + B beta)^-1 B,  w = beta e,
+//   y = scale (g Q S + P w),   S' = g_63 S + K^T (h w).
+// k_gdn_factors computes N, P and the gate products of every chunk at once; k_gdn_scan then walks the
 // chunks of one (sequence, head, 128 columns of the state).  The products G are products of gates,
-// never quotients or exponentials of sums, so a gate of zero is exact.
+// never quotients or exponentials of sums, and N does not divide by beta, so gates of zero are exact.
 //
 // Precision: the state and every sum are fp32.  k and q are exact operands.  What the state depends on
-// and is not a bf16 number enters the MMAs as bf16 parts: S, Z - I and beta (v - g K S) as two (16
-// significant bits; products of two lower parts are left out), h w, whose rounding the state would
-// keep, as three.  Z's unit diagonal is taken in fp32.  y alone takes P rounded to bf16 once, as y is.
-#include "gdn_internal.h"
-#include "tc_common.cuh"
-
-#include <cuda.h>
-#include <cudaTypedefs.h>
+// and is not a bf16 number enters the MMAs as bf16 parts: S, N and beta r as two (16 significant
+// bits; products of two lower parts are left out), h w, whose rounding the state would keep, as three.
+// e takes r itself in fp32.  y alone takes P rounded to bf16 once, as y is.
+#include "gdn_tc.cuh"
 
 namespace sdm {
 
 namespace {
 
 using namespace tc;
-
-constexpr int C = GDN_C64;
-constexpr uint32_t MAT = C * C * 2;          // bytes of one [64][64] bf16 matrix
-constexpr uint32_t GATES = 3 * C * 4;
-
-PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
-    static PFN_cuTensorMapEncodeTiled_v12000 fn = []() -> PFN_cuTensorMapEncodeTiled_v12000 {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-        return nullptr;
-    }();
-    return fn;
-}
-
-// [B, heads, T, d] or [B, T, heads, d] bf16 as {d, T, heads, B}, boxes of 64 values x 64 tokens.
-bool token_map(CUtensorMap* m, const void* base, int token_major, int B, int heads, int T, int d) {
-    PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
-    if (!enc) return false;
-    const cuuint64_t row = static_cast<cuuint64_t>(d) * 2, uT = T, uH = heads;
-    cuuint64_t dim[4] = {static_cast<cuuint64_t>(d), uT, uH, static_cast<cuuint64_t>(B)};
-    cuuint64_t str[3] = {token_major ? row * uH : row, token_major ? row : row * uT, row * uH * uT};
-    cuuint32_t box[4] = {64, C, 1, 1}, es[4] = {1, 1, 1, 1};
-    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dim, str, box, es,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-// The chunks' matrices as one [chunks * 3 * 64][64] matrix, boxes of one of them.
-bool mat_map(CUtensorMap* m, const void* base, int64_t mats) {
-    PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
-    if (!enc) return false;
-    cuuint64_t dim[2] = {C, static_cast<cuuint64_t>(mats) * C};
-    cuuint64_t str[1] = {C * 2};
-    cuuint32_t box[2] = {C, C}, es[2] = {1, 1};
-    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dim, str, box, es,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
+using namespace gdn;
 
 // ------------------------------------------------------------------------------------------
 // Factors of a chunk: one CTA of 128 threads.  One MMA chain gives [K; Q] K^T (128 x 64); thread r
 // takes row r of it (k_i.k_j for r < 64, q_i.k_j above) and multiplies it by G along the row.
 //
-// Z is inverted in fp32 by blocks of 16: the diagonal blocks by a column per thread in registers, then
-// the block diagonals below in order, Z_ij = -Z_ii (sum_k L_ik Z_kj), a warp per 16 x 16 product, a lane per
-// 4 x 2 outputs (one 16-byte and one 8-byte shared-memory read per 8 multiply-adds; L and the diagonal
-// blocks lie transposed for that).  Shared-memory reads bound the kernel: with 4 x 1 outputs per thread they
+// N is solved for in fp32 by blocks of 16: the diagonal blocks by a column per thread in registers, then
+// the block diagonals below in order, with Z_ii = (I + B_ii beta)^-1 = I + N_ii beta:
+//   N_ij = -Z_ii (B_ij + sum_{j <= k < i} B_ik beta N_kj),  a warp per 16 x 16 product, a lane per
+// 4 x 2 outputs (one 16-byte and one 8-byte shared-memory read per 8 multiply-adds; B and Z_ii lie
+// transposed for that).  Shared-memory reads bound the kernel: with 4 x 1 outputs per thread they
 // kept the pipe 80% busy.  Eliminating whole columns of 64 in registers was slower still: 2016 unrolled
 // instructions, whose fetching took 11,600 of a CTA's 20,000 cycles.
 // ------------------------------------------------------------------------------------------
@@ -87,9 +46,9 @@ struct FactorSmem {
 };
 // The K and Q tiles make room for these once the MMAs have read them.
 struct FactorLate {
-    float Lt[C][C];                           // L transposed
-    float Z[C][LP];                           // below and on the diagonal
-    float Zt[C][BL];                          // diagonal blocks transposed: [16 block + column][row]
+    float Bt[C][C];                           // B transposed
+    float N[C][LP];                           // below and on the diagonal
+    float Zt[C][BL];                          // Z_ii transposed: [16 block + column][row]
     float X[NB][BL][BL + 4];
 };
 template <int DK>
@@ -98,12 +57,12 @@ struct FactorSize {
     static constexpr size_t BYTES = 1024 + TILE + sizeof(FactorSmem);
 };
 
-// acc[r][c] = sum_k At[k][4 (lane / 8) + r] B[k][2 (lane % 8) + c] over 16 k, B the sum of `terms` blocks.
-__device__ __forceinline__ void block_mul(const float* At, int lda, const float* B, int ldb, int terms, int term, float (&acc)[4][2], int lane) {
+// acc[r][c] += sum_k At[k][4 (lane / 8) + r] x_k B[k][2 (lane % 8) + c] over 16 k, B the sum of `terms`
+// blocks, x_k = 1 without `scale`.
+__device__ __forceinline__ void block_mul(const float* At, int lda, const float* B, int ldb, int terms, int term, const float* scale,
+                                          float (&acc)[4][2], int lane) {
     const float* ap = At + 4 * (lane >> 3);
     const float* bp = B + 2 * (lane & 7);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) acc[r][0] = acc[r][1] = 0.f;
 #pragma unroll 4
     for (int k = 0; k < BL; ++k) {
         const float4 a = *reinterpret_cast<const float4*>(ap + k * lda);
@@ -112,6 +71,10 @@ __device__ __forceinline__ void block_mul(const float* At, int lda, const float*
             const float2 o = *reinterpret_cast<const float2*>(bp + t * term + k * ldb);
             b.x += o.x;
             b.y += o.y;
+        }
+        if (scale != nullptr) {
+            b.x *= scale[k];
+            b.y *= scale[k];
         }
         acc[0][0] = fmaf(a.x, b.x, acc[0][0]); acc[0][1] = fmaf(a.x, b.y, acc[0][1]);
         acc[1][0] = fmaf(a.y, b.x, acc[1][0]); acc[1][1] = fmaf(a.y, b.y, acc[1][1]);
@@ -202,22 +165,24 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
         *reinterpret_cast<float2*>(gates + C + 2 * l) = make_float2(sm.be[2 * l], sm.be[2 * l + 1]);
         *reinterpret_cast<float2*>(gates + 2 * C + 2 * l) = make_float2(a1 * h1, h1);
     }
-    // row i of the decay products, from the diagonal to the left: G_ii = 1, G_i,j-1 = G_ij alpha_j (times
-    // beta_i where the row is one of L, whose diagonal is not used)
+    // row i of the decay products, from the diagonal to the left: G_ii = 1, G_i,j-1 = G_ij alpha_j (B's diagonal
+    // is not used)
     const int i = tid & 63;
     const bool isk = tid < C;
     mbar_wait_or_dead(done, 0, &sm.dead);
     __syncwarp();
     tc_after_sync();
-    const float G0 = isk ? sm.be[i] : 1.f;
     float G = 0.f;
-    uint4* const P = reinterpret_cast<uint4*>(static_cast<char*>(f.mat) + (cid * 3 + 2) * MAT + i * C * 2);
+    uint4* const P = reinterpret_cast<uint4*>(static_cast<char*>(f.mat) + (cid * f.mats + 2) * MAT + i * C * 2);
 #pragma unroll
     for (int half = 1; half >= 0; --half) {               // columns 32.. , then 0..; rows 0-31 have none of the first
         if (half == 1 && (warp & 1) == 0) {
             if (!isk) {
 #pragma unroll
-                for (int j = 4; j < 8; ++j) P[j] = make_uint4(0, 0, 0, 0);
+                for (int j = 4; j < 8; ++j) {
+                    P[j] = make_uint4(0, 0, 0, 0);
+                    if (f.mats == 4) P[MAT / 16 + j] = make_uint4(0, 0, 0, 0);
+                }
             }
             continue;
         }
@@ -230,21 +195,25 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
 #pragma unroll
             for (int e = 7; e >= 0; --e) {
                 const int j = 32 * half + 8 * q + e;
-                G = j == i ? G0 : G;
+                G = j == i ? 1.f : G;
                 x[8 * q + e] *= G;
                 G *= __uint_as_float(e & 1 ? al[e / 2] & 0xffff0000u : al[e / 2] << 16);
             }
         }
         if (isk) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) lt.Lt[32 * half + j][i] = x[j];
+            for (int j = 0; j < 32; ++j) lt.Bt[32 * half + j][i] = x[j];
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 float v[8];
+                uint32_t w[4];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = 32 * half + 8 * j + e <= i ? x[8 * j + e] : 0.f;
-                P[4 * half + j] = pack16<BF16>(v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
+                P[4 * half + j] = make_uint4(w[0], w[1], w[2], w[3]);
+                if (f.mats == 4) P[MAT / 16 + 4 * half + j] = pack16<BF16>(v);     // its lower part
             }
         }
     }
@@ -253,22 +222,26 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
         const int o = tid & ~15, c = tid & 15;
         float z[BL];
 #pragma unroll
-        for (int j = 0; j < BL; ++j) z[j] = j == c ? 1.f : 0.f;
+        for (int j = 0; j < BL; ++j) z[j] = 0.f;
 #pragma unroll
         for (int k = 0; k < BL - 1; ++k) {
+            const float y = k == c ? 1.f : sm.be[o + k] * z[k];
 #pragma unroll
             for (int q = (k + 1) / 4; q < BL / 4; ++q) {
-                const float4 l = *reinterpret_cast<const float4*>(&lt.Lt[o + k][o + 4 * q]);
-                if (4 * q > k) z[4 * q] = fmaf(-l.x, z[k], z[4 * q]);
-                if (4 * q + 1 > k) z[4 * q + 1] = fmaf(-l.y, z[k], z[4 * q + 1]);
-                if (4 * q + 2 > k) z[4 * q + 2] = fmaf(-l.z, z[k], z[4 * q + 2]);
-                z[4 * q + 3] = fmaf(-l.w, z[k], z[4 * q + 3]);
+                const float4 l = *reinterpret_cast<const float4*>(&lt.Bt[o + k][o + 4 * q]);
+                if (4 * q > k) z[4 * q] = fmaf(-l.x, y, z[4 * q]);
+                if (4 * q + 1 > k) z[4 * q + 1] = fmaf(-l.y, y, z[4 * q + 1]);
+                if (4 * q + 2 > k) z[4 * q + 2] = fmaf(-l.z, y, z[4 * q + 2]);
+                z[4 * q + 3] = fmaf(-l.w, y, z[4 * q + 3]);
             }
         }
+        const float be = sm.be[tid];
 #pragma unroll
-        for (int j = 0; j < BL; ++j) lt.Z[o + j][o + c] = z[j];
+        for (int j = 0; j < BL; ++j) lt.N[o + j][o + c] = z[j];
 #pragma unroll
-        for (int j = 0; j < BL; j += 4) *reinterpret_cast<float4*>(&lt.Zt[tid][j]) = make_float4(z[j], z[j + 1], z[j + 2], z[j + 3]);
+        for (int j = 0; j < BL; j += 4)
+            *reinterpret_cast<float4*>(&lt.Zt[tid][j]) = make_float4(j == c ? 1.f : be * z[j], j + 1 == c ? 1.f : be * z[j + 1],
+                                                                     j + 2 == c ? 1.f : be * z[j + 2], j + 3 == c ? 1.f : be * z[j + 3]);
     }
     __syncthreads();
     const int lane = tid & 31, br = 4 * (lane >> 3), bc = 2 * (lane & 7);
@@ -277,32 +250,38 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
         if (warp < (NB - d) * d) {                                            // warp: block j = warp / d, its term k = j + warp % d
             const int j = warp / d, k = j + warp % d;
             float acc[4][2];
-            block_mul(&lt.Lt[k * BL][(j + d) * BL], C, &lt.Z[k * BL][j * BL], LP, 1, 0, acc, lane);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {                                     // the term of the unit diagonal
+                const float4 x = *reinterpret_cast<const float4*>(&lt.Bt[j * BL + bc + c][(j + d) * BL + br]);
+                acc[0][c] = k == j ? x.x : 0.f; acc[1][c] = k == j ? x.y : 0.f;
+                acc[2][c] = k == j ? x.z : 0.f; acc[3][c] = k == j ? x.w : 0.f;
+            }
+            block_mul(&lt.Bt[k * BL][(j + d) * BL], C, &lt.N[k * BL][j * BL], LP, 1, 0, &sm.be[k * BL], acc, lane);
 #pragma unroll
             for (int r = 0; r < 4; ++r) *reinterpret_cast<float2*>(&lt.X[warp][br + r][bc]) = make_float2(acc[r][0], acc[r][1]);
         }
         __syncthreads();
         if (warp < NB - d) {
-            float acc[4][2];
-            block_mul(&lt.Zt[(warp + d) * BL][0], BL, &lt.X[warp * d][0][0], BL + 4, d, BL * (BL + 4), acc, lane);
+            float acc[4][2] = {};
+            block_mul(&lt.Zt[(warp + d) * BL][0], BL, &lt.X[warp * d][0][0], BL + 4, d, BL * (BL + 4), nullptr, acc, lane);
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                *reinterpret_cast<float2*>(&lt.Z[(warp + d) * BL + br + r][warp * BL + bc]) = make_float2(-acc[r][0], -acc[r][1]);
+                *reinterpret_cast<float2*>(&lt.N[(warp + d) * BL + br + r][warp * BL + bc]) = make_float2(-acc[r][0], -acc[r][1]);
         }
         __syncthreads();
     }
-    for (int p = tid; p < C * C / 8; p += FT) {                               // Z - I as upper and lower parts
+    for (int p = tid; p < C * C / 8; p += FT) {                               // N as upper and lower parts
         const int r = p / (C / 8), c = (p % (C / 8)) * 8;
         float v[8];
         uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c + e < r ? lt.Z[r][c + e] : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = c + e < r ? lt.N[r][c + e] : 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             hi[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
             lo[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
         }
-        char* dst = static_cast<char*>(f.mat) + cid * 3 * MAT + p * 16;
+        char* dst = static_cast<char*>(f.mat) + cid * f.mats * MAT + p * 16;
         *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *reinterpret_cast<uint4*>(dst + MAT) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
@@ -315,17 +294,20 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
 // ------------------------------------------------------------------------------------------
 // The walk over the chunks.  A CTA owns 128 columns of one state; everything is transposed, so that a
 // TMEM lane is a column: S^T [columns, d_k], w^T [columns, tokens] are A operands written to TMEM from
-// registers, and K, Q, Z, P are B operands as TMA leaves them in shared memory (K twice: along d_k for
+// registers, and K, Q, N, P are B operands as TMA leaves them in shared memory (K twice: along d_k for
 // K S, along the tokens for the update).  Per chunk:
 //   1  U = S^T K^T, then S^T Q^T                      (MMA; the second runs under step 2)
-//   2  R = beta (v - g U)                             (registers, bf16 parts to TMEM)
-//   3  R (Z - I)^T                                    (MMA; g Q S is taken out meanwhile)
-//   4  w = R + .., h w                                (registers, bf16 parts to TMEM)
+//   2  r = v - g U, beta r                            (registers, bf16 parts to TMEM)
+//   3  beta r N^T                                     (MMA; g Q S is taken out meanwhile)
+//   4  e = r + .., w = beta e, h w                    (registers, bf16 parts to TMEM)
 //   5  h w K, then w P^T                              (MMA)
 //   6  S = g_63 S + ..                                (registers, bf16 parts to TMEM)
 // Warps 0-7 compute: two share a lane quarter; in steps 2 and 4 each takes 32 tokens, in step 6 half of
 // d_k.  Warps 8-11 add up the outputs of a chunk beside that, in the place of its v, for TMA to store.
 // Warp 12 issues the MMAs, warp 13 the copies.
+//
+// With KEEP (for the backward) nothing is read out: the states before the chunks and e are stored instead, as
+// bf16, column by column as the threads hold them, and the state stays as it was.
 //
 // The chain of six stages is what bounds it, then the tensor pipe (2432 cycles of MMAs per chunk at d_k =
 // 128).
@@ -334,9 +316,9 @@ constexpr int SW = 8;                          // compute warps
 constexpr int OW = 4;                          // output warps
 constexpr int ST = 32 * (SW + OW + 4);
 constexpr int SCAN_REGS = 184, OUT_REGS = 104, IDLE_REGS = 40;   // the split of the launch's 128 per thread
-constexpr int NS = 2;                          // bf16 parts of S, of R and of w as the factor of P
+constexpr int NS = 2;                          // bf16 parts of S, of beta r and of w as the factor of P
 constexpr int NH = 3;                          // bf16 parts of h w
-// TMEM columns: X: steps 1, 3, 5; Y: w P^T; S; R, then w.  h w lies where S is, which steps 2 to 6 do not read.
+// TMEM columns: X: steps 1, 3, 5; Y: w P^T; S; R: beta r, then w.  h w lies where S is, which steps 2 to 6 do not read.
 constexpr uint32_t X_COL = 0, Y_COL = 128, S_COL = 192, R_COL = S_COL + 128, T_COLS = 512;
 static_assert(R_COL + 32 * NS <= T_COLS && 32 * NH <= 128 && 64 * NS <= 128, "TMEM columns");
 
@@ -346,9 +328,9 @@ struct ScanTile {
     static constexpr uint32_t LOAD = G + GATES;
     static constexpr int STAGES = 3;
 };
-// Barriers.  Completed by MMAs or copies: a stage's tile; U; Q S; R (Z - I); h w K; w P.  Completed by warps:
+// Barriers.  Completed by MMAs or copies: a stage's tile; U; Q S; beta r N; h w K; w P.  Completed by warps:
 // operands in TMEM, Q S taken out, y in shared memory.
-enum { B_FULL = 0, B_U = 3, B_QS, B_RZ, B_HK, B_WP, B_S, B_R, B_H, B_W, B_TAKEN, B_Y, B_COUNT };
+enum { B_FULL = 0, B_U = 3, B_QS, B_RN, B_HK, B_WP, B_S, B_R, B_H, B_W, B_TAKEN, B_Y, B_COUNT };
 struct ScanCtl {
     unsigned long long bar[B_COUNT];
     uint32_t tmem;
@@ -357,43 +339,7 @@ struct ScanCtl {
 template <int DK>
 constexpr size_t scan_smem() { return 1024 + ScanTile<DK>::BYTES * ScanTile<DK>::STAGES + sizeof(ScanCtl); }
 
-// The next bf16 part of 32 values into 16 packed columns; the values keep what its rounding left.
-__device__ __forceinline__ void put_part(uint32_t taddr, float (&v)[32]) {
-    uint32_t u[16];
-#pragma unroll
-    for (int j = 0; j < 16; ++j) u[j] = split2(v[2 * j], v[2 * j + 1], v[2 * j], v[2 * j + 1]);
-    tmem_st16(taddr, u);
-}
-__device__ __forceinline__ void put_last(uint32_t taddr, const float (&v)[32]) {
-    uint32_t u[16];
-#pragma unroll
-    for (int j = 0; j < 16; ++j) u[j] = pack2(v[2 * j], v[2 * j + 1]);
-    tmem_st16(taddr, u);
-}
-// 32 neighbouring floats of shared memory (16-byte aligned, the same for the whole warp).
-__device__ __forceinline__ void get32(const float* p, float (&v)[32]) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        const float4 f = *reinterpret_cast<const float4*>(p + 4 * q);
-        v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
-    }
-}
-// A warp's share of an operand is in TMEM: tells the issuing warp.
-__device__ __forceinline__ void announce(uint32_t bar, int lane) {
-    tmem_st_wait();
-    tc_before_sync();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(bar);
-}
-__device__ __forceinline__ void await(uint32_t bar, uint32_t parity, volatile int* dead) {
-    mbar_wait_or_dead(bar, parity, dead);
-    __syncwarp();
-    tc_after_sync();
-}
-// Element (row, x) of a tile of 64-value, 128-byte rows, swizzled as TMA leaves it.
-__device__ __forceinline__ uint32_t sw128_at(int row, int x) { return row * 128 + ((x * 2) ^ ((row & 7) << 4)); }
-
-template <int DK>
+template <int DK, bool KEEP>
 __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tq,
                                                     const __grid_constant__ CUtensorMap tv, const __grid_constant__ CUtensorMap ty,
                                                     const __grid_constant__ CUtensorMap tm, const GdnScan r, const GdnFactors f, int nc) {
@@ -442,12 +388,14 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                         for (int kk = 0; kk < DK / 16; ++kk)
                             mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * SB + kk * 8, dk + (kk / 4) * 1024 + (kk % 4) * 2, id64, (p | kk) != 0);
                     mma_commit(bar(B_U));
+                    if (!KEEP) {
 #pragma unroll
                     for (int p = 0; p < NS; ++p)
 #pragma unroll
                         for (int kk = 0; kk < DK / 16; ++kk)
                             mma_bf16_ta(tmem + X_COL + 64, tmem + S_COL + p * SB + kk * 8, dq + (kk / 4) * 1024 + (kk % 4) * 2, id64, (p | kk) != 0);
                     mma_commit(bar(B_QS));
+                    }
                 }
                 __syncwarp();
                 await(bar(B_R), ph, dead);
@@ -457,10 +405,10 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
                             mma_bf16_ta(tmem + X_COL, tmem + R_COL + (m == 2 ? 32 : 0) + kk * 8, dm + (m == 1 ? MAT / 16 : 0) + kk * 2, id64, (m | kk) != 0);
-                    mma_commit(bar(B_RZ));
+                    mma_commit(bar(B_RN));
                 }
                 __syncwarp();
-                await(bar(B_TAKEN), ph, dead);
+                if (!KEEP) await(bar(B_TAKEN), ph, dead);
                 await(bar(B_H), ph, dead);
                 if (elect_one()) {                           // step 5
 #pragma unroll
@@ -471,6 +419,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                     mma_commit(bar(B_HK));
                 }
                 __syncwarp();
+                if (KEEP) continue;
                 await(bar(B_W), ph, dead);
                 if (elect_one()) {
 #pragma unroll
@@ -495,14 +444,18 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 tma_load_4d(t + L::V, &tv, col0, c * C, h, b, fb);
                 tma_load_4d(t + L::V + 8192, &tv, col0 + 64, c * C, h, b, fb);
 #pragma unroll
-                for (int m = 0; m < 3; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * 3 + m) * C), fb);
+                for (int m = 0; m < 3; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * f.mats + m) * C), fb);
                 bulk_load(t + L::G, f.gates + cid * 3 * C, GATES, fb);
             };
             int loaded = 0;
             for (; loaded < chunks && loaded < L::STAGES; ++loaded) load(loaded);
             for (int c = 0; c < chunks; ++c) {
-                mbar_wait_or_dead(bar(B_Y), c & 1, dead);    // y of chunk c lies where its v was
+                mbar_wait_or_dead(bar(KEEP ? B_HK : B_Y), c & 1, dead);    // y of chunk c lies where its v was
                 if (*dead) break;
+                if (KEEP) {
+                    if (loaded < chunks) load(loaded++);
+                    continue;
+                }
                 const uint32_t t = ring + (c % L::STAGES) * L::BYTES + L::V;
                 tma_store_4d(&ty, t, col0, c * C, h, b);
                 if (col0 + 64 < a.dv) tma_store_4d(&ty, t + 8192, col0 + 64, c * C, h, b);
@@ -521,7 +474,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
         regs_dec<OUT_REGS>();
         const int quad = warp & 3, row = quad * 32 + lane;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
-        for (int c = 0; c < chunks; ++c) {
+        for (int c = 0; !KEEP && c < chunks; ++c) {
             const uint32_t ph = c & 1;
             unsigned char* tile = ringp + (c % L::STAGES) * L::BYTES;
             const float* gate = reinterpret_cast<const float*>(tile + L::G);
@@ -559,7 +512,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
             announce(bar(B_Y), lane);
         }
         const int col = col0 + row;                          // chunks past the length
-        if (col < a.dv) {
+        if (!KEEP && col < a.dv) {
             __nv_bfloat16* y = static_cast<__nv_bfloat16*>(r.y) + gdn_base(a.token_major, b, h, a.H, a.T, a.dv) + col;
             const int64_t ys = gdn_stride(a.token_major, a.H, a.dv);
             for (int t = chunks * C; t < a.T; ++t) y[t * ys] = __float2bfloat16_rn(0.f);
@@ -571,7 +524,9 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
         const bool live = col < a.dv;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         const int64_t per = static_cast<int64_t>(a.dk) * a.dv;
-        float* st = r.state + chain * per + col;
+        float* st = const_cast<float*>(KEEP ? r.state_in : r.state) + chain * per + col;
+        // saved rows of this column: [chain][chunk][column][d_k], [chain][chunk][part][column][tokens]
+        const int64_t dvp = static_cast<int64_t>(gridDim.x) * 128;
         constexpr int RD = DK / 2;                           // rows of d_k of a warp
         float S[RD];
         if (chunks > 0) {
@@ -587,7 +542,9 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 float v[32];
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = S[x + j];
-                put_part(lanes + S_COL + (half * RD + x) / 2, v);
+                uint4* const keep = KEEP ? reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(r.keep_S) +
+                                                                    ((chain * nc + next) * dvp + col) * DK + half * RD + x) : nullptr;
+                put_part<KEEP>(lanes + S_COL + (half * RD + x) / 2, v, keep);
                 put_last(lanes + S_COL + SB + (half * RD + x) / 2, v);
             }
             if (len - next * C < C) {                        // K rows past the length: zeros, whatever was there
@@ -611,7 +568,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
             const float* gate = reinterpret_cast<const float*>(tile + L::G);
             const int n = len - c * C;                       // live tokens (64 or more: all)
             mbar_wait_or_dead(bar(B_FULL + s), (c / L::STAGES) & 1, dead);
-            float u[32], w[32];
+            float u[32], w[32];                              // r; then w (with KEEP: e)
             uint32_t v[16];                                  // this column's v, two tokens in a word
 #pragma unroll
             for (int j = 0; j < 16; ++j)
@@ -619,41 +576,59 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                        (static_cast<uint32_t>(*reinterpret_cast<const unsigned short*>(tile + vat + sw128_at(i0 + 2 * j + 1, row % 64))) << 16);
             await(bar(B_U), ph, dead);
             tmem_ld32(lanes + X_COL + i0, u);                // step 2
+            float be[32];
+            get32(gate + C + i0, be);
 #pragma unroll
             for (int j = 0; j < 32; j += 4) {
-                const float4 g = *reinterpret_cast<const float4*>(gate + i0 + j), be = *reinterpret_cast<const float4*>(gate + C + i0 + j);
-                u[j] = be.x * (__uint_as_float(v[j / 2] << 16) - g.x * u[j]);
-                u[j + 1] = be.y * (__uint_as_float(v[j / 2] & 0xffff0000u) - g.y * u[j + 1]);
-                u[j + 2] = be.z * (__uint_as_float(v[j / 2 + 1] << 16) - g.z * u[j + 2]);
-                u[j + 3] = be.w * (__uint_as_float(v[j / 2 + 1] & 0xffff0000u) - g.w * u[j + 3]);
+                const float4 g = *reinterpret_cast<const float4*>(gate + i0 + j);
+                u[j] = __uint_as_float(v[j / 2] << 16) - g.x * u[j];
+                u[j + 1] = __uint_as_float(v[j / 2] & 0xffff0000u) - g.y * u[j + 1];
+                u[j + 2] = __uint_as_float(v[j / 2 + 1] << 16) - g.z * u[j + 2];
+                u[j + 3] = __uint_as_float(v[j / 2 + 1] & 0xffff0000u) - g.w * u[j + 3];
             }
             if (n < C) {
 #pragma unroll
                 for (int j = 0; j < 32; ++j) u[j] = i0 + j < n ? u[j] : 0.f;
             }
 #pragma unroll
-            for (int j = 0; j < 32; ++j) w[j] = u[j];
+            for (int j = 0; j < 32; ++j) w[j] = be[j] * u[j];
             put_part(lanes + R_COL + i0 / 2, w);
             put_last(lanes + R_COL + 32 + i0 / 2, w);
             announce(bar(B_R), lane);
-            float hh[32];
-            get32(gate + 2 * C + i0, hh);
             const float g63 = gate[C - 1];
-            await(bar(B_QS), ph, dead);                      // S is read: h w may lie there
-            await(bar(B_RZ), ph, dead);
+            if (!KEEP) await(bar(B_QS), ph, dead);           // S is read: h w may lie there
+            await(bar(B_RN), ph, dead);
             tmem_ld32(lanes + X_COL + i0, w);                // step 4
+            if (KEEP) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                w[j] += u[j];
-                u[j] = w[j] * hh[j];
+                for (int j = 0; j < 32; ++j) w[j] += u[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                const float4 b4 = *reinterpret_cast<const float4*>(gate + C + i0 + j), h4 = *reinterpret_cast<const float4*>(gate + 2 * C + i0 + j);
+                const float bj[4] = {b4.x, b4.y, b4.z, b4.w}, hj[4] = {h4.x, h4.y, h4.z, h4.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (KEEP) {                              // e stays in w
+                        u[j + e] = hj[e] * (bj[e] * w[j + e]);
+                    } else {
+                        w[j + e] = bj[e] * (w[j + e] + u[j + e]);
+                        u[j + e] = hj[e] * w[j + e];
+                    }
+                }
             }
             put_part(lanes + S_COL + i0 / 2, u);
             put_part(lanes + S_COL + 32 + i0 / 2, u);
             put_last(lanes + S_COL + 64 + i0 / 2, u);
             announce(bar(B_H), lane);
-            put_part(lanes + R_COL + i0 / 2, w);
-            put_last(lanes + R_COL + 32 + i0 / 2, w);
-            announce(bar(B_W), lane);
+            if (KEEP) {
+                __nv_bfloat16* const keep = static_cast<__nv_bfloat16*>(r.keep_e) + ((chain * nc + c) * 2 * dvp + col) * C + i0;
+                keep_parts(reinterpret_cast<uint4*>(keep), reinterpret_cast<uint4*>(keep + dvp * C), w);
+            } else {
+                put_part(lanes + R_COL + i0 / 2, w);
+                put_last(lanes + R_COL + 32 + i0 / 2, w);
+                announce(bar(B_W), lane);
+            }
             await(bar(B_HK), ph, dead);
 #pragma unroll
             for (int x = 0; x < RD; x += 32) {               // step 6
@@ -664,7 +639,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
             }
             if (c + 1 < chunks) put_state(c + 1);
         }
-        if (chunks > 0 && live) {
+        if (!KEEP && chunks > 0 && live) {
 #pragma unroll
             for (int x = 0; x < RD; ++x) {
                 const int rw = half * RD + x;
@@ -688,26 +663,26 @@ cudaError_t factors(const CUtensorMap& tk, const CUtensorMap& tq, const GdnArgs&
     return cudaGetLastError();
 }
 
-template <int DK>
+template <int DK, bool KEEP>
 cudaError_t scan(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap& tv, const CUtensorMap& ty, const CUtensorMap& tm, const GdnScan& s,
                  const GdnFactors& f, cudaStream_t stream) {
     constexpr size_t smem = scan_smem<DK>();
     // the compute warpgroups' registers come out of what the CTA is launched with
     static const int regs = [] {
         cudaFuncAttributes at;
-        return cudaFuncGetAttributes(&at, k_gdn_scan<DK>) == cudaSuccess ? at.numRegs : 0;
+        return cudaFuncGetAttributes(&at, k_gdn_scan<DK, KEEP>) == cudaSuccess ? at.numRegs : 0;
     }();
     if (regs * ST < 32 * (SW * SCAN_REGS + OW * OUT_REGS + 4 * IDLE_REGS)) return cudaErrorInvalidConfiguration;
     static std::atomic<unsigned long long> seen;
-    cudaError_t e = allow_smem(k_gdn_scan<DK>, smem, seen);
+    cudaError_t e = allow_smem(k_gdn_scan<DK, KEEP>, smem, seen);
     if (e != cudaSuccess) return e;
-    k_gdn_scan<DK><<<dim3((s.a.dv + 127) / 128, s.a.H, s.a.B), ST, smem, stream>>>(tk, tq, tv, ty, tm, s, f, (s.a.T + C - 1) / C);
+    k_gdn_scan<DK, KEEP><<<dim3((s.a.dv + 127) / 128, s.a.H, s.a.B), ST, smem, stream>>>(tk, tq, tv, ty, tm, s, f, (s.a.T + C - 1) / C);
     return cudaGetLastError();
 }
 
 }  // namespace
 
-size_t gdn_factor_mat_bytes(int64_t chunks) { return static_cast<size_t>(chunks) * 3 * MAT; }
+size_t gdn_factor_mat_bytes(int64_t chunks, int mats) { return static_cast<size_t>(chunks) * mats * MAT; }
 size_t gdn_factor_gate_bytes(int64_t chunks) { return static_cast<size_t>(chunks) * GATES; }
 
 // From one whole chunk up: below, the token recurrence is one launch of about the same length.
@@ -725,9 +700,11 @@ cudaError_t launch_gdn_scan(const GdnScan& s, const GdnFactors& f, cudaStream_t 
     const int64_t chunks = static_cast<int64_t>(a.B) * a.H * ((a.T + C - 1) / C);
     CUtensorMap tk, tq, tv, ty, tm;
     if (!token_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk) || !token_map(&tq, a.q, a.token_major, a.B, a.Hk, a.T, a.dk) ||
-        !token_map(&tv, a.v, a.token_major, a.B, a.H, a.T, a.dv) || !token_map(&ty, s.y, a.token_major, a.B, a.H, a.T, a.dv) || !mat_map(&tm, f.mat, chunks * 3))
+        !token_map(&tv, a.v, a.token_major, a.B, a.H, a.T, a.dv) || !token_map(&ty, s.keep_S != nullptr ? a.v : s.y, a.token_major, a.B, a.H, a.T, a.dv) || !row_map(&tm, f.mat, chunks * f.mats * C, C, C))
         return cudaErrorInvalidValue;
-    return a.dk <= 64 ? scan<64>(tk, tq, tv, ty, tm, s, f, stream) : scan<128>(tk, tq, tv, ty, tm, s, f, stream);
+    if (s.keep_S != nullptr)
+        return a.dk <= 64 ? scan<64, true>(tk, tq, tv, ty, tm, s, f, stream) : scan<128, true>(tk, tq, tv, ty, tm, s, f, stream);
+    return a.dk <= 64 ? scan<64, false>(tk, tq, tv, ty, tm, s, f, stream) : scan<128, false>(tk, tq, tv, ty, tm, s, f, stream);
 }
 
 }  // namespace sdm
