@@ -85,8 +85,8 @@ sdm_status gdn_check(const sdm_gdn_shape* s) {
     if (s->d_k < 1 || s->d_v < 1) return fail(SDM_ERR_INVALID_ARG, "d_k and d_v must be >= 1 (got %d, %d)", s->d_k, s->d_v);
     if (s->d_k > 256) return fail(SDM_ERR_UNSUPPORTED, "d_k > 256 is not supported (d_k=%d)", s->d_k);
     if (s->d_v > (1 << 20)) return fail(SDM_ERR_UNSUPPORTED, "d_v too large (%d)", s->d_v);
-    if (static_cast<int64_t>(s->B) * s->H * ((static_cast<int64_t>(s->T) + 63) / 64) > INT_MAX / 256)
-        return fail(SDM_ERR_UNSUPPORTED, "B * H * T / 64 must be at most 2^23 (got %d, %d, %d)", s->B, s->H, s->T);
+    if (static_cast<int64_t>(s->B) * s->H * ((static_cast<int64_t>(s->T) + 63) / 64) > INT_MAX / 256 / ((s->d_v + 127) / 128))
+        return fail(SDM_ERR_UNSUPPORTED, "B * H * T / 64 * d_v / 128 must be below 2^23 (got %d, %d, %d, %d)", s->B, s->H, s->T, s->d_v);
     const size_t es = esize(s->dtype);
     if (s->d_k * es % 16 != 0 || s->d_v * es % 16 != 0)
         return fail(SDM_ERR_UNSUPPORTED, "d_k and d_v times the element size must be multiples of 16 bytes (d_k=%d, d_v=%d)", s->d_k, s->d_v);
@@ -127,17 +127,28 @@ FwdLayout fwd_layout(const sdm_gdn_shape* s) {
     return L;
 }
 
-// Saved states and rows of the fp32 backward.
+// What the walks of the backward store: the fp32 kernels states and rows, the tensor-core kernels the
+// chunks' factors, then states and rows as bf16 (see GdnScan, GdnBack).
 struct BwdLayout {
-    size_t S, dE, e, d, total;
+    bool tc;
+    size_t mat, gates, S, dE, e, d, total;
 };
 BwdLayout bwd_layout(const sdm_gdn_shape* s) {
-    const size_t nc = (static_cast<size_t>(s->T) + sdm::GDN_C32 - 1) / sdm::GDN_C32;
-    const size_t marks = static_cast<size_t>(s->B) * s->H * nc * s->d_k * s->d_v * 4;
-    const size_t rows = static_cast<size_t>(s->B) * s->H * s->T * s->d_v * 4;
     BwdLayout L{};
-    L.S = 0;
-    L.dE = align256(marks);
+    const size_t bh = static_cast<size_t>(s->B) * s->H, T = static_cast<size_t>(s->T);
+    L.tc = sdm::gdn_chunk_supported(s->dtype, s->d_k, s->T);
+    size_t marks, rows;
+    if (L.tc) {
+        const size_t chunks = bh * ((T + sdm::GDN_C64 - 1) / sdm::GDN_C64), dvp = (static_cast<size_t>(s->d_v) + 127) / 128 * 128;
+        L.gates = align256(sdm::gdn_factor_mat_bytes(static_cast<int64_t>(chunks), 4));
+        L.S = L.gates + align256(sdm::gdn_factor_gate_bytes(static_cast<int64_t>(chunks)));
+        marks = chunks * dvp * (s->d_k <= 64 ? 64 : 128) * 2;
+        rows = chunks * 2 * dvp * sdm::GDN_C64 * 2;
+    } else {
+        marks = bh * ((T + sdm::GDN_C32 - 1) / sdm::GDN_C32) * s->d_k * s->d_v * 4;
+        rows = bh * T * s->d_v * 4;
+    }
+    L.dE = L.S + align256(marks);
     L.e = L.dE + align256(marks);
     L.d = L.e + align256(rows);
     L.total = L.d + align256(rows);
@@ -271,8 +282,18 @@ sdm_status sdm_gdn_backward(const sdm_gdn_shape* s, const void* q, const void* k
     SDM_TRY(sdm::api_status_word(&err));
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
+    const sdm::GdnArgs a = gdn_args(s, q, k, v, alpha, beta, lengths, err);
+    if (L.tc) {
+        const sdm::GdnFactors fa{ws + L.mat, 4, reinterpret_cast<float*>(ws + L.gates)};
+        cudaError_t e = sdm::launch_gdn_factors(a, fa, st);
+        if (e == cudaSuccess) e = sdm::launch_gdn_scan(sdm::GdnScan{a, nullptr, nullptr, state0, ws + L.S, ws + L.e}, fa, st);
+        if (e == cudaSuccess) e = sdm::launch_gdn_back(sdm::GdnBack{a, dy, dstate, dv, dstate0, ws + L.dE, ws + L.d}, fa, st);
+        if (e == cudaSuccess)
+            e = sdm::launch_gdn_grads_tc(sdm::GdnGradsTc{a, dy, fa.gates, ws + L.S, ws + L.dE, ws + L.e, ws + L.d, dq, dk, dalpha, dbeta}, st);
+        return done(e, "sdm_gdn_backward");
+    }
     sdm::GdnRecur f{};
-    f.a = gdn_args(s, q, k, v, alpha, beta, lengths, err);
+    f.a = a;
     sdm::GdnRecur r = f;
     cudaError_t e = cudaSuccess;
     if (s->T > 0) {

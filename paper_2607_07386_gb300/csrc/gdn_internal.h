@@ -107,6 +107,28 @@ struct GdnScan {
 };
 cudaError_t launch_gdn_scan(const GdnScan& s, const GdnFactors& f, cudaStream_t stream);
 
+// The backward's walk (k_gdn_back.cu), with f.mats == 4.
+struct GdnBack {
+    GdnArgs a;
+    const void* dy;
+    const float* dstate;      // dL/dS_T or nullptr (zero)
+    void* dv;
+    float* dstate0;           // dL/dS_0 or nullptr
+    void* keep_D;             // [B, H, nc, dv', dk'] bf16: the gradients of the states after the chunks, transposed
+    void* keep_d;             // [B, H, nc, 2, dv', 64] bf16: d as upper and lower parts, transposed
+};
+cudaError_t launch_gdn_back(const GdnBack& r, const GdnFactors& f, cudaStream_t stream);
+
+// Gradients of q, k and the gates from what the two walks stored (k_gdn_grads_tc.cu).
+struct GdnGradsTc {
+    GdnArgs a;
+    const void* dy;
+    const float* gates;       // GdnFactors::gates
+    const void* S; const void* D; const void* e; const void* d;   // as GdnScan and GdnBack store them
+    void* dq; void* dk; void* dalpha; void* dbeta;
+};
+cudaError_t launch_gdn_grads_tc(const GdnGradsTc& g, cudaStream_t stream);
+
 // ---- linear layer (k_linear.cu): bf16 matrices, row-major ----
 // out [M, N] = residual + act(x W^T + bias); pre (optional) receives x W^T + bias.
 struct LinearOut {

@@ -1,0 +1,359 @@
+// Gated delta rule in chunks of 64 tokens, the walk of the backward pass (bf16 storage, d_k <= 128): the
+// gradient D of the state, from the last chunk to the first.  With B, N, P, g and h of a chunk as in the
+// forward (N = -(I + B beta)^-1 B), D the gradient of the state after it and dy scaled:
+//   x = h K D + P^T dy                       the gradient of w = beta e, but for what later e take from it
+//   d = (I + beta B)^-T x = x + N^T (beta x)
+//   dv = beta d,   D' = g_63 D + Q^T (g dy) - K^T (beta g d)
+// The layout is the forward walk's: a CTA owns 128 columns of one state, a TMEM lane is a column, every
+// product is D^T-like, its A operand written to TMEM from registers.  Per chunk:
+//   1  dy^T P, D^T K^T, then (g dy)^T Q              (MMA; the first needs nothing of the chain, the last runs
+//                                                    under step 2)
+//   2  x = h .. + ..                                 (registers, bf16 parts to TMEM)
+//   3  (beta x)^T N                                  (MMA)
+//   4  d = x + ..,  beta g d                         (registers, bf16 parts to TMEM)
+//   5  .. += (-beta g d)^T K                         (MMA; dv, d and the next chunk's dy are put away meanwhile)
+//   6  D = g_63 D + ..                               (registers, bf16 parts to TMEM)
+// D before every step 6 (as bf16) and d (as two bf16 parts) are stored for the gradients of q, k and the gates.
+// Operands are split as in the forward: what D would keep the rounding of has three parts, the others two.
+// The chain of the six stages bounds it.
+#include "gdn_tc.cuh"
+
+namespace sdm {
+
+namespace {
+
+using namespace tc;
+using namespace gdn;
+
+constexpr int SW = 8;                          // compute warps: two share a lane quarter
+constexpr int ST = 32 * (SW + 4);
+constexpr int BACK_REGS = 232, IDLE_REGS = 40; // the split of the launch's 168 per thread
+constexpr int NS = 2, NH = 3;                  // bf16 parts
+// TMEM columns: X: D^T K^T, then step 3; Z: dy^T P, then beta x; A: the update; S: D, then beta g d; dy; g dy.
+constexpr uint32_t X_COL = 0, Z_COL = 64, A_COL = 128, S_COL = 256, Y_COL = 384, GY_COL = 416, T_COLS = 512;
+
+template <int DK>
+struct BackTile {
+    static constexpr uint32_t KQ = 0, Y = 128 * 2 * DK, M = Y + C * 256, G = M + 4 * MAT, BYTES = G + 1024;
+    static constexpr uint32_t LOAD = G + GATES;
+    static constexpr int STAGES = 2;
+};
+enum { B_FULL = 0, B_U = 2, B_XN, B_UP, B_S, B_DY, B_X, B_H, B_OUT, B_COUNT };
+struct BackCtl {
+    unsigned long long bar[B_COUNT];
+    uint32_t tmem;
+    int dead;
+};
+template <int DK>
+constexpr size_t back_smem() { return 1024 + BackTile<DK>::BYTES * BackTile<DK>::STAGES + sizeof(BackCtl); }
+
+// Both warps of a lane quarter.
+__device__ __forceinline__ void bar_pair(int quad) {
+    tc_before_sync();
+    asm volatile("bar.sync %0, 64;\n" ::"r"(1 + quad) : "memory");
+    tc_after_sync();
+}
+
+template <int DK>
+__global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tq,
+                                                    const __grid_constant__ CUtensorMap ty, const __grid_constant__ CUtensorMap tdv,
+                                                    const __grid_constant__ CUtensorMap tm, const GdnBack r, const GdnFactors f, int nc) {
+    using L = BackTile<DK>;
+    extern __shared__ unsigned char raw[];
+    const GdnArgs& a = r.a;
+    const uint32_t base = smem_u32(raw);
+    const uint32_t ring = (base + 1023u) & ~1023u;
+    unsigned char* const ringp = raw + (ring - base);
+    BackCtl& ctl = *reinterpret_cast<BackCtl*>(ringp + L::BYTES * L::STAGES);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int b = blockIdx.z, h = blockIdx.y, col0 = blockIdx.x * 128, hk = h / (a.H / a.Hk);
+    const int len = gdn_length(a, b);
+    const int64_t chain = static_cast<int64_t>(b) * a.H + h;
+    const int chunks = (len + C - 1) / C;
+    const uint32_t bars = smem_u32(&ctl.bar[0]);
+    auto bar = [&](int i) { return bars + 8 * i; };
+    if (tid == 0) {
+        ctl.dead = 0;
+        for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), i < B_S ? 1 : SW);
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        fence_async();
+    }
+    if (warp == 0) tmem_alloc(smem_u32(&ctl.tmem), T_COLS);
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    const uint32_t tmem = ctl.tmem;
+    volatile int* dead = &ctl.dead;
+    constexpr int SB = DK / 2;                               // TMEM columns of a part of D
+
+    if (warp >= SW) {
+        regs_dec<IDLE_REGS>();
+        if (warp == SW) {                                    // MMAs
+            const uint32_t id64 = mma_idesc(64), idm = id64 | MN_B, idk = mma_idesc(DK) | MN_B;
+            for (int it = 0; it < chunks; ++it) {
+                const uint32_t t = ring + (it % L::STAGES) * L::BYTES, ph = it & 1;
+                const uint64_t dk = sw128_desc(t + L::KQ), dn = sw128_mn_desc(t + L::M, 8192), dp = sw128_mn_desc(t + L::M + 2 * MAT, 8192),
+                               dkt = sw128_mn_desc(t + L::KQ, 16384), dqt = sw128_mn_desc(t + L::KQ + 8192, 16384);
+                await(bar(B_FULL + it % L::STAGES), (it / L::STAGES) & 1, dead);
+                await(bar(B_DY), ph, dead);
+                if (elect_one()) {                           // step 1
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int kk = 0; kk < C / 16; ++kk)
+                            mma_bf16_ta(tmem + Z_COL, tmem + Y_COL + kk * 8, dp + p * (MAT / 16) + kk * 128, idm, (p | kk) != 0);
+                }
+                __syncwarp();
+                await(bar(B_S), ph, dead);
+                if (elect_one()) {
+#pragma unroll
+                    for (int p = 0; p < NS; ++p)
+#pragma unroll
+                        for (int kk = 0; kk < DK / 16; ++kk)
+                            mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * SB + kk * 8, dk + (kk / 4) * 1024 + (kk % 4) * 2, id64, (p | kk) != 0);
+                    mma_commit(bar(B_U));
+#pragma unroll
+                    for (int p = 0; p < NH; ++p)
+#pragma unroll
+                        for (int kk = 0; kk < C / 16; ++kk)
+                            mma_bf16_ta(tmem + A_COL, tmem + GY_COL + p * 32 + kk * 8, dqt + kk * 128, idk, (p | kk) != 0);
+                }
+                __syncwarp();
+                await(bar(B_X), ph, dead);
+                if (elect_one()) {                           // step 3: (upper, upper), (upper, lower), (lower, upper)
+#pragma unroll
+                    for (int m = 0; m < 3; ++m)
+#pragma unroll
+                        for (int kk = 0; kk < C / 16; ++kk)
+                            mma_bf16_ta(tmem + X_COL, tmem + Z_COL + (m == 2 ? 32 : 0) + kk * 8, dn + (m == 1 ? MAT / 16 : 0) + kk * 128, idm, (m | kk) != 0);
+                    mma_commit(bar(B_XN));
+                }
+                __syncwarp();
+                await(bar(B_H), ph, dead);
+                if (elect_one()) {                           // step 5
+#pragma unroll
+                    for (int p = 0; p < NH; ++p)
+#pragma unroll
+                        for (int kk = 0; kk < C / 16; ++kk)
+                            mma_bf16_ta(tmem + A_COL, tmem + S_COL + p * 32 + kk * 8, dkt + kk * 128, idk, 1);
+                    mma_commit(bar(B_UP));
+                }
+                __syncwarp();
+            }
+        } else if (warp == SW + 1 && lane == 0) {            // copies
+            auto load = [&](int it) {
+                const int c = chunks - 1 - it;
+                const uint32_t t = ring + (it % L::STAGES) * L::BYTES, fb = bar(B_FULL + it % L::STAGES);
+                const int64_t cid = chain * nc + c;
+                mbar_expect_tx(fb, L::LOAD);
+#pragma unroll
+                for (int x = 0; x < DK / 64; ++x) {
+                    tma_load_4d(t + L::KQ + x * 16384, &tk, 64 * x, c * C, hk, b, fb);
+                    tma_load_4d(t + L::KQ + x * 16384 + 8192, &tq, 64 * x, c * C, hk, b, fb);
+                }
+                tma_load_4d(t + L::Y, &ty, col0, c * C, h, b, fb);
+                tma_load_4d(t + L::Y + 8192, &ty, col0 + 64, c * C, h, b, fb);
+#pragma unroll
+                for (int m = 0; m < 4; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * 4 + m) * C), fb);
+                bulk_load(t + L::G, f.gates + cid * 3 * C, GATES, fb);
+            };
+            int loaded = 0;
+            for (; loaded < chunks && loaded < L::STAGES; ++loaded) load(loaded);
+            for (int it = 0; it < chunks; ++it) {
+                mbar_wait_or_dead(bar(B_OUT), it & 1, dead); // dv of the chunk lies where its dy was
+                if (*dead) break;
+                const uint32_t t = ring + (it % L::STAGES) * L::BYTES + L::Y;
+                const int c = chunks - 1 - it;
+                tma_store_4d(&tdv, t, col0, c * C, h, b);
+                if (col0 + 64 < a.dv) tma_store_4d(&tdv, t + 8192, col0 + 64, c * C, h, b);
+                bulk_commit();
+                if (loaded < chunks) {
+                    bulk_wait_read();
+                    mbar_wait_or_dead(bar(B_UP), it & 1, dead);
+                    if (*dead) break;
+                    load(loaded++);
+                }
+            }
+            bulk_wait();
+            if (*dead)                                       // the copies in flight land before the CTA ends
+                for (int j = loaded > L::STAGES ? loaded - L::STAGES : 0; j < loaded; ++j)
+                    mbar_wait(bar(B_FULL + j % L::STAGES), (j / L::STAGES) & 1);
+        }
+    } else {
+        regs_inc<BACK_REGS>();
+        const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane, col = col0 + row;
+        const int i0 = 32 * half;                            // this warp's tokens of a chunk
+        const bool live = col < a.dv;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+        const int64_t per = static_cast<int64_t>(a.dk) * a.dv, dvp = static_cast<int64_t>(gridDim.x) * 128;
+        constexpr int RD = DK / 2;                           // rows of d_k of a warp
+        const uint32_t yat = L::Y + (row / 64) * 8192;
+        float D[RD];
+#pragma unroll
+        for (int x = 0; x < RD; ++x) {
+            const int rw = half * RD + x;
+            D[x] = r.dstate != nullptr && live && rw < a.dk ? __ldcs(r.dstate + chain * per + static_cast<int64_t>(rw) * a.dv + col) : 0.f;
+        }
+        auto put_state = [&](int it) {                       // D after the chunk
+            const int64_t at = ((chain * nc + chunks - 1 - it) * dvp + col) * DK + half * RD;
+#pragma unroll
+            for (int x = 0; x < RD; x += 32) {
+                float v[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = D[x + j];
+                put_part<true>(lanes + S_COL + (half * RD + x) / 2, v, reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(r.keep_D) + at + x));
+                put_last(lanes + S_COL + SB + (half * RD + x) / 2, v);
+            }
+            announce(bar(B_S), lane);
+        };
+        auto put_dy = [&](int it) {                          // dy and g dy of the chunk
+            const int s = it % L::STAGES, n = len - (chunks - 1 - it) * C;
+            const unsigned char* tile = ringp + s * L::BYTES;
+            const float* gate = reinterpret_cast<const float*>(tile + L::G);
+            mbar_wait_or_dead(bar(B_FULL + s), (it / L::STAGES) & 1, dead);
+            if (n < C) {                                     // K and Q rows past the length: zeros, whatever was there
+                for (int p = tid; p < (C - n) * DK / 4; p += 32 * SW) {
+                    const int e = p % 2, rw = n + (p / 2) / (DK / 8), x = (p / 2) % (DK / 8);
+                    *reinterpret_cast<uint4*>(ringp + s * L::BYTES + L::KQ + (x / 8) * 16384 + e * 8192 + rw * 128 + (x % 8) * 16) = make_uint4(0, 0, 0, 0);
+                }
+                fence_async();
+            }
+            uint32_t y[16];
+            float v[32];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int i = i0 + 2 * j;
+                const uint32_t lo = *reinterpret_cast<const unsigned short*>(tile + yat + sw128_at(i, row % 64));
+                const uint32_t hi = *reinterpret_cast<const unsigned short*>(tile + yat + sw128_at(i + 1, row % 64));
+                y[j] = (i < n ? lo : 0u) | (i + 1 < n ? hi << 16 : 0u);
+            }
+            tmem_st16(lanes + Y_COL + i0 / 2, y);
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                const float4 g = *reinterpret_cast<const float4*>(gate + i0 + j);
+                v[j] = a.scale * g.x * __uint_as_float(y[j / 2] << 16);
+                v[j + 1] = a.scale * g.y * __uint_as_float(y[j / 2] & 0xffff0000u);
+                v[j + 2] = a.scale * g.z * __uint_as_float(y[j / 2 + 1] << 16);
+                v[j + 3] = a.scale * g.w * __uint_as_float(y[j / 2 + 1] & 0xffff0000u);
+            }
+            put_part(lanes + GY_COL + i0 / 2, v);
+            put_part(lanes + GY_COL + 32 + i0 / 2, v);
+            put_last(lanes + GY_COL + 64 + i0 / 2, v);
+            __syncwarp();
+            announce(bar(B_DY), lane);
+        };
+        if (chunks > 0) {
+            put_dy(0);
+            put_state(0);
+        }
+        for (int it = 0; it < chunks; ++it) {
+            const int s = it % L::STAGES, c = chunks - 1 - it, n = len - c * C;
+            const uint32_t ph = it & 1;
+            unsigned char* tile = ringp + s * L::BYTES;
+            const float* gate = reinterpret_cast<const float*>(tile + L::G);
+            float u[32], w[32];
+            await(bar(B_U), ph, dead);
+            tmem_ld32(lanes + X_COL + i0, u);                // step 2
+            tmem_ld32(lanes + Z_COL + i0, w);
+            bar_pair(quad);                                  // beta x goes where this quarter's dy^T P was
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                const float4 h4 = *reinterpret_cast<const float4*>(gate + 2 * C + i0 + j), b4 = *reinterpret_cast<const float4*>(gate + C + i0 + j);
+                const float hj[4] = {h4.x, h4.y, h4.z, h4.w}, bj[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    u[j + e] = fmaf(hj[e], u[j + e], a.scale * w[j + e]);
+                    w[j + e] = bj[e] * u[j + e];
+                }
+            }
+            put_part(lanes + Z_COL + i0 / 2, w);
+            put_last(lanes + Z_COL + 32 + i0 / 2, w);
+            announce(bar(B_X), lane);
+            const float g63 = gate[C - 1];
+            await(bar(B_XN), ph, dead);
+            tmem_ld32(lanes + X_COL + i0, w);                // step 4
+#pragma unroll
+            for (int j = 0; j < 32; ++j) u[j] += w[j];       // d
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                const float4 g4 = *reinterpret_cast<const float4*>(gate + i0 + j), b4 = *reinterpret_cast<const float4*>(gate + C + i0 + j);
+                w[j] = -g4.x * (b4.x * u[j]);
+                w[j + 1] = -g4.y * (b4.y * u[j + 1]);
+                w[j + 2] = -g4.z * (b4.z * u[j + 2]);
+                w[j + 3] = -g4.w * (b4.w * u[j + 3]);
+            }
+            put_part(lanes + S_COL + i0 / 2, w);
+            put_part(lanes + S_COL + 32 + i0 / 2, w);
+            put_last(lanes + S_COL + 64 + i0 / 2, w);
+            announce(bar(B_H), lane);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                const int i = i0 + j;
+                *reinterpret_cast<__nv_bfloat16*>(tile + yat + sw128_at(i, row % 64)) = __float2bfloat16_rn(i < n ? gate[C + i] * u[j] : 0.f);
+            }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(B_OUT));
+            __nv_bfloat16* const keep = static_cast<__nv_bfloat16*>(r.keep_d) + ((chain * nc + c) * 2 * dvp + col) * C + i0;
+            keep_parts(reinterpret_cast<uint4*>(keep), reinterpret_cast<uint4*>(keep + dvp * C), u);
+            if (it + 1 < chunks) put_dy(it + 1);
+            await(bar(B_UP), ph, dead);
+#pragma unroll
+            for (int x = 0; x < RD; x += 32) {               // step 6
+                float v[32];
+                tmem_ld32(lanes + A_COL + half * RD + x, v);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) D[x + j] = fmaf(g63, D[x + j], v[j]);
+            }
+            if (it + 1 < chunks) put_state(it + 1);
+        }
+        if (live) {
+            if (r.dstate0 != nullptr) {
+#pragma unroll
+                for (int x = 0; x < RD; ++x) {
+                    const int rw = half * RD + x;
+                    if (rw < a.dk) __stcs(r.dstate0 + chain * per + static_cast<int64_t>(rw) * a.dv + col, D[x]);
+                }
+            }
+            __nv_bfloat16* dv = static_cast<__nv_bfloat16*>(r.dv) + gdn_base(a.token_major, b, h, a.H, a.T, a.dv) + col;
+            const int64_t vs = gdn_stride(a.token_major, a.H, a.dv);          // chunks past the length
+            for (int t = chunks * C + half; t < a.T; t += 2) dv[t * vs] = __float2bfloat16_rn(0.f);
+        }
+    }
+    tc_before_sync();
+    __syncthreads();
+    if (tid == 0 && ctl.dead) flag_error(a.err, ERR_TIMEOUT);
+    if (warp == 0) tmem_free(tmem, T_COLS);
+}
+
+template <int DK>
+cudaError_t back(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap& ty, const CUtensorMap& tdv, const CUtensorMap& tm,
+                 const GdnBack& r, const GdnFactors& f, cudaStream_t stream) {
+    constexpr size_t smem = back_smem<DK>();
+    // the compute warpgroups' registers come out of what the CTA is launched with
+    static const int regs = [] {
+        cudaFuncAttributes at;
+        return cudaFuncGetAttributes(&at, k_gdn_back<DK>) == cudaSuccess ? at.numRegs : 0;
+    }();
+    if (regs * ST < 32 * (SW * BACK_REGS + 4 * IDLE_REGS)) return cudaErrorInvalidConfiguration;
+    static std::atomic<unsigned long long> seen;
+    cudaError_t e = allow_smem(k_gdn_back<DK>, smem, seen);
+    if (e != cudaSuccess) return e;
+    k_gdn_back<DK><<<dim3((r.a.dv + 127) / 128, r.a.H, r.a.B), ST, smem, stream>>>(tk, tq, ty, tdv, tm, r, f, (r.a.T + C - 1) / C);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_gdn_back(const GdnBack& r, const GdnFactors& f, cudaStream_t stream) {
+    const GdnArgs& a = r.a;
+    const int64_t chunks = static_cast<int64_t>(a.B) * a.H * ((a.T + C - 1) / C);
+    CUtensorMap tk, tq, ty, tdv, tm;
+    if (!token_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk) || !token_map(&tq, a.q, a.token_major, a.B, a.Hk, a.T, a.dk) ||
+        !token_map(&ty, r.dy, a.token_major, a.B, a.H, a.T, a.dv) || !token_map(&tdv, r.dv, a.token_major, a.B, a.H, a.T, a.dv) ||
+        !row_map(&tm, f.mat, chunks * 4 * C, C, C))
+        return cudaErrorInvalidValue;
+    return a.dk <= 64 ? back<64>(tk, tq, ty, tdv, tm, r, f, stream) : back<128>(tk, tq, ty, tdv, tm, r, f, stream);
+}
+
+}  // namespace sdm

@@ -1,0 +1,506 @@
+// Gated delta rule, gradients of q, k and the gates on the tensor cores (bf16 storage, d_k <= 128), every
+// chunk of 64 tokens on its own, from what the two walks stored: the states S before and the gradients D
+// after the chunks (transposed, bf16), e and d (transposed, two bf16 parts).  With the decay products G, g, h
+// of a chunk, w = beta e and dy scaled:
+//   dq_i = g_i S dy_i + sum_{j <= i} M_ij k_j,                           M_ij = G_ij beta_j <dy_i, e_j>
+//   dk_j = beta_j h_j D e_j - beta_j g_j S d_j + sum_{i >= j} M_ij q_i
+//          - sum_{i > j} A_ij k_i - sum_{i < j} A_ji k_i,                A_ij = beta_i beta_j G_ij <d_i, e_j>
+//   dbeta_i = <d_i, e_i>
+// and dalpha_t = sum_{j < t} (sum_{i >= t} prod_{t < l <= i} alpha_l X_ij) prod_{j < l < t} alpha_l over the
+// gradients X of the decay products, with the chunk's start as column -1 and its end as row 64 (nothing is
+// divided by a gate):
+//   X_ij = beta_j <dy_i, e_j> q_i.k_j - beta_i beta_j <d_i, e_j> k_i.k_j,   X_{i,-1} = q_i.S dy_i - beta_i k_i.S d_i,
+//   X_{64,j} = beta_j k_j.D e_j,   X_{64,-1} = <D, S>.
+//
+// One CTA per SM walks over the chunks of the key heads and adds up the value heads that share one.  The
+// products over d_v have d_k as TMEM lanes (S and D are A operands as they lie), <dy, e> the tokens in
+// lanes 0-63 and <d, e> in lanes 64-127, beside q.k and k.k.  Warps 0-7 take the products through registers,
+// warp 8 issues the MMAs, warp 9 the copies, warps 10 and 11 run the sums of dalpha, a column a thread.
+// The tiles of the next (head, block of d_v) load while this one's products are taken.  Bound by the loads
+// (112 KB of tiles a chunk and head at d_k = d_v = 128, and 32 KB of K and Q) and the MMAs, one after the other.
+#include "gdn_tc.cuh"
+
+namespace sdm {
+
+namespace {
+
+using namespace tc;
+using namespace gdn;
+
+constexpr int SW = 8, NT = 32 * (SW + 4);
+constexpr int GRAD_REGS = 224, REST_REGS = 56; // the split of the launch's 168 per thread // the split of the launch's 168 per thread // the split of the launch's 168 per thread // the split of the launch's 168 per thread
+constexpr int XP = C + 1;                      // columns of X: -1 .. 63
+// TMEM columns
+constexpr uint32_t SY = 0, SD = 64, DE = 128, QK = 192, YE = 256, GE = 320, IQ = 384, IK = 448, T_COLS = 512;
+
+template <int DK>
+struct Tile {
+    // per 64 values of d_k: 64 rows of Q, 64 of K.  The d tile has 16 KB before it and the dy tile 8 KB after
+    // it that the other half of the lanes of their products reads.
+    static constexpr uint32_t QK = 0, S = 128 * 2 * DK, D = S + 256 * DK, E = D + 256 * DK, DT = E + 32768, Y = DT + 32768, M = Y + 16384,
+                              G = M + 3 * MAT, BYTES = G + 1024;
+    static constexpr uint32_t LOAD = 512 * DK + 65536 + 16384 + GATES;
+};
+enum { B_KQ = 0, B_TILE, B_INTER, B_INTRA, B_KREADY, B_M, B_X, B_OUT, B_XFREE, B_EMPTY, B_COUNT };
+struct Ctl {
+    float X[C + 1][XP];
+    float dots[3][4][C];                       // q.S dy, k.S d, k.D e of each lane quarter
+    float gt[3][C];                            // g, beta, h of the head's chunk
+    float db[C];
+    float es[SW];
+    uint4 al[C / 8];
+    unsigned long long bar[B_COUNT];
+    uint32_t tmem;
+    int dead;
+};
+template <int DK>
+constexpr size_t grads_smem() { return 1024 + Tile<DK>::BYTES + sizeof(Ctl); }
+
+__device__ __forceinline__ void bar_compute() { asm volatile("bar.sync 1, %0;\n" ::"n"(32 * SW) : "memory"); }
+
+// Sums over the lanes of 32 values per lane: lane l gets the sum of value l.
+__device__ __forceinline__ float sum_lanes(float (&v)[32], int lane) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int j = 0; j < o; ++j) {
+            const float give = up ? v[j] : v[j + o], keep = up ? v[j + o] : v[j];
+            v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+    }
+    return v[0];
+}
+
+// A warp of which every lane has put something into shared memory for the MMAs or other warps.
+__device__ __forceinline__ void arrive(uint32_t bar, int lane) {
+    tc_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+}
+
+template <int DK>
+__global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
+                                                        const __grid_constant__ CUtensorMap ty, const __grid_constant__ CUtensorMap tS,
+                                                        const __grid_constant__ CUtensorMap tD, const __grid_constant__ CUtensorMap te,
+                                                        const __grid_constant__ CUtensorMap td, const __grid_constant__ CUtensorMap tdq,
+                                                        const __grid_constant__ CUtensorMap tdk, const GdnGradsTc r, int nc) {
+    using L = Tile<DK>;
+    extern __shared__ unsigned char raw[];
+    const GdnArgs& a = r.a;
+    const uint32_t base = smem_u32(raw);
+    const uint32_t t = (base + 1023u) & ~1023u;
+    unsigned char* const tp = raw + (t - base);
+    Ctl& ctl = *reinterpret_cast<Ctl*>(tp + L::BYTES);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t bars = smem_u32(&ctl.bar[0]);
+    auto bar = [&](int i) { return bars + 8 * i; };
+    if (tid == 0) {
+        ctl.dead = 0;
+        for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), i < B_KREADY ? 1 : i == B_XFREE ? 2 : i == B_EMPTY ? SW + 1 : SW);
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        fence_async();
+    }
+    if (warp == 0) tmem_alloc(smem_u32(&ctl.tmem), T_COLS);
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    const uint32_t tmem = ctl.tmem;
+    volatile int* dead = &ctl.dead;
+    const int group = a.H / a.Hk, nblk = (a.dv + 127) / 128, subs = group * nblk;
+    const int64_t items = static_cast<int64_t>(a.B) * a.Hk * nc;
+    // the chunks with tokens, in the order in which every warp of the CTA meets them
+    struct Item {
+        int b, hk, c, n;
+    };
+    auto item_of = [&](int64_t w) {
+        Item x;
+        x.c = static_cast<int>(w % nc);
+        x.hk = static_cast<int>(w / nc % a.Hk);
+        x.b = static_cast<int>(w / nc / a.Hk);
+        const int left = gdn_length(a, x.b) - x.c * C;
+        x.n = left < 0 ? 0 : left < C ? left : C;
+        return x;
+    };
+
+    if (warp >= SW) regs_dec<REST_REGS>();
+    else regs_inc<GRAD_REGS>();
+    if (warp == SW) {                                        // MMAs
+        const uint32_t id = mma_idesc(64), idA = id | MN_A, idB = id | MN_B, idAB = id | MN_A | MN_B;
+        const uint64_t q = sw128_desc(t + L::QK), k = sw128_desc(t + L::QK + 8192), qt = sw128_mn_desc(t + L::QK, 16384),
+                       kt = sw128_mn_desc(t + L::QK + 8192, 16384), S = sw128_mn_desc(t + L::S, 16384), D = sw128_mn_desc(t + L::D, 16384),
+                       e = sw128_mn_desc(t + L::E, 8192), d = sw128_mn_desc(t + L::DT, 8192), dh = sw128_mn_desc(t + L::DT - 16384, 16384),
+                       y = sw128_desc(t + L::Y), m = sw128_desc(t + L::M), mt = sw128_mn_desc(t + L::M, 8192);
+        // rolled loops: unrolled, the descriptors of 80 MMAs are kept in registers and spilled
+        uint32_t ni = 0, ns = 0, nh = 0;
+        for (int64_t w = blockIdx.x; w < items; w += gridDim.x) {
+            if (item_of(w).n == 0) continue;
+            await(bar(B_KQ), ni & 1, dead);
+            await(bar(B_KREADY), ni & 1, dead);
+            ++ni;
+            if (elect_one()) {
+#pragma unroll 1
+                for (int kk = 0; kk < DK / 16; ++kk)
+                    mma_bf16(tmem + QK, q + (kk / 4) * 1024 + (kk % 4) * 2, k + (kk / 4) * 1024 + (kk % 4) * 2, id, kk != 0);
+            }
+            __syncwarp();
+            for (int sub = 0; sub < subs; ++sub, ++ns) {
+                const uint32_t first = sub % nblk == 0 ? 0u : 1u;
+                await(bar(B_TILE), ns & 1, dead);
+                if (elect_one()) {
+#pragma unroll 1
+                    for (int kk = 0; kk < 8; ++kk)           // S dy^T, <dy, e>
+                        mma_bf16(tmem + SY, S + kk * 128, y + (kk / 4) * 512 + (kk % 4) * 2, idA, first | (kk != 0));
+#pragma unroll 1
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll 1
+                        for (int kk = 0; kk < 8; ++kk) {
+                            mma_bf16(tmem + SD, S + kk * 128, d + p * 1024 + kk * 128, idAB, first | (p | kk) != 0);
+                            mma_bf16(tmem + DE, D + kk * 128, e + p * 1024 + kk * 128, idAB, first | (p | kk) != 0);
+                            mma_bf16(tmem + YE, y + (kk / 4) * 512 + (kk % 4) * 2, e + p * 1024 + kk * 128, idB, first | (p | kk) != 0);
+                        }
+#pragma unroll 1
+                    for (int p = 0; p < 3; ++p)              // <d, e>: (upper, upper), (upper, lower), (lower, upper)
+#pragma unroll 1
+                        for (int kk = 0; kk < 8; ++kk)
+                            mma_bf16(tmem + GE, dh + (p == 2 ? 1024 : 0) + kk * 128, e + (p == 1 ? 1024 : 0) + kk * 128, idAB, first | (p | kk) != 0);
+                    mma_commit(bar(B_EMPTY));
+                    if (sub % nblk == nblk - 1) mma_commit(bar(B_INTER));
+                }
+                __syncwarp();
+                if (sub % nblk == nblk - 1) {
+                    await(bar(B_M), nh & 1, dead);
+                    ++nh;
+                    if (elect_one()) {
+#pragma unroll 1
+                        for (int p = 0; p < 2; ++p)
+#pragma unroll 1
+                            for (int kk = 0; kk < C / 16; ++kk) {
+                                mma_bf16(tmem + IQ, kt + kk * 128, m + p * (MAT / 16) + kk * 2, idA, (p | kk) != 0);
+                                mma_bf16(tmem + IK, qt + kk * 128, mt + p * (MAT / 16) + kk * 128, idAB, (p | kk) != 0);
+                            }
+#pragma unroll 1
+                        for (int kk = 0; kk < C / 16; ++kk) {
+                            mma_bf16(tmem + IK, kt + kk * 128, mt + 2 * (MAT / 16) + kk * 128, idAB, 1);
+                            mma_bf16(tmem + IK, kt + kk * 128, m + 2 * (MAT / 16) + kk * 2, idA, 1);
+                        }
+                        mma_commit(bar(B_INTRA));
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+    } else if (warp == SW + 1) {                             // copies
+        if (lane == 0) {
+            uint32_t ni = 0, ns = 0;
+            for (int64_t w = blockIdx.x; w < items && !*dead; w += gridDim.x) {
+                const Item x = item_of(w);
+                if (x.n == 0) continue;
+                mbar_expect_tx(bar(B_KQ), 256 * DK);
+#pragma unroll
+                for (int i = 0; i < DK / 64; ++i) {
+                    tma_load_4d(t + L::QK + i * 16384, &tq, 64 * i, x.c * C, x.hk, x.b, bar(B_KQ));
+                    tma_load_4d(t + L::QK + i * 16384 + 8192, &tk, 64 * i, x.c * C, x.hk, x.b, bar(B_KQ));
+                }
+                for (int sub = 0; sub < subs; ++sub, ++ns) {
+                    const int h = x.hk * group + sub / nblk, blk = sub % nblk;
+                    const int64_t cid = (static_cast<int64_t>(x.b) * a.H + h) * nc + x.c;
+                    const int rs = static_cast<int>((cid * nblk + blk) * 128), rp = static_cast<int>((cid * 2 * nblk + blk) * 128);
+                    if (ns > 0) {
+                        mbar_wait_or_dead(bar(B_EMPTY), (ns - 1) & 1, dead);
+                        if (*dead) break;
+                    }
+                    mbar_expect_tx(bar(B_TILE), L::LOAD);
+#pragma unroll
+                    for (int i = 0; i < DK / 64; ++i) tma_load_2d(t + L::S + i * 16384, &tS, 64 * i, rs, bar(B_TILE));
+                    tma_load_4d(t + L::Y, &ty, blk * 128, x.c * C, h, x.b, bar(B_TILE));
+                    tma_load_4d(t + L::Y + 8192, &ty, blk * 128 + 64, x.c * C, h, x.b, bar(B_TILE));
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        tma_load_2d(t + L::E + i * 16384, &te, 0, rp + i * nblk * 128, bar(B_TILE));
+                        tma_load_2d(t + L::DT + i * 16384, &td, 0, rp + i * nblk * 128, bar(B_TILE));
+                    }
+#pragma unroll
+                    for (int i = 0; i < DK / 64; ++i) tma_load_2d(t + L::D + i * 16384, &tD, 64 * i, rs, bar(B_TILE));
+                    bulk_load(t + L::G, r.gates + cid * 3 * C, GATES, bar(B_TILE));
+                }
+                mbar_wait_or_dead(bar(B_OUT), ni & 1, dead);
+                ++ni;
+                if (*dead) break;
+#pragma unroll
+                for (int i = 0; i < DK / 64; ++i) {          // dq and dk lie where q and k were
+                    if (64 * i < a.dk) {
+                        tma_store_4d(&tdq, t + L::QK + i * 16384, 64 * i, x.c * C, x.hk, x.b);
+                        tma_store_4d(&tdk, t + L::QK + i * 16384 + 8192, 64 * i, x.c * C, x.hk, x.b);
+                    }
+                }
+                bulk_commit();
+                bulk_wait_read();
+            }
+            bulk_wait();
+            if (*dead && ns > 0) mbar_wait(bar(B_TILE), (ns - 1) & 1);   // the copies in flight land before the CTA ends
+        }
+    } else if (warp > SW + 1) {                              // dalpha, dbeta: column j = tj - 1, then token tj
+        const int tj = tid - 32 * (SW + 2);
+        uint32_t nh = 0;
+        for (int64_t w = blockIdx.x; w < items; w += gridDim.x) {
+            const Item x = item_of(w);
+            const int t0 = x.c * C, nt = a.T - t0 < C ? a.T - t0 : C;
+            for (int hv = 0; hv < group; ++hv) {
+                const int64_t at = (static_cast<int64_t>(x.b) * a.H + x.hk * group + hv) * a.T + t0 + tj;
+                float s = 0.f, db = 0.f;
+                if (x.n > 0) {
+                    mbar_wait_or_dead(bar(B_X), nh & 1, dead);
+                    ++nh;
+                    const unsigned short* al = reinterpret_cast<const unsigned short*>(ctl.al);
+                    auto alpha = [&](int i) { return __uint_as_float(static_cast<uint32_t>(al[i]) << 16); };
+                    float acc = ctl.X[C - 1][tj] + ctl.X[C][tj];
+                    ctl.X[C - 1][tj] = acc;
+#pragma unroll 8
+                    for (int i = C - 2; i >= 0; --i) {
+                        acc = fmaf(alpha(i + 1), acc, ctl.X[i][tj]);
+                        if (i >= tj) ctl.X[i][tj] = acc;
+                    }
+                    float p = 1.f;
+#pragma unroll 8
+                    for (int i = 0; i < C; ++i) {
+                        if (i >= tj) {
+                            ctl.X[i][tj] *= p;
+                            p *= alpha(i);
+                        }
+                    }
+                    asm volatile("bar.sync 2, 64;\n" ::: "memory");
+#pragma unroll 8
+                    for (int i = 0; i < C; ++i) s += i <= tj ? ctl.X[tj][i] : 0.f;
+                    db = ctl.db[tj];
+                    arrive(bar(B_XFREE), lane);
+                }
+                if (tj < nt) {
+                    static_cast<__nv_bfloat16*>(r.dalpha)[at] = __float2bfloat16_rn(tj < x.n ? s : 0.f);
+                    static_cast<__nv_bfloat16*>(r.dbeta)[at] = __float2bfloat16_rn(tj < x.n ? db : 0.f);
+                }
+            }
+        }
+    } else {
+        const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane, i0 = 32 * half;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+        const float* gate = reinterpret_cast<const float*>(tp + L::G);
+        const unsigned char* kq = tp + L::QK + (row / 64) * 16384;   // this lane's column of Q; K 8192 bytes on
+        const int i = row & 63;                              // token of this lane in <dy, e> and <d, e>
+        uint32_t ni = 0, ns = 0, nh = 0;
+        for (int64_t w = blockIdx.x; w < items; w += gridDim.x) {
+            const Item x = item_of(w);
+            const int t0 = x.c * C, n = x.n, nt = a.T - t0 < C ? a.T - t0 : C;
+            if (n == 0) {                                    // past the length
+                const int64_t at = gdn_base(a.token_major, x.b, x.hk, a.Hk, a.T, a.dk), ks = gdn_stride(a.token_major, a.Hk, a.dk);
+                for (int p = tid; p < nt * (a.dk / 8); p += 32 * SW) {
+                    const int64_t o = at + (t0 + p / (a.dk / 8)) * ks + (p % (a.dk / 8)) * 8;
+                    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(r.dq) + o) = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(r.dk) + o) = make_uint4(0, 0, 0, 0);
+                }
+                continue;
+            }
+            mbar_wait_or_dead(bar(B_KQ), ni & 1, dead);
+            ++ni;
+            if (n < C) {                                     // rows past the length: zeros, whatever was there
+                for (int p = tid; p < (C - n) * DK / 4; p += 32 * SW) {
+                    const int e = p % 2, rw = n + (p / 2) / (DK / 8), c = (p / 2) % (DK / 8);
+                    *reinterpret_cast<uint4*>(tp + L::QK + (c / 8) * 16384 + e * 8192 + rw * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
+                }
+                fence_async();
+            }
+            arrive(bar(B_KREADY), lane);
+            if (n < C) bar_compute();                        // the other warps' zeros, before q and k are read below
+            float dq[32], dk[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) dq[j] = dk[j] = 0.f;
+            for (int hv = 0; hv < group; ++hv, ++nh) {
+                const int64_t chain = static_cast<int64_t>(x.b) * a.H + x.hk * group + hv;
+                unsigned short al = 0x3f80;
+                if (tid < n) al = __ldg(static_cast<const unsigned short*>(a.alpha) + chain * a.T + t0 + tid);
+                float es = 0.f, gv = 0.f;                    // <D, S>; a gate product of the head
+                for (int blk = 0; blk < nblk; ++blk, ++ns) {
+                    mbar_wait_or_dead(bar(B_TILE), ns & 1, dead);
+                    for (int p = tid; p < 16 * DK; p += 32 * SW) {
+                        float u[8], v[8];
+                        unpack16<BF16>(*reinterpret_cast<const uint4*>(tp + L::S + p * 16), u);
+                        unpack16<BF16>(*reinterpret_cast<const uint4*>(tp + L::D + p * 16), v);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) es = fmaf(u[e], v[e], es);
+                    }
+                    if (tid < 3 * C) gv = gate[tid];
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(B_EMPTY));
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) es += __shfl_xor_sync(0xffffffffu, es, o);
+                if (nh > 0) mbar_wait_or_dead(bar(B_XFREE), (nh - 1) & 1, dead);
+                // from here on nothing of the last head is read any more
+                if (lane == 0) ctl.es[warp] = es;
+                if (tid < 3 * C) (&ctl.gt[0][0])[tid] = gv;
+                if (tid < C) reinterpret_cast<unsigned short*>(ctl.al)[tid] = al;
+                bar_compute();
+                await(bar(B_INTER), nh & 1, dead);
+                {   // M (lanes 0-63) and -A (lanes 64-127), 32 columns of token i; their share of X
+                    const bool isq = quad < 2;
+                    float u[32], v[32];
+                    tmem_ld32(lanes + (isq ? YE : GE) + i0, u);
+                    tmem_ld32(lanes + QK + i0, v);
+                    if (!isq && (i >> 5) == half) {
+                        float diag = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) diag = (i & 31) == j ? u[j] : diag;
+                        ctl.db[i] = diag;
+                    }
+                    float G = 0.f;
+                    auto alphas = [&](int q8, float (&f)[8]) { unpack16<BF16>(ctl.al[q8], f); };
+                    if (half == 0) {
+#pragma unroll
+                        for (int q8 = 7; q8 >= 4; --q8) {
+                            float f[8];
+                            alphas(q8, f);
+#pragma unroll
+                            for (int e = 7; e >= 0; --e) {
+                                G = 8 * q8 + e == i ? 1.f : G;
+                                G *= f[e];
+                            }
+                        }
+                    }
+                    const float bi = isq ? a.scale : ctl.gt[1][i];
+#pragma unroll
+                    for (int q8 = 3; q8 >= 0; --q8) {
+                        float f[8];
+                        alphas(i0 / 8 + q8, f);
+#pragma unroll
+                        for (int e = 7; e >= 0; --e) {
+                            const int jj = 8 * q8 + e, j = i0 + jj;
+                            G = j == i ? 1.f : G;
+                            const bool on = i < n && (isq ? j <= i : j < i);
+                            const float c = on ? bi * ctl.gt[1][j] * u[jj] : 0.f;
+                            v[jj] *= isq ? c : -c;           // X
+                            u[jj] = isq ? G * c : -G * c;
+                            G *= f[e];
+                        }
+                    }
+                    unsigned char* const mp = tp + L::M + (isq ? 0 : 2 * MAT) + i * 128;
+#pragma unroll
+                    for (int q4 = 0; q4 < 4; ++q4) {
+                        uint32_t hi[4], lo[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float& x0 = u[8 * q4 + 2 * e];
+                            float& x1 = u[8 * q4 + 2 * e + 1];
+                            hi[e] = split2(x0, x1, x0, x1);
+                            lo[e] = pack2(x0, x1);
+                        }
+                        const uint32_t at = static_cast<uint32_t>(i0 / 8 + q4) ^ (i & 7);
+                        *reinterpret_cast<uint4*>(mp + at * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                        if (isq) *reinterpret_cast<uint4*>(mp + MAT + at * 16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    }
+                    if (isq) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) ctl.X[i][i0 + j + 1] = v[j];
+                    }
+                    // the products over d_v: lanes are rows of d_k (the lanes past them are left out), columns tokens
+                    const bool in = row < DK;
+#pragma unroll
+                    for (int kind = 0; kind < 3; ++kind) {
+                        float p[32];
+                        tmem_ld32(lanes + (kind == 0 ? SY : kind == 1 ? SD : DE) + i0, p);
+                        const unsigned char* x16 = kq + (kind == 0 ? 0 : 8192);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const int tok = i0 + j;
+                            const float be = ctl.gt[1][tok];
+                            p[j] = in && tok < n ? p[j] : 0.f;
+                            if (kind == 0) dq[j] = fmaf(a.scale * ctl.gt[0][tok], p[j], dq[j]);
+                            if (kind == 1) dk[j] = fmaf(-be * ctl.gt[0][tok], p[j], dk[j]);
+                            if (kind == 2) dk[j] = fmaf(be * ctl.gt[2][tok], p[j], dk[j]);
+                            const float xv = in ? __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const unsigned short*>(x16 + sw128_at(tok, row % 64))) << 16) : 0.f;
+                            p[j] *= xv;
+                        }
+                        ctl.dots[kind][quad][i0 + lane] = sum_lanes(p, lane);
+                    }
+                    fence_async();
+                    arrive(bar(B_M), lane);
+                    bar_compute();
+                    if (!isq) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            ctl.X[i][i0 + j + 1] += v[j];
+                    }
+                    if (tid < C) {
+                        const float* d0 = &ctl.dots[0][0][tid];
+                        float s[3];
+#pragma unroll
+                        for (int kind = 0; kind < 3; ++kind) s[kind] = (d0[kind * 4 * C] + d0[kind * 4 * C + C]) + (d0[kind * 4 * C + 2 * C] + d0[kind * 4 * C + 3 * C]);
+                        ctl.X[tid][0] = a.scale * s[0] - ctl.gt[1][tid] * s[1];
+                        ctl.X[C][tid + 1] = ctl.gt[1][tid] * s[2];
+                        if (tid == 0) {
+                            float e = 0.f;
+                            for (int wp = 0; wp < SW; ++wp) e += ctl.es[wp];
+                            ctl.X[C][0] = e;
+                        }
+                    }
+                    arrive(bar(B_X), lane);
+                    await(bar(B_INTRA), nh & 1, dead);
+                    tmem_ld32(lanes + IQ + i0, u);
+                    tmem_ld32(lanes + IK + i0, v);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        dq[j] += u[j];
+                        dk[j] += v[j];
+                    }
+                }
+            }
+            if (row < DK) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    unsigned char* const to = tp + L::QK + (row / 64) * 16384 + sw128_at(i0 + j, row % 64);
+                    *reinterpret_cast<__nv_bfloat16*>(to) = __float2bfloat16_rn(i0 + j < n ? dq[j] : 0.f);
+                    *reinterpret_cast<__nv_bfloat16*>(to + 8192) = __float2bfloat16_rn(i0 + j < n ? dk[j] : 0.f);
+                }
+            }
+            fence_async();
+            arrive(bar(B_OUT), lane);
+        }
+    }
+    tc_before_sync();
+    __syncthreads();
+    if (tid == 0 && ctl.dead) flag_error(a.err, ERR_TIMEOUT);
+    if (warp == 0) tmem_free(tmem, T_COLS);
+}
+
+template <int DK>
+cudaError_t grads(const GdnGradsTc& r, cudaStream_t stream) {
+    const GdnArgs& a = r.a;
+    const int nc = (a.T + C - 1) / C, nblk = (a.dv + 127) / 128;
+    const int64_t chunks = static_cast<int64_t>(a.B) * a.H * nc, items = static_cast<int64_t>(a.B) * a.Hk * nc;
+    CUtensorMap tq, tk, ty, tS, tD, te, td, tdq, tdk;
+    if (!token_map(&tq, a.q, a.token_major, a.B, a.Hk, a.T, a.dk) || !token_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk) ||
+        !token_map(&ty, r.dy, a.token_major, a.B, a.H, a.T, a.dv) || !row_map(&tS, r.S, chunks * nblk * 128, DK, 128) ||
+        !row_map(&tD, r.D, chunks * nblk * 128, DK, 128) || !row_map(&te, r.e, chunks * 2 * nblk * 128, C, 128) ||
+        !row_map(&td, r.d, chunks * 2 * nblk * 128, C, 128) || !token_map(&tdq, r.dq, a.token_major, a.B, a.Hk, a.T, a.dk) ||
+        !token_map(&tdk, r.dk, a.token_major, a.B, a.Hk, a.T, a.dk))
+        return cudaErrorInvalidValue;
+    constexpr size_t smem = grads_smem<DK>();
+    // the compute warpgroups' registers come out of what the CTA is launched with
+    static const int regs = [] {
+        cudaFuncAttributes at;
+        return cudaFuncGetAttributes(&at, k_gdn_grads_tc<DK>) == cudaSuccess ? at.numRegs : 0;
+    }();
+    if (regs * NT < 32 * (SW * GRAD_REGS + 4 * REST_REGS)) return cudaErrorInvalidConfiguration;
+    static std::atomic<unsigned long long> seen;
+    cudaError_t e = allow_smem(k_gdn_grads_tc<DK>, smem, seen);
+    if (e != cudaSuccess) return e;
+    k_gdn_grads_tc<DK><<<static_cast<unsigned>(items < 152 ? items : 152), NT, smem, stream>>>(tq, tk, ty, tS, tD, te, td, tdq, tdk, r, nc);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_gdn_grads_tc(const GdnGradsTc& r, cudaStream_t stream) {
+    return r.a.dk <= 64 ? grads<64>(r, stream) : grads<128>(r, stream);
+}
+
+}  // namespace sdm
