@@ -28,7 +28,7 @@ using namespace tc;
 using namespace gdn;
 
 constexpr int SW = 8, NT = 32 * (SW + 4);
-constexpr int GRAD_REGS = 224, REST_REGS = 56; // the split of the launch's 168 per thread // the split of the launch's 168 per thread // the split of the launch's 168 per thread // the split of the launch's 168 per thread
+constexpr int GRAD_REGS = 224, REST_REGS = 56; // the split of the launch's 168 per thread
 constexpr int XP = C + 1;                      // columns of X: -1 .. 63
 // TMEM columns
 constexpr uint32_t SY = 0, SD = 64, DE = 128, QK = 192, YE = 256, GE = 320, IQ = 384, IK = 448, T_COLS = 512;
@@ -123,8 +123,8 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
         return x;
     };
 
-    if (warp >= SW) regs_dec<REST_REGS>();
-    else regs_inc<GRAD_REGS>();
+    if (warp >= SW) {
+    regs_dec<REST_REGS>();
     if (warp == SW) {                                        // MMAs
         const uint32_t id = mma_idesc(64), idA = id | MN_A, idB = id | MN_B, idAB = id | MN_A | MN_B;
         const uint64_t q = sw128_desc(t + L::QK), k = sw128_desc(t + L::QK + 8192), qt = sw128_mn_desc(t + L::QK, 16384),
@@ -281,7 +281,9 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                 }
             }
         }
+    }
     } else {
+        regs_inc<GRAD_REGS>();
         const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane, i0 = 32 * half;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         const float* gate = reinterpret_cast<const float*>(tp + L::G);
