@@ -20,6 +20,8 @@
 // (112 KB of tiles a chunk and head at d_k = d_v = 128, and 32 KB of K and Q) and the MMAs, one after the other.
 #include "gdn_tc.cuh"
 
+#include <stddef.h>
+
 namespace sdm {
 
 namespace {
@@ -41,11 +43,11 @@ struct Tile {
                               G = M + 3 * MAT, BYTES = G + 1024;
     static constexpr uint32_t LOAD = 512 * DK + 65536 + 16384 + GATES;
 };
-enum { B_KQ = 0, B_TILE, B_INTER, B_INTRA, B_KREADY, B_M, B_X, B_OUT, B_XFREE, B_EMPTY, B_COUNT };
+enum { B_KQ = 0, B_TILE, B_INTER, B_INTRA, B_KREADY, B_M, B_READ, B_X, B_OUT, B_XFREE, B_EMPTY, B_COUNT };
 struct Ctl {
     float X[C + 1][XP];
-    float dots[3][4][C];                       // q.S dy, k.S d, k.D e of each lane quarter
-    float gt[3][C];                            // g, beta, h of the head's chunk
+    float dots[2][4][C];                       // X_{i,-1} and X_{64,j}, the share of each lane quarter
+    alignas(16) float gt[3][C];                // g, beta, h of the head's chunk
     float db[C];
     float es[SW];
     uint4 al[C / 8];
@@ -53,6 +55,7 @@ struct Ctl {
     uint32_t tmem;
     int dead;
 };
+static_assert(offsetof(Ctl, gt) % 16 == 0 && offsetof(Ctl, al) % 16 == 0 && offsetof(Ctl, bar) % 8 == 0, "alignment of the wide reads");
 template <int DK>
 constexpr size_t grads_smem() { return 1024 + Tile<DK>::BYTES + sizeof(Ctl); }
 
@@ -124,7 +127,7 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
     };
 
     if (warp >= SW) {
-    regs_dec<REST_REGS>();
+        regs_dec<REST_REGS>();
     if (warp == SW) {                                        // MMAs
         const uint32_t id = mma_idesc(64), idA = id | MN_A, idB = id | MN_B, idAB = id | MN_A | MN_B;
         const uint64_t q = sw128_desc(t + L::QK), k = sw128_desc(t + L::QK + 8192), qt = sw128_mn_desc(t + L::QK, 16384),
@@ -135,17 +138,9 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
         uint32_t ni = 0, ns = 0, nh = 0;
         for (int64_t w = blockIdx.x; w < items; w += gridDim.x) {
             if (item_of(w).n == 0) continue;
-            await(bar(B_KQ), ni & 1, dead);
-            await(bar(B_KREADY), ni & 1, dead);
-            ++ni;
-            if (elect_one()) {
-#pragma unroll 1
-                for (int kk = 0; kk < DK / 16; ++kk)
-                    mma_bf16(tmem + QK, q + (kk / 4) * 1024 + (kk % 4) * 2, k + (kk / 4) * 1024 + (kk % 4) * 2, id, kk != 0);
-            }
-            __syncwarp();
             for (int sub = 0; sub < subs; ++sub, ++ns) {
                 const uint32_t first = sub % nblk == 0 ? 0u : 1u;
+                if (first == 0 && nh > 0) await(bar(B_READ), (nh - 1) & 1, dead);   // the last head's are taken
                 await(bar(B_TILE), ns & 1, dead);
                 if (elect_one()) {
 #pragma unroll 1
@@ -165,10 +160,22 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                         for (int kk = 0; kk < 8; ++kk)
                             mma_bf16(tmem + GE, dh + (p == 2 ? 1024 : 0) + kk * 128, e + (p == 1 ? 1024 : 0) + kk * 128, idAB, first | (p | kk) != 0);
                     mma_commit(bar(B_EMPTY));
-                    if (sub % nblk == nblk - 1) mma_commit(bar(B_INTER));
                 }
                 __syncwarp();
+                if (sub == nblk - 1) {                       // first head: q.k and k.k, now that Q and K are there
+                    await(bar(B_KQ), ni & 1, dead);
+                    await(bar(B_KREADY), ni & 1, dead);
+                    ++ni;
+                    if (elect_one()) {
+#pragma unroll 1
+                        for (int kk = 0; kk < DK / 16; ++kk)
+                            mma_bf16(tmem + QK, q + (kk / 4) * 1024 + (kk % 4) * 2, k + (kk / 4) * 1024 + (kk % 4) * 2, id, kk != 0);
+                    }
+                    __syncwarp();
+                }
                 if (sub % nblk == nblk - 1) {
+                    if (elect_one()) mma_commit(bar(B_INTER));
+                    __syncwarp();
                     await(bar(B_M), nh & 1, dead);
                     ++nh;
                     if (elect_one()) {
@@ -302,17 +309,6 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                 }
                 continue;
             }
-            mbar_wait_or_dead(bar(B_KQ), ni & 1, dead);
-            ++ni;
-            if (n < C) {                                     // rows past the length: zeros, whatever was there
-                for (int p = tid; p < (C - n) * DK / 4; p += 32 * SW) {
-                    const int e = p % 2, rw = n + (p / 2) / (DK / 8), c = (p / 2) % (DK / 8);
-                    *reinterpret_cast<uint4*>(tp + L::QK + (c / 8) * 16384 + e * 8192 + rw * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
-                }
-                fence_async();
-            }
-            arrive(bar(B_KREADY), lane);
-            if (n < C) bar_compute();                        // the other warps' zeros, before q and k are read below
             float dq[32], dk[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) dq[j] = dk[j] = 0.f;
@@ -334,6 +330,18 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(B_EMPTY));
                 }
+                if (hv == 0) {
+                    mbar_wait_or_dead(bar(B_KQ), ni & 1, dead);
+                    ++ni;
+                    if (n < C) {                             // rows past the length: zeros, whatever was there
+                        for (int p = tid; p < (C - n) * DK / 4; p += 32 * SW) {
+                            const int e = p % 2, rw = n + (p / 2) / (DK / 8), c = (p / 2) % (DK / 8);
+                            *reinterpret_cast<uint4*>(tp + L::QK + (c / 8) * 16384 + e * 8192 + rw * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_async();
+                    }
+                    arrive(bar(B_KREADY), lane);
+                }
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) es += __shfl_xor_sync(0xffffffffu, es, o);
                 if (nh > 0) mbar_wait_or_dead(bar(B_XFREE), (nh - 1) & 1, dead);
@@ -354,34 +362,37 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                         for (int j = 0; j < 32; ++j) diag = (i & 31) == j ? u[j] : diag;
                         ctl.db[i] = diag;
                     }
-                    float G = 0.f;
-                    auto alphas = [&](int q8, float (&f)[8]) { unpack16<BF16>(ctl.al[q8], f); };
-                    if (half == 0) {
+                    if ((quad & 1) == 0 && half == 1) {      // tokens 0-31 have no columns 32-63
 #pragma unroll
-                        for (int q8 = 7; q8 >= 4; --q8) {
-                            float f[8];
-                            alphas(q8, f);
+                        for (int j = 0; j < 32; ++j) u[j] = v[j] = 0.f;
+                    } else {
+                        float G = 0.f;
+                        if ((quad & 1) == 1 && half == 0) {  // from the diagonal down to column 32
 #pragma unroll
-                            for (int e = 7; e >= 0; --e) {
-                                G = 8 * q8 + e == i ? 1.f : G;
-                                G *= f[e];
+                            for (int q8 = 7; q8 >= 4; --q8) {
+                                float f[8];
+                                unpack16<BF16>(ctl.al[q8], f);
+#pragma unroll
+                                for (int e = 7; e >= 0; --e) G = (8 * q8 + e == i ? 1.f : G) * f[e];
                             }
                         }
-                    }
-                    const float bi = isq ? a.scale : ctl.gt[1][i];
+                        const float bi = i < n ? (isq ? a.scale : -ctl.gt[1][i]) : 0.f;
+                        const int last = isq ? i : i - 1;
 #pragma unroll
-                    for (int q8 = 3; q8 >= 0; --q8) {
-                        float f[8];
-                        alphas(i0 / 8 + q8, f);
+                        for (int q8 = 3; q8 >= 0; --q8) {
+                            float f[8];
+                            unpack16<BF16>(ctl.al[i0 / 8 + q8], f);
+                            const float4 b0 = *reinterpret_cast<const float4*>(&ctl.gt[1][i0 + 8 * q8]), b1 = *reinterpret_cast<const float4*>(&ctl.gt[1][i0 + 8 * q8 + 4]);
+                            const float be[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
 #pragma unroll
-                        for (int e = 7; e >= 0; --e) {
-                            const int jj = 8 * q8 + e, j = i0 + jj;
-                            G = j == i ? 1.f : G;
-                            const bool on = i < n && (isq ? j <= i : j < i);
-                            const float c = on ? bi * ctl.gt[1][j] * u[jj] : 0.f;
-                            v[jj] *= isq ? c : -c;           // X
-                            u[jj] = isq ? G * c : -G * c;
-                            G *= f[e];
+                            for (int e = 7; e >= 0; --e) {
+                                const int jj = 8 * q8 + e, j = i0 + jj;
+                                G = j == i ? 1.f : G;
+                                const float c = j <= last && i < n ? bi * (be[e] * u[jj]) : 0.f;
+                                v[jj] *= c;                  // X
+                                u[jj] = G * c;               // M, or -A
+                                G *= f[e];
+                            }
                         }
                     }
                     unsigned char* const mp = tp + L::M + (isq ? 0 : 2 * MAT) + i * 128;
@@ -403,28 +414,72 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
 #pragma unroll
                         for (int j = 0; j < 32; ++j) ctl.X[i][i0 + j + 1] = v[j];
                     }
-                    // the products over d_v: lanes are rows of d_k (the lanes past them are left out), columns tokens
-                    const bool in = row < DK;
-#pragma unroll
-                    for (int kind = 0; kind < 3; ++kind) {
-                        float p[32];
-                        tmem_ld32(lanes + (kind == 0 ? SY : kind == 1 ? SD : DE) + i0, p);
-                        const unsigned char* x16 = kq + (kind == 0 ? 0 : 8192);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const int tok = i0 + j;
-                            const float be = ctl.gt[1][tok];
-                            p[j] = in && tok < n ? p[j] : 0.f;
-                            if (kind == 0) dq[j] = fmaf(a.scale * ctl.gt[0][tok], p[j], dq[j]);
-                            if (kind == 1) dk[j] = fmaf(-be * ctl.gt[0][tok], p[j], dk[j]);
-                            if (kind == 2) dk[j] = fmaf(be * ctl.gt[2][tok], p[j], dk[j]);
-                            const float xv = in ? __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const unsigned short*>(x16 + sw128_at(tok, row % 64))) << 16) : 0.f;
-                            p[j] *= xv;
-                        }
-                        ctl.dots[kind][quad][i0 + lane] = sum_lanes(p, lane);
-                    }
                     fence_async();
                     arrive(bar(B_M), lane);
+                    // the products over d_v: lanes are rows of d_k (the lanes past them are left out), columns tokens
+                    const bool in = DK == 128 || row < DK;
+                    uint32_t qc[16], kc[16];                 // this lane's q and k, two tokens in a word
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const unsigned char* x0 = kq + sw128_at(i0 + 2 * j, row % 64);
+                        const unsigned char* x1 = kq + sw128_at(i0 + 2 * j + 1, row % 64);
+                        qc[j] = *reinterpret_cast<const unsigned short*>(x0) | (static_cast<uint32_t>(*reinterpret_cast<const unsigned short*>(x1)) << 16);
+                        kc[j] = *reinterpret_cast<const unsigned short*>(x0 + 8192) | (static_cast<uint32_t>(*reinterpret_cast<const unsigned short*>(x1 + 8192)) << 16);
+                        if (!in) qc[j] = kc[j] = 0u;
+                    }
+                    auto at16 = [](const uint32_t (&w)[16], int j) { return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16); };
+                    // tokens past the length, and lanes past d_k, hold whatever was in the tiles
+                    auto only = [&](float (&p)[32]) {
+                        if (n < C || !in) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) p[j] = in && i0 + j < n ? p[j] : 0.f;
+                        }
+                    };
+                    {
+                        float p[32], c[32];
+                        tmem_ld32(lanes + SY + i0, p);
+                        only(p);
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) {
+                            const float4 g = *reinterpret_cast<const float4*>(&ctl.gt[0][i0 + j]);
+                            const float gj[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float x = a.scale * p[j + e];
+                                dq[j + e] = fmaf(gj[e], x, dq[j + e]);
+                                c[j + e] = x * at16(qc, j + e);
+                            }
+                        }
+                        tmem_ld32(lanes + SD + i0, p);
+                        only(p);
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) {
+                            const float4 g = *reinterpret_cast<const float4*>(&ctl.gt[0][i0 + j]), b4 = *reinterpret_cast<const float4*>(&ctl.gt[1][i0 + j]);
+                            const float gj[4] = {g.x, g.y, g.z, g.w}, bj[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float x = -bj[e] * p[j + e];
+                                dk[j + e] = fmaf(gj[e], x, dk[j + e]);
+                                c[j + e] = fmaf(x, at16(kc, j + e), c[j + e]);
+                            }
+                        }
+                        ctl.dots[0][quad][i0 + lane] = sum_lanes(c, lane);
+                        tmem_ld32(lanes + DE + i0, p);
+                        only(p);
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) {
+                            const float4 h4 = *reinterpret_cast<const float4*>(&ctl.gt[2][i0 + j]), b4 = *reinterpret_cast<const float4*>(&ctl.gt[1][i0 + j]);
+                            const float hj[4] = {h4.x, h4.y, h4.z, h4.w}, bj[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float x = bj[e] * p[j + e];
+                                dk[j + e] = fmaf(hj[e], x, dk[j + e]);
+                                p[j + e] = x * at16(kc, j + e);
+                            }
+                        }
+                        ctl.dots[1][quad][i0 + lane] = sum_lanes(p, lane);
+                    }
+                    arrive(bar(B_READ), lane);
                     bar_compute();
                     if (!isq) {
 #pragma unroll
@@ -432,12 +487,8 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                             ctl.X[i][i0 + j + 1] += v[j];
                     }
                     if (tid < C) {
-                        const float* d0 = &ctl.dots[0][0][tid];
-                        float s[3];
-#pragma unroll
-                        for (int kind = 0; kind < 3; ++kind) s[kind] = (d0[kind * 4 * C] + d0[kind * 4 * C + C]) + (d0[kind * 4 * C + 2 * C] + d0[kind * 4 * C + 3 * C]);
-                        ctl.X[tid][0] = a.scale * s[0] - ctl.gt[1][tid] * s[1];
-                        ctl.X[C][tid + 1] = ctl.gt[1][tid] * s[2];
+                        ctl.X[tid][0] = (ctl.dots[0][0][tid] + ctl.dots[0][1][tid]) + (ctl.dots[0][2][tid] + ctl.dots[0][3][tid]);
+                        ctl.X[C][tid + 1] = (ctl.dots[1][0][tid] + ctl.dots[1][1][tid]) + (ctl.dots[1][2][tid] + ctl.dots[1][3][tid]);
                         if (tid == 0) {
                             float e = 0.f;
                             for (int wp = 0; wp < SW; ++wp) e += ctl.es[wp];
