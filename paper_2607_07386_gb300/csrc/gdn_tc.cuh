@@ -52,21 +52,23 @@ inline bool row_map(CUtensorMap* m, const void* base, int64_t rows, int cols, in
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The next bf16 part of 32 values into 16 packed columns (and to `keep` in memory); the values keep what
-// its rounding left.
-template <bool KEEP = false>
-__device__ __forceinline__ void put_part(uint32_t taddr, float (&v)[32], uint4* keep = nullptr) {
+// The next bf16 part of 32 values into 16 packed columns (and to `keep`); the values keep what its rounding left.
+struct KeepNone {
+    __device__ __forceinline__ void operator()(int, const uint4&) const {}
+};
+template <class Keep = KeepNone>
+__device__ __forceinline__ void put_part(uint32_t taddr, float (&v)[32], Keep keep = Keep{}) {
     uint32_t u[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) u[j] = split2(v[2 * j], v[2 * j + 1], v[2 * j], v[2 * j + 1]);
     tmem_st16(taddr, u);
-    if (KEEP) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) __stcs(keep + j, make_uint4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]));
-    }
+    for (int j = 0; j < 4; ++j) keep(j, make_uint4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]));
 }
-// 32 values as two bf16 parts in memory.
-__device__ __forceinline__ void keep_parts(uint4* hi, uint4* lo, float (&v)[32]) {
+// Where the 16-byte piece `piece` of row `row` lies in a swizzled box of 128-byte rows.
+__device__ __forceinline__ uint32_t box_at(int row, int piece) { return row * 128 + ((piece ^ (row & 7)) << 4); }
+// 32 values (pieces piece0 .. + 3 of the row) as two bf16 parts in two boxes of 128 rows, one after the other.
+__device__ __forceinline__ void keep_parts(unsigned char* box, int row, int piece0, float (&v)[32]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         uint32_t u[4], w[4];
@@ -77,8 +79,9 @@ __device__ __forceinline__ void keep_parts(uint4* hi, uint4* lo, float (&v)[32])
             u[e] = split2(x, y, x, y);
             w[e] = pack2(x, y);
         }
-        __stcs(hi + j, make_uint4(u[0], u[1], u[2], u[3]));
-        __stcs(lo + j, make_uint4(w[0], w[1], w[2], w[3]));
+        unsigned char* const at = box + box_at(row, piece0 + j);
+        *reinterpret_cast<uint4*>(at) = make_uint4(u[0], u[1], u[2], u[3]);
+        *reinterpret_cast<uint4*>(at + 16384) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 __device__ __forceinline__ void put_last(uint32_t taddr, const float (&v)[32]) {
@@ -106,6 +109,12 @@ __device__ __forceinline__ void await(uint32_t bar, uint32_t parity, volatile in
     mbar_wait_or_dead(bar, parity, dead);
     __syncwarp();
     tc_after_sync();
+}
+// The same for what a warp has put into shared memory for the copies.
+__device__ __forceinline__ void hand_over(uint32_t bar, int lane) {
+    fence_async();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
 }
 // Element (row, x) of a tile of 64-value, 128-byte rows, swizzled as TMA leaves it.
 __device__ __forceinline__ uint32_t sw128_at(int row, int x) { return row * 128 + ((x * 2) ^ ((row & 7) << 4)); }

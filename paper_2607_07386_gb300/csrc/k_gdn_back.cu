@@ -34,18 +34,20 @@ constexpr uint32_t X_COL = 0, Z_COL = 64, A_COL = 128, S_COL = 256, Y_COL = 384,
 
 template <int DK>
 struct BackTile {
-    static constexpr uint32_t KQ = 0, Y = 128 * 2 * DK, M = Y + C * 256, G = M + 4 * MAT, BYTES = G + 1024;
-    static constexpr uint32_t LOAD = G + GATES;
+    static constexpr uint32_t KQ = 0, Y = 128 * 2 * DK, M = Y + C * 256, BYTES = M + 4 * MAT;
+    static constexpr uint32_t LOAD = BYTES + GATES;
     static constexpr int STAGES = 2;
+    // boxes of 128 columns on their way to memory (D per 64 of d_k, d per part), then the stages' gate products
+    static constexpr uint32_t KS = BYTES * STAGES, KE = KS + 256 * DK, G = KE + 32768, CTL = G + STAGES * GATES;
 };
-enum { B_FULL = 0, B_U = 2, B_XN, B_UP, B_S, B_DY, B_X, B_H, B_OUT, B_COUNT };
+enum { B_FULL = 0, B_U = 2, B_XN, B_UP, B_FREE, B_S, B_DY, B_X, B_H, B_KS, B_OUT, B_COUNT };
 struct BackCtl {
     unsigned long long bar[B_COUNT];
     uint32_t tmem;
     int dead;
 };
 template <int DK>
-constexpr size_t back_smem() { return 1024 + BackTile<DK>::BYTES * BackTile<DK>::STAGES + sizeof(BackCtl); }
+constexpr size_t back_smem() { return 1024 + BackTile<DK>::CTL + sizeof(BackCtl); }
 
 // Both warps of a lane quarter.
 __device__ __forceinline__ void bar_pair(int quad) {
@@ -57,14 +59,15 @@ __device__ __forceinline__ void bar_pair(int quad) {
 template <int DK>
 __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tq,
                                                     const __grid_constant__ CUtensorMap ty, const __grid_constant__ CUtensorMap tdv,
-                                                    const __grid_constant__ CUtensorMap tm, const GdnBack r, const GdnFactors f, int nc) {
+                                                    const __grid_constant__ CUtensorMap tm, const __grid_constant__ CUtensorMap tD, const __grid_constant__ CUtensorMap td,
+                                                    const GdnBack r, const GdnFactors f, int nc) {
     using L = BackTile<DK>;
     extern __shared__ unsigned char raw[];
     const GdnArgs& a = r.a;
     const uint32_t base = smem_u32(raw);
     const uint32_t ring = (base + 1023u) & ~1023u;
     unsigned char* const ringp = raw + (ring - base);
-    BackCtl& ctl = *reinterpret_cast<BackCtl*>(ringp + L::BYTES * L::STAGES);
+    BackCtl& ctl = *reinterpret_cast<BackCtl*>(ringp + L::CTL);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int b = blockIdx.z, h = blockIdx.y, col0 = blockIdx.x * 128, hk = h / (a.H / a.Hk);
     const int len = gdn_length(a, b);
@@ -155,24 +158,31 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 tma_load_4d(t + L::Y + 8192, &ty, col0 + 64, c * C, h, b, fb);
 #pragma unroll
                 for (int m = 0; m < 4; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * 4 + m) * C), fb);
-                bulk_load(t + L::G, f.gates + cid * 3 * C, GATES, fb);
+                bulk_load(ring + L::G + (it % L::STAGES) * GATES, f.gates + cid * 3 * C, GATES, fb);
             };
             int loaded = 0;
             for (; loaded < chunks && loaded < L::STAGES; ++loaded) load(loaded);
             for (int it = 0; it < chunks; ++it) {
-                mbar_wait_or_dead(bar(B_OUT), it & 1, dead); // dv of the chunk lies where its dy was
-                if (*dead) break;
                 const uint32_t t = ring + (it % L::STAGES) * L::BYTES + L::Y;
-                const int c = chunks - 1 - it;
+                const int c = chunks - 1 - it, nblk = gridDim.x, blk = blockIdx.x;
+                const int64_t cid = chain * nc + c;
+                const int rs = static_cast<int>((cid * nblk + blk) * 128), rp = static_cast<int>((cid * 2 * nblk + blk) * 128);
+                mbar_wait_or_dead(bar(B_KS), it & 1, dead);
+                if (*dead) break;
+#pragma unroll
+                for (int x = 0; x < DK / 64; ++x) tma_store_2d(&tD, ring + L::KS + x * 16384, 64 * x, rs);
+                mbar_wait_or_dead(bar(B_OUT), it & 1, dead); // d, and dv where the chunk's dy was
+                if (*dead) break;
+#pragma unroll
+                for (int p = 0; p < 2; ++p) tma_store_2d(&td, ring + L::KE + p * 16384, 0, rp + p * nblk * 128);
                 tma_store_4d(&tdv, t, col0, c * C, h, b);
                 if (col0 + 64 < a.dv) tma_store_4d(&tdv, t + 8192, col0 + 64, c * C, h, b);
                 bulk_commit();
-                if (loaded < chunks) {
-                    bulk_wait_read();
-                    mbar_wait_or_dead(bar(B_UP), it & 1, dead);
-                    if (*dead) break;
-                    load(loaded++);
-                }
+                bulk_wait_read();
+                mbar_arrive(bar(B_FREE));
+                mbar_wait_or_dead(bar(B_UP), it & 1, dead);
+                if (*dead) break;
+                if (loaded < chunks) load(loaded++);
             }
             bulk_wait();
             if (*dead)                                       // the copies in flight land before the CTA ends
@@ -185,7 +195,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
         const int i0 = 32 * half;                            // this warp's tokens of a chunk
         const bool live = col < a.dv;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
-        const int64_t per = static_cast<int64_t>(a.dk) * a.dv, dvp = static_cast<int64_t>(gridDim.x) * 128;
+        const int64_t per = static_cast<int64_t>(a.dk) * a.dv;
         constexpr int RD = DK / 2;                           // rows of d_k of a warp
         const uint32_t yat = L::Y + (row / 64) * 8192;
         float D[RD];
@@ -195,21 +205,27 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
             D[x] = r.dstate != nullptr && live && rw < a.dk ? __ldcs(r.dstate + chain * per + static_cast<int64_t>(rw) * a.dv + col) : 0.f;
         }
         auto put_state = [&](int it) {                       // D after the chunk
-            const int64_t at = ((chain * nc + chunks - 1 - it) * dvp + col) * DK + half * RD;
+            if (it > 0) mbar_wait_or_dead(bar(B_FREE), (it - 1) & 1, dead);
+            __syncwarp();
 #pragma unroll
             for (int x = 0; x < RD; x += 32) {
                 float v[32];
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = D[x + j];
-                put_part<true>(lanes + S_COL + (half * RD + x) / 2, v, reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(r.keep_D) + at + x));
+                auto keep = [&](int j, const uint4& w) {     // 8 rows of d_k
+                    const int at = half * RD + x + 8 * j;
+                    *reinterpret_cast<uint4*>(ringp + L::KS + at / 64 * 16384 + box_at(row, at % 64 / 8)) = w;
+                };
+                put_part(lanes + S_COL + (half * RD + x) / 2, v, keep);
                 put_last(lanes + S_COL + SB + (half * RD + x) / 2, v);
             }
             announce(bar(B_S), lane);
+            hand_over(bar(B_KS), lane);
         };
         auto put_dy = [&](int it) {                          // dy and g dy of the chunk
             const int s = it % L::STAGES, n = len - (chunks - 1 - it) * C;
             const unsigned char* tile = ringp + s * L::BYTES;
-            const float* gate = reinterpret_cast<const float*>(tile + L::G);
+            const float* gate = reinterpret_cast<const float*>(ringp + L::G + s * GATES);
             mbar_wait_or_dead(bar(B_FULL + s), (it / L::STAGES) & 1, dead);
             if (n < C) {                                     // K and Q rows past the length: zeros, whatever was there
                 for (int p = tid; p < (C - n) * DK / 4; p += 32 * SW) {
@@ -250,7 +266,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
             const int s = it % L::STAGES, c = chunks - 1 - it, n = len - c * C;
             const uint32_t ph = it & 1;
             unsigned char* tile = ringp + s * L::BYTES;
-            const float* gate = reinterpret_cast<const float*>(tile + L::G);
+            const float* gate = reinterpret_cast<const float*>(ringp + L::G + s * GATES);
             float u[32], w[32];
             await(bar(B_U), ph, dead);
             tmem_ld32(lanes + X_COL + i0, u);                // step 2
@@ -291,11 +307,8 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 const int i = i0 + j;
                 *reinterpret_cast<__nv_bfloat16*>(tile + yat + sw128_at(i, row % 64)) = __float2bfloat16_rn(i < n ? gate[C + i] * u[j] : 0.f);
             }
-            fence_async();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(B_OUT));
-            __nv_bfloat16* const keep = static_cast<__nv_bfloat16*>(r.keep_d) + ((chain * nc + c) * 2 * dvp + col) * C + i0;
-            keep_parts(reinterpret_cast<uint4*>(keep), reinterpret_cast<uint4*>(keep + dvp * C), u);
+            keep_parts(ringp + L::KE, row, i0 / 8, u);
+            hand_over(bar(B_OUT), lane);
             if (it + 1 < chunks) put_dy(it + 1);
             await(bar(B_UP), ph, dead);
 #pragma unroll
@@ -328,7 +341,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
 
 template <int DK>
 cudaError_t back(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap& ty, const CUtensorMap& tdv, const CUtensorMap& tm,
-                 const GdnBack& r, const GdnFactors& f, cudaStream_t stream) {
+                 const CUtensorMap& tD, const CUtensorMap& td, const GdnBack& r, const GdnFactors& f, cudaStream_t stream) {
     constexpr size_t smem = back_smem<DK>();
     // the compute warpgroups' registers come out of what the CTA is launched with
     static const int regs = [] {
@@ -339,7 +352,7 @@ cudaError_t back(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap
     static std::atomic<unsigned long long> seen;
     cudaError_t e = allow_smem(k_gdn_back<DK>, smem, seen);
     if (e != cudaSuccess) return e;
-    k_gdn_back<DK><<<dim3((r.a.dv + 127) / 128, r.a.H, r.a.B), ST, smem, stream>>>(tk, tq, ty, tdv, tm, r, f, (r.a.T + C - 1) / C);
+    k_gdn_back<DK><<<dim3((r.a.dv + 127) / 128, r.a.H, r.a.B), ST, smem, stream>>>(tk, tq, ty, tdv, tm, tD, td, r, f, (r.a.T + C - 1) / C);
     return cudaGetLastError();
 }
 
@@ -348,12 +361,14 @@ cudaError_t back(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap
 cudaError_t launch_gdn_back(const GdnBack& r, const GdnFactors& f, cudaStream_t stream) {
     const GdnArgs& a = r.a;
     const int64_t chunks = static_cast<int64_t>(a.B) * a.H * ((a.T + C - 1) / C);
-    CUtensorMap tk, tq, ty, tdv, tm;
+    const int nblk = (a.dv + 127) / 128;
+    CUtensorMap tk, tq, ty, tdv, tm, tD, td;
     if (!token_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk) || !token_map(&tq, a.q, a.token_major, a.B, a.Hk, a.T, a.dk) ||
         !token_map(&ty, r.dy, a.token_major, a.B, a.H, a.T, a.dv) || !token_map(&tdv, r.dv, a.token_major, a.B, a.H, a.T, a.dv) ||
-        !row_map(&tm, f.mat, chunks * 4 * C, C, C))
+        !row_map(&tm, f.mat, chunks * 4 * C, C, C) || !row_map(&tD, r.keep_D, chunks * nblk * 128, a.dk <= 64 ? 64 : 128, 128) ||
+        !row_map(&td, r.keep_d, chunks * 2 * nblk * 128, C, 128))
         return cudaErrorInvalidValue;
-    return a.dk <= 64 ? back<64>(tk, tq, ty, tdv, tm, r, f, stream) : back<128>(tk, tq, ty, tdv, tm, r, f, stream);
+    return a.dk <= 64 ? back<64>(tk, tq, ty, tdv, tm, tD, td, r, f, stream) : back<128>(tk, tq, ty, tdv, tm, tD, td, r, f, stream);
 }
 
 }  // namespace sdm

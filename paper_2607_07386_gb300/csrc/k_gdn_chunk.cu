@@ -307,7 +307,8 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
 // Warp 12 issues the MMAs, warp 13 the copies.
 //
 // With KEEP (for the backward) nothing is read out: the states before the chunks and e are stored instead, as
-// bf16, column by column as the threads hold them, and the state stays as it was.
+// bf16, transposed as the threads hold them, through boxes in shared memory (16-byte stores of the threads' own,
+// a row of 256 bytes apart, cost 95 us of 310 at the layer shape), and the state stays as it was.
 //
 // The chain of six stages is what bounds it, then the tensor pipe (2432 cycles of MMAs per chunk at d_k =
 // 128).
@@ -322,34 +323,37 @@ constexpr int NH = 3;                          // bf16 parts of h w
 constexpr uint32_t X_COL = 0, Y_COL = 128, S_COL = 192, R_COL = S_COL + 128, T_COLS = 512;
 static_assert(R_COL + 32 * NS <= T_COLS && 32 * NH <= 128 && 64 * NS <= 128, "TMEM columns");
 
-template <int DK>
+template <int DK, bool KEEP>
 struct ScanTile {
     static constexpr uint32_t KQ = 0, V = 128 * 2 * DK, M = V + C * 256, G = M + 3 * MAT, BYTES = G + 1024;
-    static constexpr uint32_t LOAD = G + GATES;
-    static constexpr int STAGES = 3;
+    static constexpr uint32_t LOAD = KEEP ? 128 * DK + C * 256 + 2 * MAT + GATES : G + GATES;     // KEEP: no Q, no P
+    static constexpr int STAGES = KEEP ? 2 : 3;
+    // KEEP: boxes of 128 columns on their way to memory, S per 64 of d_k, e per part
+    static constexpr uint32_t KS = BYTES * STAGES, KE = KS + 256 * DK, CTL = KEEP ? KE + 32768 : KS;
 };
 // Barriers.  Completed by MMAs or copies: a stage's tile; U; Q S; beta r N; h w K; w P.  Completed by warps:
-// operands in TMEM, Q S taken out, y in shared memory.
-enum { B_FULL = 0, B_U = 3, B_QS, B_RN, B_HK, B_WP, B_S, B_R, B_H, B_W, B_TAKEN, B_Y, B_COUNT };
+// operands in TMEM, S and e to be kept in shared memory, Q S taken out, y in shared memory; by the copying
+// thread: the kept ones have left it.
+enum { B_FULL = 0, B_U = 3, B_QS, B_RN, B_HK, B_WP, B_S, B_R, B_H, B_W, B_KS, B_KE, B_TAKEN, B_Y, B_FREE, B_COUNT };
 struct ScanCtl {
     unsigned long long bar[B_COUNT];
     uint32_t tmem;
     int dead;
 };
-template <int DK>
-constexpr size_t scan_smem() { return 1024 + ScanTile<DK>::BYTES * ScanTile<DK>::STAGES + sizeof(ScanCtl); }
+template <int DK, bool KEEP>
+constexpr size_t scan_smem() { return 1024 + ScanTile<DK, KEEP>::CTL + sizeof(ScanCtl); }
 
 template <int DK, bool KEEP>
 __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tq,
                                                     const __grid_constant__ CUtensorMap tv, const __grid_constant__ CUtensorMap ty,
                                                     const __grid_constant__ CUtensorMap tm, const GdnScan r, const GdnFactors f, int nc) {
-    using L = ScanTile<DK>;
+    using L = ScanTile<DK, KEEP>;
     extern __shared__ unsigned char raw[];
     const GdnArgs& a = r.a;
     const uint32_t base = smem_u32(raw);
     const uint32_t ring = (base + 1023u) & ~1023u;
     unsigned char* const ringp = raw + (ring - base);
-    ScanCtl& ctl = *reinterpret_cast<ScanCtl*>(ringp + L::BYTES * L::STAGES);
+    ScanCtl& ctl = *reinterpret_cast<ScanCtl*>(ringp + L::CTL);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int b = blockIdx.z, h = blockIdx.y, col0 = blockIdx.x * 128, hk = h / (a.H / a.Hk);
     const int len = gdn_length(a, b);
@@ -359,7 +363,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
     auto bar = [&](int i) { return bars + 8 * i; };
     if (tid == 0) {
         ctl.dead = 0;
-        for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), i < B_S ? 1 : i == B_TAKEN || i == B_Y ? OW : SW);
+        for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), i < B_S || i == B_FREE ? 1 : i == B_TAKEN || i == B_Y ? OW : SW);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         fence_async();
     }
@@ -439,23 +443,39 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
 #pragma unroll
                 for (int x = 0; x < DK / 64; ++x) {
                     tma_load_4d(t + L::KQ + x * 16384, &tk, 64 * x, c * C, hk, b, fb);
-                    tma_load_4d(t + L::KQ + x * 16384 + 8192, &tq, 64 * x, c * C, hk, b, fb);
+                    if (!KEEP) tma_load_4d(t + L::KQ + x * 16384 + 8192, &tq, 64 * x, c * C, hk, b, fb);
                 }
                 tma_load_4d(t + L::V, &tv, col0, c * C, h, b, fb);
                 tma_load_4d(t + L::V + 8192, &tv, col0 + 64, c * C, h, b, fb);
 #pragma unroll
-                for (int m = 0; m < 3; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * f.mats + m) * C), fb);
+                for (int m = 0; m < (KEEP ? 2 : 3); ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * f.mats + m) * C), fb);
                 bulk_load(t + L::G, f.gates + cid * 3 * C, GATES, fb);
             };
             int loaded = 0;
             for (; loaded < chunks && loaded < L::STAGES; ++loaded) load(loaded);
             for (int c = 0; c < chunks; ++c) {
-                mbar_wait_or_dead(bar(KEEP ? B_HK : B_Y), c & 1, dead);    // y of chunk c lies where its v was
-                if (*dead) break;
-                if (KEEP) {
+                if (KEEP) {                                  // S and e on their way, then the next tile
+                    const int64_t cid = chain * nc + c;
+                    const int nblk = gridDim.x, blk = blockIdx.x;
+                    const int rs = static_cast<int>((cid * nblk + blk) * 128), rp = static_cast<int>((cid * 2 * nblk + blk) * 128);
+                    mbar_wait_or_dead(bar(B_KS), c & 1, dead);
+                    if (*dead) break;
+#pragma unroll
+                    for (int x = 0; x < DK / 64; ++x) tma_store_2d(&tq, ring + L::KS + x * 16384, 64 * x, rs);
+                    mbar_wait_or_dead(bar(B_KE), c & 1, dead);
+                    if (*dead) break;
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) tma_store_2d(&ty, ring + L::KE + p * 16384, 0, rp + p * nblk * 128);
+                    bulk_commit();
+                    bulk_wait_read();
+                    mbar_arrive(bar(B_FREE));
+                    mbar_wait_or_dead(bar(B_HK), c & 1, dead);
+                    if (*dead) break;
                     if (loaded < chunks) load(loaded++);
                     continue;
                 }
+                mbar_wait_or_dead(bar(B_Y), c & 1, dead);    // y of chunk c lies where its v was
+                if (*dead) break;
                 const uint32_t t = ring + (c % L::STAGES) * L::BYTES + L::V;
                 tma_store_4d(&ty, t, col0, c * C, h, b);
                 if (col0 + 64 < a.dv) tma_store_4d(&ty, t + 8192, col0 + 64, c * C, h, b);
@@ -525,8 +545,6 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         const int64_t per = static_cast<int64_t>(a.dk) * a.dv;
         float* st = const_cast<float*>(KEEP ? r.state_in : r.state) + chain * per + col;
-        // saved rows of this column: [chain][chunk][column][d_k], [chain][chunk][part][column][tokens]
-        const int64_t dvp = static_cast<int64_t>(gridDim.x) * 128;
         constexpr int RD = DK / 2;                           // rows of d_k of a warp
         float S[RD];
         if (chunks > 0) {
@@ -537,14 +555,18 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
             }
         }
         auto put_state = [&](int next) {                     // S before chunk `next`
+            if (KEEP && next > 0) mbar_wait_or_dead(bar(B_FREE), (next - 1) & 1, dead);
+            __syncwarp();
 #pragma unroll
             for (int x = 0; x < RD; x += 32) {
                 float v[32];
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = S[x + j];
-                uint4* const keep = KEEP ? reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(r.keep_S) +
-                                                                    ((chain * nc + next) * dvp + col) * DK + half * RD + x) : nullptr;
-                put_part<KEEP>(lanes + S_COL + (half * RD + x) / 2, v, keep);
+                auto keep = [&](int j, const uint4& w) {     // 8 rows of d_k
+                    const int at = half * RD + x + 8 * j;
+                    if (KEEP) *reinterpret_cast<uint4*>(ringp + L::KS + at / 64 * 16384 + box_at(row, at % 64 / 8)) = w;
+                };
+                put_part(lanes + S_COL + (half * RD + x) / 2, v, keep);
                 put_last(lanes + S_COL + SB + (half * RD + x) / 2, v);
             }
             if (len - next * C < C) {                        // K rows past the length: zeros, whatever was there
@@ -558,6 +580,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 __syncwarp();
             }
             announce(bar(B_S), lane);
+            if (KEEP) hand_over(bar(B_KS), lane);
         };
         const uint32_t vat = L::V + (row / 64) * 8192;
         if (chunks > 0) put_state(0);
@@ -622,8 +645,8 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
             put_last(lanes + S_COL + 64 + i0 / 2, u);
             announce(bar(B_H), lane);
             if (KEEP) {
-                __nv_bfloat16* const keep = static_cast<__nv_bfloat16*>(r.keep_e) + ((chain * nc + c) * 2 * dvp + col) * C + i0;
-                keep_parts(reinterpret_cast<uint4*>(keep), reinterpret_cast<uint4*>(keep + dvp * C), w);
+                keep_parts(ringp + L::KE, row, i0 / 8, w);
+                hand_over(bar(B_KE), lane);
             } else {
                 put_part(lanes + R_COL + i0 / 2, w);
                 put_last(lanes + R_COL + 32 + i0 / 2, w);
@@ -666,7 +689,7 @@ cudaError_t factors(const CUtensorMap& tk, const CUtensorMap& tq, const GdnArgs&
 template <int DK, bool KEEP>
 cudaError_t scan(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap& tv, const CUtensorMap& ty, const CUtensorMap& tm, const GdnScan& s,
                  const GdnFactors& f, cudaStream_t stream) {
-    constexpr size_t smem = scan_smem<DK>();
+    constexpr size_t smem = scan_smem<DK, KEEP>();
     // the compute warpgroups' registers come out of what the CTA is launched with
     static const int regs = [] {
         cudaFuncAttributes at;
@@ -699,11 +722,17 @@ cudaError_t launch_gdn_scan(const GdnScan& s, const GdnFactors& f, cudaStream_t 
     const GdnArgs& a = s.a;
     const int64_t chunks = static_cast<int64_t>(a.B) * a.H * ((a.T + C - 1) / C);
     CUtensorMap tk, tq, tv, ty, tm;
-    if (!token_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk) || !token_map(&tq, a.q, a.token_major, a.B, a.Hk, a.T, a.dk) ||
-        !token_map(&tv, a.v, a.token_major, a.B, a.H, a.T, a.dv) || !token_map(&ty, s.keep_S != nullptr ? a.v : s.y, a.token_major, a.B, a.H, a.T, a.dv) || !row_map(&tm, f.mat, chunks * f.mats * C, C, C))
-        return cudaErrorInvalidValue;
-    if (s.keep_S != nullptr)
+    if (s.keep_S != nullptr) {                  // the boxes go where q and y are otherwise
+        const int nblk = (a.dv + 127) / 128, dkp = a.dk <= 64 ? 64 : 128;
+        if (!token_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk) || !row_map(&tq, s.keep_S, chunks * nblk * 128, dkp, 128) ||
+            !token_map(&tv, a.v, a.token_major, a.B, a.H, a.T, a.dv) || !row_map(&ty, s.keep_e, chunks * 2 * nblk * 128, C, 128) ||
+            !row_map(&tm, f.mat, chunks * f.mats * C, C, C))
+            return cudaErrorInvalidValue;
         return a.dk <= 64 ? scan<64, true>(tk, tq, tv, ty, tm, s, f, stream) : scan<128, true>(tk, tq, tv, ty, tm, s, f, stream);
+    }
+    if (!token_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk) || !token_map(&tq, a.q, a.token_major, a.B, a.Hk, a.T, a.dk) ||
+        !token_map(&tv, a.v, a.token_major, a.B, a.H, a.T, a.dv) || !token_map(&ty, s.y, a.token_major, a.B, a.H, a.T, a.dv) || !row_map(&tm, f.mat, chunks * f.mats * C, C, C))
+        return cudaErrorInvalidValue;
     return a.dk <= 64 ? scan<64, false>(tk, tq, tv, ty, tm, s, f, stream) : scan<128, false>(tk, tq, tv, ty, tm, s, f, stream);
 }
 

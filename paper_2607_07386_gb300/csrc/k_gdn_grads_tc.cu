@@ -200,15 +200,23 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
     } else if (warp == SW + 1) {                             // copies
         if (lane == 0) {
             uint32_t ni = 0, ns = 0;
+            Item last{0, 0, 0, 0};                           // whose dq and dk are still to be stored
+            auto store = [&]() {                             // they lie where its q and k were
+                mbar_wait_or_dead(bar(B_OUT), (ni - 1) & 1, dead);
+                if (*dead) return;
+#pragma unroll
+                for (int i = 0; i < DK / 64; ++i) {
+                    if (64 * i < a.dk) {
+                        tma_store_4d(&tdq, t + L::QK + i * 16384, 64 * i, last.c * C, last.hk, last.b);
+                        tma_store_4d(&tdk, t + L::QK + i * 16384 + 8192, 64 * i, last.c * C, last.hk, last.b);
+                    }
+                }
+                bulk_commit();
+                bulk_wait_read();
+            };
             for (int64_t w = blockIdx.x; w < items && !*dead; w += gridDim.x) {
                 const Item x = item_of(w);
                 if (x.n == 0) continue;
-                mbar_expect_tx(bar(B_KQ), 256 * DK);
-#pragma unroll
-                for (int i = 0; i < DK / 64; ++i) {
-                    tma_load_4d(t + L::QK + i * 16384, &tq, 64 * i, x.c * C, x.hk, x.b, bar(B_KQ));
-                    tma_load_4d(t + L::QK + i * 16384 + 8192, &tk, 64 * i, x.c * C, x.hk, x.b, bar(B_KQ));
-                }
                 for (int sub = 0; sub < subs; ++sub, ++ns) {
                     const int h = x.hk * group + sub / nblk, blk = sub % nblk;
                     const int64_t cid = (static_cast<int64_t>(x.b) * a.H + h) * nc + x.c;
@@ -230,22 +238,29 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
 #pragma unroll
                     for (int i = 0; i < DK / 64; ++i) tma_load_2d(t + L::D + i * 16384, &tD, 64 * i, rs, bar(B_TILE));
                     bulk_load(t + L::G, r.gates + cid * 3 * C, GATES, bar(B_TILE));
-                }
-                mbar_wait_or_dead(bar(B_OUT), ni & 1, dead);
-                ++ni;
-                if (*dead) break;
+                    if (sub == 0) {                          // Q and K, once the last chunk's outputs have left their place
+                        if (ni > 0) store();
+                        if (*dead) {
+                            ++ns;
+                            break;
+                        }
+                        mbar_expect_tx(bar(B_KQ), 256 * DK);
 #pragma unroll
-                for (int i = 0; i < DK / 64; ++i) {          // dq and dk lie where q and k were
-                    if (64 * i < a.dk) {
-                        tma_store_4d(&tdq, t + L::QK + i * 16384, 64 * i, x.c * C, x.hk, x.b);
-                        tma_store_4d(&tdk, t + L::QK + i * 16384 + 8192, 64 * i, x.c * C, x.hk, x.b);
+                        for (int i = 0; i < DK / 64; ++i) {
+                            tma_load_4d(t + L::QK + i * 16384, &tq, 64 * i, x.c * C, x.hk, x.b, bar(B_KQ));
+                            tma_load_4d(t + L::QK + i * 16384 + 8192, &tk, 64 * i, x.c * C, x.hk, x.b, bar(B_KQ));
+                        }
+                        last = x;
+                        ++ni;
                     }
                 }
-                bulk_commit();
-                bulk_wait_read();
             }
+            if (ni > 0 && !*dead) store();
             bulk_wait();
-            if (*dead && ns > 0) mbar_wait(bar(B_TILE), (ns - 1) & 1);   // the copies in flight land before the CTA ends
+            if (*dead) {                                     // the copies in flight land before the CTA ends
+                if (ns > 0) mbar_wait(bar(B_TILE), (ns - 1) & 1);
+                if (ni > 0) mbar_wait(bar(B_KQ), (ni - 1) & 1);
+            }
         }
     } else if (warp > SW + 1) {                              // dalpha, dbeta: column j = tj - 1, then token tj
         const int tj = tid - 32 * (SW + 2);
