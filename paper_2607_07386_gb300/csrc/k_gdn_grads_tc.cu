@@ -31,21 +31,22 @@ using namespace gdn;
 
 constexpr int SW = 8, NT = 32 * (SW + 4);
 constexpr int GRAD_REGS = 224, REST_REGS = 56; // the split of the launch's 168 per thread
-constexpr int XP = C + 1;                      // columns of X: -1 .. 63
+// X below its diagonal, row by row: row i (0 .. 64) has columns -1 .. i - 1
+__device__ __forceinline__ constexpr int x_at(int i, int col) { return i * (i + 1) / 2 + col; }      // column j: col = j + 1
 // TMEM columns
 constexpr uint32_t SY = 0, SD = 64, DE = 128, QK = 192, YE = 256, GE = 320, IQ = 384, IK = 448, T_COLS = 512;
 
 template <int DK>
 struct Tile {
-    // per 64 values of d_k: 64 rows of Q, 64 of K.  The d tile has 16 KB before it and the dy tile 8 KB after
+    // per 64 values of d_k: 64 rows of Q, 64 of K.  M: M in two parts, -A; then dq and dk on their way to memory.  The d tile has 16 KB before it and the dy tile 8 KB after
     // it that the other half of the lanes of their products reads.
     static constexpr uint32_t QK = 0, S = 128 * 2 * DK, D = S + 256 * DK, E = D + 256 * DK, DT = E + 32768, Y = DT + 32768, M = Y + 16384,
-                              G = M + 3 * MAT, BYTES = G + 1024;
+                              G = M + 4 * MAT, BYTES = G + 1024;
     static constexpr uint32_t LOAD = 512 * DK + 65536 + 16384 + GATES;
 };
-enum { B_KQ = 0, B_TILE, B_INTER, B_INTRA, B_KREADY, B_M, B_READ, B_X, B_OUT, B_XFREE, B_EMPTY, B_COUNT };
+enum { B_KQ = 0, B_TILE, B_INTER, B_INTRA, B_KREADY, B_M, B_READ, B_X, B_KFREE, B_OUT, B_XFREE, B_EMPTY, B_MFREE, B_COUNT };
 struct Ctl {
-    float X[C + 1][XP];
+    float X[(C + 1) * (C + 2) / 2];
     float dots[2][4][C];                       // X_{i,-1} and X_{64,j}, the share of each lane quarter
     alignas(16) float gt[3][C];                // g, beta, h of the head's chunk
     float db[C];
@@ -100,7 +101,7 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
     auto bar = [&](int i) { return bars + 8 * i; };
     if (tid == 0) {
         ctl.dead = 0;
-        for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), i < B_KREADY ? 1 : i == B_XFREE ? 2 : i == B_EMPTY ? SW + 1 : SW);
+        for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), i < B_KREADY ? 1 : i == B_XFREE ? 2 : i == B_EMPTY ? SW + 1 : i == B_MFREE ? 1 : SW);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         fence_async();
     }
@@ -201,18 +202,19 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
         if (lane == 0) {
             uint32_t ni = 0, ns = 0;
             Item last{0, 0, 0, 0};                           // whose dq and dk are still to be stored
-            auto store = [&]() {                             // they lie where its q and k were
+            auto store = [&]() {                             // they lie where M and A were
                 mbar_wait_or_dead(bar(B_OUT), (ni - 1) & 1, dead);
                 if (*dead) return;
 #pragma unroll
                 for (int i = 0; i < DK / 64; ++i) {
                     if (64 * i < a.dk) {
-                        tma_store_4d(&tdq, t + L::QK + i * 16384, 64 * i, last.c * C, last.hk, last.b);
-                        tma_store_4d(&tdk, t + L::QK + i * 16384 + 8192, 64 * i, last.c * C, last.hk, last.b);
+                        tma_store_4d(&tdq, t + L::M + i * 8192, 64 * i, last.c * C, last.hk, last.b);
+                        tma_store_4d(&tdk, t + L::M + 16384 + i * 8192, 64 * i, last.c * C, last.hk, last.b);
                     }
                 }
                 bulk_commit();
                 bulk_wait_read();
+                mbar_arrive(bar(B_MFREE));
             };
             for (int64_t w = blockIdx.x; w < items && !*dead; w += gridDim.x) {
                 const Item x = item_of(w);
@@ -238,18 +240,15 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
 #pragma unroll
                     for (int i = 0; i < DK / 64; ++i) tma_load_2d(t + L::D + i * 16384, &tD, 64 * i, rs, bar(B_TILE));
                     bulk_load(t + L::G, r.gates + cid * 3 * C, GATES, bar(B_TILE));
-                    if (sub == 0) {                          // Q and K, once the last chunk's outputs have left their place
-                        if (ni > 0) store();
-                        if (*dead) {
-                            ++ns;
-                            break;
-                        }
+                    if (sub == 0) {                          // Q and K, once the last chunk's are done with
+                        if (ni > 0) mbar_wait_or_dead(bar(B_KFREE), (ni - 1) & 1, dead);
                         mbar_expect_tx(bar(B_KQ), 256 * DK);
 #pragma unroll
                         for (int i = 0; i < DK / 64; ++i) {
                             tma_load_4d(t + L::QK + i * 16384, &tq, 64 * i, x.c * C, x.hk, x.b, bar(B_KQ));
                             tma_load_4d(t + L::QK + i * 16384 + 8192, &tk, 64 * i, x.c * C, x.hk, x.b, bar(B_KQ));
                         }
+                        if (ni > 0) store();
                         last = x;
                         ++ni;
                     }
@@ -274,26 +273,39 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                 if (x.n > 0) {
                     mbar_wait_or_dead(bar(B_X), nh & 1, dead);
                     ++nh;
-                    const unsigned short* al = reinterpret_cast<const unsigned short*>(ctl.al);
-                    auto alpha = [&](int i) { return __uint_as_float(static_cast<uint32_t>(al[i]) << 16); };
-                    float acc = ctl.X[C - 1][tj] + ctl.X[C][tj];
-                    ctl.X[C - 1][tj] = acc;
-#pragma unroll 8
-                    for (int i = C - 2; i >= 0; --i) {
-                        acc = fmaf(alpha(i + 1), acc, ctl.X[i][tj]);
-                        if (i >= tj) ctl.X[i][tj] = acc;
+                    // blocks of eight rows, read before any of them is written: the loads do not wait for each other
+                    float acc = ctl.X[x_at(C, tj)], next = 1.f;              // the end's row; alpha of the row below
+#pragma unroll 1
+                    for (int q8 = C / 8 - 1; q8 >= tj / 8; --q8) {
+                        float al[8], v[8];
+                        unpack16<BF16>(ctl.al[q8], al);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = 8 * q8 + e >= tj ? ctl.X[x_at(8 * q8 + e, tj)] : 0.f;
+#pragma unroll
+                        for (int e = 7; e >= 0; --e) {
+                            acc = fmaf(next, acc, v[e]);
+                            next = al[e];
+                            if (8 * q8 + e >= tj) ctl.X[x_at(8 * q8 + e, tj)] = acc;
+                        }
                     }
                     float p = 1.f;
-#pragma unroll 8
-                    for (int i = 0; i < C; ++i) {
-                        if (i >= tj) {
-                            ctl.X[i][tj] *= p;
-                            p *= alpha(i);
+#pragma unroll 1
+                    for (int q8 = tj / 8; q8 < C / 8; ++q8) {
+                        float al[8], v[8];
+                        unpack16<BF16>(ctl.al[q8], al);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = 8 * q8 + e >= tj ? ctl.X[x_at(8 * q8 + e, tj)] : 0.f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            if (8 * q8 + e >= tj) {
+                                ctl.X[x_at(8 * q8 + e, tj)] = v[e] * p;
+                                p *= al[e];
+                            }
                         }
                     }
                     asm volatile("bar.sync 2, 64;\n" ::: "memory");
 #pragma unroll 8
-                    for (int i = 0; i < C; ++i) s += i <= tj ? ctl.X[tj][i] : 0.f;
+                    for (int i = 0; i < C; ++i) s += i <= tj ? ctl.X[x_at(tj, i)] : 0.f;
                     db = ctl.db[tj];
                     arrive(bar(B_XFREE), lane);
                 }
@@ -365,6 +377,7 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                 if (tid < 3 * C) (&ctl.gt[0][0])[tid] = gv;
                 if (tid < C) reinterpret_cast<unsigned short*>(ctl.al)[tid] = al;
                 bar_compute();
+                if (hv == 0 && ni > 1) mbar_wait_or_dead(bar(B_MFREE), ni & 1, dead);   // the last outputs have left M's place
                 await(bar(B_INTER), nh & 1, dead);
                 {   // M (lanes 0-63) and -A (lanes 64-127), 32 columns of token i; their share of X
                     const bool isq = quad < 2;
@@ -427,7 +440,8 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                     }
                     if (isq) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) ctl.X[i][i0 + j + 1] = v[j];
+                        for (int j = 0; j < 32; ++j)
+                            if (i0 + j < i) ctl.X[x_at(i, i0 + j + 1)] = v[j];
                     }
                     fence_async();
                     arrive(bar(B_M), lane);
@@ -499,19 +513,20 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                     if (!isq) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
-                            ctl.X[i][i0 + j + 1] += v[j];
+                            if (i0 + j < i) ctl.X[x_at(i, i0 + j + 1)] += v[j];
                     }
                     if (tid < C) {
-                        ctl.X[tid][0] = (ctl.dots[0][0][tid] + ctl.dots[0][1][tid]) + (ctl.dots[0][2][tid] + ctl.dots[0][3][tid]);
-                        ctl.X[C][tid + 1] = (ctl.dots[1][0][tid] + ctl.dots[1][1][tid]) + (ctl.dots[1][2][tid] + ctl.dots[1][3][tid]);
+                        ctl.X[x_at(tid, 0)] = (ctl.dots[0][0][tid] + ctl.dots[0][1][tid]) + (ctl.dots[0][2][tid] + ctl.dots[0][3][tid]);
+                        ctl.X[x_at(C, tid + 1)] = (ctl.dots[1][0][tid] + ctl.dots[1][1][tid]) + (ctl.dots[1][2][tid] + ctl.dots[1][3][tid]);
                         if (tid == 0) {
                             float e = 0.f;
                             for (int wp = 0; wp < SW; ++wp) e += ctl.es[wp];
-                            ctl.X[C][0] = e;
+                            ctl.X[x_at(C, 0)] = e;
                         }
                     }
                     arrive(bar(B_X), lane);
                     await(bar(B_INTRA), nh & 1, dead);
+                    if (hv == group - 1) arrive(bar(B_KFREE), lane);         // q and k are done with
                     tmem_ld32(lanes + IQ + i0, u);
                     tmem_ld32(lanes + IK + i0, v);
 #pragma unroll
@@ -524,9 +539,9 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
             if (row < DK) {
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
-                    unsigned char* const to = tp + L::QK + (row / 64) * 16384 + sw128_at(i0 + j, row % 64);
+                    unsigned char* const to = tp + L::M + (row / 64) * 8192 + sw128_at(i0 + j, row % 64);
                     *reinterpret_cast<__nv_bfloat16*>(to) = __float2bfloat16_rn(i0 + j < n ? dq[j] : 0.f);
-                    *reinterpret_cast<__nv_bfloat16*>(to + 8192) = __float2bfloat16_rn(i0 + j < n ? dk[j] : 0.f);
+                    *reinterpret_cast<__nv_bfloat16*>(to + 16384) = __float2bfloat16_rn(i0 + j < n ? dk[j] : 0.f);
                 }
             }
             fence_async();
