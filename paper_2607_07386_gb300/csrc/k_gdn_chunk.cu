@@ -28,7 +28,7 @@ using namespace gdn;
 //
 // N is solved for in fp32 by blocks of 16: the diagonal blocks by a column per thread in registers, then
 // the block diagonals below in order, with Z_ii = (I + B_ii beta)^-1 = I + N_ii beta:
-//   N_ij = -Z_ii (B_ij + sum_{j <= k < i} B_ik beta N_kj),  a warp per 16 x 16 product, a lane per
+//   N_ij = -Z_ii sum_{j <= k < i} B_ik Y_kj,  Y = I + beta N,  a warp per 16 x 16 product, a lane per
 // 4 x 2 outputs (one 16-byte and one 8-byte shared-memory read per 8 multiply-adds; B and Z_ii lie
 // transposed for that).  Shared-memory reads bound the kernel: with 4 x 1 outputs per thread they
 // kept the pipe 80% busy.  Eliminating whole columns of 64 in registers was slower still: 2016 unrolled
@@ -47,7 +47,7 @@ struct FactorSmem {
 // The K and Q tiles make room for these once the MMAs have read them.
 struct FactorLate {
     float Bt[C][C];                           // B transposed
-    float N[C][LP];                           // below and on the diagonal
+    float Y[C][LP];                           // on and below the diagonal; four of the blocks above hold N_ii
     float Zt[C][BL];                          // Z_ii transposed: [16 block + column][row]
     float X[NB][BL][BL + 4];
 };
@@ -57,12 +57,12 @@ struct FactorSize {
     static constexpr size_t BYTES = 1024 + TILE + sizeof(FactorSmem);
 };
 
-// acc[r][c] += sum_k At[k][4 (lane / 8) + r] x_k B[k][2 (lane % 8) + c] over 16 k, B the sum of `terms`
-// blocks, x_k = 1 without `scale`.
-__device__ __forceinline__ void block_mul(const float* At, int lda, const float* B, int ldb, int terms, int term, const float* scale,
-                                          float (&acc)[4][2], int lane) {
+// acc[r][c] = sum_k At[k][4 (lane / 8) + r] B[k][2 (lane % 8) + c] over 16 k, B the sum of `terms` blocks.
+__device__ __forceinline__ void block_mul(const float* At, int lda, const float* B, int ldb, int terms, int term, float (&acc)[4][2], int lane) {
     const float* ap = At + 4 * (lane >> 3);
     const float* bp = B + 2 * (lane & 7);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc[r][0] = acc[r][1] = 0.f;
 #pragma unroll 4
     for (int k = 0; k < BL; ++k) {
         const float4 a = *reinterpret_cast<const float4*>(ap + k * lda);
@@ -72,16 +72,15 @@ __device__ __forceinline__ void block_mul(const float* At, int lda, const float*
             b.x += o.x;
             b.y += o.y;
         }
-        if (scale != nullptr) {
-            b.x *= scale[k];
-            b.y *= scale[k];
-        }
         acc[0][0] = fmaf(a.x, b.x, acc[0][0]); acc[0][1] = fmaf(a.x, b.y, acc[0][1]);
         acc[1][0] = fmaf(a.y, b.x, acc[1][0]); acc[1][1] = fmaf(a.y, b.y, acc[1][1]);
         acc[2][0] = fmaf(a.z, b.x, acc[2][0]); acc[2][1] = fmaf(a.z, b.y, acc[2][1]);
         acc[3][0] = fmaf(a.w, b.x, acc[3][0]); acc[3][1] = fmaf(a.w, b.y, acc[3][1]);
     }
 }
+// Where the diagonal block b of N is kept: (0, b), or (1, 2) for the first.
+__device__ __forceinline__ int diag_row(int b) { return b == 0 ? BL : 0; }
+__device__ __forceinline__ int diag_col(int b) { return b == 0 ? 2 * BL : b * BL; }
 
 template <int DK>
 __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tq,
@@ -236,54 +235,63 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
             }
         }
         const float be = sm.be[tid];
+        const int dr = diag_row(o / BL), dc = diag_col(o / BL);
 #pragma unroll
-        for (int j = 0; j < BL; ++j) lt.N[o + j][o + c] = z[j];
+        for (int j = 0; j < BL; ++j) {
+            lt.Y[dr + j][dc + c] = z[j];
+            lt.Y[o + j][o + c] = j == c ? 1.f : sm.be[o + j] * z[j];
+        }
 #pragma unroll
         for (int j = 0; j < BL; j += 4)
             *reinterpret_cast<float4*>(&lt.Zt[tid][j]) = make_float4(j == c ? 1.f : be * z[j], j + 1 == c ? 1.f : be * z[j + 1],
                                                                      j + 2 == c ? 1.f : be * z[j + 2], j + 3 == c ? 1.f : be * z[j + 3]);
     }
     __syncthreads();
+    char* const mat = static_cast<char*>(f.mat) + cid * f.mats * MAT;
+    {   // N's diagonal blocks as upper and lower parts, half a row a thread, and zeros to the right of them
+        const int r = tid >> 1, bl = r / BL, c0 = (tid & 1) * 8;
+        float v[8];
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c0 + e < r % BL ? lt.Y[diag_row(bl) + r % BL][diag_col(bl) + c0 + e] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            hi[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
+            lo[e] = pack2(v[2 * e], v[2 * e + 1]);
+        }
+        char* const at = mat + (r * C + bl * BL + c0) * 2;
+        *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(at + MAT) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        for (int k = bl + 1; k < NB; ++k) {
+            *reinterpret_cast<uint4*>(at + (k - bl) * BL * 2) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(at + MAT + (k - bl) * BL * 2) = make_uint4(0, 0, 0, 0);
+        }
+    }
     const int lane = tid & 31, br = 4 * (lane >> 3), bc = 2 * (lane & 7);
 #pragma unroll
     for (int d = 1; d < NB; ++d) {                                            // blocks (j + d, j)
         if (warp < (NB - d) * d) {                                            // warp: block j = warp / d, its term k = j + warp % d
             const int j = warp / d, k = j + warp % d;
             float acc[4][2];
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {                                     // the term of the unit diagonal
-                const float4 x = *reinterpret_cast<const float4*>(&lt.Bt[j * BL + bc + c][(j + d) * BL + br]);
-                acc[0][c] = k == j ? x.x : 0.f; acc[1][c] = k == j ? x.y : 0.f;
-                acc[2][c] = k == j ? x.z : 0.f; acc[3][c] = k == j ? x.w : 0.f;
-            }
-            block_mul(&lt.Bt[k * BL][(j + d) * BL], C, &lt.N[k * BL][j * BL], LP, 1, 0, &sm.be[k * BL], acc, lane);
+            block_mul(&lt.Bt[k * BL][(j + d) * BL], C, &lt.Y[k * BL][j * BL], LP, 1, 0, acc, lane);
 #pragma unroll
             for (int r = 0; r < 4; ++r) *reinterpret_cast<float2*>(&lt.X[warp][br + r][bc]) = make_float2(acc[r][0], acc[r][1]);
         }
         __syncthreads();
         if (warp < NB - d) {
-            float acc[4][2] = {};
-            block_mul(&lt.Zt[(warp + d) * BL][0], BL, &lt.X[warp * d][0][0], BL + 4, d, BL * (BL + 4), nullptr, acc, lane);
+            float acc[4][2];
+            block_mul(&lt.Zt[(warp + d) * BL][0], BL, &lt.X[warp * d][0][0], BL + 4, d, BL * (BL + 4), acc, lane);
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                *reinterpret_cast<float2*>(&lt.N[(warp + d) * BL + br + r][warp * BL + bc]) = make_float2(-acc[r][0], -acc[r][1]);
+            for (int r = 0; r < 4; ++r) {
+                const int row = (warp + d) * BL + br + r, col = warp * BL + bc;
+                float x = -acc[r][0], y = -acc[r][1];
+                *reinterpret_cast<float2*>(&lt.Y[row][col]) = make_float2(sm.be[row] * x, sm.be[row] * y);
+                const uint32_t hi = split2(x, y, x, y);
+                *reinterpret_cast<uint32_t*>(mat + (row * C + col) * 2) = hi;
+                *reinterpret_cast<uint32_t*>(mat + MAT + (row * C + col) * 2) = pack2(x, y);
+            }
         }
-        __syncthreads();
-    }
-    for (int p = tid; p < C * C / 8; p += FT) {                               // N as upper and lower parts
-        const int r = p / (C / 8), c = (p % (C / 8)) * 8;
-        float v[8];
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c + e < r ? lt.N[r][c + e] : 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            hi[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
-            lo[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
-        }
-        char* dst = static_cast<char*>(f.mat) + cid * f.mats * MAT + p * 16;
-        *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4*>(dst + MAT) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        if (d + 1 < NB) __syncthreads();
     }
     if (tid == 0 && sm.dead) flag_error(a.err, ERR_TIMEOUT);
     tc_before_sync();
