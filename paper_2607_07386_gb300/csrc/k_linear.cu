@@ -33,7 +33,7 @@ constexpr int SMS = 152;
 
 __host__ __device__ constexpr int stages_of(int bn) { return bn == 256 ? 4 : 6; }
 __host__ __device__ constexpr uint32_t stage_bytes(int bn) { return (BM + bn) * 128u; }
-__host__ __device__ constexpr uint32_t smem_bytes(int bn) { return 1024u + stage_bytes(bn) * stages_of(bn) + 256u; }
+__host__ __device__ constexpr uint32_t smem_bytes(int bn) { return 1024u + stage_bytes(bn) * stages_of(bn) + 256u + EPI_WARPS * 512u; }
 
 PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
     static PFN_cuTensorMapEncodeTiled_v12000 fn = []() -> PFN_cuTensorMapEncodeTiled_v12000 {
@@ -82,10 +82,10 @@ __device__ __forceinline__ float act_slope(float z, int act) {
 __device__ __forceinline__ uint4 residual8(const LinearOut& o, int64_t at) {
     return *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(o.residual) + at);
 }
-// Epilogue of eight neighbouring columns of one row: bias, pre-activation, activation, residual.
-__device__ __forceinline__ void finish8(float (&v)[8], const LinearOut& o, int64_t at, int n, const uint4& res) {
+// Epilogue of eight neighbouring columns of one row: bias (theirs at `bias`), pre-activation, activation, residual.
+__device__ __forceinline__ void finish8(float (&v)[8], const LinearOut& o, int64_t at, const float* bias, const uint4& res) {
     if (o.bias != nullptr) {
-        const float4 b0 = __ldg(reinterpret_cast<const float4*>(o.bias + n)), b1 = __ldg(reinterpret_cast<const float4*>(o.bias + n) + 1);
+        const float4 b0 = *reinterpret_cast<const float4*>(bias), b1 = *reinterpret_cast<const float4*>(bias + 4);
         v[0] += b0.x; v[1] += b0.y; v[2] += b0.z; v[3] += b0.w;
         v[4] += b1.x; v[5] += b1.y; v[6] += b1.z; v[7] += b1.w;
     }
@@ -121,6 +121,7 @@ __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtens
     const uint32_t bars = ring + STAGE * S;            // full[S], empty[S], acc full[2], acc empty[2], TMEM address
     const uint32_t full = bars, empty = bars + 8 * S, afull = bars + 16 * S, aempty = afull + 16;
     uint32_t* slot = reinterpret_cast<uint32_t*>(raw + (bars - base) + 16 * S + 32);
+    float* const bias_sm = reinterpret_cast<float*>(raw + (bars - base) + 256);
     const int tid = threadIdx.x, warp = tid >> 5;
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(slot)), "r"(COLS) : "memory");
@@ -205,21 +206,35 @@ __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtens
             const int c0 = part_of * (BN / 2);
             const uint32_t src = tmem + (n & 1) * BN + c0 + (static_cast<uint32_t>(quad * 32) << 16);
             const bool res = o.residual != nullptr && part == nullptr && row < g.M;
-            uint4 r[2][4];                                 // the residual, one block ahead
-            auto fetch = [&](int cb, uint4 (&to)[4]) {
+            float* const bias = bias_sm + (warp - 2) * 128;    // this warp's columns
+            if (o.bias != nullptr && part == nullptr) {
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < BN / 64; ++i) {
+                    const int col = n0 + c0 + i * 32 + lane;
+                    bias[i * 32 + lane] = col < g.N ? __ldg(o.bias + col) : 0.f;
+                }
+                __syncwarp();
+            }
+            uint4 r[4], rn[4];                             // the residual, one block ahead
+            auto fetch = [&](int cb) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int col = n0 + c0 + cb * 32 + q * 8;
-                    to[q] = res && col < g.N ? residual8(o, row * g.N + col) : make_uint4(0, 0, 0, 0);
+                    rn[q] = res && cb < BLOCKS && col < g.N ? residual8(o, row * g.N + col) : make_uint4(0, 0, 0, 0);
                 }
             };
-            fetch(0, r[0]);
+            fetch(0);
             ok = __all_sync(0xffffffffu, mbar_wait(afull + 8 * (n & 1), (n >> 1) & 1));
             if (!ok) break;
             tc_after_sync();
-#pragma unroll
+            // rolled: the four blocks unrolled, with an activation inlined 128 times, do not fit the
+            // instruction cache (an odd shape with gelu took 57 us for them)
+#pragma unroll 1
             for (int cb = 0; cb < BLOCKS; ++cb) {
-                if (cb + 1 < BLOCKS) fetch(cb + 1, r[(cb + 1) & 1]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) r[q] = rn[q];
+                fetch(cb + 1);
                 float v[32];
                 tmem_ld32(src + cb * 32, v);
                 if (cb == BLOCKS - 1) {
@@ -240,7 +255,7 @@ __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtens
                                 dst[0] = make_float4(f[0], f[1], f[2], f[3]);
                                 dst[1] = make_float4(f[4], f[5], f[6], f[7]);
                             } else {
-                                finish8(f, o, at, col, r[cb & 1][q]);
+                                finish8(f, o, at, bias + cb * 32 + q * 8, r[q]);
                             }
                         }
                     }
@@ -266,7 +281,7 @@ __global__ void __launch_bounds__(256) k_linear_join(const float* __restrict__ p
         v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
     }
     const uint4 r = o.residual != nullptr ? residual8(o, i) : make_uint4(0, 0, 0, 0);
-    finish8(v, o, i, static_cast<int>(i % N), r);
+    finish8(v, o, i, o.bias + i % N, r);
 }
 
 // Up to MR rows of x: a warp owns two rows of W (output columns), its lanes take 16-byte pieces of
