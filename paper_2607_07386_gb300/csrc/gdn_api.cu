@@ -114,13 +114,22 @@ sdm::GdnArgs gdn_args(const sdm_gdn_shape* s, const void* q, const void* k, cons
     return a;
 }
 
-// Factors of the chunked form.
+// Factors of the chunked forms: bf16 matrices and gate products, or fp32 factors.
 struct FwdLayout {
     size_t mat, gates, total;
+    bool tc;
 };
+size_t walk_bytes(const sdm_gdn_shape* s) {
+    if (!sdm::gdn_walk_supported(s->dtype, s->B, s->H, s->T, s->d_v)) return 0;
+    return align256(sdm::gdn_walk_bytes(static_cast<int64_t>(s->B) * s->H * ((s->T + sdm::GDN_C32 - 1) / sdm::GDN_C32)));
+}
 FwdLayout fwd_layout(const sdm_gdn_shape* s) {
     FwdLayout L{};
-    if (!sdm::gdn_chunk_supported(s->dtype, s->d_k, s->T)) return L;
+    L.tc = sdm::gdn_chunk_supported(s->dtype, s->d_k, s->T);
+    if (!L.tc) {
+        L.total = walk_bytes(s);
+        return L;
+    }
     const int64_t chunks = static_cast<int64_t>(s->B) * s->H * ((s->T + sdm::GDN_C64 - 1) / sdm::GDN_C64);
     L.gates = align256(sdm::gdn_factor_mat_bytes(chunks, 3));
     L.total = L.gates + align256(sdm::gdn_factor_gate_bytes(chunks));
@@ -131,7 +140,7 @@ FwdLayout fwd_layout(const sdm_gdn_shape* s) {
 // chunks' factors, then states and rows as bf16 (see GdnScan, GdnBack).
 struct BwdLayout {
     bool tc;
-    size_t mat, gates, S, dE, e, d, total;
+    size_t mat, gates, S, dE, e, d, fact, total;
 };
 BwdLayout bwd_layout(const sdm_gdn_shape* s) {
     BwdLayout L{};
@@ -151,7 +160,8 @@ BwdLayout bwd_layout(const sdm_gdn_shape* s) {
     L.dE = L.S + align256(marks);
     L.e = L.dE + align256(marks);
     L.d = L.e + align256(rows);
-    L.total = L.d + align256(rows);
+    L.fact = L.d + align256(rows);
+    L.total = L.fact + (L.tc ? 0 : walk_bytes(s));
     return L;
 }
 
@@ -219,8 +229,8 @@ sdm_status sdm_gdn_forward(const sdm_gdn_shape* s, const void* q, const void* k,
     int* err = nullptr;
     SDM_TRY(sdm::api_status_word(&err));
     const sdm::GdnArgs a = gdn_args(s, q, k, v, alpha, beta, lengths, err);
-    if (L.total > 0) {
-        cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (L.tc) {
         char* ws = static_cast<char*>(workspace);
         const sdm::GdnFactors f{ws + L.mat, 3, reinterpret_cast<float*>(ws + L.gates)};
         cudaError_t e = sdm::launch_gdn_factors(a, f, st);
@@ -232,7 +242,8 @@ sdm_status sdm_gdn_forward(const sdm_gdn_shape* s, const void* q, const void* k,
     r.state = state;
     r.n_slots = s->B;
     r.y = y;
-    return done(sdm::launch_gdn_recur(s->dtype, 0, r, reinterpret_cast<cudaStream_t>(stream)), "sdm_gdn_forward");
+    return done(L.total > 0 ? sdm::launch_gdn_walk(0, r, static_cast<float*>(workspace), st)
+                            : sdm::launch_gdn_recur(s->dtype, 0, r, st), "sdm_gdn_forward");
 }
 
 sdm_status sdm_gdn_step(const sdm_gdn_shape* s, const void* q, const void* k, const void* v, const void* alpha,
@@ -292,6 +303,7 @@ sdm_status sdm_gdn_backward(const sdm_gdn_shape* s, const void* q, const void* k
             e = sdm::launch_gdn_grads_tc(sdm::GdnGradsTc{a, dy, fa.gates, ws + L.S, ws + L.dE, ws + L.e, ws + L.d, dq, dk, dalpha, dbeta}, st);
         return done(e, "sdm_gdn_backward");
     }
+    float* const fact = L.total > L.fact ? reinterpret_cast<float*>(ws + L.fact) : nullptr;
     sdm::GdnRecur f{};
     f.a = a;
     sdm::GdnRecur r = f;
@@ -300,7 +312,7 @@ sdm_status sdm_gdn_backward(const sdm_gdn_shape* s, const void* q, const void* k
         f.state_in = state0;
         f.marks = reinterpret_cast<float*>(ws + L.S);
         f.rows = reinterpret_cast<float*>(ws + L.e);
-        e = sdm::launch_gdn_recur(s->dtype, 1, f, st);
+        e = fact != nullptr ? sdm::launch_gdn_walk(1, f, fact, st) : sdm::launch_gdn_recur(s->dtype, 1, f, st);
     }
     r.state_in = dstate;
     r.y = dv;
@@ -308,7 +320,7 @@ sdm_status sdm_gdn_backward(const sdm_gdn_shape* s, const void* q, const void* k
     r.marks = reinterpret_cast<float*>(ws + L.dE);
     r.rows = reinterpret_cast<float*>(ws + L.d);
     r.state_out = dstate0;
-    if (e == cudaSuccess) e = sdm::launch_gdn_recur(s->dtype, 2, r, st);
+    if (e == cudaSuccess) e = fact != nullptr ? sdm::launch_gdn_walk(2, r, fact, st) : sdm::launch_gdn_recur(s->dtype, 2, r, st);
     if (e == cudaSuccess && s->T > 0) {
         sdm::GdnGrads g{};
         g.a = f.a;

@@ -74,6 +74,11 @@ struct GdnRecur {
 // mode 0: forward; 1: forward with saved states and e, no y; 2: reverse.
 cudaError_t launch_gdn_recur(int dtype, int mode, const GdnRecur& r, cudaStream_t stream);
 
+// The same walks in chunks of 32 (k_gdn_walk.cu): float32, few chains.  fact: gdn_walk_bytes of scratch.
+bool gdn_walk_supported(int dtype, int B, int H, int T, int dv);
+size_t gdn_walk_bytes(int64_t chunks);
+cudaError_t launch_gdn_walk(int mode, const GdnRecur& r, float* fact, cudaStream_t stream);
+
 // ---- gradients of q, k and the gates from the saved states (k_gdn_grads.cu), chunks of 32 ----
 struct GdnGrads {
     GdnArgs a;
