@@ -36,7 +36,7 @@ struct Smem {
     float y[C][CP], d[C][CP], w[C][CP];
     float kk[C][C + 1], qk[C][C + 1];
     float yw[C][C + 1], dw[C][C + 1];       // <dy_i, w_j>, <d_i, w_j>; then M and A
-    float X[C + 1][C + 2], G[C][C + 1];     // X: column j at j + 1
+    float X[C + 1][C + 1], G[C][C + 1];     // X: column j at j + 1
     float al[C], be[C], g[C], h[C], db[C];
     float part[NT / 32];
 };
@@ -127,23 +127,26 @@ __global__ void __launch_bounds__(NT) k_gdn_grads(const GdnGrads r) {
             __syncthreads();
             const float* Sp = r.S + (chain * nc + ch) * per;
             const float* Ep = r.dE + (chain * nc + ch) * per;
-            for (int i = tid; i < DKP * CB; i += NT) {
-                const int x = i / CB, c = i % CB;
+#pragma unroll(DKP <= 128 ? 4 : 1)
+            for (int i = 0; i < DKP * CB / 4 / NT; ++i) {        // four columns of a row (d_v is a multiple of 4)
+                const int p = tid + i * NT, x = p / (CB / 4), c = p % (CB / 4) * 4;
                 const bool on = x < a.dk && c0 + c < a.dv;
                 const int64_t o = static_cast<int64_t>(x) * a.dv + c0 + c;
-                const float s = on ? __ldg(Sp + o) : 0.f, e = on ? __ldg(Ep + o) : 0.f;
-                sm.S[x][c] = s;
-                sm.E[x][c] = e;
-                es = fmaf(s, e, es);
+                const float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+                const float4 s = on ? __ldg(reinterpret_cast<const float4*>(Sp + o)) : z, e = on ? __ldg(reinterpret_cast<const float4*>(Ep + o)) : z;
+                *reinterpret_cast<float4*>(&sm.S[x][c]) = s;
+                *reinterpret_cast<float4*>(&sm.E[x][c]) = e;
+                es = fmaf(s.x, e.x, fmaf(s.y, e.y, fmaf(s.z, e.z, fmaf(s.w, e.w, es))));
             }
-            for (int i = tid; i < C * CB; i += NT) {
-                const int t = i / CB, c = i % CB;
+            {
+                const int t = tid / (CB / 4), c = tid % (CB / 4) * 4;          // 32 tokens x 8 quads: one each
                 const bool on = t < n && c0 + c < a.dv;
                 const int64_t o = (chain * a.T + t0 + t) * a.dv + c0 + c;
-                const float e = on ? __ldg(r.e + o) : 0.f;
-                sm.d[t][c] = on ? __ldg(r.d + o) : 0.f;
-                sm.w[t][c] = e;                                  // e until its product with d is taken
-                sm.y[t][c] = on ? a.scale * load_elem<D>(r.dy, vb + (t0 + t) * vs + c0 + c) : 0.f;
+                const float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+                *reinterpret_cast<float4*>(&sm.d[t][c]) = on ? __ldg(reinterpret_cast<const float4*>(r.d + o)) : z;
+                *reinterpret_cast<float4*>(&sm.w[t][c]) = on ? __ldg(reinterpret_cast<const float4*>(r.e + o)) : z;   // e until its product with d is taken
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sm.y[t][c + j] = on ? a.scale * load_elem<D>(r.dy, vb + (t0 + t) * vs + c0 + c + j) : 0.f;
             }
             __syncthreads();
             {   // dbeta, then w = beta e; four columns of one token per thread
@@ -233,22 +236,47 @@ __global__ void __launch_bounds__(NT) k_gdn_grads(const GdnGrads r) {
         }
         __syncthreads();                                         // X[C][0]
         if (tid < 32) {
-            // lane l walks column l - 1 (the start for l = 0); column C - 1 has no factor to its
-            // right inside the chunk, so it gives nothing
-            float acc = 0.f, nxt = 0.f;
-            for (int t = C - 1; t >= 0; --t) {
-                acc = t == C - 1 ? sm.X[C - 1][tid] + sm.X[C][tid] : fmaf(nxt, acc, sm.X[t][tid]);
-                nxt = sm.al[t];
-                // prod_{j < l < t} alpha_l for j = tid - 1: empty (1) at t = tid
-                float p = 0.f;
-                if (t >= tid) p = tid == 0 ? (t == 0 ? 1.f : sm.g[t - 1]) : (t == tid ? 1.f : sm.G[t - 1][tid - 1]);
-                float s = t >= tid ? acc * p : 0.f;
+            // lane l walks column l - 1 (the start for l = 0), in place and eight rows at a time; column C - 1 has no
+            // factor to its right inside the chunk, so it gives nothing.  Then lane t sums row t.
+            float acc = sm.X[C][tid], next = 1.f;
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                if (tid == 0 && t < nt) {
-                    put_elem<D>(r.dalpha, chain * a.T + t0 + t, t < n ? s : 0.f);
-                    put_elem<D>(r.dbeta, chain * a.T + t0 + t, t < n ? sm.db[t] : 0.f);
+            for (int q = C / 8 - 1; q >= 0; --q) {
+                float v[8], al[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[e] = sm.X[8 * q + e][tid];
+                    al[e] = sm.al[8 * q + e];
                 }
+#pragma unroll
+                for (int e = 7; e >= 0; --e) {
+                    acc = fmaf(next, acc, v[e]);
+                    next = al[e];
+                    sm.X[8 * q + e][tid] = acc;
+                }
+            }
+            float p = 1.f;                                       // prod_{j < l < t} alpha_l
+#pragma unroll
+            for (int q = 0; q < C / 8; ++q) {
+                float v[8], al[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[e] = sm.X[8 * q + e][tid];
+                    al[e] = sm.al[8 * q + e];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool on = 8 * q + e >= tid;
+                    sm.X[8 * q + e][tid] = on ? v[e] * p : 0.f;
+                    if (on) p *= al[e];
+                }
+            }
+            __syncwarp();
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < C; ++j) s += sm.X[tid][j];
+            if (tid < nt) {
+                put_elem<D>(r.dalpha, chain * a.T + t0 + tid, tid < n ? s : 0.f);
+                put_elem<D>(r.dbeta, chain * a.T + t0 + tid, tid < n ? sm.db[tid] : 0.f);
             }
         }
     }

@@ -36,7 +36,7 @@ __device__ __forceinline__ float dot4(const float4& x, const float4& y, float s)
 // acc[r][c] += sum_x A[4 rows of a][x] B[rows b and b + db][x], x < n (a multiple of 4).
 template <int R>
 __device__ __forceinline__ void tile(const float* a, int lda, const float* b, int db, int n, float (&acc)[R][2]) {
-#pragma unroll 2
+#pragma unroll 4
     for (int x = 0; x < n; x += 4) {
         const float4 b0 = *reinterpret_cast<const float4*>(b + x), b1 = *reinterpret_cast<const float4*>(b + db + x);
 #pragma unroll
@@ -65,11 +65,13 @@ __global__ void __launch_bounds__(NT) k_gdn_factors32(const GdnArgs a, float* __
     const int n = len - t0 < C ? len - t0 : C;
     const int64_t chain = static_cast<int64_t>(b) * a.H + h;
     const int64_t kb = gdn_base(a.token_major, b, hk, a.Hk, a.T, a.dk), ks = gdn_stride(a.token_major, a.Hk, a.dk);
-    for (int i = tid; i < 64 * (a.dk / 4); i += NT) {
-        const int r = i / (a.dk / 4), x = (i % (a.dk / 4)) * 4, t = r % C;
-        const float* src = static_cast<const float*>(r < C ? a.k : a.q) + kb + (t0 + t) * ks + x;
-        *reinterpret_cast<float4*>(kq + r * ld + x) = t < n ? __ldg(reinterpret_cast<const float4*>(src)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int row = tid >> 4; row < 2 * C; row += NT / 16) {            // 16 threads a row
+        const int t = row % C;
+        const float* src = static_cast<const float*>(row < C ? a.k : a.q) + kb + (t0 + t) * ks;
+        for (int x = (tid & 15) * 4; x < a.dk; x += 64) cp16(kq + row * ld + x, t < n ? src + x : static_cast<const float*>(a.k), t < n);
     }
+    asm volatile("cp.async.commit_group;\n" ::: "memory");
+    asm volatile("cp.async.wait_group 0;\n" ::: "memory");
     if (tid < C) {
         al[tid] = tid < n ? __ldg(static_cast<const float*>(a.alpha) + chain * a.T + t0 + tid) : 1.f;
         al[C + tid] = tid < n ? __ldg(static_cast<const float*>(a.beta) + chain * a.T + t0 + tid) : 0.f;
@@ -200,12 +202,12 @@ __global__ void __launch_bounds__(NT) k_gdn_walk(const GdnRecur r, const float* 
     auto chunk_of = [&](int it) { return MODE == 2 ? chunks - 1 - it : it; };
     auto stage = [&](int it) {
         float* const to = sm + (it & 1) * L.stage;
-        const int ch = chunk_of(it), t0 = ch * C, pk = a.dk / 4;
-        for (int i = tid; i < (MODE == 1 ? C : 2 * C) * pk; i += NT) {
-            const int row = i / pk, x = (i % pk) * 4, t = row % C;
-            const bool on = t0 + t < len;
-            const float* p = static_cast<const float*>(row < C ? a.k : a.q) + kb + (on ? (t0 + t) * ks + x : 0);
-            cp16(to + L.kq + row * L.ld + x, p, on);
+        const int ch = chunk_of(it), t0 = ch * C;
+        for (int row = tid >> 4; row < (MODE == 1 ? C : 2 * C); row += NT / 16) {      // 16 threads a row
+            const int t = t0 + row % C;
+            const bool on = t < len;
+            const float* p = static_cast<const float*>(row < C ? a.k : a.q) + kb + (on ? t * ks : 0);
+            for (int x = (tid & 15) * 4; x < a.dk; x += 64) cp16(to + L.kq + row * L.ld + x, p + x, on);
         }
         const float* vp = static_cast<const float*>(MODE == 2 ? r.dy : a.v) + vb;
         for (int i = tid; i < C * (CW / 4); i += NT) {
@@ -333,7 +335,7 @@ __global__ void __launch_bounds__(NT) k_gdn_walk(const GdnRecur r, const float* 
             for (int pass = 0; pass < (MODE == 2 ? 2 : 1); ++pass) {
                 const float* const A = K + pass * C * L.ld + x;
                 const float* const B0 = (pass ? Y : W) + c * CP;
-#pragma unroll 2
+#pragma unroll 4
                 for (int t = 0; t < C; t += 4) {
                     const float4 w0 = *reinterpret_cast<const float4*>(B0 + t), w1 = *reinterpret_cast<const float4*>(B0 + 8 * CP + t);
                     const float a0[4] = {w0.x, w0.y, w0.z, w0.w}, a1[4] = {w1.x, w1.y, w1.z, w1.w};
