@@ -13,40 +13,87 @@
 // A chunk is four dependent products in place of 32 dependent tokens: with few sequences and heads the
 // latency of the chain is what counts, and this form has about a fifth of the token recurrence's.  With many, the
 // token recurrence's registers win over these shared-memory reads (see launch_gdn_walk's rule).
-#include "gdn_internal.h"
+#include "gdn_tc.cuh"
 
 namespace sdm {
 
 namespace {
 
+using namespace tc;
+
 constexpr int C = GDN_C32;
 constexpr int CW = 16;                   // columns of a CTA
-constexpr int NT = 128;
+constexpr int NT = 128;                  // computing threads; a warp beside them fetches
 constexpr int CP = C + 4;                // padded row of a [.][32] matrix
-constexpr int FACT = 2 * C * C + 3 * C;  // floats of a chunk's factors: N, P, g, beta, h
+constexpr int FACT = 2 * C * C + 3 * C;  // floats of a chunk's factors: N, P, g, beta, h (67 rows of 32)
+constexpr int BOX = C * 128;             // bytes of 32 rows x 32 floats, swizzled as TMA leaves them
 
 __device__ __forceinline__ void cp16(void* dst, const void* src, bool on) {
     const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(dst));
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(s), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
 
-__device__ __forceinline__ float dot4(const float4& x, const float4& y, float s) {
-    return fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s))));
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<unsigned long long&>(d))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)),
+          "l"(reinterpret_cast<unsigned long long&>(c)));
+    return d;
 }
-// acc[r][c] += sum_x A[4 rows of a][x] B[rows b and b + db][x], x < n (a multiple of 4).
-template <int R>
-__device__ __forceinline__ void tile(const float* a, int lda, const float* b, int db, int n, float (&acc)[R][2]) {
-#pragma unroll 4
-    for (int x = 0; x < n; x += 4) {
-        const float4 b0 = *reinterpret_cast<const float4*>(b + x), b1 = *reinterpret_cast<const float4*>(b + db + x);
+// acc[r][c] += sum_x A[row r of a][x] B[row c of b, db floats apart][x], x < n (a multiple of 4), in packed pairs:
+// with a warp or two on a scheduler it is the number of instructions that counts.  The reads of the next four x are
+// issued before this four's products.
+template <int R, int S, class A>
+__device__ __forceinline__ void tile(A a, const float* b, int db, int n, float (&acc)[R][S]) {
+    float4 va[2][R], vb[2][S];
+    float2 sum[R][S];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const float4 v = *reinterpret_cast<const float4*>(a + r * lda + x);
-            acc[r][0] = dot4(v, b0, acc[r][0]);
-            acc[r][1] = dot4(v, b1, acc[r][1]);
-        }
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int c = 0; c < S; ++c) sum[r][c] = make_float2(acc[r][c], 0.f);
+    auto load = [&](int w, int x) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) va[w][r] = a(r, x);
+#pragma unroll
+        for (int c = 0; c < S; ++c) vb[w][c] = *reinterpret_cast<const float4*>(b + c * db + x);
+    };
+    auto mul = [&](int w) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < S; ++c) {
+                sum[r][c] = fma2(make_float2(va[w][r].x, va[w][r].y), make_float2(vb[w][c].x, vb[w][c].y), sum[r][c]);
+                sum[r][c] = fma2(make_float2(va[w][r].z, va[w][r].w), make_float2(vb[w][c].z, vb[w][c].w), sum[r][c]);
+            }
+    };
+    load(0, 0);
+#pragma unroll 1
+    for (int x = 0; x < n; x += 8) {
+        load(1, x + 4 < n ? x + 4 : x);
+        mul(0);
+        load(0, x + 8 < n ? x + 8 : x);
+        if (x + 4 < n) mul(1);
     }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int c = 0; c < S; ++c) acc[r][c] = sum[r][c].x + sum[r][c].y;
 }
+// Rows of a padded matrix, and of swizzled boxes (32 floats of every row a box): four values of row r from x on.
+struct Padded {
+    const float* p;
+    int ld;
+    __device__ __forceinline__ float4 operator()(int r, int x) const { return *reinterpret_cast<const float4*>(p + r * ld + x); }
+};
+struct Boxed {
+    const unsigned char* p;
+    int row;
+    __device__ __forceinline__ float4 operator()(int r, int x) const {
+        const int i = row + r;
+        return *reinterpret_cast<const float4*>(p + (x >> 5) * BOX + i * 128 + (((x >> 2 & 7) ^ (i & 7)) << 4));
+    }
+};
 
 // ------------------------------------------------------------------------------------------
 // Factors of a chunk: 128 threads; threads 0-63 take k.k, 64-127 q.k, 4 x 4 each.  N by a column per lane of the
@@ -81,26 +128,27 @@ __global__ void __launch_bounds__(NT) k_gdn_factors32(const GdnArgs a, float* __
     const bool isq = tid >= 64;
     const int i0 = 4 * ((tid & 63) >> 3), j0 = 4 * (tid & 7);          // rows and columns of this thread's tile
     {
-        float acc[2][4][2] = {};
-        if (j0 <= i0 + 3) {
-            const float* A = kq + ((isq ? C : 0) + i0) * ld;
-            tile<4>(A, ld, kq + j0 * ld, ld, a.dk, acc[0]);
-            tile<4>(A, ld, kq + (j0 + 2) * ld, ld, a.dk, acc[1]);
+        float acc[4][4] = {};
+        if (j0 <= i0 + 3) tile<4, 4>(Padded{kq + ((isq ? C : 0) + i0) * ld, ld}, kq + j0 * ld, ld, a.dk, acc);
+        float p[4] = {1.f, 1.f, 1.f, 1.f};     // prod_{j0 + 3 < l <= i} alpha_l of the four rows
+#pragma unroll 8
+        for (int l = i0 + 3; l > j0 + 3; --l) {
+            const float f = al[l];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) p[r] *= l <= i0 + r ? f : 1.f;
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int i = i0 + r;
             float G[4];                        // prod_{j < l <= i}, 0 above the diagonal
-            float p = 1.f;
-            for (int l = i; l > j0 + 3; --l) p *= al[l];
 #pragma unroll
             for (int c = 3; c >= 0; --c) {
                 const int j = j0 + c;
-                G[c] = j <= i ? p : 0.f;
-                if (j <= i) p *= al[j];
+                G[c] = j <= i ? p[r] : 0.f;
+                if (j <= i) p[r] *= al[j];
             }
             float4 v;
-            v.x = G[0] * acc[0][r][0]; v.y = G[1] * acc[0][r][1]; v.z = G[2] * acc[1][r][0]; v.w = G[3] * acc[1][r][1];
+            v.x = G[0] * acc[r][0]; v.y = G[1] * acc[r][1]; v.z = G[2] * acc[r][2]; v.w = G[3] * acc[r][3];
             if (!isq) {
                 B[(j0 + 0) * CP + i] = v.x; B[(j0 + 1) * CP + i] = v.y; B[(j0 + 2) * CP + i] = v.z; B[(j0 + 3) * CP + i] = v.w;
             } else if (!transposed) {
@@ -153,39 +201,45 @@ __global__ void __launch_bounds__(NT) k_gdn_factors32(const GdnArgs a, float* __
 // The walk.  MODE 0: forward; 1: forward, keeping the states before the chunks and e; 2: reverse.
 // Grid (column blocks of 16, H, B).
 // ------------------------------------------------------------------------------------------
-struct WalkLayout {
-    int ld, kq, v, f, stage, S, u, w, y, floats;
+struct WalkLayout {                            // bytes
+    int nb, ld, Q, F, V, G, stage, S, U, W, Y, bytes;
     __host__ __device__ explicit WalkLayout(int dk) {
-        ld = dk + 4;
-        kq = 0;                                // K, Q: [64][dk + 4]
-        v = kq + 64 * ld;                      // v or dy: [32][16]
-        f = v + C * CW;                        // N, P: [64][36]; g, beta, h
-        stage = f + 2 * C * CP + 3 * C;
+        nb = (dk + 31) / 32;                   // boxes of K (and Q)
+        ld = dk + 4;                           // floats of a row of S
+        Q = nb * BOX;
+        F = 2 * Q;                             // N, P
+        V = F + 2 * BOX;                       // v or dy: [32][16]
+        G = V + C * CW * 4;                    // g, beta, h
+        stage = G + 1024;
         S = 2 * stage;                         // [16][dk + 4]
-        u = S + CW * ld;                       // [16][36] each: beta r (or beta x); h w (or -beta g d); w (or dy)
-        w = u + CW * CP;
-        y = w + CW * CP;
-        floats = y + CW * CP;
+        U = S + CW * ld * 4;                   // [16][36] each: beta r (or beta x); h w (or -beta g d); w (or dy)
+        W = U + CW * CP * 4;
+        Y = W + CW * CP * 4;
+        bytes = 1024 + Y + CW * CP * 4;
     }
 };
 
+__device__ __forceinline__ void bar_walk() { asm volatile("bar.sync 1, %0;\n" ::"n"(NT) : "memory"); }
+
 template <int MODE>
-__global__ void __launch_bounds__(NT) k_gdn_walk(const GdnRecur r, const float* __restrict__ fact) {
-    extern __shared__ __align__(16) float sm[];
+__global__ void __launch_bounds__(NT + 32) k_gdn_walk(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tq,
+                                                      const __grid_constant__ CUtensorMap tv, const __grid_constant__ CUtensorMap tf,
+                                                      const GdnRecur r, const float* __restrict__ fact) {
+    extern __shared__ unsigned char raw[];
+    unsigned char* const sm = raw + ((smem_u32(raw) + 1023u & ~1023u) - smem_u32(raw));
     const GdnArgs& a = r.a;
     const WalkLayout L(a.dk);
     const int tid = threadIdx.x, b = blockIdx.z, h = blockIdx.y, hk = h / (a.H / a.Hk), col0 = blockIdx.x * CW;
     const int len = gdn_length(a, b), chunks = (len + C - 1) / C, nc = (a.T + C - 1) / C;
     const int64_t chain = static_cast<int64_t>(b) * a.H + h, per = static_cast<int64_t>(a.dk) * a.dv;
     const int64_t vb = gdn_base(a.token_major, b, h, a.H, a.T, a.dv), vs = gdn_stride(a.token_major, a.H, a.dv);
-    const int64_t kb = gdn_base(a.token_major, b, hk, a.Hk, a.T, a.dk), ks = gdn_stride(a.token_major, a.Hk, a.dk);
     float* const y = static_cast<float*>(r.y);
-    float* const S = sm + L.S;
-    float* const U = sm + L.u;
-    float* const W = sm + L.w;
-    float* const Y = sm + L.y;
+    float* const S = reinterpret_cast<float*>(sm + L.S);
+    float* const U = reinterpret_cast<float*>(sm + L.U);
+    float* const W = reinterpret_cast<float*>(sm + L.W);
+    float* const Y = reinterpret_cast<float*>(sm + L.Y);
     const float* const src = MODE == 0 ? r.state + chain * per : (r.state_in ? r.state_in + chain * per : nullptr);
-    for (int i = tid; i < a.dk * (CW / 4); i += NT) {          // 4 columns of a row
+    for (int i = tid; i < a.dk * (CW / 4); i += NT + 32) {     // 4 columns of a row
         const int x = i / (CW / 4), c = (i % (CW / 4)) * 4;
         float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
         if (src != nullptr && col0 + c < a.dv) f = *reinterpret_cast<const float4*>(src + static_cast<int64_t>(x) * a.dv + col0 + c);
@@ -200,57 +254,77 @@ __global__ void __launch_bounds__(NT) k_gdn_walk(const GdnRecur r, const float* 
         }
     };
     auto chunk_of = [&](int it) { return MODE == 2 ? chunks - 1 - it : it; };
-    auto stage = [&](int it) {
-        float* const to = sm + (it & 1) * L.stage;
-        const int ch = chunk_of(it), t0 = ch * C;
-        for (int row = tid >> 4; row < (MODE == 1 ? C : 2 * C); row += NT / 16) {      // 16 threads a row
-            const int t = t0 + row % C;
-            const bool on = t < len;
-            const float* p = static_cast<const float*>(row < C ? a.k : a.q) + kb + (on ? t * ks : 0);
-            for (int x = (tid & 15) * 4; x < a.dk; x += 64) cp16(to + L.kq + row * L.ld + x, p + x, on);
+    // the tiles of the chunks, by a thread beside the computing ones (16-byte cp.async by all of them took 2,460 cycles a
+    // chunk to issue, a bulk copy per row 10,000 to go through)
+    __shared__ unsigned long long full[2], empty[2];
+    __shared__ int dead;
+    if (tid == 0) {
+        dead = 0;
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&full[i]), 1);
+            mbar_init(smem_u32(&empty[i]), NT);
         }
-        const float* vp = static_cast<const float*>(MODE == 2 ? r.dy : a.v) + vb;
-        for (int i = tid; i < C * (CW / 4); i += NT) {
-            const int t = i / (CW / 4), c = (i % (CW / 4)) * 4;
-            const bool on = t0 + t < len && col0 + c < a.dv;
-            cp16(to + L.v + t * CW + c, vp + (on ? (t0 + t) * vs + col0 + c : 0), on);
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    }
+    __syncthreads();
+    if (tid >= NT) {
+        if (tid == NT) {
+            int it = 0;
+            for (; it < chunks; ++it) {
+                if (it >= 2) mbar_wait_or_dead(smem_u32(&empty[it & 1]), (it / 2 - 1) & 1, &dead);
+                if (dead) break;
+                const uint32_t to = smem_u32(sm) + (it & 1) * L.stage, bar = smem_u32(&full[it & 1]);
+                const int t0 = chunk_of(it) * C;
+                const int64_t cid = chain * nc + chunk_of(it);
+                mbar_expect_tx(bar, static_cast<uint32_t>((MODE == 1 ? 1 : 2) * L.nb * BOX + 2 * BOX + C * CW * 4 + 3 * C * 4));
+                for (int i = 0; i < L.nb; ++i) {
+                    tma_load_4d(to + i * BOX, &tk, 32 * i, t0, hk, b, bar);
+                    if (MODE != 1) tma_load_4d(to + L.Q + i * BOX, &tq, 32 * i, t0, hk, b, bar);
+                }
+                tma_load_4d(to + L.F, &tf, 0, static_cast<int>(cid * (FACT / C)), 0, 0, bar);
+                tma_load_4d(to + L.F + BOX, &tf, 0, static_cast<int>(cid * (FACT / C)) + C, 0, 0, bar);
+                tma_load_4d(to + L.V, &tv, col0, t0, h, b, bar);
+                bulk_load(to + L.G, fact + cid * FACT + 2 * C * C, 3 * C * 4, bar);
+            }
+            if (dead)                                          // the copies in flight land before the CTA ends
+                for (int j = it > 2 ? it - 2 : 0; j < it; ++j) mbar_wait(smem_u32(&full[j & 1]), j / 2 & 1);
         }
-        const float* f = fact + (chain * nc + ch) * FACT;
-        for (int i = tid; i < (2 * C * C + 3 * C) / 4; i += NT) {
-            const int row = i / (C / 4), x = (i % (C / 4)) * 4;
-            cp16(row < 2 * C ? to + L.f + row * CP + x : to + L.f + 2 * C * CP + (row - 2 * C) * C + x, f + 4 * i, true);
-        }
-        asm volatile("cp.async.commit_group;\n" ::: "memory");
-    };
-    if (chunks > 0) stage(0);
+    } else {
     // 4 x 2 tiles: tokens 4 tr .. and columns tc, tc + 8; threads 0-63 take K's (N's) rows, 64-127 Q's (P's)
     const int tr = tid >> 3 & 7, tc = tid & 7, hi = tid >> 6;
     for (int it = 0; it < chunks; ++it) {
         const int ch = chunk_of(it), t0 = ch * C, n = len - t0 < C ? len - t0 : C;
-        const float* const st = sm + (it & 1) * L.stage;
-        const float* const K = st + L.kq;
-        const float* const V = st + L.v;
-        const float* const F = st + L.f;
-        const float* const g = F + 2 * C * CP;
+        unsigned char* const st = sm + (it & 1) * L.stage;
+        const unsigned char* const K = st;
+        const unsigned char* const F = st + L.F;
+        float* const V = reinterpret_cast<float*>(st + L.V);
+        const float* const g = reinterpret_cast<const float*>(st + L.G);
         const float* const be = g + C;
         const float* const hh = be + C;
-        asm volatile("cp.async.wait_group 0;\n" ::: "memory");
-        __syncthreads();                                       // the tiles are in; the last chunk is done with
-        if (it + 1 < chunks) stage(it + 1);
+        mbar_wait_or_dead(smem_u32(&full[it & 1]), it / 2 & 1, &dead);
+        if (n < C) {                                           // rows past the length: zeros, whatever was there
+            for (int i = tid; i < (C - n) * 8 * L.nb; i += NT) {
+                const int row = n + i / (8 * L.nb), piece = i % (8 * L.nb), at = piece / 8 * BOX + row * 128 + piece % 8 * 16;
+                *reinterpret_cast<float4*>(st + at) = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (MODE != 1) *reinterpret_cast<float4*>(st + L.Q + at) = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            for (int i = tid; i < (C - n) * CW; i += NT) V[n * CW + i] = 0.f;
+        }
+        bar_walk();                                            // the tiles are in; the last chunk's S is written
         if (MODE != 0) save(r.marks + (chain * nc + ch) * per);
         float acc[4][2] = {}, out[4][2] = {};
         if (MODE == 2) {                                       // dy, and scale P^T dy (threads 64-127)
             for (int i = tid; i < C * CW; i += NT) Y[(i % CW) * CP + i / CW] = V[i];
-            __syncthreads();
-            if (hi) tile<4>(F + (C + 4 * tr) * CP, CP, Y + tc * CP, 8 * CP, C, acc);
-            else tile<4>(K + 4 * tr * L.ld, L.ld, S + tc * L.ld, 8 * L.ld, a.dk, acc);
+            bar_walk();
+            if (hi) tile<4, 2>(Boxed{F + BOX, 4 * tr}, Y + tc * CP, 8 * CP, C, acc);
+            else tile<4, 2>(Boxed{K, 4 * tr}, S + tc * L.ld, 8 * L.ld, a.dk, acc);
             if (hi) {
 #pragma unroll
                 for (int m = 0; m < 4; ++m)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) W[(tc + 8 * c) * CP + 4 * tr + m] = a.scale * acc[m][c];
             }
-            __syncthreads();
+            bar_walk();
             if (!hi) {                                         // x
 #pragma unroll
                 for (int m = 0; m < 4; ++m)
@@ -261,9 +335,9 @@ __global__ void __launch_bounds__(NT) k_gdn_walk(const GdnRecur r, const float* 
                         U[(tc + 8 * c) * CP + t] = be[t] * acc[m][c];
                     }
             }
-            __syncthreads();
+            bar_walk();
             if (!hi) {                                         // d; N is strictly lower, its transpose upper
-                tile<4>(F + 4 * tr * CP, CP, U + tc * CP, 8 * CP, C, acc);
+                tile<4, 2>(Boxed{F, 4 * tr}, U + tc * CP, 8 * CP, C, acc);
 #pragma unroll
                 for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -284,9 +358,9 @@ __global__ void __launch_bounds__(NT) k_gdn_walk(const GdnRecur r, const float* 
                         Y[(tc + 8 * c) * CP + t] *= a.scale * g[t];
                     }
             }
-            __syncthreads();
+            bar_walk();
         } else {
-            if (MODE == 0 || !hi) tile<4>(K + (C * hi + 4 * tr) * L.ld, L.ld, S + tc * L.ld, 8 * L.ld, a.dk, acc);   // K S, Q S
+            if (MODE == 0 || !hi) tile<4, 2>(Boxed{hi ? st + L.Q : K, 4 * tr}, S + tc * L.ld, 8 * L.ld, a.dk, acc);   // K S, Q S
             if (!hi) {
 #pragma unroll
                 for (int m = 0; m < 4; ++m)
@@ -297,9 +371,9 @@ __global__ void __launch_bounds__(NT) k_gdn_walk(const GdnRecur r, const float* 
                         U[(tc + 8 * c) * CP + t] = be[t] * acc[m][c];
                     }
             }
-            __syncthreads();
+            bar_walk();
             if (!hi) {                                         // e
-                tile<4>(F + 4 * tr * CP, CP, U + tc * CP, 8 * CP, 4 * tr + 4, acc);
+                tile<4, 2>(Boxed{F, 4 * tr}, U + tc * CP, 8 * CP, 4 * tr + 4, acc);
 #pragma unroll
                 for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -311,9 +385,9 @@ __global__ void __launch_bounds__(NT) k_gdn_walk(const GdnRecur r, const float* 
                         if (MODE == 1 && t < n && col < a.dv) r.rows[(chain * a.T + t0 + t) * a.dv + col] = acc[m][c];
                     }
             }
-            __syncthreads();
+            bar_walk();
             if (MODE == 0 && hi) {
-                tile<4>(F + (C + 4 * tr) * CP, CP, Y + tc * CP, 8 * CP, 4 * tr + 4, out);
+                tile<4, 2>(Boxed{F + BOX, 4 * tr}, Y + tc * CP, 8 * CP, 4 * tr + 4, out);
 #pragma unroll
                 for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -322,50 +396,89 @@ __global__ void __launch_bounds__(NT) k_gdn_walk(const GdnRecur r, const float* 
                         if (t < n && col < a.dv) y[vb + (t0 + t) * vs + col] = a.scale * fmaf(g[t], acc[m][c], out[m][c]);
                     }
             }
-            if (MODE == 0) __syncthreads();                    // Q S is out of S
         }
         // S[c][x] = g_31 S + sum_t (h w)[c][t] K[t][x]: four x and two columns a thread
         const float gl = g[C - 1];
         for (int p = tid; p < a.dk * 2; p += NT) {             // dk / 4 quads x 8 column pairs
             const int x = (p >> 3) * 4, c = p & 7;
-            float4 s0 = *reinterpret_cast<const float4*>(S + c * L.ld + x), s1 = *reinterpret_cast<const float4*>(S + (c + 8) * L.ld + x);
-            s0.x *= gl; s0.y *= gl; s0.z *= gl; s0.w *= gl;
-            s1.x *= gl; s1.y *= gl; s1.z *= gl; s1.w *= gl;
+            float2 s0[2], s1[2];
+            {
+                const float4 f0 = *reinterpret_cast<const float4*>(S + c * L.ld + x), f1 = *reinterpret_cast<const float4*>(S + (c + 8) * L.ld + x);
+                s0[0] = make_float2(gl * f0.x, gl * f0.y); s0[1] = make_float2(gl * f0.z, gl * f0.w);
+                s1[0] = make_float2(gl * f1.x, gl * f1.y); s1[1] = make_float2(gl * f1.z, gl * f1.w);
+            }
 #pragma unroll
             for (int pass = 0; pass < (MODE == 2 ? 2 : 1); ++pass) {
-                const float* const A = K + pass * C * L.ld + x;
+                const Boxed A{pass ? st + L.Q : K, 0};
                 const float* const B0 = (pass ? Y : W) + c * CP;
-#pragma unroll 4
-                for (int t = 0; t < C; t += 4) {
-                    const float4 w0 = *reinterpret_cast<const float4*>(B0 + t), w1 = *reinterpret_cast<const float4*>(B0 + 8 * CP + t);
-                    const float a0[4] = {w0.x, w0.y, w0.z, w0.w}, a1[4] = {w1.x, w1.y, w1.z, w1.w};
+                float4 w[2][2], k[2][4];
+                auto load = [&](int to, int t) {
+                    w[to][0] = *reinterpret_cast<const float4*>(B0 + t);
+                    w[to][1] = *reinterpret_cast<const float4*>(B0 + 8 * CP + t);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) k[to][e] = A(t + e, x);
+                };
+                auto add = [&](int of) {
+                    const float a0[4] = {w[of][0].x, w[of][0].y, w[of][0].z, w[of][0].w}, a1[4] = {w[of][1].x, w[of][1].y, w[of][1].z, w[of][1].w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float4 k = *reinterpret_cast<const float4*>(A + (t + e) * L.ld);
-                        s0.x = fmaf(a0[e], k.x, s0.x); s0.y = fmaf(a0[e], k.y, s0.y); s0.z = fmaf(a0[e], k.z, s0.z); s0.w = fmaf(a0[e], k.w, s0.w);
-                        s1.x = fmaf(a1[e], k.x, s1.x); s1.y = fmaf(a1[e], k.y, s1.y); s1.z = fmaf(a1[e], k.z, s1.z); s1.w = fmaf(a1[e], k.w, s1.w);
+                        const float2 lo = make_float2(k[of][e].x, k[of][e].y), up = make_float2(k[of][e].z, k[of][e].w);
+                        const float2 d0 = make_float2(a0[e], a0[e]), d1 = make_float2(a1[e], a1[e]);
+                        s0[0] = fma2(d0, lo, s0[0]); s0[1] = fma2(d0, up, s0[1]);
+                        s1[0] = fma2(d1, lo, s1[0]); s1[1] = fma2(d1, up, s1[1]);
                     }
+                };
+                load(0, 0);
+#pragma unroll 1
+                for (int t = 0; t < C; t += 8) {
+                    load(1, t + 4);
+                    add(0);
+                    load(0, t + 8 < C ? t + 8 : t);
+                    add(1);
                 }
             }
-            *reinterpret_cast<float4*>(S + c * L.ld + x) = s0;
-            *reinterpret_cast<float4*>(S + (c + 8) * L.ld + x) = s1;
+            *reinterpret_cast<float4*>(S + c * L.ld + x) = make_float4(s0[0].x, s0[0].y, s0[1].x, s0[1].y);
+            *reinterpret_cast<float4*>(S + (c + 8) * L.ld + x) = make_float4(s1[0].x, s1[0].y, s1[1].x, s1[1].y);
         }
+        fence_async();                                     // this chunk's reads before its place is filled again
+        mbar_arrive(smem_u32(&empty[it & 1]));
+    }
     }
     __syncthreads();
+    if (tid == 0 && dead) flag_error(a.err, ERR_TIMEOUT);
     if (MODE == 0 && chunks > 0) save(r.state + chain * per);
     if (MODE == 2 && r.state_out != nullptr) save(r.state_out + chain * per);
     if (MODE != 1)                                             // tokens past the length
-        for (int t = len + tid / CW; t < a.T; t += NT / CW)
+        for (int t = len + tid / CW; t < a.T; t += (NT + 32) / CW)
             if (col0 + tid % CW < a.dv) y[vb + t * vs + col0 + tid % CW] = 0.f;
+}
+
+// [B, heads, T, d] or [B, T, heads, d] float32 as {d, T, heads, B}, boxes of `cols` values x 32 tokens.
+bool float_map(CUtensorMap* m, const void* base, int token_major, int B, int heads, int T, int d, int cols) {
+    PFN_cuTensorMapEncodeTiled_v12000 enc = gdn::encode_fn();
+    if (!enc) return false;
+    const cuuint64_t row = static_cast<cuuint64_t>(d) * 4, uT = T, uH = heads;
+    cuuint64_t dim[4] = {static_cast<cuuint64_t>(d), uT, uH, static_cast<cuuint64_t>(B)};
+    cuuint64_t str[3] = {token_major ? row * uH : row, token_major ? row : row * uT, row * uH * uT};
+    cuuint32_t box[4] = {static_cast<cuuint32_t>(cols), C, 1, 1}, es[4] = {1, 1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, const_cast<void*>(base), dim, str, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               cols == 32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int MODE>
 cudaError_t walk(const GdnRecur& r, const float* fact, cudaStream_t stream) {
-    const size_t smem = static_cast<size_t>(WalkLayout(r.a.dk).floats) * 4;
+    const GdnArgs& a = r.a;
     static std::atomic<unsigned long long> seen;
-    cudaError_t e = allow_smem(k_gdn_walk<MODE>, static_cast<size_t>(WalkLayout(256).floats) * 4, seen);
+    cudaError_t e = allow_smem(k_gdn_walk<MODE>, static_cast<size_t>(WalkLayout(256).bytes), seen);
     if (e != cudaSuccess) return e;
-    k_gdn_walk<MODE><<<dim3((r.a.dv + CW - 1) / CW, r.a.H, r.a.B), NT, smem, stream>>>(r, fact);
+    const int64_t rows = static_cast<int64_t>(a.B) * a.H * ((a.T + C - 1) / C) * (FACT / C);
+    CUtensorMap tk, tq, tv, tf;
+    if (!float_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk, 32) || !float_map(&tq, a.q, a.token_major, a.B, a.Hk, a.T, a.dk, 32) ||
+        !float_map(&tv, MODE == 2 ? r.dy : a.v, a.token_major, a.B, a.H, a.T, a.dv, CW) ||
+        !float_map(&tf, fact, 0, 1, 1, static_cast<int>(rows), C, 32))
+        return cudaErrorInvalidValue;
+    k_gdn_walk<MODE><<<dim3((a.dv + CW - 1) / CW, a.H, a.B), NT + 32, WalkLayout(a.dk).bytes, stream>>>(tk, tq, tv, tf, r, fact);
     return cudaGetLastError();
 }
 
