@@ -27,7 +27,8 @@ using namespace gdn;
 
 constexpr int SW = 8;                          // compute warps: two share a lane quarter
 constexpr int ST = 32 * (SW + 4);
-constexpr int BACK_REGS = 232, IDLE_REGS = 40; // the split of the launch's 168 per thread
+constexpr int LAUNCH_REGS = 168, BACK_REGS = 232, IDLE_REGS = 40;   // a thread's registers, at first and after the split
+static_assert(BACK_REGS >= LAUNCH_REGS && IDLE_REGS <= LAUNCH_REGS && SW * BACK_REGS + 4 * IDLE_REGS <= (SW + 4) * LAUNCH_REGS, "register split");
 constexpr int NS = 2, NH = 3;                  // bf16 parts
 // TMEM columns: X: D^T K^T, then step 3; Z: dy^T P, then beta x; A: the update; S: D, then beta g d; dy; g dy.
 constexpr uint32_t X_COL = 0, Z_COL = 64, A_COL = 128, S_COL = 256, Y_COL = 384, GY_COL = 416, T_COLS = 512;
@@ -348,7 +349,7 @@ cudaError_t back(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap
         cudaFuncAttributes at;
         return cudaFuncGetAttributes(&at, k_gdn_back<DK>) == cudaSuccess ? at.numRegs : 0;
     }();
-    if (regs * ST < 32 * (SW * BACK_REGS + 4 * IDLE_REGS)) return cudaErrorInvalidConfiguration;
+    if (regs != LAUNCH_REGS) return cudaErrorInvalidConfiguration;
     static std::atomic<unsigned long long> seen;
     cudaError_t e = allow_smem(k_gdn_back<DK>, smem, seen);
     if (e != cudaSuccess) return e;

@@ -324,7 +324,9 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
 constexpr int SW = 8;                          // compute warps
 constexpr int OW = 4;                          // output warps
 constexpr int ST = 32 * (SW + OW + 4);
-constexpr int SCAN_REGS = 184, OUT_REGS = 104, IDLE_REGS = 40;   // the split of the launch's 128 per thread
+constexpr int LAUNCH_REGS = 128, SCAN_REGS = 184, OUT_REGS = 104, IDLE_REGS = 40;   // a thread's registers, at first and after the split
+static_assert(SCAN_REGS >= LAUNCH_REGS && OUT_REGS <= LAUNCH_REGS && IDLE_REGS <= LAUNCH_REGS &&
+              SW * SCAN_REGS + OW * OUT_REGS + 4 * IDLE_REGS <= (SW + OW + 4) * LAUNCH_REGS, "register split");
 constexpr int NS = 2;                          // bf16 parts of S, of beta r and of w as the factor of P
 constexpr int NH = 3;                          // bf16 parts of h w
 // TMEM columns: X: steps 1, 3, 5; Y: w P^T; S; R: beta r, then w.  h w lies where S is, which steps 2 to 6 do not read.
@@ -703,7 +705,7 @@ cudaError_t scan(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap
         cudaFuncAttributes at;
         return cudaFuncGetAttributes(&at, k_gdn_scan<DK, KEEP>) == cudaSuccess ? at.numRegs : 0;
     }();
-    if (regs * ST < 32 * (SW * SCAN_REGS + OW * OUT_REGS + 4 * IDLE_REGS)) return cudaErrorInvalidConfiguration;
+    if (regs != LAUNCH_REGS) return cudaErrorInvalidConfiguration;
     static std::atomic<unsigned long long> seen;
     cudaError_t e = allow_smem(k_gdn_scan<DK, KEEP>, smem, seen);
     if (e != cudaSuccess) return e;

@@ -30,7 +30,8 @@ using namespace tc;
 using namespace gdn;
 
 constexpr int SW = 8, NT = 32 * (SW + 4);
-constexpr int GRAD_REGS = 224, REST_REGS = 56; // the split of the launch's 168 per thread
+constexpr int LAUNCH_REGS = 168, GRAD_REGS = 224, REST_REGS = 56;   // a thread's registers, at first and after the split
+static_assert(GRAD_REGS >= LAUNCH_REGS && REST_REGS <= LAUNCH_REGS && SW * GRAD_REGS + 4 * REST_REGS <= (SW + 4) * LAUNCH_REGS, "register split");
 // X below its diagonal, row by row: row i (0 .. 64) has columns -1 .. i - 1
 __device__ __forceinline__ constexpr int x_at(int i, int col) { return i * (i + 1) / 2 + col; }      // column j: col = j + 1
 // TMEM columns
@@ -572,7 +573,7 @@ cudaError_t grads(const GdnGradsTc& r, cudaStream_t stream) {
         cudaFuncAttributes at;
         return cudaFuncGetAttributes(&at, k_gdn_grads_tc<DK>) == cudaSuccess ? at.numRegs : 0;
     }();
-    if (regs * NT < 32 * (SW * GRAD_REGS + 4 * REST_REGS)) return cudaErrorInvalidConfiguration;
+    if (regs != LAUNCH_REGS) return cudaErrorInvalidConfiguration;
     static std::atomic<unsigned long long> seen;
     cudaError_t e = allow_smem(k_gdn_grads_tc<DK>, smem, seen);
     if (e != cudaSuccess) return e;
