@@ -83,6 +83,8 @@ def lib_path() -> str:
 def lib():
     """Load libsdm.so (built in-tree); raises if it has not been built."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(_LIB_PATH):
