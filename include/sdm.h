@@ -317,7 +317,7 @@ sdm_status sdm_recur_backward_q(const sdm_shape* shape, const int32_t* idx_w, co
 
 /* Reads (host pointer `code`, synchronising on `stream`) and clears the device
  * status word of the current device: 0 = no fault; bit 0 = a slot index outside
- * [0, N) was skipped; bit 1 = a slot list given to the recurrence (forward, chunkwise
+ * [0, N) (or, of the gated delta rule, a length outside [0, T] or a slot not below n_slots) was skipped; bit 1 = a slot list given to the recurrence (forward, chunkwise
  * or backward) was not strictly ascending; bit 2 = a bounded device wait gave up (the
  * tensor-core score kernel's mbarrier waits, or the writer/reader hand-over of the
  * recurrence): the kernel returned early and its results are undefined; bit 3 = a
@@ -423,9 +423,11 @@ size_t sdm_gdn_backward_workspace_bytes(const sdm_gdn_shape* shape);
  * device: sequence b has lengths[b] tokens, and what q, k, v, alpha and beta hold past them is
  * never used (it may be NaN); y is zero there and the state stays.  A length outside [0, T] is
  * clamped and sets bit 0 of the device status word.  With T = 0 nothing is done.  bf16 calls with
- * d_k <= 128 take a chunked form on the tensor cores from 64 tokens up (chunks of 64 tokens;
- * operands split into bf16 parts wherever the state depends on them); others go token by token
- * in fp32. */
+ * d_k <= 128 and T >= 64 run in chunks of 64 tokens on the tensor cores (operands that the state
+ * depends on are split into bf16 parts, so that the state is off by about 1e-6); float32 calls with
+ * T >= 32 and few sequences and heads in chunks of 32 tokens in fp32; others token by token in
+ * fp32.  Infinities in a live token reach the tokens of its chunk, earlier ones too.
+ * workspace: sdm_gdn_workspace_bytes(shape), 256-byte aligned; calls that overlap must not share it. */
 sdm_status sdm_gdn_forward(const sdm_gdn_shape* shape, const void* q, const void* k, const void* v,
                            const void* alpha, const void* beta, const int32_t* lengths, float* state,
                            void* y, void* workspace, size_t workspace_bytes, sdm_stream_t stream);
