@@ -90,11 +90,11 @@ struct GdnGrads {
 cudaError_t launch_gdn_grads(int dtype, const GdnGrads& g, cudaStream_t stream);
 
 // ---- chunked form on the tensor cores (k_gdn_chunk.cu): bf16, d_k <= 128, chunks of 64 ----
-// What the chunks' own products are, per (sequence, head, chunk): three or four bf16 matrices [64][64]
-// (N as upper and lower parts, P and, for the backward, P's lower part) and three rows of 64 floats.
+// What the chunks' own products are, per (sequence, head, chunk): three to five bf16 matrices [64][64]
+// (N as upper and lower parts, P and, for the backward, P's lower parts) and three rows of 64 floats.
 struct GdnFactors {
     void* mat;                // [B, H, nc, mats, 64, 64] bf16
-    int mats;
+    int mats;                 // 3, or for the backward gdn_back_mats
     float* gates;             // [B, H, nc, 3, 64]: prod_{l <= i} alpha_l, beta_i, prod_{l > i} alpha_l
 };
 size_t gdn_factor_mat_bytes(int64_t chunks, int mats);
@@ -112,7 +112,9 @@ struct GdnScan {
 };
 cudaError_t launch_gdn_scan(const GdnScan& s, const GdnFactors& f, cudaStream_t stream);
 
-// The backward's walk (k_gdn_back.cu), with f.mats == 4.
+// The backward's walk (k_gdn_back.cu), with f.mats == gdn_back_mats(dk): N in two bf16 parts, P in two, or three
+// with d_k <= 64, where its entries are larger.
+__host__ __device__ constexpr int gdn_back_mats(int dk) { return dk <= 64 ? 5 : 4; }
 struct GdnBack {
     GdnArgs a;
     const void* dy;

@@ -29,13 +29,16 @@ constexpr int SW = 8;                          // compute warps: two share a lan
 constexpr int ST = 32 * (SW + 4);
 constexpr int LAUNCH_REGS = 168, BACK_REGS = 232, IDLE_REGS = 40;   // a thread's registers, at first and after the split
 static_assert(BACK_REGS >= LAUNCH_REGS && IDLE_REGS <= LAUNCH_REGS && SW * BACK_REGS + 4 * IDLE_REGS <= (SW + 4) * LAUNCH_REGS, "register split");
-constexpr int NS = 2, NH = 3;                  // bf16 parts
-// TMEM columns: X: D^T K^T, then step 3; Z: dy^T P, then beta x; A: the update; S: D, then beta g d; dy; g dy.
-constexpr uint32_t X_COL = 0, Z_COL = 64, A_COL = 128, S_COL = 256, Y_COL = 384, GY_COL = 416, T_COLS = 512;
+constexpr int NH = 3;                          // bf16 parts of what is added to D
+template <int DK> constexpr int PARTS = DK == 64 ? 3 : 2;        // of D and of beta x (see the forward walk)
+// TMEM columns: X: D^T K^T, then step 3; Z: dy^T P, then beta x (with d_k <= 64 its third part behind A); A: the update;
+// S: D, then beta g d; dy; g dy.
+constexpr uint32_t X_COL = 0, Z_COL = 64, A_COL = 128, S_COL = 256, Z3_COL = 192, Y_COL = 384, GY_COL = 416, T_COLS = 512;
 
 template <int DK>
 struct BackTile {
-    static constexpr uint32_t KQ = 0, Y = 128 * 2 * DK, M = Y + C * 256, BYTES = M + 4 * MAT;
+    static constexpr int MATS = gdn_back_mats(DK);            // N and P in their parts
+    static constexpr uint32_t KQ = 0, Y = 128 * 2 * DK, M = Y + C * 256, BYTES = M + MATS * MAT;
     static constexpr uint32_t LOAD = BYTES + GATES;
     static constexpr int STAGES = 2;
     // boxes of 128 columns on their way to memory (D per 64 of d_k, d per part), then the stages' gate products
@@ -88,7 +91,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
     tc_after_sync();
     const uint32_t tmem = ctl.tmem;
     volatile int* dead = &ctl.dead;
-    constexpr int SB = DK / 2;                               // TMEM columns of a part of D
+    constexpr int SB = DK / 2, NP = PARTS<DK>;               // TMEM columns of a part of D; parts
 
     if (warp >= SW) {
         regs_dec<IDLE_REGS>();
@@ -102,7 +105,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 await(bar(B_DY), ph, dead);
                 if (elect_one()) {                           // step 1
 #pragma unroll
-                    for (int p = 0; p < 2; ++p)
+                    for (int p = 0; p < L::MATS - 2; ++p)
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
                             mma_bf16_ta(tmem + Z_COL, tmem + Y_COL + kk * 8, dp + p * (MAT / 16) + kk * 128, idm, (p | kk) != 0);
@@ -111,7 +114,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 await(bar(B_S), ph, dead);
                 if (elect_one()) {
 #pragma unroll
-                    for (int p = 0; p < NS; ++p)
+                    for (int p = 0; p < NP; ++p)
 #pragma unroll
                         for (int kk = 0; kk < DK / 16; ++kk)
                             mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * SB + kk * 8, dk + (kk / 4) * 1024 + (kk % 4) * 2, id64, (p | kk) != 0);
@@ -124,12 +127,15 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 }
                 __syncwarp();
                 await(bar(B_X), ph, dead);
-                if (elect_one()) {                           // step 3: (upper, upper), (upper, lower), (lower, upper)
+                if (elect_one()) {                           // step 3: part xa of beta x with part nb of N
 #pragma unroll
-                    for (int m = 0; m < 3; ++m)
+                    for (int m = 0; m < (NP == 3 ? 5 : 3); ++m) {
+                        const int xa = m / 2, nb = m % 2;    // (0, 0), (0, 1), (1, 0) and then (1, 1), (2, 0)
+                        const uint32_t from = xa == 2 ? Z3_COL : Z_COL + xa * 32;
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
-                            mma_bf16_ta(tmem + X_COL, tmem + Z_COL + (m == 2 ? 32 : 0) + kk * 8, dn + (m == 1 ? MAT / 16 : 0) + kk * 128, idm, (m | kk) != 0);
+                            mma_bf16_ta(tmem + X_COL, tmem + from + kk * 8, dn + nb * (MAT / 16) + kk * 128, idm, (m | kk) != 0);
+                    }
                     mma_commit(bar(B_XN));
                 }
                 __syncwarp();
@@ -158,7 +164,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 tma_load_4d(t + L::Y, &ty, col0, c * C, h, b, fb);
                 tma_load_4d(t + L::Y + 8192, &ty, col0 + 64, c * C, h, b, fb);
 #pragma unroll
-                for (int m = 0; m < 4; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * 4 + m) * C), fb);
+                for (int m = 0; m < L::MATS; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * L::MATS + m) * C), fb);
                 bulk_load(ring + L::G + (it % L::STAGES) * GATES, f.gates + cid * 3 * C, GATES, fb);
             };
             int loaded = 0;
@@ -218,7 +224,8 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                     *reinterpret_cast<uint4*>(ringp + L::KS + at / 64 * 16384 + box_at(row, at % 64 / 8)) = w;
                 };
                 put_part(lanes + S_COL + (half * RD + x) / 2, v, keep);
-                put_last(lanes + S_COL + SB + (half * RD + x) / 2, v);
+                if (NP == 3) put_part(lanes + S_COL + SB + (half * RD + x) / 2, v);
+                put_last(lanes + S_COL + (NP - 1) * SB + (half * RD + x) / 2, v);
             }
             announce(bar(B_S), lane);
             hand_over(bar(B_KS), lane);
@@ -284,7 +291,8 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 }
             }
             put_part(lanes + Z_COL + i0 / 2, w);
-            put_last(lanes + Z_COL + 32 + i0 / 2, w);
+            if (NP == 3) put_part(lanes + Z_COL + 32 + i0 / 2, w);
+            put_last(lanes + (NP == 3 ? Z3_COL : Z_COL + 32) + i0 / 2, w);
             announce(bar(B_X), lane);
             const float g63 = gate[C - 1];
             await(bar(B_XN), ph, dead);
@@ -361,12 +369,13 @@ cudaError_t back(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap
 
 cudaError_t launch_gdn_back(const GdnBack& r, const GdnFactors& f, cudaStream_t stream) {
     const GdnArgs& a = r.a;
+    if (f.mats != gdn_back_mats(a.dk)) return cudaErrorInvalidValue;
     const int64_t chunks = static_cast<int64_t>(a.B) * a.H * ((a.T + C - 1) / C);
     const int nblk = (a.dv + 127) / 128;
     CUtensorMap tk, tq, ty, tdv, tm, tD, td;
     if (!token_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk) || !token_map(&tq, a.q, a.token_major, a.B, a.Hk, a.T, a.dk) ||
         !token_map(&ty, r.dy, a.token_major, a.B, a.H, a.T, a.dv) || !token_map(&tdv, r.dv, a.token_major, a.B, a.H, a.T, a.dv) ||
-        !row_map(&tm, f.mat, chunks * 4 * C, C, C) || !row_map(&tD, r.keep_D, chunks * nblk * 128, a.dk <= 64 ? 64 : 128, 128) ||
+        !row_map(&tm, f.mat, chunks * f.mats * C, C, C) || !row_map(&tD, r.keep_D, chunks * nblk * 128, a.dk <= 64 ? 64 : 128, 128) ||
         !row_map(&td, r.keep_d, chunks * 2 * nblk * 128, C, 128))
         return cudaErrorInvalidValue;
     return a.dk <= 64 ? back<64>(tk, tq, ty, tdv, tm, tD, td, r, f, stream) : back<128>(tk, tq, ty, tdv, tm, tD, td, r, f, stream);

@@ -12,7 +12,9 @@
 // Precision: the state and every sum are fp32.  k and q are exact operands.  What the state depends on
 // and is not a bf16 number enters the MMAs as bf16 parts: S, N and beta r as two (16 significant
 // bits; products of two lower parts are left out), h w, whose rounding the state would keep, as three.
-// e takes r itself in fp32.  y alone takes P rounded to bf16 once, as y is.
+// e takes r itself in fp32.  With d_k <= 64, where keys are less orthogonal and the products shorter, S and beta r
+// have three parts as well and the product of two lower parts is taken (the state's error at d_k = 32 is 1.5e-6
+// without).  y alone takes P rounded to bf16 once, as y is.
 #include "gdn_tc.cuh"
 
 namespace sdm {
@@ -180,7 +182,8 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
 #pragma unroll
                 for (int j = 4; j < 8; ++j) {
                     P[j] = make_uint4(0, 0, 0, 0);
-                    if (f.mats == 4) P[MAT / 16 + j] = make_uint4(0, 0, 0, 0);
+                    if (f.mats > 3) P[MAT / 16 + j] = make_uint4(0, 0, 0, 0);
+                    if (f.mats > 4) P[2 * MAT / 16 + j] = make_uint4(0, 0, 0, 0);
                 }
             }
             continue;
@@ -212,7 +215,12 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
 #pragma unroll
                 for (int e = 0; e < 4; ++e) w[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
                 P[4 * half + j] = make_uint4(w[0], w[1], w[2], w[3]);
-                if (f.mats == 4) P[MAT / 16 + 4 * half + j] = pack16<BF16>(v);     // its lower part
+                if (f.mats > 3) {                                             // its lower parts
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
+                    P[MAT / 16 + 4 * half + j] = make_uint4(w[0], w[1], w[2], w[3]);
+                    if (f.mats > 4) P[2 * MAT / 16 + 4 * half + j] = pack16<BF16>(v);
+                }
             }
         }
     }
@@ -327,11 +335,12 @@ constexpr int ST = 32 * (SW + OW + 4);
 constexpr int LAUNCH_REGS = 128, SCAN_REGS = 184, OUT_REGS = 104, IDLE_REGS = 40;   // a thread's registers, at first and after the split
 static_assert(SCAN_REGS >= LAUNCH_REGS && OUT_REGS <= LAUNCH_REGS && IDLE_REGS <= LAUNCH_REGS &&
               SW * SCAN_REGS + OW * OUT_REGS + 4 * IDLE_REGS <= (SW + OW + 4) * LAUNCH_REGS, "register split");
-constexpr int NS = 2;                          // bf16 parts of S, of beta r and of w as the factor of P
+constexpr int NS = 2;                          // bf16 parts of S and of w as the factors of Q and P
+template <int DK> constexpr int PARTS = DK == 64 ? 3 : 2;        // of S as the factor of K, and of beta r
 constexpr int NH = 3;                          // bf16 parts of h w
 // TMEM columns: X: steps 1, 3, 5; Y: w P^T; S; R: beta r, then w.  h w lies where S is, which steps 2 to 6 do not read.
 constexpr uint32_t X_COL = 0, Y_COL = 128, S_COL = 192, R_COL = S_COL + 128, T_COLS = 512;
-static_assert(R_COL + 32 * NS <= T_COLS && 32 * NH <= 128 && 64 * NS <= 128, "TMEM columns");
+static_assert(R_COL + 32 * 3 <= T_COLS && 32 * NH <= 128 && 64 * PARTS<128> <= 128 && 32 * PARTS<64> <= 128, "TMEM columns");
 
 template <int DK, bool KEEP>
 struct ScanTile {
@@ -383,7 +392,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
     tc_after_sync();
     const uint32_t tmem = ctl.tmem;
     volatile int* dead = &ctl.dead;
-    constexpr int SB = DK / 2;                               // TMEM columns of a part of S
+    constexpr int SB = DK / 2, NP = PARTS<DK>;               // TMEM columns of a part of S; parts
 
     if (warp >= SW + OW) {
         regs_dec<IDLE_REGS>();
@@ -397,7 +406,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 await(bar(B_S), ph, dead);
                 if (elect_one()) {                           // step 1
 #pragma unroll
-                    for (int p = 0; p < NS; ++p)
+                    for (int p = 0; p < NP; ++p)
 #pragma unroll
                         for (int kk = 0; kk < DK / 16; ++kk)
                             mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * SB + kk * 8, dk + (kk / 4) * 1024 + (kk % 4) * 2, id64, (p | kk) != 0);
@@ -413,12 +422,14 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 }
                 __syncwarp();
                 await(bar(B_R), ph, dead);
-                if (elect_one()) {                           // step 3: (upper, upper), (upper, lower), (lower, upper)
+                if (elect_one()) {                           // step 3: part ra of beta r with part nb of N
 #pragma unroll
-                    for (int m = 0; m < 3; ++m)
+                    for (int m = 0; m < (NP == 3 ? 5 : 3); ++m) {
+                        const int ra = m / 2, nb = m % 2;    // (0, 0), (0, 1), (1, 0) and then (1, 1), (2, 0)
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
-                            mma_bf16_ta(tmem + X_COL, tmem + R_COL + (m == 2 ? 32 : 0) + kk * 8, dm + (m == 1 ? MAT / 16 : 0) + kk * 2, id64, (m | kk) != 0);
+                            mma_bf16_ta(tmem + X_COL, tmem + R_COL + ra * 32 + kk * 8, dm + nb * (MAT / 16) + kk * 2, id64, (m | kk) != 0);
+                    }
                     mma_commit(bar(B_RN));
                 }
                 __syncwarp();
@@ -577,7 +588,8 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                     if (KEEP) *reinterpret_cast<uint4*>(ringp + L::KS + at / 64 * 16384 + box_at(row, at % 64 / 8)) = w;
                 };
                 put_part(lanes + S_COL + (half * RD + x) / 2, v, keep);
-                put_last(lanes + S_COL + SB + (half * RD + x) / 2, v);
+                if (NP == 3) put_part(lanes + S_COL + SB + (half * RD + x) / 2, v);
+                put_last(lanes + S_COL + (NP - 1) * SB + (half * RD + x) / 2, v);
             }
             if (len - next * C < C) {                        // K rows past the length: zeros, whatever was there
                 const int n = len - next * C, s = next % L::STAGES;
@@ -626,7 +638,8 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
 #pragma unroll
             for (int j = 0; j < 32; ++j) w[j] = be[j] * u[j];
             put_part(lanes + R_COL + i0 / 2, w);
-            put_last(lanes + R_COL + 32 + i0 / 2, w);
+            if (NP == 3) put_part(lanes + R_COL + 32 + i0 / 2, w);
+            put_last(lanes + R_COL + 32 * (NP - 1) + i0 / 2, w);
             announce(bar(B_R), lane);
             const float g63 = gate[C - 1];
             if (!KEEP) await(bar(B_QS), ph, dead);           // S is read: h w may lie there
