@@ -423,7 +423,7 @@ size_t sdm_gdn_backward_workspace_bytes(const sdm_gdn_shape* shape);
  * device: sequence b has lengths[b] tokens, and what q, k, v, alpha and beta hold past them is
  * never used (it may be NaN); y is zero there and the state stays.  A length outside [0, T] is
  * clamped and sets bit 0 of the device status word.  With T = 0 nothing is done.  bf16 calls with
- * d_k <= 128 and T >= 64 run in chunks of 64 tokens on the tensor cores (operands that the state
+ * d_k <= 128 and T >= 32 run in chunks of 64 tokens on the tensor cores (operands that the state
  * depends on are split into bf16 parts, so that the state is off by about 1e-6); float32 calls with
  * T >= 32 and few sequences and heads in chunks of 32 tokens in fp32; others token by token in
  * fp32.  Infinities in a live token reach the tokens of its chunk, earlier ones too.

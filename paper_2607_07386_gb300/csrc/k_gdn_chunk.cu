@@ -32,8 +32,8 @@ using namespace gdn;
 // the block diagonals below in order, with Z_ii = (I + B_ii beta)^-1 = I + N_ii beta:
 //   N_ij = -Z_ii sum_{j <= k < i} B_ik Y_kj,  Y = I + beta N,  a warp per 16 x 16 product, a lane per
 // 4 x 2 outputs (one 16-byte and one 8-byte shared-memory read per 8 multiply-adds; B and Z_ii lie
-// transposed for that).  Shared-memory reads bound the kernel: with 4 x 1 outputs per thread they
-// kept the pipe 80% busy.  Eliminating whole columns of 64 in registers was slower still: 2016 unrolled
+// transposed for that).  Shared-memory reads bound the kernel (64% of the pipe; 80% with 4 x 1 outputs per thread): 119 us
+// at B = 8, H = 16, T = 4096, d_k = 128, where q, k, N and P alone take 69.  Eliminating whole columns of 64 in registers was slower still: 2016 unrolled
 // instructions, whose fetching took 11,600 of a CTA's 20,000 cycles.
 // ------------------------------------------------------------------------------------------
 constexpr int FT = 128;
@@ -326,8 +326,8 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
 // bf16, transposed as the threads hold them, through boxes in shared memory (16-byte stores of the threads' own,
 // a row of 256 bytes apart, cost 95 us of 310 at the layer shape), and the state stays as it was.
 //
-// The chain of six stages is what bounds it, then the tensor pipe (2432 cycles of MMAs per chunk at d_k =
-// 128).
+// The chain of six stages is what bounds it: 5,700 cycles a chunk (200 us at B = 8, H = 16, T = 4096, 128 x 128), of which
+// the MMAs take 2,432, the hand-overs about 700 and the registers (sums and conversions to bf16 parts) the rest.
 // ------------------------------------------------------------------------------------------
 constexpr int SW = 8;                          // compute warps
 constexpr int OW = 4;                          // output warps
@@ -731,8 +731,10 @@ cudaError_t scan(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap
 size_t gdn_factor_mat_bytes(int64_t chunks, int mats) { return static_cast<size_t>(chunks) * mats * MAT; }
 size_t gdn_factor_gate_bytes(int64_t chunks) { return static_cast<size_t>(chunks) * GATES; }
 
-// From one whole chunk up: below, the token recurrence is one launch of about the same length.
-bool gdn_chunk_supported(int dtype, int dk, int T) { return dtype == SDM_BF16 && dk <= 128 && T >= C; }
+// A chunk costs the same however few tokens it holds.  Forward, H = 16, 128 x 128: 18.9 us for one chunk against 18.8 (31.0)
+// token by token for 32 (63) tokens at B = 2, 29 against 39 for 31 tokens at B = 16; backward, B = 2: 45 us against
+// 81 for 31 tokens.
+bool gdn_chunk_supported(int dtype, int dk, int T) { return dtype == SDM_BF16 && dk <= 128 && T >= 32; }
 
 cudaError_t launch_gdn_factors(const GdnArgs& a, const GdnFactors& f, cudaStream_t stream) {
     CUtensorMap tk, tq;

@@ -11,7 +11,7 @@
 // three butterfly steps over the groups.  Blocks of TB tokens of q, k and v come through a
 // double-buffered cp.async ring shared by the warps of the CTA.
 //
-// Long calls are bound by the instructions of the chain.  A single token has a kernel of its own,
+// Bound by the latency of the chain, about 0.27 us a token up to two CTAs an SM.  A single token has a kernel of its own,
 // k_gdn_step, below.
 #include "gdn_internal.h"
 
@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS) k_gdn_recur(const GdnRecur r) 
 // a warp 32 rows of them, a lane 8 rows x 4 columns (a warp's load is four whole 128-byte row pieces), all
 // in flight before anything is waited for but the slot.  Sums over d_k: two butterfly steps, then the warps'
 // shares through shared memory.  At B = 256, H = 16, d_k = d_v = 128 the kernel above, with its staging and
-// 1,420 instructions a warp, took 145 us for 541 MB.
+// 1,420 instructions a warp, took 145 us for 541 MB; this one takes 84, 0.95 of the rate of a plain copy.
 template <class D>
 __device__ __forceinline__ void load8(const void* base, int64_t at, int left, float (&f)[8]) {
 #pragma unroll

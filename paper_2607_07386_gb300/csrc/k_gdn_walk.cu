@@ -11,8 +11,9 @@
 // 4 x 2 tile of them (six 16-byte reads per 32 multiply-adds).
 //
 // A chunk is four dependent products in place of 32 dependent tokens: with few sequences and heads the
-// latency of the chain is what counts, and this form has about a fifth of the token recurrence's.  With many, the
-// token recurrence's registers win over these shared-memory reads (see launch_gdn_walk's rule).
+// latency of the chain is what counts (one head, T = 256, 64 x 64: 31 us here and 8 us for the factors, 70 us token by
+// token).  With many, the token recurrence's registers win over these shared-memory reads (see gdn_walk_supported).
+// A warp or two on a scheduler issue an instruction every third cycle or so: that bounds it, not the reads.
 #include "gdn_tc.cuh"
 
 namespace sdm {
@@ -486,9 +487,10 @@ cudaError_t walk(const GdnRecur& r, const float* fact, cudaStream_t stream) {
 
 size_t gdn_walk_bytes(int64_t chunks) { return static_cast<size_t>(chunks) * FACT * 4; }
 
+// Up to two CTAs an SM.  Forward, T = 512, d_k = d_v = 128: 126 us here against 191 of the token recurrence at 256 CTAs,
+// 246 against 195 at 512; with 64 x 64: 97 against 141 at 256, 187 against 148 at 576.
 bool gdn_walk_supported(int dtype, int B, int H, int T, int dv) {
-    // the rule: the token recurrence has 0.27 us a token whatever the width, up to its 8 warps an SM
-    return dtype == SDM_F32 && T >= C && static_cast<int64_t>(B) * H * ((dv + CW - 1) / CW) <= 152 * 8;
+    return dtype == SDM_F32 && T >= C && static_cast<int64_t>(B) * H * ((dv + CW - 1) / CW) <= 152 * 2;
 }
 
 cudaError_t launch_gdn_walk(int mode, const GdnRecur& r, float* fact, cudaStream_t stream) {

@@ -7,7 +7,9 @@
 // contiguous along k or along its rows (the MMA descriptors take either, so nothing is transposed).
 // It is persistent and specialised by warp: one thread streams K-blocks of 64 of both operands
 // through a ring of shared memory by TMA, one thread issues the MMAs into one of two TMEM
-// accumulators, four warps take the other accumulator through the epilogue.  Every wait is bounded.
+// accumulators, eight warps take the other accumulator through the epilogue.  Every wait is bounded.  Bound by the
+// tensor pipe under the power limit: 32768 x 2048 x 2048 with silu, bias and residual takes 178 us alone (1.55
+// PFLOP/s) and 207 us in a row of calls; dx and dW of it 165 and 176 us alone.
 //
 // Two CTAs of a cluster take tiles one above the other and share the columns' operand: each loads half of it
 // for both (TMA multicast), so a K-block costs 256 rows of loads in place of 384.  A stage is free once the MMAs of
