@@ -7,13 +7,14 @@
 //             D' = g_31 D + scale Q^T (g dy) - K^T (beta g d)
 // k_gdn_factors32 makes N and P (or their transposes) and g, beta, h of every chunk at once.  k_gdn_walk
 // owns 16 columns of one state, which stay in shared memory, transposed, beside the double-buffered tiles
-// of the chunk.  Every product is a dot product along rows of two padded shared-memory matrices, a thread a
-// 4 x 2 tile of them (six 16-byte reads per 32 multiply-adds).
+// of the chunk.  Every product is a dot product along rows of two shared-memory matrices, a thread a 2 x 2 tile
+// of them (four 16-byte reads per 16 multiply-adds).  Eight warps: four for K's and N's products, four for Q's and P's
+// beside them; four warps with 4 x 2 tiles read less and took 31 us in place of 25 below.
 //
 // A chunk is four dependent products in place of 32 dependent tokens: with few sequences and heads the
-// latency of the chain is what counts (one head, T = 256, 64 x 64: 31 us here and 8 us for the factors, 70 us token by
+// latency of the chain is what counts (one head, T = 256, 64 x 64: 25 us here and 8 us for the factors, 70 us token by
 // token).  With many, the token recurrence's registers win over these shared-memory reads (see gdn_walk_supported).
-// A warp or two on a scheduler issue an instruction every third cycle or so: that bounds it, not the reads.
+// Two warps on a scheduler and a barrier after each product: that latency bounds it, not the reads.
 #include "gdn_tc.cuh"
 
 namespace sdm {
@@ -24,7 +25,8 @@ using namespace tc;
 
 constexpr int C = GDN_C32;
 constexpr int CW = 16;                   // columns of a CTA
-constexpr int NT = 128;                  // computing threads; a warp beside them fetches
+constexpr int NT = 256;                  // computing threads of the walk; a warp beside them fetches
+constexpr int FT = 128;                  // threads of the factors
 constexpr int CP = C + 4;                // padded row of a [.][32] matrix
 constexpr int FACT = 2 * C * C + 3 * C;  // floats of a chunk's factors: N, P, g, beta, h (67 rows of 32)
 constexpr int BOX = C * 128;             // bytes of 32 rows x 32 floats, swizzled as TMA leaves them
@@ -100,7 +102,7 @@ struct Boxed {
 // Factors of a chunk: 128 threads; threads 0-63 take k.k, 64-127 q.k, 4 x 4 each.  N by a column per lane of the
 // first warp: N_ic = -(B_ic + sum_{c < k < i} B_ik beta_k N_kc).
 // ------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(NT) k_gdn_factors32(const GdnArgs a, float* __restrict__ out, int transposed) {
+__global__ void __launch_bounds__(FT) k_gdn_factors32(const GdnArgs a, float* __restrict__ out, int transposed) {
     extern __shared__ __align__(16) float sm[];
     const int ld = a.dk + 4;
     float* const kq = sm;                      // [64][dk + 4]: K, then Q
@@ -113,7 +115,7 @@ __global__ void __launch_bounds__(NT) k_gdn_factors32(const GdnArgs a, float* __
     const int n = len - t0 < C ? len - t0 : C;
     const int64_t chain = static_cast<int64_t>(b) * a.H + h;
     const int64_t kb = gdn_base(a.token_major, b, hk, a.Hk, a.T, a.dk), ks = gdn_stride(a.token_major, a.Hk, a.dk);
-    for (int row = tid >> 4; row < 2 * C; row += NT / 16) {            // 16 threads a row
+    for (int row = tid >> 4; row < 2 * C; row += FT / 16) {            // 16 threads a row
         const int t = row % C;
         const float* src = static_cast<const float*>(row < C ? a.k : a.q) + kb + (t0 + t) * ks;
         for (int x = (tid & 15) * 4; x < a.dk; x += 64) cp16(kq + row * ld + x, t < n ? src + x : static_cast<const float*>(a.k), t < n);
@@ -203,7 +205,7 @@ __global__ void __launch_bounds__(NT) k_gdn_factors32(const GdnArgs a, float* __
 // Grid (column blocks of 16, H, B).
 // ------------------------------------------------------------------------------------------
 struct WalkLayout {                            // bytes
-    int nb, ld, Q, F, V, G, stage, S, U, W, Y, bytes;
+    int nb, ld, Q, F, V, G, stage, S, X, U, W, Y, bytes;
     __host__ __device__ explicit WalkLayout(int dk) {
         nb = (dk + 31) / 32;                   // boxes of K (and Q)
         ld = dk + 4;                           // floats of a row of S
@@ -213,7 +215,8 @@ struct WalkLayout {                            // bytes
         G = V + C * CW * 4;                    // g, beta, h
         stage = G + 1024;
         S = 2 * stage;                         // [16][dk + 4]
-        U = S + CW * ld * 4;                   // [16][36] each: beta r (or beta x); h w (or -beta g d); w (or dy)
+        X = S + CW * ld * 4;                   // reverse: Q's share of the update, as S
+        U = X + CW * ld * 4;                   // [16][36] each: beta r (or beta x); h w (or -beta g d); w (or dy)
         W = U + CW * CP * 4;
         Y = W + CW * CP * 4;
         bytes = 1024 + Y + CW * CP * 4;
@@ -291,8 +294,8 @@ __global__ void __launch_bounds__(NT + 32) k_gdn_walk(const __grid_constant__ CU
                 for (int j = it > 2 ? it - 2 : 0; j < it; ++j) mbar_wait(smem_u32(&full[j & 1]), j / 2 & 1);
         }
     } else {
-    // 4 x 2 tiles: tokens 4 tr .. and columns tc, tc + 8; threads 0-63 take K's (N's) rows, 64-127 Q's (P's)
-    const int tr = tid >> 3 & 7, tc = tid & 7, hi = tid >> 6;
+    // 2 x 2 tiles: tokens 2 tr, 2 tr + 1 and columns tc, tc + 8; threads 0-127 take K's (N's) rows, 128-255 Q's (P's)
+    const int tr = tid >> 3 & 15, tc = tid & 7, hi = tid >> 7, upto = (2 * tr + 5) & ~3;     // tokens up to the tile's last
     for (int it = 0; it < chunks; ++it) {
         const int ch = chunk_of(it), t0 = ch * C, n = len - t0 < C ? len - t0 : C;
         unsigned char* const st = sm + (it & 1) * L.stage;
@@ -313,37 +316,37 @@ __global__ void __launch_bounds__(NT + 32) k_gdn_walk(const __grid_constant__ CU
         }
         bar_walk();                                            // the tiles are in; the last chunk's S is written
         if (MODE != 0) save(r.marks + (chain * nc + ch) * per);
-        float acc[4][2] = {}, out[4][2] = {};
-        if (MODE == 2) {                                       // dy, and scale P^T dy (threads 64-127)
+        float acc[2][2] = {}, out[2][2] = {};
+        if (MODE == 2) {                                       // dy, and scale P^T dy (the upper half of the threads)
             for (int i = tid; i < C * CW; i += NT) Y[(i % CW) * CP + i / CW] = V[i];
             bar_walk();
-            if (hi) tile<4, 2>(Boxed{F + BOX, 4 * tr}, Y + tc * CP, 8 * CP, C, acc);
-            else tile<4, 2>(Boxed{K, 4 * tr}, S + tc * L.ld, 8 * L.ld, a.dk, acc);
+            if (hi) tile<2, 2>(Boxed{F + BOX, 2 * tr}, Y + tc * CP, 8 * CP, C, acc);
+            else tile<2, 2>(Boxed{K, 2 * tr}, S + tc * L.ld, 8 * L.ld, a.dk, acc);
             if (hi) {
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) W[(tc + 8 * c) * CP + 4 * tr + m] = a.scale * acc[m][c];
+                    for (int c = 0; c < 2; ++c) W[(tc + 8 * c) * CP + 2 * tr + m] = a.scale * acc[m][c];
             }
             bar_walk();
             if (!hi) {                                         // x
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const int t = 4 * tr + m;
+                        const int t = 2 * tr + m;
                         acc[m][c] = fmaf(hh[t], acc[m][c], W[(tc + 8 * c) * CP + t]);
                         U[(tc + 8 * c) * CP + t] = be[t] * acc[m][c];
                     }
             }
             bar_walk();
             if (!hi) {                                         // d; N is strictly lower, its transpose upper
-                tile<4, 2>(Boxed{F, 4 * tr}, U + tc * CP, 8 * CP, C, acc);
+                tile<2, 2>(Boxed{F, 2 * tr}, U + tc * CP, 8 * CP, C, acc);
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const int t = 4 * tr + m, col = col0 + tc + 8 * c;
+                        const int t = 2 * tr + m, col = col0 + tc + 8 * c;
                         W[(tc + 8 * c) * CP + t] = -be[t] * g[t] * acc[m][c];
                         if (t < n && col < a.dv) {
                             y[vb + (t0 + t) * vs + col] = be[t] * acc[m][c];
@@ -352,34 +355,34 @@ __global__ void __launch_bounds__(NT + 32) k_gdn_walk(const __grid_constant__ CU
                     }
             } else {                                           // scale g dy
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const int t = 4 * tr + m;
+                        const int t = 2 * tr + m;
                         Y[(tc + 8 * c) * CP + t] *= a.scale * g[t];
                     }
             }
             bar_walk();
         } else {
-            if (MODE == 0 || !hi) tile<4, 2>(Boxed{hi ? st + L.Q : K, 4 * tr}, S + tc * L.ld, 8 * L.ld, a.dk, acc);   // K S, Q S
+            if (MODE == 0 || !hi) tile<2, 2>(Boxed{hi ? st + L.Q : K, 2 * tr}, S + tc * L.ld, 8 * L.ld, a.dk, acc);   // K S, Q S
             if (!hi) {
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const int t = 4 * tr + m;
+                        const int t = 2 * tr + m;
                         acc[m][c] = t < n ? V[t * CW + tc + 8 * c] - g[t] * acc[m][c] : 0.f;
                         U[(tc + 8 * c) * CP + t] = be[t] * acc[m][c];
                     }
             }
             bar_walk();
             if (!hi) {                                         // e
-                tile<4, 2>(Boxed{F, 4 * tr}, U + tc * CP, 8 * CP, 4 * tr + 4, acc);
+                tile<2, 2>(Boxed{F, 2 * tr}, U + tc * CP, 8 * CP, upto, acc);
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const int t = 4 * tr + m, col = col0 + tc + 8 * c;
+                        const int t = 2 * tr + m, col = col0 + tc + 8 * c;
                         const float w = be[t] * acc[m][c];
                         W[(tc + 8 * c) * CP + t] = hh[t] * w;
                         if (MODE == 0) Y[(tc + 8 * c) * CP + t] = w;
@@ -388,58 +391,77 @@ __global__ void __launch_bounds__(NT + 32) k_gdn_walk(const __grid_constant__ CU
             }
             bar_walk();
             if (MODE == 0 && hi) {
-                tile<4, 2>(Boxed{F + BOX, 4 * tr}, Y + tc * CP, 8 * CP, 4 * tr + 4, out);
+                tile<2, 2>(Boxed{F + BOX, 2 * tr}, Y + tc * CP, 8 * CP, upto, out);
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const int t = 4 * tr + m, col = col0 + tc + 8 * c;
+                        const int t = 2 * tr + m, col = col0 + tc + 8 * c;
                         if (t < n && col < a.dv) y[vb + (t0 + t) * vs + col] = a.scale * fmaf(g[t], acc[m][c], out[m][c]);
                     }
             }
         }
-        // S[c][x] = g_31 S + sum_t (h w)[c][t] K[t][x]: four x and two columns a thread
+        // S[c][x] = g_31 S + sum_t (h w)[c][t] K[t][x]: four x and two columns a thread; in reverse the other half of the
+        // threads takes Q's share
         const float gl = g[C - 1];
-        for (int p = tid; p < a.dk * 2; p += NT) {             // dk / 4 quads x 8 column pairs
+        float* const X = reinterpret_cast<float*>(sm + L.X);
+        const int first = MODE == 2 ? tid & 127 : tid, step = MODE == 2 ? 128 : NT;
+        auto share = [&](int p, const Boxed& A, const float* B0, float2 (&s0)[2], float2 (&s1)[2]) {
+            const int x = (p >> 3) * 4;
+            float4 w[2][2], k[2][4];
+            auto load = [&](int to, int t) {
+                w[to][0] = *reinterpret_cast<const float4*>(B0 + t);
+                w[to][1] = *reinterpret_cast<const float4*>(B0 + 8 * CP + t);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) k[to][e] = A(t + e, x);
+            };
+            auto add = [&](int of) {
+                const float a0[4] = {w[of][0].x, w[of][0].y, w[of][0].z, w[of][0].w}, a1[4] = {w[of][1].x, w[of][1].y, w[of][1].z, w[of][1].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 lo = make_float2(k[of][e].x, k[of][e].y), up = make_float2(k[of][e].z, k[of][e].w);
+                    const float2 d0 = make_float2(a0[e], a0[e]), d1 = make_float2(a1[e], a1[e]);
+                    s0[0] = fma2(d0, lo, s0[0]); s0[1] = fma2(d0, up, s0[1]);
+                    s1[0] = fma2(d1, lo, s1[0]); s1[1] = fma2(d1, up, s1[1]);
+                }
+            };
+            load(0, 0);
+#pragma unroll 1
+            for (int t = 0; t < C; t += 8) {
+                load(1, t + 4);
+                add(0);
+                load(0, t + 8 < C ? t + 8 : t);
+                add(1);
+            }
+        };
+        auto put = [&](float* to, const float2 (&v)[2]) { *reinterpret_cast<float4*>(to) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y); };
+        for (int p = first; p < a.dk * 2; p += step) {         // dk / 4 quads x 8 column pairs
             const int x = (p >> 3) * 4, c = p & 7;
-            float2 s0[2], s1[2];
-            {
-                const float4 f0 = *reinterpret_cast<const float4*>(S + c * L.ld + x), f1 = *reinterpret_cast<const float4*>(S + (c + 8) * L.ld + x);
+            float* const at0 = S + c * L.ld + x;
+            float* const at1 = S + (c + 8) * L.ld + x;
+            float2 s0[2] = {}, s1[2] = {};
+            if (MODE == 2 && hi) {
+                share(p, Boxed{st + L.Q, 0}, Y + c * CP, s0, s1);
+                put(X + c * L.ld + x, s0);
+                put(X + (c + 8) * L.ld + x, s1);
+            } else {
+                const float4 f0 = *reinterpret_cast<const float4*>(at0), f1 = *reinterpret_cast<const float4*>(at1);
                 s0[0] = make_float2(gl * f0.x, gl * f0.y); s0[1] = make_float2(gl * f0.z, gl * f0.w);
                 s1[0] = make_float2(gl * f1.x, gl * f1.y); s1[1] = make_float2(gl * f1.z, gl * f1.w);
+                share(p, Boxed{K, 0}, W + c * CP, s0, s1);
+                put(at0, s0);
+                put(at1, s1);
             }
-#pragma unroll
-            for (int pass = 0; pass < (MODE == 2 ? 2 : 1); ++pass) {
-                const Boxed A{pass ? st + L.Q : K, 0};
-                const float* const B0 = (pass ? Y : W) + c * CP;
-                float4 w[2][2], k[2][4];
-                auto load = [&](int to, int t) {
-                    w[to][0] = *reinterpret_cast<const float4*>(B0 + t);
-                    w[to][1] = *reinterpret_cast<const float4*>(B0 + 8 * CP + t);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) k[to][e] = A(t + e, x);
-                };
-                auto add = [&](int of) {
-                    const float a0[4] = {w[of][0].x, w[of][0].y, w[of][0].z, w[of][0].w}, a1[4] = {w[of][1].x, w[of][1].y, w[of][1].z, w[of][1].w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 lo = make_float2(k[of][e].x, k[of][e].y), up = make_float2(k[of][e].z, k[of][e].w);
-                        const float2 d0 = make_float2(a0[e], a0[e]), d1 = make_float2(a1[e], a1[e]);
-                        s0[0] = fma2(d0, lo, s0[0]); s0[1] = fma2(d0, up, s0[1]);
-                        s1[0] = fma2(d1, lo, s1[0]); s1[1] = fma2(d1, up, s1[1]);
-                    }
-                };
-                load(0, 0);
-#pragma unroll 1
-                for (int t = 0; t < C; t += 8) {
-                    load(1, t + 4);
-                    add(0);
-                    load(0, t + 8 < C ? t + 8 : t);
-                    add(1);
-                }
+        }
+        if (MODE == 2) {
+            bar_walk();
+            for (int i = tid; i < a.dk * (CW / 4); i += NT) {
+                const int at = i / (a.dk / 4) * L.ld + i % (a.dk / 4) * 4;
+                float4 f = *reinterpret_cast<const float4*>(S + at);
+                const float4 x = *reinterpret_cast<const float4*>(X + at);
+                f.x += x.x; f.y += x.y; f.z += x.z; f.w += x.w;
+                *reinterpret_cast<float4*>(S + at) = f;
             }
-            *reinterpret_cast<float4*>(S + c * L.ld + x) = make_float4(s0[0].x, s0[0].y, s0[1].x, s0[1].y);
-            *reinterpret_cast<float4*>(S + (c + 8) * L.ld + x) = make_float4(s1[0].x, s1[0].y, s1[1].x, s1[1].y);
         }
         fence_async();                                     // this chunk's reads before its place is filled again
         mbar_arrive(smem_u32(&empty[it & 1]));
@@ -487,8 +509,8 @@ cudaError_t walk(const GdnRecur& r, const float* fact, cudaStream_t stream) {
 
 size_t gdn_walk_bytes(int64_t chunks) { return static_cast<size_t>(chunks) * FACT * 4; }
 
-// Up to two CTAs an SM.  Forward, T = 512, d_k = d_v = 128: 126 us here against 191 of the token recurrence at 256 CTAs,
-// 246 against 195 at 512; with 64 x 64: 97 against 141 at 256, 187 against 148 at 576.
+// Up to two CTAs an SM.  Forward, T = 512, d_k = d_v = 128: 122 us here against 191 of the token recurrence at 256 CTAs,
+// 246 against 195 at 512; with 64 x 64: 88 against 141 at 256, 187 against 148 at 576.
 bool gdn_walk_supported(int dtype, int B, int H, int T, int dv) {
     return dtype == SDM_F32 && T >= C && static_cast<int64_t>(B) * H * ((dv + CW - 1) / CW) <= 152 * 2;
 }
@@ -499,7 +521,7 @@ cudaError_t launch_gdn_walk(int mode, const GdnRecur& r, float* fact, cudaStream
     static std::atomic<unsigned long long> seen;
     cudaError_t e = allow_smem(k_gdn_factors32, static_cast<size_t>(64 * 260 + C * CP + 2 * C) * 4, seen);
     if (e != cudaSuccess) return e;
-    k_gdn_factors32<<<dim3((a.T + C - 1) / C, a.H, a.B), NT, smem, stream>>>(a, fact, mode == 2);
+    k_gdn_factors32<<<dim3((a.T + C - 1) / C, a.H, a.B), FT, smem, stream>>>(a, fact, mode == 2);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     return mode == 0 ? walk<0>(r, fact, stream) : mode == 1 ? walk<1>(r, fact, stream) : walk<2>(r, fact, stream);
