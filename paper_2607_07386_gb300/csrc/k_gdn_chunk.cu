@@ -28,16 +28,20 @@ using namespace gdn;
 // Factors of a chunk: one CTA of 128 threads.  One MMA chain gives [K; Q] K^T (128 x 64); thread r
 // takes row r of it (k_i.k_j for r < 64, q_i.k_j above) and multiplies it by G along the row.
 //
-// N is solved for in fp32 by blocks of 16: the diagonal blocks by a column per thread in registers, then
-// the block diagonals below in order, with Z_ii = (I + B_ii beta)^-1 = I + N_ii beta:
-//   N_ij = -Z_ii sum_{j <= k < i} B_ik Y_kj,  Y = I + beta N,  a warp per 16 x 16 product, a lane per
-// 4 x 2 outputs (one 16-byte and one 8-byte shared-memory read per 8 multiply-adds; B and Z_ii lie
-// transposed for that).  Shared-memory reads bound the kernel (64% of the pipe; 80% with 4 x 1 outputs per thread): 119 us
-// at B = 8, H = 16, T = 4096, d_k = 128, where q, k, N and P alone take 69.  Eliminating whole columns of 64 in registers was slower still: 2016 unrolled
-// instructions, whose fetching took 11,600 of a CTA's 20,000 cycles.
+// N is solved for by blocks of 16: the diagonal blocks in fp32 by a column per thread in registers, then the
+// block diagonals below in order, with Z_ii = (I + B_ii beta)^-1 = I + N_ii beta:
+//   N_ij = -Z_ii sum_{j <= k < i} B_ik Y_kj,  Y = I + beta N,  a warp per block, transposed so that the sum is an
+// operand of the product with Z as it lies in registers.  These 16 x 16 products are too small for tcgen05 (at least 64
+// rows, and a trip through shared memory or TMEM between any two of a chain); they are mma.sync on tf32, each operand as two
+// parts of 11 bits, lower times lower left out: 21 bits, where N is kept at 16.  P and N leave through swizzled boxes and TMA.
+// At B = 8, H = 16, T = 4096, d_k = 128: 88 us (119 with the products in fp32 from shared memory and 16-byte stores by the
+// threads), where q, k, N and P alone take 49 at the copy rate.  Five CTAs an SM issue half of the time and wait for
+// one another's chains the rest; the parts cut off with a mask in place of a conversion gave 10 us, loops kept short for
+// the instruction cache 5.  Halves of 32 in place of block diagonals (a shorter chain, more products) took 6 us more;
+// eliminating whole columns of 64 in registers 2016 unrolled instructions, whose fetching took 11,600 of a CTA's 20,000 cycles.
 // ------------------------------------------------------------------------------------------
 constexpr int FT = 128;
-constexpr int LP = C + 4;
+constexpr int LP = C + 8;                     // a row; 8 mod 32: the fragments' reads (four rows, eight columns) meet no bank twice
 constexpr int BL = 16, NB = C / BL;
 struct FactorSmem {
     uint4 al[C / 8];                          // alpha, bf16
@@ -46,47 +50,48 @@ struct FactorSmem {
     uint32_t tmem;
     int dead;
 };
-// The K and Q tiles make room for these once the MMAs have read them.
+// The K and Q tiles make room for these once the MMAs have read them, P's boxes for N and Z, and Bt for N's boxes.
 struct FactorLate {
-    float Bt[C][C];                           // B transposed
-    float Y[C][LP];                           // on and below the diagonal; four of the blocks above hold N_ii
-    float Zt[C][BL];                          // Z_ii transposed: [16 block + column][row]
-    float X[NB][BL][BL + 4];
+    float Bt[C][LP];                          // B transposed
+    float N[C][LP];                           // on and below the diagonal blocks
+    float Zt[C][BL + 4];                      // Z_ii transposed: [16 block + column][row]
 };
+constexpr uint32_t P_BOX = sizeof(FactorLate::Bt), FACTOR_LATE = P_BOX + 3 * MAT;
+static_assert(P_BOX % 1024 == 0 && 2 * MAT <= P_BOX && sizeof(FactorLate) <= FACTOR_LATE, "boxes");
 template <int DK>
 struct FactorSize {
-    static constexpr size_t TILE = 128 * 2 * DK > sizeof(FactorLate) ? 128 * 2 * DK : (sizeof(FactorLate) + 15) / 16 * 16;
+    static constexpr size_t TILE = 128 * 2 * DK > FACTOR_LATE ? 128 * 2 * DK : FACTOR_LATE;
     static constexpr size_t BYTES = 1024 + TILE + sizeof(FactorSmem);
 };
 
-// acc[r][c] = sum_k At[k][4 (lane / 8) + r] B[k][2 (lane % 8) + c] over 16 k, B the sum of `terms` blocks.
-__device__ __forceinline__ void block_mul(const float* At, int lda, const float* B, int ldb, int terms, int term, float (&acc)[4][2], int lane) {
-    const float* ap = At + 4 * (lane >> 3);
-    const float* bp = B + 2 * (lane & 7);
+__device__ __forceinline__ uint32_t tf32(float x) { return __float_as_uint(x) & 0xffffe000u; }   // rounded towards zero
+// Upper and lower tf32 parts (21 significant bits together) of a fragment.
+template <int M>
+struct Parts {
+    uint32_t hi[M], lo[M];
+    __device__ __forceinline__ explicit Parts(const float (&v)[M]) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) acc[r][0] = acc[r][1] = 0.f;
-#pragma unroll 4
-    for (int k = 0; k < BL; ++k) {
-        const float4 a = *reinterpret_cast<const float4*>(ap + k * lda);
-        float2 b = *reinterpret_cast<const float2*>(bp + k * ldb);
-        for (int t = 1; t < terms; ++t) {
-            const float2 o = *reinterpret_cast<const float2*>(bp + t * term + k * ldb);
-            b.x += o.x;
-            b.y += o.y;
+        for (int i = 0; i < M; ++i) {
+            hi[i] = tf32(v[i]);
+            lo[i] = tf32(v[i] - __uint_as_float(hi[i]));
         }
-        acc[0][0] = fmaf(a.x, b.x, acc[0][0]); acc[0][1] = fmaf(a.x, b.y, acc[0][1]);
-        acc[1][0] = fmaf(a.y, b.x, acc[1][0]); acc[1][1] = fmaf(a.y, b.y, acc[1][1]);
-        acc[2][0] = fmaf(a.z, b.x, acc[2][0]); acc[2][1] = fmaf(a.z, b.y, acc[2][1]);
-        acc[3][0] = fmaf(a.w, b.x, acc[3][0]); acc[3][1] = fmaf(a.w, b.y, acc[3][1]);
     }
+};
+__device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
-// Where the diagonal block b of N is kept: (0, b), or (1, 2) for the first.
-__device__ __forceinline__ int diag_row(int b) { return b == 0 ? BL : 0; }
-__device__ __forceinline__ int diag_col(int b) { return b == 0 ? 2 * BL : b * BL; }
+// big + small += A B, 16 x 8 x 8, all but the product of the lower parts.
+__device__ __forceinline__ void mma_parts(float (&big)[4], float (&small)[4], const Parts<4>& a, const Parts<2>& b) {
+    mma_tf32(big, a.hi, b.hi);
+    mma_tf32(small, a.lo, b.hi);
+    mma_tf32(small, a.hi, b.lo);
+}
 
 template <int DK>
 __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tq,
-                                                    const GdnArgs a, const GdnFactors f) {
+                                                       const __grid_constant__ CUtensorMap tm, const GdnArgs a, const GdnFactors f) {
     extern __shared__ unsigned char raw[];
     const uint32_t base = smem_u32(raw);
     const uint32_t tile = (base + 1023u) & ~1023u;        // per 64 values of d_k: 64 rows of K, 64 of Q
@@ -174,17 +179,14 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
     __syncwarp();
     tc_after_sync();
     float G = 0.f;
-    uint4* const P = reinterpret_cast<uint4*>(static_cast<char*>(f.mat) + (cid * f.mats + 2) * MAT + i * C * 2);
-#pragma unroll
+    unsigned char* const P = raw + (tile - base) + P_BOX;
+#pragma unroll 1
     for (int half = 1; half >= 0; --half) {               // columns 32.. , then 0..; rows 0-31 have none of the first
         if (half == 1 && (warp & 1) == 0) {
             if (!isk) {
 #pragma unroll
-                for (int j = 4; j < 8; ++j) {
-                    P[j] = make_uint4(0, 0, 0, 0);
-                    if (f.mats > 3) P[MAT / 16 + j] = make_uint4(0, 0, 0, 0);
-                    if (f.mats > 4) P[2 * MAT / 16 + j] = make_uint4(0, 0, 0, 0);
-                }
+                for (int j = 4; j < 8; ++j)
+                    for (int p = 0; p < f.mats - 2; ++p) *reinterpret_cast<uint4*>(P + p * MAT + box_at(i, j)) = make_uint4(0, 0, 0, 0);
             }
             continue;
         }
@@ -214,18 +216,30 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
                 for (int e = 0; e < 8; ++e) v[e] = 32 * half + 8 * j + e <= i ? x[8 * j + e] : 0.f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) w[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
-                P[4 * half + j] = make_uint4(w[0], w[1], w[2], w[3]);
+                unsigned char* const at = P + box_at(i, 4 * half + j);
+                *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
                 if (f.mats > 3) {                                             // its lower parts
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
-                    P[MAT / 16 + 4 * half + j] = make_uint4(w[0], w[1], w[2], w[3]);
-                    if (f.mats > 4) P[2 * MAT / 16 + 4 * half + j] = pack16<BF16>(v);
+                    *reinterpret_cast<uint4*>(at + MAT) = make_uint4(w[0], w[1], w[2], w[3]);
+                    if (f.mats > 4) *reinterpret_cast<uint4*>(at + 2 * MAT) = pack16<BF16>(v);
                 }
             }
         }
     }
+    if (!isk) fence_async();
     __syncthreads();
-    if (isk) {                                                                // diagonal block tid / 16, column tid % 16
+    const int row0 = static_cast<int>(cid * f.mats * C);
+    if (warp == 2) {                                      // P leaves
+        if (elect_one()) {
+            for (int p = 0; p < f.mats - 2; ++p) tma_store_2d(&tm, tile + P_BOX + p * MAT, 0, row0 + (2 + p) * C);
+            bulk_commit();
+            bulk_wait_read();
+        }
+        __syncwarp();
+        asm volatile("bar.sync 1, 96;\n" ::: "memory");
+    }
+    if (isk) {                                            // diagonal block tid / 16, column tid % 16
         const int o = tid & ~15, c = tid & 15;
         float z[BL];
 #pragma unroll
@@ -243,67 +257,103 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
             }
         }
         const float be = sm.be[tid];
-        const int dr = diag_row(o / BL), dc = diag_col(o / BL);
+        asm volatile("bar.sync 1, 96;\n" ::: "memory");   // P has left the place
 #pragma unroll
-        for (int j = 0; j < BL; ++j) {
-            lt.Y[dr + j][dc + c] = z[j];
-            lt.Y[o + j][o + c] = j == c ? 1.f : sm.be[o + j] * z[j];
-        }
+        for (int j = 0; j < BL; ++j) lt.N[o + j][o + c] = z[j];
 #pragma unroll
         for (int j = 0; j < BL; j += 4)
             *reinterpret_cast<float4*>(&lt.Zt[tid][j]) = make_float4(j == c ? 1.f : be * z[j], j + 1 == c ? 1.f : be * z[j + 1],
                                                                      j + 2 == c ? 1.f : be * z[j + 2], j + 3 == c ? 1.f : be * z[j + 3]);
     }
     __syncthreads();
-    char* const mat = static_cast<char*>(f.mat) + cid * f.mats * MAT;
-    {   // N's diagonal blocks as upper and lower parts, half a row a thread, and zeros to the right of them
-        const int r = tid >> 1, bl = r / BL, c0 = (tid & 1) * 8;
-        float v[8];
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c0 + e < r % BL ? lt.Y[diag_row(bl) + r % BL][diag_col(bl) + c0 + e] : 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            hi[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
-            lo[e] = pack2(v[2 * e], v[2 * e + 1]);
+    // fragments of 16 x 8 x 8 products, transposed: a lane has column g of N's block (rows t of B, Z, N in turn)
+    const int lane = tid & 31, g = lane >> 2, t = lane & 3;
+    auto y_part = [&](int k, int c, bool diagonal) {       // Y^T: columns c + g, c + g + 8, rows k + t, k + t + 4 (c: of the diagonal block)
+        const float b0 = sm.be[k + t], b1 = sm.be[k + t + 4];
+        float v[4] = {b0 * lt.N[k + t][c + g], b0 * lt.N[k + t][c + g + 8], b1 * lt.N[k + t + 4][c + g], b1 * lt.N[k + t + 4][c + g + 8]};
+        if (diagonal) {
+            v[0] = k + t == c + g ? 1.f : v[0]; v[1] = k + t == c + g + 8 ? 1.f : v[1];
+            v[2] = k + t + 4 == c + g ? 1.f : v[2]; v[3] = k + t + 4 == c + g + 8 ? 1.f : v[3];
         }
-        char* const at = mat + (r * C + bl * BL + c0) * 2;
-        *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4*>(at + MAT) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-        for (int k = bl + 1; k < NB; ++k) {
-            *reinterpret_cast<uint4*>(at + (k - bl) * BL * 2) = make_uint4(0, 0, 0, 0);
-            *reinterpret_cast<uint4*>(at + MAT + (k - bl) * BL * 2) = make_uint4(0, 0, 0, 0);
+        return Parts<4>(v);
+    };
+    auto b_part = [&](int k, int i) {                      // B^T: rows k + t, k + t + 4, column i + g
+        const float v[2] = {lt.Bt[k + t][i + g], lt.Bt[k + t + 4][i + g]};
+        return Parts<2>(v);
+    };
+    // An accumulator's columns 2 t, 2 t + 1 take the places of the operand's t, t + 4; the other operand's rows do the same.
+    auto x_part = [&](const float (&x)[4], const float (&xs)[4]) {
+        const float v[4] = {x[0] + xs[0], x[2] + xs[2], x[1] + xs[1], x[3] + xs[3]};
+        return Parts<4>(v);
+    };
+    auto z_part = [&](int i, int o) {                      // Z_ii^T: rows i + 2 t, i + 2 t + 1, column o + g of the block
+        const float v[2] = {lt.Zt[i + 2 * t][o + g], lt.Zt[i + 2 * t + 1][o + g]};
+        return Parts<2>(v);
+    };
+    auto put = [&](int i, int c, const float (&r)[2][4], const float (&rs)[2][4]) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int row = i + 8 * q + 2 * t;
+            lt.N[row][c + g] = -(r[q][0] + rs[q][0]); lt.N[row + 1][c + g] = -(r[q][1] + rs[q][1]);
+            lt.N[row][c + g + 8] = -(r[q][2] + rs[q][2]); lt.N[row + 1][c + g + 8] = -(r[q][3] + rs[q][3]);
         }
-    }
-    const int lane = tid & 31, br = 4 * (lane >> 3), bc = 2 * (lane & 7);
+    };
+#pragma unroll 1
+    for (int d = 1; d < NB; ++d) {                         // blocks (j + d, j)
+        if (warp < NB - d) {
+            const int j = warp * BL, i = j + d * BL;
+            float x[2][4] = {}, xs[2][4] = {}, r[2][4] = {}, rs[2][4] = {};
 #pragma unroll
-    for (int d = 1; d < NB; ++d) {                                            // blocks (j + d, j)
-        if (warp < (NB - d) * d) {                                            // warp: block j = warp / d, its term k = j + warp % d
-            const int j = warp / d, k = j + warp % d;
-            float acc[4][2];
-            block_mul(&lt.Bt[k * BL][(j + d) * BL], C, &lt.Y[k * BL][j * BL], LP, 1, 0, acc, lane);
+            for (int k8 = 0; k8 < BL; k8 += 8) {
+                const Parts<4> A = y_part(j + k8, j, true);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) *reinterpret_cast<float2*>(&lt.X[warp][br + r][bc]) = make_float2(acc[r][0], acc[r][1]);
+                for (int m = 0; m < 2; ++m) mma_parts(x[m], xs[m], A, b_part(j + k8, i + 8 * m));
+            }
+#pragma unroll 1
+            for (int k = j + BL; k < i; k += BL) {
+#pragma unroll
+                for (int k8 = 0; k8 < BL; k8 += 8) {
+                    const Parts<4> A = y_part(k + k8, j, false);
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) mma_parts(x[m], xs[m], A, b_part(k + k8, i + 8 * m));
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const Parts<4> A = x_part(x[m], xs[m]);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) mma_parts(r[q], rs[q], A, z_part(i + 8 * m, 8 * q));
+            }
+            put(i, j, r, rs);
         }
         __syncthreads();
-        if (warp < NB - d) {
-            float acc[4][2];
-            block_mul(&lt.Zt[(warp + d) * BL][0], BL, &lt.X[warp * d][0][0], BL + 4, d, BL * (BL + 4), acc, lane);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = (warp + d) * BL + br + r, col = warp * BL + bc;
-                float x = -acc[r][0], y = -acc[r][1];
-                *reinterpret_cast<float2*>(&lt.Y[row][col]) = make_float2(sm.be[row] * x, sm.be[row] * y);
-                const uint32_t hi = split2(x, y, x, y);
-                *reinterpret_cast<uint32_t*>(mat + (row * C + col) * 2) = hi;
-                *reinterpret_cast<uint32_t*>(mat + MAT + (row * C + col) * 2) = pack2(x, y);
-            }
-        }
-        if (d + 1 < NB) __syncthreads();
     }
+    {   // N as upper and lower parts, into boxes where Bt was: 16 rows a warp, four values a lane at a time
+        const int row = warp * BL + (lane >> 1);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int x = 8 * q + 4 * (lane & 1);
+            uint2 hi = make_uint2(0, 0), lo = hi;
+            if (q / 2 <= warp) {                          // zeros from the diagonal on
+                const float4 f4 = *reinterpret_cast<const float4*>(&lt.N[row][x]);
+                float v[4] = {x < row ? f4.x : 0.f, x + 1 < row ? f4.y : 0.f, x + 2 < row ? f4.z : 0.f, x + 3 < row ? f4.w : 0.f};
+                hi.x = split2(v[0], v[1], v[0], v[1]); lo.x = pack2(v[0], v[1]);
+                hi.y = split2(v[2], v[3], v[2], v[3]); lo.y = pack2(v[2], v[3]);
+            }
+            unsigned char* const at = raw + (tile - base) + box_at(row, q) + 8 * (lane & 1);
+            *reinterpret_cast<uint2*>(at) = hi;
+            *reinterpret_cast<uint2*>(at + MAT) = lo;
+        }
+    }
+    fence_async();
     if (tid == 0 && sm.dead) flag_error(a.err, ERR_TIMEOUT);
     tc_before_sync();
     __syncthreads();
+    if (tid == 0) {
+        for (int p = 0; p < 2; ++p) tma_store_2d(&tm, tile + p * MAT, 0, row0 + p * C);
+        bulk_commit();
+        bulk_wait_read();
+    }
     if (warp == 1) tmem_free(tmem, 64);
 }
 
@@ -700,12 +750,12 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
 }
 
 template <int DK>
-cudaError_t factors(const CUtensorMap& tk, const CUtensorMap& tq, const GdnArgs& a, const GdnFactors& f, cudaStream_t stream) {
+cudaError_t factors(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap& tm, const GdnArgs& a, const GdnFactors& f, cudaStream_t stream) {
     constexpr size_t smem = FactorSize<DK>::BYTES;
     static std::atomic<unsigned long long> seen;
     cudaError_t e = allow_smem(k_gdn_factors<DK>, smem, seen);
     if (e != cudaSuccess) return e;
-    k_gdn_factors<DK><<<dim3((a.T + C - 1) / C, a.H, a.B), FT, smem, stream>>>(tk, tq, a, f);
+    k_gdn_factors<DK><<<dim3((a.T + C - 1) / C, a.H, a.B), FT, smem, stream>>>(tk, tq, tm, a, f);
     return cudaGetLastError();
 }
 
@@ -737,10 +787,12 @@ size_t gdn_factor_gate_bytes(int64_t chunks) { return static_cast<size_t>(chunks
 bool gdn_chunk_supported(int dtype, int dk, int T) { return dtype == SDM_BF16 && dk <= 128 && T >= 32; }
 
 cudaError_t launch_gdn_factors(const GdnArgs& a, const GdnFactors& f, cudaStream_t stream) {
-    CUtensorMap tk, tq;
-    if (!token_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk) || !token_map(&tq, a.q, a.token_major, a.B, a.Hk, a.T, a.dk))
+    const int64_t chunks = static_cast<int64_t>(a.B) * a.H * ((a.T + C - 1) / C);
+    CUtensorMap tk, tq, tm;
+    if (!token_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk) || !token_map(&tq, a.q, a.token_major, a.B, a.Hk, a.T, a.dk) ||
+        !row_map(&tm, f.mat, chunks * f.mats * C, C, C))
         return cudaErrorInvalidValue;
-    return a.dk <= 64 ? factors<64>(tk, tq, a, f, stream) : factors<128>(tk, tq, a, f, stream);
+    return a.dk <= 64 ? factors<64>(tk, tq, tm, a, f, stream) : factors<128>(tk, tq, tm, a, f, stream);
 }
 
 cudaError_t launch_gdn_scan(const GdnScan& s, const GdnFactors& f, cudaStream_t stream) {
