@@ -11,9 +11,8 @@
 // tensor pipe under the power limit: 32768 x 2048 x 2048 with silu, bias and residual takes 178 us alone (1.55
 // PFLOP/s) and 207 us in a row of calls; dx and dW of it 165 and 176 us alone.
 //
-// Two CTAs of a cluster take tiles one above the other and share the columns' operand: each loads half of it
-// for both (TMA multicast), so a K-block costs 256 rows of loads in place of 384.  A stage is free once the MMAs of
-// both have read it.
+// Every CTA loads both operands of its tiles itself: operands may lie in another GPU's memory (every rank of a run on
+// several GPUs loads this library), so no load is shared between CTAs.
 //
 // Few tiles (a narrow layer over many rows, a batch of tokens being decoded) leave SMs idle, so the
 // contraction is split and the fp32 shares are joined, in a fixed order, by k_linear_join, which
@@ -135,8 +134,7 @@ struct LinearGeom {
     int ntm, ntn, splits, kbs;  // tiles, splits, K-blocks per split
 };
 
-// CL: CTAs of a cluster, 1 or 2.
-template <int BN, bool AMN, bool BMN, int CL>
+template <int BN, bool AMN, bool BMN>
 __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
                                                   const LinearGeom g, const LinearOut o, float* part, int* err) {
     constexpr int S = stages_of(BN);
@@ -157,7 +155,7 @@ __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtens
     if (tid == 0) {
         for (int s = 0; s < S; ++s) {
             mbar_init(full + 8 * s, 1);
-            mbar_init(empty + 8 * s, CL);
+            mbar_init(empty + 8 * s, 1);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(afull + 8 * s, 1);
@@ -170,16 +168,14 @@ __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtens
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
     const uint32_t tmem = *slot;
-    const int rank = CL == 2 ? static_cast<int>(cluster_rank()) : 0;
-    const int items = (g.ntm + CL - 1) / CL * g.ntn * g.splits, first = blockIdx.x / CL, step = gridDim.x / CL;
-    if (CL == 2) cluster_sync();                       // the other CTA's barriers are there
+    const int items = g.ntm * g.ntn * g.splits;
     bool ok = true;
 
     if (tid == 0) {                                    // loads
         uint32_t it = 0;
-        for (int w = first; w < items && ok; w += step) {
+        for (int w = blockIdx.x; w < items && ok; w += gridDim.x) {
             const int sp = w % g.splits, tile = w / g.splits;
-            const int m0 = (tile / g.ntn * CL + rank) * BM, n0 = (tile % g.ntn) * BN;
+            const int m0 = (tile / g.ntn) * BM, n0 = (tile % g.ntn) * BN;
             const int k0 = sp * g.kbs, k1 = k0 + g.kbs < g.nkb ? k0 + g.kbs : g.nkb;
             for (int kb = k0; kb < k1; ++kb, ++it) {
                 const int s = it % S;
@@ -192,16 +188,7 @@ __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtens
                 } else {
                     tma_load_2d(a, &ta, kb * BK, m0, bar);
                 }
-                if (CL == 2) {                         // this CTA's half, for both
-                    constexpr int HB = BN / CL;
-                    const uint32_t to = b + rank * HB * 128;
-                    if (BMN) {
-#pragma unroll
-                        for (int j = 0; j < HB / 64; ++j) tma_load_2d_mc(to + j * 8192, &tb, n0 + rank * HB + 64 * j, kb * BK, bar, 3);
-                    } else {
-                        tma_load_2d_mc(to, &tb, kb * BK, n0 + rank * HB, bar, 3);
-                    }
-                } else if (BMN) {
+                if (BMN) {
 #pragma unroll
                     for (int j = 0; j < BN / 64; ++j) tma_load_2d(b + j * 8192, &tb, n0 + 64 * j, kb * BK, bar);
                 } else {
@@ -214,7 +201,7 @@ __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtens
     } else if (tid == 32) {                            // MMAs
         const uint32_t idesc = mma_idesc(BN) | (AMN ? MN_A : 0u) | (BMN ? MN_B : 0u);
         uint32_t it = 0, n = 0;
-        for (int w = first; w < items && ok; w += step, ++n) {
+        for (int w = blockIdx.x; w < items && ok; w += gridDim.x, ++n) {
             const int sp = w % g.splits;
             const int k0 = sp * g.kbs, k1 = k0 + g.kbs < g.nkb ? k0 + g.kbs : g.nkb;
             const uint32_t acc = tmem + (n & 1) * BN;
@@ -229,18 +216,17 @@ __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtens
                 for (int kk = 0; kk < BK / 16; ++kk)
                     mma_bf16(acc, AMN ? sw128_mn_desc(a + kk * 2048, 8192) : sw128_desc(a + kk * 32),
                              BMN ? sw128_mn_desc(b + kk * 2048, 8192) : sw128_desc(b + kk * 32), idesc, (kb != k0 || kk != 0) ? 1u : 0u);
-                if (CL == 2) mma_commit_mc(empty + 8 * s, 3);
-                else mma_commit(empty + 8 * s);
+                mma_commit(empty + 8 * s);
             }
             if (ok) mma_commit(afull + 8 * (n & 1));
         }
     } else if (warp >= 2) {                            // epilogue: TMEM lanes of this warp's quadrant
         const int quad = warp & 3, part_of = (warp - 2) >> 2, lane = tid & 31;
         uint32_t n = 0;
-        for (int w = first; w < items && ok; w += step, ++n) {
+        for (int w = blockIdx.x; w < items && ok; w += gridDim.x, ++n) {
             const int sp = w % g.splits, tile = w / g.splits;
             const int n0 = (tile % g.ntn) * BN;
-            const int64_t row = static_cast<int64_t>(tile / g.ntn * CL + rank) * BM + quad * 32 + lane;
+            const int64_t row = static_cast<int64_t>(tile / g.ntn) * BM + quad * 32 + lane;
             constexpr int BLOCKS = BN / 64;                // blocks of 32 columns of this warp
             const int c0 = part_of * (BN / 2);
             const uint32_t src = tmem + (n & 1) * BN + c0 + (static_cast<uint32_t>(quad * 32) << 16);
@@ -306,7 +292,6 @@ __global__ void __launch_bounds__(LT, 1) k_linear(const __grid_constant__ CUtens
     asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
     __syncthreads();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(COLS) : "memory");
-    if (CL == 2) cluster_sync();                       // nothing arrives at a CTA that has ended
 }
 
 // Sum of the splits' shares, in order, and the epilogue; eight columns per thread.
@@ -471,46 +456,24 @@ __global__ void __launch_bounds__(256) k_linear_dbias(const float* __restrict__ 
     }
 }
 
-template <int BN, bool AMN, bool BMN, int CL>
+template <int BN, bool AMN, bool BMN>
 cudaError_t launch_tiles(const CUtensorMap& ta, const CUtensorMap& tb, const LinearGeom& g, const LinearOut& o, float* part,
                          int* err, cudaStream_t stream) {
     constexpr uint32_t smem = smem_bytes(BN);
     static std::atomic<unsigned long long> seen;
-    cudaError_t e = allow_smem(k_linear<BN, AMN, BMN, CL>, smem, seen);
+    cudaError_t e = allow_smem(k_linear<BN, AMN, BMN>, smem, seen);
     if (e != cudaSuccess) return e;
-    const int64_t items = static_cast<int64_t>((g.ntm + CL - 1) / CL) * g.ntn * g.splits;
-    cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = CL;
-    at.val.clusterDim.y = at.val.clusterDim.z = 1;
-    cfg.blockDim = dim3(LT);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cfg.attrs = &at;
-    cfg.numAttrs = CL > 1 ? 1 : 0;
-    int most = SMS / CL;                               // clusters that the SMs hold at once
-    if (CL > 1) {
-        static std::atomic<int> held{0};
-        most = held.load(std::memory_order_acquire);
-        if (most == 0) {
-            cfg.gridDim = dim3(SMS);
-            e = cudaOccupancyMaxActiveClusters(&most, k_linear<BN, AMN, BMN, CL>, &cfg);
-            if (e != cudaSuccess) return e;
-            if (most < 1) return cudaErrorInvalidConfiguration;
-            held.store(most, std::memory_order_release);
-        }
-    }
-    cfg.gridDim = dim3(static_cast<unsigned>(CL * (items < most ? items : most)));
-    return cudaLaunchKernelEx(&cfg, k_linear<BN, AMN, BMN, CL>, ta, tb, g, o, part, err);
+    const int64_t items = static_cast<int64_t>(g.ntm) * g.ntn * g.splits;
+    k_linear<BN, AMN, BMN><<<static_cast<unsigned>(items < SMS ? items : SMS), LT, smem, stream>>>(ta, tb, g, o, part, err);
+    return cudaGetLastError();
 }
 
-template <int BN, int CL>
+template <int BN>
 cudaError_t launch_majors(bool a_mn, bool b_mn, const CUtensorMap& ta, const CUtensorMap& tb, const LinearGeom& g,
                           const LinearOut& o, float* part, int* err, cudaStream_t stream) {
-    if (!a_mn && !b_mn) return launch_tiles<BN, false, false, CL>(ta, tb, g, o, part, err, stream);
-    if (!a_mn) return launch_tiles<BN, false, true, CL>(ta, tb, g, o, part, err, stream);
-    return launch_tiles<BN, true, true, CL>(ta, tb, g, o, part, err, stream);
+    if (!a_mn && !b_mn) return launch_tiles<BN, false, false>(ta, tb, g, o, part, err, stream);
+    if (!a_mn) return launch_tiles<BN, false, true>(ta, tb, g, o, part, err, stream);
+    return launch_tiles<BN, true, true>(ta, tb, g, o, part, err, stream);
 }
 
 }  // namespace
@@ -543,7 +506,7 @@ cudaError_t launch_linear(const void* A, bool a_mn, const void* B, bool b_mn, in
     const LinearPlan p = linear_plan(M, N, K);
     CUtensorMap ta, tb;
     if (!(a_mn ? make_map(&ta, A, K, M, BK) : make_map(&ta, A, M, K, BM)) ||
-        !(b_mn ? make_map(&tb, B, K, N, BK) : make_map(&tb, B, N, K, p.bn == 256 ? p.bn / 2 : p.bn)))
+        !(b_mn ? make_map(&tb, B, K, N, BK) : make_map(&tb, B, N, K, p.bn)))
         return cudaErrorInvalidValue;
     LinearGeom g{};
     g.M = M;
@@ -554,9 +517,9 @@ cudaError_t launch_linear(const void* A, bool a_mn, const void* B, bool b_mn, in
     g.splits = p.splits;
     g.kbs = (g.nkb + p.splits - 1) / p.splits;
     float* part = p.splits > 1 ? split_ws : nullptr;
-    cudaError_t e = p.bn == 256   ? launch_majors<256, 2>(a_mn, b_mn, ta, tb, g, o, part, err, stream)
-                    : p.bn == 128 ? launch_majors<128, 1>(a_mn, b_mn, ta, tb, g, o, part, err, stream)
-                                  : launch_majors<64, 1>(a_mn, b_mn, ta, tb, g, o, part, err, stream);
+    cudaError_t e = p.bn == 256   ? launch_majors<256>(a_mn, b_mn, ta, tb, g, o, part, err, stream)
+                    : p.bn == 128 ? launch_majors<128>(a_mn, b_mn, ta, tb, g, o, part, err, stream)
+                                  : launch_majors<64>(a_mn, b_mn, ta, tb, g, o, part, err, stream);
     if (e != cudaSuccess || part == nullptr) return e;
     const int64_t pieces = M * N / 8;
     k_linear_join<<<static_cast<unsigned>((pieces + 255) / 256), 256, 0, stream>>>(part, p.splits, M, g.N, o);

@@ -211,3 +211,25 @@ def test_infinities_stay_in_their_rows_and_columns(sdm):
     keep_c = torch.arange(136, device="cuda") != 11
     assert torch.equal(out[keep_r][:, keep_c], bad[keep_r][:, keep_c])
     assert torch.isnan(bad[:, 11]).all() and not torch.isfinite(bad[7]).any()
+
+
+# 128 x 256 tiles in every order of the operands, over more K-blocks than the ring holds, with an odd number of row
+# tiles: x W^T at exactly 76 tiles (and two splits), x W^T and dz W at 95 and 133, x W^T and dz^T x at 90 and 95.
+WIDE = [(2305, 1024, 520), (2305, 1032, 1544), (1100, 2312, 1032)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", WIDE)
+def test_wide_tiles(sdm, M, N, K):
+    test_forward_parity(sdm, M, N, K, "silu", True, True, True)
+    test_backward_parity(sdm, M, N, K, "gelu")
+
+
+def test_no_load_is_shared_between_ctas():
+    """Every rank of a run on several GPUs loads this library, and a caller's matrix may be in another GPU's memory:
+    no copy of a source goes to more than one CTA's shared memory."""
+    import re
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2607_07386_gb300", "csrc")
+    shared = re.compile("multi" + "cast", re.I)
+    names = sorted(n for n in os.listdir(csrc) if n.endswith((".cu", ".cuh", ".h")))
+    assert names and [n for n in names if shared.search(open(os.path.join(csrc, n)).read())] == []
