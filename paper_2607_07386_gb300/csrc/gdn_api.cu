@@ -35,9 +35,9 @@ struct Buf {
     bool written;
 };
 
-// Presence, alignment, and that nothing written overlaps anything else (`same`: a pair that may be
+// Presence, alignment, and that nothing written overlaps anything else (but b[in] and b[out], unless negative, may be
 // one buffer).
-sdm_status check_bufs(const char* who, const Buf* b, int n, const void* same = nullptr) {
+sdm_status check_bufs(const char* who, const Buf* b, int n, int in = -1, int out = -1) {
     for (int i = 0; i < n; ++i) {
         if (b[i].p == nullptr && !b[i].optional && b[i].bytes > 0) return fail(SDM_ERR_INVALID_ARG, "%s: %s is NULL", who, b[i].name);
         if (reinterpret_cast<uintptr_t>(b[i].p) % b[i].align != 0)
@@ -48,7 +48,7 @@ sdm_status check_bufs(const char* who, const Buf* b, int n, const void* same = n
         for (int j = 0; j < n; ++j) {
             if (j == i || b[j].p == nullptr || b[j].bytes == 0) continue;
             const uintptr_t x = reinterpret_cast<uintptr_t>(b[i].p), y = reinterpret_cast<uintptr_t>(b[j].p);
-            if (b[i].p == b[j].p && same != nullptr && same == b[j].p && !b[j].written && b[i].bytes == b[j].bytes) continue;
+            if (i == out && j == in && b[i].p == b[j].p && b[i].bytes == b[j].bytes) continue;
             if (x < y + b[j].bytes && y < x + b[i].bytes)
                 return fail(SDM_ERR_INVALID_ARG, "%s: %s overlaps %s", who, b[i].name, b[j].name);
         }
@@ -354,8 +354,8 @@ sdm_status sdm_linear(const sdm_linear_shape* s, const void* x, const void* W, c
                         {"bias", bias, static_cast<size_t>(s->N) * 4, 16, true, false},
                         {"residual", residual, mn, 16, true, false}, {"out", out, mn, 16, false, true},
                         {"pre", pre, mn, 16, true, true}, {"workspace", workspace, need, 16, true, true}};
-    // residual == out is allowed (each element is read by the thread that overwrites it); pre is not out
-    SDM_TRY(check_bufs("sdm_linear", bufs, 7, residual == out ? residual : nullptr));
+    // residual == out is allowed: each element is read by the thread that overwrites it
+    SDM_TRY(check_bufs("sdm_linear", bufs, 7, 3, 4));
     SDM_TRY(check_ws("sdm_linear", workspace, workspace_bytes, need));
     int* err = nullptr;
     SDM_TRY(sdm::api_status_word(&err));

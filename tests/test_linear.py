@@ -233,3 +233,13 @@ def test_no_load_is_shared_between_ctas():
     shared = re.compile("multi" + "cast", re.I)
     names = sorted(n for n in os.listdir(csrc) if n.endswith((".cu", ".cuh", ".h")))
     assert names and [n for n in names if shared.search(open(os.path.join(csrc, n)).read())] == []
+
+
+@pytest.mark.parametrize("M,N,K", [(64, 64, 64), (64, 72, 64), (4096, 2048, 2048), (64, 4096, 4096), (16, 64, 64), (16, 64, 16)])
+def test_only_the_residual_may_be_the_output(sdm, M, N, K):
+    """In place over x or W is refused, with the residual there too: tiles, split tiles and up to 16 rows."""
+    shape = sdm.LinearShape.make(M, N, K)
+    far = dict(x=1 << 40, W=1 << 41, workspace=1 << 42)
+    for other in [n for n, same in (("x", N == K), ("W", M == K)) if same]:
+        with pytest.raises(sdm.SdmError, match="out overlaps " + other):
+            _call(sdm, shape, **{**far, other: 3 * A, "residual": 3 * A})
