@@ -80,7 +80,7 @@ __device__ __forceinline__ float normal_cdf(float z, float& pdf) {
     return z >= 0.f ? 1.f - tail : tail;
 }
 __device__ __forceinline__ float act_fwd(float z, int act) {
-    if (act == SDM_ACT_RELU) return z > 0.f ? z : 0.f;
+    if (act == SDM_ACT_RELU) return z <= 0.f ? 0.f : z;             // NaN stays
     if (act == SDM_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));     // a few float32 ulps, rounded to bf16 below
     if (act == SDM_ACT_GELU) {
         float pdf;
@@ -89,7 +89,7 @@ __device__ __forceinline__ float act_fwd(float z, int act) {
     return z;
 }
 __device__ __forceinline__ float act_slope(float z, int act) {
-    if (act == SDM_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+    if (act == SDM_ACT_RELU) return z <= 0.f ? 0.f : z > 0.f ? 1.f : z;
     if (act == SDM_ACT_SILU) {
         const float p = __fdividef(1.f, 1.f + __expf(-z));
         return p * (1.f + z * (1.f - p));

@@ -243,3 +243,29 @@ def test_only_the_residual_may_be_the_output(sdm, M, N, K):
     for other in [n for n, same in (("x", N == K), ("W", M == K)) if same]:
         with pytest.raises(sdm.SdmError, match="out overlaps " + other):
             _call(sdm, shape, **{**far, other: 3 * A, "residual": 3 * A})
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [5, 200])
+@pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
+def test_nan_is_not_lost(sdm, act, M):
+    """A NaN in a row of x is in every output of the row; one pre-activation's is in its row of dx, its row of dW and its
+    dbias, and nowhere else."""
+    import torch
+    N, K = 72, 136
+    t = _inputs(M, N, K, 8)
+    t["x"][3, 9] = float("nan")
+    shape = sdm.LinearShape.make(M, N, K, act=act)
+    out, pre = (torch.empty((M, N), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    sdm.linear(shape, t["x"], t["W"], out, bias=t["bias"], pre=pre, workspace=_ws(sdm.linear_workspace_bytes(shape)))
+    row = torch.arange(M, device="cuda") == 3
+    assert torch.equal(torch.isnan(out), row[:, None].expand(M, N)) and torch.equal(torch.isnan(pre), torch.isnan(out))
+    if act == "none":
+        return
+    t["x"][3, 9] = 1.0
+    t["pre"][3, 11] = float("nan")
+    dx, dW, db = torch.empty_like(t["x"]), torch.empty_like(t["W"]), torch.empty((N,), device="cuda")
+    sdm.linear_backward(shape, t["x"], t["W"], t["pre"], t["dout"], dx, dW, db, _ws(sdm.linear_backward_workspace_bytes(shape)))
+    col = torch.arange(N, device="cuda") == 11
+    assert torch.equal(torch.isnan(dx), row[:, None].expand(M, K))
+    assert torch.equal(torch.isnan(dW), col[:, None].expand(N, K)) and torch.equal(torch.isnan(db), col)
