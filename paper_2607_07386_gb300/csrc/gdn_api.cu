@@ -131,7 +131,7 @@ FwdLayout fwd_layout(const sdm_gdn_shape* s) {
         return L;
     }
     const int64_t chunks = static_cast<int64_t>(s->B) * s->H * ((s->T + sdm::GDN_C64 - 1) / sdm::GDN_C64);
-    L.gates = align256(sdm::gdn_factor_mat_bytes(chunks, 3));
+    L.gates = align256(sdm::gdn_factor_mat_bytes(chunks, sdm::GDN_SCAN_MATS));
     L.total = L.gates + align256(sdm::gdn_factor_gate_bytes(chunks));
     return L;
 }
@@ -232,7 +232,7 @@ sdm_status sdm_gdn_forward(const sdm_gdn_shape* s, const void* q, const void* k,
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     if (L.tc) {
         char* ws = static_cast<char*>(workspace);
-        const sdm::GdnFactors f{ws + L.mat, 3, reinterpret_cast<float*>(ws + L.gates)};
+        const sdm::GdnFactors f{ws + L.mat, sdm::GDN_SCAN_MATS, reinterpret_cast<float*>(ws + L.gates)};
         cudaError_t e = sdm::launch_gdn_factors(a, f, st);
         if (e == cudaSuccess) e = sdm::launch_gdn_scan(sdm::GdnScan{a, state, y, nullptr, nullptr, nullptr}, f, st);
         return done(e, "sdm_gdn_forward");

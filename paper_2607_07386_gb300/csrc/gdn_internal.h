@@ -90,11 +90,12 @@ struct GdnGrads {
 cudaError_t launch_gdn_grads(int dtype, const GdnGrads& g, cudaStream_t stream);
 
 // ---- chunked form on the tensor cores (k_gdn_chunk.cu): bf16, d_k <= 128, chunks of 64 ----
-// What the chunks' own products are, per (sequence, head, chunk): three to five bf16 matrices [64][64]
-// (N as upper and lower parts, P and, for the backward, P's lower parts) and three rows of 64 floats.
+// What the chunks' own products are, per (sequence, head, chunk): four or five bf16 matrices [64][64]
+// (N as upper and lower parts, P as two or, for the backward, up to three) and three rows of 64 floats.
+constexpr int GDN_SCAN_MATS = 4;
 struct GdnFactors {
     void* mat;                // [B, H, nc, mats, 64, 64] bf16
-    int mats;                 // 3, or for the backward gdn_back_mats
+    int mats;                 // GDN_SCAN_MATS, or for the backward gdn_back_mats
     float* gates;             // [B, H, nc, 3, 64]: prod_{l <= i} alpha_l, beta_i, prod_{l > i} alpha_l
 };
 size_t gdn_factor_mat_bytes(int64_t chunks, int mats);

@@ -14,7 +14,8 @@
 // bits; products of two lower parts are left out), h w, whose rounding the state would keep, as three.
 // e takes r itself in fp32.  With d_k <= 64, where keys are less orthogonal and the products shorter, S and beta r
 // have three parts as well and the product of two lower parts is taken (the state's error at d_k = 32 is 1.5e-6
-// without).  y alone takes P rounded to bf16 once, as y is.
+// without).  y takes S, P and w as two: with P as one, keys of a cosine of 0.64 and slow gates gave y an error of 9.6e-3,
+// where its own rounding to bf16 is 1.7e-3 (g Q S and P w cancel).
 #include "gdn_tc.cuh"
 
 namespace sdm {
@@ -394,9 +395,10 @@ static_assert(R_COL + 32 * 3 <= T_COLS && 32 * NH <= 128 && 64 * PARTS<128> <= 1
 
 template <int DK, bool KEEP>
 struct ScanTile {
-    static constexpr uint32_t KQ = 0, V = 128 * 2 * DK, M = V + C * 256, G = M + 3 * MAT, BYTES = G + 1024;
-    static constexpr uint32_t LOAD = KEEP ? 128 * DK + C * 256 + 2 * MAT + GATES : G + GATES;     // KEEP: no Q, no P
-    static constexpr int STAGES = KEEP ? 2 : 3;
+    static constexpr int MATS = KEEP ? 2 : GDN_SCAN_MATS;                                         // KEEP: no P, no Q
+    static constexpr uint32_t KQ = 0, V = 128 * 2 * DK, M = V + C * 256, G = M + MATS * MAT, BYTES = G + 1024;
+    static constexpr uint32_t LOAD = KEEP ? 128 * DK + C * 256 + MATS * MAT + GATES : G + GATES;
+    static constexpr int STAGES = 2;
     // KEEP: boxes of 128 columns on their way to memory, S per 64 of d_k, e per part
     static constexpr uint32_t KS = BYTES * STAGES, KE = KS + 256 * DK, CTL = KEEP ? KE + 32768 : KS;
 };
@@ -498,10 +500,11 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 await(bar(B_W), ph, dead);
                 if (elect_one()) {
 #pragma unroll
-                    for (int p = 0; p < NS; ++p)
+                    for (int m = 0; m < 3; ++m) {            // part m / 2 of w with part m % 2 of P
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
-                            mma_bf16_ta(tmem + Y_COL, tmem + R_COL + p * 32 + kk * 8, dm + 2 * (MAT / 16) + kk * 2, id64, (p | kk) != 0);
+                            mma_bf16_ta(tmem + Y_COL, tmem + R_COL + m / 2 * 32 + kk * 8, dm + (2 + m % 2) * (MAT / 16) + kk * 2, id64, (m | kk) != 0);
+                    }
                     mma_commit(bar(B_WP));
                 }
                 __syncwarp();
@@ -519,7 +522,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 tma_load_4d(t + L::V, &tv, col0, c * C, h, b, fb);
                 tma_load_4d(t + L::V + 8192, &tv, col0 + 64, c * C, h, b, fb);
 #pragma unroll
-                for (int m = 0; m < (KEEP ? 2 : 3); ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * f.mats + m) * C), fb);
+                for (int m = 0; m < L::MATS; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * f.mats + m) * C), fb);
                 bulk_load(t + L::G, f.gates + cid * 3 * C, GATES, fb);
             };
             int loaded = 0;

@@ -419,3 +419,40 @@ def test_offsets_past_32_bits(sdm):
     ry, rS = gdn(x["q"], x["k"], x["v"], x["alpha"], x["beta"], x["state"], 1.0)
     assert rel(cache[n - 1], rS[0]) <= TOL_F32 and rel(y, ry) <= TOL_Y
     assert float(cache[: n - 1].abs().max()) == 0.0
+
+
+# ------------------------------------------------------------------ correlated keys and slow gates
+# Keys and queries of a cosine of rho with each other (a silu before the projection's normalisation, neighbouring tokens),
+# alpha = sigmoid(N(mu, 1)), beta = sigmoid(N(bmu, 1)): what a chunk's products cancel down to is far below the products.
+REGIMES = [(0.25, 3, 0), (0.64, 8, 4), (0.9, 3, 4), (0.98, 3, 4), (0.98, 8, 0)]
+
+
+def _correlated(c, rho, mu, bmu, seed):
+    import torch
+    x, _ = _prepared(c, seed)
+    g = torch.Generator(device="cuda").manual_seed(seed + 1000)
+
+    def rand(*s):
+        return torch.randn(s, generator=g, device="cuda")
+
+    unit = lambda t: t / t.norm(dim=-1, keepdim=True)  # noqa: E731
+    mean = unit(rand(c["B"], c["Hk"], 1, c["dk"]))
+    for n in ("q", "k"):
+        x[n] = unit(rho ** 0.5 * mean + (1 - rho) ** 0.5 * unit(rand(c["B"], c["Hk"], c["T"], c["dk"]))).to(x[n].dtype)
+    x["alpha"] = torch.sigmoid(rand(c["B"], c["H"], c["T"]) + mu).to(x["alpha"].dtype)
+    x["beta"] = torch.sigmoid(rand(c["B"], c["H"], c["T"]) + bmu).to(x["beta"].dtype)
+    return x
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dk", [32, 64, 128])
+@pytest.mark.parametrize("rho,mu,bmu", REGIMES)
+def test_correlated_keys_output(sdm, rho, mu, bmu, dk, dtype):
+    """A bf16 y is off by its one rounding, 0.43 * 2^-8 in the root mean square, and what 16 bits of each factor add: 2e-3."""
+    from gdn_reference import gdn, rel
+    c = case(B=2, H=2, Hk=2, T=320, dk=dk, dv=64, dtype=dtype)
+    x = _correlated(c, rho, mu, bmu, 20)
+    ry, _ = gdn(x["q"], x["k"], x["v"], x["alpha"], x["beta"], x["state"], dk ** -0.5)
+    y, _ = _run_forward(sdm, x, c)
+    assert rel(y, ry) <= (TOL_F32 if dtype == "f32" else 2e-3)
