@@ -149,7 +149,7 @@ BwdLayout bwd_layout(const sdm_gdn_shape* s) {
     size_t marks, rows;
     if (L.tc) {
         const size_t chunks = bh * ((T + sdm::GDN_C64 - 1) / sdm::GDN_C64), dvp = (static_cast<size_t>(s->d_v) + 127) / 128 * 128;
-        L.gates = align256(sdm::gdn_factor_mat_bytes(static_cast<int64_t>(chunks), sdm::gdn_back_mats(s->d_k)));
+        L.gates = align256(sdm::gdn_factor_mat_bytes(static_cast<int64_t>(chunks), sdm::GDN_BACK_MATS));
         L.S = L.gates + align256(sdm::gdn_factor_gate_bytes(static_cast<int64_t>(chunks)));
         marks = chunks * dvp * (s->d_k <= 64 ? 64 : 128) * 2;
         rows = chunks * 2 * dvp * sdm::GDN_C64 * 2;
@@ -295,7 +295,7 @@ sdm_status sdm_gdn_backward(const sdm_gdn_shape* s, const void* q, const void* k
     char* ws = static_cast<char*>(workspace);
     const sdm::GdnArgs a = gdn_args(s, q, k, v, alpha, beta, lengths, err);
     if (L.tc) {
-        const sdm::GdnFactors fa{ws + L.mat, sdm::gdn_back_mats(s->d_k), reinterpret_cast<float*>(ws + L.gates)};
+        const sdm::GdnFactors fa{ws + L.mat, sdm::GDN_BACK_MATS, reinterpret_cast<float*>(ws + L.gates)};
         cudaError_t e = sdm::launch_gdn_factors(a, fa, st);
         if (e == cudaSuccess) e = sdm::launch_gdn_scan(sdm::GdnScan{a, nullptr, nullptr, state0, ws + L.S, ws + L.e}, fa, st);
         if (e == cudaSuccess) e = sdm::launch_gdn_back(sdm::GdnBack{a, dy, dstate, dv, dstate0, ws + L.dE, ws + L.d}, fa, st);

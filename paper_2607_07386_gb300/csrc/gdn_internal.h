@@ -90,12 +90,12 @@ struct GdnGrads {
 cudaError_t launch_gdn_grads(int dtype, const GdnGrads& g, cudaStream_t stream);
 
 // ---- chunked form on the tensor cores (k_gdn_chunk.cu): bf16, d_k <= 128, chunks of 64 ----
-// What the chunks' own products are, per (sequence, head, chunk): four or five bf16 matrices [64][64]
-// (N as upper and lower parts, P as two or, for the backward, up to three) and three rows of 64 floats.
-constexpr int GDN_SCAN_MATS = 4;
+// What the chunks' own products are, per (sequence, head, chunk): bf16 matrices [64][64], N as three parts (24
+// significant bits), then P as two, or for the backward, whose state depends on it, as three; and three rows of 64 floats.
+constexpr int GDN_N_PARTS = 3, GDN_SCAN_MATS = GDN_N_PARTS + 2, GDN_BACK_MATS = GDN_N_PARTS + 3;
 struct GdnFactors {
     void* mat;                // [B, H, nc, mats, 64, 64] bf16
-    int mats;                 // GDN_SCAN_MATS, or for the backward gdn_back_mats
+    int mats;                 // GDN_SCAN_MATS, or for the backward GDN_BACK_MATS
     float* gates;             // [B, H, nc, 3, 64]: prod_{l <= i} alpha_l, beta_i, prod_{l > i} alpha_l
 };
 size_t gdn_factor_mat_bytes(int64_t chunks, int mats);
@@ -113,9 +113,7 @@ struct GdnScan {
 };
 cudaError_t launch_gdn_scan(const GdnScan& s, const GdnFactors& f, cudaStream_t stream);
 
-// The backward's walk (k_gdn_back.cu), with f.mats == gdn_back_mats(dk): N in two bf16 parts, P in two, or three
-// with d_k <= 64, where its entries are larger.
-__host__ __device__ constexpr int gdn_back_mats(int dk) { return dk <= 64 ? 5 : 4; }
+// The backward's walk (k_gdn_back.cu), with f.mats == GDN_BACK_MATS.
 struct GdnBack {
     GdnArgs a;
     const void* dy;

@@ -14,7 +14,8 @@
 //   5  .. += (-beta g d)^T K                         (MMA; dv, d and the next chunk's dy are put away meanwhile)
 //   6  D = g_63 D + ..                               (registers, bf16 parts to TMEM)
 // D before every step 6 (as bf16) and d (as two bf16 parts) are stored for the gradients of q, k and the gates.
-// Operands are split as in the forward: what D would keep the rounding of has three parts, the others two.
+// Operands are split as in the forward, into three bf16 parts, and so is P, which D depends on (with two, 1e-5 of D at keys
+// of a cosine of 0.98).
 // The chain of the six stages bounds it: 280 us at B = 8, H = 16, T = 4096, 128 x 128, 8,000 cycles a chunk.
 #include "gdn_tc.cuh"
 
@@ -29,22 +30,27 @@ constexpr int SW = 8;                          // compute warps: two share a lan
 constexpr int ST = 32 * (SW + 4);
 constexpr int LAUNCH_REGS = 168, BACK_REGS = 232, IDLE_REGS = 40;   // a thread's registers, at first and after the split
 static_assert(BACK_REGS >= LAUNCH_REGS && IDLE_REGS <= LAUNCH_REGS && SW * BACK_REGS + 4 * IDLE_REGS <= (SW + 4) * LAUNCH_REGS, "register split");
-constexpr int NH = 3;                          // bf16 parts of what is added to D
-template <int DK> constexpr int PARTS = DK == 64 ? 3 : 2;        // of D and of beta x (see the forward walk)
-// TMEM columns: X: D^T K^T, then step 3; Z: dy^T P, then beta x (with d_k <= 64 its third part behind A); A: the update;
-// S: D, then beta g d; dy; g dy.
-constexpr uint32_t X_COL = 0, Z_COL = 64, A_COL = 128, S_COL = 256, Z3_COL = 192, Y_COL = 384, GY_COL = 416, T_COLS = 512;
+constexpr int NP = 3;                          // bf16 parts of D, of beta x and of what is added to D (see the forward walk)
+// TMEM columns: X: D^T K^T, then step 3; Z: dy^T P, then beta x; A: the update, and before that, with d_k > 64, the third
+// part of D, of every 64 rows in the first 32 of their own columns, which the warp that writes it has read; S: D, then
+// beta g d and the third part of beta x; dy; g dy.
+constexpr uint32_t X_COL = 0, Z_COL = 64, A_COL = 128, S_COL = 256, Z3_COL = S_COL + 32 * NP, Y_COL = 384, GY_COL = 416, T_COLS = 512;
+// Where 16 rows of d_k from x on of part p of D lie.
+template <int DK>
+__device__ __forceinline__ constexpr uint32_t d_at(int p, int x) {
+    return DK == 128 && p == 2 ? A_COL + x / 64 * 64 + x % 64 / 2 : S_COL + p * (DK / 2) + x / 2;
+}
 
 template <int DK>
 struct BackTile {
-    static constexpr int MATS = gdn_back_mats(DK);            // N and P in their parts
-    static constexpr uint32_t KQ = 0, Y = 128 * 2 * DK, M = Y + C * 256, BYTES = M + MATS * MAT;
+    static constexpr uint32_t KQ = 0, Y = 128 * 2 * DK, M = Y + C * 256, BYTES = M + GDN_BACK_MATS * MAT;   // M: N and P
     static constexpr uint32_t LOAD = BYTES + GATES;
     static constexpr int STAGES = 2;
-    // boxes of 128 columns on their way to memory (D per 64 of d_k, d per part), then the stages' gate products
-    static constexpr uint32_t KS = BYTES * STAGES, KE = KS + 256 * DK, G = KE + 32768, CTL = G + STAGES * GATES;
+    // boxes of 128 columns on their way to memory (D per 64 of d_k; then, where it was, d per part), then the stages'
+    // gate products
+    static constexpr uint32_t KS = BYTES * STAGES, G = KS + 32768, CTL = G + STAGES * GATES;
 };
-enum { B_FULL = 0, B_U = 2, B_XN, B_UP, B_FREE, B_S, B_DY, B_X, B_H, B_KS, B_OUT, B_COUNT };
+enum { B_FULL = 0, B_U = 2, B_XN, B_UP, B_DFREE, B_FREE, B_S, B_DY, B_X, B_H, B_KS, B_OUT, B_COUNT };
 struct BackCtl {
     unsigned long long bar[B_COUNT];
     uint32_t tmem;
@@ -91,7 +97,6 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
     tc_after_sync();
     const uint32_t tmem = ctl.tmem;
     volatile int* dead = &ctl.dead;
-    constexpr int SB = DK / 2, NP = PARTS<DK>;               // TMEM columns of a part of D; parts
 
     if (warp >= SW) {
         regs_dec<IDLE_REGS>();
@@ -99,50 +104,54 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
             const uint32_t id64 = mma_idesc(64), idm = id64 | MN_B, idk = mma_idesc(DK) | MN_B;
             for (int it = 0; it < chunks; ++it) {
                 const uint32_t t = ring + (it % L::STAGES) * L::BYTES, ph = it & 1;
-                const uint64_t dk = sw128_desc(t + L::KQ), dn = sw128_mn_desc(t + L::M, 8192), dp = sw128_mn_desc(t + L::M + 2 * MAT, 8192),
+                const uint64_t dk = sw128_desc(t + L::KQ), dn = sw128_mn_desc(t + L::M, 8192), dp = sw128_mn_desc(t + L::M + GDN_N_PARTS * MAT, 8192),
                                dkt = sw128_mn_desc(t + L::KQ, 16384), dqt = sw128_mn_desc(t + L::KQ + 8192, 16384);
                 await(bar(B_FULL + it % L::STAGES), (it / L::STAGES) & 1, dead);
                 await(bar(B_DY), ph, dead);
                 if (elect_one()) {                           // step 1
-#pragma unroll
-                    for (int p = 0; p < L::MATS - 2; ++p)
+#pragma unroll 1
+                    for (int p = GDN_BACK_MATS - GDN_N_PARTS - 1, first = 0; p >= 0; --p, first = 1)
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
-                            mma_bf16_ta(tmem + Z_COL, tmem + Y_COL + kk * 8, dp + p * (MAT / 16) + kk * 128, idm, (p | kk) != 0);
+                            mma_bf16_ta(tmem + Z_COL, tmem + Y_COL + kk * 8, dp + p * (MAT / 16) + kk * 128, idm, first != 0 || kk != 0);
                 }
                 __syncwarp();
                 await(bar(B_S), ph, dead);
                 if (elect_one()) {
-#pragma unroll
-                    for (int p = 0; p < NP; ++p)
+#pragma unroll                                               // lower parts first, here and below: their sums are small
+                    for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
                         for (int kk = 0; kk < DK / 16; ++kk)
-                            mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * SB + kk * 8, dk + (kk / 4) * 1024 + (kk % 4) * 2, id64, (p | kk) != 0);
+                            mma_bf16_ta(tmem + X_COL, tmem + d_at<DK>(p, 16 * kk), dk + (kk / 4) * 1024 + (kk % 4) * 2, id64, p != NP - 1 || kk != 0);
                     mma_commit(bar(B_U));
-#pragma unroll
-                    for (int p = 0; p < NH; ++p)
+                }
+                __syncwarp();
+                if (DK == 128) await(bar(B_U), ph, dead);    // D's third part is read
+                if (elect_one()) {
+#pragma unroll 1
+                    for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
-                            mma_bf16_ta(tmem + A_COL, tmem + GY_COL + p * 32 + kk * 8, dqt + kk * 128, idk, (p | kk) != 0);
+                            mma_bf16_ta(tmem + A_COL, tmem + GY_COL + p * 32 + kk * 8, dqt + kk * 128, idk, p != NP - 1 || kk != 0);
                 }
                 __syncwarp();
                 await(bar(B_X), ph, dead);
                 if (elect_one()) {                           // step 3: part xa of beta x with part nb of N
-#pragma unroll
-                    for (int m = 0; m < (NP == 3 ? 5 : 3); ++m) {
-                        const int xa = m / 2, nb = m % 2;    // (0, 0), (0, 1), (1, 0) and then (1, 1), (2, 0)
+#pragma unroll 1
+                    for (int m = 5; m >= 0; --m) {
+                        const int xa = m < 5 ? m / 2 : 0, nb = m < 5 ? m % 2 : 2;    // (0, 2), (2, 0), (1, 1), (1, 0), (0, 1), (0, 0)
                         const uint32_t from = xa == 2 ? Z3_COL : Z_COL + xa * 32;
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
-                            mma_bf16_ta(tmem + X_COL, tmem + from + kk * 8, dn + nb * (MAT / 16) + kk * 128, idm, (m | kk) != 0);
+                            mma_bf16_ta(tmem + X_COL, tmem + from + kk * 8, dn + nb * (MAT / 16) + kk * 128, idm, m != 5 || kk != 0);
                     }
                     mma_commit(bar(B_XN));
                 }
                 __syncwarp();
                 await(bar(B_H), ph, dead);
                 if (elect_one()) {                           // step 5
-#pragma unroll
-                    for (int p = 0; p < NH; ++p)
+#pragma unroll 1
+                    for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
                             mma_bf16_ta(tmem + A_COL, tmem + S_COL + p * 32 + kk * 8, dkt + kk * 128, idk, 1);
@@ -164,7 +173,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 tma_load_4d(t + L::Y, &ty, col0, c * C, h, b, fb);
                 tma_load_4d(t + L::Y + 8192, &ty, col0 + 64, c * C, h, b, fb);
 #pragma unroll
-                for (int m = 0; m < L::MATS; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * L::MATS + m) * C), fb);
+                for (int m = 0; m < GDN_BACK_MATS; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * GDN_BACK_MATS + m) * C), fb);
                 bulk_load(ring + L::G + (it % L::STAGES) * GATES, f.gates + cid * 3 * C, GATES, fb);
             };
             int loaded = 0;
@@ -178,10 +187,13 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 if (*dead) break;
 #pragma unroll
                 for (int x = 0; x < DK / 64; ++x) tma_store_2d(&tD, ring + L::KS + x * 16384, 64 * x, rs);
+                bulk_commit();
+                bulk_wait_read();
+                mbar_arrive(bar(B_DFREE));
                 mbar_wait_or_dead(bar(B_OUT), it & 1, dead); // d, and dv where the chunk's dy was
                 if (*dead) break;
 #pragma unroll
-                for (int p = 0; p < 2; ++p) tma_store_2d(&td, ring + L::KE + p * 16384, 0, rp + p * nblk * 128);
+                for (int p = 0; p < 2; ++p) tma_store_2d(&td, ring + L::KS + p * 16384, 0, rp + p * nblk * 128);
                 tma_store_4d(&tdv, t, col0, c * C, h, b);
                 if (col0 + 64 < a.dv) tma_store_4d(&tdv, t + 8192, col0 + 64, c * C, h, b);
                 bulk_commit();
@@ -223,9 +235,9 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                     const int at = half * RD + x + 8 * j;
                     *reinterpret_cast<uint4*>(ringp + L::KS + at / 64 * 16384 + box_at(row, at % 64 / 8)) = w;
                 };
-                put_part(lanes + S_COL + (half * RD + x) / 2, v, keep);
-                if (NP == 3) put_part(lanes + S_COL + SB + (half * RD + x) / 2, v);
-                put_last(lanes + S_COL + (NP - 1) * SB + (half * RD + x) / 2, v);
+                put_part(lanes + d_at<DK>(0, half * RD + x), v, keep);
+                put_part(lanes + d_at<DK>(1, half * RD + x), v);
+                put_last(lanes + d_at<DK>(2, half * RD + x), v);
             }
             announce(bar(B_S), lane);
             hand_over(bar(B_KS), lane);
@@ -291,8 +303,8 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 }
             }
             put_part(lanes + Z_COL + i0 / 2, w);
-            if (NP == 3) put_part(lanes + Z_COL + 32 + i0 / 2, w);
-            put_last(lanes + (NP == 3 ? Z3_COL : Z_COL + 32) + i0 / 2, w);
+            put_part(lanes + Z_COL + 32 + i0 / 2, w);
+            put_last(lanes + Z3_COL + i0 / 2, w);
             announce(bar(B_X), lane);
             const float g63 = gate[C - 1];
             await(bar(B_XN), ph, dead);
@@ -316,7 +328,9 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 const int i = i0 + j;
                 *reinterpret_cast<__nv_bfloat16*>(tile + yat + sw128_at(i, row % 64)) = __float2bfloat16_rn(i < n ? gate[C + i] * u[j] : 0.f);
             }
-            keep_parts(ringp + L::KE, row, i0 / 8, u);
+            mbar_wait_or_dead(bar(B_DFREE), ph, dead);       // D has left the place
+            __syncwarp();
+            keep_parts(ringp + L::KS, row, i0 / 8, u);
             hand_over(bar(B_OUT), lane);
             if (it + 1 < chunks) put_dy(it + 1);
             await(bar(B_UP), ph, dead);
@@ -369,7 +383,7 @@ cudaError_t back(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap
 
 cudaError_t launch_gdn_back(const GdnBack& r, const GdnFactors& f, cudaStream_t stream) {
     const GdnArgs& a = r.a;
-    if (f.mats != gdn_back_mats(a.dk)) return cudaErrorInvalidValue;
+    if (f.mats != GDN_BACK_MATS) return cudaErrorInvalidValue;
     const int64_t chunks = static_cast<int64_t>(a.B) * a.H * ((a.T + C - 1) / C);
     const int nblk = (a.dv + 127) / 128;
     CUtensorMap tk, tq, ty, tdv, tm, tD, td;

@@ -9,14 +9,15 @@
 // chunks of one (sequence, head, 128 columns of the state).  The products G are products of gates,
 // never quotients or exponentials of sums, and N does not divide by beta, so gates of zero are exact.
 //
-// Precision: the state and every sum are fp32.  k and q are exact operands.  What the state depends on
-// and is not a bf16 number enters the MMAs as bf16 parts: S, N and beta r as two (16 significant
-// bits; products of two lower parts are left out), h w, whose rounding the state would keep, as three.
-// e takes r itself in fp32.  With d_k <= 64, where keys are less orthogonal and the products shorter, S and beta r
-// have three parts as well and the product of two lower parts is taken (the state's error at d_k = 32 is 1.5e-6
-// without).  y takes S, P and w as two: with P as one, keys of a cosine of 0.64 and slow gates gave y an error of 9.6e-3,
-// where its own rounding to bf16 is 1.7e-3 (g Q S and P w cancel).
+// Precision: the state and every sum are fp32.  k and q are exact operands.  What the state depends on and is not a bf16
+// number enters the MMAs as three bf16 parts (24 significant bits): S, N, beta r and h w; of N (beta r), products below
+// 2^-24 are left out.  With two parts of S, N and beta r, keys of a cosine of 0.98 gave the state an error of 8e-6 and the
+// backward's, which ends at a hundredth of where it starts, 4.7e-5, where independent keys give 6e-7.  e takes r itself in
+// fp32.  y takes S, P and w as two parts: with P as one, keys of a cosine of 0.64 and slow gates gave y an error of
+// 9.6e-3, where its own rounding to bf16 is 1.7e-3 (g Q S and P w cancel).
 #include "gdn_tc.cuh"
+
+#include <limits.h>
 
 namespace sdm {
 
@@ -34,7 +35,7 @@ using namespace gdn;
 //   N_ij = -Z_ii sum_{j <= k < i} B_ik Y_kj,  Y = I + beta N,  a warp per block, transposed so that the sum is an
 // operand of the product with Z as it lies in registers.  These 16 x 16 products are too small for tcgen05 (at least 64
 // rows, and a trip through shared memory or TMEM between any two of a chain); they are mma.sync on tf32, each operand as two
-// parts of 11 bits, lower times lower left out: 21 bits, where N is kept at 16.  P and N leave through swizzled boxes and TMA.
+// parts of 11 bits, lower times lower left out: 21 bits.  P and N leave through swizzled boxes and TMA.
 // At B = 8, H = 16, T = 4096, d_k = 128: 88 us (119 with the products in fp32 from shared memory and 16-byte stores by the
 // threads), where q, k, N and P alone take 49 at the copy rate.  Five CTAs an SM issue half of the time and wait for
 // one another's chains the rest; the parts cut off with a mask in place of a conversion gave 10 us, loops kept short for
@@ -51,14 +52,14 @@ struct FactorSmem {
     uint32_t tmem;
     int dead;
 };
-// The K and Q tiles make room for these once the MMAs have read them, P's boxes for N and Z, and Bt for N's boxes.
+// The K and Q tiles make room for these once the MMAs have read them, P's boxes for N and Z, and all of it for N's boxes.
 struct FactorLate {
     float Bt[C][LP];                          // B transposed
     float N[C][LP];                           // on and below the diagonal blocks
     float Zt[C][BL + 4];                      // Z_ii transposed: [16 block + column][row]
 };
 constexpr uint32_t P_BOX = sizeof(FactorLate::Bt), FACTOR_LATE = P_BOX + 3 * MAT;
-static_assert(P_BOX % 1024 == 0 && 2 * MAT <= P_BOX && sizeof(FactorLate) <= FACTOR_LATE, "boxes");
+static_assert(P_BOX % 1024 == 0 && sizeof(FactorLate) <= FACTOR_LATE && GDN_N_PARTS * MAT <= FACTOR_LATE, "boxes");
 template <int DK>
 struct FactorSize {
     static constexpr size_t TILE = 128 * 2 * DK > FACTOR_LATE ? 128 * 2 * DK : FACTOR_LATE;
@@ -187,7 +188,7 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
             if (!isk) {
 #pragma unroll
                 for (int j = 4; j < 8; ++j)
-                    for (int p = 0; p < f.mats - 2; ++p) *reinterpret_cast<uint4*>(P + p * MAT + box_at(i, j)) = make_uint4(0, 0, 0, 0);
+                    for (int p = 0; p < f.mats - GDN_N_PARTS; ++p) *reinterpret_cast<uint4*>(P + p * MAT + box_at(i, j)) = make_uint4(0, 0, 0, 0);
             }
             continue;
         }
@@ -219,12 +220,10 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
                 for (int e = 0; e < 4; ++e) w[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
                 unsigned char* const at = P + box_at(i, 4 * half + j);
                 *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
-                if (f.mats > 3) {                                             // its lower parts
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
-                    *reinterpret_cast<uint4*>(at + MAT) = make_uint4(w[0], w[1], w[2], w[3]);
-                    if (f.mats > 4) *reinterpret_cast<uint4*>(at + 2 * MAT) = pack16<BF16>(v);
-                }
+                for (int e = 0; e < 4; ++e) w[e] = split2(v[2 * e], v[2 * e + 1], v[2 * e], v[2 * e + 1]);
+                *reinterpret_cast<uint4*>(at + MAT) = make_uint4(w[0], w[1], w[2], w[3]);
+                if (f.mats == GDN_BACK_MATS) *reinterpret_cast<uint4*>(at + 2 * MAT) = pack16<BF16>(v);
             }
         }
     }
@@ -233,7 +232,7 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
     const int row0 = static_cast<int>(cid * f.mats * C);
     if (warp == 2) {                                      // P leaves
         if (elect_one()) {
-            for (int p = 0; p < f.mats - 2; ++p) tma_store_2d(&tm, tile + P_BOX + p * MAT, 0, row0 + (2 + p) * C);
+            for (int p = 0; p < f.mats - GDN_N_PARTS; ++p) tma_store_2d(&tm, tile + P_BOX + p * MAT, 0, row0 + (GDN_N_PARTS + p) * C);
             bulk_commit();
             bulk_wait_read();
         }
@@ -329,21 +328,23 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
         }
         __syncthreads();
     }
-    {   // N as upper and lower parts, into boxes where Bt was: 16 rows a warp, four values a lane at a time
+    {   // N in its parts, into boxes where Bt and N were: 16 rows a warp, four values a lane at a time
         const int row = warp * BL + (lane >> 1);
+        float v[8][4];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
             const int x = 8 * q + 4 * (lane & 1);
-            uint2 hi = make_uint2(0, 0), lo = hi;
-            if (q / 2 <= warp) {                          // zeros from the diagonal on
-                const float4 f4 = *reinterpret_cast<const float4*>(&lt.N[row][x]);
-                float v[4] = {x < row ? f4.x : 0.f, x + 1 < row ? f4.y : 0.f, x + 2 < row ? f4.z : 0.f, x + 3 < row ? f4.w : 0.f};
-                hi.x = split2(v[0], v[1], v[0], v[1]); lo.x = pack2(v[0], v[1]);
-                hi.y = split2(v[2], v[3], v[2], v[3]); lo.y = pack2(v[2], v[3]);
-            }
+            float4 f4 = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (q / 2 <= warp) f4 = *reinterpret_cast<const float4*>(&lt.N[row][x]);      // zeros from the diagonal on
+            v[q][0] = x < row ? f4.x : 0.f; v[q][1] = x + 1 < row ? f4.y : 0.f; v[q][2] = x + 2 < row ? f4.z : 0.f; v[q][3] = x + 3 < row ? f4.w : 0.f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
             unsigned char* const at = raw + (tile - base) + box_at(row, q) + 8 * (lane & 1);
-            *reinterpret_cast<uint2*>(at) = hi;
-            *reinterpret_cast<uint2*>(at + MAT) = lo;
+#pragma unroll
+            for (int p = 0; p < GDN_N_PARTS; ++p)
+                *reinterpret_cast<uint2*>(at + p * MAT) = make_uint2(split2(v[q][0], v[q][1], v[q][0], v[q][1]), split2(v[q][2], v[q][3], v[q][2], v[q][3]));
         }
     }
     fence_async();
@@ -351,7 +352,7 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
     tc_before_sync();
     __syncthreads();
     if (tid == 0) {
-        for (int p = 0; p < 2; ++p) tma_store_2d(&tm, tile + p * MAT, 0, row0 + p * C);
+        for (int p = 0; p < GDN_N_PARTS; ++p) tma_store_2d(&tm, tile + p * MAT, 0, row0 + p * C);
         bulk_commit();
         bulk_wait_read();
     }
@@ -387,15 +388,14 @@ constexpr int LAUNCH_REGS = 128, SCAN_REGS = 184, OUT_REGS = 104, IDLE_REGS = 40
 static_assert(SCAN_REGS >= LAUNCH_REGS && OUT_REGS <= LAUNCH_REGS && IDLE_REGS <= LAUNCH_REGS &&
               SW * SCAN_REGS + OW * OUT_REGS + 4 * IDLE_REGS <= (SW + OW + 4) * LAUNCH_REGS, "register split");
 constexpr int NS = 2;                          // bf16 parts of S and of w as the factors of Q and P
-template <int DK> constexpr int PARTS = DK == 64 ? 3 : 2;        // of S as the factor of K, and of beta r
-constexpr int NH = 3;                          // bf16 parts of h w
+constexpr int NP = 3;                          // of S as the factor of K, of beta r and of h w
 // TMEM columns: X: steps 1, 3, 5; Y: w P^T; S; R: beta r, then w.  h w lies where S is, which steps 2 to 6 do not read.
-constexpr uint32_t X_COL = 0, Y_COL = 128, S_COL = 192, R_COL = S_COL + 128, T_COLS = 512;
-static_assert(R_COL + 32 * 3 <= T_COLS && 32 * NH <= 128 && 64 * PARTS<128> <= 128 && 32 * PARTS<64> <= 128, "TMEM columns");
+constexpr uint32_t X_COL = 0, Y_COL = 128, S_COL = 192, R_COL = S_COL + 64 * NP, T_COLS = 512;
+static_assert(R_COL + 32 * NP <= T_COLS, "TMEM columns");
 
 template <int DK, bool KEEP>
 struct ScanTile {
-    static constexpr int MATS = KEEP ? 2 : GDN_SCAN_MATS;                                         // KEEP: no P, no Q
+    static constexpr int MATS = KEEP ? GDN_N_PARTS : GDN_SCAN_MATS;                                       // KEEP: no P, no Q
     static constexpr uint32_t KQ = 0, V = 128 * 2 * DK, M = V + C * 256, G = M + MATS * MAT, BYTES = G + 1024;
     static constexpr uint32_t LOAD = KEEP ? 128 * DK + C * 256 + MATS * MAT + GATES : G + GATES;
     static constexpr int STAGES = 2;
@@ -444,7 +444,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
     tc_after_sync();
     const uint32_t tmem = ctl.tmem;
     volatile int* dead = &ctl.dead;
-    constexpr int SB = DK / 2, NP = PARTS<DK>;               // TMEM columns of a part of S; parts
+    constexpr int SB = DK / 2;                               // TMEM columns of a part of S
 
     if (warp >= SW + OW) {
         regs_dec<IDLE_REGS>();
@@ -456,31 +456,31 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                                dkt = sw128_mn_desc(t + L::KQ, 16384);
                 await(bar(B_FULL + c % L::STAGES), (c / L::STAGES) & 1, dead);
                 await(bar(B_S), ph, dead);
-                if (elect_one()) {                           // step 1
-#pragma unroll
-                    for (int p = 0; p < NP; ++p)
+                if (elect_one()) {                           // step 1; lower parts first, here and below: their sums are small
+#pragma unroll 1
+                    for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
                         for (int kk = 0; kk < DK / 16; ++kk)
-                            mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * SB + kk * 8, dk + (kk / 4) * 1024 + (kk % 4) * 2, id64, (p | kk) != 0);
+                            mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * SB + kk * 8, dk + (kk / 4) * 1024 + (kk % 4) * 2, id64, p != NP - 1 || kk != 0);
                     mma_commit(bar(B_U));
                     if (!KEEP) {
-#pragma unroll
-                    for (int p = 0; p < NS; ++p)
+#pragma unroll 1
+                    for (int p = NS - 1; p >= 0; --p)
 #pragma unroll
                         for (int kk = 0; kk < DK / 16; ++kk)
-                            mma_bf16_ta(tmem + X_COL + 64, tmem + S_COL + p * SB + kk * 8, dq + (kk / 4) * 1024 + (kk % 4) * 2, id64, (p | kk) != 0);
+                            mma_bf16_ta(tmem + X_COL + 64, tmem + S_COL + p * SB + kk * 8, dq + (kk / 4) * 1024 + (kk % 4) * 2, id64, p != NS - 1 || kk != 0);
                     mma_commit(bar(B_QS));
                     }
                 }
                 __syncwarp();
                 await(bar(B_R), ph, dead);
                 if (elect_one()) {                           // step 3: part ra of beta r with part nb of N
-#pragma unroll
-                    for (int m = 0; m < (NP == 3 ? 5 : 3); ++m) {
-                        const int ra = m / 2, nb = m % 2;    // (0, 0), (0, 1), (1, 0) and then (1, 1), (2, 0)
+#pragma unroll 1
+                    for (int m = 5; m >= 0; --m) {
+                        const int ra = m < 5 ? m / 2 : 0, nb = m < 5 ? m % 2 : 2;    // (0, 2), (2, 0), (1, 1), (1, 0), (0, 1), (0, 0)
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
-                            mma_bf16_ta(tmem + X_COL, tmem + R_COL + ra * 32 + kk * 8, dm + nb * (MAT / 16) + kk * 2, id64, (m | kk) != 0);
+                            mma_bf16_ta(tmem + X_COL, tmem + R_COL + ra * 32 + kk * 8, dm + nb * (MAT / 16) + kk * 2, id64, m != 5 || kk != 0);
                     }
                     mma_commit(bar(B_RN));
                 }
@@ -488,22 +488,22 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 if (!KEEP) await(bar(B_TAKEN), ph, dead);
                 await(bar(B_H), ph, dead);
                 if (elect_one()) {                           // step 5
-#pragma unroll
-                    for (int p = 0; p < NH; ++p)
+#pragma unroll 1
+                    for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
-                            mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * 32 + kk * 8, dkt + kk * 128, idk, (p | kk) != 0);
+                            mma_bf16_ta(tmem + X_COL, tmem + S_COL + p * 32 + kk * 8, dkt + kk * 128, idk, p != NP - 1 || kk != 0);
                     mma_commit(bar(B_HK));
                 }
                 __syncwarp();
                 if (KEEP) continue;
                 await(bar(B_W), ph, dead);
                 if (elect_one()) {
-#pragma unroll
-                    for (int m = 0; m < 3; ++m) {            // part m / 2 of w with part m % 2 of P
+#pragma unroll 1
+                    for (int m = 2; m >= 0; --m) {           // part m / 2 of w with part m % 2 of P
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
-                            mma_bf16_ta(tmem + Y_COL, tmem + R_COL + m / 2 * 32 + kk * 8, dm + (2 + m % 2) * (MAT / 16) + kk * 2, id64, (m | kk) != 0);
+                            mma_bf16_ta(tmem + Y_COL, tmem + R_COL + m / 2 * 32 + kk * 8, dm + (GDN_N_PARTS + m % 2) * (MAT / 16) + kk * 2, id64, m != 2 || kk != 0);
                     }
                     mma_commit(bar(B_WP));
                 }
@@ -641,7 +641,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                     if (KEEP) *reinterpret_cast<uint4*>(ringp + L::KS + at / 64 * 16384 + box_at(row, at % 64 / 8)) = w;
                 };
                 put_part(lanes + S_COL + (half * RD + x) / 2, v, keep);
-                if (NP == 3) put_part(lanes + S_COL + SB + (half * RD + x) / 2, v);
+                put_part(lanes + S_COL + SB + (half * RD + x) / 2, v);
                 put_last(lanes + S_COL + (NP - 1) * SB + (half * RD + x) / 2, v);
             }
             if (len - next * C < C) {                        // K rows past the length: zeros, whatever was there
@@ -691,7 +691,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
 #pragma unroll
             for (int j = 0; j < 32; ++j) w[j] = be[j] * u[j];
             put_part(lanes + R_COL + i0 / 2, w);
-            if (NP == 3) put_part(lanes + R_COL + 32 + i0 / 2, w);
+            put_part(lanes + R_COL + 32 + i0 / 2, w);
             put_last(lanes + R_COL + 32 * (NP - 1) + i0 / 2, w);
             announce(bar(B_R), lane);
             const float g63 = gate[C - 1];
@@ -791,6 +791,7 @@ bool gdn_chunk_supported(int dtype, int dk, int T) { return dtype == SDM_BF16 &&
 
 cudaError_t launch_gdn_factors(const GdnArgs& a, const GdnFactors& f, cudaStream_t stream) {
     const int64_t chunks = static_cast<int64_t>(a.B) * a.H * ((a.T + C - 1) / C);
+    if (chunks * f.mats * C > INT_MAX) return cudaErrorInvalidValue;       // rows of the matrices, 275 GB of them
     CUtensorMap tk, tq, tm;
     if (!token_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk) || !token_map(&tq, a.q, a.token_major, a.B, a.Hk, a.T, a.dk) ||
         !row_map(&tm, f.mat, chunks * f.mats * C, C, C))

@@ -456,3 +456,18 @@ def test_correlated_keys_output(sdm, rho, mu, bmu, dk, dtype):
     ry, _ = gdn(x["q"], x["k"], x["v"], x["alpha"], x["beta"], x["state"], dk ** -0.5)
     y, _ = _run_forward(sdm, x, c)
     assert rel(y, ry) <= (TOL_F32 if dtype == "f32" else 2e-3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dk", [32, 64, 128])
+@pytest.mark.parametrize("rho,mu,bmu", REGIMES)
+def test_correlated_keys_states(sdm, rho, mu, bmu, dk, dtype):
+    """The last state and the first state's gradient, which a chunk's products may take down to a hundredth of where it
+    starts, are float32 results all the same."""
+    from gdn_reference import gdn, gdn_grads, rel
+    c = case(B=2, H=2, Hk=2, T=320, dk=dk, dv=64, dtype=dtype)
+    x = _correlated(c, rho, mu, bmu, 21)
+    args = [x[n] for n in ("q", "k", "v", "alpha", "beta", "state")]
+    assert rel(_run_forward(sdm, x, c)[1], gdn(*args, dk ** -0.5)[1]) <= TOL_F32
+    assert rel(_run_backward(sdm, x, c)["state"], gdn_grads(*args, dk ** -0.5, x["dy"], x["dstate"])[-1]) <= TOL_F32
