@@ -140,19 +140,20 @@ FwdLayout fwd_layout(const sdm_gdn_shape* s) {
 // chunks' factors, then states and rows as bf16 (see GdnScan, GdnBack).
 struct BwdLayout {
     bool tc;
-    size_t mat, gates, S, dE, e, d, fact, total;
+    size_t mat, gates, S, dE, e, d, ke, fact, total;
 };
 BwdLayout bwd_layout(const sdm_gdn_shape* s) {
     BwdLayout L{};
     const size_t bh = static_cast<size_t>(s->B) * s->H, T = static_cast<size_t>(s->T);
     L.tc = sdm::gdn_chunk_supported(s->dtype, s->d_k, s->T);
-    size_t marks, rows;
+    size_t marks, rows, ke = 0;
     if (L.tc) {
         const size_t chunks = bh * ((T + sdm::GDN_C64 - 1) / sdm::GDN_C64), dvp = (static_cast<size_t>(s->d_v) + 127) / 128 * 128;
         L.gates = align256(sdm::gdn_factor_mat_bytes(static_cast<int64_t>(chunks), sdm::GDN_BACK_MATS));
         L.S = L.gates + align256(sdm::gdn_factor_gate_bytes(static_cast<int64_t>(chunks)));
         marks = chunks * dvp * (s->d_k <= 64 ? 64 : 128) * 2;
         rows = chunks * 2 * dvp * sdm::GDN_C64 * 2;
+        ke = chunks * (dvp / 32) * sdm::GDN_C64 * 4;
     } else {
         marks = bh * ((T + sdm::GDN_C32 - 1) / sdm::GDN_C32) * s->d_k * s->d_v * 4;
         rows = bh * T * s->d_v * 4;
@@ -160,7 +161,8 @@ BwdLayout bwd_layout(const sdm_gdn_shape* s) {
     L.dE = L.S + align256(marks);
     L.e = L.dE + align256(marks);
     L.d = L.e + align256(rows);
-    L.fact = L.d + align256(rows);
+    L.ke = L.d + align256(rows);
+    L.fact = L.ke + align256(ke);
     L.total = L.fact + (L.tc ? 0 : walk_bytes(s));
     return L;
 }
@@ -295,12 +297,13 @@ sdm_status sdm_gdn_backward(const sdm_gdn_shape* s, const void* q, const void* k
     char* ws = static_cast<char*>(workspace);
     const sdm::GdnArgs a = gdn_args(s, q, k, v, alpha, beta, lengths, err);
     if (L.tc) {
+        float* const ke = reinterpret_cast<float*>(ws + L.ke);
         const sdm::GdnFactors fa{ws + L.mat, sdm::GDN_BACK_MATS, reinterpret_cast<float*>(ws + L.gates)};
         cudaError_t e = sdm::launch_gdn_factors(a, fa, st);
         if (e == cudaSuccess) e = sdm::launch_gdn_scan(sdm::GdnScan{a, nullptr, nullptr, state0, ws + L.S, ws + L.e}, fa, st);
-        if (e == cudaSuccess) e = sdm::launch_gdn_back(sdm::GdnBack{a, dy, dstate, dv, dstate0, ws + L.dE, ws + L.d}, fa, st);
+        if (e == cudaSuccess) e = sdm::launch_gdn_back(sdm::GdnBack{a, dy, dstate, dv, dstate0, ws + L.dE, ws + L.d, ws + L.e, ke}, fa, st);
         if (e == cudaSuccess)
-            e = sdm::launch_gdn_grads_tc(sdm::GdnGradsTc{a, dy, fa.gates, ws + L.S, ws + L.dE, ws + L.e, ws + L.d, dq, dk, dalpha, dbeta}, st);
+            e = sdm::launch_gdn_grads_tc(sdm::GdnGradsTc{a, dy, fa.gates, ws + L.S, ws + L.dE, ws + L.e, ws + L.d, ke, dq, dk, dalpha, dbeta}, st);
         return done(e, "sdm_gdn_backward");
     }
     float* const fact = L.total > L.fact ? reinterpret_cast<float*>(ws + L.fact) : nullptr;

@@ -122,6 +122,8 @@ struct GdnBack {
     float* dstate0;           // dL/dS_0 or nullptr
     void* keep_D;             // [B, H, nc, dv', dk'] bf16: the gradients of the states after the chunks, transposed
     void* keep_d;             // [B, H, nc, 2, dv', 64] bf16: d as upper and lower parts, transposed
+    const void* e;            // as the forward walk stored it (GdnScan::keep_e)
+    float* ke;                // [B, H, nc, dv' / 32, 64]: <D^T k_j, e_j> over 32 columns, D after the chunk
 };
 cudaError_t launch_gdn_back(const GdnBack& r, const GdnFactors& f, cudaStream_t stream);
 
@@ -130,7 +132,7 @@ struct GdnGradsTc {
     GdnArgs a;
     const void* dy;
     const float* gates;       // GdnFactors::gates
-    const void* S; const void* D; const void* e; const void* d;   // as GdnScan and GdnBack store them
+    const void* S; const void* D; const void* e; const void* d; const float* ke;   // as GdnScan and GdnBack store them
     void* dq; void* dk; void* dalpha; void* dbeta;
 };
 cudaError_t launch_gdn_grads_tc(const GdnGradsTc& g, cudaStream_t stream);

@@ -98,6 +98,20 @@ __device__ __forceinline__ void get32(const float* p, float (&v)[32]) {
         v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
     }
 }
+// Sums over the lanes of 32 values per lane: lane l gets the sum of value l.
+__device__ __forceinline__ float sum_lanes(float (&v)[32], int lane) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int j = 0; j < o; ++j) {
+            const float give = up ? v[j] : v[j + o], keep = up ? v[j + o] : v[j];
+            v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+    }
+    return v[0];
+}
+
 // A warp's share of an operand is in TMEM: tells the issuing warp.
 __device__ __forceinline__ void announce(uint32_t bar, int lane) {
     tmem_st_wait();

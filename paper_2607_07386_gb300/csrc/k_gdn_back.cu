@@ -13,7 +13,8 @@
 //   4  d = x + ..,  beta g d                         (registers, bf16 parts to TMEM)
 //   5  .. += (-beta g d)^T K                         (MMA; dv, d and the next chunk's dy are put away meanwhile)
 //   6  D = g_63 D + ..                               (registers, bf16 parts to TMEM)
-// D before every step 6 (as bf16) and d (as two bf16 parts) are stored for the gradients of q, k and the gates.
+// D before every step 6 (as bf16), d (as two bf16 parts) and the products <D^T k_j, e_j> with the forward's e are stored for the
+// gradients of q, k and the gates.
 // Operands are split as in the forward, into three bf16 parts, and so is P, which D depends on (with two, 1e-5 of D at keys
 // of a cosine of 0.98).
 // The chain of the six stages bounds it: 280 us at B = 8, H = 16, T = 4096, 128 x 128, 8,000 cycles a chunk.
@@ -43,14 +44,16 @@ __device__ __forceinline__ constexpr uint32_t d_at(int p, int x) {
 
 template <int DK>
 struct BackTile {
-    static constexpr uint32_t KQ = 0, Y = 128 * 2 * DK, M = Y + C * 256, BYTES = M + GDN_BACK_MATS * MAT;   // M: N and P
-    static constexpr uint32_t LOAD = BYTES + GATES;
+    static constexpr uint32_t KQ = 0, Y = 128 * 2 * DK, BYTES = Y + C * 256, LOAD = BYTES + GATES;
     static constexpr int STAGES = 2;
-    // boxes of 128 columns on their way to memory (D per 64 of d_k; then, where it was, d per part), then the stages'
-    // gate products
-    static constexpr uint32_t KS = BYTES * STAGES, G = KS + 32768, CTL = G + STAGES * GATES;
+    // N and P in their parts; e, per part; a box of 128 columns on its way to memory (D per 64 of d_k, then d per part);
+    // the stages' gate products
+    static constexpr uint32_t N = BYTES * STAGES, P = N + GDN_N_PARTS * MAT, E = N + GDN_BACK_MATS * MAT, KS = E + 32768, G = KS + 32768,
+                              CTL = G + STAGES * GATES;
 };
-enum { B_FULL = 0, B_U = 2, B_XN, B_UP, B_DFREE, B_FREE, B_S, B_DY, B_X, B_H, B_KS, B_OUT, B_COUNT };
+// Barriers.  Completed by copies: a stage's tile, P, N, e; by MMAs: U, beta x N, the update; by the copying thread: D (all)
+// has left the box; by warps: the rest.
+enum { B_FULL = 0, B_P = 2, B_N, B_E, B_U, B_XN, B_UP, B_DFREE, B_FREE, B_S, B_DY, B_X, B_H, B_KS, B_OUT, B_COUNT };
 struct BackCtl {
     unsigned long long bar[B_COUNT];
     uint32_t tmem;
@@ -70,6 +73,7 @@ template <int DK>
 __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tq,
                                                     const __grid_constant__ CUtensorMap ty, const __grid_constant__ CUtensorMap tdv,
                                                     const __grid_constant__ CUtensorMap tm, const __grid_constant__ CUtensorMap tD, const __grid_constant__ CUtensorMap td,
+                                                    const __grid_constant__ CUtensorMap te,
                                                     const GdnBack r, const GdnFactors f, int nc) {
     using L = BackTile<DK>;
     extern __shared__ unsigned char raw[];
@@ -104,9 +108,10 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
             const uint32_t id64 = mma_idesc(64), idm = id64 | MN_B, idk = mma_idesc(DK) | MN_B;
             for (int it = 0; it < chunks; ++it) {
                 const uint32_t t = ring + (it % L::STAGES) * L::BYTES, ph = it & 1;
-                const uint64_t dk = sw128_desc(t + L::KQ), dn = sw128_mn_desc(t + L::M, 8192), dp = sw128_mn_desc(t + L::M + GDN_N_PARTS * MAT, 8192),
+                const uint64_t dk = sw128_desc(t + L::KQ), dn = sw128_mn_desc(ring + L::N, 8192), dp = sw128_mn_desc(ring + L::P, 8192),
                                dkt = sw128_mn_desc(t + L::KQ, 16384), dqt = sw128_mn_desc(t + L::KQ + 8192, 16384);
                 await(bar(B_FULL + it % L::STAGES), (it / L::STAGES) & 1, dead);
+                await(bar(B_P), ph, dead);
                 await(bar(B_DY), ph, dead);
                 if (elect_one()) {                           // step 1
 #pragma unroll 1
@@ -135,6 +140,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                             mma_bf16_ta(tmem + A_COL, tmem + GY_COL + p * 32 + kk * 8, dqt + kk * 128, idk, p != NP - 1 || kk != 0);
                 }
                 __syncwarp();
+                await(bar(B_N), ph, dead);
                 await(bar(B_X), ph, dead);
                 if (elect_one()) {                           // step 3: part xa of beta x with part nb of N
 #pragma unroll 1
@@ -172,16 +178,36 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 }
                 tma_load_4d(t + L::Y, &ty, col0, c * C, h, b, fb);
                 tma_load_4d(t + L::Y + 8192, &ty, col0 + 64, c * C, h, b, fb);
-#pragma unroll
-                for (int m = 0; m < GDN_BACK_MATS; ++m) tma_load_2d(t + L::M + m * MAT, &tm, 0, static_cast<int>((cid * GDN_BACK_MATS + m) * C), fb);
                 bulk_load(ring + L::G + (it % L::STAGES) * GATES, f.gates + cid * 3 * C, GATES, fb);
             };
-            int loaded = 0;
-            for (; loaded < chunks && loaded < L::STAGES; ++loaded) load(loaded);
+            const int nblk = gridDim.x, blk = blockIdx.x;
+            auto cid_of = [&](int it) { return chain * nc + chunks - 1 - it; };
+            auto load_mats = [&](int it, int first, int n, int fb) {
+                mbar_expect_tx(bar(fb), n * MAT);
+                for (int m = first; m < first + n; ++m)
+                    tma_load_2d(ring + L::N + m * MAT, &tm, 0, static_cast<int>((cid_of(it) * GDN_BACK_MATS + m) * C), bar(fb));
+            };
+            auto load_p = [&](int it) { load_mats(it, GDN_N_PARTS, GDN_BACK_MATS - GDN_N_PARTS, B_P); };
+            auto load_n = [&](int it) { load_mats(it, 0, GDN_N_PARTS, B_N); };
+            auto load_e = [&](int it) {
+                mbar_expect_tx(bar(B_E), 32768);
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+                    tma_load_2d(ring + L::E + p * 16384, &te, 0, static_cast<int>(((cid_of(it) * 2 + p) * nblk + blk) * 128), bar(B_E));
+            };
+            int loaded = 0, np = 0, nn = 0, ne = 0;
+            if (chunks > 0) {
+                load(loaded++);
+                load_p(np++);
+                load_n(nn++);
+                load_e(ne++);
+                if (chunks > 1) load(loaded++);
+            }
             for (int it = 0; it < chunks; ++it) {
                 const uint32_t t = ring + (it % L::STAGES) * L::BYTES + L::Y;
-                const int c = chunks - 1 - it, nblk = gridDim.x, blk = blockIdx.x;
-                const int64_t cid = chain * nc + c;
+                const int c = chunks - 1 - it;
+                const bool more = it + 1 < chunks;
+                const int64_t cid = cid_of(it);
                 const int rs = static_cast<int>((cid * nblk + blk) * 128), rp = static_cast<int>((cid * 2 * nblk + blk) * 128);
                 mbar_wait_or_dead(bar(B_KS), it & 1, dead);
                 if (*dead) break;
@@ -190,8 +216,15 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 bulk_commit();
                 bulk_wait_read();
                 mbar_arrive(bar(B_DFREE));
+                mbar_wait_or_dead(bar(B_U), it & 1, dead);   // P, then N, then e are read: the next chunk's
+                if (*dead) break;
+                if (more) load_p(np++);
+                mbar_wait_or_dead(bar(B_XN), it & 1, dead);
+                if (*dead) break;
+                if (more) load_n(nn++);
                 mbar_wait_or_dead(bar(B_OUT), it & 1, dead); // d, and dv where the chunk's dy was
                 if (*dead) break;
+                if (more) load_e(ne++);
 #pragma unroll
                 for (int p = 0; p < 2; ++p) tma_store_2d(&td, ring + L::KS + p * 16384, 0, rp + p * nblk * 128);
                 tma_store_4d(&tdv, t, col0, c * C, h, b);
@@ -204,9 +237,13 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 if (loaded < chunks) load(loaded++);
             }
             bulk_wait();
-            if (*dead)                                       // the copies in flight land before the CTA ends
+            if (*dead) {                                     // the copies in flight land before the CTA ends
                 for (int j = loaded > L::STAGES ? loaded - L::STAGES : 0; j < loaded; ++j)
                     mbar_wait(bar(B_FULL + j % L::STAGES), (j / L::STAGES) & 1);
+                if (np > 0) mbar_wait(bar(B_P), (np - 1) & 1);
+                if (nn > 0) mbar_wait(bar(B_N), (nn - 1) & 1);
+                if (ne > 0) mbar_wait(bar(B_E), (ne - 1) & 1);
+            }
         }
     } else {
         regs_inc<BACK_REGS>();
@@ -287,7 +324,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
             const uint32_t ph = it & 1;
             unsigned char* tile = ringp + s * L::BYTES;
             const float* gate = reinterpret_cast<const float*>(ringp + L::G + s * GATES);
-            float u[32], w[32];
+            float u[32], w[32], ke[32];                      // ke: D^T k_j, then times e_j
             await(bar(B_U), ph, dead);
             tmem_ld32(lanes + X_COL + i0, u);                // step 2
             tmem_ld32(lanes + Z_COL + i0, w);
@@ -298,6 +335,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
                 const float hj[4] = {h4.x, h4.y, h4.z, h4.w}, bj[4] = {b4.x, b4.y, b4.z, b4.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
+                    ke[j + e] = u[j + e];
                     u[j + e] = fmaf(hj[e], u[j + e], a.scale * w[j + e]);
                     w[j + e] = bj[e] * u[j + e];
                 }
@@ -307,6 +345,17 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
             put_last(lanes + Z3_COL + i0 / 2, w);
             announce(bar(B_X), lane);
             const float g63 = gate[C - 1];
+            mbar_wait_or_dead(bar(B_E), ph, dead);
+            const unsigned char* const ep = ringp + L::E;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float hi[8], lo[8];
+                unpack16<BF16>(*reinterpret_cast<const uint4*>(ep + box_at(row, i0 / 8 + j)), hi);
+                unpack16<BF16>(*reinterpret_cast<const uint4*>(ep + 16384 + box_at(row, i0 / 8 + j)), lo);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ke[8 * j + e] *= hi[e] + lo[e];
+            }
+            r.ke[(((chain * nc + c) * gridDim.x + blockIdx.x) * 4 + quad) * C + i0 + lane] = sum_lanes(ke, lane);
             await(bar(B_XN), ph, dead);
             tmem_ld32(lanes + X_COL + i0, w);                // step 4
 #pragma unroll
@@ -364,7 +413,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_back(const __grid_constant__ CUte
 
 template <int DK>
 cudaError_t back(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap& ty, const CUtensorMap& tdv, const CUtensorMap& tm,
-                 const CUtensorMap& tD, const CUtensorMap& td, const GdnBack& r, const GdnFactors& f, cudaStream_t stream) {
+                 const CUtensorMap& tD, const CUtensorMap& td, const CUtensorMap& te, const GdnBack& r, const GdnFactors& f, cudaStream_t stream) {
     constexpr size_t smem = back_smem<DK>();
     // the compute warpgroups' registers come out of what the CTA is launched with
     static const int regs = [] {
@@ -375,7 +424,7 @@ cudaError_t back(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap
     static std::atomic<unsigned long long> seen;
     cudaError_t e = allow_smem(k_gdn_back<DK>, smem, seen);
     if (e != cudaSuccess) return e;
-    k_gdn_back<DK><<<dim3((r.a.dv + 127) / 128, r.a.H, r.a.B), ST, smem, stream>>>(tk, tq, ty, tdv, tm, tD, td, r, f, (r.a.T + C - 1) / C);
+    k_gdn_back<DK><<<dim3((r.a.dv + 127) / 128, r.a.H, r.a.B), ST, smem, stream>>>(tk, tq, ty, tdv, tm, tD, td, te, r, f, (r.a.T + C - 1) / C);
     return cudaGetLastError();
 }
 
@@ -386,13 +435,13 @@ cudaError_t launch_gdn_back(const GdnBack& r, const GdnFactors& f, cudaStream_t 
     if (f.mats != GDN_BACK_MATS) return cudaErrorInvalidValue;
     const int64_t chunks = static_cast<int64_t>(a.B) * a.H * ((a.T + C - 1) / C);
     const int nblk = (a.dv + 127) / 128;
-    CUtensorMap tk, tq, ty, tdv, tm, tD, td;
+    CUtensorMap tk, tq, ty, tdv, tm, tD, td, te;
     if (!token_map(&tk, a.k, a.token_major, a.B, a.Hk, a.T, a.dk) || !token_map(&tq, a.q, a.token_major, a.B, a.Hk, a.T, a.dk) ||
         !token_map(&ty, r.dy, a.token_major, a.B, a.H, a.T, a.dv) || !token_map(&tdv, r.dv, a.token_major, a.B, a.H, a.T, a.dv) ||
         !row_map(&tm, f.mat, chunks * f.mats * C, C, C) || !row_map(&tD, r.keep_D, chunks * nblk * 128, a.dk <= 64 ? 64 : 128, 128) ||
-        !row_map(&td, r.keep_d, chunks * 2 * nblk * 128, C, 128))
+        !row_map(&td, r.keep_d, chunks * 2 * nblk * 128, C, 128) || !row_map(&te, r.e, chunks * 2 * nblk * 128, C, 128))
         return cudaErrorInvalidValue;
-    return a.dk <= 64 ? back<64>(tk, tq, ty, tdv, tm, tD, td, r, f, stream) : back<128>(tk, tq, ty, tdv, tm, tD, td, r, f, stream);
+    return a.dk <= 64 ? back<64>(tk, tq, ty, tdv, tm, tD, td, te, r, f, stream) : back<128>(tk, tq, ty, tdv, tm, tD, td, te, r, f, stream);
 }
 
 }  // namespace sdm

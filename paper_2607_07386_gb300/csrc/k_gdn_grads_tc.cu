@@ -10,7 +10,9 @@
 // gradients X of the decay products, with the chunk's start as column -1 and its end as row 64 (nothing is
 // divided by a gate):
 //   X_ij = beta_j <dy_i, e_j> q_i.k_j - beta_i beta_j <d_i, e_j> k_i.k_j,   X_{i,-1} = q_i.S dy_i - beta_i k_i.S d_i,
-//   X_{64,j} = beta_j k_j.D e_j,   X_{64,-1} = <D, S>.
+//   X_{64,j} = beta_j <D^T k_j, e_j>,   X_{64,-1} = <D, S>.
+// The reverse walk has D^T k_j in fp32 and stores <D^T k_j, e_j>; from D as it is stored here, rounded to bf16, dalpha was off
+// by 8e-3 at keys of a cosine of 0.98, along which D is small.
 //
 // One CTA per SM walks over the chunks of the key heads and adds up the value heads that share one.  The
 // products over d_v have d_k as TMEM lanes (S and D are A operands as they lie), <dy, e> the tokens in
@@ -49,7 +51,7 @@ struct Tile {
 enum { B_KQ = 0, B_TILE, B_INTER, B_INTRA, B_KREADY, B_M, B_READ, B_X, B_KFREE, B_OUT, B_XFREE, B_EMPTY, B_MFREE, B_COUNT };
 struct Ctl {
     float X[(C + 1) * (C + 2) / 2];
-    float dots[2][4][C];                       // X_{i,-1} and X_{64,j}, the share of each lane quarter
+    float dots[4][C];                          // X_{i,-1}, the share of each lane quarter
     alignas(16) float gt[3][C];                // g, beta, h of the head's chunk
     float db[C];
     float es[SW];
@@ -63,20 +65,6 @@ template <int DK>
 constexpr size_t grads_smem() { return 1024 + Tile<DK>::BYTES + sizeof(Ctl); }
 
 __device__ __forceinline__ void bar_compute() { asm volatile("bar.sync 1, %0;\n" ::"n"(32 * SW) : "memory"); }
-
-// Sums over the lanes of 32 values per lane: lane l gets the sum of value l.
-__device__ __forceinline__ float sum_lanes(float (&v)[32], int lane) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const bool up = lane & o;
-#pragma unroll
-        for (int j = 0; j < o; ++j) {
-            const float give = up ? v[j] : v[j + o], keep = up ? v[j + o] : v[j];
-            v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-        }
-    }
-    return v[0];
-}
 
 // A warp of which every lane has put something into shared memory for the MMAs or other warps.
 __device__ __forceinline__ void arrive(uint32_t bar, int lane) {
@@ -345,7 +333,11 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                 const int64_t chain = static_cast<int64_t>(x.b) * a.H + x.hk * group + hv;
                 unsigned short al = 0x3f80;
                 if (tid < n) al = __ldg(static_cast<const unsigned short*>(a.alpha) + chain * a.T + t0 + tid);
-                float es = 0.f, gv = 0.f;                    // <D, S>; a gate product of the head
+                float es = 0.f, gv = 0.f, ke = 0.f;          // <D, S>; a gate product of the head; <D^T k_j, e_j>
+                if (tid < C) {
+                    const float* at = r.ke + (chain * nc + x.c) * nblk * 4 * C + tid;
+                    for (int p = 0; p < 4 * nblk; ++p) ke += __ldg(at + p * C);
+                }
                 for (int blk = 0; blk < nblk; ++blk, ++ns) {
                     mbar_wait_or_dead(bar(B_TILE), ns & 1, dead);
                     for (int p = tid; p < 16 * DK; p += 32 * SW) {
@@ -494,7 +486,7 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                                 c[j + e] = fmaf(x, at16(kc, j + e), c[j + e]);
                             }
                         }
-                        ctl.dots[0][quad][i0 + lane] = sum_lanes(c, lane);
+                        ctl.dots[quad][i0 + lane] = sum_lanes(c, lane);
                         tmem_ld32(lanes + DE + i0, p);
                         only(p);
 #pragma unroll
@@ -502,13 +494,8 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                             const float4 h4 = *reinterpret_cast<const float4*>(&ctl.gt[2][i0 + j]), b4 = *reinterpret_cast<const float4*>(&ctl.gt[1][i0 + j]);
                             const float hj[4] = {h4.x, h4.y, h4.z, h4.w}, bj[4] = {b4.x, b4.y, b4.z, b4.w};
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float x = bj[e] * p[j + e];
-                                dk[j + e] = fmaf(hj[e], x, dk[j + e]);
-                                p[j + e] = x * at16(kc, j + e);
-                            }
+                            for (int e = 0; e < 4; ++e) dk[j + e] = fmaf(hj[e], bj[e] * p[j + e], dk[j + e]);
                         }
-                        ctl.dots[1][quad][i0 + lane] = sum_lanes(p, lane);
                     }
                     arrive(bar(B_READ), lane);
                     bar_compute();
@@ -518,8 +505,8 @@ __global__ void __launch_bounds__(NT, 1) k_gdn_grads_tc(const __grid_constant__ 
                             if (i0 + j < i) ctl.X[x_at(i, i0 + j + 1)] += v[j];
                     }
                     if (tid < C) {
-                        ctl.X[x_at(tid, 0)] = (ctl.dots[0][0][tid] + ctl.dots[0][1][tid]) + (ctl.dots[0][2][tid] + ctl.dots[0][3][tid]);
-                        ctl.X[x_at(C, tid + 1)] = (ctl.dots[1][0][tid] + ctl.dots[1][1][tid]) + (ctl.dots[1][2][tid] + ctl.dots[1][3][tid]);
+                        ctl.X[x_at(tid, 0)] = (ctl.dots[0][tid] + ctl.dots[1][tid]) + (ctl.dots[2][tid] + ctl.dots[3][tid]);
+                        ctl.X[x_at(C, tid + 1)] = ctl.gt[1][tid] * ke;
                         if (tid == 0) {
                             float e = 0.f;
                             for (int wp = 0; wp < SW; ++wp) e += ctl.es[wp];

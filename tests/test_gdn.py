@@ -471,3 +471,26 @@ def test_correlated_keys_states(sdm, rho, mu, bmu, dk, dtype):
     args = [x[n] for n in ("q", "k", "v", "alpha", "beta", "state")]
     assert rel(_run_forward(sdm, x, c)[1], gdn(*args, dk ** -0.5)[1]) <= TOL_F32
     assert rel(_run_backward(sdm, x, c)["state"], gdn_grads(*args, dk ** -0.5, x["dy"], x["dstate"])[-1]) <= TOL_F32
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dk", [32, 64, 128])
+@pytest.mark.parametrize("rho,mu,bmu", REGIMES)
+def test_correlated_keys_gradients(sdm, rho, mu, bmu, dk, dtype):
+    """A bf16 gradient is rounded, 0.43 * 2^-8 in the root mean square, and has up to two once rounded factors (S, D):
+    0.74 * 2^-8, and 2^-8 allowed.  dalpha: where the gates forget a chunk's start (mu = 3) its terms, up to a hundred times
+    what they cancel down to, have factors of 16 bits: 0.6 * 2^-8 with its rounding; else <D, S> of rounded S and D is in it,
+    with one error for all 64 tokens of a chunk, so that a test of few chunks may be off by twice the root mean square:
+    1.5 * 2^-8.  In float32 the same terms' sums, a few roundings each: 100 * 2^-22."""
+    from gdn_reference import gdn_grads, rel
+    c = case(B=2, H=2, Hk=2, T=320, dk=dk, dv=64, dtype=dtype)
+    x = _correlated(c, rho, mu, bmu, 22)
+    ref = gdn_grads(*[x[n] for n in ("q", "k", "v", "alpha", "beta", "state")], dk ** -0.5, x["dy"], x["dstate"])
+    got = _run_backward(sdm, x, c)
+    far = {n: rel(got[n], r) for n, r in zip(("q", "k", "v", "alpha", "beta"), ref)}
+    for n, f in far.items():
+        if dtype == "f32":
+            assert f <= (100 * 2.0 ** -22 if n == "alpha" else TOL_F32), far
+        else:
+            assert f <= (1.0 if n != "alpha" else 0.6 if mu == 3 else 1.5) * 2.0 ** -8, far
