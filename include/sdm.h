@@ -426,7 +426,8 @@ size_t sdm_gdn_backward_workspace_bytes(const sdm_gdn_shape* shape);
  * d_k <= 128 and T >= 32 run in chunks of 64 tokens on the tensor cores (operands that the state
  * depends on are split into bf16 parts, so that the state is off by about 1e-6); float32 calls with
  * T >= 32 and few sequences and heads in chunks of 32 tokens in fp32; others token by token in
- * fp32.  Infinities in a live token reach the tokens of its chunk, earlier ones too.
+ * fp32.  An infinity or NaN in a live token reaches its own output and, from k, alpha and beta in every column, from v in its
+ * own, later outputs and the state; never an earlier token's.
  * workspace: sdm_gdn_workspace_bytes(shape), 256-byte aligned; calls that overlap must not share it. */
 sdm_status sdm_gdn_forward(const sdm_gdn_shape* shape, const void* q, const void* k, const void* v,
                            const void* alpha, const void* beta, const int32_t* lengths, float* state,
@@ -444,8 +445,8 @@ sdm_status sdm_gdn_step(const sdm_gdn_shape* shape, const void* q, const void* k
  * call of sdm_gdn_forward that started from state0 [B, H, d_k, d_v] float32 (not changed).  The
  * forward is recomputed; nothing of it has to be kept.  dq, dk, dv, dalpha, dbeta: layout and dtype
  * of what they are the gradients of, written (zero past the lengths; dq and dk summed over the value
- * heads that share a key head); dstate0: [B, H, d_k, d_v] float32, or NULL.  Gates may be 0.  Same
- * results on every call. */
+ * heads that share a key head); dstate0: [B, H, d_k, d_v] float32, or NULL.  Gates may be 0.  An infinity or
+ * NaN in a live token may reach every gradient of its sequence.  Same results on every call. */
 sdm_status sdm_gdn_backward(const sdm_gdn_shape* shape, const void* q, const void* k, const void* v,
                             const void* alpha, const void* beta, const int32_t* lengths,
                             const float* state0, const void* dy, const float* dstate, void* dq, void* dk,

@@ -41,6 +41,9 @@ __device__ __forceinline__ int gdn_length(const GdnArgs& a, int b) {
     return n;
 }
 
+__device__ __forceinline__ bool gdn_finite(float x) { return fabsf(x) <= 3.402823466e+38f; }
+__device__ __forceinline__ float gdn_nan() { return __int_as_float(0x7fffffff); }
+
 // Dynamic shared memory above 48 KB has to be allowed once per kernel and device; the call costs about
 // as much as a launch, so it is not repeated.
 template <class K>
@@ -96,7 +99,8 @@ constexpr int GDN_N_PARTS = 3, GDN_SCAN_MATS = GDN_N_PARTS + 2, GDN_BACK_MATS = 
 struct GdnFactors {
     void* mat;                // [B, H, nc, mats, 64, 64] bf16
     int mats;                 // GDN_SCAN_MATS, or for the backward GDN_BACK_MATS
-    float* gates;             // [B, H, nc, 3, 64]: prod_{l <= i} alpha_l, beta_i, prod_{l > i} alpha_l
+    float* gates;             // [B, H, nc, 3, 64]: prod_{l <= i} alpha_l, beta_i, prod_{l > i} alpha_l.  From a chunk's first
+                              // token on whose k, alpha or beta is not finite, the first are not, and N, P and beta are 0
 };
 size_t gdn_factor_mat_bytes(int64_t chunks, int mats);
 size_t gdn_factor_gate_bytes(int64_t chunks);

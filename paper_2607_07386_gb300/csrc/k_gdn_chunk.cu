@@ -50,7 +50,7 @@ struct FactorSmem {
     float be[C];
     unsigned long long bar[2];
     uint32_t tmem;
-    int dead;
+    int dead, first;                          // first: token with a k, alpha or beta that is not finite
 };
 // The K and Q tiles make room for these once the MMAs have read them, P's boxes for N and Z, and all of it for N's boxes.
 struct FactorLate {
@@ -110,6 +110,7 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
 
     if (tid == 0) {
         sm.dead = 0;
+        sm.first = C;
         mbar_init(bar, 1);
         mbar_init(done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -228,7 +229,26 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
         }
     }
     if (!isk) fence_async();
-    __syncthreads();
+    // A token that is not finite must not reach the ones before it by way of zero times infinity: it and the ones
+    // after it are taken out here (the walk makes their outputs and the state NaN).
+    const bool bad = tid < n && !(gdn_finite(lt.Bt[tid & 63][tid & 63]) && gdn_finite(sm.be[tid & 63]) &&      // B's diagonal is k.k
+                                  (reinterpret_cast<const unsigned short*>(sm.al)[tid & 63] & 0x7f80) != 0x7f80);
+    if (__syncthreads_or(bad)) {
+        if (bad) atomicMin(&sm.first, tid);
+        __syncthreads();
+        if (i >= sm.first) {
+            if (isk) {
+                for (int k = 0; k < C; ++k) lt.Bt[k][i] = 0.f;
+                sm.be[i] = 0.f;
+                f.gates[cid * 3 * C + i] = gdn_nan();
+                f.gates[cid * 3 * C + C + i] = 0.f;
+            } else {
+                for (int p = 0; p < 8 * (f.mats - GDN_N_PARTS); ++p) *reinterpret_cast<uint4*>(P + p / 8 * MAT + box_at(i, p % 8)) = make_uint4(0, 0, 0, 0);
+                fence_async();
+            }
+        }
+        __syncthreads();
+    }
     const int row0 = static_cast<int>(cid * f.mats * C);
     if (warp == 2) {                                      // P leaves
         if (elect_one()) {
@@ -371,8 +391,11 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
 //   5  h w K, then w P^T                              (MMA)
 //   6  S = g_63 S + ..                                (registers, bf16 parts to TMEM)
 // Warps 0-7 compute: two share a lane quarter; in steps 2 and 4 each takes 32 tokens, in step 6 half of
-// d_k.  Warps 8-11 add up the outputs of a chunk beside that, in the place of its v, for TMA to store.
-// Warp 12 issues the MMAs, warp 13 the copies.
+// d_k.  Warps 8-11 add up the outputs of a chunk beside that, into a box for TMA to store.
+// Warp 12 issues the MMAs, warp 13 the copies, warps 14 and 15 look for values of v that are not finite.
+//
+// A token with such a value (of k, alpha, beta: all columns, of v: its column) and the ones after it are left out of a chunk's
+// products, where zero times infinity would take it to the ones before it; their outputs and the state after the chunk are NaN.
 //
 // With KEEP (for the backward) nothing is read out: the states before the chunks and e are stored instead, as
 // bf16, transposed as the threads hold them, through boxes in shared memory (16-byte stores of the threads' own,
@@ -384,7 +407,7 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
 constexpr int SW = 8;                          // compute warps
 constexpr int OW = 4;                          // output warps
 constexpr int ST = 32 * (SW + OW + 4);
-constexpr int LAUNCH_REGS = 128, SCAN_REGS = 184, OUT_REGS = 104, IDLE_REGS = 40;   // a thread's registers, at first and after the split
+constexpr int LAUNCH_REGS = 128, SCAN_REGS = 168, OUT_REGS = 120, IDLE_REGS = 56;   // a thread's registers, at first and after the split
 static_assert(SCAN_REGS >= LAUNCH_REGS && OUT_REGS <= LAUNCH_REGS && IDLE_REGS <= LAUNCH_REGS &&
               SW * SCAN_REGS + OW * OUT_REGS + 4 * IDLE_REGS <= (SW + OW + 4) * LAUNCH_REGS, "register split");
 constexpr int NS = 2;                          // bf16 parts of S and of w as the factors of Q and P
@@ -399,17 +422,18 @@ struct ScanTile {
     static constexpr uint32_t KQ = 0, V = 128 * 2 * DK, M = V + C * 256, G = M + MATS * MAT, BYTES = G + 1024;
     static constexpr uint32_t LOAD = KEEP ? 128 * DK + C * 256 + MATS * MAT + GATES : G + GATES;
     static constexpr int STAGES = 2;
-    // KEEP: boxes of 128 columns on their way to memory, S per 64 of d_k, e per part
-    static constexpr uint32_t KS = BYTES * STAGES, KE = KS + 256 * DK, CTL = KEEP ? KE + 32768 : KS;
+    // boxes on their way to memory: y, per 64 columns; KEEP: of 128 columns, S per 64 of d_k, e per part
+    static constexpr uint32_t KS = BYTES * STAGES, KE = KS + 256 * DK, CTL = KEEP ? KE + 32768 : KS + C * 256;
 };
 // Barriers.  Completed by MMAs or copies: a stage's tile; U; Q S; beta r N; h w K; w P.  Completed by warps:
 // operands in TMEM, S and e to be kept in shared memory, Q S taken out, y in shared memory; by the copying
 // thread: the kept ones have left it.
-enum { B_FULL = 0, B_U = 3, B_QS, B_RN, B_HK, B_WP, B_S, B_R, B_H, B_W, B_KS, B_KE, B_TAKEN, B_Y, B_FREE, B_COUNT };
+enum { B_FULL = 0, B_U = 2, B_QS, B_RN, B_HK, B_WP, B_S, B_R, B_H, B_W, B_KS, B_KE, B_TAKEN, B_Y, B_FREE, B_V, B_COUNT = B_V + 2 };
 struct ScanCtl {
     unsigned long long bar[B_COUNT];
     uint32_t tmem;
     int dead;
+    int odd[2][2];                             // of a stage, by each of two warps: a gate product or value of v is not finite
 };
 template <int DK, bool KEEP>
 constexpr size_t scan_smem() { return 1024 + ScanTile<DK, KEEP>::CTL + sizeof(ScanCtl); }
@@ -434,7 +458,7 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
     auto bar = [&](int i) { return bars + 8 * i; };
     if (tid == 0) {
         ctl.dead = 0;
-        for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), i < B_S || i == B_FREE ? 1 : i == B_TAKEN || i == B_Y ? OW : SW);
+        for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), i < B_S || i == B_FREE ? 1 : i >= B_V ? 2 : i == B_TAKEN || i == B_Y ? OW : SW);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         fence_async();
     }
@@ -445,6 +469,21 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
     const uint32_t tmem = ctl.tmem;
     volatile int* dead = &ctl.dead;
     constexpr int SB = DK / 2;                               // TMEM columns of a part of S
+    // Whether chunk c has a token that is not finite (the same for the whole CTA), and the first such of a column's.
+    auto odd_chunk = [&](int c) {
+        const int s = c % L::STAGES;
+        mbar_wait_or_dead(bar(B_V + s), (c / L::STAGES) & 1, dead);
+        return __any_sync(0xffffffffu, (ctl.odd[s][0] | ctl.odd[s][1]) != 0);
+    };
+    auto first_odd = [&](int c, int n, int column) {
+        const unsigned char* const tile = ringp + (c % L::STAGES) * L::BYTES;
+        const float* const gate = reinterpret_cast<const float*>(tile + L::G);
+        const unsigned char* const v = tile + L::V + (column / 64) * 8192;
+        int i = 0;
+#pragma unroll 1
+        while (i < n && gdn_finite(gate[i]) && (*reinterpret_cast<const unsigned short*>(v + sw128_at(i, column % 64)) & 0x7f80) != 0x7f80) ++i;
+        return i;
+    };
 
     if (warp >= SW + OW) {
         regs_dec<IDLE_REGS>();
@@ -548,21 +587,41 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                     if (loaded < chunks) load(loaded++);
                     continue;
                 }
-                mbar_wait_or_dead(bar(B_Y), c & 1, dead);    // y of chunk c lies where its v was
+                mbar_wait_or_dead(bar(B_WP), c & 1, dead);   // the last that reads chunk c's tile
                 if (*dead) break;
-                const uint32_t t = ring + (c % L::STAGES) * L::BYTES + L::V;
-                tma_store_4d(&ty, t, col0, c * C, h, b);
-                if (col0 + 64 < a.dv) tma_store_4d(&ty, t + 8192, col0 + 64, c * C, h, b);
+                if (loaded < chunks) load(loaded++);
+                mbar_wait_or_dead(bar(B_Y), c & 1, dead);
+                if (*dead) break;
+                tma_store_4d(&ty, ring + L::KS, col0, c * C, h, b);
+                if (col0 + 64 < a.dv) tma_store_4d(&ty, ring + L::KS + 8192, col0 + 64, c * C, h, b);
                 bulk_commit();
-                if (loaded < chunks) {
-                    bulk_wait_read();
-                    load(loaded++);
-                }
+                bulk_wait_read();
+                mbar_arrive(bar(B_FREE));
             }
             bulk_wait();
             if (*dead)                                       // the copies in flight land before the CTA ends
                 for (int j = loaded > L::STAGES ? loaded - L::STAGES : 0; j < loaded; ++j)
                     mbar_wait(bar(B_FULL + j % L::STAGES), (j / L::STAGES) & 1);
+        }
+        else if (warp >= SW + OW + 2) {                      // v
+            const int part = warp - (SW + OW + 2);
+            for (int c = 0; c < chunks; ++c) {
+                const int s = c % L::STAGES, n = len - c * C;
+                mbar_wait_or_dead(bar(B_FULL + s), (c / L::STAGES) & 1, dead);
+                unsigned odd = !gdn_finite(reinterpret_cast<const float*>(ringp + s * L::BYTES + L::G)[C - 1]);
+#pragma unroll 4
+                for (int p = part * 32 + lane; p < 16 * C; p += 64) {        // 16-byte pieces: 8 a row of 64 columns
+                    if ((p / 8) % C >= n) continue;
+                    const uint4 w = *reinterpret_cast<const uint4*>(ringp + s * L::BYTES + L::V + p * 16);
+                    odd |= __vcmpeq2(w.x & 0x7f807f80u, 0x7f807f80u) | __vcmpeq2(w.y & 0x7f807f80u, 0x7f807f80u) |
+                           __vcmpeq2(w.z & 0x7f807f80u, 0x7f807f80u) | __vcmpeq2(w.w & 0x7f807f80u, 0x7f807f80u);
+                }
+                const bool any = __any_sync(0xffffffffu, odd != 0);
+                if (lane == 0) {
+                    ctl.odd[s][part] = any;
+                    mbar_arrive(bar(B_V + s));
+                }
+            }
         }
     } else if (warp >= SW) {                                 // outputs: column `row`, all tokens
         regs_dec<OUT_REGS>();
@@ -570,11 +629,12 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         for (int c = 0; !KEEP && c < chunks; ++c) {
             const uint32_t ph = c & 1;
-            unsigned char* tile = ringp + (c % L::STAGES) * L::BYTES;
-            const float* gate = reinterpret_cast<const float*>(tile + L::G);
-            unsigned char* vt = tile + L::V + (row / 64) * 8192;
-            const int n = len - c * C;
+            const float* gate = reinterpret_cast<const float*>(ringp + (c % L::STAGES) * L::BYTES + L::G);
+            unsigned char* const yt = ringp + L::KS + (row / 64) * 8192;
+            const int n = len - c * C < C ? len - c * C : C;
             mbar_wait_or_dead(bar(B_FULL + c % L::STAGES), (c / L::STAGES) & 1, dead);
+            const bool odd = odd_chunk(c);
+            const int m = odd ? first_odd(c, n, row) : n;
             await(bar(B_QS), ph, dead);
             float out[C];
 #pragma unroll
@@ -582,25 +642,26 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 float v[32];
                 tmem_ld32(lanes + X_COL + 64 + 32 * e, v);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) out[32 * e + j] = v[j];
+                for (int j = 0; j < 32; j += 4) {
+                    const float4 g = *reinterpret_cast<const float4*>(gate + 32 * e + j);
+                    out[32 * e + j] = g.x * v[j]; out[32 * e + j + 1] = g.y * v[j + 1];
+                    out[32 * e + j + 2] = g.z * v[j + 2]; out[32 * e + j + 3] = g.w * v[j + 3];
+                }
             }
-            announce(bar(B_TAKEN), lane);
+            announce(bar(B_TAKEN), lane);                    // and nothing of the tile is read from here on
+            if (odd || n < C) {
 #pragma unroll
-            for (int j = 0; j < C; j += 4) {
-                const float4 g = *reinterpret_cast<const float4*>(gate + j);
-                out[j] *= g.x; out[j + 1] *= g.y; out[j + 2] *= g.z; out[j + 3] *= g.w;
+                for (int j = 0; j < C; ++j) out[j] = j < m ? out[j] : j < n ? gdn_nan() : 0.f;
             }
+            if (c > 0) mbar_wait_or_dead(bar(B_FREE), (c - 1) & 1, dead);
             await(bar(B_WP), ph, dead);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 float v[32];
                 tmem_ld32(lanes + Y_COL + 32 * e, v);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const int i = 32 * e + j;
-                    *reinterpret_cast<__nv_bfloat16*>(vt + sw128_at(i, row % 64)) =
-                        __float2bfloat16_rn(i < n ? a.scale * (out[i] + v[j]) : 0.f);
-                }
+                for (int j = 0; j < 32; ++j)
+                    *reinterpret_cast<__nv_bfloat16*>(yt + sw128_at(32 * e + j, row % 64)) = __float2bfloat16_rn(a.scale * (out[32 * e + j] + v[j]));
             }
             fence_async();
             announce(bar(B_Y), lane);
@@ -664,8 +725,10 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
             const uint32_t ph = c & 1;
             const unsigned char* tile = ringp + s * L::BYTES;
             const float* gate = reinterpret_cast<const float*>(tile + L::G);
-            const int n = len - c * C;                       // live tokens (64 or more: all)
             mbar_wait_or_dead(bar(B_FULL + s), (c / L::STAGES) & 1, dead);
+            const int n = len - c * C < C ? len - c * C : C;
+            const bool odd = odd_chunk(c);
+            const int m = odd ? first_odd(c, n, row) : n;    // tokens that the products take
             float u[32], w[32];                              // r; then w (with KEEP: e)
             uint32_t v[16];                                  // this column's v, two tokens in a word
 #pragma unroll
@@ -684,9 +747,9 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 u[j + 2] = __uint_as_float(v[j / 2 + 1] << 16) - g.z * u[j + 2];
                 u[j + 3] = __uint_as_float(v[j / 2 + 1] & 0xffff0000u) - g.w * u[j + 3];
             }
-            if (n < C) {
+            if (odd || n < C) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) u[j] = i0 + j < n ? u[j] : 0.f;
+                for (int j = 0; j < 32; ++j) u[j] = i0 + j < m ? u[j] : 0.f;
             }
 #pragma unroll
             for (int j = 0; j < 32; ++j) w[j] = be[j] * u[j];
@@ -714,6 +777,13 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                         w[j + e] = bj[e] * (w[j + e] + u[j + e]);
                         u[j + e] = hj[e] * w[j + e];
                     }
+                }
+            }
+            if (odd && m < n) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    if (i0 + j >= m) u[j] = gdn_nan();
+                    if (KEEP && i0 + j >= m && i0 + j < n) w[j] = gdn_nan();
                 }
             }
             put_part(lanes + S_COL + i0 / 2, u);

@@ -100,7 +100,8 @@ struct Boxed {
 
 // ------------------------------------------------------------------------------------------
 // Factors of a chunk: 128 threads; threads 0-63 take k.k, 64-127 q.k, 4 x 4 each.  N by a column per lane of the
-// first warp: N_ic = -(B_ic + sum_{c < k < i} B_ik beta_k N_kc).
+// first warp: N_ic = -(B_ic + sum_{c < k < i} B_ik beta_k N_kc).  From a token on whose k, alpha or beta is not finite, B, P
+// and beta are zero and the gate products g are not finite, so that no zero times infinity takes it to the tokens before it.
 // ------------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(FT) k_gdn_factors32(const GdnArgs a, float* __restrict__ out, int transposed) {
     extern __shared__ __align__(16) float sm[];
@@ -128,6 +129,9 @@ __global__ void __launch_bounds__(FT) k_gdn_factors32(const GdnArgs a, float* __
     }
     __syncthreads();
     float* const f = out + (chain * gridDim.x + ch) * FACT;
+    __shared__ int first;
+    if (tid == 0) first = C;
+    bool bad = tid < C && !(gdn_finite(al[tid]) && gdn_finite(al[C + tid]));
     const bool isq = tid >= 64;
     const int i0 = 4 * ((tid & 63) >> 3), j0 = 4 * (tid & 7);          // rows and columns of this thread's tile
     {
@@ -143,15 +147,15 @@ __global__ void __launch_bounds__(FT) k_gdn_factors32(const GdnArgs a, float* __
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int i = i0 + r;
-            float G[4];                        // prod_{j < l <= i}, 0 above the diagonal
+            float G[4];                        // prod_{j < l <= i} times the product; 0 above the diagonal
 #pragma unroll
             for (int c = 3; c >= 0; --c) {
                 const int j = j0 + c;
-                G[c] = j <= i ? p[r] : 0.f;
+                G[c] = j <= i ? p[r] * acc[r][c] : 0.f;
+                if (j == i && !isq) bad = bad || !gdn_finite(acc[r][c]);      // k.k
                 if (j <= i) p[r] *= al[j];
             }
-            float4 v;
-            v.x = G[0] * acc[r][0]; v.y = G[1] * acc[r][1]; v.z = G[2] * acc[r][2]; v.w = G[3] * acc[r][3];
+            const float4 v = make_float4(G[0], G[1], G[2], G[3]);
             if (!isq) {
                 B[(j0 + 0) * CP + i] = v.x; B[(j0 + 1) * CP + i] = v.y; B[(j0 + 2) * CP + i] = v.z; B[(j0 + 3) * CP + i] = v.w;
             } else if (!transposed) {
@@ -162,7 +166,20 @@ __global__ void __launch_bounds__(FT) k_gdn_factors32(const GdnArgs a, float* __
             }
         }
     }
-    __syncthreads();
+    if (__syncthreads_or(bad)) {
+        if (bad && tid < C && !(gdn_finite(al[tid]) && gdn_finite(al[C + tid]))) atomicMin(&first, tid);
+        if (tid < C && !gdn_finite(B[tid * CP + tid])) atomicMin(&first, tid);
+        __syncthreads();
+        if (tid < C && tid >= first) {
+            for (int k = 0; k < C; ++k) {
+                B[k * CP + tid] = 0.f;
+                f[C * C + (transposed ? k * C + tid : tid * C + k)] = 0.f;
+            }
+            al[C + tid] = 0.f;
+            if (tid == first) al[tid] = gdn_nan();
+        }
+        __syncthreads();
+    }
     if (tid < C) {
         const int c = tid;
         float z[C];
@@ -202,7 +219,8 @@ __global__ void __launch_bounds__(FT) k_gdn_factors32(const GdnArgs a, float* __
 
 // ------------------------------------------------------------------------------------------
 // The walk.  MODE 0: forward; 1: forward, keeping the states before the chunks and e; 2: reverse.
-// Grid (column blocks of 16, H, B).
+// Grid (column blocks of 16, H, B).  Forward, a token whose k, alpha, beta (all columns) or v (its column) is not finite and
+// the ones after it are left out of the chunk's products; their outputs and the state after the chunk are NaN.
 // ------------------------------------------------------------------------------------------
 struct WalkLayout {                            // bytes
     int nb, ld, Q, F, V, G, stage, S, X, U, W, Y, bytes;
@@ -224,6 +242,13 @@ struct WalkLayout {                            // bytes
 };
 
 __device__ __forceinline__ void bar_walk() { asm volatile("bar.sync 1, %0;\n" ::"n"(NT) : "memory"); }
+// The same; true if any of the threads brings true.
+__device__ __forceinline__ bool bar_walk_or(bool mine) {
+    uint32_t any;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(any) : "r"(static_cast<uint32_t>(mine)), "n"(NT) : "memory");
+    return any != 0;
+}
 
 template <int MODE>
 __global__ void __launch_bounds__(NT + 32) k_gdn_walk(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tq,
@@ -314,7 +339,19 @@ __global__ void __launch_bounds__(NT + 32) k_gdn_walk(const __grid_constant__ CU
             }
             for (int i = tid; i < (C - n) * CW; i += NT) V[n * CW + i] = 0.f;
         }
-        bar_walk();                                            // the tiles are in; the last chunk's S is written
+        bool odd = false;                                      // a value of v is not finite
+        if (MODE != 2)
+            for (int i = tid; i < n * CW; i += NT) odd = odd || !gdn_finite(V[i]);
+        odd = bar_walk_or(odd);                                // the tiles are in; the last chunk's S is written
+        int m2[2] = {n, n};                                    // tokens that the products of this thread's columns take
+        if (MODE != 2 && (odd || !gdn_finite(g[C - 1]))) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                int i = 0;
+                while (i < n && gdn_finite(g[i]) && gdn_finite(V[i * CW + tc + 8 * c])) ++i;
+                m2[c] = i;
+            }
+        }
         if (MODE != 0) save(r.marks + (chain * nc + ch) * per);
         float acc[2][2] = {}, out[2][2] = {};
         if (MODE == 2) {                                       // dy, and scale P^T dy (the upper half of the threads)
@@ -371,7 +408,7 @@ __global__ void __launch_bounds__(NT + 32) k_gdn_walk(const __grid_constant__ CU
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         const int t = 2 * tr + m;
-                        acc[m][c] = t < n ? V[t * CW + tc + 8 * c] - g[t] * acc[m][c] : 0.f;
+                        acc[m][c] = t < m2[c] ? V[t * CW + tc + 8 * c] - g[t] * acc[m][c] : 0.f;
                         U[(tc + 8 * c) * CP + t] = be[t] * acc[m][c];
                     }
             }
@@ -384,9 +421,10 @@ __global__ void __launch_bounds__(NT + 32) k_gdn_walk(const __grid_constant__ CU
                     for (int c = 0; c < 2; ++c) {
                         const int t = 2 * tr + m, col = col0 + tc + 8 * c;
                         const float w = be[t] * acc[m][c];
-                        W[(tc + 8 * c) * CP + t] = hh[t] * w;
+                        const bool gone = t >= m2[c] && t < n;
+                        W[(tc + 8 * c) * CP + t] = gone ? gdn_nan() : hh[t] * w;
                         if (MODE == 0) Y[(tc + 8 * c) * CP + t] = w;
-                        if (MODE == 1 && t < n && col < a.dv) r.rows[(chain * a.T + t0 + t) * a.dv + col] = acc[m][c];
+                        if (MODE == 1 && t < n && col < a.dv) r.rows[(chain * a.T + t0 + t) * a.dv + col] = gone ? gdn_nan() : acc[m][c];
                     }
             }
             bar_walk();
@@ -397,7 +435,7 @@ __global__ void __launch_bounds__(NT + 32) k_gdn_walk(const __grid_constant__ CU
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         const int t = 2 * tr + m, col = col0 + tc + 8 * c;
-                        if (t < n && col < a.dv) y[vb + (t0 + t) * vs + col] = a.scale * fmaf(g[t], acc[m][c], out[m][c]);
+                        if (t < n && col < a.dv) y[vb + (t0 + t) * vs + col] = t < m2[c] ? a.scale * fmaf(g[t], acc[m][c], out[m][c]) : gdn_nan();
                     }
             }
         }

@@ -494,3 +494,40 @@ def test_correlated_keys_gradients(sdm, rho, mu, bmu, dk, dtype):
             assert f <= (100 * 2.0 ** -22 if n == "alpha" else TOL_F32), far
         else:
             assert f <= (1.0 if n != "alpha" else 0.6 if mu == 3 else 1.5) * 2.0 ** -8, far
+
+
+# ------------------------------------------------------------------ values that are not finite in a live token
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("c", [
+    case(B=2, H=4, Hk=2, T=200, dk=128, dv=136), case(B=2, H=2, Hk=2, T=130, dk=40, dv=64, layout="token_major"),      # chunks of 64
+    case(B=2, H=2, Hk=1, T=100, dk=64, dv=40, dtype="f32"),                                                             # chunks of 32
+    case(B=2, H=2, Hk=2, T=20, dk=64, dv=64), case(B=1, H=2, Hk=2, T=100, dk=136, dv=64),                               # tokens
+    case(B=4, H=16, Hk=16, T=70, dk=16, dv=96, dtype="f32")], ids=_id)
+def test_nothing_reaches_earlier_tokens(sdm, c, value):
+    """The outputs before the token are those without it, bit for bit, and so are those of other sequences, heads and (for v)
+    columns; from it on they are not finite, nor is the state, but for q, which only its own output takes."""
+    import torch
+    x, _ = _prepared(c, 30)
+    clean, S = _run_forward(sdm, x, c)
+    tokens = (lambda t: t.transpose(1, 2)) if c["layout"] == "token_major" else (lambda t: t)      # -> [B, heads, T, ...]
+    group = c["H"] // c["Hk"]
+    mine = (torch.arange(c["H"], device="cuda") // group == 0)[None, :, None, None] & (torch.arange(c["B"], device="cuda") == c["B"] - 1)[:, None, None, None]
+    for at in (0, 5, c["T"] // 2 + 3, c["T"] - 1):
+        for n in ("q", "k", "v", "alpha", "beta"):
+            z = {m: t.clone() for m, t in x.items()}
+            if n in ("alpha", "beta"):
+                z[n][c["B"] - 1, :group, at] = value
+            elif n == "v":
+                tokens(z[n])[c["B"] - 1, :group, at, 3] = value
+            else:
+                tokens(z[n])[c["B"] - 1, 0, at, 3] = value
+            y, T = _run_forward(sdm, z, c)
+            t = torch.arange(c["T"], device="cuda")[None, None, :, None]
+            hit = mine & (t == at if n == "q" else t >= at)
+            hit = (hit & (torch.arange(c["dv"], device="cuda") == 3)) if n == "v" else hit.expand(tokens(y).shape)
+            left = (mine & (torch.arange(c["dv"], device="cuda") == 3)).expand(S.shape) if n == "v" else (mine & (n != "q")).expand(S.shape)
+            assert not torch.isfinite(tokens(y)[hit]).any(), (n, at)
+            assert torch.equal(tokens(y)[~hit], tokens(clean)[~hit]), (n, at)
+            assert not torch.isfinite(T[left]).any() and torch.equal(T[~left], S[~left]), (n, at)
+    assert sdm.device_status() == 0
