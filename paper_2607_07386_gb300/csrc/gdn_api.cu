@@ -65,6 +65,9 @@ sdm_status check_ws(const char* who, const void* ws, size_t have, size_t need) {
 }
 
 sdm_status done(cudaError_t e, const char* who) {
+    if (e == cudaErrorInvalidConfiguration)
+        return fail(SDM_ERR_CUDA, "%s: %s (%s): a launch is out of range, or a kernel was compiled to another number of registers than the split "
+                    "among its warps needs", who, cudaGetErrorString(e), cudaGetErrorName(e));
     if (e != cudaSuccess) return fail(SDM_ERR_CUDA, "%s: %s (%s)", who, cudaGetErrorString(e), cudaGetErrorName(e));
     return sdm::api_ok();
 }

@@ -59,6 +59,28 @@ inline cudaError_t allow_smem(K kernel, size_t bytes, std::atomic<unsigned long 
     return e;
 }
 
+// A kernel that splits its registers among its warps takes them out of what the CTA is launched with, so that has to be
+// `want` a thread.  `get(int*)` asks for the count once; only an answer is kept, a failure is not.
+template <class Get>
+inline cudaError_t check_registers(int want, std::atomic<int>& known, Get get) {
+    int n = known.load(std::memory_order_acquire);
+    if (n == 0) {
+        const cudaError_t e = get(&n);
+        if (e != cudaSuccess) return e;
+        known.store(n, std::memory_order_release);
+    }
+    return n == want ? cudaSuccess : cudaErrorInvalidConfiguration;
+}
+template <class K>
+inline cudaError_t check_kernel_registers(K kernel, int want, std::atomic<int>& known) {
+    return check_registers(want, known, [kernel](int* n) {
+        cudaFuncAttributes at;
+        const cudaError_t e = cudaFuncGetAttributes(&at, kernel);
+        if (e == cudaSuccess) *n = at.numRegs;
+        return e;
+    });
+}
+
 // ---- token recurrence (k_gdn_recur.cu) ----
 struct GdnRecur {
     GdnArgs a;

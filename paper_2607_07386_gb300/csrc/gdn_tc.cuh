@@ -4,9 +4,6 @@
 #include "gdn_internal.h"
 #include "tc_common.cuh"
 
-#include <cuda.h>
-#include <cudaTypedefs.h>
-
 namespace sdm {
 namespace gdn {
 
@@ -16,21 +13,9 @@ constexpr int C = GDN_C64;
 constexpr uint32_t MAT = C * C * 2;          // bytes of one [64][64] bf16 matrix
 constexpr uint32_t GATES = 3 * C * 4;
 
-inline PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
-    static PFN_cuTensorMapEncodeTiled_v12000 fn = []() -> PFN_cuTensorMapEncodeTiled_v12000 {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-        return nullptr;
-    }();
-    return fn;
-}
-
 // [B, heads, T, d] or [B, T, heads, d] bf16 as {d, T, heads, B}, boxes of 64 values x 64 tokens.
 inline bool token_map(CUtensorMap* m, const void* base, int token_major, int B, int heads, int T, int d) {
-    PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
+    PFN_cuTensorMapEncodeTiled_v12000 enc = map_encoder();
     if (!enc) return false;
     const cuuint64_t row = static_cast<cuuint64_t>(d) * 2, uT = T, uH = heads;
     cuuint64_t dim[4] = {static_cast<cuuint64_t>(d), uT, uH, static_cast<cuuint64_t>(B)};
@@ -42,7 +27,7 @@ inline bool token_map(CUtensorMap* m, const void* base, int token_major, int B, 
 }
 // Row-major [rows][cols] bf16, boxes of 64 values x box_rows.
 inline bool row_map(CUtensorMap* m, const void* base, int64_t rows, int cols, int box_rows) {
-    PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
+    PFN_cuTensorMapEncodeTiled_v12000 enc = map_encoder();
     if (!enc) return false;
     cuuint64_t dim[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
     cuuint64_t str[1] = {static_cast<cuuint64_t>(cols) * 2};

@@ -415,14 +415,11 @@ template <int DK>
 cudaError_t back(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap& ty, const CUtensorMap& tdv, const CUtensorMap& tm,
                  const CUtensorMap& tD, const CUtensorMap& td, const CUtensorMap& te, const GdnBack& r, const GdnFactors& f, cudaStream_t stream) {
     constexpr size_t smem = back_smem<DK>();
-    // the compute warpgroups' registers come out of what the CTA is launched with
-    static const int regs = [] {
-        cudaFuncAttributes at;
-        return cudaFuncGetAttributes(&at, k_gdn_back<DK>) == cudaSuccess ? at.numRegs : 0;
-    }();
-    if (regs != LAUNCH_REGS) return cudaErrorInvalidConfiguration;
+    static std::atomic<int> regs{0};
+    cudaError_t e = check_kernel_registers(k_gdn_back<DK>, LAUNCH_REGS, regs);
+    if (e != cudaSuccess) return e;
     static std::atomic<unsigned long long> seen;
-    cudaError_t e = allow_smem(k_gdn_back<DK>, smem, seen);
+    e = allow_smem(k_gdn_back<DK>, smem, seen);
     if (e != cudaSuccess) return e;
     k_gdn_back<DK><<<dim3((r.a.dv + 127) / 128, r.a.H, r.a.B), ST, smem, stream>>>(tk, tq, ty, tdv, tm, tD, td, te, r, f, (r.a.T + C - 1) / C);
     return cudaGetLastError();

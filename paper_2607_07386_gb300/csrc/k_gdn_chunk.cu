@@ -836,14 +836,11 @@ template <int DK, bool KEEP>
 cudaError_t scan(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap& tv, const CUtensorMap& ty, const CUtensorMap& tm, const GdnScan& s,
                  const GdnFactors& f, cudaStream_t stream) {
     constexpr size_t smem = scan_smem<DK, KEEP>();
-    // the compute warpgroups' registers come out of what the CTA is launched with
-    static const int regs = [] {
-        cudaFuncAttributes at;
-        return cudaFuncGetAttributes(&at, k_gdn_scan<DK, KEEP>) == cudaSuccess ? at.numRegs : 0;
-    }();
-    if (regs != LAUNCH_REGS) return cudaErrorInvalidConfiguration;
+    static std::atomic<int> regs{0};
+    cudaError_t e = check_kernel_registers(k_gdn_scan<DK, KEEP>, LAUNCH_REGS, regs);
+    if (e != cudaSuccess) return e;
     static std::atomic<unsigned long long> seen;
-    cudaError_t e = allow_smem(k_gdn_scan<DK, KEEP>, smem, seen);
+    e = allow_smem(k_gdn_scan<DK, KEEP>, smem, seen);
     if (e != cudaSuccess) return e;
     k_gdn_scan<DK, KEEP><<<dim3((s.a.dv + 127) / 128, s.a.H, s.a.B), ST, smem, stream>>>(tk, tq, tv, ty, tm, s, f, (s.a.T + C - 1) / C);
     return cudaGetLastError();

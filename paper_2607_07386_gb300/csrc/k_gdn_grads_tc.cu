@@ -556,14 +556,11 @@ cudaError_t grads(const GdnGradsTc& r, cudaStream_t stream) {
         !token_map(&tdk, r.dk, a.token_major, a.B, a.Hk, a.T, a.dk))
         return cudaErrorInvalidValue;
     constexpr size_t smem = grads_smem<DK>();
-    // the compute warpgroups' registers come out of what the CTA is launched with
-    static const int regs = [] {
-        cudaFuncAttributes at;
-        return cudaFuncGetAttributes(&at, k_gdn_grads_tc<DK>) == cudaSuccess ? at.numRegs : 0;
-    }();
-    if (regs != LAUNCH_REGS) return cudaErrorInvalidConfiguration;
+    static std::atomic<int> regs{0};
+    cudaError_t e = check_kernel_registers(k_gdn_grads_tc<DK>, LAUNCH_REGS, regs);
+    if (e != cudaSuccess) return e;
     static std::atomic<unsigned long long> seen;
-    cudaError_t e = allow_smem(k_gdn_grads_tc<DK>, smem, seen);
+    e = allow_smem(k_gdn_grads_tc<DK>, smem, seen);
     if (e != cudaSuccess) return e;
     k_gdn_grads_tc<DK><<<static_cast<unsigned>(items < 152 ? items : 152), NT, smem, stream>>>(tq, tk, ty, tS, tD, te, td, tdq, tdk, r, nc);
     return cudaGetLastError();

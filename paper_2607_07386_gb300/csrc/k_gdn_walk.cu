@@ -516,7 +516,7 @@ __global__ void __launch_bounds__(NT + 32) k_gdn_walk(const __grid_constant__ CU
 
 // [B, heads, T, d] or [B, T, heads, d] float32 as {d, T, heads, B}, boxes of `cols` values x 32 tokens.
 bool float_map(CUtensorMap* m, const void* base, int token_major, int B, int heads, int T, int d, int cols) {
-    PFN_cuTensorMapEncodeTiled_v12000 enc = gdn::encode_fn();
+    PFN_cuTensorMapEncodeTiled_v12000 enc = map_encoder();
     if (!enc) return false;
     const cuuint64_t row = static_cast<cuuint64_t>(d) * 4, uT = T, uH = heads;
     cuuint64_t dim[4] = {static_cast<cuuint64_t>(d), uT, uH, static_cast<cuuint64_t>(B)};

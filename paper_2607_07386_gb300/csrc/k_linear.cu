@@ -21,10 +21,6 @@
 #include "gdn_internal.h"
 #include "tc_common.cuh"
 
-#include <cuda.h>
-#include <cudaTypedefs.h>
-#include <mutex>
-
 namespace sdm {
 
 namespace {
@@ -40,21 +36,9 @@ __host__ __device__ constexpr int stages_of(int bn) { return bn == 256 ? 4 : 6; 
 __host__ __device__ constexpr uint32_t stage_bytes(int bn) { return (BM + bn) * 128u; }
 __host__ __device__ constexpr uint32_t smem_bytes(int bn) { return 1024u + stage_bytes(bn) * stages_of(bn) + 256u + EPI_WARPS * 512u; }
 
-PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
-    static PFN_cuTensorMapEncodeTiled_v12000 fn = []() -> PFN_cuTensorMapEncodeTiled_v12000 {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-        return nullptr;
-    }();
-    return fn;
-}
-
 // Row-major [rows, cols] bf16, box {64 columns, box_rows}, 128-byte swizzle.
 bool make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int box_rows) {
-    PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
+    PFN_cuTensorMapEncodeTiled_v12000 enc = map_encoder();
     if (!enc) return false;
     cuuint64_t dim[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
     cuuint64_t str[1] = {static_cast<cuuint64_t>(cols) * 2};

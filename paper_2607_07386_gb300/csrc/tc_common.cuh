@@ -3,6 +3,9 @@
 #pragma once
 #include <cstdint>
 #include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include <atomic>
 
 namespace sdm {
 namespace tc {
@@ -186,6 +189,21 @@ __device__ __forceinline__ uint32_t split2(float a, float b, float& ra, float& r
     ra = a - __uint_as_float(u << 16);
     rb = b - __uint_as_float(u & 0xffff0000u);
     return u;
+}
+
+// The driver's encoder of tensor maps, or nullptr; asked for until it is there.
+inline PFN_cuTensorMapEncodeTiled_v12000 map_encoder() {
+    static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> known{nullptr};
+    PFN_cuTensorMapEncodeTiled_v12000 fn = known.load(std::memory_order_acquire);
+    if (fn != nullptr) return fn;
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+        return nullptr;
+    fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    known.store(fn, std::memory_order_release);
+    return fn;
 }
 
 }  // namespace tc

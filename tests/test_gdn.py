@@ -531,3 +531,30 @@ def test_nothing_reaches_earlier_tokens(sdm, c, value):
             assert torch.equal(tokens(y)[~hit], tokens(clean)[~hit]), (n, at)
             assert not torch.isfinite(T[left]).any() and torch.equal(T[~left], S[~left]), (n, at)
     assert sdm.device_status() == 0
+
+
+def test_a_failed_query_is_not_remembered(tmp_path):
+    """The register counts of the kernels that split them: asked for again after a failure, once after an answer."""
+    import subprocess
+    from paper_2607_07386_gb300 import build as B
+    try:
+        nvcc = B.nvcc()
+    except RuntimeError:
+        pytest.skip("nvcc not available")
+    src = tmp_path / "query.cu"
+    src.write_text("""#include "gdn_internal.h"
+int main() {
+    std::atomic<int> known{0};
+    int asked = 0;
+    cudaError_t answer = cudaErrorInitializationError;
+    auto get = [&](int* n) { ++asked; if (answer == cudaSuccess) *n = 128; return answer; };
+    if (sdm::check_registers(128, known, get) != cudaErrorInitializationError) return 1;
+    answer = cudaSuccess;
+    if (sdm::check_registers(128, known, get) != cudaSuccess || asked != 2) return 2;
+    if (sdm::check_registers(128, known, get) != cudaSuccess || asked != 2) return 3;
+    return sdm::check_registers(168, known, get) == cudaErrorInvalidConfiguration ? 0 : 4;
+}
+""")
+    exe = tmp_path / "query"
+    subprocess.run([nvcc, "-std=c++17", "-I", B.INCLUDE, "-I", B.CSRC, str(src), "-o", str(exe)], check=True, capture_output=True)
+    assert subprocess.run([str(exe)]).returncode == 0
