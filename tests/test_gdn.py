@@ -533,6 +533,25 @@ def test_nothing_reaches_earlier_tokens(sdm, c, value):
     assert sdm.device_status() == 0
 
 
+# ------------------------------------------------------------------ the token recurrence and the forms on either side of it
+RECURRENCE = [
+    case(B=5, H=16, Hk=16, T=70, dk=64, dv=64, dtype="f32"), case(B=5, H=16, Hk=8, T=96, dk=24, dv=64, dtype="f32", lengths=[96, 0, 1, 64, 33]),
+    case(B=5, H=16, Hk=16, T=70, dk=136, dv=72, dtype="f32", layout="token_major", lengths=[31, 70, 32, 0, 69]),
+    case(B=5, T=20, dk=64, dv=64, Hk=2, lengths=[20, 0, 1, 16, 17]), case(B=4, T=31, dk=128, dv=40, layout="token_major", lengths=[0, 31, 30, 2]),
+    case(B=5, T=70, dk=136, dv=64, Hk=1, lengths=[70, 0, 1, 32, 65]), case(B=3, T=24, dk=16, dv=64, dtype="f32", lengths=[0, 24, 7]),
+    case(B=4, T=100, dk=256, dv=24, lengths=[100, 0, 64, 33], layout="token_major"),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("c", RECURRENCE, ids=_id)
+def test_token_recurrence(sdm, c):
+    """float32 above the chunked walk's number of CTAs, bf16 below 32 tokens and above d_k = 128, with and without ragged
+    batches whose padding is not finite: outputs, states and gradients."""
+    test_forward_parity(sdm, c)
+    test_backward_parity(sdm, c)
+
+
 def test_a_failed_query_is_not_remembered(tmp_path):
     """The register counts of the kernels that split them: asked for again after a failure, once after an answer."""
     import subprocess
