@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
 //   6  S = g_63 S + ..                                (registers, bf16 parts to TMEM)
 // Warps 0-7 compute: two share a lane quarter; in steps 2 and 4 each takes 32 tokens, in step 6 half of
 // d_k.  Warps 8-11 add up the outputs of a chunk beside that, into a box for TMA to store.
-// Warp 12 issues the MMAs, warp 13 the copies, warps 14 and 15 look for values of v that are not finite.
+// Warp 12 issues the MMAs, warp 13 the copies.
 //
 // A token with such a value (of k, alpha, beta: all columns, of v: its column) and the ones after it are left out of a chunk's
 // products, where zero times infinity would take it to the ones before it; their outputs and the state after the chunk are NaN.
@@ -428,12 +428,12 @@ struct ScanTile {
 // Barriers.  Completed by MMAs or copies: a stage's tile; U; Q S; beta r N; h w K; w P.  Completed by warps:
 // operands in TMEM, S and e to be kept in shared memory, Q S taken out, y in shared memory; by the copying
 // thread: the kept ones have left it.
-enum { B_FULL = 0, B_U = 2, B_QS, B_RN, B_HK, B_WP, B_S, B_R, B_H, B_W, B_KS, B_KE, B_TAKEN, B_Y, B_FREE, B_V, B_COUNT = B_V + 2 };
+enum { B_FULL = 0, B_U = 2, B_QS, B_RN, B_HK, B_WP, B_S, B_R, B_H, B_W, B_KS, B_KE, B_TAKEN, B_Y, B_FREE, B_COUNT };
 struct ScanCtl {
     unsigned long long bar[B_COUNT];
     uint32_t tmem;
     int dead;
-    int odd[2][2];                             // of a stage, by each of two warps: a gate product or value of v is not finite
+    int odd[2];                                // of a stage: the last chunk in it with a value of v that is not finite
 };
 template <int DK, bool KEEP>
 constexpr size_t scan_smem() { return 1024 + ScanTile<DK, KEEP>::CTL + sizeof(ScanCtl); }
@@ -458,7 +458,8 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
     auto bar = [&](int i) { return bars + 8 * i; };
     if (tid == 0) {
         ctl.dead = 0;
-        for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), i < B_S || i == B_FREE ? 1 : i >= B_V ? 2 : i == B_TAKEN || i == B_Y ? OW : SW);
+        ctl.odd[0] = ctl.odd[1] = -1;
+        for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), i < B_S || i == B_FREE ? 1 : i == B_TAKEN || i == B_Y ? OW : SW);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         fence_async();
     }
@@ -469,17 +470,12 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
     const uint32_t tmem = ctl.tmem;
     volatile int* dead = &ctl.dead;
     constexpr int SB = DK / 2;                               // TMEM columns of a part of S
-    // Whether chunk c has a token that is not finite (the same for the whole CTA), and the first such of a column's.
-    auto odd_chunk = [&](int c) {
-        const int s = c % L::STAGES;
-        mbar_wait_or_dead(bar(B_V + s), (c / L::STAGES) & 1, dead);
-        return __any_sync(0xffffffffu, (ctl.odd[s][0] | ctl.odd[s][1]) != 0);
-    };
-    auto first_odd = [&](int c, int n, int column) {
+    // The first of the chunk's tokens from `from` on that is not finite, in a column of v or for all.
+    auto first_odd = [&](int c, int from, int n, int column) {
         const unsigned char* const tile = ringp + (c % L::STAGES) * L::BYTES;
         const float* const gate = reinterpret_cast<const float*>(tile + L::G);
         const unsigned char* const v = tile + L::V + (column / 64) * 8192;
-        int i = 0;
+        int i = from;
 #pragma unroll 1
         while (i < n && gdn_finite(gate[i]) && (*reinterpret_cast<const unsigned short*>(v + sw128_at(i, column % 64)) & 0x7f80) != 0x7f80) ++i;
         return i;
@@ -603,26 +599,6 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                 for (int j = loaded > L::STAGES ? loaded - L::STAGES : 0; j < loaded; ++j)
                     mbar_wait(bar(B_FULL + j % L::STAGES), (j / L::STAGES) & 1);
         }
-        else if (warp >= SW + OW + 2) {                      // v
-            const int part = warp - (SW + OW + 2);
-            for (int c = 0; c < chunks; ++c) {
-                const int s = c % L::STAGES, n = len - c * C;
-                mbar_wait_or_dead(bar(B_FULL + s), (c / L::STAGES) & 1, dead);
-                unsigned odd = !gdn_finite(reinterpret_cast<const float*>(ringp + s * L::BYTES + L::G)[C - 1]);
-#pragma unroll 4
-                for (int p = part * 32 + lane; p < 16 * C; p += 64) {        // 16-byte pieces: 8 a row of 64 columns
-                    if ((p / 8) % C >= n) continue;
-                    const uint4 w = *reinterpret_cast<const uint4*>(ringp + s * L::BYTES + L::V + p * 16);
-                    odd |= __vcmpeq2(w.x & 0x7f807f80u, 0x7f807f80u) | __vcmpeq2(w.y & 0x7f807f80u, 0x7f807f80u) |
-                           __vcmpeq2(w.z & 0x7f807f80u, 0x7f807f80u) | __vcmpeq2(w.w & 0x7f807f80u, 0x7f807f80u);
-                }
-                const bool any = __any_sync(0xffffffffu, odd != 0);
-                if (lane == 0) {
-                    ctl.odd[s][part] = any;
-                    mbar_arrive(bar(B_V + s));
-                }
-            }
-        }
     } else if (warp >= SW) {                                 // outputs: column `row`, all tokens
         regs_dec<OUT_REGS>();
         const int quad = warp & 3, row = quad * 32 + lane;
@@ -633,8 +609,6 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
             unsigned char* const yt = ringp + L::KS + (row / 64) * 8192;
             const int n = len - c * C < C ? len - c * C : C;
             mbar_wait_or_dead(bar(B_FULL + c % L::STAGES), (c / L::STAGES) & 1, dead);
-            const bool odd = odd_chunk(c);
-            const int m = odd ? first_odd(c, n, row) : n;
             await(bar(B_QS), ph, dead);
             float out[C];
 #pragma unroll
@@ -648,6 +622,9 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
                     out[32 * e + j + 2] = g.z * v[j + 2]; out[32 * e + j + 3] = g.w * v[j + 3];
                 }
             }
+            mbar_wait_or_dead(bar(B_R), ph, dead);           // the computing warps have seen the chunk's v
+            const bool odd = __any_sync(0xffffffffu, ctl.odd[c % L::STAGES] == c || !gdn_finite(gate[C - 1]));
+            const int m = odd ? first_odd(c, 0, n, row) : n;
             announce(bar(B_TAKEN), lane);                    // and nothing of the tile is read from here on
             if (odd || n < C) {
 #pragma unroll
@@ -727,14 +704,22 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
             const float* gate = reinterpret_cast<const float*>(tile + L::G);
             mbar_wait_or_dead(bar(B_FULL + s), (c / L::STAGES) & 1, dead);
             const int n = len - c * C < C ? len - c * C : C;
-            const bool odd = odd_chunk(c);
-            const int m = odd ? first_odd(c, n, row) : n;    // tokens that the products take
             float u[32], w[32];                              // r; then w (with KEEP: e)
             uint32_t v[16];                                  // this column's v, two tokens in a word
 #pragma unroll
             for (int j = 0; j < 16; ++j)
                 v[j] = *reinterpret_cast<const unsigned short*>(tile + vat + sw128_at(i0 + 2 * j, row % 64)) |
                        (static_cast<uint32_t>(*reinterpret_cast<const unsigned short*>(tile + vat + sw128_at(i0 + 2 * j + 1, row % 64))) << 16);
+            uint32_t odd_v = 0;                              // an exponent of all ones
+#pragma unroll
+            for (int j = 0; j < 16; ++j) odd_v |= __vcmpeq2(v[j] & 0x7f807f80u, 0x7f807f80u);
+            const float g63 = gate[C - 1];
+            const bool odd = __any_sync(0xffffffffu, odd_v != 0 || !gdn_finite(g63));
+            int m = n;                                       // tokens that the products take (of this warp's)
+            if (odd) {
+                m = first_odd(c, i0, n, row);
+                if (m < n && m < i0 + 32) ctl.odd[s] = c;
+            }
             await(bar(B_U), ph, dead);
             tmem_ld32(lanes + X_COL + i0, u);                // step 2
             float be[32];
@@ -757,7 +742,6 @@ __global__ void __launch_bounds__(ST, 1) k_gdn_scan(const __grid_constant__ CUte
             put_part(lanes + R_COL + 32 + i0 / 2, w);
             put_last(lanes + R_COL + 32 * (NP - 1) + i0 / 2, w);
             announce(bar(B_R), lane);
-            const float g63 = gate[C - 1];
             if (!KEEP) await(bar(B_QS), ph, dead);           // S is read: h w may lie there
             await(bar(B_RN), ph, dead);
             tmem_ld32(lanes + X_COL + i0, w);                // step 4
