@@ -424,7 +424,7 @@ size_t sdm_gdn_backward_workspace_bytes(const sdm_gdn_shape* shape);
  * never used (it may be NaN); y is zero there and the state stays.  A length outside [0, T] is
  * clamped and sets bit 0 of the device status word.  With T = 0 nothing is done.  bf16 calls with
  * d_k <= 128 and T >= 32 run in chunks of 64 tokens on the tensor cores (operands that the state
- * depends on are split into bf16 parts, so that the state is off by about 1e-6); float32 calls with
+ * depends on are split into bf16 parts, so that the state is off by about 1e-6, for keys of any correlation); float32 calls with
  * T >= 32 and few sequences and heads in chunks of 32 tokens in fp32; others token by token in
  * fp32.  An infinity or NaN in a live token reaches its own output and, from k, alpha and beta in every column, from v in its
  * own, later outputs and the state; never an earlier token's.

@@ -17,7 +17,9 @@
 // gradients of q, k and the gates.
 // Operands are split as in the forward, into three bf16 parts, and so is P, which D depends on (with two, 1e-5 of D at keys
 // of a cosine of 0.98).
-// The chain of the six stages bounds it: 280 us at B = 8, H = 16, T = 4096, 128 x 128, 8,000 cycles a chunk.
+// The chain of the six stages bounds it: 374 us at B = 8, H = 16, T = 4096, 128 x 128, 10,700 cycles a chunk.  It was 280 with
+// two parts of D, N, P and beta x, 324 with three; the products with e, whose lane sums give the gradients' kernel back
+// 40, are the rest.
 #include "gdn_tc.cuh"
 
 namespace sdm {

@@ -36,11 +36,12 @@ using namespace gdn;
 // operand of the product with Z as it lies in registers.  These 16 x 16 products are too small for tcgen05 (at least 64
 // rows, and a trip through shared memory or TMEM between any two of a chain); they are mma.sync on tf32, each operand as two
 // parts of 11 bits, lower times lower left out: 21 bits.  P and N leave through swizzled boxes and TMA.
-// At B = 8, H = 16, T = 4096, d_k = 128: 88 us (119 with the products in fp32 from shared memory and 16-byte stores by the
-// threads), where q, k, N and P alone take 49 at the copy rate.  Five CTAs an SM issue half of the time and wait for
-// one another's chains the rest; the parts cut off with a mask in place of a conversion gave 10 us, loops kept short for
-// the instruction cache 5.  Halves of 32 in place of block diagonals (a shorter chain, more products) took 6 us more;
-// eliminating whole columns of 64 in registers 2016 unrolled instructions, whose fetching took 11,600 of a CTA's 20,000 cycles.
+// At B = 8, H = 16, T = 4096, d_k = 128: 102 us (107 with the backward's six matrices), where q, k, N and P, 0.6 GB, would
+// take 89 at the copy rate; with three matrices 88 us, and 119 with the products in fp32 from shared memory and 16-byte stores
+// by the threads.  Five CTAs an SM issue half of the time and wait for one another's chains the rest; the parts cut off with a
+// mask in place of a conversion gave 10 us, loops kept short for the instruction cache 5.  Halves of 32 in place of block
+// diagonals (a shorter chain, more products) took 6 us more; eliminating whole columns of 64 in registers 2016 unrolled
+// instructions, whose fetching took 11,600 of a CTA's 20,000 cycles.
 // ------------------------------------------------------------------------------------------
 constexpr int FT = 128;
 constexpr int LP = C + 8;                     // a row; 8 mod 32: the fragments' reads (four rows, eight columns) meet no bank twice
@@ -401,8 +402,10 @@ __global__ void __launch_bounds__(FT, 5) k_gdn_factors(const __grid_constant__ C
 // bf16, transposed as the threads hold them, through boxes in shared memory (16-byte stores of the threads' own,
 // a row of 256 bytes apart, cost 95 us of 310 at the layer shape), and the state stays as it was.
 //
-// The chain of six stages is what bounds it: 5,700 cycles a chunk (200 us at B = 8, H = 16, T = 4096, 128 x 128), of which
-// the MMAs take 2,432, the hand-overs about 700 and the registers (sums and conversions to bf16 parts) the rest.
+// The chain of six stages is what bounds it: 7,100 cycles a chunk (250 us at B = 8, H = 16, T = 4096, 128 x 128), of which
+// the MMAs take 3,200, the hand-overs about 700 and the registers (sums and conversions to bf16 parts) the rest.  With two
+// parts of S, N and beta r and one of P it was 200 us (see the precision above); the look for values that are not finite
+// and y's own box are 10 of the rest.
 // ------------------------------------------------------------------------------------------
 constexpr int SW = 8;                          // compute warps
 constexpr int OW = 4;                          // output warps
@@ -835,9 +838,10 @@ cudaError_t scan(const CUtensorMap& tk, const CUtensorMap& tq, const CUtensorMap
 size_t gdn_factor_mat_bytes(int64_t chunks, int mats) { return static_cast<size_t>(chunks) * mats * MAT; }
 size_t gdn_factor_gate_bytes(int64_t chunks) { return static_cast<size_t>(chunks) * GATES; }
 
-// A chunk costs the same however few tokens it holds.  Forward, H = 16, 128 x 128: 18.9 us for one chunk against 18.8 (31.0)
-// token by token for 32 (63) tokens at B = 2, 29 against 39 for 31 tokens at B = 16; backward, B = 2: 45 us against
-// 81 for 31 tokens.
+// A chunk costs the same however few tokens it holds.  Forward, H = 16, 128 x 128, 32 (63) tokens: 18.8 (18.7) us against
+// 18.7 (30.9) token by token at B = 2, 31 (31) against 39 (70) at B = 16, 93 (99) against 123 (226) at B = 64; backward: 48 (48)
+// against 78 (102) at B = 2, 88 against 184 at B = 16.  Small heads in large batches would do better token by token: 66 (66)
+// against 19 (33) at B = 64 with 32 x 32.
 bool gdn_chunk_supported(int dtype, int dk, int T) { return dtype == SDM_BF16 && dk <= 128 && T >= 32; }
 
 cudaError_t launch_gdn_factors(const GdnArgs& a, const GdnFactors& f, cudaStream_t stream) {

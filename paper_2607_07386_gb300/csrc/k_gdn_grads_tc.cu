@@ -18,9 +18,9 @@
 // products over d_v have d_k as TMEM lanes (S and D are A operands as they lie), <dy, e> the tokens in
 // lanes 0-63 and <d, e> in lanes 64-127, beside q.k and k.k.  Warps 0-7 take the products through registers,
 // warp 8 issues the MMAs, warp 9 the copies, warps 10 and 11 run the sums of dalpha, a column a thread.
-// The tiles of the next (head, block of d_v) load while this one's products are taken.  422 us at B = 8, H = 16, T = 4096,
-// 128 x 128: 14,400 cycles a chunk and head, of which the register stages take 11,000 (144 KB of tiles and 32 KB of
-// Q and K would load in 7,400, the MMAs take 5,000).
+// The tiles of the next (head, block of d_v) load while this one's products are taken.  390 us at B = 8, H = 16, T = 4096,
+// 128 x 128: 13,300 cycles a chunk and head, most of them the register stages (144 KB of tiles and 32 KB of Q and K would load
+// in 7,400, the MMAs take 5,000); a third lane sum, in place of the walk's <D^T k_j, e_j>, cost 35 us more.
 #include "gdn_tc.cuh"
 
 #include <stddef.h>

@@ -9,10 +9,10 @@
 // owns 16 columns of one state, which stay in shared memory, transposed, beside the double-buffered tiles
 // of the chunk.  Every product is a dot product along rows of two shared-memory matrices, a thread a 2 x 2 tile
 // of them (four 16-byte reads per 16 multiply-adds).  Eight warps: four for K's and N's products, four for Q's and P's
-// beside them; four warps with 4 x 2 tiles read less and took 31 us in place of 25 below.
+// beside them; four warps with 4 x 2 tiles read less and took 31 us where these took 25.
 //
 // A chunk is four dependent products in place of 32 dependent tokens: with few sequences and heads the
-// latency of the chain is what counts (one head, T = 256, 64 x 64: 25 us here and 8 us for the factors, 70 us token by
+// latency of the chain is what counts (one head, T = 256, 64 x 64: 26 us here and 8.5 us for the factors, 70 us token by
 // token).  With many, the token recurrence's registers win over these shared-memory reads (see gdn_walk_supported).
 // Two warps on a scheduler and a barrier after each product: that latency bounds it, not the reads.
 #include "gdn_tc.cuh"
@@ -547,8 +547,9 @@ cudaError_t walk(const GdnRecur& r, const float* fact, cudaStream_t stream) {
 
 size_t gdn_walk_bytes(int64_t chunks) { return static_cast<size_t>(chunks) * FACT * 4; }
 
-// Up to two CTAs an SM.  Forward, T = 512, d_k = d_v = 128: 122 us here against 191 of the token recurrence at 256 CTAs,
-// 246 against 195 at 512; with 64 x 64: 88 against 141 at 256, 187 against 148 at 576.
+// Up to two CTAs an SM.  Forward, T = 512, H = 16, factors and walk: with 128 x 128 and 256 CTAs 130 us against 191 of the
+// token recurrence, at 512 CTAs, measured when the walk took 6% less, 246 against 195; with 64 x 64 94 against 140 at 256 CTAs,
+// then 187 against 148 at 576.
 bool gdn_walk_supported(int dtype, int B, int H, int T, int dv) {
     return dtype == SDM_F32 && T >= C && static_cast<int64_t>(B) * H * ((dv + CW - 1) / CW) <= 152 * 2;
 }

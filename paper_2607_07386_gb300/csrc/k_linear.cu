@@ -8,8 +8,9 @@
 // It is persistent and specialised by warp: one thread streams K-blocks of 64 of both operands
 // through a ring of shared memory by TMA, one thread issues the MMAs into one of two TMEM
 // accumulators, eight warps take the other accumulator through the epilogue.  Every wait is bounded.  Bound by the
-// tensor pipe under the power limit: 32768 x 2048 x 2048 with silu, bias and residual takes 178 us alone (1.55
-// PFLOP/s) and 207 us in a row of calls; dx and dW of it 165 and 176 us alone.
+// tensor pipe under the power limit: 32768 x 2048 x 2048 with silu, bias and residual takes 185 us alone (1.49
+// PFLOP/s) and 210 to 214 us in a row of calls; dx and dW of it 173 and 164 us alone.  A K-block of a 128 x 256 tile is
+// 384 rows of loads, which bounds sizes of a few tiles an SM: 1531 x 5448 x 2056 with gelu takes 57 us.
 //
 // Every CTA loads both operands of its tiles itself: operands may lie in another GPU's memory (every rank of a run on
 // several GPUs loads this library), so no load is shared between CTAs.
@@ -50,8 +51,9 @@ bool make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int 
 }
 
 // The normal distribution function and, in `pdf`, its density times sqrt(2 pi): Abramowitz and Stegun 7.1.26 on
-// x = |z| / sqrt(2), off by at most 7.5e-8, from the one exponential that the slope of gelu needs as well
-// (with erff the activation gradient of 8192 x 504 values took 11.6 us, so 9.8).
+// x = |z| / sqrt(2), off by at most 7.5e-8 (and the tail by at most its own 0.4% down to -6, where gelu is 6e-9, by 3%
+// at -12), from the one exponential that the slope of gelu needs as well (with erff the activation gradient of 8192 x 504
+// values took 11.6 us, so 9.8).
 __device__ __forceinline__ float normal_cdf(float z, float& pdf) {
     const float x = fabsf(z) * 0.70710678118654752f;
     pdf = __expf(-0.5f * z * z);
@@ -466,7 +468,10 @@ bool linear_skinny(int64_t M) { return M <= 16; }
 
 // 128 x 256 tiles read least from L2 per product; narrower ones only where fewer than half of the SMs
 // would have a tile.  Then the contraction is split until the tiles cover the SMs, each share
-// keeping at least 4 K-blocks (256 terms).
+// keeping at least 4 K-blocks (256 terms).  Measured at K = 2048: 96 to 128 wide tiles (512 x 6144, 1531 x 2048,
+// 1024 x 4096) 18.7 to 20.7 us, in half the width, twice as many, 24.7 to 24.9; 256 x 6144 in 96 tiles of 128 columns 16.5, in
+// 192 of 64 22.8; 96 wide tiles in two splits 32 to 41.  At 76 wide tiles, which the rule splits in two, half the width
+// would do better (2432 x 1024: 16.4 against 23.1).
 LinearPlan linear_plan(int64_t M, int64_t N, int64_t K) {
     const int64_t tm = (M + BM - 1) / BM, nkb = (K + BK - 1) / BK;
     int bn = 256;
