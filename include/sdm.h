@@ -486,6 +486,118 @@ sdm_status sdm_linear_backward(const sdm_linear_shape* shape, const void* x, con
                                const void* dout, void* dx, void* dW, float* dbias, void* workspace,
                                size_t workspace_bytes, sdm_stream_t stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Linear attention with a decay per head: the recurrence without the delta, which only adds to its
+ * state.  For every sequence b, value head h and token t, with S [d_k, d_v] and lam_h = exp(log_decay_h):
+ *   S = lam_h S + k_t v_t^T;  y_t = scale S^T q_t.
+ * State, layouts and shared key heads as for the gated delta rule.  log_decay: [H] float32, at most 0
+ * (-inf: lam = 0; above 0 the state grows); it is a setting of the model and has no gradient.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+    int32_t B, H, H_k, T;     /* sequences, value heads, key heads (H a multiple of H_k), tokens */
+    int32_t d_k, d_v;         /* at most 256; times the element size multiples of 16 bytes */
+    int32_t dtype;            /* sdm_dtype of q, k, v, y and of their gradients */
+    int32_t layout;           /* SDM_HEAD_MAJOR or SDM_TOKEN_MAJOR, of q, k, v, y and their gradients */
+    float scale;              /* of the read */
+} sdm_dla_shape;
+
+/* Bytes of workspace of sdm_dla_forward / sdm_dla_backward (0 if none is needed; 0 with
+ * sdm_last_error set for an invalid shape). */
+size_t sdm_dla_workspace_bytes(const sdm_dla_shape* shape);
+size_t sdm_dla_backward_workspace_bytes(const sdm_dla_shape* shape);
+
+/* The recurrence over T tokens.  state: [B, H, d_k, d_v] float32, updated in place; y written.
+ * lengths: NULL, or [B] int32 on the device, as in sdm_gdn_forward: what q, k and v hold past a
+ * sequence's length is never used, y is zero there and the state stays; a length outside [0, T] is
+ * clamped and sets bit 0 of the device status word.  With T = 0 nothing is done.  An infinity or NaN in
+ * a live token reaches its own and later outputs and the state; never an earlier token's.
+ * workspace: sdm_dla_workspace_bytes(shape), 256-byte aligned; calls that overlap must not share it. */
+sdm_status sdm_dla_forward(const sdm_dla_shape* shape, const void* q, const void* k, const void* v,
+                           const float* log_decay, const int32_t* lengths, float* state, void* y,
+                           void* workspace, size_t workspace_bytes, sdm_stream_t stream);
+
+/* One token of B sequences (shape->T must be 1) on a cache of n_slots states [n_slots, H, d_k, d_v]
+ * float32, updated in place; slots as in sdm_gdn_step. */
+sdm_status sdm_dla_step(const sdm_dla_shape* shape, const void* q, const void* k, const void* v,
+                        const float* log_decay, const int32_t* slots, int32_t n_slots, float* state, void* y,
+                        sdm_stream_t stream);
+
+/* Gradients of L = sum <dy, y> + <dstate, S_T> (dstate: [B, H, d_k, d_v] float32, or NULL) for the
+ * call of sdm_dla_forward that started from state0 [B, H, d_k, d_v] float32 (not changed); nothing of
+ * the forward has to be kept.  dq, dk, dv: layout and dtype of what they are the gradients of, written
+ * (zero past the lengths; dq and dk summed over the value heads that share a key head); dstate0:
+ * [B, H, d_k, d_v] float32, or NULL.  An infinity or NaN in a live token may reach every gradient of its
+ * sequence.  Same results on every call. */
+sdm_status sdm_dla_backward(const sdm_dla_shape* shape, const void* q, const void* k, const void* v,
+                            const float* log_decay, const int32_t* lengths, const float* state0,
+                            const void* dy, const float* dstate, void* dq, void* dk, void* dv, float* dstate0,
+                            void* workspace, size_t workspace_bytes, sdm_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The norms around a block, with its gate, residual scale and residual, row by row:
+ *   u = gamma_post y / rms(y);  h = x + res_scale gate u;  z = gamma_pre h / rms(h),
+ *   rms(a)^2 = mean(a^2) + eps,
+ * where y is what the block gives, x and h are the residual stream before and after it, and z is what the
+ * next block takes.  Products are element by element; z is the norm of h as stored.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+    int64_t M;                /* rows */
+    int64_t gate_rows;        /* rows that share a row of the gate: 1, or for example the tokens of a sequence */
+    int32_t D;                /* row width, at most 16384; times the element size a multiple of 16 bytes */
+    int32_t dtype;            /* sdm_dtype of x, y, gate, h, z and of their gradients */
+    float eps;
+} sdm_block_norm_shape;
+
+/* x, y, h, z: [M, D]; gate: [ceil(M / gate_rows), D]; res_scale, gamma_post, gamma_pre: [D] float32.
+ * gate, res_scale: NULL for 1.  gamma_post NULL: no norm after the block (u = y).  gamma_pre and z NULL: no norm
+ * before the next.  y NULL (and with it gate, res_scale, gamma_post and h): before the first block, z is the norm of x.
+ * h may be x itself; h and z overlap nothing else. */
+sdm_status sdm_block_norm(const sdm_block_norm_shape* shape, const void* x, const void* y, const void* gate,
+                          const float* res_scale, const float* gamma_post, const float* gamma_pre, void* h, void* z,
+                          sdm_stream_t stream);
+
+/* Bytes of workspace (0 for an empty shape; 0 with sdm_last_error set for an invalid one). */
+size_t sdm_block_norm_backward_workspace_bytes(const sdm_block_norm_shape* shape);
+
+/* Gradients for dz (NULL with gamma_pre) and dh (NULL: zero) [M, D].  h: as the forward stored it (x where y is NULL;
+ * may be NULL without gamma_pre).  dx [M, D] is written, and unless y is NULL dy [M, D]; dgate, dres_scale,
+ * dgamma_post, dgamma_pre: shapes and types of what they are the gradients of, or NULL (not computed).  dx may be dh
+ * itself.  With M = 0 the gradients of the vectors are zero.  Same results on every call.  Calls that overlap must not
+ * share the workspace (256-byte aligned). */
+sdm_status sdm_block_norm_backward(const sdm_block_norm_shape* shape, const void* y, const void* h, const void* gate,
+                                   const float* res_scale, const float* gamma_post, const float* gamma_pre,
+                                   const void* dz, const void* dh, void* dx, void* dy, void* dgate, float* dres_scale,
+                                   float* dgamma_post, float* dgamma_pre, void* workspace, size_t workspace_bytes,
+                                   sdm_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The norm of all gradients of a model at once, and clipping by it:
+ *   norm = sqrt(sum over the tensors of the sum of grad^2);  out = grad min(1, max_norm / norm).
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+    const void* grad;         /* n values of `dtype`, aligned to one of them */
+    void* out;                /* n values of `out_dtype`: grad itself (of the same type), or another buffer */
+    int64_t n;
+    int32_t dtype, out_dtype; /* sdm_dtype */
+} sdm_grad_tensor;
+
+/* Bytes of workspace for a list of n tensors (host memory; 0 if there is no element, or with
+ * sdm_last_error set for an invalid list). */
+size_t sdm_grad_workspace_bytes(int64_t n, const sdm_grad_tensor* tensors);
+
+/* stats: [2] float32 on the device, the norm and the factor min(1, max_norm / norm).  The norm of finite gradients is
+ * right over float32's whole range (squares that do not fit are no loss).  `tensors` is host memory, read during the
+ * call; `out` of the entries is not used.  Same results on every call. */
+sdm_status sdm_grad_norm(int64_t n, const sdm_grad_tensor* tensors, float max_norm, float* stats, void* workspace,
+                         size_t workspace_bytes, sdm_stream_t stream);
+
+/* The same, and out = grad * factor (rounded once to out_dtype).  max_norm: at least 0; infinity scales nothing.
+ * Where a gradient is infinite or NaN (or the norm is above float32's range) the norm says so, the factor is NaN and the
+ * gradients stay as they are (out is a copy): the caller sees it in stats and leaves the step out.  An out may overlap no
+ * grad but its own, if it is that very buffer, and no other out. */
+sdm_status sdm_grad_clip(int64_t n, const sdm_grad_tensor* tensors, float max_norm, float* stats, void* workspace,
+                         size_t workspace_bytes, sdm_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

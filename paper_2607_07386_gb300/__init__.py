@@ -14,4 +14,7 @@ from ._binding import (  # noqa: F401
     RECUR_PLAN_FIELDS, test_scores,
     GdnShape, LinearShape, gdn_workspace_bytes, gdn_backward_workspace_bytes, gdn_forward, gdn_step, gdn_backward,
     linear_workspace_bytes, linear_backward_workspace_bytes, linear, linear_backward,
+    DlaShape, dla_workspace_bytes, dla_backward_workspace_bytes, dla_forward, dla_step, dla_backward,
+    BlockNormShape, block_norm, block_norm_backward_workspace_bytes, block_norm_backward,
+    GradList, grad_workspace_bytes, grad_norm, grad_clip,
 )

@@ -70,6 +70,60 @@ class LinearShape(ctypes.Structure):
         return cls(M, N, K, ACTS[act] if isinstance(act, str) else int(act))
 
 
+class DlaShape(ctypes.Structure):
+    """sdm_dla_shape: linear attention with a decay per head."""
+    _fields_ = GdnShape._fields_
+    make = GdnShape.__dict__["make"]
+
+    def replace(self, **kw) -> "DlaShape":
+        vals = {f: getattr(self, f) for f, _ in self._fields_}
+        vals.update(kw)
+        return DlaShape(**vals)
+
+
+class BlockNormShape(ctypes.Structure):
+    """sdm_block_norm_shape: rows [M, D], a row of the gate for every gate_rows of them."""
+    _fields_ = [("M", ctypes.c_int64), ("gate_rows", ctypes.c_int64), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
+
+    @classmethod
+    def make(cls, M, D, dtype="bf16", gate_rows=1, eps=1e-6) -> "BlockNormShape":
+        dt = {"f32": DTYPE_F32, "bf16": DTYPE_BF16}[dtype] if isinstance(dtype, str) else int(dtype)
+        return cls(M, gate_rows, D, dt, eps)
+
+
+class GradTensor(ctypes.Structure):
+    """sdm_grad_tensor."""
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32)]
+
+
+class GradList:
+    """The gradients of a model for grad_norm and grad_clip, made once and used on every step: the tensors (which it keeps
+    alive) must stay where they are."""
+
+    def __init__(self, entries, tensors):
+        self.array = (GradTensor * len(entries))(*entries)
+        self.n, self.tensors = len(entries), tensors
+
+    @classmethod
+    def make(cls, grads, out=None) -> "GradList":
+        """grads: float32 and bfloat16 tensors; out: where the clipped ones go, float32 or bfloat16 (None: in place)."""
+        import torch
+        types = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+        grads = list(grads)
+        out = grads if out is None else list(out)
+        if len(out) != len(grads):
+            raise ValueError("out must have a tensor for every gradient")
+        for g, o in zip(grads, out):
+            if g.dtype not in types or o.dtype not in types:
+                raise ValueError("gradients must be float32 or bfloat16")
+            if g.shape != o.shape:
+                raise ValueError("a gradient and its output must have the same shape")
+        return cls([GradTensor(_ptr(g), _ptr(o), g.numel(), types[g.dtype], types[o.dtype]) for g, o in zip(grads, out)],
+                   (grads, out))
+
+
 _lib = None
 _lock = threading.Lock()
 _VP, _SZ, _I32P = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p
@@ -161,6 +215,21 @@ def lib():
             L.sdm_gdn_backward.argtypes = [_GSP] + [_VP] * 16 + [_SZ, _VP]
             L.sdm_linear.argtypes = [_LSP] + [_VP] * 7 + [_SZ, _VP]
             L.sdm_linear_backward.argtypes = [_LSP] + [_VP] * 8 + [_SZ, _VP]
+            _DSP, _BSP, _GTP = ctypes.POINTER(DlaShape), ctypes.POINTER(BlockNormShape), ctypes.POINTER(GradTensor)
+            for f, args in (("sdm_dla_workspace_bytes", [_DSP]), ("sdm_dla_backward_workspace_bytes", [_DSP]),
+                            ("sdm_block_norm_backward_workspace_bytes", [_BSP]),
+                            ("sdm_grad_workspace_bytes", [ctypes.c_int64, _GTP])):
+                getattr(L, f).restype = ctypes.c_size_t
+                getattr(L, f).argtypes = args
+            L.sdm_dla_forward.argtypes = [_DSP] + [_VP] * 8 + [_SZ, _VP]
+            L.sdm_dla_step.argtypes = [_DSP] + [_VP] * 5 + [ctypes.c_int32, _VP, _VP, _VP]
+            L.sdm_dla_backward.argtypes = [_DSP] + [_VP] * 13 + [_SZ, _VP]
+            L.sdm_block_norm.argtypes = [_BSP] + [_VP] * 9
+            L.sdm_block_norm_backward.argtypes = [_BSP] + [_VP] * 15 + [_SZ, _VP]
+            L.sdm_grad_norm.argtypes = L.sdm_grad_clip.argtypes = [ctypes.c_int64, _GTP, ctypes.c_float, _VP, _VP, _SZ, _VP]
+            for f in ("sdm_dla_forward", "sdm_dla_step", "sdm_dla_backward", "sdm_block_norm", "sdm_block_norm_backward",
+                      "sdm_grad_norm", "sdm_grad_clip"):
+                getattr(L, f).restype = ctypes.c_int
             for f in ("sdm_gdn_forward", "sdm_gdn_step", "sdm_gdn_backward", "sdm_linear", "sdm_linear_backward"):
                 getattr(L, f).restype = ctypes.c_int
             for f in ("sdm_init_memory", "sdm_forward", "sdm_decode_step", "sdm_address", "sdm_recur",
@@ -521,3 +590,77 @@ def linear_backward(shape: LinearShape, x, W, pre, dout, dx, dW, dbias, workspac
     nb = workspace_nbytes if workspace_nbytes is not None else (_nbytes(workspace) or 0)
     _check(lib().sdm_linear_backward(ctypes.byref(shape), _ptr(x), _ptr(W), _ptr(pre), _ptr(dout), _ptr(dx), _ptr(dW),
                                      _ptr(dbias), _ptr(workspace), nb, _stream(stream)))
+
+
+def dla_workspace_bytes(shape: DlaShape) -> int:
+    return _size(lib().sdm_dla_workspace_bytes, shape)
+
+
+def dla_backward_workspace_bytes(shape: DlaShape) -> int:
+    return _size(lib().sdm_dla_backward_workspace_bytes, shape)
+
+
+def dla_forward(shape: DlaShape, q, k, v, log_decay, state, y, workspace=None, lengths=None, stream=None,
+                workspace_nbytes=None):
+    """sdm_dla_forward: linear attention with a decay per head over T tokens; state (float32) is updated in place."""
+    nb = workspace_nbytes if workspace_nbytes is not None else (_nbytes(workspace) or 0)
+    _check(lib().sdm_dla_forward(ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lengths),
+                                 _ptr(state), _ptr(y), _ptr(workspace), nb, _stream(stream)))
+
+
+def dla_step(shape: DlaShape, q, k, v, log_decay, state, y, slots=None, n_slots=None, stream=None):
+    """sdm_dla_step: one token of B sequences on a cache of states [n_slots, H, d_k, d_v] (n_slots: by default the
+    rows of `state`), slots: the row of each sequence (a negative one skips it)."""
+    n = n_slots if n_slots is not None else (state.shape[0] if hasattr(state, "shape") else shape.B)
+    _check(lib().sdm_dla_step(ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(slots), int(n),
+                              _ptr(state), _ptr(y), _stream(stream)))
+
+
+def dla_backward(shape: DlaShape, q, k, v, log_decay, state0, dy, dstate, dq, dk, dv, dstate0, workspace=None,
+                 lengths=None, stream=None, workspace_nbytes=None):
+    """sdm_dla_backward: gradients of the call of dla_forward that started from state0 (dstate and dstate0, the
+    gradients of the last and the first state, may be None)."""
+    nb = workspace_nbytes if workspace_nbytes is not None else (_nbytes(workspace) or 0)
+    _check(lib().sdm_dla_backward(ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lengths),
+                                  _ptr(state0), _ptr(dy), _ptr(dstate), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dstate0),
+                                  _ptr(workspace), nb, _stream(stream)))
+
+
+def block_norm(shape: BlockNormShape, x, y, h, z, gate=None, res_scale=None, gamma_post=None, gamma_pre=None, stream=None):
+    """sdm_block_norm: h = x + res_scale * gate * (gamma_post * y / rms(y)), z = gamma_pre * h / rms(h)."""
+    _check(lib().sdm_block_norm(ctypes.byref(shape), _ptr(x), _ptr(y), _ptr(gate), _ptr(res_scale), _ptr(gamma_post),
+                                _ptr(gamma_pre), _ptr(h), _ptr(z), _stream(stream)))
+
+
+def block_norm_backward_workspace_bytes(shape: BlockNormShape) -> int:
+    return _size(lib().sdm_block_norm_backward_workspace_bytes, shape)
+
+
+def block_norm_backward(shape: BlockNormShape, y, h, dz, dh, dx, dy, gate=None, res_scale=None, gamma_post=None,
+                        gamma_pre=None, dgate=None, dres_scale=None, dgamma_post=None, dgamma_pre=None, workspace=None,
+                        stream=None, workspace_nbytes=None):
+    """sdm_block_norm_backward: gradients of block_norm for dz and dh, h as the forward stored it."""
+    nb = workspace_nbytes if workspace_nbytes is not None else (_nbytes(workspace) or 0)
+    _check(lib().sdm_block_norm_backward(ctypes.byref(shape), _ptr(y), _ptr(h), _ptr(gate), _ptr(res_scale),
+                                         _ptr(gamma_post), _ptr(gamma_pre), _ptr(dz), _ptr(dh), _ptr(dx), _ptr(dy),
+                                         _ptr(dgate), _ptr(dres_scale), _ptr(dgamma_post), _ptr(dgamma_pre),
+                                         _ptr(workspace), nb, _stream(stream)))
+
+
+def grad_workspace_bytes(grads: GradList) -> int:
+    n = lib().sdm_grad_workspace_bytes(grads.n, grads.array)
+    if n == 0 and last_error():
+        raise SdmError(1, last_error())
+    return n
+
+
+def grad_norm(grads: GradList, max_norm: float, stats, workspace=None, stream=None, workspace_nbytes=None):
+    """sdm_grad_norm: stats [2] float32 = the norm of all gradients and min(1, max_norm / norm)."""
+    nb = workspace_nbytes if workspace_nbytes is not None else (_nbytes(workspace) or 0)
+    _check(lib().sdm_grad_norm(grads.n, grads.array, max_norm, _ptr(stats), _ptr(workspace), nb, _stream(stream)))
+
+
+def grad_clip(grads: GradList, max_norm: float, stats, workspace=None, stream=None, workspace_nbytes=None):
+    """sdm_grad_clip: grad_norm, and every output = its gradient times the factor."""
+    nb = workspace_nbytes if workspace_nbytes is not None else (_nbytes(workspace) or 0)
+    _check(lib().sdm_grad_clip(grads.n, grads.array, max_norm, _ptr(stats), _ptr(workspace), nb, _stream(stream)))

@@ -1,0 +1,101 @@
+// Linear attention with a decay per head: what the C ABI hands to the kernels.
+#pragma once
+#include "gdn_internal.h"
+
+namespace sdm {
+
+constexpr int DLA_C32 = 32;               // tokens per chunk of the fp32 walk
+
+// One walk over the tokens of every (sequence, head): with a state S [da, db] and, for each token in the walk's order,
+// operands r and k [da] and v [db] and an output o [db],
+//   forwards   S = lam S + add k v^T;  o = S-part: inter S^T r, own chunk: intra (r.k_j) lam^(i - j) v_j
+//   backwards  the state is read before the token's own decay and after it only through the token itself.
+// The forward pass is one such walk, the backward pass three:
+//   y: r = q, k = k, v = v;  dq: r = dy, k = v, v = k on S^T;
+//   dv: backwards, r = k, k = q, v = dy on R = dL/dS;  dk: backwards, r = v, k = dy, v = q on R^T.
+struct DlaRole {
+    const void* r; const void* k; const void* v;
+    void* out;
+    int hr, hk, hv;           // heads of r, k and v (H or H_k)
+    int da, db;
+    const float* state_in;    // [slots, H, d_k, d_v], or nullptr (zero)
+    float* state_out;         // or nullptr; may be state_in
+    int transposed;           // da is d_v
+    int reverse;
+    int partial;              // out is float32 [B, H, T, db], a share of a key head's gradient
+    float inter, intra, add;
+};
+struct DlaWalk {
+    int B, H, T, token_major;
+    const float* log_decay;   // [H]
+    const int32_t* lengths;   // [B] or nullptr
+    int* err;
+    int roles;
+    DlaRole role[3];
+    // The tokens may be cut into `segs` pieces of `seg_chunks` chunks that run at once: a first launch copies the first
+    // state and takes what each piece but the last adds to it into seg_state [role][B * H][segs][da * db], the second
+    // starts every piece from their sums.
+    int segs, seg_chunks;
+    float* seg_state;
+    int64_t seg_role[3];      // where a role's sums start, in floats
+};
+
+// lam^n for lam = exp(ld): 1 at n = 0 whatever ld is, 0 for ld = -inf.  The product is taken in two parts.
+__device__ __forceinline__ float dla_pow(float ld, int n) {
+    if (n == 0) return 1.f;
+    const float f = static_cast<float>(n), hi = f * ld, e = expf(hi);
+    if (!gdn_finite(hi)) return e;
+    return fmaf(e, fmaf(f, ld, -hi), e);
+}
+__device__ __forceinline__ int dla_length(const DlaWalk& w, int b) {
+    if (w.lengths == nullptr) return w.T;
+    const int n = __ldg(w.lengths + b);
+    if (n < 0 || n > w.T) {
+        if (threadIdx.x == 0) flag_error(w.err, ERR_BAD_INDEX);
+        return n < 0 ? 0 : w.T;
+    }
+    return n;
+}
+
+// Fills in segs and seg_chunks; runs the walks.
+void dla_plan(int dtype, DlaWalk& w);
+cudaError_t launch_dla(int dtype, const DlaWalk& w, cudaStream_t stream);
+// dq and dk [heads of k] = sums over the `group` value heads of their shares [B, H, T, d] float32.
+cudaError_t launch_dla_join(int dtype, const float* pq, const float* pk, void* dq, void* dk, int B, int Hk, int group, int T, int d, int token_major,
+                            cudaStream_t stream);
+
+struct DlaStep {
+    const void* q; const void* k; const void* v;
+    const float* log_decay;
+    const int32_t* slots;
+    float* state;
+    void* y;
+    int B, H, Hk, dk, dv, n_slots;
+    float scale;
+    int* err;
+};
+cudaError_t launch_dla_step(int dtype, const DlaStep& s, cudaStream_t stream);
+
+// ---- block norm (k_block_norm.cu) ----
+struct BlockNorm {
+    int64_t M, gate_rows;
+    int D;
+    float eps;
+    const void* x; const void* y; const void* gate;                          // forward; backward reads h in place of x
+    const float* res_scale; const float* gamma_post; const float* gamma_pre;
+    void* h; void* z;                                                        // forward
+    const void* dz; const void* dh;                                          // backward
+    void* dx; void* dy; void* dgate;
+    float* dres_scale; float* dgamma_post; float* dgamma_pre;
+    float* ws;
+};
+bool block_norm_supported(int D);
+cudaError_t launch_block_norm(int dtype, const BlockNorm& a, cudaStream_t stream);
+size_t block_norm_backward_bytes(int64_t M, int64_t gate_rows, int D);
+cudaError_t launch_block_norm_backward(int dtype, const BlockNorm& a, cudaStream_t stream);
+
+// ---- gradient norm and clipping (k_grad_clip.cu) ----
+size_t grad_bytes(int64_t n, const sdm_grad_tensor* t);
+cudaError_t launch_grad(int64_t n, const sdm_grad_tensor* t, bool write, float max_norm, float* stats, void* ws, cudaStream_t stream);
+
+}  // namespace sdm

@@ -1,0 +1,414 @@
+// Linear attention with a decay per head, in fp32: the walk in chunks of 32 tokens, and the single token.
+//
+// Within a chunk of n tokens (walked forwards, i and j from 0)
+//   o_i = inter lam^(i+1) S^T r_i + intra sum_{j <= i} lam^(i-j) (r_i.k_j) v_j
+//   S  <- lam^n S + add sum_j lam^(n-1-j) k_j v_j^T
+// and, walked backwards from the last token, o_i takes lam^(n-1-i) S and j >= i, S takes lam^(j+1).  No power of
+// the decay is above 1 for log_decay <= 0, so nothing can overflow however fast a head forgets.
+//
+// A CTA takes 32 columns of one state: the state lies in registers and, for the reads, in shared memory;
+// r, k and v of the next chunk are on their way while this one is computed.
+#include "dla_internal.h"
+#include "sdm_common.cuh"
+
+namespace sdm {
+
+namespace {
+
+constexpr int C = DLA_C32, WT = 256, COLS = 32;
+
+template <int DA>
+struct WalkSmem {
+    float r[C][DA + 4], k[C][DA + 4], v[C][COLS + 4], S[DA][COLS + 4], P[C][C + 1];
+    float pw[C + 1];
+};
+
+template <class D>
+__device__ __forceinline__ const uint4* token_ptr(const void* base, int64_t at) {
+    return reinterpret_cast<const uint4*>(static_cast<const typename D::T*>(base) + at);
+}
+template <class D>
+__device__ __forceinline__ void put_pair(void* out, int64_t at, float a, float b);
+template <> __device__ __forceinline__ void put_pair<F32>(void* out, int64_t at, float a, float b) {
+    *reinterpret_cast<float2*>(static_cast<float*>(out) + at) = make_float2(a, b);
+}
+template <> __device__ __forceinline__ void put_pair<BF16>(void* out, int64_t at, float a, float b) {
+    *reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(out) + at) = __floats2bfloat162_rn(a, b);
+}
+
+template <class D, int DA, bool SUMS>
+__global__ void __launch_bounds__(WT) k_dla_walk(const DlaWalk w, const int3 slices) {
+    extern __shared__ __align__(16) unsigned char raw[];
+    WalkSmem<DA>& sm = *reinterpret_cast<WalkSmem<DA>*>(raw);
+    const int tid = threadIdx.x;
+    const int nseg = SUMS ? w.segs - 1 : w.segs;
+    const int seg = blockIdx.x % nseg;
+    int slice = blockIdx.x / nseg, role = 0;
+    if (slice >= slices.x) {
+        slice -= slices.x;
+        role = 1;
+        if (slice >= slices.y) {
+            slice -= slices.y;
+            role = 2;
+        }
+    }
+    const DlaRole& ro = w.role[role];
+    const int b = blockIdx.z, h = blockIdx.y, col0 = slice * COLS;
+    const int len = dla_length(w, b);
+    const int da = ro.da, db = ro.db;
+    const int64_t chain = static_cast<int64_t>(b) * w.H + h;
+    const float ld = __ldg(w.log_decay + h);
+    const int chunks = (len + C - 1) / C;
+    const int c0 = min(seg * w.seg_chunks, chunks), c1 = seg == w.segs - 1 ? chunks : min(c0 + w.seg_chunks, chunks);
+    auto chunk_at = [&](int c) { return ro.reverse ? chunks - 1 - c : c; };
+    auto tokens_in = [&](int c) { return min(C, len - chunk_at(c) * C); };
+
+    const int hr = h / (w.H / ro.hr), hk = h / (w.H / ro.hk), hv = h / (w.H / ro.hv);
+    const int64_t rb = gdn_base(w.token_major, b, hr, ro.hr, w.T, da), rs = gdn_stride(w.token_major, ro.hr, da);
+    const int64_t kb = gdn_base(w.token_major, b, hk, ro.hk, w.T, da), ks = gdn_stride(w.token_major, ro.hk, da);
+    const int64_t vb = gdn_base(w.token_major, b, hv, ro.hv, w.T, db), vs = gdn_stride(w.token_major, ro.hv, db);
+
+    // pieces of 16 bytes: PR per row of r and k, NR of them a thread
+    constexpr int PR = DA / D::E, NR = C * PR / WT, PV = COLS / D::E;
+    uint4 ru[NR > 0 ? NR : 1], ku[NR > 0 ? NR : 1], vu;
+    auto fetch = [&](int c) {
+        const int t0 = chunk_at(c) * C, n = tokens_in(c);
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int p = tid + i * WT, row = p / PR, x = p % PR * D::E;
+            const bool on = row < n && x < da;
+            if (!SUMS) ru[i] = on ? __ldg(token_ptr<D>(ro.r, rb + (t0 + row) * rs + x)) : make_uint4(0, 0, 0, 0);
+            ku[i] = on ? __ldg(token_ptr<D>(ro.k, kb + (t0 + row) * ks + x)) : make_uint4(0, 0, 0, 0);
+        }
+        const int row = tid / PV, x = col0 + tid % PV * D::E;
+        vu = row < n && x < db ? __ldg(token_ptr<D>(ro.v, vb + (t0 + row) * vs + x)) : make_uint4(0, 0, 0, 0);
+    };
+    auto put = [&]() {
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int p = tid + i * WT, row = p / PR, x = p % PR * D::E;
+            float f[8];
+            if (!SUMS) {
+                unpack16<D>(ru[i], f);
+#pragma unroll
+                for (int e = 0; e < D::E; e += 4) *reinterpret_cast<float4*>(&sm.r[row][x + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+            }
+            unpack16<D>(ku[i], f);
+#pragma unroll
+            for (int e = 0; e < D::E; e += 4) *reinterpret_cast<float4*>(&sm.k[row][x + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+        }
+        const int row = tid / PV, x = tid % PV * D::E;
+        if (row < C) {
+            float f[8];
+            unpack16<D>(vu, f);
+#pragma unroll
+            for (int e = 0; e < D::E; e += 4) *reinterpret_cast<float4*>(&sm.v[row][x + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+        }
+    };
+
+    if (c0 < c1) fetch(c0);
+    if (tid <= C) sm.pw[tid] = dla_pow(ld, tid);
+    // This thread's part of the state: R rows x 4 columns.
+    constexpr int R = DA / 32;
+    const int cg = (tid & 7) * 4, x0 = (tid >> 3) * R;
+    float S[R][4];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[i][e] = 0.f;
+    const int64_t per = static_cast<int64_t>(da) * db;
+    auto at = [&](int x, int c) { return ro.transposed ? static_cast<int64_t>(col0 + c) * da + x : static_cast<int64_t>(x) * db + col0 + c; };
+    // Pieces: [0] is the first state, [s + 1] what segment s adds.
+    float* const pieces = w.seg_state + w.seg_role[role] + chain * w.segs * per;
+    if (SUMS ? seg == 0 : w.segs == 1) {
+        if (ro.state_in != nullptr) {
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (x0 + i < da && col0 + cg + e < db) S[i][e] = ro.state_in[chain * per + at(x0 + i, cg + e)];
+        }
+        if (SUMS) {
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (x0 + i < da && col0 + cg + e < db) pieces[at(x0 + i, cg + e)] = S[i][e];
+                    S[i][e] = 0.f;
+                }
+        }
+    } else if (!SUMS) {
+        const float full = dla_pow(ld, w.seg_chunks * C);
+        for (int s = -1; s < seg; ++s) {
+            const int s0 = min(s * w.seg_chunks, chunks), s1 = min(s0 + w.seg_chunks, chunks);
+            if (s >= 0 && s0 == s1) break;
+            int n = (s1 - s0) * C;                           // the walk's partial chunk is the sequence's last
+            if (ro.reverse ? s0 == 0 : s1 == chunks) n -= chunks * C - len;
+            const float f = s < 0 ? 0.f : n == w.seg_chunks * C ? full : dla_pow(ld, n);
+            const float* add = pieces + (s + 1) * per;
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (x0 + i < da && col0 + cg + e < db) S[i][e] = s < 0 ? add[at(x0 + i, cg + e)] : fmaf(f, S[i][e], add[at(x0 + i, cg + e)]);
+        }
+    }
+
+    const int ti = (tid >> 4) * 2, tc = (tid & 15) * 2;
+    for (int c = c0; c < c1; ++c) {
+        const int t0 = chunk_at(c) * C, n = tokens_in(c);
+        __syncthreads();
+        put();
+        if (!SUMS) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) *reinterpret_cast<float4*>(&sm.S[x0 + i][cg]) = x0 + i < da ? make_float4(S[i][0], S[i][1], S[i][2], S[i][3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        __syncthreads();
+        if (c + 1 < c1) fetch(c + 1);
+        if (!SUMS) {
+            float p[2][2] = {{0.f, 0.f}, {0.f, 0.f}}, o[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+#pragma unroll 4
+            for (int x = 0; x < DA; x += 4) {
+                float r[2][4], k[2][4], s[4][2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float4 a = *reinterpret_cast<const float4*>(&sm.r[ti + i][x]), d = *reinterpret_cast<const float4*>(&sm.k[tc + i][x]);
+                    r[i][0] = a.x; r[i][1] = a.y; r[i][2] = a.z; r[i][3] = a.w;
+                    k[i][0] = d.x; k[i][1] = d.y; k[i][2] = d.z; k[i][3] = d.w;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 f = *reinterpret_cast<const float2*>(&sm.S[x + e][tc]);
+                    s[e][0] = f.x; s[e][1] = f.y;
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            p[i][j] = fmaf(r[i][e], k[j][e], p[i][j]);
+                            o[i][j] = fmaf(r[i][e], s[e][j], o[i][j]);
+                        }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = ti + i;
+                const float f = ro.inter * (ro.reverse ? sm.pw[max(n - 1 - row, 0)] : sm.pw[row + 1]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int far = ro.reverse ? tc + j - row : row - tc - j;
+                    sm.P[row][tc + j] = far >= 0 ? ro.intra * sm.pw[far >= 0 ? far : 0] * p[i][j] : 0.f;
+                    o[i][j] *= f;
+                }
+            }
+            __syncthreads();
+            // a token past this one in the walk is left out by the test, not by a zero: its v may not be finite
+#pragma unroll 4
+            for (int j = 0; j < C; ++j) {
+                const float2 v = *reinterpret_cast<const float2*>(&sm.v[j][tc]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const bool on = ro.reverse ? j >= ti + i : j <= ti + i;
+                    const float q = sm.P[ti + i][j];
+                    if (on) {
+                        o[i][0] = fmaf(q, v.x, o[i][0]);
+                        o[i][1] = fmaf(q, v.y, o[i][1]);
+                    }
+                }
+            }
+            if (col0 + tc < db) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (ti + i >= n) continue;
+                    if (ro.partial) put_pair<F32>(ro.out, (chain * w.T + t0 + ti + i) * db + col0 + tc, o[i][0], o[i][1]);
+                    else put_pair<D>(ro.out, gdn_base(w.token_major, b, h, w.H, w.T, db) + (t0 + ti + i) * gdn_stride(w.token_major, w.H, db) + col0 + tc, o[i][0], o[i][1]);
+                }
+            }
+        }
+        const float f = sm.pw[n];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[i][e] *= f;
+        for (int j = 0; j < n; ++j) {
+            const float4 v = *reinterpret_cast<const float4*>(&sm.v[j][cg]);
+            const float g = ro.add * (ro.reverse ? sm.pw[j + 1] : sm.pw[n - 1 - j]);
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const float k = g * sm.k[j][x0 + i];
+                S[i][0] = fmaf(k, v.x, S[i][0]); S[i][1] = fmaf(k, v.y, S[i][1]);
+                S[i][2] = fmaf(k, v.z, S[i][2]); S[i][3] = fmaf(k, v.w, S[i][3]);
+            }
+        }
+    }
+    float* out = SUMS ? pieces + (seg + 1) * per : ro.state_out != nullptr ? ro.state_out + chain * per : nullptr;
+    if (out != nullptr && (SUMS || seg == w.segs - 1)) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (x0 + i < da && col0 + cg + e < db) out[at(x0 + i, cg + e)] = S[i][e];
+    }
+    if (!SUMS && seg == w.segs - 1) {                        // tokens past the length
+        for (int p = tid; p < (w.T - len) * (COLS / 2); p += WT) {
+            const int t = len + p / (COLS / 2), x = col0 + p % (COLS / 2) * 2;
+            if (x >= db) continue;
+            if (ro.partial) put_pair<F32>(ro.out, (chain * w.T + t) * db + x, 0.f, 0.f);
+            else put_pair<D>(ro.out, gdn_base(w.token_major, b, h, w.H, w.T, db) + t * gdn_stride(w.token_major, w.H, db) + x, 0.f, 0.f);
+        }
+    }
+}
+
+template <class D, int DA, bool SUMS>
+cudaError_t walk(const DlaWalk& w, cudaStream_t stream) {
+    constexpr size_t smem = sizeof(WalkSmem<DA>);
+    static std::atomic<unsigned long long> seen;
+    cudaError_t e = allow_smem(k_dla_walk<D, DA, SUMS>, smem, seen);
+    if (e != cudaSuccess) return e;
+    int n[3] = {0, 0, 0};
+    for (int i = 0; i < w.roles; ++i) n[i] = (w.role[i].db + COLS - 1) / COLS;
+    const unsigned segs = static_cast<unsigned>(SUMS ? w.segs - 1 : w.segs);
+    k_dla_walk<D, DA, SUMS><<<dim3((n[0] + n[1] + n[2]) * segs, w.H, w.B), WT, smem, stream>>>(w, make_int3(n[0], n[1], n[2]));
+    return cudaGetLastError();
+}
+template <class D, int DA>
+cudaError_t walks(const DlaWalk& w, cudaStream_t stream) {
+    if (w.segs > 1) {
+        cudaError_t e = walk<D, DA, true>(w, stream);
+        if (e != cudaSuccess) return e;
+    }
+    return walk<D, DA, false>(w, stream);
+}
+template <class D>
+cudaError_t walk_width(const DlaWalk& w, cudaStream_t stream) {
+    int da = 0;
+    for (int i = 0; i < w.roles; ++i) da = w.role[i].da > da ? w.role[i].da : da;
+    return da <= 64 ? walks<D, 64>(w, stream) : da <= 128 ? walks<D, 128>(w, stream) : walks<D, 256>(w, stream);
+}
+
+// Sum over the value heads of a key head, in order, rounded once; four values a thread.
+template <class D>
+__global__ void __launch_bounds__(256) k_dla_join(const float* __restrict__ pq, const float* __restrict__ pk, void* dq, void* dk, int B, int Hk, int group, int T, int d, int token_major) {
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4, total = static_cast<int64_t>(B) * Hk * T * d;
+    if (i >= total) return;
+    const float* const part = blockIdx.y == 0 ? pq : pk;
+    void* const out = blockIdx.y == 0 ? dq : dk;
+    const int x = static_cast<int>(i % d);
+    const int64_t row = i / d;
+    const int t = static_cast<int>(row % T), hk = static_cast<int>(row / T % Hk), b = static_cast<int>(row / T / Hk);
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int g = 0; g < group; ++g) {
+        const float4 p = __ldcs(reinterpret_cast<const float4*>(part + ((static_cast<int64_t>(b) * Hk * group + hk * group + g) * T + t) * d + x));
+        s.x += p.x; s.y += p.y; s.z += p.z; s.w += p.w;
+    }
+    const int64_t at = gdn_base(token_major, b, hk, Hk, T, d) + t * gdn_stride(token_major, Hk, d) + x;
+    put_pair<D>(out, at, s.x, s.y);
+    put_pair<D>(out, at + 2, s.z, s.w);
+}
+
+// One token: the state's two trips through HBM are all that counts.  A CTA takes 32 columns of one state, a warp 32 rows
+// of them, a lane 8 rows x 4 columns, all in flight at once.
+template <class D>
+__device__ __forceinline__ void load_8(const void* base, int64_t at, int left, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; i += D::E) {
+        const uint4 u = left > i ? __ldg(token_ptr<D>(base, at + i)) : make_uint4(0, 0, 0, 0);
+        unpack16<D>(u, f + i);
+    }
+}
+template <class D>
+__global__ void __launch_bounds__(256) k_dla_step(const DlaStep r) {
+    __shared__ __align__(16) float sh[8][32];
+    const int b = blockIdx.z, h = blockIdx.y, hk = h / (r.H / r.Hk);
+    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+    const int row0 = 32 * warp + 8 * (lane >> 3), col = 32 * blockIdx.x + 4 * (lane & 7);
+    const bool live = col < r.dv;                                // d_v is a multiple of 4
+    int64_t slot = b;
+    bool skip = false;
+    if (r.slots != nullptr) {
+        slot = __ldg(r.slots + b);
+        if (slot >= r.n_slots && threadIdx.x == 0) flag_error(r.err, ERR_BAD_INDEX);
+        skip = slot < 0 || slot >= r.n_slots;
+    }
+    const int64_t chain = static_cast<int64_t>(b) * r.H + h, kb = (static_cast<int64_t>(b) * r.Hk + hk) * r.dk;
+    float* const st = r.state + (slot * r.H + h) * r.dk * r.dv + col;
+    const int left = r.dk - row0;
+    float4 S[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        S[i] = !skip && live && i < left ? __ldcs(reinterpret_cast<const float4*>(st + static_cast<int64_t>(row0 + i) * r.dv)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    float k[8], q[8], v[4] = {0.f, 0.f, 0.f, 0.f};
+    load_8<D>(r.k, kb + row0, left, k);
+    load_8<D>(r.q, kb + row0, left, q);
+    if (live) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] = load_elem<D>(r.v, chain * r.dv + col + c);
+    }
+    const float lam = dla_pow(__ldg(r.log_decay + h), 1);
+    float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        S[i].x = fmaf(k[i], v[0], lam * S[i].x); S[i].y = fmaf(k[i], v[1], lam * S[i].y);
+        S[i].z = fmaf(k[i], v[2], lam * S[i].z); S[i].w = fmaf(k[i], v[3], lam * S[i].w);
+        if (!skip && live && i < left) __stcs(reinterpret_cast<float4*>(st + static_cast<int64_t>(row0 + i) * r.dv), S[i]);
+        if (i < left) {                                          // past d_k: zero times a v that is not finite
+            o[0] = fmaf(q[i], S[i].x, o[0]); o[1] = fmaf(q[i], S[i].y, o[1]);
+            o[2] = fmaf(q[i], S[i].z, o[2]); o[3] = fmaf(q[i], S[i].w, o[3]);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        o[c] += __shfl_xor_sync(0xffffffffu, o[c], 8);
+        o[c] += __shfl_xor_sync(0xffffffffu, o[c], 16);
+    }
+    if (warps > 1) {
+        float4* const at = reinterpret_cast<float4*>(&sh[0][4 * (lane & 7)]);
+        if (lane < 8) at[warp * 8] = make_float4(o[0], o[1], o[2], o[3]);
+        __syncthreads();
+        if (warp == 0 && lane < 8) {
+            o[0] = o[1] = o[2] = o[3] = 0.f;
+            for (int w = 0; w < warps; ++w) {
+                const float4 p = at[w * 8];
+                o[0] += p.x; o[1] += p.y; o[2] += p.z; o[3] += p.w;
+            }
+        }
+    }
+    if (warp == 0 && lane < 8 && live) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] = skip ? 0.f : r.scale * o[c];
+        put_pair<D>(r.y, chain * r.dv + col, o[0], o[1]);
+        put_pair<D>(r.y, chain * r.dv + col + 2, o[2], o[3]);
+    }
+}
+
+}  // namespace
+
+void dla_plan(int, DlaWalk& w) {
+    w.segs = 1;
+    w.seg_chunks = (w.T + C - 1) / C;
+}
+
+cudaError_t launch_dla(int dtype, const DlaWalk& w, cudaStream_t stream) {
+    return dtype == SDM_F32 ? walk_width<F32>(w, stream) : walk_width<BF16>(w, stream);
+}
+
+cudaError_t launch_dla_join(int dtype, const float* pq, const float* pk, void* dq, void* dk, int B, int Hk, int group, int T, int d, int token_major,
+                            cudaStream_t stream) {
+    const int64_t pieces = static_cast<int64_t>(B) * Hk * T * d / 4;
+    if (pieces == 0) return cudaSuccess;
+    const dim3 grid(static_cast<unsigned>((pieces + 255) / 256), 2);
+    if (dtype == SDM_F32) k_dla_join<F32><<<grid, 256, 0, stream>>>(pq, pk, dq, dk, B, Hk, group, T, d, token_major);
+    else k_dla_join<BF16><<<grid, 256, 0, stream>>>(pq, pk, dq, dk, B, Hk, group, T, d, token_major);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_dla_step(int dtype, const DlaStep& s, cudaStream_t stream) {
+    const dim3 grid((s.dv + 31) / 32, s.H, s.B);
+    const int threads = 32 * ((s.dk + 31) / 32);
+    if (dtype == SDM_F32) k_dla_step<F32><<<grid, threads, 0, stream>>>(s);
+    else k_dla_step<BF16><<<grid, threads, 0, stream>>>(s);
+    return cudaGetLastError();
+}
+
+}  // namespace sdm
