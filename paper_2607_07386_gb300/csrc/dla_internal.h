@@ -60,6 +60,10 @@ __device__ __forceinline__ int dla_length(const DlaWalk& w, int b) {
 // Fills in segs and seg_chunks; runs the walks.
 void dla_plan(int dtype, DlaWalk& w);
 cudaError_t launch_dla(int dtype, const DlaWalk& w, cudaStream_t stream);
+// The walks on the tensor cores (k_dla_scan.cu): bf16, da <= 128, chunks of 64.
+bool dla_scan_supported(int dtype, const DlaWalk& w);
+void dla_scan_plan(DlaWalk& w);
+cudaError_t launch_dla_scan(const DlaWalk& w, cudaStream_t stream);
 // dq and dk [heads of k] = sums over the `group` value heads of their shares [B, H, T, d] float32.
 cudaError_t launch_dla_join(int dtype, const float* pq, const float* pk, void* dq, void* dk, int B, int Hk, int group, int T, int d, int token_major,
                             cudaStream_t stream);

@@ -384,12 +384,17 @@ __global__ void __launch_bounds__(256) k_dla_step(const DlaStep r) {
 
 }  // namespace
 
-void dla_plan(int, DlaWalk& w) {
+void dla_plan(int dtype, DlaWalk& w) {
+    if (dla_scan_supported(dtype, w)) {
+        dla_scan_plan(w);
+        return;
+    }
     w.segs = 1;
     w.seg_chunks = (w.T + C - 1) / C;
 }
 
 cudaError_t launch_dla(int dtype, const DlaWalk& w, cudaStream_t stream) {
+    if (dla_scan_supported(dtype, w)) return launch_dla_scan(w, stream);
     return dtype == SDM_F32 ? walk_width<F32>(w, stream) : walk_width<BF16>(w, stream);
 }
 
