@@ -3,7 +3,7 @@
 // A CTA walks one state, 128 columns of it (db), over its chunks; every product has 128 rows, TMEM lanes = columns of the state:
 //   1  P[i, j]  = r_i.k_j                       A = [r; k] in shared memory (the k half is not used), B = k
 //   2  I[c, i]  = sum_x S[x, c] r_i[x]          A = S transposed, two bf16 parts in TMEM
-//   3  O[c, i]  = sum_j v_j[c] W_ij P_ij        A = v transposed in TMEM, B = the weighted P as two bf16 parts in shared memory
+//   3  O[c, i]  = sum_j v_j[c] W_ij P_ij        A = v as TMA leaves it, B = the weighted P as two bf16 parts in shared memory
 //   4  D[c, x]  = sum_j g_j v_j[c] k_j[x]       A = g v transposed, three bf16 parts in TMEM, B = k
 // and out_i = w_i I + O, S <- lam^n S + D, in float32 and with lam^n in two parts.  W, w and g hold the powers of the decay
 // (dla_internal.h).  r and k are used as TMA leaves them; v goes through registers, which transposes it, scales it and keeps
@@ -27,28 +27,31 @@ namespace {
 
 using namespace gdn;
 
-constexpr int SW = 8, VW = 4, OW = 4, PW = 4;  // warps: state, v, outputs, and (the last four) P, P, products, copies
+constexpr int SW = 8, VW = 8, OW = 4, PW = 4;  // warps: state, v, outputs, and (the last four) P, P, products, copies
 constexpr int ST = 32 * (SW + VW + OW + PW);
-constexpr int LAUNCH_REGS = 96, STATE_REGS = 120, REST_REGS = 80;
-static_assert(SW * STATE_REGS + (VW + OW + PW) * REST_REGS <= (SW + VW + OW + PW) * LAUNCH_REGS, "register split");
+constexpr int LAUNCH_REGS = 80, STATE_REGS = 104, V_REGS = 80, REST_REGS = 56;
+static_assert(SW * STATE_REGS + VW * V_REGS + (OW + PW) * REST_REGS <= (SW + VW + OW + PW) * LAUNCH_REGS, "register split");
 
-// TMEM columns.  O lies where P was.
-constexpr uint32_t S_COL = 0, D_COL = 128, V_COL = 256, P_COL = 384, I_COL = 448, T_COLS = 512;
+// TMEM columns: S, two parts; D, 64 rows of da at a time; g v, three parts; P; O; I.
+constexpr uint32_t S_COL = 0, D_COL = 128, V_COL = 192, P_COL = 288, O_COL = 352, I_COL = 416, T_COLS = 512;
 constexpr int WP = 68;                         // floats of a row of W, so that rows start four banks apart
 
 template <int DA>
 struct ScanTile {
     static constexpr uint32_t RK = 0, V = DA / 64 * 16384, BYTES = V + 16384;        // [r; k] per 64 of da; v per 64 columns
     static constexpr int STAGES = DA == 128 ? 3 : 4;
-    static constexpr uint32_t PS = BYTES * STAGES, OUT = PS + 2 * MAT, CTL = OUT + 2 * 16384;
+    static constexpr uint32_t PS = BYTES * STAGES, OUT = PS + 4 * MAT, CTL = OUT + 16384;       // P's parts, of two chunks; outputs
 };
-enum { B_FULL = 0, B_FREE = 4, B_P = 8, B_PS, B_D, B_D2, B_O, B_VFREE, B_V, B_OFREE, B_S, B_COUNT };
+// Barriers.  Completed by copies and MMAs: a stage's tile; P; D (per 64 rows of da); S's parts read; O, and with it I.  By
+// warps: the parts of P (and P taken out); of g v; of S; D taken out; O and I taken out; what lies past the length is zero.
+// By both: a stage is free.
+enum { B_FULL = 0, B_FREE = 4, B_P = 8, B_D, B_D1, B_SFREE, B_O, B_PS, B_V, B_S, B_DFREE, B_DFREE1, B_OFREE, B_ZERO, B_COUNT };
 struct ScanCtl {
     float W[C * WP];
     float add[2][C], inter[2][C];              // weights of a whole chunk and of the partial one
     float pw[C + 1];
     float lam[2][2];                           // lam^n of both in two parts
-    short first[2][128];                       // of a column: the chunk's first value (in the walk's order) that is not finite
+    short first[4][2][128];                      // of a column: the chunk's first value (in the walk's order) that is not finite
     unsigned long long bar[B_COUNT];
     uint32_t tmem;
     int dead;
@@ -61,12 +64,18 @@ struct ScanMaps {
     CUtensorMap r[3], k[3], v[3], out[3];
 };
 
-// The upper halves of two floats as a pair of bf16, and what they leave.
-__device__ __forceinline__ uint32_t cut2(float2& v) {
-    const uint32_t x = __float_as_uint(v.x), y = __float_as_uint(v.y);
-    const float2 hi = make_float2(__uint_as_float(x & 0xffff0000u), __uint_as_float(y & 0xffff0000u));
-    v = __ffma2_rn(hi, make_float2(-1.f, -1.f), v);
-    return __byte_perm(x, y, 0x7632);
+// The next bf16 part of two floats, which keep what its rounding left: exact, in one mixed multiply-add each.
+__device__ __forceinline__ uint32_t part2(float2& v) {
+    const uint32_t u = pack2(v.x, v.y);
+    asm("{\n .reg .b16 l, h, m;\n mov.b32 {l, h}, %2;\n mov.b16 m, 0xBF80;\n fma.rn.f32.bf16 %0, l, m, %0;\n fma.rn.f32.bf16 %1, h, m, %1;\n}\n"
+        : "+f"(v.x), "+f"(v.y) : "r"(u));
+    return u;
+}
+// A bf16 value of shared memory as a float.
+__device__ __forceinline__ float load_bf16(const unsigned char* p) {
+    float f;
+    asm("{\n .reg .b16 h;\n mov.b16 h, %1;\n add.rn.f32.bf16 %0, h, 0f00000000;\n}\n" : "=f"(f) : "h"(*reinterpret_cast<const unsigned short*>(p)));
+    return f;
 }
 
 template <int DA, bool SUMS>
@@ -103,7 +112,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
     if (tid == 0) {
         ctl.dead = 0;
         for (int i = 0; i < B_COUNT; ++i)
-            mbar_init(bar(i), i >= B_FREE && i < B_P ? VW + 1 : i == B_PS ? 2 : i == B_V ? VW : i == B_OFREE ? OW : i == B_S ? SW : 1);
+            mbar_init(bar(i), i >= B_FREE && i < B_P ? VW + 1 : i == B_PS ? 2 : i == B_V || i == B_ZERO ? VW : i == B_OFREE ? OW : i == B_S ? SW : i == B_DFREE || i == B_DFREE1 ? SW * 64 / DA : 1);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         fence_async();
     }
@@ -145,87 +154,106 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
             unsigned char* const ps = ringp + L::PS;
             for (int c = 0; !SUMS && c < todo; ++c) {
                 await(bar(B_P), c & 1, dead);
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
+                unsigned char* const to = ps + (c & 1) * 2 * MAT;
+                // A token past this one counts as zero, and where it is not finite, not as 0 times it: such products show in
+                // `odd` (0 times each, added up), and are then left out by choice.
+                float2 odd = make_float2(0.f, 0.f);
+                auto row = [&](int e, auto choose) {         // 32 columns
                     float p[32];
                     tmem_ld32(lanes + P_COL + 32 * e, p);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         uint32_t u[4], l[4];
                         const float4 wa = *reinterpret_cast<const float4*>(wt + 32 * e + 8 * q), wb = *reinterpret_cast<const float4*>(wt + 32 * e + 8 * q + 4);
-                        const float ww[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
+                        const float2 ww[4] = {make_float2(wa.x, wa.y), make_float2(wa.z, wa.w), make_float2(wb.x, wb.y), make_float2(wb.z, wb.w)};
 #pragma unroll
                         for (int s = 0; s < 4; ++s) {
-                            // zero by choice: a token past this one may not be finite
-                            float2 f = make_float2(ww[2 * s] != 0.f ? ww[2 * s] * p[8 * q + 2 * s] : 0.f,
-                                                   ww[2 * s + 1] != 0.f ? ww[2 * s + 1] * p[8 * q + 2 * s + 1] : 0.f);
-                            u[s] = cut2(f);
+                            float2 f = __fmul2_rn(ww[s], make_float2(p[8 * q + 2 * s], p[8 * q + 2 * s + 1]));
+                            if (choose) {
+                                if (ww[s].x == 0.f) f.x = 0.f;
+                                if (ww[s].y == 0.f) f.y = 0.f;
+                            } else {
+                                odd = __ffma2_rn(f, make_float2(0.f, 0.f), odd);
+                            }
+                            u[s] = part2(f);
                             l[s] = pack2(f.x, f.y);
                         }
-                        unsigned char* const at = ps + box_at(i, 4 * e + q);
+                        unsigned char* const at = to + box_at(i, 4 * e + q);
                         *reinterpret_cast<uint4*>(at) = make_uint4(u[0], u[1], u[2], u[3]);
                         *reinterpret_cast<uint4*>(at + MAT) = make_uint4(l[0], l[1], l[2], l[3]);
                     }
+                };
+#pragma unroll 1
+                for (int e = 0; e < 2; ++e) row(e, false);
+                if (__any_sync(0xffffffffu, !(odd.x + odd.y == 0.f))) {
+#pragma unroll 1
+                    for (int e = 0; e < 2; ++e) row(e, true);
                 }
                 tc_before_sync();
                 hand_over(bar(B_PS), lane);
             }
-        } else if (me == 2) {                                // products
+        } else if (me == 2) {                                // products, in an order that leaves every group of warps time
             const uint32_t id64 = mma_idesc(64);
+            auto rk = [&](int c) {                           // 1
+                const int s = c % L::STAGES;
+                const uint32_t t = ring + s * L::BYTES;
+                const uint64_t dr = sw128_desc(t + L::RK), dk = sw128_desc(t + L::RK + 8192);
+                await(bar(B_FULL + s), (c / L::STAGES) & 1, dead);
+                if (partial(c)) await(bar(B_ZERO), 0, dead);
+                if (elect_one()) {
+#pragma unroll
+                    for (int kk = 0; kk < DA / 16; ++kk)
+                        mma_bf16(tmem + P_COL, dr + (kk / 4) * 1024 + (kk % 4) * 2, dk + (kk / 4) * 1024 + (kk % 4) * 2, id64, kk != 0);
+                    mma_commit(bar(B_P));
+                }
+                __syncwarp();
+            };
+            if (!SUMS && todo > 0) rk(0);
             for (int c = 0; c < todo; ++c) {
                 const int s = c % L::STAGES;
                 const uint32_t t = ring + s * L::BYTES, ph = c & 1;
-                const uint64_t dr = sw128_desc(t + L::RK), dk = sw128_desc(t + L::RK + 8192), dkt = sw128_mn_desc(t + L::RK + 8192, 16384),
-                               dp = sw128_desc(ring + L::PS);
-                await(bar(B_FULL + s), (c / L::STAGES) & 1, dead);
-                if (!SUMS) {
-                    if (partial(c)) await(bar(B_V), ph, dead);       // k's rows past the length are zero by then
-                    if (c > 0) await(bar(B_OFREE), (c - 1) & 1, dead);
+                const uint64_t dr = sw128_desc(t + L::RK), dkt = sw128_mn_desc(t + L::RK + 8192, 16384), dv = sw128_mn_desc(t + L::V, 8192),
+                               dp = sw128_desc(ring + L::PS + (c & 1) * 2 * MAT);
+                auto kv = [&](int x) {                       // 4, for 64 rows of da; lower parts first, here and below: their sums are small
                     if (elect_one()) {
+#pragma unroll 1
+                        for (int p = 2; p >= 0; --p)
 #pragma unroll
-                        for (int kk = 0; kk < DA / 16; ++kk)
-                            mma_bf16(tmem + P_COL, dr + (kk / 4) * 1024 + (kk % 4) * 2, dk + (kk / 4) * 1024 + (kk % 4) * 2, id64, kk != 0);
-                        mma_commit(bar(B_P));
+                            for (int kk = 0; kk < C / 16; ++kk)
+                                mma_bf16_ta(tmem + D_COL, tmem + V_COL + p * 32 + kk * 8, dkt + x * 1024 + kk * 128, id64 | MN_B, p != 2 || kk != 0);
+                        mma_commit(bar(B_D + x));
+                        if (SUMS && x == DA / 64 - 1) mma_commit(bar(B_FREE + s));
                     }
                     __syncwarp();
+                };
+                if (SUMS) await(bar(B_FULL + s), (c / L::STAGES) & 1, dead);
+                await(bar(B_V), ph, dead);
+                if (c > 0) await(bar(B_DFREE + DA / 64 - 1), (c - 1) & 1, dead);
+                kv(0);
+                if (!SUMS) {
+                    await(bar(B_PS), ph, dead);
+                    if (c + 1 < todo) rk(c + 1);
                 }
+                if (DA > 64) {
+                    await(bar(B_DFREE), ph, dead);
+                    kv(1);
+                }
+                if (SUMS) continue;
                 await(bar(B_S), ph, dead);
-                if (!SUMS && elect_one()) {                  // lower parts first, here and below: their sums are small
+                if (c > 0) await(bar(B_OFREE), (c - 1) & 1, dead);
+                if (elect_one()) {                           // 2
 #pragma unroll 1
                     for (int p = 1; p >= 0; --p)
 #pragma unroll
                         for (int kk = 0; kk < DA / 16; ++kk)
                             mma_bf16_ta(tmem + I_COL, tmem + S_COL + p * SB + kk * 8, dr + (kk / 4) * 1024 + (kk % 4) * 2, id64, p != 1 || kk != 0);
-                }
-                __syncwarp();
-                await(bar(B_V), ph, dead);
-                if (elect_one()) {
+                    mma_commit(bar(B_SFREE));
 #pragma unroll 1
-                    for (int x = 0; x < DA / 64; ++x) {
-#pragma unroll 1
-                        for (int p = 2; p >= 0; --p)
-#pragma unroll
-                            for (int kk = 0; kk < C / 16; ++kk)
-                                mma_bf16_ta(tmem + D_COL + x * 64, tmem + V_COL + 32 + p * 32 + kk * 8, dkt + x * 1024 + kk * 128, id64 | MN_B, p != 2 || kk != 0);
-                        mma_commit(bar(B_D + x));
-                    }
-                    if (DA == 64) mma_commit(bar(B_D2));
-                    if (SUMS) {
-                        mma_commit(bar(B_VFREE));
-                        mma_commit(bar(B_FREE + s));
-                    }
-                }
-                __syncwarp();
-                if (SUMS) continue;
-                await(bar(B_PS), ph, dead);
-                if (elect_one()) {
-#pragma unroll 1
-                    for (int p = 1; p >= 0; --p)
+                    for (int p = 1; p >= 0; --p)             // 3
 #pragma unroll
                         for (int kk = 0; kk < C / 16; ++kk)
-                            mma_bf16_ta(tmem + P_COL, tmem + V_COL + kk * 8, dp + p * (MAT / 16) + kk * 2, id64, p != 1 || kk != 0);
+                            mma_bf16(tmem + O_COL, dv + kk * 128, dp + p * (MAT / 16) + kk * 2, id64 | MN_A, p != 1 || kk != 0);
                     mma_commit(bar(B_O));
-                    mma_commit(bar(B_VFREE));
                     mma_commit(bar(B_FREE + s));
                 }
                 __syncwarp();
@@ -263,21 +291,23 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
         for (int c = 0; !SUMS && c < todo; ++c) {
             const bool part = partial(c);
             const int n = part ? last_n : C, t0 = chunk_at(c) * C;
-            unsigned char* const box = ringp + L::OUT + (c & 1) * 16384;
+            unsigned char* const box = ringp + L::OUT;
             unsigned char* const yt = box + (row / 64) * 8192;
             const float* const wi = ctl.inter[part];
-            if (!share) {                                    // the copy before the last has left this box
-                if (warp == SW + VW && lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;\n" ::: "memory");
+            if (!share) {                                    // the last copy has left the box
+                if (warp == SW + VW && lane == 0) bulk_wait_read();
                 asm volatile("bar.sync 1, %0;\n" ::"n"(32 * OW) : "memory");
             }
             await(bar(B_O), c & 1, dead);
-            const int first = ctl.first[c & 1][row];
+            const int f0 = ctl.first[c & 3][0][row], f1 = ctl.first[c & 3][1][row], first = reverse ? max(f0, f1) : min(f0, f1);
             const bool odd = __any_sync(0xffffffffu, first != (reverse ? -1 : C));
-#pragma unroll
+#pragma unroll 1
             for (int e = 0; e < 4; ++e) {                    // 16 tokens at a time
                 float y[16], o[16];
-                tmem_ld16(lanes + I_COL + 16 * e, y);
-                tmem_ld16(lanes + P_COL + 16 * e, o);
+                tmem_ld16_begin(lanes + I_COL + 16 * e, y);
+                tmem_ld16_begin(lanes + O_COL + 16 * e, o);
+                tmem_ld_wait(y);
+                tmem_ld_wait(o);
                 if (e == 3) {
                     tc_before_sync();
                     __syncwarp();
@@ -293,7 +323,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
                 if (odd || part) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
-                        const int i = 16 * e + j;
+                        const int i = 16 * e + j;            // a column's outputs from its first odd value on
                         y[j] = i >= n ? 0.f : (reverse ? i <= first : i >= first) ? gdn_nan() : y[j];
                     }
                 }
@@ -335,92 +365,64 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
                 }
             }
         }
-    } else if (warp >= SW) {                                 // v: column `row`, all tokens
-        regs_dec<REST_REGS>();
-        const int quad = warp & 3, row = quad * 32 + lane;
+    } else if (warp >= SW) {                                 // v: column `row`, 32 tokens from i0 on
+        if (V_REGS < LAUNCH_REGS) regs_dec<V_REGS>();
+        const int quad = warp & 3, half = (warp - SW) >> 2, row = quad * 32 + lane, i0 = half * 32;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
-        const bool live = col0 + row < ro.db;
         for (int c = 0; c < todo; ++c) {
             const int s = c % L::STAGES;
             const bool part = partial(c);
-            const int n = part ? last_n : C;
             unsigned char* const tile = ringp + s * L::BYTES;
-            const unsigned char* const vt = tile + L::V + (row / 64) * 8192;
-            const float* const add = ctl.add[part];
+            unsigned char* const vt = tile + L::V + (row / 64) * 8192 + i0 * 128;
+            const float* const add = ctl.add[part] + i0;
             mbar_wait_or_dead(bar(B_FULL + s), (c / L::STAGES) & 1, dead);
             __syncwarp();
-            uint32_t v[C / 2];                               // two tokens in a word
+            if (part) {                                      // rows past the length: zeros, whatever was there
+                for (int p = tid - 32 * SW; p < (C - last_n) * (DA / 8 + 16); p += 32 * VW) {
+                    const int rw = last_n + p / (DA / 8 + 16), x = p % (DA / 8 + 16), k = x - 16;
+                    *reinterpret_cast<uint4*>(tile + (x < 16 ? L::V + (x / 8) * 8192 : L::RK + (k / 8) * 16384 + 8192) + rw * 128 + (x % 8) * 16) = make_uint4(0, 0, 0, 0);
+                }
+                fence_async();
+                asm volatile("bar.sync 2, %0;\n" ::"n"(32 * VW) : "memory");
+                if (lane == 0) mbar_arrive(bar(B_ZERO));     // once: a walk has one partial chunk
+            }
+            uint32_t u[3][16];                               // the parts, two tokens in a word
+            float2 left = make_float2(0.f, 0.f);             // not 0 where a value is not finite
 #pragma unroll
-            for (int j = 0; j < C / 2; ++j)
-                v[j] = *reinterpret_cast<const unsigned short*>(vt + sw128_at(2 * j, row % 64)) |
-                       (static_cast<uint32_t>(*reinterpret_cast<const unsigned short*>(vt + sw128_at(2 * j + 1, row % 64))) << 16);
-            if (part) {                                      // v and the rows of k past the length: zeros, whatever was there
+            for (int j = 0; j < 16; j += 2) {
+                const float4 g = *reinterpret_cast<const float4*>(add + 2 * j);
+                float2 f[2];
 #pragma unroll
-                for (int j = 0; j < C / 2; ++j) v[j] &= 2 * j + 1 < n ? 0xffffffffu : 2 * j < n ? 0x0000ffffu : 0u;
-                for (int p = tid - 32 * SW; p < (C - n) * DA / 8; p += 32 * VW) {
-                    const int rw = n + p / (DA / 8), x = p % (DA / 8);
-                    *reinterpret_cast<uint4*>(tile + L::RK + (x / 8) * 16384 + 8192 + rw * 128 + (x % 8) * 16) = make_uint4(0, 0, 0, 0);
+                for (int e = 0; e < 2; ++e) {
+                    const int i = 2 * (j + e);
+                    f[e] = make_float2(load_bf16(vt + sw128_at(i, row % 64)), load_bf16(vt + sw128_at(i + 1, row % 64)));
+                    f[e] = __fmul2_rn(e ? make_float2(g.z, g.w) : make_float2(g.x, g.y), f[e]);
+                    u[0][j + e] = part2(f[e]);
+                    u[1][j + e] = part2(f[e]);
+                    u[2][j + e] = pack2(f[e].x, f[e].y);
+                    left = __ffma2_rn(f[e], make_float2(0.f, 0.f), left);
+                }
+            }
+            const bool odd = !(left.x + left.y == 0.f);
+            int first = reverse ? -1 : C;
+            if (__any_sync(0xffffffffu, odd)) {              // g v is not finite and makes its column of D so; v goes
+                if (odd) {
+#pragma unroll 1
+                    for (int j = 0; j < 32; ++j) {
+                        unsigned short* const p = reinterpret_cast<unsigned short*>(vt + sw128_at(j, row % 64));
+                        if ((*p & 0x7f80u) != 0x7f80u) continue;
+                        first = reverse ? max(first, i0 + j) : min(first, i0 + j);
+                        *p = 0;
+                    }
                 }
                 fence_async();
             }
+            if (!SUMS) ctl.first[c & 3][half][row] = static_cast<short>(first);
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(B_FREE + s));
-            uint32_t top = 0;                                // the largest exponent
+            if (c > 0) await(bar(B_D + DA / 64 - 1), (c - 1) & 1, dead);
 #pragma unroll
-            for (int j = 0; j < C / 2; ++j) top = __vmaxu2(top, v[j] & 0x7fff7fffu);
-            const bool mine = live && ((top & 0xffffu) >= 0x7f80u || (top >> 16) >= 0x7f80u);
-            const bool odd = __any_sync(0xffffffffu, mine);
-            int first = reverse ? -1 : C;
-            if (odd) {
-                if (mine) {
-#pragma unroll
-                    for (int j = 0; j < C; ++j)
-                        if (((v[j / 2] >> (j % 2 * 16)) & 0x7f80u) == 0x7f80u) first = reverse ? max(first, j) : min(first, j);
-                }
-#pragma unroll
-                for (int j = 0; j < C; ++j)
-                    if (reverse ? j <= first : j >= first) v[j / 2] &= j % 2 ? 0x0000ffffu : 0xffff0000u;
-            }
-            if (c > 0) await(bar(B_VFREE), (c - 1) & 1, dead);
-            if (!SUMS) {
-                ctl.first[c & 1][row] = static_cast<short>(first);
-                uint32_t u[16];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) u[j] = v[16 * e + j];
-                    tmem_st16(lanes + V_COL + 16 * e, u);
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {                    // 16 tokens at a time
-                float2 f[8];
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    const float4 g = *reinterpret_cast<const float4*>(add + 16 * e + 2 * j);
-                    const uint32_t a = v[8 * e + j], d = v[8 * e + j + 1];
-                    f[j] = __fmul2_rn(make_float2(g.x, g.y), make_float2(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u)));
-                    f[j + 1] = __fmul2_rn(make_float2(g.z, g.w), make_float2(__uint_as_float(d << 16), __uint_as_float(d & 0xffff0000u)));
-                }
-                if (odd) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int i = 16 * e + 2 * j;
-                        if (reverse ? i <= first : i >= first) f[j].x = gdn_nan();
-                        if (reverse ? i + 1 <= first : i + 1 >= first) f[j].y = gdn_nan();
-                    }
-                }
-                uint32_t u[8];
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) u[j] = cut2(f[j]);
-                    tmem_st8(lanes + V_COL + 32 + 32 * p + 8 * e, u);
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) u[j] = pack2(f[j].x, f[j].y);
-                tmem_st8(lanes + V_COL + 96 + 8 * e, u);
-            }
+            for (int p = 0; p < 3; ++p) tmem_st16(lanes + V_COL + 32 * p + i0 / 2, u[p]);
             announce(bar(B_V), lane);
         }
     } else {                                                 // the state: column `row`, half of da
@@ -437,6 +439,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
         auto read = [&](const float* p, float keep, bool start) {
 #pragma unroll
             for (int x = 0; x < RD / 2; ++x) {
+                if (x % 4 == 0) asm volatile("" ::: "memory");       // eight values in flight, and no more registers
                 const int r = x0 + 2 * x;                    // da is a multiple of 8
                 const bool on = live && r < da && p != nullptr;
                 const float a = on ? __ldcg(p + at + r * step) : 0.f, d = on ? __ldcg(p + at + (r + 1) * step) : 0.f;
@@ -476,14 +479,15 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
             }
         }
         auto put = [&]() {                                   // S before the next chunk
-            if (!SUMS) {
+            if (SUMS) return;
+            {
 #pragma unroll
                 for (int x = 0; x < RD / 2; x += 8) {
                     uint32_t u[8], l[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         float2 f = S[x + j];
-                        u[j] = cut2(f);
+                        u[j] = part2(f);
                         l[j] = pack2(f.x, f.y);
                     }
                     tmem_st8(lanes + S_COL + x0 / 2 + x, u);
@@ -496,16 +500,24 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
         for (int c = 0; c < todo; ++c) {
             const float* const lam = ctl.lam[partial(c)];
             const float2 hi = make_float2(lam[0], lam[0]), lo = make_float2(lam[1], lam[1]);
-            await(bar(B_D + half), c & 1, dead);
+            const int hd = DA > 64 ? half : 0;
+            const uint32_t dcol = lanes + D_COL + (DA > 64 ? 0 : x0);
+            await(bar(B_D + hd), c & 1, dead);
+            float d[2][16];                                  // the next 16 rows are on their way
+            tmem_ld16_begin(dcol, d[0]);
 #pragma unroll
             for (int x = 0; x < RD / 2; x += 8) {
-                float d[16];
-                tmem_ld16(lanes + D_COL + x0 + 2 * x, d);
+                float (&dx)[16] = d[x / 8 % 2];
+                tmem_ld_wait(dx);
+                if (x + 8 < RD / 2) tmem_ld16_begin(dcol + 2 * (x + 8), d[(x / 8 + 1) % 2]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) S[x + j] = __ffma2_rn(hi, S[x + j], __ffma2_rn(lo, S[x + j], make_float2(d[2 * j], d[2 * j + 1])));
+                for (int j = 0; j < 8; ++j) S[x + j] = __ffma2_rn(hi, S[x + j], __ffma2_rn(lo, S[x + j], make_float2(dx[2 * j], dx[2 * j + 1])));
             }
+            tc_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(B_DFREE + hd));
             if (c + 1 < todo) {
-                tc_before_sync();
+                if (!SUMS) await(bar(B_SFREE), c & 1, dead);
                 put();
             }
         }
