@@ -28,18 +28,30 @@ template <class D>
 __device__ __forceinline__ void store16(void* base, int64_t at, const uint4& u) {
     *reinterpret_cast<uint4*>(static_cast<typename D::T*>(base) + at) = u;
 }
-template <int E>
-__device__ __forceinline__ void put_floats(float* to, const float (&f)[E]) {
+// Values in pairs: the packed units take two at once.
+template <int P>
+__device__ __forceinline__ void put_pairs(float* to, const float2 (&f)[P]) {
 #pragma unroll
-    for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(to + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+    for (int p = 0; p < P; p += 2) *reinterpret_cast<float4*>(to + 2 * p) = make_float4(f[p].x, f[p].y, f[p + 1].x, f[p + 1].y);
 }
-template <class D>
-__device__ __forceinline__ void vec(const float* p, int x, float (&f)[D::E]) {
+__device__ __forceinline__ float2 two(float x) { return make_float2(x, x); }
+// The values at column c of a vector, or ones where it is missing.
+template <int P>
+__device__ __forceinline__ void ones_or(const float* v, int c, float2 (&f)[P]) {
 #pragma unroll
-    for (int e = 0; e < D::E; e += 4) {
-        const float4 a = __ldg(reinterpret_cast<const float4*>(p + x + e));
-        f[e] = a.x; f[e + 1] = a.y; f[e + 2] = a.z; f[e + 3] = a.w;
+    for (int p = 0; p < P; p += 2) {
+        const float4 a = v != nullptr ? __ldg(reinterpret_cast<const float4*>(v + c + 2 * p)) : make_float4(1.f, 1.f, 1.f, 1.f);
+        f[p] = make_float2(a.x, a.y);
+        f[p + 1] = make_float2(a.z, a.w);
     }
+}
+template <int P>
+__device__ __forceinline__ void product(const float* v, const float* w, int c, float2 (&f)[P]) {
+    float2 g[P];
+    ones_or<P>(v, c, f);
+    ones_or<P>(w, c, g);
+#pragma unroll
+    for (int p = 0; p < P; ++p) f[p] = __fmul2_rn(f[p], g[p]);
 }
 
 // Sums of up to eight values over the TPR threads of a row, the same in all of them; other rows' threads are not waited
@@ -98,28 +110,9 @@ constexpr int SMS = 152, FORE_CTAS = 3, BACK_CTAS = 2;       // CTAs of 256 thre
 // Threads a row, values a thread in pieces of 16 bytes, rows of a CTA at once.
 template <class D, int TPR, int VE>
 struct Row {
-    static constexpr int E = D::E, V = VE / E, ROWS = cta(TPR) / TPR;
-    static constexpr bool KEEP = VE == 8;        // the vectors' values of a thread stay in registers
+    static constexpr int E = D::E, P = E / 2, V = VE / E, ROWS = cta(TPR) / TPR;
+    static constexpr bool KEEP = VE <= 16;       // the vectors' values of a thread stay in registers
 };
-// The values at column c of a vector that may be missing (ones), times those of another.
-template <class D>
-__device__ __forceinline__ void ones_or(const float* p, int c, float (&f)[D::E]) {
-    if (p != nullptr) {
-        vec<D>(p, c, f);
-    } else {
-#pragma unroll
-        for (int e = 0; e < D::E; ++e) f[e] = 1.f;
-    }
-}
-template <class D>
-__device__ __forceinline__ void product(const float* p, const float* q, int c, float (&f)[D::E]) {
-    float g[D::E];
-    ones_or<D>(p, c, f);
-    ones_or<D>(q, c, g);
-#pragma unroll
-    for (int e = 0; e < D::E; ++e) f[e] *= g[e];
-}
-
 // Rows on their way: each thread copies its own pieces of N arrays' next S rows into slots of its own in shared memory
 // (asynchronously, so no registers are held and nothing has to be waited for but its own copies).  With S = 0, where S
 // rows of the widest type do not fit, rows are loaded when they are due.
@@ -178,7 +171,7 @@ template <class D, int TPR, int VE, int S>
 __global__ void __launch_bounds__(cta(TPR), TPR > 256 ? 1 : FORE_CTAS) k_block_norm(const BlockNorm a, const int64_t span) {
     extern __shared__ __align__(16) unsigned char ring[];
     using R = Row<D, TPR, VE>;
-    constexpr int E = R::E, V = R::V;
+    constexpr int E = R::E, P = R::P, V = R::V;
     __shared__ __align__(16) float sh[2][16][8];
     int turn = 0;
     const int lane = threadIdx.x % TPR;
@@ -200,14 +193,14 @@ __global__ void __launch_bounds__(cta(TPR), TPR > 256 ? 1 : FORE_CTAS) k_block_n
     };
     int64_t g = a.gate != nullptr ? first / a.gate_rows : 0, until = a.gate != nullptr ? (g + 1) * a.gate_rows : last;
     if (a.gate != nullptr) gate(g);
-    float ck[R::KEEP ? V : 1][E], pk[R::KEEP ? V : 1][E];
+    float2 ck[R::KEEP ? V : 1][P], pk[R::KEEP ? V : 1][P];
     if (R::KEEP) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int c = (lane + i * TPR) * E;
             if (c < a.D) {
-                product<D>(a.res_scale, a.gamma_post, c, ck[i]);
-                ones_or<D>(a.gamma_pre, c, pk[i]);
+                product<P>(a.res_scale, a.gamma_post, c, ck[i]);
+                ones_or<P>(a.gamma_pre, c, pk[i]);
             }
         }
     }
@@ -226,228 +219,272 @@ __global__ void __launch_bounds__(cta(TPR), TPR > 256 ? 1 : FORE_CTAS) k_block_n
         }
         float r = 1.f;
         if (post) {
-            float s[1] = {0.f};
+            float2 q = two(0.f);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                float f[8];
-                unpack16<D>(yu[i], f);
+                float2 y[4];
+                unpack16x2<D>(yu[i], y);
 #pragma unroll
-                for (int e = 0; e < E; ++e) s[0] = fmaf(f[e], f[e], s[0]);
+                for (int p = 0; p < P; ++p) q = __ffma2_rn(y[p], y[p], q);
             }
+            float s[1] = {q.x + q.y};
             row_sum<TPR>(s, sh, turn);
             r = rsqrtf(fmaf(s[0], inv, a.eps));
         }
-        float s[1] = {0.f};
         if (has_y) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int c = (lane + i * TPR) * E;
                 if (c >= a.D) continue;
-                float x[8], y[8], k[E], ga[8];
-                unpack16<D>(xu[i], x);
-                unpack16<D>(yu[i], y);
-                if (a.gate != nullptr) unpack16<D>(gu[i], ga);
-                if (!R::KEEP) product<D>(a.res_scale, a.gamma_post, c, k);
+                float2 x[4], y[4], k[P];
+                unpack16x2<D>(xu[i], x);
+                unpack16x2<D>(yu[i], y);
+                if (!R::KEEP) product<P>(a.res_scale, a.gamma_post, c, k);
+                if (a.gate != nullptr) {
+                    float2 ga[4];
+                    unpack16x2<D>(gu[i], ga);
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    y[e] = y[e] * r * (R::KEEP ? ck[i][e] : k[e]);
-                    if (a.gate != nullptr) y[e] *= ga[e];
-                    x[e] += y[e];
+                    for (int p = 0; p < P; ++p) y[p] = __fmul2_rn(y[p], ga[p]);
                 }
-                xu[i] = pack16<D>(x);
+#pragma unroll
+                for (int p = 0; p < P; ++p) x[p] = __ffma2_rn(__fmul2_rn(y[p], two(r)), R::KEEP ? ck[i][p] : k[p], x[p]);
+                xu[i] = pack16x2<D>(x);
                 store16<D>(a.h, m * a.D + c, xu[i]);
             }
         }
         if (!pre) continue;
+        float2 q = two(0.f);
 #pragma unroll
         for (int i = 0; i < V; ++i) {                        // of what is stored
-            float x[8];
-            unpack16<D>(xu[i], x);
+            float2 x[4];
+            unpack16x2<D>(xu[i], x);
 #pragma unroll
-            for (int e = 0; e < E; ++e) s[0] = fmaf(x[e], x[e], s[0]);
+            for (int p = 0; p < P; ++p) q = __ffma2_rn(x[p], x[p], q);
         }
+        float s[1] = {q.x + q.y};
         row_sum<TPR>(s, sh, turn);
         r = rsqrtf(fmaf(s[0], inv, a.eps));
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int c = (lane + i * TPR) * E;
             if (c >= a.D) continue;
-            float x[8], k[E];
-            unpack16<D>(xu[i], x);
-            if (!R::KEEP) vec<D>(a.gamma_pre, c, k);
+            float2 x[4], k[P];
+            unpack16x2<D>(xu[i], x);
+            if (!R::KEEP) ones_or<P>(a.gamma_pre, c, k);
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = x[e] * r * (R::KEEP ? pk[i][e] : k[e]);
-            store16<D>(a.z, m * a.D + c, pack16<D>(x));
+            for (int p = 0; p < P; ++p) x[p] = __fmul2_rn(__fmul2_rn(x[p], two(r)), R::KEEP ? pk[i][p] : k[p]);
+            store16<D>(a.z, m * a.D + c, pack16x2<D>(x));
         }
     }
 }
 
-// The gradients.  The rows are cut into items: ranges of `span` rows that, where the gradient of a gate shared by several
-// rows is wanted, end with the gate's rows (`spans` to each), else anywhere.  A group of TPR threads takes every so many'th
-// item, its rows one by one.  Column sums stay in registers: q's over an item, the others' over all the
-// group's items; the shares go to `ws` and are joined in order.
+// The gradients.  A group of TPR threads takes `span` rows one after the other.  Column sums stay in registers: dz n's over
+// all of them, q's over the rows of one gate (times the gate it is those rows' share of G, which the group adds up in
+// `ws`), or, where every row has its gate (ROWGATE), G's own.  A gate whose rows one group has is done with there; a
+// gate of several groups has a share from each, the group's first or second (a gate that starts within its rows).  Shares are
+// joined in order.
 struct NormCut {
-    int64_t rows, span, items;   // rows that an item does not leave: a gate's, or all
-    int64_t spans;
+    int64_t span;
     unsigned grid;
     int groups;                  // of all CTAs
-    size_t gate_at, total;       // floats of `ws`: [2][groups][D], then [items][D] where a gate has several items
+    size_t gate_at, total;       // floats of `ws`: [2][groups][D], then [groups][2][D] where a gate may have several groups
 };
 
-template <class D, int TPR, int VE, int S>
+template <class D, int TPR, int VE, int S, bool ROWGATE>
 __global__ void __launch_bounds__(cta(TPR), TPR > 256 ? 1 : BACK_CTAS) k_block_norm_backward(const BlockNorm a, const NormCut cut) {
     extern __shared__ __align__(16) unsigned char ring[];
     using R = Row<D, TPR, VE>;
-    constexpr int E = R::E, V = R::V;
+    constexpr int E = R::E, P = R::P, V = R::V;
     __shared__ __align__(16) float sh[2][16][8];
     int turn = 0;
     const int lane = threadIdx.x % TPR, group = blockIdx.x * R::ROWS + threadIdx.x / TPR;
     const float inv = 1.f / static_cast<float>(a.D);
     const bool post = a.gamma_post != nullptr, pre = a.dz != nullptr, has_y = a.y != nullptr, has_gate = a.gate != nullptr;
-    const bool shared_gate = a.dgate != nullptr && a.gate_rows > 1;
-    float sp[V][E], sq[V][E], sG[V][E];                      // sums of dz n, of q, and G
-    float ck[R::KEEP ? V : 1][E], pk[R::KEEP ? V : 1][E];
+    float2 sp[V][P], sq[V][P];                               // sums of dz n and of q
+    float2 ck[R::KEEP ? V : 1][P], pk[R::KEEP ? V : 1][P];   // c (times the gate, unless that is the row's) and gamma_pre
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int c = (lane + i * TPR) * E;
 #pragma unroll
-        for (int e = 0; e < E; ++e) sp[i][e] = sG[i][e] = 0.f;
+        for (int p = 0; p < P; ++p) sp[i][p] = sq[i][p] = two(0.f);
         if (R::KEEP && c < a.D) {
-            product<D>(a.res_scale, a.gamma_post, c, ck[i]);
-            ones_or<D>(a.gamma_pre, c, pk[i]);
+            product<P>(a.res_scale, a.gamma_post, c, ck[i]);
+            ones_or<P>(a.gamma_pre, c, pk[i]);
         }
     }
-    const void* const src[4] = {pre ? a.h : nullptr, a.dz, a.y, a.dh};
-    for (int64_t it = group; it < cut.items; it += cut.groups) {
-        const int64_t part = it / cut.spans, g0 = part * cut.rows;
-        const int64_t first = g0 + (it - part * cut.spans) * cut.span;
-        int64_t last = g0 + cut.rows < first + cut.span ? g0 + cut.rows : first + cut.span;
-        last = last < a.M ? last : a.M;
-        uint4 gu[V];
-        int64_t g = -1, until = first;                       // the gate's row at hand, and its end
-        auto gate = [&](int64_t m) {
+    constexpr int N = ROWGATE ? 5 : 4;
+    const void* src[N];
+    src[0] = pre ? a.h : nullptr;
+    src[1] = a.dz;
+    src[2] = a.y;
+    src[3] = a.dh;
+    if (ROWGATE) src[N - 1] = a.gate;
+    const void* const (&from)[N] = src;
+    auto gate_at = [&](int64_t g, int c, float2 (&f)[4]) {
+        unpack16x2<D>(__ldg(reinterpret_cast<const uint4*>(static_cast<const typename D::T*>(a.gate) + g * a.D + c)), f);
+    };
+    bool added = false;                                      // a share of G is in `ws`
+    const int64_t first = group * cut.span;
+    const int64_t last = first + cut.span < a.M ? first + cut.span : a.M;
+    int64_t g = 0, until = !ROWGATE && has_gate ? first : last;      // the gate's row at hand, and its end
+    Ahead<D, TPR, VE, N, S> rows(ring, first, last, a.D);
+    rows.start(from);
+    for (int64_t m = first; m < last; ++m) {
+        uint4 hu[V], yu[V], zu[V], du[V], gu[V];
+        rows.wait();
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            hu[i] = rows.get(from, m, 0, i);
+            zu[i] = rows.get(from, m, 1, i);
+            yu[i] = rows.get(from, m, 2, i);
+            du[i] = rows.get(from, m, 3, i);
+            if (ROWGATE) gu[i] = rows.get(from, m, N - 1, i);
+        }
+        rows.advance(from);
+        if (m == until) {
             g = m / a.gate_rows;
             until = (g + 1) * a.gate_rows;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int c = (lane + i * TPR) * E;
-                gu[i] = c < a.D ? __ldg(reinterpret_cast<const uint4*>(static_cast<const typename D::T*>(a.gate) + g * a.D + c)) : make_uint4(0, 0, 0, 0);
-            }
-        };
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-#pragma unroll
-            for (int e = 0; e < E; ++e) sq[i][e] = 0.f;
-        Ahead<D, TPR, VE, 4, S> rows(ring, first, last, a.D);
-        rows.start(src);
-        for (int64_t m = first; m < last; ++m) {
-            uint4 hu[V], yu[V], zu[V], du[V];
-            rows.wait();
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                hu[i] = rows.get(src, m, 0, i);
-                zu[i] = rows.get(src, m, 1, i);
-                yu[i] = rows.get(src, m, 2, i);
-                du[i] = rows.get(src, m, 3, i);
-            }
-            rows.advance(src);
-            if (has_gate && m == until) gate(m);
-            // sums of h^2, dn h, y^2 and, with b = gate c y, of b dh, b dn and b h
-            float s[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int c = (lane + i * TPR) * E;
-                if (c >= a.D) continue;
-                float h[8], z[8], y[8], d[8], ga[8], k[E], kc[E];
-                unpack16<D>(hu[i], h);
-                unpack16<D>(zu[i], z);
-                unpack16<D>(yu[i], y);
-                unpack16<D>(du[i], d);
-                if (has_gate) unpack16<D>(gu[i], ga);
-                if (!R::KEEP) ones_or<D>(a.gamma_pre, c, k);
-                if (!R::KEEP) product<D>(a.res_scale, a.gamma_post, c, kc);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float n = z[e] * (R::KEEP ? pk[i][e] : k[e]);
-                    float b = y[e] * (R::KEEP ? ck[i][e] : kc[e]);
-                    if (has_gate) b *= ga[e];
-                    s[0] = fmaf(h[e], h[e], s[0]);
-                    s[1] = fmaf(n, h[e], s[1]);
-                    s[2] = fmaf(y[e], y[e], s[2]);
-                    s[3] = fmaf(b, d[e], s[3]);
-                    s[4] = fmaf(b, n, s[4]);
-                    s[5] = fmaf(b, h[e], s[5]);
-                }
-            }
-            if (pre || post) row_sum<TPR>(s, sh, turn);
-            const float rh = pre ? rsqrtf(fmaf(s[0], inv, a.eps)) : 0.f, ch = s[1] * rh * rh * inv;      // mean(dn n) rh = ch rh; n = h rh
-            const float ry = post ? rsqrtf(fmaf(s[2], inv, a.eps)) : 1.f;
-            // mean(dn' n') = ry mean(b dx), dx = dh + rh (dn - h ch)
-            const float mean = post ? ry * inv * (pre ? s[3] + rh * (s[4] - ch * s[5]) : s[3]) : 0.f;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int c = (lane + i * TPR) * E;
-                if (c >= a.D) continue;
-                float dx[8], k[E];
-                unpack16<D>(du[i], dx);
-                if (pre) {
-                    float h[8], z[8];
-                    unpack16<D>(hu[i], h);
-                    unpack16<D>(zu[i], z);
-                    if (!R::KEEP) vec<D>(a.gamma_pre, c, k);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        sp[i][e] = fmaf(z[e], h[e] * rh, sp[i][e]);
-                        dx[e] += rh * (z[e] * (R::KEEP ? pk[i][e] : k[e]) - h[e] * ch);
-                    }
-                }
-                store16<D>(a.dx, m * a.D + c, pack16<D>(dx));
-                if (!has_y) continue;
-                float y[8], ga[8], dg[8];
-                unpack16<D>(yu[i], y);
-                if (has_gate) {
-                    unpack16<D>(gu[i], ga);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) ga[e] = 1.f;
-                }
-                if (!R::KEEP) product<D>(a.res_scale, a.gamma_post, c, k);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float n = y[e] * ry, q = dx[e] * n, ce = R::KEEP ? ck[i][e] : k[e];       // n': y itself without a norm
-                    if (shared_gate) sq[i][e] += q;
-                    else sG[i][e] = fmaf(ga[e], q, sG[i][e]);
-                    dg[e] = q * ce;
-                    const float dn = dx[e] * ga[e] * ce;
-                    dx[e] = post ? ry * (dn - n * mean) : dn;
-                }
-                if (a.dgate != nullptr && !shared_gate) store16<D>(a.dgate, m * a.D + c, pack16<D>(dg));
-                store16<D>(a.dy, m * a.D + c, pack16<D>(dx));
-            }
-        }
-        if (shared_gate) {
-            if (first < last || cut.spans > 1) {
-                if (first < last && g < 0) gate(first);
+            if (R::KEEP) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     const int c = (lane + i * TPR) * E;
                     if (c >= a.D) continue;
-                    float ga[8], f[8], k[E];
-                    if (first < last) {
-                        unpack16<D>(gu[i], ga);
+                    float2 ga[4];
+                    gate_at(g, c, ga);
+                    product<P>(a.res_scale, a.gamma_post, c, ck[i]);
 #pragma unroll
-                        for (int e = 0; e < E; ++e) sG[i][e] = fmaf(ga[e], sq[i][e], sG[i][e]);
-                    }
-                    if (cut.spans == 1) {
-                        if (!R::KEEP) product<D>(a.res_scale, a.gamma_post, c, k);
-#pragma unroll
-                        for (int e = 0; e < E; ++e) f[e] = sq[i][e] * (R::KEEP ? ck[i][e] : k[e]);
-                        store16<D>(a.dgate, part * a.D + c, pack16<D>(f));
-                    } else {
-                        put_floats<E>(a.ws + cut.gate_at + it * a.D + c, sq[i]);
-                    }
+                    for (int p = 0; p < P; ++p) ck[i][p] = __fmul2_rn(ck[i][p], ga[p]);
                 }
             }
+        }
+        auto gate_c = [&](int c, float2 (&k)[P]) {       // where it is not kept
+            product<P>(a.res_scale, a.gamma_post, c, k);
+            if (ROWGATE || !has_gate) return;
+            float2 ga[4];
+            gate_at(g, c, ga);
+#pragma unroll
+            for (int p = 0; p < P; ++p) k[p] = __fmul2_rn(k[p], ga[p]);
+        };
+        // sums of h^2, dn h, y^2 and, with b = gate c y, of b dh, b dn and b h
+        float2 t[6];
+#pragma unroll
+        for (int j = 0; j < 6; ++j) t[j] = two(0.f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int c = (lane + i * TPR) * E;
+            if (c >= a.D) continue;
+            float2 h[4], z[4], y[4], d[4], k[P], kc[P];
+            unpack16x2<D>(hu[i], h);
+            unpack16x2<D>(zu[i], z);
+            unpack16x2<D>(yu[i], y);
+            unpack16x2<D>(du[i], d);
+            if (!R::KEEP) ones_or<P>(a.gamma_pre, c, k);
+            if (!R::KEEP) gate_c(c, kc);
+            if (ROWGATE) {
+                float2 ga[4];
+                unpack16x2<D>(gu[i], ga);
+#pragma unroll
+                for (int p = 0; p < P; ++p) kc[p] = __fmul2_rn(ga[p], R::KEEP ? ck[i][p] : kc[p]);
+            }
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const float2 n = __fmul2_rn(z[p], R::KEEP ? pk[i][p] : k[p]), b = __fmul2_rn(y[p], R::KEEP && !ROWGATE ? ck[i][p] : kc[p]);
+                t[0] = __ffma2_rn(h[p], h[p], t[0]);
+                t[1] = __ffma2_rn(n, h[p], t[1]);
+                t[2] = __ffma2_rn(y[p], y[p], t[2]);
+                t[3] = __ffma2_rn(b, d[p], t[3]);
+                t[4] = __ffma2_rn(b, n, t[4]);
+                t[5] = __ffma2_rn(b, h[p], t[5]);
+            }
+        }
+        float s[6];
+#pragma unroll
+        for (int j = 0; j < 6; ++j) s[j] = t[j].x + t[j].y;
+        if (pre || post) row_sum<TPR>(s, sh, turn);
+        const float rh = pre ? rsqrtf(fmaf(s[0], inv, a.eps)) : 0.f, ch = s[1] * rh * rh * inv;      // mean(dn n) rh = ch rh; n = h rh
+        const float ry = post ? rsqrtf(fmaf(s[2], inv, a.eps)) : 1.f;
+        // mean(dn' n') = ry mean(b dx), dx = dh + rh (dn - h ch)
+        const float mean = post ? ry * inv * (pre ? s[3] + rh * (s[4] - ch * s[5]) : s[3]) : 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int c = (lane + i * TPR) * E;
+            if (c >= a.D) continue;
+            float2 dx[4], k[P];
+            unpack16x2<D>(du[i], dx);
+            if (pre) {
+                float2 h[4], z[4];
+                unpack16x2<D>(hu[i], h);
+                unpack16x2<D>(zu[i], z);
+                if (!R::KEEP) ones_or<P>(a.gamma_pre, c, k);
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    sp[i][p] = __ffma2_rn(z[p], __fmul2_rn(h[p], two(rh)), sp[i][p]);
+                    dx[p] = __ffma2_rn(two(rh), __ffma2_rn(h[p], two(-ch), __fmul2_rn(z[p], R::KEEP ? pk[i][p] : k[p])), dx[p]);
+                }
+            }
+            store16<D>(a.dx, m * a.D + c, pack16x2<D>(dx));
+            if (!has_y) continue;
+            float2 y[4];
+            unpack16x2<D>(yu[i], y);
+#pragma unroll
+            for (int p = 0; p < P; ++p) y[p] = __fmul2_rn(y[p], two(ry));        // n': y itself without a norm
+            if (!R::KEEP) gate_c(c, k);
+            if (ROWGATE) {
+                float2 ga[4], q[4];
+                unpack16x2<D>(gu[i], ga);
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const float2 ce = R::KEEP ? ck[i][p] : k[p];
+                    q[p] = __fmul2_rn(dx[p], y[p]);
+                    sq[i][p] = __ffma2_rn(ga[p], q[p], sq[i][p]);
+                    q[p] = __fmul2_rn(q[p], ce);
+                    dx[p] = __fmul2_rn(dx[p], __fmul2_rn(ga[p], ce));
+                }
+                if (a.dgate != nullptr) store16<D>(a.dgate, m * a.D + c, pack16x2<D>(q));
+            } else {
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    sq[i][p] = __ffma2_rn(dx[p], y[p], sq[i][p]);
+                    dx[p] = __fmul2_rn(dx[p], R::KEEP ? ck[i][p] : k[p]);
+                }
+            }
+            if (post) {
+#pragma unroll
+                for (int p = 0; p < P; ++p) dx[p] = __fmul2_rn(two(ry), __ffma2_rn(y[p], two(-mean), dx[p]));
+            }
+            store16<D>(a.dy, m * a.D + c, pack16x2<D>(dx));
+        }
+        if (!ROWGATE && has_gate && (m + 1 == last || m + 1 == until)) {         // the gate's share of G, and its own sum
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int c = (lane + i * TPR) * E;
+                if (c >= a.D) continue;
+                float2 ga[4], k[4], f[P];
+                gate_at(g, c, ga);
+                float* const at = a.ws + (static_cast<int64_t>(cut.groups) + group) * a.D + c;
+#pragma unroll
+                for (int p = 0; p < P; ++p) f[p] = __fmul2_rn(ga[p], sq[i][p]);
+                if (added) {
+#pragma unroll
+                    for (int p = 0; p < P; ++p) f[p] = __fadd2_rn(f[p], *reinterpret_cast<const float2*>(at + 2 * p));
+                }
+                put_pairs<P>(at, f);
+                if (a.dgate != nullptr) {
+                    const int64_t from_row = g * a.gate_rows, to_row = until < a.M ? until : a.M;
+                    if (from_row < first || to_row > last) {
+                        put_pairs<P>(a.ws + cut.gate_at + (2 * static_cast<int64_t>(group) + (from_row > first)) * a.D + c, sq[i]);
+                    } else {
+                        float2 kc[P];
+                        product<P>(a.res_scale, a.gamma_post, c, kc);
+#pragma unroll
+                        for (int p = 0; p < P; ++p) k[p] = __fmul2_rn(sq[i][p], kc[p]);
+                        store16<D>(a.dgate, g * a.D + c, pack16x2<D>(k));
+                    }
+                }
+#pragma unroll
+                for (int p = 0; p < P; ++p) sq[i][p] = two(0.f);
+            }
+            added = true;
         }
     }
 #pragma unroll
@@ -455,62 +492,76 @@ __global__ void __launch_bounds__(cta(TPR), TPR > 256 ? 1 : BACK_CTAS) k_block_n
         const int c = (lane + i * TPR) * E;
         if (c >= a.D) continue;
         float* const at = a.ws + static_cast<int64_t>(group) * a.D + c;
-        if (a.dgamma_pre != nullptr) put_floats<E>(at, sp[i]);
-        if (a.dgamma_post != nullptr || a.dres_scale != nullptr) put_floats<E>(at + static_cast<int64_t>(cut.groups) * a.D, sG[i]);
+        put_pairs<P>(at, sp[i]);
+        if (!added) put_pairs<P>(at + static_cast<int64_t>(cut.groups) * a.D, sq[i]);
     }
 }
 
-// Sums over the shares, in order: JC columns a CTA, JR ranges of rows.  Job 0: dgamma_pre, 1: dres_scale and dgamma_post from
-// G, 2 and on: the rows of dgate.
-constexpr int JC = 8, JR = 32;
+// Sums over the shares, in order: JC columns a CTA, JR ranges of groups.  Job 0: dgamma_pre, 1: dres_scale and dgamma_post from
+// G, 2 and on: the gates of several groups, a CTA every so many'th.
+constexpr int JC = 16, JR = 16, GATE_JOBS = 16;
 template <class D>
-__global__ void __launch_bounds__(JC * JR) k_block_norm_join(const BlockNorm a, const NormCut cut) {
+__global__ void __launch_bounds__(JC * JR) k_block_norm_join(const BlockNorm a, const NormCut cut, const int64_t gates) {
     __shared__ float sum[JR][JC + 1];
-    const int cols = (a.D + JC - 1) / JC, job = blockIdx.x / cols;
-    const int x = threadIdx.x % JC, y = threadIdx.x / JC, c = blockIdx.x % cols * JC + x;
-    if (job == 0 ? a.dgamma_pre == nullptr : job == 1 && a.dgamma_post == nullptr && a.dres_scale == nullptr) return;
-    const int64_t n = job < 2 ? cut.groups : cut.spans;
-    const float* p = a.ws + (job < 2 ? static_cast<int64_t>(job) * cut.groups * a.D : cut.gate_at + (job - 2) * cut.spans * a.D);
-    float s = 0.f;
-    if (c < a.D)
-#pragma unroll 4
-        for (int64_t i = y; i < n; i += JR) s += __ldcs(p + i * a.D + c);
-    sum[y][x] = s;
-    __syncthreads();
-    if (y != 0 || c >= a.D) return;
-    for (int i = 1; i < JR; ++i) s += sum[i][x];
-    if (job == 0) {
-        a.dgamma_pre[c] = s;
-    } else if (job == 1) {
+    const unsigned cols = static_cast<unsigned>((a.D + JC - 1) / JC), job = blockIdx.x / cols;
+    const int x = threadIdx.x % JC, y = threadIdx.x / JC, c = static_cast<int>(blockIdx.x - job * cols) * JC + x;
+    auto total = [&](float s) {                              // in the threads of y = 0
+        __syncthreads();
+        sum[y][x] = s;
+        __syncthreads();
+        for (int i = 1; i < JR; ++i) s += sum[i][x];
+        return s;
+    };
+    if (job < 2) {
+        if (job == 0 ? a.dgamma_pre == nullptr : a.dgamma_post == nullptr && a.dres_scale == nullptr) return;
+        const float* p = a.ws + static_cast<int64_t>(job) * cut.groups * a.D + c;
+        float s = 0.f;
+        if (c < a.D)
+#pragma unroll 8
+            for (int i = y; i < cut.groups; i += JR) s += __ldcs(p + static_cast<int64_t>(i) * a.D);
+        s = total(s);
+        if (y != 0 || c >= a.D) return;
+        if (job == 0) {
+            a.dgamma_pre[c] = s;
+            return;
+        }
         if (a.dres_scale != nullptr) a.dres_scale[c] = a.gamma_post != nullptr ? s * a.gamma_post[c] : s;
         if (a.dgamma_post != nullptr) a.dgamma_post[c] = a.res_scale != nullptr ? s * a.res_scale[c] : s;
-    } else {
+        return;
+    }
+    // where gates outnumber groups, the gates at the groups' ends are all that may have several
+    const bool ends = gates > cut.groups;
+    const int64_t jobs = ends ? cut.groups : gates;
+    for (int64_t j = job - 2; j < jobs; j += GATE_JOBS) {
+        const int64_t last = (j + 1) * cut.span - 1;
+        if (ends && last >= a.M) break;
+        const int64_t g = ends ? last / a.gate_rows : j, from = g * a.gate_rows, to = from + a.gate_rows < a.M ? from + a.gate_rows : a.M;
+        const int64_t g0 = from / cut.span, g1 = (to - 1) / cut.span;
+        if (g0 == g1 || (ends && g0 != j)) continue;
+        float s = 0.f;
+        if (c < a.D)
+            for (int64_t i = g0 + y; i <= g1; i += JR) s += __ldcs(a.ws + cut.gate_at + (2 * i + (from > i * cut.span)) * a.D + c);
+        s = total(s);
+        if (y != 0 || c >= a.D) continue;
         if (a.res_scale != nullptr) s *= a.res_scale[c];
         if (a.gamma_post != nullptr) s *= a.gamma_post[c];
-        const int64_t at = static_cast<int64_t>(job - 2) * a.D + c;
+        const int64_t at = g * a.D + c;
         if (D::BYTES == 4) static_cast<float*>(a.dgate)[at] = s;
         else static_cast<__nv_bfloat16*>(a.dgate)[at] = __float2bfloat16_rn(s);
     }
 }
 
-
 // `shared`: the gradient of a gate shared by several rows is wanted.
-NormCut norm_cut(int64_t M, int64_t gate_rows, int D, int tpr, bool shared) {
+NormCut norm_cut(int64_t M, int D, int tpr, bool shared) {
     NormCut c{};
     const int rows = cta(tpr) / tpr;
-    const int64_t ctas_most = static_cast<int64_t>(SMS) * (tpr > 256 ? 1 : BACK_CTAS);
-    c.rows = shared && gate_rows < M ? gate_rows : M;
-    const int64_t parts = (M + c.rows - 1) / c.rows, want = ctas_most * rows;
-    c.spans = (want + parts - 1) / parts;
-    if (c.spans > c.rows) c.spans = c.rows;
-    c.span = (c.rows + c.spans - 1) / c.spans;
-    c.spans = (c.rows + c.span - 1) / c.span;
-    c.items = parts * c.spans;
-    const int64_t ctas = (c.items + rows - 1) / rows;
-    c.grid = static_cast<unsigned>(ctas < ctas_most ? ctas : ctas_most);
+    const int64_t most = static_cast<int64_t>(SMS) * (tpr > 256 ? 1 : BACK_CTAS) * rows;
+    c.span = (M + most - 1) / most;
+    const int64_t groups = (M + c.span - 1) / c.span;
+    c.grid = static_cast<unsigned>((groups + rows - 1) / rows);
     c.groups = static_cast<int>(c.grid) * rows;
     c.gate_at = static_cast<size_t>(2) * c.groups * D;
-    c.total = c.gate_at + (shared && c.spans > 1 ? static_cast<size_t>(c.items) * D : 0);
+    c.total = c.gate_at + (shared ? static_cast<size_t>(2) * c.groups * D : 0);
     return c;
 }
 
@@ -557,22 +608,22 @@ cudaError_t forward(const RowPlan& p, const BlockNorm& a, cudaStream_t stream) {
         return cudaGetLastError();
     });
 }
-template <class D>
+template <class D, bool ROWGATE>
 cudaError_t backward(const RowPlan& p, const BlockNorm& a, cudaStream_t stream) {
     const bool shared = a.dgate != nullptr && a.gate_rows > 1;
-    const NormCut cut = norm_cut(a.M, a.gate_rows, a.D, p.tpr, shared);
+    const NormCut cut = norm_cut(a.M, a.D, p.tpr, shared);
     cudaError_t e = with_plan(p, [&](auto T, auto V) {
-        constexpr int S = stages<D, T.value, V.value, 4>(BACK_CTAS);
-        constexpr size_t smem = S * stage_bytes<D, T.value, V.value, 4>();
+        constexpr int S = stages<D, T.value, V.value, ROWGATE ? 5 : 4>(BACK_CTAS);
+        constexpr size_t smem = S * stage_bytes<D, T.value, V.value, ROWGATE ? 5 : 4>();
         static std::atomic<unsigned long long> seen;
-        const cudaError_t e = allow_smem(k_block_norm_backward<D, T.value, V.value, S>, smem, seen);
+        const cudaError_t e = allow_smem(k_block_norm_backward<D, T.value, V.value, S, ROWGATE>, smem, seen);
         if (e != cudaSuccess) return e;
-        k_block_norm_backward<D, T.value, V.value, S><<<cut.grid, cta(T.value), smem, stream>>>(a, cut);
+        k_block_norm_backward<D, T.value, V.value, S, ROWGATE><<<cut.grid, cta(T.value), smem, stream>>>(a, cut);
         return cudaGetLastError();
     });
-    if (e != cudaSuccess || (a.dgamma_pre == nullptr && a.dgamma_post == nullptr && a.dres_scale == nullptr && !(shared && cut.spans > 1))) return e;
-    const int64_t jobs = 2 + (shared && cut.spans > 1 ? cut.items / cut.spans : 0);
-    k_block_norm_join<D><<<static_cast<unsigned>(jobs * ((a.D + JC - 1) / JC)), JC * JR, 0, stream>>>(a, cut);
+    if (e != cudaSuccess || (a.dgamma_pre == nullptr && a.dgamma_post == nullptr && a.dres_scale == nullptr && !shared)) return e;
+    const int64_t gates = shared ? (a.M + a.gate_rows - 1) / a.gate_rows : 0, gate_jobs = gates < GATE_JOBS ? gates : GATE_JOBS;
+    k_block_norm_join<D><<<static_cast<unsigned>((2 + gate_jobs) * ((a.D + JC - 1) / JC)), JC * JR, 0, stream>>>(a, cut, gates);
     return cudaGetLastError();
 }
 
@@ -585,13 +636,12 @@ cudaError_t launch_block_norm(int dtype, const BlockNorm& a, cudaStream_t stream
 }
 size_t block_norm_backward_bytes(int64_t M, int64_t gate_rows, int D) {
     if (M == 0) return 0;
-    const int tpr = row_plan(D).tpr;
-    const size_t one = norm_cut(M, gate_rows, D, tpr, false).total, each = norm_cut(M, gate_rows, D, tpr, gate_rows > 1).total;
-    return (one > each ? one : each) * 4;
+    return norm_cut(M, D, row_plan(D).tpr, gate_rows > 1).total * 4;
 }
 cudaError_t launch_block_norm_backward(int dtype, const BlockNorm& a, cudaStream_t stream) {
     const RowPlan p = row_plan(a.D);
-    return dtype == SDM_F32 ? backward<F32>(p, a, stream) : backward<BF16>(p, a, stream);
+    if (a.gate != nullptr && a.gate_rows == 1) return dtype == SDM_F32 ? backward<F32, true>(p, a, stream) : backward<BF16, true>(p, a, stream);
+    return dtype == SDM_F32 ? backward<F32, false>(p, a, stream) : backward<BF16, false>(p, a, stream);
 }
 
 }  // namespace sdm

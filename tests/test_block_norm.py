@@ -89,6 +89,8 @@ CASES = [  # M, D, dtype, gate_rows, which of gate, res_scale, gamma_post, gamma
     (130, 516, "f32", 1, "gsop"), (67, 2048, "bf16", 30, "gsop"), (9, 4100, "f32", 4, "gsop"), (7, 8200, "bf16", 3, "gsop"), (3, 16384, "bf16", 1, "gsop"),
     (5, 16384, "f32", 5, "gsop"), (4000, 128, "bf16", 1500, "gsop"), (1300, 1032, "bf16", 1300, "gsop"), (64, 512, "bf16", 100, "gp"), (21, 320, "f32", 1, ""),
     (21, 320, "bf16", 1, "p"), (40, 1024, "bf16", 1, "sp"), (40, 1024, "bf16", 7, "go"), (2500, 64, "f32", 2, "gso"), (40, 72, "bf16", 1, "op"),
+    (3000, 2048, "bf16", 7, "gsop"), (3001, 1544, "f32", 17, "gsop"), (9000, 256, "bf16", 2, "gp"), (2000, 2048, "f32", 290, "go"),
+    (900, 8192, "bf16", 3, "gsop"), (700, 8192, "bf16", 200, "gsop"), (700, 8192, "bf16", 1, "gsop"),
 ]
 
 
