@@ -1,16 +1,16 @@
 // The global norm of many gradients, and clipping by it:
 //   norm = sqrt(sum over all tensors of g^2),  out = g min(1, max_norm / norm).
 //
-// Bound by memory: one pass reads everything for the norm, the second reads it again and writes.  The second walks the
-// blocks backwards, so that what the first read last is still in L2.
+// Bound by memory: one pass reads everything for the norm, the second reads it again and writes.  Both cut the list's blocks
+// of 32 KB into one range a CTA, and the second walks every range backwards, so that what the first read last is still in L2.
+// The loads of a block are on their way while the one before is worked on.
 //
-// The list goes to the kernels in their parameters (TABLE tensors a launch): nothing is copied to the device first, and a
-// captured launch holds its list.  A CTA takes blocks of BLOCK bytes of one tensor; its sums go to the workspace, and
-// are joined in order, so the norm is the same on every call.
+// The list goes to the kernels in their parameters: nothing is copied to the device first, and a captured launch holds its
+// list.  A CTA's sums go to the workspace and are joined in order (by every CTA of the second pass for itself), so the
+// norm is the same on every call.
 //
 // Squares of float32 values run out of float32's range at 2^64 and 2^-63, long before the values do, so three sums are kept:
-// of x^2, (2^-80 x)^2 and (2^80 x)^2.  The joining kernel takes the first unless it overflowed or is so small that
-// squares were lost.
+// of x^2, (2^-80 x)^2 and (2^80 x)^2.  The first counts unless it overflowed or is so small that squares were lost.
 #include "dla_internal.h"
 #include "sdm_common.cuh"
 
@@ -20,37 +20,41 @@ namespace {
 
 constexpr int GT = 256, PIECES = 8;              // threads; pieces of 16 bytes of the gradient a thread
 constexpr int64_t BLOCK = GT * PIECES * 16;      // bytes of the gradient a block
-constexpr int TABLE = 120;
+constexpr int CTAS = 152 * 2;                    // of 256 threads of up to 128 registers, a launch
+constexpr int FEW = 64, MANY = 960;              // tensors a launch: a long table takes longer to launch
 
-struct GradTable {
-    const void* src[TABLE];
-    void* dst[TABLE];
-    int64_t n[TABLE];
-    int first[TABLE + 1];                        // the tensor's first block of this launch
-    unsigned char kind[TABLE];                   // bit 0: src is bf16; bit 1: dst is bf16; bit 2: one by one (addresses that do not match)
-    int count;
+struct Entry {
+    const void* src;
+    void* dst;
+    int64_t n;
+    int first;                                   // the tensor's first block of this launch
+    int kind;                                    // bit 0: src is bf16; bit 1: dst is bf16; bit 2: one by one (addresses that do not match)
 };
-static_assert(sizeof(GradTable) <= 3900, "kernel parameters");
+template <int N>
+struct GradTable {
+    int count, blocks, per;                      // tensors, their blocks, blocks a CTA
+    Entry e[N];
+};
+static_assert(sizeof(GradTable<MANY>) <= 32000, "kernel parameters");
 
-template <bool B> struct Type { using D = F32; };
-template <> struct Type<true> { using D = BF16; };
-
-__device__ __forceinline__ int find(const GradTable& t, int block) {
-    int lo = 0, hi = t.count;                    // first[lo] <= block < first[hi]
+// The tensor of a block.
+template <int N>
+__device__ __forceinline__ int find(const GradTable<N>& t, int block) {
+    int lo = 0, hi = t.count;
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        if (t.first[mid] <= block) lo = mid;
+        if (t.e[mid].first <= block) lo = mid;
         else hi = mid;
     }
     return lo;
 }
 constexpr float UP = 1208925819614629174706176.f, DOWN = 1.f / UP;      // 2^80
 
-__device__ __forceinline__ void add_square(float x, float (&s)[3]) {
-    const float d = x * DOWN, u = x * UP;
-    s[0] = fmaf(x, x, s[0]);
-    s[1] = fmaf(d, d, s[1]);
-    s[2] = fmaf(u, u, s[2]);
+__device__ __forceinline__ void add_squares(float2 x, float2 (&s)[3]) {
+    const float2 d = __fmul2_rn(x, make_float2(DOWN, DOWN)), u = __fmul2_rn(x, make_float2(UP, UP));
+    s[0] = __ffma2_rn(x, x, s[0]);
+    s[1] = __ffma2_rn(d, d, s[1]);
+    s[2] = __ffma2_rn(u, u, s[2]);
 }
 
 // Elements of a tensor before its first 16-byte boundary (all of them are whole elements away from it).
@@ -59,40 +63,67 @@ template <class D> __device__ __forceinline__ int head_of(const void* p, int64_t
     return h < n ? h : static_cast<int>(n);
 }
 
+// Where the pieces of a block lie.
+struct Span {
+    const uint4* at;                             // this thread's first
+    int64_t left;                                // pieces from there to the tensor's end
+};
 template <class D>
-__device__ __forceinline__ void squares(const void* src, int64_t n, int64_t block, float (&s)[3]) {
-    using T = typename D::T;
-    const T* p = static_cast<const T*>(src);
-    const int head = head_of<D>(src, n);
-    const int64_t pieces = (n - head) / D::E, first = block * (GT * PIECES) + threadIdx.x;
-    const uint4* v = reinterpret_cast<const uint4*>(p + head);
-    uint4 u[PIECES];
+__device__ __forceinline__ Span span_of(const Entry& e, int block, int& head) {
+    head = head_of<D>(e.src, e.n);
+    const int64_t first = static_cast<int64_t>(block - e.first) * (GT * PIECES) + threadIdx.x;
+    return Span{reinterpret_cast<const uint4*>(static_cast<const typename D::T*>(e.src) + head) + first, (e.n - head) / D::E - first};
+}
+__device__ __forceinline__ void load_block(const Entry& e, int block, uint4 (&u)[PIECES]) {
+    int head;
+    const Span p = e.kind & 1 ? span_of<BF16>(e, block, head) : span_of<F32>(e, block, head);
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) u[i] = first + i * GT < pieces ? __ldg(v + first + i * GT) : make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < PIECES; ++i) u[i] = i * GT < p.left ? __ldg(p.at + i * GT) : make_uint4(0, 0, 0, 0);
+}
+template <class D>
+__device__ __forceinline__ void squares(const Entry& e, int block, const uint4 (&u)[PIECES], float2 (&s)[3]) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        float f[8];
-        unpack16<D>(u[i], f);
+        float2 f[4];
+        unpack16x2<D>(u[i], f);
 #pragma unroll
-        for (int e = 0; e < D::E; ++e) add_square(f[e], s);
+        for (int j = 0; j < D::E / 2; ++j) add_squares(f[j], s);
     }
-    if (block == 0) {                            // what lies before and behind the pieces
-        const int64_t tail = head + pieces * D::E;
-        if (threadIdx.x < head) add_square(load_elem<D>(src, threadIdx.x), s);
-        if (tail + threadIdx.x < n) add_square(load_elem<D>(src, tail + threadIdx.x), s);
+    if (block == e.first) {                      // what lies before and behind the pieces
+        const int head = head_of<D>(e.src, e.n);
+        const int64_t tail = head + (e.n - head) / D::E * D::E;
+        if (threadIdx.x < head) add_squares(make_float2(load_elem<D>(e.src, threadIdx.x), 0.f), s);
+        if (tail + threadIdx.x < e.n) add_squares(make_float2(load_elem<D>(e.src, tail + threadIdx.x), 0.f), s);
     }
 }
 
-__global__ void __launch_bounds__(GT) k_grad_squares(const __grid_constant__ GradTable t, float* __restrict__ part) {
+template <int N>
+__global__ void __launch_bounds__(GT, 2) k_grad_squares(const __grid_constant__ GradTable<N> t, float* __restrict__ part) {
     __shared__ float sh[GT / 32][3];
-    const int at = find(t, blockIdx.x);
-    float s[3] = {0.f, 0.f, 0.f};
-    if (t.kind[at] & 1) squares<BF16>(t.src[at], t.n[at], blockIdx.x - t.first[at], s);
-    else squares<F32>(t.src[at], t.n[at], blockIdx.x - t.first[at], s);
+    const int b0 = blockIdx.x * t.per, b1 = min(b0 + t.per, t.blocks);
+    float2 s2[3] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    int at = find(t, b0);
+    uint4 next[PIECES];
+    load_block(t.e[at], b0, next);
+    for (int b = b0; b < b1; ++b) {
+        const Entry& e = t.e[at];
+        uint4 u[PIECES];
 #pragma unroll
-    for (int i = 0; i < 3; ++i)
+        for (int i = 0; i < PIECES; ++i) u[i] = next[i];
+        if (b + 1 < b1) {
+            while (at + 1 < t.count && t.e[at + 1].first <= b + 1) ++at;
+            load_block(t.e[at], b + 1, next);
+        }
+        if (e.kind & 1) squares<BF16>(e, b, u, s2);
+        else squares<F32>(e, b, u, s2);
+    }
+    float s[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        s[i] = s2[i].x + s2[i].y;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
+    }
     const int warp = threadIdx.x >> 5;
     if ((threadIdx.x & 31) == 0) {
         sh[warp][0] = s[0];
@@ -107,32 +138,33 @@ __global__ void __launch_bounds__(GT) k_grad_squares(const __grid_constant__ Gra
     }
 }
 
-// The norm and the factor from the blocks' sums, in 64 bits and in order.
-__global__ void __launch_bounds__(1024) k_grad_norm(const float* __restrict__ part, int64_t blocks, float max_norm, float* __restrict__ stats) {
-    __shared__ double sh[32][3];
+// The norm and the factor from the shares, in 64 bits and in order; in every thread of the CTA.
+__device__ __forceinline__ float2 norm_of(const float* __restrict__ part, int shares, float max_norm) {
+    __shared__ double sh[GT / 32][3];
     double s[3] = {0, 0, 0};
-    for (int64_t i = threadIdx.x; i < blocks; i += 1024)
+    for (int i = threadIdx.x; i < shares; i += GT)
 #pragma unroll
         for (int j = 0; j < 3; ++j) s[j] += __ldg(part + i * 3 + j);
 #pragma unroll
     for (int j = 0; j < 3; ++j)
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) s[j] += __shfl_xor_sync(0xffffffffu, s[j], o);
-    const int warp = threadIdx.x >> 5;
     if ((threadIdx.x & 31) == 0)
-        for (int j = 0; j < 3; ++j) sh[warp][j] = s[j];
+        for (int j = 0; j < 3; ++j) sh[threadIdx.x >> 5][j] = s[j];
     __syncthreads();
-    if (threadIdx.x != 0) return;
     for (int j = 0; j < 3; ++j) {
         s[j] = 0;
-        for (int w = 0; w < 32; ++w) s[j] += sh[w][j];
+        for (int w = 0; w < GT / 32; ++w) s[j] += sh[w][j];
     }
     const double big = 3.4e38, small = 1e-20;    // below, squares of 2^-63 and less may have counted
     double norm = s[0] <= big && s[0] >= small ? sqrt(s[0]) : s[0] < small ? sqrt(s[2]) * static_cast<double>(DOWN) : sqrt(s[1]) * static_cast<double>(UP);
     if (s[0] != s[0]) norm = s[0];
     const float f = static_cast<float>(norm);
-    stats[0] = f;
-    stats[1] = !(fabsf(f) <= 3.402823466e+38f) ? __int_as_float(0x7fffffff) : norm > max_norm ? static_cast<float>(max_norm / norm) : 1.f;
+    return make_float2(f, !(fabsf(f) <= 3.402823466e+38f) ? __int_as_float(0x7fffffff) : norm > max_norm ? static_cast<float>(max_norm / norm) : 1.f);
+}
+__global__ void __launch_bounds__(GT) k_grad_norm(const float* __restrict__ part, int shares, float max_norm, float* __restrict__ stats) {
+    const float2 f = norm_of(part, shares, max_norm);
+    if (threadIdx.x < 2) stats[threadIdx.x] = threadIdx.x == 0 ? f.x : f.y;
 }
 
 template <class S, class O>
@@ -159,55 +191,63 @@ template <class S, class O> __device__ __forceinline__ void put_piece(void* dst,
     }
 }
 template <class S, class O>
-__device__ __forceinline__ void scale(const void* src, void* dst, int64_t n, int64_t block, bool singly, float f) {
-    if (singly) {
-        const int64_t per = GT * PIECES * S::E, first = block * per;
-        const int64_t last = first + per < n ? first + per : n;
-        for (int64_t i = first + threadIdx.x; i < last; i += GT) put_elem<S, O>(src, dst, i, f);
+__device__ __forceinline__ void scale(const Entry& e, int block, const uint4 (&u)[PIECES], float f) {
+    if (e.kind & 4) {
+        constexpr int64_t per = GT * PIECES * S::E;
+        const int64_t first = static_cast<int64_t>(block - e.first) * per, last = first + per < e.n ? first + per : e.n;
+        for (int64_t i = first + threadIdx.x; i < last; i += GT) put_elem<S, O>(e.src, e.dst, i, f);
         return;
     }
-    const int head = head_of<S>(src, n);
-    const int64_t pieces = (n - head) / S::E, first = block * (GT * PIECES) + threadIdx.x;
-    const uint4* v = reinterpret_cast<const uint4*>(static_cast<const typename S::T*>(src) + head);
-    uint4 u[PIECES];
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) u[i] = first + i * GT < pieces ? __ldcs(v + first + i * GT) : make_uint4(0, 0, 0, 0);
+    int head;
+    const Span p = span_of<S>(e, block, head);
+    const int64_t first = static_cast<int64_t>(block - e.first) * (GT * PIECES) + threadIdx.x;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        if (first + i * GT >= pieces) break;
+        if (i * GT >= p.left) break;
+        const int64_t to = head + (first + i * GT) * S::E;
         if (S::BYTES == O::BYTES && f == 1.f) {
-            *reinterpret_cast<uint4*>(static_cast<typename O::T*>(dst) + head + (first + i * GT) * S::E) = u[i];
+            *reinterpret_cast<uint4*>(static_cast<typename O::T*>(e.dst) + to) = u[i];
             continue;
         }
         float x[8];
         unpack16<S>(u[i], x);
 #pragma unroll
-        for (int e = 0; e < S::E; ++e) x[e] *= f;
-        put_piece<S, O>(dst, head + (first + i * GT) * S::E, x);
+        for (int j = 0; j < S::E; ++j) x[j] *= f;
+        put_piece<S, O>(e.dst, to, x);
     }
-    if (block == 0) {
-        const int64_t tail = head + pieces * S::E;
-        if (threadIdx.x < head) put_elem<S, O>(src, dst, threadIdx.x, f);
-        if (tail + threadIdx.x < n) put_elem<S, O>(src, dst, tail + threadIdx.x, f);
+    if (block == e.first) {
+        const int64_t tail = head + (e.n - head) / S::E * S::E;
+        if (threadIdx.x < head) put_elem<S, O>(e.src, e.dst, threadIdx.x, f);
+        if (tail + threadIdx.x < e.n) put_elem<S, O>(e.src, e.dst, tail + threadIdx.x, f);
     }
 }
 
-__global__ void __launch_bounds__(GT) k_grad_scale(const __grid_constant__ GradTable t, const float* __restrict__ stats) {
-    const int block = gridDim.x - 1 - blockIdx.x;
-    const int at = find(t, block);
-    float f = __ldg(stats + 1);
-    if (f != f) f = 1.f;                         // the norm is not finite: the gradients stay as they are
-    const int kind = t.kind[at];
-    const void* src = t.src[at];
-    void* dst = t.dst[at];
-    if (f == 1.f && src == dst) return;
-    const int64_t n = t.n[at], b = block - t.first[at];
-    const bool singly = kind & 4;
-    switch (kind & 3) {
-        case 0: scale<F32, F32>(src, dst, n, b, singly, f); break;
-        case 1: scale<BF16, F32>(src, dst, n, b, singly, f); break;
-        case 2: scale<F32, BF16>(src, dst, n, b, singly, f); break;
-        default: scale<BF16, BF16>(src, dst, n, b, singly, f); break;
+template <int N>
+__global__ void __launch_bounds__(GT, 2) k_grad_scale(const __grid_constant__ GradTable<N> t, const float* __restrict__ part, int shares, float max_norm,
+                                                      float* __restrict__ stats) {
+    const int b0 = blockIdx.x * t.per, b1 = min(b0 + t.per, t.blocks);
+    int at = find(t, b1 - 1);
+    uint4 next[PIECES];
+    load_block(t.e[at], b1 - 1, next);           // on its way while the shares are joined
+    const float2 nf = norm_of(part, shares, max_norm);
+    if (stats != nullptr && blockIdx.x == 0 && threadIdx.x < 2) stats[threadIdx.x] = threadIdx.x == 0 ? nf.x : nf.y;
+    const float f = nf.y == nf.y ? nf.y : 1.f;   // the norm is not finite: the gradients stay as they are
+    for (int b = b1 - 1; b >= b0; --b) {
+        const Entry& e = t.e[at];
+        uint4 u[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) u[i] = next[i];
+        if (b > b0) {
+            while (t.e[at].first > b - 1) --at;
+            if (f != 1.f || t.e[at].src != t.e[at].dst) load_block(t.e[at], b - 1, next);
+        }
+        if (f == 1.f && e.src == e.dst) continue;
+        switch (e.kind & 3) {
+            case 0: scale<F32, F32>(e, b, u, f); break;
+            case 1: scale<BF16, F32>(e, b, u, f); break;
+            case 2: scale<F32, BF16>(e, b, u, f); break;
+            default: scale<BF16, BF16>(e, b, u, f); break;
+        }
     }
 }
 
@@ -216,61 +256,79 @@ int64_t blocks_of(const sdm_grad_tensor& t) {
     return (bytes + BLOCK - 1) / BLOCK;
 }
 // The next launch's table; `i` goes past what it took.
-int64_t fill(GradTable& t, int64_t n, const sdm_grad_tensor* list, int64_t& i) {
+template <int N>
+void fill(GradTable<N>& t, int64_t n, const sdm_grad_tensor* list, int64_t& i) {
     t.count = 0;
     int64_t blocks = 0;
-    for (; i < n && t.count < TABLE; ++i) {
+    for (; i < n && t.count < N; ++i) {
         const sdm_grad_tensor& g = list[i];
         const int64_t b = blocks_of(g);
         if (b == 0) continue;
-        if (blocks + b > INT32_MAX) break;
-        const int k = t.count++;
-        t.src[k] = g.grad;
-        t.dst[k] = g.out;
-        t.n[k] = g.n;
-        t.first[k] = static_cast<int>(blocks);
+        if (blocks + b > INT32_MAX / 2) break;
         const bool half = g.dtype == SDM_BF16, out_half = g.out_dtype == SDM_BF16;
         // the pieces of src begin on 16 bytes; those of dst must begin on their own size
         const uintptr_t s = reinterpret_cast<uintptr_t>(g.grad), d = reinterpret_cast<uintptr_t>(g.out);
         const uintptr_t head = ((16 - s % 16) % 16) / (half ? 2 : 4) * (out_half ? 2 : 4);
         const uintptr_t need = !half && out_half ? 8 : 16;
-        t.kind[k] = static_cast<unsigned char>((half ? 1 : 0) | (out_half ? 2 : 0) | ((d + head) % need != 0 ? 4 : 0));
+        t.e[t.count++] = Entry{g.grad, g.out, g.n, static_cast<int>(blocks), (half ? 1 : 0) | (out_half ? 2 : 0) | ((d + head) % need != 0 ? 4 : 0)};
         blocks += b;
     }
-    t.first[t.count] = static_cast<int>(blocks);
-    return blocks;
+    t.blocks = static_cast<int>(blocks);
+    t.per = static_cast<int>((blocks + CTAS - 1) / CTAS);
+}
+template <int N>
+unsigned grid_of(const GradTable<N>& t) { return static_cast<unsigned>((t.blocks + t.per - 1) / t.per); }
+
+int64_t tensors_of(int64_t n, const sdm_grad_tensor* t) {
+    int64_t some = 0;
+    for (int64_t i = 0; i < n; ++i) some += t[i].n > 0;
+    return some;
+}
+
+template <int N>
+cudaError_t run(int64_t n, const sdm_grad_tensor* list, bool write, float max_norm, float* stats, float* part, cudaStream_t stream) {
+    GradTable<N> t;
+    int64_t shares = 0;
+    bool one = false;                            // table: it still stands for the second pass
+    for (int64_t i = 0; i < n;) {
+        fill(t, n, list, i);
+        if (t.count == 0) break;
+        one = shares == 0 && i == n;
+        k_grad_squares<N><<<grid_of(t), GT, 0, stream>>>(t, part + shares * 3);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        shares += grid_of(t);
+    }
+    const int s = static_cast<int>(shares);
+    if (!write || shares == 0) {
+        k_grad_norm<<<1, GT, 0, stream>>>(part, s, max_norm, stats);
+        return cudaGetLastError();
+    }
+    for (int64_t i = 0; i < n;) {
+        if (one) i = n;
+        else fill(t, n, list, i);
+        if (t.count == 0) break;
+        k_grad_scale<N><<<grid_of(t), GT, 0, stream>>>(t, part, s, max_norm, stats);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace
 
+// A share is three floats; every launch has at most CTAS of them, and at least MANY tensors or 2^30 blocks but the last.
 size_t grad_bytes(int64_t n, const sdm_grad_tensor* t) {
-    size_t blocks = 0;
+    size_t shares = 0, blocks = 0;
     for (int64_t i = 0; i < n; ++i) blocks += static_cast<size_t>(blocks_of(t[i]));
-    return blocks * 3 * 4;
+    shares = (static_cast<size_t>(tensors_of(n, t)) + FEW - 1) / FEW + blocks / (1u << 29) + 1;
+    shares *= CTAS;
+    return (blocks < shares ? blocks : shares) * 3 * 4;
 }
 
 cudaError_t launch_grad(int64_t n, const sdm_grad_tensor* list, bool write, float max_norm, float* stats, void* ws, cudaStream_t stream) {
-    GradTable t;
-    float* const part = static_cast<float*>(ws);
-    int64_t done = 0;
-    for (int64_t i = 0; i < n;) {
-        const int64_t blocks = fill(t, n, list, i);
-        if (blocks == 0) break;
-        k_grad_squares<<<static_cast<unsigned>(blocks), GT, 0, stream>>>(t, part + done * 3);
-        const cudaError_t e = cudaGetLastError();
-        if (e != cudaSuccess) return e;
-        done += blocks;
-    }
-    k_grad_norm<<<1, 1024, 0, stream>>>(part, done, max_norm, stats);
-    cudaError_t e = cudaGetLastError();
-    if (!write) return e;
-    for (int64_t i = 0; i < n && e == cudaSuccess;) {
-        const int64_t blocks = fill(t, n, list, i);
-        if (blocks == 0) break;
-        k_grad_scale<<<static_cast<unsigned>(blocks), GT, 0, stream>>>(t, stats);
-        e = cudaGetLastError();
-    }
-    return e;
+    return tensors_of(n, list) <= FEW ? run<FEW>(n, list, write, max_norm, stats, static_cast<float*>(ws), stream)
+                                      : run<MANY>(n, list, write, max_norm, stats, static_cast<float*>(ws), stream);
 }
 
 }  // namespace sdm
