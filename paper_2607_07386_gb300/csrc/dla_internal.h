@@ -33,8 +33,8 @@ struct DlaWalk {
     int roles;
     DlaRole role[3];
     // The tokens may be cut into `segs` pieces of `seg_chunks` chunks that run at once: a first launch copies the first
-    // state and takes what each piece but the last adds to it into seg_state [role][B * H][segs][da * db], the second
-    // starts every piece from their sums.
+    // state and takes what each piece but the last adds to it into seg_state [role][B * H][segs][da * db], a small one turns
+    // that into the states that the pieces start from, and the walk proper takes them.
     int segs, seg_chunks;
     float* seg_state;
     int64_t seg_role[3];      // where a role's sums start, in floats
@@ -64,6 +64,8 @@ cudaError_t launch_dla(int dtype, const DlaWalk& w, cudaStream_t stream);
 bool dla_scan_supported(int dtype, const DlaWalk& w);
 void dla_scan_plan(DlaWalk& w);
 cudaError_t launch_dla_scan(const DlaWalk& w, cudaStream_t stream);
+// The states that the pieces start from, chunks of `chunk` tokens.
+cudaError_t launch_dla_prefix(const DlaWalk& w, int chunk, cudaStream_t stream);
 // dq and dk [heads of k] = sums over the `group` value heads of their shares [B, H, T, d] float32.
 cudaError_t launch_dla_join(int dtype, const float* pq, const float* pk, void* dq, void* dk, int B, int Hk, int group, int T, int d, int token_major,
                             cudaStream_t stream);

@@ -435,15 +435,14 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
         const int64_t per = static_cast<int64_t>(da) * db;
         const int64_t at = ro.transposed ? static_cast<int64_t>(col) * da : col, step = ro.transposed ? 1 : db;
         float2 S[RD / 2];
-        // `keep` times S plus the state at p
-        auto read = [&](const float* p, float keep, bool start) {
+        auto read = [&](const float* p) {
+            const float* q = p + at + x0 * step;
 #pragma unroll
             for (int x = 0; x < RD / 2; ++x) {
-                if (x % 4 == 0) asm volatile("" ::: "memory");       // eight values in flight, and no more registers
-                const int r = x0 + 2 * x;                    // da is a multiple of 8
-                const bool on = live && r < da && p != nullptr;
-                const float a = on ? __ldcg(p + at + r * step) : 0.f, d = on ? __ldcg(p + at + (r + 1) * step) : 0.f;
-                S[x] = start ? make_float2(a, d) : make_float2(fmaf(keep, S[x].x, a), fmaf(keep, S[x].y, d));
+                if (x % 16 == 0) asm volatile("" ::: "memory");      // 32 values in flight, and no more registers
+                const bool on = live && x0 + 2 * x < da && p != nullptr;     // da is a multiple of 8
+                S[x] = make_float2(on ? __ldcg(q) : 0.f, on ? __ldcg(q + step) : 0.f);
+                q += 2 * step;
             }
         };
         auto write = [&](float* p) {
@@ -456,27 +455,17 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
                 }
             }
         };
-        // Pieces: [0] is the first state, [s + 1] what segment s adds.
+        // Pieces: [0] is the first state, [s + 1] what segment s adds, and for the second launch the state after it.
         float* const pieces = w.seg_state + w.seg_role[role] + chain * w.segs * per;
         if (SUMS) {
             if (seg == 0) {
-                read(ro.state_in == nullptr ? nullptr : ro.state_in + chain * per, 0.f, true);
+                read(ro.state_in == nullptr ? nullptr : ro.state_in + chain * per);
                 write(pieces);
             }
 #pragma unroll
             for (int x = 0; x < RD / 2; ++x) S[x] = make_float2(0.f, 0.f);
-        } else if (w.segs == 1) {
-            read(ro.state_in == nullptr ? nullptr : ro.state_in + chain * per, 0.f, true);
         } else {
-            read(pieces, 0.f, true);
-            const float full = dla_pow(ld, w.seg_chunks * C);
-            for (int s = 0; s < seg; ++s) {
-                const int s0 = min(s * w.seg_chunks, chunks), s1 = min(s0 + w.seg_chunks, chunks);
-                if (s0 == s1) break;
-                int n = (s1 - s0) * C;                       // the walk's partial chunk is the sequence's last
-                if (reverse ? s0 == 0 : s1 == chunks) n -= C - last_n;
-                read(pieces + (s + 1) * per, n == w.seg_chunks * C ? full : dla_pow(ld, n), false);
-            }
+            read(w.segs > 1 ? pieces + seg * per : ro.state_in == nullptr ? nullptr : ro.state_in + chain * per);
         }
         auto put = [&]() {                                   // S before the next chunk
             if (SUMS) return;
@@ -549,6 +538,7 @@ template <int DA>
 cudaError_t scans(const ScanMaps& maps, const DlaWalk& w, cudaStream_t stream) {
     if (w.segs > 1) {
         cudaError_t e = scan<DA, true>(maps, w, stream);
+        if (e == cudaSuccess) e = launch_dla_prefix(w, C, stream);
         if (e != cudaSuccess) return e;
     }
     return scan<DA, false>(maps, w, stream);
@@ -564,9 +554,19 @@ int widest(const DlaWalk& w) {
 
 bool dla_scan_supported(int dtype, const DlaWalk& w) { return dtype == SDM_BF16 && widest(w) <= 128 && w.T >= 32; }
 
+// With fewer CTAs than half of the SMs the tokens are cut, so that every SM has a piece, where that pays: a chunk takes 2.1 us
+// in the walk and about 1.1 in the walk for the sums, which with the joining launch costs 10 us more to begin with.
 void dla_scan_plan(DlaWalk& w) {
-    w.segs = 1;
-    w.seg_chunks = (w.T + C - 1) / C;
+    constexpr int64_t SMS = 152;
+    int64_t ctas = 0;
+    for (int i = 0; i < w.roles; ++i) ctas += (w.role[i].db + 127) / 128;
+    ctas *= static_cast<int64_t>(w.B) * w.H;
+    const int64_t chunks = (w.T + C - 1) / C;
+    int64_t segs = SMS / ctas;
+    if (segs > chunks / 2) segs = chunks / 2;
+    if (segs < 2 || chunks * (2 * segs - 3) <= 10 * segs) segs = 1;
+    w.seg_chunks = static_cast<int>((chunks + segs - 1) / segs);
+    w.segs = static_cast<int>((chunks + w.seg_chunks - 1) / w.seg_chunks);
 }
 
 cudaError_t launch_dla_scan(const DlaWalk& w, cudaStream_t stream) {

@@ -118,40 +118,21 @@ __global__ void __launch_bounds__(WT) k_dla_walk(const DlaWalk w, const int3 sli
         for (int e = 0; e < 4; ++e) S[i][e] = 0.f;
     const int64_t per = static_cast<int64_t>(da) * db;
     auto at = [&](int x, int c) { return ro.transposed ? static_cast<int64_t>(col0 + c) * da + x : static_cast<int64_t>(x) * db + col0 + c; };
-    // Pieces: [0] is the first state, [s + 1] what segment s adds.
+    // Pieces: [0] is the first state, [s + 1] what segment s adds, and for the second launch the state after it.
     float* const pieces = w.seg_state + w.seg_role[role] + chain * w.segs * per;
-    if (SUMS ? seg == 0 : w.segs == 1) {
-        if (ro.state_in != nullptr) {
+    if (!SUMS || seg == 0) {
+        const float* const from = !SUMS && w.segs > 1 ? pieces + seg * per : ro.state_in == nullptr ? nullptr : ro.state_in + chain * per;
 #pragma unroll
-            for (int i = 0; i < R; ++i)
+        for (int i = 0; i < R; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (x0 + i < da && col0 + cg + e < db) S[i][e] = ro.state_in[chain * per + at(x0 + i, cg + e)];
-        }
-        if (SUMS) {
-#pragma unroll
-            for (int i = 0; i < R; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (x0 + i < da && col0 + cg + e < db) pieces[at(x0 + i, cg + e)] = S[i][e];
+            for (int e = 0; e < 4; ++e) {
+                const bool on = x0 + i < da && col0 + cg + e < db;
+                if (on && from != nullptr) S[i][e] = from[at(x0 + i, cg + e)];
+                if (SUMS) {
+                    if (on) pieces[at(x0 + i, cg + e)] = S[i][e];
                     S[i][e] = 0.f;
                 }
-        }
-    } else if (!SUMS) {
-        const float full = dla_pow(ld, w.seg_chunks * C);
-        for (int s = -1; s < seg; ++s) {
-            const int s0 = min(s * w.seg_chunks, chunks), s1 = min(s0 + w.seg_chunks, chunks);
-            if (s >= 0 && s0 == s1) break;
-            int n = (s1 - s0) * C;                           // the walk's partial chunk is the sequence's last
-            if (ro.reverse ? s0 == 0 : s1 == chunks) n -= chunks * C - len;
-            const float f = s < 0 ? 0.f : n == w.seg_chunks * C ? full : dla_pow(ld, n);
-            const float* add = pieces + (s + 1) * per;
-#pragma unroll
-            for (int i = 0; i < R; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (x0 + i < da && col0 + cg + e < db) S[i][e] = s < 0 ? add[at(x0 + i, cg + e)] : fmaf(f, S[i][e], add[at(x0 + i, cg + e)]);
-        }
+            }
     }
 
     const int ti = (tid >> 4) * 2, tc = (tid & 15) * 2;
@@ -276,6 +257,7 @@ template <class D, int DA>
 cudaError_t walks(const DlaWalk& w, cudaStream_t stream) {
     if (w.segs > 1) {
         cudaError_t e = walk<D, DA, true>(w, stream);
+        if (e == cudaSuccess) e = launch_dla_prefix(w, C, stream);
         if (e != cudaSuccess) return e;
     }
     return walk<D, DA, false>(w, stream);
@@ -285,6 +267,29 @@ cudaError_t walk_width(const DlaWalk& w, cudaStream_t stream) {
     int da = 0;
     for (int i = 0; i < w.roles; ++i) da = w.role[i].da > da ? w.role[i].da : da;
     return da <= 64 ? walks<D, 64>(w, stream) : da <= 128 ? walks<D, 128>(w, stream) : walks<D, 256>(w, stream);
+}
+
+// The states at the starts of the pieces from what the pieces add; four values a thread.
+__global__ void __launch_bounds__(256) k_dla_prefix(const DlaWalk w, int C) {
+    const int role = blockIdx.z % w.roles, b = blockIdx.z / w.roles, h = blockIdx.y;
+    const DlaRole& ro = w.role[role];
+    const int per = ro.da * ro.db, i = (blockIdx.x * 256 + threadIdx.x) * 4;      // a multiple of 16
+    if (i >= per) return;
+    const int len = dla_length(w, b), chunks = (len + C - 1) / C;
+    const float ld = __ldg(w.log_decay + h);
+    float4* p = reinterpret_cast<float4*>(w.seg_state + w.seg_role[role] + (static_cast<int64_t>(b) * w.H + h) * w.segs * per + i);
+    float4 S = *p;
+    for (int s = 0; s + 1 < w.segs; ++s) {
+        p += per / 4;
+        const int s0 = min(s * w.seg_chunks, chunks), s1 = min(s0 + w.seg_chunks, chunks);
+        int n = (s1 - s0) * C;                               // the walk's partial chunk is the sequence's last
+        if (s0 < s1 && (ro.reverse ? s0 == 0 : s1 == chunks)) n -= chunks * C - len;
+        const float f = dla_pow(ld, n);
+        const float4 add = *p;
+        S.x = fmaf(f, S.x, add.x); S.y = fmaf(f, S.y, add.y);
+        S.z = fmaf(f, S.z, add.z); S.w = fmaf(f, S.w, add.w);
+        *p = S;
+    }
 }
 
 // Sum over the value heads of a key head, in order, rounded once; four values a thread.
@@ -396,6 +401,13 @@ void dla_plan(int dtype, DlaWalk& w) {
 cudaError_t launch_dla(int dtype, const DlaWalk& w, cudaStream_t stream) {
     if (dla_scan_supported(dtype, w)) return launch_dla_scan(w, stream);
     return dtype == SDM_F32 ? walk_width<F32>(w, stream) : walk_width<BF16>(w, stream);
+}
+
+cudaError_t launch_dla_prefix(const DlaWalk& w, int chunk, cudaStream_t stream) {
+    int per = 0;
+    for (int i = 0; i < w.roles; ++i) per = w.role[i].da * w.role[i].db > per ? w.role[i].da * w.role[i].db : per;
+    k_dla_prefix<<<dim3((per / 4 + 255) / 256, w.H, w.B * w.roles), 256, 0, stream>>>(w, chunk);
+    return cudaGetLastError();
 }
 
 cudaError_t launch_dla_join(int dtype, const float* pq, const float* pk, void* dq, void* dk, int B, int Hk, int group, int T, int d, int token_major,

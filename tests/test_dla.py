@@ -160,6 +160,12 @@ CASES = [  # B, H, Hk, T, dk, dv, dtype, layout, lengths
     (2, 1, 1, 777, 8, 8, "bf16", "head_major", [777, 129]),
     (1, 3, 1, 500, 32, 192, "bf16", "head_major", None),
     (2, 20, 20, 150, 160, 32, "bf16", "token_major", None),
+    # few chains: the tokens in pieces, some past a sequence's end
+    (3, 2, 1, 1100, 128, 128, "bf16", "token_major", [1100, 0, 513]),
+    (1, 1, 1, 3000, 64, 64, "bf16", "head_major", None),
+    (2, 1, 1, 900, 96, 200, "bf16", "head_major", [300, 897]),
+    (1, 1, 1, 700, 40, 64, "f32", "head_major", None),
+    (2, 2, 1, 420, 128, 96, "f32", "token_major", [33, 420]),
 ]
 
 
