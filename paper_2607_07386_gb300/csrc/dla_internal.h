@@ -1,6 +1,7 @@
 // Linear attention with a decay per head: what the C ABI hands to the kernels.
 #pragma once
 #include "gdn_internal.h"
+#include "sdm_common.cuh"
 
 namespace sdm {
 
@@ -47,6 +48,12 @@ __device__ __forceinline__ float dla_pow(float ld, int n) {
     if (!gdn_finite(hi)) return e;
     return fmaf(e, fmaf(f, ld, -hi), e);
 }
+// The same as two floats: multiplied on once a chunk, a factor that is off by 2^-25 would be off by as much again every time.
+__device__ __forceinline__ float2 dla_pow2(float ld, int n) {
+    const double f = n == 0 ? 1.0 : exp(static_cast<double>(n) * static_cast<double>(ld));
+    const float hi = static_cast<float>(f);
+    return make_float2(hi, gdn_finite(hi) ? static_cast<float>(f - static_cast<double>(hi)) : 0.f);
+}
 __device__ __forceinline__ int dla_length(const DlaWalk& w, int b) {
     if (w.lengths == nullptr) return w.T;
     const int n = __ldg(w.lengths + b);
@@ -55,6 +62,22 @@ __device__ __forceinline__ int dla_length(const DlaWalk& w, int b) {
         return n < 0 ? 0 : w.T;
     }
     return n;
+}
+
+// Zeros in columns [col0, col0 + cols) of the outputs of tokens `from` and on, in pieces of 16 bytes; every segment's CTA writes
+// its share.
+template <class D>
+__device__ __forceinline__ void dla_zero_tail(const DlaWalk& w, const DlaRole& ro, int b, int h, int col0, int cols, int from, int seg, int tid, int threads) {
+    const int es = ro.partial ? 4 : D::BYTES, pieces = cols * es / 16, each = (w.T - from + w.segs - 1) / w.segs;
+    const int t0 = from + seg * each, t1 = t0 + each < w.T ? t0 + each : w.T;
+    if (t0 >= t1) return;
+    const int64_t stride = ro.partial ? ro.db : gdn_stride(w.token_major, w.H, ro.db);
+    const int64_t base = ro.partial ? (static_cast<int64_t>(b) * w.H + h) * w.T * ro.db : gdn_base(w.token_major, b, h, w.H, w.T, ro.db);
+    char* const out = static_cast<char*>(ro.out) + (base + col0) * es;
+    const int rows = threads / pieces, row = tid / pieces;       // rows at once
+    if (row >= rows) return;
+    for (int64_t t = t0 + row; t < t1; t += rows)
+        *reinterpret_cast<uint4*>(out + t * stride * es + tid % pieces * 16) = make_uint4(0, 0, 0, 0);
 }
 
 // Fills in segs and seg_chunks; runs the walks.

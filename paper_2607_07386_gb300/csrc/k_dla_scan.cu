@@ -10,7 +10,8 @@
 // what lies past the length out of the products.
 //
 // bf16 parts: g v has 8 + 24 significant bits, three parts keep 24 of them, so that the state is as good as a float32
-// sum; S and the weighted P only reach outputs that are rounded to 2^-9, and two parts keep 16 bits.
+// sum; S and the weighted P only reach outputs that are rounded to 2^-9, and two parts keep 16 bits, as they do for g v where
+// no state is asked for.
 //
 // Only D goes from one chunk to the next, and it does not depend on S: six groups of warps work on different stages of
 // neighbouring chunks, each handing over through mbarriers.
@@ -107,6 +108,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
     auto partial = [&](int c) { return chunk_at(c) == chunks - 1 && last_n < C; };
     const int64_t chain = static_cast<int64_t>(b) * w.H + h;
     const float ld = __ldg(w.log_decay + h);
+    const int parts = ro.state_out != nullptr ? 3 : 2;       // of g v
     const uint32_t bars = smem_u32(&ctl.bar[0]);
     auto bar = [&](int i) { return bars + 8 * i; };
     if (tid == 0) {
@@ -120,10 +122,9 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
     if (tid <= C) ctl.pw[tid] = dla_pow(ld, tid);
     if (tid >= 96 && tid < 98) {
         const int n = tid == 96 ? C : last_n;
-        const double f = n == 0 ? 1.0 : exp(static_cast<double>(n) * static_cast<double>(ld));
-        const float hi = static_cast<float>(f), lo = static_cast<float>(f - static_cast<double>(hi));
-        ctl.lam[tid - 96][0] = hi;
-        ctl.lam[tid - 96][1] = gdn_finite(hi) ? lo : 0.f;
+        const float2 f = dla_pow2(ld, n);
+        ctl.lam[tid - 96][0] = f.x;
+        ctl.lam[tid - 96][1] = f.y;
     }
     __syncthreads();
     if (tid < 2 * C) {
@@ -152,7 +153,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
             const uint32_t lanes = tmem + (static_cast<uint32_t>(me * 32) << 16);
             const float* const wt = ctl.W + i * WP;
             unsigned char* const ps = ringp + L::PS;
-            for (int c = 0; !SUMS && c < todo; ++c) {
+            for (int c = 0; c < (SUMS ? 0 : todo); ++c) {
                 await(bar(B_P), c & 1, dead);
                 unsigned char* const to = ps + (c & 1) * 2 * MAT;
                 // A token past this one counts as zero, and where it is not finite, not as 0 times it: such products show in
@@ -217,10 +218,10 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
                 auto kv = [&](int x) {                       // 4, for 64 rows of da; lower parts first, here and below: their sums are small
                     if (elect_one()) {
 #pragma unroll 1
-                        for (int p = 2; p >= 0; --p)
+                        for (int p = parts - 1; p >= 0; --p)
 #pragma unroll
                             for (int kk = 0; kk < C / 16; ++kk)
-                                mma_bf16_ta(tmem + D_COL, tmem + V_COL + p * 32 + kk * 8, dkt + x * 1024 + kk * 128, id64 | MN_B, p != 2 || kk != 0);
+                                mma_bf16_ta(tmem + D_COL, tmem + V_COL + p * 32 + kk * 8, dkt + x * 1024 + kk * 128, id64 | MN_B, p != parts - 1 || kk != 0);
                         mma_commit(bar(B_D + x));
                         if (SUMS && x == DA / 64 - 1) mma_commit(bar(B_FREE + s));
                     }
@@ -356,14 +357,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
         }
         if (!SUMS) {
             if (warp == SW + VW && lane == 0) bulk_wait();
-            if (seg == w.segs - 1 && col < ro.db) {          // chunks past the length
-                __nv_bfloat16* y = static_cast<__nv_bfloat16*>(ro.out) + gdn_base(w.token_major, b, h, w.H, w.T, ro.db) + col;
-                const int64_t ys = gdn_stride(w.token_major, w.H, ro.db);
-                for (int64_t t = static_cast<int64_t>(chunks) * C; t < w.T; ++t) {
-                    if (share) shares[t * ro.db] = 0.f;
-                    else y[t * ys] = __float2bfloat16_rn(0.f);
-                }
-            }
+            dla_zero_tail<BF16>(w, ro, b, h, col0, ro.db - col0 < 128 ? ro.db - col0 : 128, chunks * C, seg, tid - 32 * (SW + VW), 32 * OW);
         }
     } else if (warp >= SW) {                                 // v: column `row`, 32 tokens from i0 on
         if (V_REGS < LAUNCH_REGS) regs_dec<V_REGS>();
@@ -422,7 +416,8 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
             if (lane == 0) mbar_arrive(bar(B_FREE + s));
             if (c > 0) await(bar(B_D + DA / 64 - 1), (c - 1) & 1, dead);
 #pragma unroll
-            for (int p = 0; p < 3; ++p) tmem_st16(lanes + V_COL + 32 * p + i0 / 2, u[p]);
+            for (int p = 0; p < 3; ++p)
+                if (p < parts) tmem_st16(lanes + V_COL + 32 * p + i0 / 2, u[p]);
             announce(bar(B_V), lane);
         }
     } else {                                                 // the state: column `row`, half of da

@@ -19,8 +19,9 @@ constexpr int C = DLA_C32, WT = 256, COLS = 32;
 
 template <int DA>
 struct WalkSmem {
-    float r[C][DA + 4], k[C][DA + 4], v[C][COLS + 4], S[DA][COLS + 4], P[C][C + 1];
-    float pw[C + 1];
+    float r[C][DA + 4], k[C][DA + 4], S[COLS][DA + 4];       // S transposed; rows four banks apart
+    float v[COLS][C + 4], gv[C][COLS + 4], P[C][C + 4];      // v transposed; v times its weight in the state
+    float pw[C + 1], lam[2][2];                              // lam^n; of a whole and of the partial chunk in two parts
 };
 
 template <class D>
@@ -35,6 +36,11 @@ template <> __device__ __forceinline__ void put_pair<F32>(void* out, int64_t at,
 template <> __device__ __forceinline__ void put_pair<BF16>(void* out, int64_t at, float a, float b) {
     *reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(out) + at) = __floats2bfloat162_rn(a, b);
 }
+
+template <class D>
+__device__ __forceinline__ void put_one(void* out, int64_t at, float x);
+template <> __device__ __forceinline__ void put_one<F32>(void* out, int64_t at, float x) { static_cast<float*>(out)[at] = x; }
+template <> __device__ __forceinline__ void put_one<BF16>(void* out, int64_t at, float x) { static_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(x); }
 
 template <class D, int DA, bool SUMS>
 __global__ void __launch_bounds__(WT) k_dla_walk(const DlaWalk w, const int3 slices) {
@@ -83,7 +89,7 @@ __global__ void __launch_bounds__(WT) k_dla_walk(const DlaWalk w, const int3 sli
         const int row = tid / PV, x = col0 + tid % PV * D::E;
         vu = row < n && x < db ? __ldg(token_ptr<D>(ro.v, vb + (t0 + row) * vs + x)) : make_uint4(0, 0, 0, 0);
     };
-    auto put = [&]() {
+    auto put = [&](int n) {
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             const int p = tid + i * WT, row = p / PR, x = p % PR * D::E;
@@ -101,13 +107,21 @@ __global__ void __launch_bounds__(WT) k_dla_walk(const DlaWalk w, const int3 sli
         if (row < C) {
             float f[8];
             unpack16<D>(vu, f);
+            const float g = row < n ? ro.add * (ro.reverse ? sm.pw[row + 1] : sm.pw[n - 1 - row]) : 0.f;
 #pragma unroll
-            for (int e = 0; e < D::E; e += 4) *reinterpret_cast<float4*>(&sm.v[row][x + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+            for (int e = 0; e < D::E; ++e) sm.v[x + e][row] = f[e];
+#pragma unroll
+            for (int e = 0; e < D::E; e += 4) *reinterpret_cast<float4*>(&sm.gv[row][x + e]) = make_float4(g * f[e], g * f[e + 1], g * f[e + 2], g * f[e + 3]);
         }
     };
 
     if (c0 < c1) fetch(c0);
-    if (tid <= C) sm.pw[tid] = dla_pow(ld, tid);
+    if (tid <= C) sm.pw[tid] = dla_pow(ld, tid);             // read after the loop's first barrier
+    if (tid >= 64 && tid < 66) {
+        const float2 f = dla_pow2(ld, tid == 64 ? C : len - (chunks - 1) * C);
+        sm.lam[tid - 64][0] = f.x;
+        sm.lam[tid - 64][1] = f.y;
+    }
     // This thread's part of the state: R rows x 4 columns.
     constexpr int R = DA / 32;
     const int cg = (tid & 7) * 4, x0 = (tid >> 3) * R;
@@ -135,93 +149,136 @@ __global__ void __launch_bounds__(WT) k_dla_walk(const DlaWalk w, const int3 sli
             }
     }
 
-    const int ti = (tid >> 4) * 2, tc = (tid & 15) * 2;
+    // Outputs: rows ti and ti + 1, columns tc and tc + 16 (rows of k, S and v that lie in different banks), of P alike.
+    const int ti = (tid >> 4) * 2, tc = tid & 15;
     for (int c = c0; c < c1; ++c) {
         const int t0 = chunk_at(c) * C, n = tokens_in(c);
         __syncthreads();
-        put();
+        put(n);
         if (!SUMS) {
 #pragma unroll
-            for (int i = 0; i < R; ++i) *reinterpret_cast<float4*>(&sm.S[x0 + i][cg]) = x0 + i < da ? make_float4(S[i][0], S[i][1], S[i][2], S[i][3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < R; i += 2)               // rows past da stay zero, whatever k holds of them
+                    *reinterpret_cast<float2*>(&sm.S[cg + e][x0 + i]) = x0 + i < da ? make_float2(S[i][e], S[i + 1][e]) : make_float2(0.f, 0.f);
         }
         __syncthreads();
         if (c + 1 < c1) fetch(c + 1);
         if (!SUMS) {
-            float p[2][2] = {{0.f, 0.f}, {0.f, 0.f}}, o[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+            float2 p[2][2], o[2][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) p[i][j] = o[i][j] = make_float2(0.f, 0.f);
 #pragma unroll 4
-            for (int x = 0; x < DA; x += 4) {
-                float r[2][4], k[2][4], s[4][2];
+            for (int x = 0; x < da; x += 4) {                // da is a multiple of 4
+                float4 r[2], k[2], s[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const float4 a = *reinterpret_cast<const float4*>(&sm.r[ti + i][x]), d = *reinterpret_cast<const float4*>(&sm.k[tc + i][x]);
-                    r[i][0] = a.x; r[i][1] = a.y; r[i][2] = a.z; r[i][3] = a.w;
-                    k[i][0] = d.x; k[i][1] = d.y; k[i][2] = d.z; k[i][3] = d.w;
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 f = *reinterpret_cast<const float2*>(&sm.S[x + e][tc]);
-                    s[e][0] = f.x; s[e][1] = f.y;
+                    r[i] = *reinterpret_cast<const float4*>(&sm.r[ti + i][x]);
+                    k[i] = *reinterpret_cast<const float4*>(&sm.k[tc + 16 * i][x]);
+                    s[i] = *reinterpret_cast<const float4*>(&sm.S[tc + 16 * i][x]);
                 }
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            p[i][j] = fmaf(r[i][e], k[j][e], p[i][j]);
-                            o[i][j] = fmaf(r[i][e], s[e][j], o[i][j]);
-                        }
+                    for (int j = 0; j < 2; ++j) {
+                        p[i][j] = __ffma2_rn(make_float2(r[i].x, r[i].y), make_float2(k[j].x, k[j].y), p[i][j]);
+                        p[i][j] = __ffma2_rn(make_float2(r[i].z, r[i].w), make_float2(k[j].z, k[j].w), p[i][j]);
+                        o[i][j] = __ffma2_rn(make_float2(r[i].x, r[i].y), make_float2(s[j].x, s[j].y), o[i][j]);
+                        o[i][j] = __ffma2_rn(make_float2(r[i].z, r[i].w), make_float2(s[j].z, s[j].w), o[i][j]);
+                    }
             }
+            float y[2][2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int row = ti + i;
                 const float f = ro.inter * (ro.reverse ? sm.pw[max(n - 1 - row, 0)] : sm.pw[row + 1]);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const int far = ro.reverse ? tc + j - row : row - tc - j;
-                    sm.P[row][tc + j] = far >= 0 ? ro.intra * sm.pw[far >= 0 ? far : 0] * p[i][j] : 0.f;
-                    o[i][j] *= f;
+                    const int col = tc + 16 * j, far = ro.reverse ? col - row : row - col;
+                    sm.P[row][col] = far >= 0 ? ro.intra * sm.pw[far >= 0 ? far : 0] * (p[i][j].x + p[i][j].y) : 0.f;
+                    y[i][j] = f * (o[i][j].x + o[i][j].y);
                 }
             }
             __syncthreads();
-            // a token past this one in the walk is left out by the test, not by a zero: its v may not be finite
+            float2 z[2][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) z[i][j] = make_float2(y[i][j], 0.f);
 #pragma unroll 4
-            for (int j = 0; j < C; ++j) {
-                const float2 v = *reinterpret_cast<const float2*>(&sm.v[j][tc]);
+            for (int j = 0; j < C; j += 4) {
+                float4 q[2], v[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const bool on = ro.reverse ? j >= ti + i : j <= ti + i;
-                    const float q = sm.P[ti + i][j];
-                    if (on) {
-                        o[i][0] = fmaf(q, v.x, o[i][0]);
-                        o[i][1] = fmaf(q, v.y, o[i][1]);
-                    }
+                    q[i] = *reinterpret_cast<const float4*>(&sm.P[ti + i][j]);
+                    v[i] = *reinterpret_cast<const float4*>(&sm.v[tc + 16 * i][j]);
                 }
-            }
-            if (col0 + tc < db) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if (ti + i >= n) continue;
-                    if (ro.partial) put_pair<F32>(ro.out, (chain * w.T + t0 + ti + i) * db + col0 + tc, o[i][0], o[i][1]);
-                    else put_pair<D>(ro.out, gdn_base(w.token_major, b, h, w.H, w.T, db) + (t0 + ti + i) * gdn_stride(w.token_major, w.H, db) + col0 + tc, o[i][0], o[i][1]);
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        z[i][e] = __ffma2_rn(make_float2(q[i].x, q[i].y), make_float2(v[e].x, v[e].y), z[i][e]);
+                        z[i][e] = __ffma2_rn(make_float2(q[i].z, q[i].w), make_float2(v[e].z, v[e].w), z[i][e]);
+                    }
+            }
+            // A token past this one in the walk counts with a zero, but not where its v is not finite: then it is left out by a
+            // test (tests in the loop above took it from 1 to 4.7 thousand cycles).
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float sum = z[i][j].x + z[i][j].y;
+                    if (gdn_finite(sum)) {
+                        y[i][j] = sum;
+                        continue;
+                    }
+                    float2 u = make_float2(y[i][j], 0.f);    // in the same order
+#pragma unroll 1
+                    for (int t = 0; t < C; t += 2) {
+                        if (ro.reverse ? t >= ti + i : t <= ti + i) u.x = fmaf(sm.P[ti + i][t], sm.v[tc + 16 * j][t], u.x);
+                        if (ro.reverse ? t + 1 >= ti + i : t + 1 <= ti + i) u.y = fmaf(sm.P[ti + i][t + 1], sm.v[tc + 16 * j][t + 1], u.y);
+                    }
+                    y[i][j] = u.x + u.y;
+                }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (ti + i >= n) continue;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int col = col0 + tc + 16 * j;
+                    if (col >= db) continue;
+                    if (ro.partial) static_cast<float*>(ro.out)[(chain * w.T + t0 + ti + i) * db + col] = y[i][j];
+                    else put_one<D>(ro.out, gdn_base(w.token_major, b, h, w.H, w.T, db) + (t0 + ti + i) * gdn_stride(w.token_major, w.H, db) + col, y[i][j]);
                 }
             }
         }
-        const float f = sm.pw[n];
+        const float hi = sm.lam[n < C][0], lo = sm.lam[n < C][1];
+        float add[R][4];
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) S[i][e] *= f;
-        for (int j = 0; j < n; ++j) {
-            const float4 v = *reinterpret_cast<const float4*>(&sm.v[j][cg]);
-            const float g = ro.add * (ro.reverse ? sm.pw[j + 1] : sm.pw[n - 1 - j]);
+            for (int e = 0; e < 4; ++e) add[i][e] = lo * S[i][e];
+#pragma unroll 4
+        for (int j = 0; j < (x0 < da ? n : 0); ++j) {
+            const float4 v = *reinterpret_cast<const float4*>(&sm.gv[j][cg]);
+            float k[R];
+#pragma unroll
+            for (int i = 0; i < R; i += 2) {
+                const float2 a = *reinterpret_cast<const float2*>(&sm.k[j][x0 + i]);
+                k[i] = a.x; k[i + 1] = a.y;
+            }
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                const float k = g * sm.k[j][x0 + i];
-                S[i][0] = fmaf(k, v.x, S[i][0]); S[i][1] = fmaf(k, v.y, S[i][1]);
-                S[i][2] = fmaf(k, v.z, S[i][2]); S[i][3] = fmaf(k, v.w, S[i][3]);
+                add[i][0] = fmaf(k[i], v.x, add[i][0]); add[i][1] = fmaf(k[i], v.y, add[i][1]);
+                add[i][2] = fmaf(k[i], v.z, add[i][2]); add[i][3] = fmaf(k[i], v.w, add[i][3]);
             }
         }
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[i][e] = fmaf(hi, S[i][e], add[i][e]);
     }
     float* out = SUMS ? pieces + (seg + 1) * per : ro.state_out != nullptr ? ro.state_out + chain * per : nullptr;
     if (out != nullptr && (SUMS || seg == w.segs - 1)) {
@@ -231,14 +288,7 @@ __global__ void __launch_bounds__(WT) k_dla_walk(const DlaWalk w, const int3 sli
             for (int e = 0; e < 4; ++e)
                 if (x0 + i < da && col0 + cg + e < db) out[at(x0 + i, cg + e)] = S[i][e];
     }
-    if (!SUMS && seg == w.segs - 1) {                        // tokens past the length
-        for (int p = tid; p < (w.T - len) * (COLS / 2); p += WT) {
-            const int t = len + p / (COLS / 2), x = col0 + p % (COLS / 2) * 2;
-            if (x >= db) continue;
-            if (ro.partial) put_pair<F32>(ro.out, (chain * w.T + t) * db + x, 0.f, 0.f);
-            else put_pair<D>(ro.out, gdn_base(w.token_major, b, h, w.H, w.T, db) + t * gdn_stride(w.token_major, w.H, db) + x, 0.f, 0.f);
-        }
-    }
+    if (!SUMS) dla_zero_tail<D>(w, ro, b, h, col0, db - col0 < COLS ? db - col0 : COLS, len, seg, tid, WT);
 }
 
 template <class D, int DA, bool SUMS>
@@ -394,8 +444,18 @@ void dla_plan(int dtype, DlaWalk& w) {
         dla_scan_plan(w);
         return;
     }
-    w.segs = 1;
-    w.seg_chunks = (w.T + C - 1) / C;
+    // The tokens are cut until there are three CTAs for every SM, which hide each other's waits; a piece keeps at least three
+    // chunks.
+    constexpr int64_t SMS = 152;
+    int64_t ctas = 0;
+    for (int i = 0; i < w.roles; ++i) ctas += (w.role[i].db + COLS - 1) / COLS;
+    ctas *= static_cast<int64_t>(w.B) * w.H;
+    const int64_t chunks = (w.T + C - 1) / C;
+    int64_t segs = 3 * SMS / ctas;
+    if (segs > chunks / 3) segs = chunks / 3;
+    if (segs < 1) segs = 1;
+    w.seg_chunks = static_cast<int>((chunks + segs - 1) / segs);
+    w.segs = w.seg_chunks > 0 ? static_cast<int>((chunks + w.seg_chunks - 1) / w.seg_chunks) : 1;
 }
 
 cudaError_t launch_dla(int dtype, const DlaWalk& w, cudaStream_t stream) {

@@ -10,7 +10,8 @@
 // norm is the same on every call.
 //
 // Squares of float32 values run out of float32's range at 2^64 and 2^-63, long before the values do, so three sums are kept:
-// of x^2, (2^-80 x)^2 and (2^80 x)^2.  The first counts unless it overflowed or is so small that squares were lost.
+// of x^2, (2^-80 x)^2 and (2^80 x)^2.  The first counts unless it overflowed or is so small that squares were lost.  Each is a
+// float32 sum over the 32 or 64 values of a thread in a block, then compensated over the blocks, then in 64 bits.
 #include "dla_internal.h"
 #include "sdm_common.cuh"
 
@@ -98,10 +99,10 @@ __device__ __forceinline__ void squares(const Entry& e, int block, const uint4 (
 }
 
 template <int N>
-__global__ void __launch_bounds__(GT, 2) k_grad_squares(const __grid_constant__ GradTable<N> t, float* __restrict__ part) {
-    __shared__ float sh[GT / 32][3];
+__global__ void __launch_bounds__(GT, 2) k_grad_squares(const __grid_constant__ GradTable<N> t, double* __restrict__ part) {
+    __shared__ double sh[GT / 32][3];
     const int b0 = blockIdx.x * t.per, b1 = min(b0 + t.per, t.blocks);
-    float2 s2[3] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    float hi[3] = {0.f, 0.f, 0.f}, lo[3] = {0.f, 0.f, 0.f};
     int at = find(t, b0);
     uint4 next[PIECES];
     load_block(t.e[at], b0, next);
@@ -114,13 +115,21 @@ __global__ void __launch_bounds__(GT, 2) k_grad_squares(const __grid_constant__ 
             while (at + 1 < t.count && t.e[at + 1].first <= b + 1) ++at;
             load_block(t.e[at], b + 1, next);
         }
+        float2 s2[3] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         if (e.kind & 1) squares<BF16>(e, b, u, s2);
         else squares<F32>(e, b, u, s2);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {                        // a block's sum to the blocks', with what the addition leaves
+            const float x = s2[i].x + s2[i].y, sum = hi[i] + x, back = sum - hi[i];
+            lo[i] += (hi[i] - (sum - back)) + (x - back);
+            hi[i] = sum;
+        }
     }
-    float s[3];
+    double s[3];
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-        s[i] = s2[i].x + s2[i].y;
+        // where the sum is infinite, what was left is not a number
+        s[i] = fabsf(hi[i]) <= 3.402823466e+38f ? static_cast<double>(hi[i]) + static_cast<double>(lo[i]) : static_cast<double>(hi[i]);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
     }
@@ -132,14 +141,14 @@ __global__ void __launch_bounds__(GT, 2) k_grad_squares(const __grid_constant__ 
     }
     __syncthreads();
     if (threadIdx.x < 3) {
-        float x = 0.f;
+        double x = 0;
         for (int w = 0; w < GT / 32; ++w) x += sh[w][threadIdx.x];
         part[static_cast<int64_t>(blockIdx.x) * 3 + threadIdx.x] = x;
     }
 }
 
 // The norm and the factor from the shares, in 64 bits and in order; in every thread of the CTA.
-__device__ __forceinline__ float2 norm_of(const float* __restrict__ part, int shares, float max_norm) {
+__device__ __forceinline__ float2 norm_of(const double* __restrict__ part, int shares, float max_norm) {
     __shared__ double sh[GT / 32][3];
     double s[3] = {0, 0, 0};
     for (int i = threadIdx.x; i < shares; i += GT)
@@ -162,7 +171,7 @@ __device__ __forceinline__ float2 norm_of(const float* __restrict__ part, int sh
     const float f = static_cast<float>(norm);
     return make_float2(f, !(fabsf(f) <= 3.402823466e+38f) ? __int_as_float(0x7fffffff) : norm > max_norm ? static_cast<float>(max_norm / norm) : 1.f);
 }
-__global__ void __launch_bounds__(GT) k_grad_norm(const float* __restrict__ part, int shares, float max_norm, float* __restrict__ stats) {
+__global__ void __launch_bounds__(GT) k_grad_norm(const double* __restrict__ part, int shares, float max_norm, float* __restrict__ stats) {
     const float2 f = norm_of(part, shares, max_norm);
     if (threadIdx.x < 2) stats[threadIdx.x] = threadIdx.x == 0 ? f.x : f.y;
 }
@@ -223,7 +232,7 @@ __device__ __forceinline__ void scale(const Entry& e, int block, const uint4 (&u
 }
 
 template <int N>
-__global__ void __launch_bounds__(GT, 2) k_grad_scale(const __grid_constant__ GradTable<N> t, const float* __restrict__ part, int shares, float max_norm,
+__global__ void __launch_bounds__(GT, 2) k_grad_scale(const __grid_constant__ GradTable<N> t, const double* __restrict__ part, int shares, float max_norm,
                                                       float* __restrict__ stats) {
     const int b0 = blockIdx.x * t.per, b1 = min(b0 + t.per, t.blocks);
     int at = find(t, b1 - 1);
@@ -286,7 +295,7 @@ int64_t tensors_of(int64_t n, const sdm_grad_tensor* t) {
 }
 
 template <int N>
-cudaError_t run(int64_t n, const sdm_grad_tensor* list, bool write, float max_norm, float* stats, float* part, cudaStream_t stream) {
+cudaError_t run(int64_t n, const sdm_grad_tensor* list, bool write, float max_norm, float* stats, double* part, cudaStream_t stream) {
     GradTable<N> t;
     int64_t shares = 0;
     bool one = false;                            // table: it still stands for the second pass
@@ -317,18 +326,18 @@ cudaError_t run(int64_t n, const sdm_grad_tensor* list, bool write, float max_no
 
 }  // namespace
 
-// A share is three floats; every launch has at most CTAS of them, and at least MANY tensors or 2^30 blocks but the last.
+// A share is three sums in 64 bits; every launch has at most CTAS of them, and at least MANY tensors or 2^30 blocks but the last.
 size_t grad_bytes(int64_t n, const sdm_grad_tensor* t) {
     size_t shares = 0, blocks = 0;
     for (int64_t i = 0; i < n; ++i) blocks += static_cast<size_t>(blocks_of(t[i]));
     shares = (static_cast<size_t>(tensors_of(n, t)) + FEW - 1) / FEW + blocks / (1u << 29) + 1;
     shares *= CTAS;
-    return (blocks < shares ? blocks : shares) * 3 * 4;
+    return (blocks < shares ? blocks : shares) * 3 * 8;
 }
 
 cudaError_t launch_grad(int64_t n, const sdm_grad_tensor* list, bool write, float max_norm, float* stats, void* ws, cudaStream_t stream) {
-    return tensors_of(n, list) <= FEW ? run<FEW>(n, list, write, max_norm, stats, static_cast<float*>(ws), stream)
-                                      : run<MANY>(n, list, write, max_norm, stats, static_cast<float*>(ws), stream);
+    return tensors_of(n, list) <= FEW ? run<FEW>(n, list, write, max_norm, stats, static_cast<double*>(ws), stream)
+                                      : run<MANY>(n, list, write, max_norm, stats, static_cast<double*>(ws), stream);
 }
 
 }  // namespace sdm
