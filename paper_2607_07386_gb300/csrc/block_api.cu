@@ -52,42 +52,98 @@ sdm::DlaWalk dla_walk(const sdm_dla_shape* s, const float* log_decay, const int3
     return w;
 }
 
-// The roles of a call without their buffers, and where a workspace holds what: the pieces' states, then the shares of dq
-// and dk.
+// The roles of a call, the scan's with a wide contraction in two pieces, and where a workspace holds what: the pieces'
+// states, then the shares of the outputs that are sums (of value heads that share a key head, of the contraction's pieces).
+struct DlaCall {
+    const void* r; const void* k; const void* v;
+    void* out;
+    const float* state_in;
+    float* state_out;
+};
 struct DlaLayout {
     sdm::DlaWalk w;
-    size_t seg, dq, dk, total;
+    sdm::DlaSums sums;
+    int call[sdm::DLA_ROLES];     // the buffers that a role has, and the sum that it gives a share to (-1: none)
+    int sum[sdm::DLA_ROLES];
+    size_t share[sdm::DLA_ROLES], total;
 };
 DlaLayout dla_layout(const sdm_dla_shape* s, bool back) {
     DlaLayout L{};
-    L.w = dla_walk(s, nullptr, nullptr, back ? 3 : 1);
-    sdm::DlaRole* r = L.w.role;
+    L.w = dla_walk(s, nullptr, nullptr, 0);
     const int H = s->H, Hk = s->H_k;
+    const bool scan = sdm::dla_scan_supported(s->dtype, s->T);
+    const size_t chains = static_cast<size_t>(s->B) * H;
+    size_t floats = 0;
+    size_t share[sdm::DLA_ROLES] = {};
+    auto add = [&](int call, sdm::DlaRole r, int group) {
+        const int cuts = scan && r.da > 128 ? 2 : 1;
+        const bool sum = cuts * group > 1;
+        r.width = r.da;
+        r.partial = sum;
+        const int job = sum ? L.sums.n++ : -1;
+        if (sum) L.sums.s[job] = sdm::DlaSum{nullptr, nullptr, H / group, group, cuts, r.db};
+        for (int c = 0; c < cuts; ++c) {
+            const int i = L.w.roles++;
+            L.w.role[i] = r;
+            L.w.role[i].x0 = 128 * c;
+            L.w.role[i].da = cuts == 1 ? r.width : c == 0 ? 128 : r.width - 128;
+            L.call[i] = call;
+            L.sum[i] = job;
+            if (sum) {
+                share[i] = floats;
+                floats += chains * s->T * r.db;
+            }
+        }
+    };
+    sdm::DlaRole r{};
     if (!back) {
-        r[0].hr = Hk; r[0].hk = Hk; r[0].hv = H; r[0].da = s->d_k; r[0].db = s->d_v;
-        r[0].inter = r[0].intra = s->scale; r[0].add = 1.f;
+        r.hr = Hk; r.hk = Hk; r.hv = H; r.da = s->d_k; r.db = s->d_v;
+        r.inter = r.intra = s->scale; r.add = 1.f;
+        add(0, r, 1);
     } else {
-        r[0].hr = H; r[0].hk = H; r[0].hv = Hk; r[0].da = s->d_v; r[0].db = s->d_k;          // dq
-        r[0].inter = r[0].intra = s->scale; r[0].add = 1.f; r[0].transposed = 1;
-        r[1].hr = Hk; r[1].hk = Hk; r[1].hv = H; r[1].da = s->d_k; r[1].db = s->d_v;         // dv
-        r[1].inter = 1.f; r[1].intra = r[1].add = s->scale; r[1].reverse = 1;
-        r[2].hr = H; r[2].hk = H; r[2].hv = Hk; r[2].da = s->d_v; r[2].db = s->d_k;          // dk
-        r[2].inter = 1.f; r[2].intra = r[2].add = s->scale; r[2].reverse = 1; r[2].transposed = 1;
-        r[0].partial = r[2].partial = H != Hk;
+        r.hr = H; r.hk = H; r.hv = Hk; r.da = s->d_v; r.db = s->d_k;                         // dq
+        r.inter = r.intra = s->scale; r.add = 1.f; r.transposed = 1;
+        add(0, r, H / Hk);
+        r = sdm::DlaRole{};
+        r.hr = Hk; r.hk = Hk; r.hv = H; r.da = s->d_k; r.db = s->d_v;                        // dv
+        r.inter = 1.f; r.intra = r.add = s->scale; r.reverse = 1;
+        add(1, r, 1);
+        r = sdm::DlaRole{};
+        r.hr = H; r.hk = H; r.hv = Hk; r.da = s->d_v; r.db = s->d_k;                         // dk
+        r.inter = 1.f; r.intra = r.add = s->scale; r.reverse = 1; r.transposed = 1;
+        add(2, r, H / Hk);
     }
-    const size_t chains = static_cast<size_t>(s->B) * s->H;
     if (chains == 0) return L;
     sdm::dla_plan(s->dtype, L.w);
-    size_t floats = 0;
-    for (int i = 0; i < L.w.roles; ++i) {
-        L.w.seg_role[i] = static_cast<int64_t>(floats);
-        if (L.w.segs > 1) floats += chains * L.w.segs * r[i].da * r[i].db;
+    size_t state = 0;
+    for (int i = 0; i < L.w.roles; ++i) {                    // a role's pieces have one state
+        const sdm::DlaRole& q = L.w.role[i];
+        L.w.seg_role[i] = q.x0 > 0 ? L.w.seg_role[i - 1] : static_cast<int64_t>(state);
+        if (L.w.segs > 1 && q.x0 == 0) state += chains * L.w.segs * q.width * q.db;
     }
-    const size_t share = back && H != Hk ? align256(chains * s->T * s->d_k * 4) : 0;
-    L.dq = align256(floats * 4);
-    L.dk = L.dq + share;
-    L.total = L.dk + share;
+    const size_t at = align256(state * 4);
+    for (int i = 0; i < L.w.roles; ++i) L.share[i] = at + share[i] * 4;
+    L.total = at + align256(floats * 4);
     return L;
+}
+cudaError_t dla_run(int dtype, DlaLayout& L, const DlaCall* calls, char* ws, cudaStream_t stream) {
+    L.w.seg_state = reinterpret_cast<float*>(ws);
+    for (int i = 0; i < L.w.roles; ++i) {
+        sdm::DlaRole& r = L.w.role[i];
+        const DlaCall& c = calls[L.call[i]];
+        r.r = c.r; r.k = c.k; r.v = c.v;
+        r.state_in = c.state_in;
+        r.state_out = c.state_out;
+        r.out = c.out;
+        if (L.sum[i] < 0) continue;
+        r.out = ws + L.share[i];
+        sdm::DlaSum& s = L.sums.s[L.sum[i]];
+        if (r.x0 == 0) s.part = reinterpret_cast<const float*>(r.out);
+        s.out = c.out;
+    }
+    cudaError_t e = sdm::launch_dla(dtype, L.w, stream);
+    if (e == cudaSuccess && L.sums.n > 0) e = sdm::launch_dla_join(dtype, L.sums, L.w.B, L.w.T, L.w.token_major, stream);
+    return e;
 }
 
 // ------------------------------------------------------------------ block norm
@@ -225,12 +281,8 @@ sdm_status sdm_dla_forward(const sdm_dla_shape* s, const void* q, const void* k,
     SDM_TRY(sdm::api_status_word(&L.w.err));
     L.w.log_decay = log_decay;
     L.w.lengths = lengths;
-    L.w.seg_state = static_cast<float*>(workspace);
-    sdm::DlaRole& r = L.w.role[0];
-    r.r = q; r.k = k; r.v = v; r.out = y;
-    r.state_in = state;
-    r.state_out = state;
-    return done(sdm::launch_dla(s->dtype, L.w, reinterpret_cast<cudaStream_t>(stream)), "sdm_dla_forward");
+    const DlaCall call{q, k, v, y, state, state};
+    return done(dla_run(s->dtype, L, &call, static_cast<char*>(workspace), reinterpret_cast<cudaStream_t>(stream)), "sdm_dla_forward");
 }
 
 sdm_status sdm_dla_step(const sdm_dla_shape* s, const void* q, const void* k, const void* v, const float* log_decay, const int32_t* slots,
@@ -270,25 +322,10 @@ sdm_status sdm_dla_backward(const sdm_dla_shape* s, const void* q, const void* k
     SDM_TRY(check_bufs("sdm_dla_backward", bufs, 13));
     SDM_TRY(check_ws("sdm_dla_backward", workspace, workspace_bytes, L.total));
     SDM_TRY(sdm::api_status_word(&L.w.err));
-    char* const ws = static_cast<char*>(workspace);
-    const bool shares = s->H != s->H_k;
     L.w.log_decay = log_decay;
     L.w.lengths = lengths;
-    L.w.seg_state = static_cast<float*>(workspace);
-    sdm::DlaRole* r = L.w.role;
-    r[0].r = dy; r[0].k = v; r[0].v = k; r[0].out = shares ? ws + L.dq : dq;
-    r[0].state_in = state0;
-    r[1].r = k; r[1].k = q; r[1].v = dy; r[1].out = dv;
-    r[1].state_in = dstate;
-    r[1].state_out = dstate0;
-    r[2].r = v; r[2].k = dy; r[2].v = q; r[2].out = shares ? ws + L.dk : dk;
-    r[2].state_in = dstate;
-    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    cudaError_t e = sdm::launch_dla(s->dtype, L.w, st);
-    if (shares && e == cudaSuccess)
-        e = sdm::launch_dla_join(s->dtype, reinterpret_cast<float*>(ws + L.dq), reinterpret_cast<float*>(ws + L.dk), dq, dk, s->B, s->H_k, s->H / s->H_k,
-                                 s->T, s->d_k, L.w.token_major, st);
-    return done(e, "sdm_dla_backward");
+    const DlaCall calls[] = {{dy, v, k, dq, state0, nullptr}, {k, q, dy, dv, dstate, dstate0}, {v, dy, q, dk, dstate, nullptr}};
+    return done(dla_run(s->dtype, L, calls, static_cast<char*>(workspace), reinterpret_cast<cudaStream_t>(stream)), "sdm_dla_backward");
 }
 
 sdm_status sdm_block_norm(const sdm_block_norm_shape* s, const void* x, const void* y, const void* gate, const float* res_scale,

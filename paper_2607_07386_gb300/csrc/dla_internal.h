@@ -6,6 +6,7 @@
 namespace sdm {
 
 constexpr int DLA_C32 = 32;               // tokens per chunk of the fp32 walk
+constexpr int DLA_ROLES = 6;              // walks of a call at once: up to three, each in up to two pieces of the contraction
 
 // One walk over the tokens of every (sequence, head): with a state S [da, db] and, for each token in the walk's order,
 // operands r and k [da] and v [db] and an output o [db],
@@ -19,11 +20,12 @@ struct DlaRole {
     void* out;
     int hr, hk, hv;           // heads of r, k and v (H or H_k)
     int da, db;
+    int x0, width;            // its values of r and k: [x0, x0 + da) of `width` (all, or where the scan cuts them, up to 128)
     const float* state_in;    // [slots, H, d_k, d_v], or nullptr (zero)
     float* state_out;         // or nullptr; may be state_in
-    int transposed;           // da is d_v
+    int transposed;           // r and k have width d_v
     int reverse;
-    int partial;              // out is float32 [B, H, T, db], a share of a key head's gradient
+    int partial;              // out is float32 [B, H, T, db], a share of the output: of one value head, of some of r's values
     float inter, intra, add;
 };
 struct DlaWalk {
@@ -32,13 +34,14 @@ struct DlaWalk {
     const int32_t* lengths;   // [B] or nullptr
     int* err;
     int roles;
-    DlaRole role[3];
+    DlaRole role[DLA_ROLES];
+    int slices[DLA_ROLES];    // of db, a CTA each
     // The tokens may be cut into `segs` pieces of `seg_chunks` chunks that run at once: a first launch copies the first
-    // state and takes what each piece but the last adds to it into seg_state [role][B * H][segs][da * db], a small one turns
+    // state and takes what each piece but the last adds to it into seg_state [role][B * H][segs][width * db], a small one turns
     // that into the states that the pieces start from, and the walk proper takes them.
     int segs, seg_chunks;
     float* seg_state;
-    int64_t seg_role[3];      // where a role's sums start, in floats
+    int64_t seg_role[DLA_ROLES];      // where a role's sums start, in floats
 };
 
 // lam^n for lam = exp(ld): 1 at n = 0 whatever ld is, 0 for ld = -inf.  The product is taken in two parts.
@@ -82,16 +85,25 @@ __device__ __forceinline__ void dla_zero_tail(const DlaWalk& w, const DlaRole& r
 
 // Fills in segs and seg_chunks; runs the walks.
 void dla_plan(int dtype, DlaWalk& w);
-cudaError_t launch_dla(int dtype, const DlaWalk& w, cudaStream_t stream);
-// The walks on the tensor cores (k_dla_scan.cu): bf16, da <= 128, chunks of 64.
-bool dla_scan_supported(int dtype, const DlaWalk& w);
+cudaError_t launch_dla(int dtype, DlaWalk& w, cudaStream_t stream);
+// The walks on the tensor cores (k_dla_scan.cu): bf16, chunks of 64, da <= 128.
+bool dla_scan_supported(int dtype, int T);
 void dla_scan_plan(DlaWalk& w);
-cudaError_t launch_dla_scan(const DlaWalk& w, cudaStream_t stream);
+cudaError_t launch_dla_scan(DlaWalk& w, cudaStream_t stream);
 // The states that the pieces start from, chunks of `chunk` tokens.
 cudaError_t launch_dla_prefix(const DlaWalk& w, int chunk, cudaStream_t stream);
-// dq and dk [heads of k] = sums over the `group` value heads of their shares [B, H, T, d] float32.
-cudaError_t launch_dla_join(int dtype, const float* pq, const float* pk, void* dq, void* dk, int B, int Hk, int group, int T, int d, int token_major,
-                            cudaStream_t stream);
+// Outputs [heads] that are sums, in order, over `pieces` of the contraction and `group` value heads of their shares
+// [pieces][B, heads * group, T, d] float32.
+struct DlaSum {
+    const float* part;
+    void* out;
+    int heads, group, pieces, d;
+};
+struct DlaSums {
+    int n;
+    DlaSum s[3];
+};
+cudaError_t launch_dla_join(int dtype, const DlaSums& sums, int B, int T, int token_major, cudaStream_t stream);
 
 struct DlaStep {
     const void* q; const void* k; const void* v;

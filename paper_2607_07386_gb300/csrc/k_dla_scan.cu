@@ -1,4 +1,5 @@
-// Linear attention with a decay per head on the tensor cores: bf16, widths of the contraction up to 128, chunks of 64 tokens.
+// Linear attention with a decay per head on the tensor cores: bf16, chunks of 64 tokens, widths of the contraction up to 128 (wider
+// ones are cut in two, whose shares of the outputs are added up: P and what is read of S are sums over the width).
 //
 // A CTA walks one state, 128 columns of it (db), over its chunks; every product has 128 rows, TMEM lanes = columns of the state:
 //   1  P[i, j]  = r_i.k_j                       A = [r; k] in shared memory (the k half is not used), B = k
@@ -62,7 +63,7 @@ constexpr size_t scan_smem() { return 1024 + ScanTile<DA>::CTL + sizeof(ScanCtl)
 static_assert(scan_smem<128>() <= 227 * 1024 && scan_smem<64>() <= 227 * 1024, "shared memory");
 
 struct ScanMaps {
-    CUtensorMap r[3], k[3], v[3], out[3];
+    CUtensorMap r[DLA_ROLES], k[DLA_ROLES], v[DLA_ROLES], out[DLA_ROLES];
 };
 
 // The next bf16 part of two floats, which keep what its rounding left: exact, in one mixed multiply-add each.
@@ -80,7 +81,7 @@ __device__ __forceinline__ float load_bf16(const unsigned char* p) {
 }
 
 template <int DA, bool SUMS>
-__global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ ScanMaps maps, const __grid_constant__ DlaWalk w, const int3 slices) {
+__global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ ScanMaps maps, const __grid_constant__ DlaWalk w) {
     using L = ScanTile<DA>;
     extern __shared__ unsigned char raw[];
     const uint32_t base = smem_u32(raw);
@@ -90,14 +91,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int nseg = SUMS ? w.segs - 1 : w.segs, seg = blockIdx.x % nseg;
     int slice = blockIdx.x / nseg, role = 0;
-    if (slice >= slices.x) {
-        slice -= slices.x;
-        role = 1;
-        if (slice >= slices.y) {
-            slice -= slices.y;
-            role = 2;
-        }
-    }
+    while (slice >= w.slices[role]) slice -= w.slices[role++];
     const DlaRole& ro = w.role[role];
     const int b = blockIdx.z, h = blockIdx.y, col0 = slice * 128;
     const int len = dla_length(w, b), chunks = (len + C - 1) / C;
@@ -273,8 +267,8 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
                 mbar_expect_tx(fb, SUMS ? L::BYTES - DA / 64 * 8192 : L::BYTES);
 #pragma unroll
                 for (int x = 0; x < DA / 64; ++x) {
-                    tma_load_4d(t + L::RK + x * 16384 + 8192, &maps.k[role], 64 * x, at, hk, b, fb);
-                    if (!SUMS) tma_load_4d(t + L::RK + x * 16384, &maps.r[role], 64 * x, at, hr, b, fb);
+                    tma_load_4d(t + L::RK + x * 16384 + 8192, &maps.k[role], ro.x0 + 64 * x, at, hk, b, fb);
+                    if (!SUMS) tma_load_4d(t + L::RK + x * 16384, &maps.r[role], ro.x0 + 64 * x, at, hr, b, fb);
                 }
                 tma_load_4d(t + L::V, &maps.v[role], col0, at, hv, b, fb);
                 tma_load_4d(t + L::V + 8192, &maps.v[role], col0 + 64, at, hv, b, fb);
@@ -427,8 +421,8 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
         constexpr int RD = DA / 2;                           // rows of da of a warp
         const int x0 = half * RD, da = ro.da, db = ro.db;
         const bool live = col < db;
-        const int64_t per = static_cast<int64_t>(da) * db;
-        const int64_t at = ro.transposed ? static_cast<int64_t>(col) * da : col, step = ro.transposed ? 1 : db;
+        const int64_t per = static_cast<int64_t>(ro.width) * db;
+        const int64_t at = ro.transposed ? static_cast<int64_t>(col) * ro.width + ro.x0 : static_cast<int64_t>(ro.x0) * db + col, step = ro.transposed ? 1 : db;
         float2 S[RD / 2];
         auto read = [&](const float* p) {
             const float* q = p + at + x0 * step;
@@ -523,10 +517,10 @@ cudaError_t scan(const ScanMaps& maps, const DlaWalk& w, cudaStream_t stream) {
     static std::atomic<unsigned long long> seen;
     e = allow_smem(k_dla_scan<DA, SUMS>, smem, seen);
     if (e != cudaSuccess) return e;
-    int n[3] = {0, 0, 0};
-    for (int i = 0; i < w.roles; ++i) n[i] = (w.role[i].db + 127) / 128;
+    int n = 0;
+    for (int i = 0; i < w.roles; ++i) n += w.slices[i];
     const unsigned segs = static_cast<unsigned>(SUMS ? w.segs - 1 : w.segs);
-    k_dla_scan<DA, SUMS><<<dim3((n[0] + n[1] + n[2]) * segs, w.H, w.B), ST, smem, stream>>>(maps, w, make_int3(n[0], n[1], n[2]));
+    k_dla_scan<DA, SUMS><<<dim3(n * segs, w.H, w.B), ST, smem, stream>>>(maps, w);
     return cudaGetLastError();
 }
 template <int DA>
@@ -539,15 +533,9 @@ cudaError_t scans(const ScanMaps& maps, const DlaWalk& w, cudaStream_t stream) {
     return scan<DA, false>(maps, w, stream);
 }
 
-int widest(const DlaWalk& w) {
-    int da = 0;
-    for (int i = 0; i < w.roles; ++i) da = w.role[i].da > da ? w.role[i].da : da;
-    return da;
-}
-
 }  // namespace
 
-bool dla_scan_supported(int dtype, const DlaWalk& w) { return dtype == SDM_BF16 && widest(w) <= 128 && w.T >= 32; }
+bool dla_scan_supported(int dtype, int T) { return dtype == SDM_BF16 && T >= 32; }
 
 // With fewer CTAs than half of the SMs the tokens are cut, so that every SM has a piece, where that pays: a chunk takes 2.1 us
 // in the walk and about 1.1 in the walk for the sums, which with the joining launch costs 10 us more to begin with.
@@ -564,16 +552,19 @@ void dla_scan_plan(DlaWalk& w) {
     w.segs = static_cast<int>((chunks + w.seg_chunks - 1) / w.seg_chunks);
 }
 
-cudaError_t launch_dla_scan(const DlaWalk& w, cudaStream_t stream) {
+cudaError_t launch_dla_scan(DlaWalk& w, cudaStream_t stream) {
     ScanMaps m;
+    int da = 0;
     for (int i = 0; i < w.roles; ++i) {
         const DlaRole& r = w.role[i];
-        if (!token_map(&m.r[i], r.r, w.token_major, w.B, r.hr, w.T, r.da) || !token_map(&m.k[i], r.k, w.token_major, w.B, r.hk, w.T, r.da) ||
+        da = r.da > da ? r.da : da;
+        w.slices[i] = (r.db + 127) / 128;
+        if (!token_map(&m.r[i], r.r, w.token_major, w.B, r.hr, w.T, r.width) || !token_map(&m.k[i], r.k, w.token_major, w.B, r.hk, w.T, r.width) ||
             !token_map(&m.v[i], r.v, w.token_major, w.B, r.hv, w.T, r.db) ||
             (!r.partial && !token_map(&m.out[i], r.out, w.token_major, w.B, w.H, w.T, r.db)))
             return cudaErrorInvalidValue;
     }
-    return widest(w) <= 64 ? scans<64>(m, w, stream) : scans<128>(m, w, stream);
+    return da <= 64 ? scans<64>(m, w, stream) : scans<128>(m, w, stream);
 }
 
 }  // namespace sdm

@@ -43,21 +43,14 @@ template <> __device__ __forceinline__ void put_one<F32>(void* out, int64_t at, 
 template <> __device__ __forceinline__ void put_one<BF16>(void* out, int64_t at, float x) { static_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(x); }
 
 template <class D, int DA, bool SUMS>
-__global__ void __launch_bounds__(WT) k_dla_walk(const DlaWalk w, const int3 slices) {
+__global__ void __launch_bounds__(WT) k_dla_walk(const DlaWalk w) {
     extern __shared__ __align__(16) unsigned char raw[];
     WalkSmem<DA>& sm = *reinterpret_cast<WalkSmem<DA>*>(raw);
     const int tid = threadIdx.x;
     const int nseg = SUMS ? w.segs - 1 : w.segs;
     const int seg = blockIdx.x % nseg;
     int slice = blockIdx.x / nseg, role = 0;
-    if (slice >= slices.x) {
-        slice -= slices.x;
-        role = 1;
-        if (slice >= slices.y) {
-            slice -= slices.y;
-            role = 2;
-        }
-    }
+    while (slice >= w.slices[role]) slice -= w.slices[role++];
     const DlaRole& ro = w.role[role];
     const int b = blockIdx.z, h = blockIdx.y, col0 = slice * COLS;
     const int len = dla_length(w, b);
@@ -297,10 +290,10 @@ cudaError_t walk(const DlaWalk& w, cudaStream_t stream) {
     static std::atomic<unsigned long long> seen;
     cudaError_t e = allow_smem(k_dla_walk<D, DA, SUMS>, smem, seen);
     if (e != cudaSuccess) return e;
-    int n[3] = {0, 0, 0};
-    for (int i = 0; i < w.roles; ++i) n[i] = (w.role[i].db + COLS - 1) / COLS;
+    int n = 0;
+    for (int i = 0; i < w.roles; ++i) n += w.slices[i];
     const unsigned segs = static_cast<unsigned>(SUMS ? w.segs - 1 : w.segs);
-    k_dla_walk<D, DA, SUMS><<<dim3((n[0] + n[1] + n[2]) * segs, w.H, w.B), WT, smem, stream>>>(w, make_int3(n[0], n[1], n[2]));
+    k_dla_walk<D, DA, SUMS><<<dim3(n * segs, w.H, w.B), WT, smem, stream>>>(w);
     return cudaGetLastError();
 }
 template <class D, int DA>
@@ -313,9 +306,12 @@ cudaError_t walks(const DlaWalk& w, cudaStream_t stream) {
     return walk<D, DA, false>(w, stream);
 }
 template <class D>
-cudaError_t walk_width(const DlaWalk& w, cudaStream_t stream) {
+cudaError_t walk_width(DlaWalk& w, cudaStream_t stream) {
     int da = 0;
-    for (int i = 0; i < w.roles; ++i) da = w.role[i].da > da ? w.role[i].da : da;
+    for (int i = 0; i < w.roles; ++i) {
+        da = w.role[i].da > da ? w.role[i].da : da;
+        w.slices[i] = (w.role[i].db + COLS - 1) / COLS;
+    }
     return da <= 64 ? walks<D, 64>(w, stream) : da <= 128 ? walks<D, 128>(w, stream) : walks<D, 256>(w, stream);
 }
 
@@ -323,8 +319,8 @@ cudaError_t walk_width(const DlaWalk& w, cudaStream_t stream) {
 __global__ void __launch_bounds__(256) k_dla_prefix(const DlaWalk w, int C) {
     const int role = blockIdx.z % w.roles, b = blockIdx.z / w.roles, h = blockIdx.y;
     const DlaRole& ro = w.role[role];
-    const int per = ro.da * ro.db, i = (blockIdx.x * 256 + threadIdx.x) * 4;      // a multiple of 16
-    if (i >= per) return;
+    const int per = ro.width * ro.db, i = (blockIdx.x * 256 + threadIdx.x) * 4;      // a multiple of 16
+    if (i >= per || ro.x0 != 0) return;                      // a role's pieces have one state
     const int len = dla_length(w, b), chunks = (len + C - 1) / C;
     const float ld = __ldg(w.log_decay + h);
     float4* p = reinterpret_cast<float4*>(w.seg_state + w.seg_role[role] + (static_cast<int64_t>(b) * w.H + h) * w.segs * per + i);
@@ -342,24 +338,26 @@ __global__ void __launch_bounds__(256) k_dla_prefix(const DlaWalk w, int C) {
     }
 }
 
-// Sum over the value heads of a key head, in order, rounded once; four values a thread.
+// Sums of shares, rounded once; four values a thread.
 template <class D>
-__global__ void __launch_bounds__(256) k_dla_join(const float* __restrict__ pq, const float* __restrict__ pk, void* dq, void* dk, int B, int Hk, int group, int T, int d, int token_major) {
-    const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4, total = static_cast<int64_t>(B) * Hk * T * d;
+__global__ void __launch_bounds__(256) k_dla_join(const DlaSums sums, int B, int T, int token_major) {
+    const DlaSum& j = sums.s[blockIdx.y];
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4, total = static_cast<int64_t>(B) * j.heads * T * j.d;
     if (i >= total) return;
-    const float* const part = blockIdx.y == 0 ? pq : pk;
-    void* const out = blockIdx.y == 0 ? dq : dk;
-    const int x = static_cast<int>(i % d);
-    const int64_t row = i / d;
-    const int t = static_cast<int>(row % T), hk = static_cast<int>(row / T % Hk), b = static_cast<int>(row / T / Hk);
+    const int x = static_cast<int>(i % j.d);
+    const int64_t row = i / j.d;
+    const int t = static_cast<int>(row % T), h = static_cast<int>(row / T % j.heads), b = static_cast<int>(row / T / j.heads);
+    const int64_t head = static_cast<int64_t>(T) * j.d, piece = static_cast<int64_t>(B) * j.heads * j.group * head;
+    const float* part = j.part + (static_cast<int64_t>(b) * j.heads + h) * j.group * head + static_cast<int64_t>(t) * j.d + x;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int g = 0; g < group; ++g) {
-        const float4 p = __ldcs(reinterpret_cast<const float4*>(part + ((static_cast<int64_t>(b) * Hk * group + hk * group + g) * T + t) * d + x));
-        s.x += p.x; s.y += p.y; s.z += p.z; s.w += p.w;
-    }
-    const int64_t at = gdn_base(token_major, b, hk, Hk, T, d) + t * gdn_stride(token_major, Hk, d) + x;
-    put_pair<D>(out, at, s.x, s.y);
-    put_pair<D>(out, at + 2, s.z, s.w);
+    for (int p = 0; p < j.pieces; ++p)
+        for (int g = 0; g < j.group; ++g) {
+            const float4 f = __ldcs(reinterpret_cast<const float4*>(part + p * piece + g * head));
+            s.x += f.x; s.y += f.y; s.z += f.z; s.w += f.w;
+        }
+    const int64_t at = gdn_base(token_major, b, h, j.heads, T, j.d) + t * gdn_stride(token_major, j.heads, j.d) + x;
+    put_pair<D>(j.out, at, s.x, s.y);
+    put_pair<D>(j.out, at + 2, s.z, s.w);
 }
 
 // One token: the state's two trips through HBM are all that counts.  A CTA takes 32 columns of one state, a warp 32 rows
@@ -440,7 +438,7 @@ __global__ void __launch_bounds__(256) k_dla_step(const DlaStep r) {
 }  // namespace
 
 void dla_plan(int dtype, DlaWalk& w) {
-    if (dla_scan_supported(dtype, w)) {
+    if (dla_scan_supported(dtype, w.T)) {
         dla_scan_plan(w);
         return;
     }
@@ -458,25 +456,28 @@ void dla_plan(int dtype, DlaWalk& w) {
     w.segs = w.seg_chunks > 0 ? static_cast<int>((chunks + w.seg_chunks - 1) / w.seg_chunks) : 1;
 }
 
-cudaError_t launch_dla(int dtype, const DlaWalk& w, cudaStream_t stream) {
-    if (dla_scan_supported(dtype, w)) return launch_dla_scan(w, stream);
+cudaError_t launch_dla(int dtype, DlaWalk& w, cudaStream_t stream) {
+    if (dla_scan_supported(dtype, w.T)) return launch_dla_scan(w, stream);
     return dtype == SDM_F32 ? walk_width<F32>(w, stream) : walk_width<BF16>(w, stream);
 }
 
 cudaError_t launch_dla_prefix(const DlaWalk& w, int chunk, cudaStream_t stream) {
     int per = 0;
-    for (int i = 0; i < w.roles; ++i) per = w.role[i].da * w.role[i].db > per ? w.role[i].da * w.role[i].db : per;
+    for (int i = 0; i < w.roles; ++i) per = w.role[i].width * w.role[i].db > per ? w.role[i].width * w.role[i].db : per;
     k_dla_prefix<<<dim3((per / 4 + 255) / 256, w.H, w.B * w.roles), 256, 0, stream>>>(w, chunk);
     return cudaGetLastError();
 }
 
-cudaError_t launch_dla_join(int dtype, const float* pq, const float* pk, void* dq, void* dk, int B, int Hk, int group, int T, int d, int token_major,
-                            cudaStream_t stream) {
-    const int64_t pieces = static_cast<int64_t>(B) * Hk * T * d / 4;
+cudaError_t launch_dla_join(int dtype, const DlaSums& sums, int B, int T, int token_major, cudaStream_t stream) {
+    int64_t pieces = 0;
+    for (int i = 0; i < sums.n; ++i) {
+        const int64_t n = static_cast<int64_t>(B) * sums.s[i].heads * T * sums.s[i].d / 4;
+        pieces = n > pieces ? n : pieces;
+    }
     if (pieces == 0) return cudaSuccess;
-    const dim3 grid(static_cast<unsigned>((pieces + 255) / 256), 2);
-    if (dtype == SDM_F32) k_dla_join<F32><<<grid, 256, 0, stream>>>(pq, pk, dq, dk, B, Hk, group, T, d, token_major);
-    else k_dla_join<BF16><<<grid, 256, 0, stream>>>(pq, pk, dq, dk, B, Hk, group, T, d, token_major);
+    const dim3 grid(static_cast<unsigned>((pieces + 255) / 256), sums.n);
+    if (dtype == SDM_F32) k_dla_join<F32><<<grid, 256, 0, stream>>>(sums, B, T, token_major);
+    else k_dla_join<BF16><<<grid, 256, 0, stream>>>(sums, B, T, token_major);
     return cudaGetLastError();
 }
 

@@ -166,6 +166,10 @@ CASES = [  # B, H, Hk, T, dk, dv, dtype, layout, lengths
     (2, 1, 1, 900, 96, 200, "bf16", "head_major", [300, 897]),
     (1, 1, 1, 700, 40, 64, "f32", "head_major", None),
     (2, 2, 1, 420, 128, 96, "f32", "token_major", [33, 420]),
+    # the contraction in two pieces: forwards, backwards, shared key heads
+    (1, 2, 1, 200, 136, 72, "bf16", "token_major", None),
+    (2, 4, 2, 333, 64, 256, "bf16", "head_major", [0, 330]),
+    (1, 1, 1, 1500, 256, 256, "bf16", "head_major", None),
 ]
 
 
