@@ -71,7 +71,8 @@ DlaLayout dla_layout(const sdm_dla_shape* s, bool back) {
     DlaLayout L{};
     L.w = dla_walk(s, nullptr, nullptr, 0);
     const int H = s->H, Hk = s->H_k;
-    const bool scan = sdm::dla_scan_supported(s->dtype, s->T);
+    const bool scan = sdm::dla_scan_pays(s->dtype, s->T, s->d_k, s->d_v);
+    L.w.scan = scan;
     const size_t chains = static_cast<size_t>(s->B) * H;
     size_t floats = 0;
     size_t share[sdm::DLA_ROLES] = {};
@@ -114,7 +115,7 @@ DlaLayout dla_layout(const sdm_dla_shape* s, bool back) {
         add(2, r, H / Hk);
     }
     if (chains == 0) return L;
-    sdm::dla_plan(s->dtype, L.w);
+    sdm::dla_plan(L.w);
     size_t state = 0;
     for (int i = 0; i < L.w.roles; ++i) {                    // a role's pieces have one state
         const sdm::DlaRole& q = L.w.role[i];
@@ -158,6 +159,9 @@ sdm_status block_norm_check(const sdm_block_norm_shape* s) {
     if (!(s->eps >= 0.f && s->eps - s->eps == 0.f)) return fail(SDM_ERR_INVALID_ARG, "eps must be finite and >= 0");
     return SDM_OK;
 }
+
+// A gate for more rows than there are is one for all of them.
+int64_t gate_rows(const sdm_block_norm_shape* s) { return std::max<int64_t>(1, std::min(s->gate_rows, s->M)); }
 
 sdm_status with(const char* who, const char* name, const void* p, const char* other, bool there) {
     if (p != nullptr && !there) return fail(SDM_ERR_INVALID_ARG, "%s: %s without %s", who, name, other);
@@ -279,6 +283,10 @@ sdm_status sdm_dla_forward(const sdm_dla_shape* s, const void* q, const void* k,
     SDM_TRY(check_bufs("sdm_dla_forward", bufs, 8));
     SDM_TRY(check_ws("sdm_dla_forward", workspace, workspace_bytes, L.total));
     SDM_TRY(sdm::api_status_word(&L.w.err));
+    if (s->T == 1 && lengths == nullptr) {
+        const sdm::DlaStep d{q, k, v, log_decay, nullptr, state, y, s->B, s->H, s->H_k, s->d_k, s->d_v, s->B, s->scale, L.w.err};
+        return done(sdm::launch_dla_step(s->dtype, d, reinterpret_cast<cudaStream_t>(stream)), "sdm_dla_forward");
+    }
     L.w.log_decay = log_decay;
     L.w.lengths = lengths;
     const DlaCall call{q, k, v, y, state, state};
@@ -339,7 +347,7 @@ sdm_status sdm_block_norm(const sdm_block_norm_shape* s, const void* x, const vo
     SDM_TRY(with(who, "z", z, "gamma_pre", gamma_pre != nullptr));
     SDM_TRY(with(who, "gamma_pre", gamma_pre, "z", z != nullptr || s->M == 0));
     const size_t es = esize(s->dtype), rows = static_cast<size_t>(s->M) * s->D * es, v = static_cast<size_t>(s->D) * 4;
-    const size_t gates = static_cast<size_t>((s->M + s->gate_rows - 1) / s->gate_rows) * s->D * es;
+    const size_t gates = static_cast<size_t>((s->M + gate_rows(s) - 1) / gate_rows(s)) * s->D * es;
     if (s->M > 0 && y == nullptr && z == nullptr) return fail(SDM_ERR_INVALID_ARG, "%s: neither y nor z", who);
     const Buf bufs[] = {{"x", x, rows, 16, false, false}, {"y", y, rows, 16, true, false}, {"gate", gate, gates, 16, true, false},
                         {"res_scale", res_scale, v, 16, true, false}, {"gamma_post", gamma_post, v, 16, true, false},
@@ -347,7 +355,7 @@ sdm_status sdm_block_norm(const sdm_block_norm_shape* s, const void* x, const vo
     SDM_TRY(check_bufs(who, bufs, 8, 0, 6));                 // each row of x is read by the threads that write it to h
     if (s->M == 0) return sdm::api_ok();
     sdm::BlockNorm a{};
-    a.M = s->M; a.gate_rows = s->gate_rows; a.D = s->D; a.eps = s->eps;
+    a.M = s->M; a.gate_rows = gate_rows(s); a.D = s->D; a.eps = s->eps;
     a.x = x; a.y = y; a.gate = gate; a.res_scale = res_scale; a.gamma_post = gamma_post; a.gamma_pre = gamma_pre;
     a.h = h; a.z = z;
     return done(sdm::launch_block_norm(s->dtype, a, reinterpret_cast<cudaStream_t>(stream)), who);
@@ -356,7 +364,7 @@ sdm_status sdm_block_norm(const sdm_block_norm_shape* s, const void* x, const vo
 size_t sdm_block_norm_backward_workspace_bytes(const sdm_block_norm_shape* s) {
     if (block_norm_check(s) != SDM_OK) return 0;
     sdm::api_ok();
-    return align256(sdm::block_norm_backward_bytes(s->M, s->gate_rows, s->D));
+    return align256(sdm::block_norm_backward_bytes(s->M, gate_rows(s), s->D));
 }
 
 sdm_status sdm_block_norm_backward(const sdm_block_norm_shape* s, const void* y, const void* h, const void* gate, const float* res_scale,
@@ -378,8 +386,8 @@ sdm_status sdm_block_norm_backward(const sdm_block_norm_shape* s, const void* y,
     SDM_TRY(with(who, "gamma_pre", gamma_pre, "dz", dz != nullptr || !some));
     if (some && y == nullptr && dz == nullptr) return fail(SDM_ERR_INVALID_ARG, "%s: neither y nor dz", who);
     const size_t es = esize(s->dtype), rows = static_cast<size_t>(s->M) * s->D * es, v = static_cast<size_t>(s->D) * 4;
-    const size_t gates = static_cast<size_t>((s->M + s->gate_rows - 1) / s->gate_rows) * s->D * es;
-    const size_t need = align256(sdm::block_norm_backward_bytes(s->M, s->gate_rows, s->D));
+    const size_t gates = static_cast<size_t>((s->M + gate_rows(s) - 1) / gate_rows(s)) * s->D * es;
+    const size_t need = align256(sdm::block_norm_backward_bytes(s->M, gate_rows(s), s->D));
     const Buf bufs[] = {{"y", y, rows, 16, true, false}, {"h", h, rows, 16, gamma_pre == nullptr, false}, {"gate", gate, gates, 16, true, false},
                         {"res_scale", res_scale, v, 16, true, false}, {"gamma_post", gamma_post, v, 16, true, false},
                         {"gamma_pre", gamma_pre, v, 16, true, false}, {"dz", dz, rows, 16, true, false}, {"dh", dh, rows, 16, true, false},
@@ -396,7 +404,7 @@ sdm_status sdm_block_norm_backward(const sdm_block_norm_shape* s, const void* y,
         return done(e, who);
     }
     sdm::BlockNorm a{};
-    a.M = s->M; a.gate_rows = s->gate_rows; a.D = s->D; a.eps = s->eps;
+    a.M = s->M; a.gate_rows = gate_rows(s); a.D = s->D; a.eps = s->eps;
     a.h = const_cast<void*>(h); a.y = y; a.gate = gate; a.res_scale = res_scale; a.gamma_post = gamma_post; a.gamma_pre = gamma_pre;
     a.dz = dz; a.dh = dh; a.dx = dx; a.dy = dy; a.dgate = dgate;
     a.dres_scale = dres_scale; a.dgamma_post = dgamma_post; a.dgamma_pre = dgamma_pre;

@@ -30,6 +30,7 @@ struct DlaRole {
 };
 struct DlaWalk {
     int B, H, T, token_major;
+    int scan;                 // on the tensor cores
     const float* log_decay;   // [H]
     const int32_t* lengths;   // [B] or nullptr
     int* err;
@@ -84,10 +85,10 @@ __device__ __forceinline__ void dla_zero_tail(const DlaWalk& w, const DlaRole& r
 }
 
 // Fills in segs and seg_chunks; runs the walks.
-void dla_plan(int dtype, DlaWalk& w);
+void dla_plan(DlaWalk& w);
 cudaError_t launch_dla(int dtype, DlaWalk& w, cudaStream_t stream);
 // The walks on the tensor cores (k_dla_scan.cu): bf16, chunks of 64, da <= 128.
-bool dla_scan_supported(int dtype, int T);
+bool dla_scan_pays(int dtype, int T, int dk, int dv);
 void dla_scan_plan(DlaWalk& w);
 cudaError_t launch_dla_scan(DlaWalk& w, cudaStream_t stream);
 // The states that the pieces start from, chunks of `chunk` tokens.

@@ -17,6 +17,12 @@
 // Only D goes from one chunk to the next, and it does not depend on S: six groups of warps work on different stages of
 // neighbouring chunks, each handing over through mbarriers.
 //
+// Bound by that chain: a chunk takes 1.9 us, 3,650 cycles, of which 2,050 are its 56 MMAs (32 cycles each with A in TMEM, 48
+// with A in shared memory) and most of the rest hand-overs, 250 cycles from a product's end to the warps that read it.
+// 8 x 16 heads of 128 x 4,096 tokens: forward 134 us, 0.6 of the copy bandwidth (537 MB of q, k, v and y are 79); backward,
+// three runs of this walk, 405 us.  Tried and no faster, forward: P by products of 64 rows and lanes moved by 16 (136 to 162
+// us), three warps that issue (137), the state's product first (140), waits that sleep (148).
+//
 // A value of v that is not finite must stay out of the outputs before its token, which share its products: v is zero in
 // them from that token on, its column's outputs from there are NaN, and so is the column of the state.
 #include "dla_internal.h"
@@ -97,7 +103,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
     const int len = dla_length(w, b), chunks = (len + C - 1) / C;
     const bool reverse = ro.reverse != 0;
     const int c0 = min(seg * w.seg_chunks, chunks), c1 = seg == w.segs - 1 ? chunks : min(c0 + w.seg_chunks, chunks);
-    const int todo = c1 - c0, last_n = len - (chunks - 1) * C;       // tokens of the sequence's last chunk
+    const int todo = c1 - c0, outputs = SUMS ? 0 : todo, last_n = len - (chunks - 1) * C;       // tokens of the sequence's last chunk
     auto chunk_at = [&](int c) { return reverse ? chunks - 1 - (c0 + c) : c0 + c; };
     auto partial = [&](int c) { return chunk_at(c) == chunks - 1 && last_n < C; };
     const int64_t chain = static_cast<int64_t>(b) * w.H + h;
@@ -147,7 +153,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
             const uint32_t lanes = tmem + (static_cast<uint32_t>(me * 32) << 16);
             const float* const wt = ctl.W + i * WP;
             unsigned char* const ps = ringp + L::PS;
-            for (int c = 0; c < (SUMS ? 0 : todo); ++c) {
+            for (int c = 0; c < outputs; ++c) {
                 await(bar(B_P), c & 1, dead);
                 unsigned char* const to = ps + (c & 1) * 2 * MAT;
                 // A token past this one counts as zero, and where it is not finite, not as 0 times it: such products show in
@@ -283,7 +289,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         const bool share = ro.partial != 0;
         float* const shares = static_cast<float*>(ro.out) + chain * w.T * ro.db + col;
-        for (int c = 0; !SUMS && c < todo; ++c) {
+        for (int c = 0; c < outputs; ++c) {
             const bool part = partial(c);
             const int n = part ? last_n : C, t0 = chunk_at(c) * C;
             unsigned char* const box = ringp + L::OUT;
@@ -457,8 +463,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
             read(w.segs > 1 ? pieces + seg * per : ro.state_in == nullptr ? nullptr : ro.state_in + chain * per);
         }
         auto put = [&]() {                                   // S before the next chunk
-            if (SUMS) return;
-            {
+            if (!SUMS) {
 #pragma unroll
                 for (int x = 0; x < RD / 2; x += 8) {
                     uint32_t u[8], l[8];
@@ -471,8 +476,8 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
                     tmem_st8(lanes + S_COL + x0 / 2 + x, u);
                     tmem_st8(lanes + S_COL + SB + x0 / 2 + x, l);
                 }
+                announce(bar(B_S), lane);
             }
-            announce(bar(B_S), lane);
         };
         if (todo > 0) put();
         for (int c = 0; c < todo; ++c) {
@@ -535,7 +540,11 @@ cudaError_t scans(const ScanMaps& maps, const DlaWalk& w, cudaStream_t stream) {
 
 }  // namespace
 
-bool dla_scan_supported(int dtype, int T) { return dtype == SDM_BF16 && T >= 32; }
+// A chunk costs the same however few tokens it holds, and however narrow the heads are below 64.  Forward (backward) with 16
+// heads of 128, 8 tokens: 21 (93) us against 48 (123) in the fp32 walk at B = 16, 64 (343) against 167 (460) at B = 64; 100
+// tokens: 25 (108) against 144 (408) and 87 (386) against 530 (1,554).  Heads of 32, B = 64: 56 (157) against 27 (66) with 8 tokens,
+// 50 (142) against 46 (122) with 64, 64 (189) against 74 (201) with 100.
+bool dla_scan_pays(int dtype, int T, int dk, int dv) { return dtype == SDM_BF16 && T > 0 && (dk > 64 || dv > 64 || T >= 64); }
 
 // With fewer CTAs than half of the SMs the tokens are cut, so that every SM has a piece, where that pays: a chunk takes 2.1 us
 // in the walk and about 1.1 in the walk for the sums, which with the joining launch costs 10 us more to begin with.

@@ -64,6 +64,15 @@ def test_refused_backward(sdm, kw, word):  # noqa: F811
     assert e.value.status == 1 and word in str(e.value)
 
 
+@pytest.mark.parametrize("rows", [2**40, 2**63 - 1])
+def test_gate_of_more_rows_than_there_are(sdm, rows):  # noqa: F811
+    """It is one for all of them; its row is still checked."""
+    shape = sdm.BlockNormShape.make(16, 64, gate_rows=rows)
+    assert sdm.block_norm_backward_workspace_bytes(shape) == sdm.block_norm_backward_workspace_bytes(sdm.BlockNormShape.make(16, 64, gate_rows=16))
+    with pytest.raises(sdm.SdmError, match="overlaps"):
+        _call(sdm, shape, gate=7 * A + 64)
+
+
 def test_empty_forward(sdm):  # noqa: F811
     _call(sdm, sdm.BlockNormShape.make(0, 64))
 
@@ -150,6 +159,22 @@ def test_forward_and_backward(sdm, M, D, dtype, gate_rows, have):  # noqa: F811
     place = True                                             # dx over dh
     same = back(s["dh"].clone())
     assert all(p is None or torch.equal(p, q) for p, q in zip(got, same))
+
+
+@pytest.mark.gpu
+def test_one_gate_for_any_number_of_rows(sdm):  # noqa: F811
+    import torch
+    s, got = _inputs(50, 64, "bf16", 50, "gsop"), []
+    for rows in (50, 2**40, 2**63 - 1):
+        shape = sdm.BlockNormShape.make(50, 64, gate_rows=rows)
+        h, z, dx, dy = (torch.empty_like(s["x"]) for _ in range(4))
+        vec = {n: s[n] for n in VECTORS}
+        out = {"d" + n: torch.empty_like(s[n]) for n in VECTORS}
+        sdm.block_norm(shape, s["x"], s["y"], h, z, **vec)
+        ws = torch.empty(sdm.block_norm_backward_workspace_bytes(shape), dtype=torch.uint8, device="cuda")
+        sdm.block_norm_backward(shape, s["y"], h, s["dz"], s["dh"], dx, dy, **vec, **out, workspace=ws)
+        got.append([h, z, dx, dy, *out.values()])
+    assert all(torch.equal(a, b) for g in got[1:] for a, b in zip(got[0], g))
 
 
 @pytest.mark.gpu

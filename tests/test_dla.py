@@ -170,6 +170,12 @@ CASES = [  # B, H, Hk, T, dk, dv, dtype, layout, lengths
     (1, 2, 1, 200, 136, 72, "bf16", "token_major", None),
     (2, 4, 2, 333, 64, 256, "bf16", "head_major", [0, 330]),
     (1, 1, 1, 1500, 256, 256, "bf16", "head_major", None),
+    # where the kernels change: one token, less than a chunk, narrow heads
+    (3, 2, 2, 1, 64, 64, "bf16", "head_major", [1, 0, 1]),
+    (3, 2, 1, 1, 20, 36, "f32", "head_major", [0, 1, 1]),
+    (2, 4, 2, 8, 128, 128, "bf16", "head_major", [8, 3]),
+    (2, 2, 1, 63, 64, 64, "bf16", "token_major", [0, 63]),
+    (2, 2, 1, 64, 64, 64, "bf16", "head_major", [64, 1]),
 ]
 
 
@@ -279,6 +285,19 @@ def test_step(sdm, dtype, B, H, Hk, dk, dv, layout):
     assert torch.equal(y2[2 if B > 2 else 0:], y[2 if B > 2 else 0:])
     assert B <= 2 or not y2[:2].any()
     assert sdm.device_status() == (1 if B > 2 else 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d", [("f32", 36), ("bf16", 128)])
+def test_one_token_is_a_step(sdm, dtype, d):
+    """A forward over one token and no lengths gives what a step gives, bit for bit."""
+    import torch
+    s = _inputs(2, 4, 2, 1, d, d, dtype)
+    shape = sdm.DlaShape.make(2, 4, 1, d, d, H_k=2, dtype=dtype, scale=0.7)
+    y, state = run_forward(sdm, s, shape)
+    y1, state1 = torch.empty_like(y), s["state"].clone()
+    sdm.dla_step(shape, s["q"], s["k"], s["v"], s["log_decay"], state1, y1)
+    assert torch.equal(y, y1) and torch.equal(state, state1)
 
 
 @pytest.mark.gpu
