@@ -364,7 +364,7 @@ sdm_status sdm_block_norm(const sdm_block_norm_shape* s, const void* x, const vo
 size_t sdm_block_norm_backward_workspace_bytes(const sdm_block_norm_shape* s) {
     if (block_norm_check(s) != SDM_OK) return 0;
     sdm::api_ok();
-    return align256(sdm::block_norm_backward_bytes(s->M, gate_rows(s), s->D));
+    return align256(sdm::block_norm_backward_bytes(s->dtype, s->M, gate_rows(s), s->D));
 }
 
 sdm_status sdm_block_norm_backward(const sdm_block_norm_shape* s, const void* y, const void* h, const void* gate, const float* res_scale,
@@ -387,7 +387,7 @@ sdm_status sdm_block_norm_backward(const sdm_block_norm_shape* s, const void* y,
     if (some && y == nullptr && dz == nullptr) return fail(SDM_ERR_INVALID_ARG, "%s: neither y nor dz", who);
     const size_t es = esize(s->dtype), rows = static_cast<size_t>(s->M) * s->D * es, v = static_cast<size_t>(s->D) * 4;
     const size_t gates = static_cast<size_t>((s->M + gate_rows(s) - 1) / gate_rows(s)) * s->D * es;
-    const size_t need = align256(sdm::block_norm_backward_bytes(s->M, gate_rows(s), s->D));
+    const size_t need = align256(sdm::block_norm_backward_bytes(s->dtype, s->M, gate_rows(s), s->D));
     const Buf bufs[] = {{"y", y, rows, 16, true, false}, {"h", h, rows, 16, gamma_pre == nullptr, false}, {"gate", gate, gates, 16, true, false},
                         {"res_scale", res_scale, v, 16, true, false}, {"gamma_post", gamma_post, v, 16, true, false},
                         {"gamma_pre", gamma_pre, v, 16, true, false}, {"dz", dz, rows, 16, true, false}, {"dh", dh, rows, 16, true, false},

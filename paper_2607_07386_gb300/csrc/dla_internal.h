@@ -133,7 +133,7 @@ struct BlockNorm {
 };
 bool block_norm_supported(int D);
 cudaError_t launch_block_norm(int dtype, const BlockNorm& a, cudaStream_t stream);
-size_t block_norm_backward_bytes(int64_t M, int64_t gate_rows, int D);
+size_t block_norm_backward_bytes(int dtype, int64_t M, int64_t gate_rows, int D);
 cudaError_t launch_block_norm_backward(int dtype, const BlockNorm& a, cudaStream_t stream);
 
 // ---- gradient norm and clipping (k_grad_clip.cu) ----

@@ -48,7 +48,7 @@ __device__ __forceinline__ float gdn_nan() { return __int_as_float(0x7fffffff); 
 // as much as a launch, so it is not repeated.
 template <class K>
 inline cudaError_t allow_smem(K kernel, size_t bytes, std::atomic<unsigned long long>& seen) {
-    if (bytes <= 48 * 1024) return cudaSuccess;
+    if (bytes <= 32 * 1024) return cudaSuccess;  // up to 48 KB without leave, static shared memory included
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;

@@ -6,7 +6,12 @@
 //   a row takes one reduction;
 //   dgamma_pre = sum dz n;  with q = dx n':  dgate = c sum q over the gate's rows,
 //   G = sum gate q over all:  dres_scale = gamma_post G,  dgamma_post = res_scale G.
-// So two column sums are all that the gradients of four vectors take.  Sums over a row: TPR threads a row, butterflies
+// So two column sums are all that the gradients of four vectors take.
+//
+// Bound by memory: everything is read once and written once, next rows on their way in shared memory (without: 125 and 211
+// us for rows of 2,048), the vectors in registers.  32,768 rows of 2,048 in bf16: forward 95 us, 5.6 TB/s, 0.83 of the copy bandwidth;
+// backward 152 us, 5.3 TB/s, 0.78, where the warps' issue slots are two thirds taken and the column sums' registers leave
+// two CTAs an SM.  One row: 6 and 11 us, one launch and two.  Sums over a row: TPR threads a row, butterflies
 // within a warp, then the warps' shares through shared memory.
 #include "dla_internal.h"
 #include "sdm_common.cuh"
@@ -105,13 +110,16 @@ __device__ __forceinline__ void row_sum(float (&s)[N], float (*sh)[16][8], int& 
     turn ^= 1;
 }
 
-constexpr int SMS = 152, FORE_CTAS = 3, BACK_CTAS = 2;       // CTAs of 256 threads on an SM: 80 and 128 registers a thread
+// CTAs of 256 threads on an SM: 80 and 128 registers a thread (four forward: 98 to 100 us for rows of 2,048, three: 95 to 98).
+constexpr int SMS = 152, FORE_CTAS = 3, BACK_CTAS = 2;
 
 // Threads a row, values a thread in pieces of 16 bytes, rows of a CTA at once.
 template <class D, int TPR, int VE>
 struct Row {
     static constexpr int E = D::E, P = E / 2, V = VE / E, ROWS = cta(TPR) / TPR;
-    static constexpr bool KEEP = VE <= 16;       // the vectors' values of a thread stay in registers
+    // The vectors' values of a thread stay in registers (8,192 rows of 8,192: 95 and 173 us, read again for each row 133 and 280);
+    // 32 of each are more than there are.
+    static constexpr bool KEEP = VE <= 16;
 };
 // Rows on their way: each thread copies its own pieces of N arrays' next S rows into slots of its own in shared memory
 // (asynchronously, so no registers are held and nothing has to be waited for but its own copies).  With S = 0, where S
@@ -166,8 +174,8 @@ struct Ahead {
     }
 };
 
-// A group of TPR threads takes `span` rows one after the other.
-template <class D, int TPR, int VE, int S>
+// A group of TPR threads takes `span` rows one after the other.  ROWGATE: every row has its gate, which comes with the row.
+template <class D, int TPR, int VE, int S, bool ROWGATE>
 __global__ void __launch_bounds__(cta(TPR), TPR > 256 ? 1 : FORE_CTAS) k_block_norm(const BlockNorm a, const int64_t span) {
     extern __shared__ __align__(16) unsigned char ring[];
     using R = Row<D, TPR, VE>;
@@ -181,8 +189,13 @@ __global__ void __launch_bounds__(cta(TPR), TPR > 256 ? 1 : FORE_CTAS) k_block_n
     const int64_t last = first + span < a.M ? first + span : a.M;
     if (first >= last) return;
     uint4 gu[V];
-    const void* const src[2] = {a.x, a.y};
-    Ahead<D, TPR, VE, 2, S> rows(ring, first, last, a.D);
+    constexpr int N = ROWGATE ? 3 : 2;
+    const void* from[N];
+    from[0] = a.x;
+    from[1] = a.y;
+    if (ROWGATE) from[N - 1] = a.gate;
+    const void* const (&src)[N] = from;
+    Ahead<D, TPR, VE, N, S> rows(ring, first, last, a.D);
     rows.start(src);
     auto gate = [&](int64_t g) {
 #pragma unroll
@@ -191,8 +204,9 @@ __global__ void __launch_bounds__(cta(TPR), TPR > 256 ? 1 : FORE_CTAS) k_block_n
             gu[i] = c < a.D ? __ldg(reinterpret_cast<const uint4*>(static_cast<const typename D::T*>(a.gate) + g * a.D + c)) : make_uint4(0, 0, 0, 0);
         }
     };
-    int64_t g = a.gate != nullptr ? first / a.gate_rows : 0, until = a.gate != nullptr ? (g + 1) * a.gate_rows : last;
-    if (a.gate != nullptr) gate(g);
+    const bool shared = !ROWGATE && a.gate != nullptr;
+    int64_t g = shared ? first / a.gate_rows : 0, until = shared ? (g + 1) * a.gate_rows : last;
+    if (shared) gate(g);
     float2 ck[R::KEEP ? V : 1][P], pk[R::KEEP ? V : 1][P];
     if (R::KEEP) {
 #pragma unroll
@@ -211,6 +225,7 @@ __global__ void __launch_bounds__(cta(TPR), TPR > 256 ? 1 : FORE_CTAS) k_block_n
         for (int i = 0; i < V; ++i) {
             xu[i] = rows.get(src, m, 0, i);
             yu[i] = rows.get(src, m, 1, i);
+            if (ROWGATE) gu[i] = rows.get(src, m, N - 1, i);
         }
         rows.advance(src);
         if (m == until) {
@@ -240,7 +255,7 @@ __global__ void __launch_bounds__(cta(TPR), TPR > 256 ? 1 : FORE_CTAS) k_block_n
                 unpack16x2<D>(xu[i], x);
                 unpack16x2<D>(yu[i], y);
                 if (!R::KEEP) product<P>(a.res_scale, a.gamma_post, c, k);
-                if (a.gate != nullptr) {
+                if (ROWGATE || shared) {
                     float2 ga[4];
                     unpack16x2<D>(gu[i], ga);
 #pragma unroll
@@ -565,13 +580,18 @@ NormCut norm_cut(int64_t M, int D, int tpr, bool shared) {
     return c;
 }
 
-// Threads a row and values a thread: eight values while a row has at most 512 threads of them.
+// Threads a row and values a thread: eight values (16 make the registers of the gradients' sums: bf16 rows of 2,048 99 and 200 us forward
+// and backward, with eight 95 and 152) in up to 256 threads, as several CTAs of an SM hide each other's waits.  Then it is what
+// moves with two 16-byte pieces of an array a thread: 16 bf16 values (rows of 4,096: 102 and 156 us, 512 threads of eight 107 and 176) or
+// 512 threads of eight float32 values (98 and 152, 256 of 16 101 and 231).  Then 512 threads of 16 and 32.
 struct RowPlan {
     int tpr, ve;
 };
-RowPlan row_plan(int D) {
+RowPlan row_plan(int dtype, int D) {
     RowPlan p{32, 8};
-    while (p.tpr < 512 && p.tpr * 8 < D) p.tpr *= 2;
+    while (p.tpr < 256 && p.tpr * p.ve < D) p.tpr *= 2;
+    if (p.tpr * p.ve < D && dtype == SDM_BF16) p.ve = 16;
+    if (p.tpr * p.ve < D) p.tpr = 512;
     while (p.tpr * p.ve < D) p.ve *= 2;
     return p;
 }
@@ -585,26 +605,26 @@ constexpr int stages(int ctas) {
     return most > 4 ? 4 : static_cast<int>(most);
 }
 
-template <class F>
+template <class D, class F>
 cudaError_t with_plan(const RowPlan& p, F f) {
-#define SDM_ROW(T, V) if (p.tpr == T && p.ve == V) return f(std::integral_constant<int, T>{}, std::integral_constant<int, V>{});
-    SDM_ROW(32, 8) SDM_ROW(64, 8) SDM_ROW(128, 8) SDM_ROW(256, 8) SDM_ROW(512, 8) SDM_ROW(512, 16) SDM_ROW(512, 32)
+#define SDM_ROW(T, V) if (p.tpr == (T) && p.ve == (V)) return f(std::integral_constant<int, T>{}, std::integral_constant<int, V>{});
+    SDM_ROW(32, 8) SDM_ROW(64, 8) SDM_ROW(128, 8) SDM_ROW(256, 8) SDM_ROW(D::BYTES == 2 ? 256 : 512, D::BYTES == 2 ? 16 : 8) SDM_ROW(512, 16) SDM_ROW(512, 32)
 #undef SDM_ROW
     return cudaErrorInvalidValue;
 }
 
-template <class D>
+template <class D, bool ROWGATE>
 cudaError_t forward(const RowPlan& p, const BlockNorm& a, cudaStream_t stream) {
-    return with_plan(p, [&](auto T, auto V) {
+    return with_plan<D>(p, [&](auto T, auto V) {
         constexpr int rows = cta(T.value) / T.value;
         const int64_t most = static_cast<int64_t>(SMS) * (T.value > 256 ? 1 : FORE_CTAS) * rows;
         const int64_t span = (a.M + most - 1) / most, groups = (a.M + span - 1) / span;
-        constexpr int S = stages<D, T.value, V.value, 2>(FORE_CTAS);
-        constexpr size_t smem = S * stage_bytes<D, T.value, V.value, 2>();
+        constexpr int N = ROWGATE ? 3 : 2, S = stages<D, T.value, V.value, N>(FORE_CTAS);
+        constexpr size_t smem = S * stage_bytes<D, T.value, V.value, N>();
         static std::atomic<unsigned long long> seen;
-        const cudaError_t e = allow_smem(k_block_norm<D, T.value, V.value, S>, smem, seen);
+        const cudaError_t e = allow_smem(k_block_norm<D, T.value, V.value, S, ROWGATE>, smem, seen);
         if (e != cudaSuccess) return e;
-        k_block_norm<D, T.value, V.value, S><<<static_cast<unsigned>((groups + rows - 1) / rows), cta(T.value), smem, stream>>>(a, span);
+        k_block_norm<D, T.value, V.value, S, ROWGATE><<<static_cast<unsigned>((groups + rows - 1) / rows), cta(T.value), smem, stream>>>(a, span);
         return cudaGetLastError();
     });
 }
@@ -612,7 +632,7 @@ template <class D, bool ROWGATE>
 cudaError_t backward(const RowPlan& p, const BlockNorm& a, cudaStream_t stream) {
     const bool shared = a.dgate != nullptr && a.gate_rows > 1;
     const NormCut cut = norm_cut(a.M, a.D, p.tpr, shared);
-    cudaError_t e = with_plan(p, [&](auto T, auto V) {
+    cudaError_t e = with_plan<D>(p, [&](auto T, auto V) {
         constexpr int S = stages<D, T.value, V.value, ROWGATE ? 5 : 4>(BACK_CTAS);
         constexpr size_t smem = S * stage_bytes<D, T.value, V.value, ROWGATE ? 5 : 4>();
         static std::atomic<unsigned long long> seen;
@@ -631,15 +651,16 @@ cudaError_t backward(const RowPlan& p, const BlockNorm& a, cudaStream_t stream) 
 
 bool block_norm_supported(int D) { return D <= 512 * 32; }
 cudaError_t launch_block_norm(int dtype, const BlockNorm& a, cudaStream_t stream) {
-    const RowPlan p = row_plan(a.D);
-    return dtype == SDM_F32 ? forward<F32>(p, a, stream) : forward<BF16>(p, a, stream);
+    const RowPlan p = row_plan(dtype, a.D);
+    if (a.gate != nullptr && a.gate_rows == 1) return dtype == SDM_F32 ? forward<F32, true>(p, a, stream) : forward<BF16, true>(p, a, stream);
+    return dtype == SDM_F32 ? forward<F32, false>(p, a, stream) : forward<BF16, false>(p, a, stream);
 }
-size_t block_norm_backward_bytes(int64_t M, int64_t gate_rows, int D) {
+size_t block_norm_backward_bytes(int dtype, int64_t M, int64_t gate_rows, int D) {
     if (M == 0) return 0;
-    return norm_cut(M, D, row_plan(D).tpr, gate_rows > 1).total * 4;
+    return norm_cut(M, D, row_plan(dtype, D).tpr, gate_rows > 1).total * 4;
 }
 cudaError_t launch_block_norm_backward(int dtype, const BlockNorm& a, cudaStream_t stream) {
-    const RowPlan p = row_plan(a.D);
+    const RowPlan p = row_plan(dtype, a.D);
     if (a.gate != nullptr && a.gate_rows == 1) return dtype == SDM_F32 ? backward<F32, true>(p, a, stream) : backward<BF16, true>(p, a, stream);
     return dtype == SDM_F32 ? backward<F32, false>(p, a, stream) : backward<BF16, false>(p, a, stream);
 }

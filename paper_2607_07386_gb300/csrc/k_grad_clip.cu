@@ -5,6 +5,8 @@
 // of 32 KB into one range a CTA, and the second walks every range backwards, so that what the first read last is still in L2.
 // The loads of a block are on their way while the one before is worked on.
 //
+// 1.14 GB: the norm in 175 us (6.5 TB/s), with the scaling 525 (0.96 of the copy bandwidth for three passes).
+//
 // The list goes to the kernels in their parameters: nothing is copied to the device first, and a captured launch holds its
 // list.  A CTA's sums go to the workspace and are joined in order (by every CTA of the second pass for itself), so the
 // norm is the same on every call.
@@ -22,7 +24,9 @@ namespace {
 constexpr int GT = 256, PIECES = 8;              // threads; pieces of 16 bytes of the gradient a thread
 constexpr int64_t BLOCK = GT * PIECES * 16;      // bytes of the gradient a block
 constexpr int CTAS = 152 * 2;                    // of 256 threads of up to 128 registers, a launch
-constexpr int FEW = 64, MANY = 960;              // tensors a launch: a long table takes longer to launch
+// Tensors a launch.  A long table takes longer to launch (3 MB in 28 tensors: 13.0 us, in the short one 12.7), a list in many
+// launches longer still (0.8 GB in 96 tensors: 408 us in short tables, 379 in a long one).
+constexpr int FEW = 64, MANY = 960;
 
 struct Entry {
     const void* src;
