@@ -122,7 +122,7 @@ DlaLayout dla_layout(const sdm_dla_shape* s, bool back) {
         L.w.seg_role[i] = q.x0 > 0 ? L.w.seg_role[i - 1] : static_cast<int64_t>(state);
         if (L.w.segs > 1 && q.x0 == 0) state += chains * L.w.segs * q.width * q.db;
     }
-    const size_t at = align256(state * 4);
+    const size_t at = align256(L.w.span > 0 ? sdm::dla_scan_cut_bytes() : state * 4);
     for (int i = 0; i < L.w.roles; ++i) L.share[i] = at + share[i] * 4;
     L.total = at + align256(floats * 4);
     return L;

@@ -41,6 +41,9 @@ struct DlaWalk {
     // state and takes what each piece but the last adds to it into seg_state [role][B * H][segs][width * db], a small one turns
     // that into the states that the pieces start from, and the walk proper takes them.
     int segs, seg_chunks;
+    // Or the scan spreads more chains than SMs evenly over these: a list of all chains' chunks, one chain after the other, is cut
+    // every `span` chunks (0: it is not).  A chain that is cut hands its state over in seg_state.
+    int span;
     float* seg_state;
     int64_t seg_role[DLA_ROLES];      // where a role's sums start, in floats
 };
@@ -90,6 +93,7 @@ cudaError_t launch_dla(int dtype, DlaWalk& w, cudaStream_t stream);
 // The walks on the tensor cores (k_dla_scan.cu): bf16, chunks of 64, da <= 128.
 bool dla_scan_pays(int dtype, int T, int dk, int dv);
 void dla_scan_plan(DlaWalk& w);
+size_t dla_scan_cut_bytes();
 cudaError_t launch_dla_scan(DlaWalk& w, cudaStream_t stream);
 // The states that the pieces start from, chunks of `chunk` tokens.
 cudaError_t launch_dla_prefix(const DlaWalk& w, int chunk, cudaStream_t stream);

@@ -20,7 +20,7 @@
 // Bound by that chain: a chunk takes 1.9 us, 3,650 cycles, of which 2,050 are its 56 MMAs (32 cycles each with A in TMEM, 48
 // with A in shared memory) and most of the rest hand-overs, 250 cycles from a product's end to the warps that read it.
 // 8 x 16 heads of 128 x 4,096 tokens: forward 134 us, 0.6 of the copy bandwidth (537 MB of q, k, v and y are 79); backward,
-// three runs of this walk, 405 us.  Tried and no faster, forward: P by products of 64 rows and lanes moved by 16 (136 to 162
+// three runs of this walk, 384 chains spread over the SMs, 370 us (405 in three rounds of whole chains).  Tried and no faster, forward: P by products of 64 rows and lanes moved by 16 (136 to 162
 // us), three warps that issue (137), the state's product first (140), waits that sleep (148).
 //
 // A value of v that is not finite must stay out of the outputs before its token, which share its products: v is zero in
@@ -28,6 +28,10 @@
 #include "dla_internal.h"
 #include "gdn_tc.cuh"
 #include "sdm_common.cuh"
+
+#include <algorithm>
+#include <climits>
+#include <cstddef>
 
 namespace sdm {
 
@@ -37,11 +41,15 @@ using namespace gdn;
 
 constexpr int SW = 8, VW = 8, OW = 4, PW = 4;  // warps: state, v, outputs, and (the last four) P, P, products, copies
 constexpr int ST = 32 * (SW + VW + OW + PW);
+constexpr int64_t SMS = 152;
 constexpr int LAUNCH_REGS = 80, STATE_REGS = 104, V_REGS = 80, REST_REGS = 56;
 static_assert(SW * STATE_REGS + VW * V_REGS + (OW + PW) * REST_REGS <= (SW + VW + OW + PW) * LAUNCH_REGS, "register split");
 
 // TMEM columns: S, two parts; D, 64 rows of da at a time; g v, three parts; P; O; I.
 constexpr uint32_t S_COL = 0, D_COL = 128, V_COL = 192, P_COL = 288, O_COL = 352, I_COL = 416, T_COLS = 512;
+constexpr int CUT_LEAST = 4;                   // chunks of a piece
+constexpr int SPREAD_SAVES = 9;                // chunks
+constexpr int CUT_WAITS = 4 * 1000 * 1000;    // of 0.1 us
 constexpr int WP = 68;                         // floats of a row of W, so that rows start four banks apart
 
 template <int DA>
@@ -63,6 +71,7 @@ struct ScanCtl {
     unsigned long long bar[B_COUNT];
     uint32_t tmem;
     int dead;
+    int item[4];                               // of a list of chains that is cut: chain, first chunk, last, cut
 };
 template <int DA>
 constexpr size_t scan_smem() { return 1024 + ScanTile<DA>::CTL + sizeof(ScanCtl); }
@@ -70,6 +79,20 @@ static_assert(scan_smem<128>() <= 227 * 1024 && scan_smem<64>() <= 227 * 1024, "
 
 struct ScanMaps {
     CUtensorMap r[DLA_ROLES], k[DLA_ROLES], v[DLA_ROLES], out[DLA_ROLES];
+};
+
+// Chains that are cut, in ascending order: the first `at` chunks of the walk are one piece, the rest another.  The first pieces come
+// first, then the chains that are whole, then the rests, longest first.  A piece's place is drawn from a counter when it starts, so
+// that a rest never waits for a piece that has not started (and hardly ever at all: whole chains lie between).
+struct ScanCuts {
+    int n;
+    int chain[SMS], at[SMS];
+    short order[SMS];                          // of the rests
+};
+constexpr int CUT_FLOATS = 128 * 128;          // a state that is handed over: up to 128 x 128, [x][column]
+struct CutSpace {                              // at the start of the workspace
+    unsigned next, ready[SMS];                 // zero at the launch
+    alignas(256) float state[SMS][CUT_FLOATS];
 };
 
 // The next bf16 part of two floats, which keep what its rounding left: exact, in one mixed multiply-add each.
@@ -87,7 +110,7 @@ __device__ __forceinline__ float load_bf16(const unsigned char* p) {
 }
 
 template <int DA, bool SUMS>
-__global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ ScanMaps maps, const __grid_constant__ DlaWalk w) {
+__global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ ScanMaps maps, const __grid_constant__ DlaWalk w, const __grid_constant__ ScanCuts cuts) {
     using L = ScanTile<DA>;
     extern __shared__ unsigned char raw[];
     const uint32_t base = smem_u32(raw);
@@ -95,14 +118,54 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
     unsigned char* const ringp = raw + (ring - base);
     ScanCtl& ctl = *reinterpret_cast<ScanCtl*>(ringp + L::CTL);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int nseg = SUMS ? w.segs - 1 : w.segs, seg = blockIdx.x % nseg;
-    int slice = blockIdx.x / nseg, role = 0;
+    const bool spread = !SUMS && w.span > 0;
+    const int nseg = SUMS ? w.segs - 1 : w.segs, seg = spread ? 0 : blockIdx.x % nseg;
+    int slice = blockIdx.x / nseg, role = 0, h = blockIdx.y, b = blockIdx.z, from = 0, to = INT_MAX, cut = -1;
+    CutSpace* const space = reinterpret_cast<CutSpace*>(w.seg_state);
+    if (spread) {
+        int per = 0;
+        for (int i = 0; i < w.roles; ++i) per += w.slices[i];
+        if (tid == 0) {
+            const int t = static_cast<int>(atomicAdd(&space->next, 1u)), total = per * w.H * w.B;
+            int chain, j = -1, x = 0, y = INT_MAX;
+            if (t < cuts.n) {
+                j = t;
+                chain = cuts.chain[j];
+                y = cuts.at[j];
+            } else if (t < total) {                          // the t - n'th whole one: j cut ones lie before it
+                int lo = 0, hi = cuts.n;
+                while (lo < hi) {
+                    const int mid = (lo + hi) / 2;
+                    if (cuts.chain[mid] - mid <= t - cuts.n) lo = mid + 1;
+                    else hi = mid;
+                }
+                chain = t - cuts.n + lo;
+            } else {
+                j = cuts.order[min(t - total, cuts.n - 1)];
+                chain = cuts.chain[j];
+                x = cuts.at[j];
+            }
+            ctl.item[0] = chain;
+            ctl.item[1] = x;
+            ctl.item[2] = y;
+            ctl.item[3] = j;
+        }
+        __syncthreads();
+        const int chain = ctl.item[0], bh = chain / per;
+        slice = chain % per;
+        h = bh % w.H;
+        b = bh / w.H;
+        from = ctl.item[1];
+        to = ctl.item[2];
+        cut = ctl.item[3];
+    }
     while (slice >= w.slices[role]) slice -= w.slices[role++];
     const DlaRole& ro = w.role[role];
-    const int b = blockIdx.z, h = blockIdx.y, col0 = slice * 128;
+    const int col0 = slice * 128;
     const int len = dla_length(w, b), chunks = (len + C - 1) / C;
     const bool reverse = ro.reverse != 0;
-    const int c0 = min(seg * w.seg_chunks, chunks), c1 = seg == w.segs - 1 ? chunks : min(c0 + w.seg_chunks, chunks);
+    const int c0 = min(spread ? from : seg * w.seg_chunks, chunks);
+    const int c1 = spread ? min(to, chunks) : seg == w.segs - 1 ? chunks : min(c0 + w.seg_chunks, chunks);
     const int todo = c1 - c0, outputs = SUMS ? 0 : todo, last_n = len - (chunks - 1) * C;       // tokens of the sequence's last chunk
     auto chunk_at = [&](int c) { return reverse ? chunks - 1 - (c0 + c) : c0 + c; };
     auto partial = [&](int c) { return chunk_at(c) == chunks - 1 && last_n < C; };
@@ -357,7 +420,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
         }
         if (!SUMS) {
             if (warp == SW + VW && lane == 0) bulk_wait();
-            dla_zero_tail<BF16>(w, ro, b, h, col0, ro.db - col0 < 128 ? ro.db - col0 : 128, chunks * C, seg, tid - 32 * (SW + VW), 32 * OW);
+            if (to == INT_MAX) dla_zero_tail<BF16>(w, ro, b, h, col0, ro.db - col0 < 128 ? ro.db - col0 : 128, chunks * C, seg, tid - 32 * (SW + VW), 32 * OW);
         }
     } else if (warp >= SW) {                                 // v: column `row`, 32 tokens from i0 on
         if (V_REGS < LAUNCH_REGS) regs_dec<V_REGS>();
@@ -460,7 +523,25 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
 #pragma unroll
             for (int x = 0; x < RD / 2; ++x) S[x] = make_float2(0.f, 0.f);
         } else {
-            read(w.segs > 1 ? pieces + seg * per : ro.state_in == nullptr ? nullptr : ro.state_in + chain * per);
+            if (from == 0) {
+                read(w.segs > 1 ? pieces + seg * per : ro.state_in == nullptr ? nullptr : ro.state_in + chain * per);
+            } else {                                         // what the chain's first piece left
+                if (lane == 0) {
+                    unsigned ready = 0;
+                    for (int i = 0; i < CUT_WAITS && ready == 0; ++i) {
+                        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];\n" : "=r"(ready) : "l"(&space->ready[cut]) : "memory");
+                        if (ready == 0) __nanosleep(100);
+                    }
+                    if (ready == 0) *dead = 1;
+                }
+                __syncwarp();
+                const float* p = space->state[cut] + x0 * 128 + row;
+#pragma unroll
+                for (int x = 0; x < RD / 2; ++x) {
+                    if (x % 16 == 0) asm volatile("" ::: "memory");
+                    S[x] = make_float2(__ldcg(p + 256 * x), __ldcg(p + 256 * x + 128));
+                }
+            }
         }
         auto put = [&]() {                                   // S before the next chunk
             if (!SUMS) {
@@ -504,8 +585,19 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
                 put();
             }
         }
+        if (!SUMS && to != INT_MAX) {                        // a first piece
+            float* p = space->state[cut] + x0 * 128 + row;
+#pragma unroll
+            for (int x = 0; x < RD / 2; ++x) {
+                p[256 * x] = S[x].x;
+                p[256 * x + 128] = S[x].y;
+            }
+            __threadfence();
+            asm volatile("bar.sync 3, %0;\n" ::"n"(32 * SW) : "memory");
+            if (tid == 0) asm volatile("st.release.gpu.global.u32 [%0], 1;\n" ::"l"(&space->ready[cut]) : "memory");
+        }
         float* const out = SUMS ? pieces + (seg + 1) * per : ro.state_out != nullptr ? ro.state_out + chain * per : nullptr;
-        if (out != nullptr && (SUMS || seg == w.segs - 1)) write(out);
+        if (out != nullptr && (SUMS || (seg == w.segs - 1 && to == INT_MAX))) write(out);
     }
     tc_before_sync();
     __syncthreads();
@@ -514,7 +606,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
 }
 
 template <int DA, bool SUMS>
-cudaError_t scan(const ScanMaps& maps, const DlaWalk& w, cudaStream_t stream) {
+cudaError_t scan(const ScanMaps& maps, const DlaWalk& w, const ScanCuts& cuts, cudaStream_t stream) {
     constexpr size_t smem = scan_smem<DA>();
     static std::atomic<int> regs{0};
     cudaError_t e = check_kernel_registers(k_dla_scan<DA, SUMS>, LAUNCH_REGS, regs);
@@ -525,17 +617,18 @@ cudaError_t scan(const ScanMaps& maps, const DlaWalk& w, cudaStream_t stream) {
     int n = 0;
     for (int i = 0; i < w.roles; ++i) n += w.slices[i];
     const unsigned segs = static_cast<unsigned>(SUMS ? w.segs - 1 : w.segs);
-    k_dla_scan<DA, SUMS><<<dim3(n * segs, w.H, w.B), ST, smem, stream>>>(maps, w);
+    const dim3 grid = cuts.n > 0 ? dim3(static_cast<unsigned>(n) * w.H * w.B + cuts.n) : dim3(n * segs, w.H, w.B);
+    k_dla_scan<DA, SUMS><<<grid, ST, smem, stream>>>(maps, w, cuts);
     return cudaGetLastError();
 }
 template <int DA>
-cudaError_t scans(const ScanMaps& maps, const DlaWalk& w, cudaStream_t stream) {
+cudaError_t scans(const ScanMaps& maps, const DlaWalk& w, const ScanCuts& cuts, cudaStream_t stream) {
     if (w.segs > 1) {
-        cudaError_t e = scan<DA, true>(maps, w, stream);
+        cudaError_t e = scan<DA, true>(maps, w, cuts, stream);
         if (e == cudaSuccess) e = launch_dla_prefix(w, C, stream);
         if (e != cudaSuccess) return e;
     }
-    return scan<DA, false>(maps, w, stream);
+    return scan<DA, false>(maps, w, cuts, stream);
 }
 
 }  // namespace
@@ -546,20 +639,54 @@ cudaError_t scans(const ScanMaps& maps, const DlaWalk& w, cudaStream_t stream) {
 // 50 (142) against 46 (122) with 64, 64 (189) against 74 (201) with 100.
 bool dla_scan_pays(int dtype, int T, int dk, int dv) { return dtype == SDM_BF16 && T > 0 && (dk > 64 || dv > 64 || T >= 64); }
 
-// With fewer CTAs than half of the SMs the tokens are cut, so that every SM has a piece, where that pays: a chunk takes 2.1 us
-// in the walk and about 1.1 in the walk for the sums, which with the joining launch costs 10 us more to begin with.
-void dla_scan_plan(DlaWalk& w) {
-    constexpr int64_t SMS = 152;
+namespace {
+
+int64_t scan_ctas(const DlaWalk& w) {
     int64_t ctas = 0;
     for (int i = 0; i < w.roles; ++i) ctas += (w.role[i].db + 127) / 128;
-    ctas *= static_cast<int64_t>(w.B) * w.H;
-    const int64_t chunks = (w.T + C - 1) / C;
+    return ctas * w.B * w.H;
+}
+
+}  // namespace
+
+// With fewer CTAs than half of the SMs the tokens are cut, so that every SM has a piece, where that pays: a chunk takes 2.1 us
+// in the walk and about 1.1 in the walk for the sums, which with the joining launch costs 10 us more to begin with.
+//
+// More CTAs than SMs are spread over these where the last round's time that this saves is more than its costs: about 6 us for the
+// cut chains' extra starts, and 1 us for every CTA's number.  Forward (backward), 10 x 16 heads of 128: 256 -> 154 us (532 -> 458)
+// with 64 chunks, 60 (30) of which are saved, 136 -> 93 (300 -> 274) with 32, 76 -> 60 (180 -> 174) with 16, where it is 15 (13); 133 -> 138
+// backward with 10, where it is 8; 80 x 16 heads, 16 chunks, backward, 11 saved in 26 rounds: 1,158 -> 1,182.
+void dla_scan_plan(DlaWalk& w) {
+    const int64_t ctas = scan_ctas(w), chunks = (w.T + C - 1) / C;
     int64_t segs = SMS / ctas;
     if (segs > chunks / 2) segs = chunks / 2;
     if (segs < 2 || chunks * (2 * segs - 3) <= 10 * segs) segs = 1;
     w.seg_chunks = static_cast<int>((chunks + segs - 1) / segs);
     w.segs = static_cast<int>((chunks + w.seg_chunks - 1) / w.seg_chunks);
+    const int64_t span = (ctas * chunks + SMS - 1) / SMS, rounds = (ctas + SMS - 1) / SMS;
+    w.span = ctas > SMS && rounds * chunks - span >= SPREAD_SAVES + rounds / 2 ? static_cast<int>(span) : 0;
 }
+size_t dla_scan_cut_bytes() { return sizeof(CutSpace); }
+
+namespace {
+
+ScanCuts scan_cuts(const DlaWalk& w) {
+    ScanCuts c{};
+    if (w.span == 0) return c;
+    const int64_t total = scan_ctas(w) * ((w.T + C - 1) / C), chunks = (w.T + C - 1) / C;
+    for (int64_t p = w.span; p < total && c.n < SMS; p += w.span) {
+        const int rest = static_cast<int>(p % chunks);       // behind the SM's own chains; the piece before it is the next SM's first
+        if (rest < CUT_LEAST || chunks - rest < CUT_LEAST) continue;
+        c.chain[c.n] = static_cast<int>(p / chunks);
+        c.at[c.n] = static_cast<int>(chunks - rest);
+        c.order[c.n] = static_cast<short>(c.n);
+        ++c.n;
+    }
+    std::sort(c.order, c.order + c.n, [&](short a, short b) { return c.at[a] != c.at[b] ? c.at[a] < c.at[b] : a < b; });
+    return c;
+}
+
+}  // namespace
 
 cudaError_t launch_dla_scan(DlaWalk& w, cudaStream_t stream) {
     ScanMaps m;
@@ -573,7 +700,14 @@ cudaError_t launch_dla_scan(DlaWalk& w, cudaStream_t stream) {
             (!r.partial && !token_map(&m.out[i], r.out, w.token_major, w.B, w.H, w.T, r.db)))
             return cudaErrorInvalidValue;
     }
-    return da <= 64 ? scans<64>(m, w, stream) : scans<128>(m, w, stream);
+    const ScanCuts cuts = scan_cuts(w);
+    if (cuts.n == 0) {
+        w.span = 0;
+    } else {
+        const cudaError_t e = cudaMemsetAsync(w.seg_state, 0, offsetof(CutSpace, state), stream);
+        if (e != cudaSuccess) return e;
+    }
+    return da <= 64 ? scans<64>(m, w, cuts, stream) : scans<128>(m, w, cuts, stream);
 }
 
 }  // namespace sdm

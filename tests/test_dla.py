@@ -176,6 +176,10 @@ CASES = [  # B, H, Hk, T, dk, dv, dtype, layout, lengths
     (2, 4, 2, 8, 128, 128, "bf16", "head_major", [8, 3]),
     (2, 2, 1, 63, 64, 64, "bf16", "token_major", [0, 63]),
     (2, 2, 1, 64, 64, 64, "bf16", "head_major", [64, 1]),
+    # more chains than SMs: some are cut and hand their state over
+    (10, 16, 8, 700, 64, 64, "bf16", "token_major", [700, 0, 699, 64, 1, 300, 65, 512, 700, 130]),
+    (4, 15, 5, 830, 128, 136, "bf16", "head_major", None),
+    (10, 16, 16, 641, 32, 40, "bf16", "head_major", None),
 ]
 
 
@@ -373,12 +377,12 @@ def test_gradient_against_differences(sdm):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("dtype,d,T", [("f32", 64, 100), ("bf16", 128, 700)])
-def test_captured_and_on_another_stream(sdm, dtype, d, T):
+@pytest.mark.parametrize("dtype,B,H,d,T", [("f32", 1, 2, 64, 100), ("bf16", 1, 2, 128, 700), ("bf16", 10, 16, 64, 700)])
+def test_captured_and_on_another_stream(sdm, dtype, B, H, d, T):
     """A captured forward, backward and step replay with new inputs, while another stream runs the same calls."""
     import torch
-    shape, one = sdm.DlaShape.make(1, 2, T, d, d, dtype=dtype), sdm.DlaShape.make(1, 2, 1, d, d, dtype=dtype)
-    s, new = _inputs(1, 2, 2, T, d, d, dtype), _inputs(1, 2, 2, T, d, d, dtype, seed=7)
+    shape, one = sdm.DlaShape.make(B, H, T, d, d, dtype=dtype), sdm.DlaShape.make(B, H, 1, d, d, dtype=dtype)
+    s, new = _inputs(B, H, H, T, d, d, dtype), _inputs(B, H, H, T, d, d, dtype, seed=7)
     y, state, ws = torch.empty_like(s["v"]), s["state"].clone(), _ws(sdm.dla_workspace_bytes(shape))
     wb, out = _ws(sdm.dla_backward_workspace_bytes(shape)), [torch.empty_like(s[n]) for n in ("q", "k", "v", "state")]
     tok = [s[n][:, :, :1].contiguous() for n in ("q", "k", "v")]
@@ -411,6 +415,18 @@ def test_captured_and_on_another_stream(sdm, dtype, d, T):
     torch.cuda.synchronize()
     assert torch.equal(y, want_y) and torch.equal(state, want_S) and torch.equal(y1, want_1)
     assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.gpu
+def test_cut_chains_give_what_whole_ones_give(sdm):
+    """Of ten sequences at once some chains are cut, of five none; the results are the same, bit for bit."""
+    import torch
+    s = _inputs(10, 16, 16, 1000, 64, 128, "bf16")
+    y, state = run_forward(sdm, s, sdm.DlaShape.make(10, 16, 1000, 64, 128, dtype="bf16"))
+    for i in (0, 5):
+        half = {n: x if n == "log_decay" else x[i:i + 5].contiguous() for n, x in s.items()}
+        y5, state5 = run_forward(sdm, half, sdm.DlaShape.make(5, 16, 1000, 64, 128, dtype="bf16"))
+        assert torch.equal(y[i:i + 5], y5) and torch.equal(state[i:i + 5], state5)
 
 
 @pytest.mark.gpu
