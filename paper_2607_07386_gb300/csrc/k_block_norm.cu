@@ -22,8 +22,8 @@ namespace sdm {
 
 namespace {
 
-// Threads of a CTA: one row or, where a row takes fewer than 256, several.
-__host__ __device__ constexpr int cta(int tpr) { return tpr < 256 ? 256 : tpr; }
+// Threads of a CTA: one row or, where a row takes 128 or fewer, several.
+__host__ __device__ constexpr int cta(int tpr) { return tpr < 256 ? 256 / tpr * tpr : tpr; }
 
 template <class D>
 __device__ __forceinline__ uint4 load16(const void* base, int64_t at) {
@@ -110,8 +110,11 @@ __device__ __forceinline__ void row_sum(float (&s)[N], float (*sh)[16][8], int& 
     turn ^= 1;
 }
 
-// CTAs of 256 threads on an SM: 80 and 128 registers a thread (four forward: 98 to 100 us for rows of 2,048, three: 95 to 98).
-constexpr int SMS = 152, FORE_CTAS = 3, BACK_CTAS = 2;
+// CTAs on an SM: of 256 threads three with 80 registers each (four: 98 to 100 us for rows of 2,048, three: 95 to 98), and
+// for the gradients two with 128.
+constexpr int SMS = 152;
+__host__ __device__ constexpr int fore_ctas(int tpr) { return tpr > 256 ? 1 : 768 / cta(tpr); }
+__host__ __device__ constexpr int back_ctas(int tpr) { return tpr > 256 ? 1 : 512 / cta(tpr); }
 
 // Threads a row, values a thread in pieces of 16 bytes, rows of a CTA at once.
 template <class D, int TPR, int VE>
@@ -153,8 +156,10 @@ struct Ahead {
         asm volatile("cp.async.commit_group;\n" ::: "memory");
     }
     __device__ __forceinline__ void start(const void* const (&src)[N]) {
+        if constexpr (S > 0) {
 #pragma unroll
-        for (int s = 0; s < S; ++s) copy(s, src);
+            for (int s = 0; s < S; ++s) copy(s, src);
+        }
     }
     __device__ __forceinline__ void wait() {
         if (S > 0) asm volatile("cp.async.wait_group %0;\n" ::"n"(S > 0 ? S - 1 : 0) : "memory");
@@ -176,7 +181,7 @@ struct Ahead {
 
 // A group of TPR threads takes `span` rows one after the other.  ROWGATE: every row has its gate, which comes with the row.
 template <class D, int TPR, int VE, int S, bool ROWGATE>
-__global__ void __launch_bounds__(cta(TPR), TPR > 256 ? 1 : FORE_CTAS) k_block_norm(const BlockNorm a, const int64_t span) {
+__global__ void __launch_bounds__(cta(TPR), fore_ctas(TPR)) k_block_norm(const BlockNorm a, const int64_t span) {
     extern __shared__ __align__(16) unsigned char ring[];
     using R = Row<D, TPR, VE>;
     constexpr int E = R::E, P = R::P, V = R::V;
@@ -306,7 +311,7 @@ struct NormCut {
 };
 
 template <class D, int TPR, int VE, int S, bool ROWGATE>
-__global__ void __launch_bounds__(cta(TPR), TPR > 256 ? 1 : BACK_CTAS) k_block_norm_backward(const BlockNorm a, const NormCut cut) {
+__global__ void __launch_bounds__(cta(TPR), back_ctas(TPR)) k_block_norm_backward(const BlockNorm a, const NormCut cut) {
     extern __shared__ __align__(16) unsigned char ring[];
     using R = Row<D, TPR, VE>;
     constexpr int E = R::E, P = R::P, V = R::V;
@@ -570,7 +575,7 @@ __global__ void __launch_bounds__(JC * JR) k_block_norm_join(const BlockNorm a, 
 NormCut norm_cut(int64_t M, int D, int tpr, bool shared) {
     NormCut c{};
     const int rows = cta(tpr) / tpr;
-    const int64_t most = static_cast<int64_t>(SMS) * (tpr > 256 ? 1 : BACK_CTAS) * rows;
+    const int64_t most = static_cast<int64_t>(SMS) * back_ctas(tpr) * rows;
     c.span = (M + most - 1) / most;
     const int64_t groups = (M + c.span - 1) / c.span;
     c.grid = static_cast<unsigned>((groups + rows - 1) / rows);
@@ -584,13 +589,19 @@ NormCut norm_cut(int64_t M, int D, int tpr, bool shared) {
 // and backward, with eight 95 and 152) in up to 256 threads, as several CTAs of an SM hide each other's waits.  Then it is what
 // moves with two 16-byte pieces of an array a thread: 16 bf16 values (rows of 4,096: 102 and 156 us, 512 threads of eight 107 and 176) or
 // 512 threads of eight float32 values (98 and 152, 256 of 16 101 and 231).  Then 512 threads of 16 and 32.
+// A power of two leaves threads without work where the width is none.  bf16 gradients, 134 MB an array: rows of 768 by 96 threads
+// 146 us, by 128 180; 1,280 by 160 154, by 256 204; 1,536 by 192 156, by 256 190; 2,560 by 160 of 16 163, by 256 193.  Forward: 101 and
+// 94, 97 and 115, 101 and 101, 99 and 98 (with a gate a row 117 and 112), so there it is 160 threads of eight alone.
 struct RowPlan {
     int tpr, ve;
 };
-RowPlan row_plan(int dtype, int D) {
+RowPlan row_plan(int dtype, int D, bool back) {
+    if (dtype == SDM_BF16) {
+        for (const RowPlan p : {RowPlan{32, 8}, {64, 8}, {96, 8}, {128, 8}, {160, 8}, {192, 8}, {256, 8}, {160, 16}, {256, 16}})
+            if (p.tpr * p.ve >= D && (back || (p.tpr & (p.tpr - 1)) == 0 || (p.tpr == 160 && p.ve == 8))) return p;
+    }
     RowPlan p{32, 8};
     while (p.tpr < 256 && p.tpr * p.ve < D) p.tpr *= 2;
-    if (p.tpr * p.ve < D && dtype == SDM_BF16) p.ve = 16;
     if (p.tpr * p.ve < D) p.tpr = 512;
     while (p.tpr * p.ve < D) p.ve *= 2;
     return p;
@@ -601,25 +612,33 @@ template <class D, int TPR, int VE, int N>
 constexpr size_t stage_bytes() { return static_cast<size_t>(cta(TPR)) * VE * D::BYTES * N; }
 template <class D, int TPR, int VE, int N>
 constexpr int stages(int ctas) {
-    const size_t most = 200 * 1024 / (TPR > 256 ? 1 : ctas) / stage_bytes<D, TPR, VE, N>();
+    const size_t most = 200 * 1024 / ctas / stage_bytes<D, TPR, VE, N>();
     return most > 4 ? 4 : static_cast<int>(most);
 }
 
-template <class D, class F>
+template <class D, bool BACK, class F>
 cudaError_t with_plan(const RowPlan& p, F f) {
 #define SDM_ROW(T, V) if (p.tpr == (T) && p.ve == (V)) return f(std::integral_constant<int, T>{}, std::integral_constant<int, V>{});
-    SDM_ROW(32, 8) SDM_ROW(64, 8) SDM_ROW(128, 8) SDM_ROW(256, 8) SDM_ROW(D::BYTES == 2 ? 256 : 512, D::BYTES == 2 ? 16 : 8) SDM_ROW(512, 16) SDM_ROW(512, 32)
+    if constexpr (D::BYTES == 2) {
+        if constexpr (BACK) {
+            SDM_ROW(96, 8) SDM_ROW(192, 8) SDM_ROW(160, 16)
+        }
+        SDM_ROW(160, 8) SDM_ROW(256, 16)
+    } else {
+        SDM_ROW(512, 8)
+    }
+    SDM_ROW(32, 8) SDM_ROW(64, 8) SDM_ROW(128, 8) SDM_ROW(256, 8) SDM_ROW(512, 16) SDM_ROW(512, 32)
 #undef SDM_ROW
     return cudaErrorInvalidValue;
 }
 
 template <class D, bool ROWGATE>
 cudaError_t forward(const RowPlan& p, const BlockNorm& a, cudaStream_t stream) {
-    return with_plan<D>(p, [&](auto T, auto V) {
+    return with_plan<D, false>(p, [&](auto T, auto V) {
         constexpr int rows = cta(T.value) / T.value;
-        const int64_t most = static_cast<int64_t>(SMS) * (T.value > 256 ? 1 : FORE_CTAS) * rows;
+        const int64_t most = static_cast<int64_t>(SMS) * fore_ctas(T.value) * rows;
         const int64_t span = (a.M + most - 1) / most, groups = (a.M + span - 1) / span;
-        constexpr int N = ROWGATE ? 3 : 2, S = stages<D, T.value, V.value, N>(FORE_CTAS);
+        constexpr int N = ROWGATE ? 3 : 2, S = stages<D, T.value, V.value, N>(fore_ctas(T.value));
         constexpr size_t smem = S * stage_bytes<D, T.value, V.value, N>();
         static std::atomic<unsigned long long> seen;
         const cudaError_t e = allow_smem(k_block_norm<D, T.value, V.value, S, ROWGATE>, smem, seen);
@@ -632,8 +651,8 @@ template <class D, bool ROWGATE>
 cudaError_t backward(const RowPlan& p, const BlockNorm& a, cudaStream_t stream) {
     const bool shared = a.dgate != nullptr && a.gate_rows > 1;
     const NormCut cut = norm_cut(a.M, a.D, p.tpr, shared);
-    cudaError_t e = with_plan<D>(p, [&](auto T, auto V) {
-        constexpr int S = stages<D, T.value, V.value, ROWGATE ? 5 : 4>(BACK_CTAS);
+    cudaError_t e = with_plan<D, true>(p, [&](auto T, auto V) {
+        constexpr int S = stages<D, T.value, V.value, ROWGATE ? 5 : 4>(back_ctas(T.value));
         constexpr size_t smem = S * stage_bytes<D, T.value, V.value, ROWGATE ? 5 : 4>();
         static std::atomic<unsigned long long> seen;
         const cudaError_t e = allow_smem(k_block_norm_backward<D, T.value, V.value, S, ROWGATE>, smem, seen);
@@ -651,16 +670,16 @@ cudaError_t backward(const RowPlan& p, const BlockNorm& a, cudaStream_t stream) 
 
 bool block_norm_supported(int D) { return D <= 512 * 32; }
 cudaError_t launch_block_norm(int dtype, const BlockNorm& a, cudaStream_t stream) {
-    const RowPlan p = row_plan(dtype, a.D);
+    const RowPlan p = row_plan(dtype, a.D, false);
     if (a.gate != nullptr && a.gate_rows == 1) return dtype == SDM_F32 ? forward<F32, true>(p, a, stream) : forward<BF16, true>(p, a, stream);
     return dtype == SDM_F32 ? forward<F32, false>(p, a, stream) : forward<BF16, false>(p, a, stream);
 }
 size_t block_norm_backward_bytes(int dtype, int64_t M, int64_t gate_rows, int D) {
     if (M == 0) return 0;
-    return norm_cut(M, D, row_plan(dtype, D).tpr, gate_rows > 1).total * 4;
+    return norm_cut(M, D, row_plan(dtype, D, true).tpr, gate_rows > 1).total * 4;
 }
 cudaError_t launch_block_norm_backward(int dtype, const BlockNorm& a, cudaStream_t stream) {
-    const RowPlan p = row_plan(dtype, a.D);
+    const RowPlan p = row_plan(dtype, a.D, true);
     if (a.gate != nullptr && a.gate_rows == 1) return dtype == SDM_F32 ? backward<F32, true>(p, a, stream) : backward<BF16, true>(p, a, stream);
     return dtype == SDM_F32 ? backward<F32, false>(p, a, stream) : backward<BF16, false>(p, a, stream);
 }

@@ -100,6 +100,9 @@ CASES = [  # M, D, dtype, gate_rows, which of gate, res_scale, gamma_post, gamma
     (21, 320, "bf16", 1, "p"), (40, 1024, "bf16", 1, "sp"), (40, 1024, "bf16", 7, "go"), (2500, 64, "f32", 2, "gso"), (40, 72, "bf16", 1, "op"),
     (3000, 2048, "bf16", 7, "gsop"), (3001, 1544, "f32", 17, "gsop"), (9000, 256, "bf16", 2, "gp"), (2000, 2048, "f32", 290, "go"),
     (900, 8192, "bf16", 3, "gsop"), (700, 8192, "bf16", 200, "gsop"), (700, 8192, "bf16", 1, "gsop"),
+    (1900, 768, "bf16", 30, "gsop"), (1900, 760, "bf16", 1, "gsop"), (1100, 1280, "bf16", 1, "gsop"), (1100, 1256, "bf16", 500, "gsop"),
+    (800, 1536, "bf16", 9, "gsop"), (800, 1528, "bf16", 1, "sop"), (900, 2560, "bf16", 1, "gsop"), (900, 2552, "bf16", 77, "gsp"),
+    (300, 4096, "f32", 7, "gsop"), (500, 4096, "bf16", 1, "gsop"),
 ]
 
 
