@@ -65,15 +65,14 @@ __device__ __forceinline__ void product(const float* v, const float* w, int c, f
 template <int TPR, int N>
 __device__ __forceinline__ void row_sum(float (&s)[N], float (*sh)[16][8], int& turn) {
     const int lane = threadIdx.x & 31;
-    if (N == 1) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
-        if (TPR == 32) return;
-    }
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < N ? s[i] : 0.f;
-    if (N > 1) {
+    if (N == 1) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+        s[0] = v[0];
+    } else {
 #pragma unroll
         for (int o = 16, n = 4; n > 0; o >>= 1, n >>= 1) {
             const bool up = lane & o;
@@ -88,9 +87,9 @@ __device__ __forceinline__ void row_sum(float (&s)[N], float (*sh)[16][8], int& 
         if (TPR == 32) {
 #pragma unroll
             for (int i = 0; i < N; ++i) s[i] = __shfl_sync(0xffffffffu, v[0], 4 * i);
-            return;
         }
     }
+    if (TPR == 32) return;
     const int warp = threadIdx.x >> 5, sub = warp / (TPR / 32), first = sub * (TPR / 32);
     if (N == 1 ? lane == 0 : lane % 4 == 0) sh[turn][warp][lane / 4] = v[0];
     asm volatile("bar.sync %0, %1;\n" ::"r"(sub + 1), "n"(TPR) : "memory");
