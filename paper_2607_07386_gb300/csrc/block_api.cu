@@ -74,6 +74,7 @@ DlaLayout dla_layout(const sdm_dla_shape* s, bool back) {
     const bool scan = sdm::dla_scan_pays(s->dtype, s->T, s->d_k, s->d_v);
     L.w.scan = scan;
     const size_t chains = static_cast<size_t>(s->B) * H;
+    if (chains == 0) return L;                               // H_k may be anything then
     size_t floats = 0;
     size_t share[sdm::DLA_ROLES] = {};
     auto add = [&](int call, sdm::DlaRole r, int group) {
@@ -114,7 +115,6 @@ DlaLayout dla_layout(const sdm_dla_shape* s, bool back) {
         r.inter = 1.f; r.intra = r.add = s->scale; r.reverse = 1; r.transposed = 1;
         add(2, r, H / Hk);
     }
-    if (chains == 0) return L;
     sdm::dla_plan(L.w);
     size_t state = 0;
     for (int i = 0; i < L.w.roles; ++i) {                    // a role's pieces have one state

@@ -103,6 +103,16 @@ def test_empty_calls_do_nothing(sdm):
     sdm.dla_step(_shape(sdm, T=1, B=0), None, None, None, None, None, None, n_slots=0, stream=0)
 
 
+@pytest.mark.parametrize("kw", [dict(H=0, H_k=0), dict(H=0, H_k=3), dict(B=0), dict(H=0, H_k=-1, T=0), dict(H=0, H_k=0, d_k=256, d_v=256, T=9000)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_empty_shapes_have_empty_workspaces(sdm, kw, dtype):
+    """No sequences or no heads: no bytes, no error, and the calls return."""
+    shape = _shape(sdm, dtype=dtype, **kw)
+    assert sdm.dla_workspace_bytes(shape) == 0 and sdm.dla_backward_workspace_bytes(shape) == 0
+    _forward(sdm, shape, workspace=None, workspace_nbytes=0)
+    sdm.dla_backward(shape, *[None] * 11, stream=0)
+
+
 # ------------------------------------------------------------------ parity
 def _inputs(B, H, Hk, T, dk, dv, dtype, token_major=False, seed=0, device="cuda"):
     import torch
