@@ -52,7 +52,7 @@ struct DlaWalk {
 __device__ __forceinline__ float dla_pow(float ld, int n) {
     if (n == 0) return 1.f;
     const float f = static_cast<float>(n), hi = f * ld, e = expf(hi);
-    if (!gdn_finite(hi)) return e;
+    if (!gdn_finite(hi) || !gdn_finite(e)) return e;
     return fmaf(e, fmaf(f, ld, -hi), e);
 }
 // The same as two floats: multiplied on once a chunk, a factor that is off by 2^-25 would be off by as much again every time.

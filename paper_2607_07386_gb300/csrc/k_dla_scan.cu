@@ -219,8 +219,10 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
             for (int c = 0; c < outputs; ++c) {
                 await(bar(B_P), c & 1, dead);
                 unsigned char* const to = ps + (c & 1) * 2 * MAT;
+                const int n = partial(c) ? last_n : C;
                 // A token past this one counts as zero, and where it is not finite, not as 0 times it: such products show in
-                // `odd` (0 times each, added up), and are then left out by choice.
+                // `odd` (0 times each, added up), and are then left out by choice.  So are zeros past the length times a
+                // power that is infinite (of states that grow).
                 float2 odd = make_float2(0.f, 0.f);
                 auto row = [&](int e, auto choose) {         // 32 columns
                     float p[32];
@@ -234,8 +236,9 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
                         for (int s = 0; s < 4; ++s) {
                             float2 f = __fmul2_rn(ww[s], make_float2(p[8 * q + 2 * s], p[8 * q + 2 * s + 1]));
                             if (choose) {
-                                if (ww[s].x == 0.f) f.x = 0.f;
-                                if (ww[s].y == 0.f) f.y = 0.f;
+                                const int j = 32 * e + 8 * q + 2 * s;
+                                if (ww[s].x == 0.f || j >= n) f.x = 0.f;
+                                if (ww[s].y == 0.f || j + 1 >= n) f.y = 0.f;
                             } else {
                                 odd = __ffma2_rn(f, make_float2(0.f, 0.f), odd);
                             }

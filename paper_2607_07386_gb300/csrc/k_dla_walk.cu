@@ -221,8 +221,9 @@ __global__ void __launch_bounds__(WT) k_dla_walk(const DlaWalk w) {
                         z[i][e] = __ffma2_rn(make_float2(q[i].z, q[i].w), make_float2(v[e].z, v[e].w), z[i][e]);
                     }
             }
-            // A token past this one in the walk counts with a zero, but not where its v is not finite: then it is left out by a
-            // test (tests in the loop above took it from 1 to 4.7 thousand cycles).
+            // A token past this one in the walk counts with a zero, but not where its v is not finite; one past the length does too,
+            // but not where its power is infinite (of states that grow).  Then it is left out by a test (tests in the loop above took
+            // it from 1 to 4.7 thousand cycles).
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -235,8 +236,8 @@ __global__ void __launch_bounds__(WT) k_dla_walk(const DlaWalk w) {
                     float2 u = make_float2(y[i][j], 0.f);    // in the same order
 #pragma unroll 1
                     for (int t = 0; t < C; t += 2) {
-                        if (ro.reverse ? t >= ti + i : t <= ti + i) u.x = fmaf(sm.P[ti + i][t], sm.v[tc + 16 * j][t], u.x);
-                        if (ro.reverse ? t + 1 >= ti + i : t + 1 <= ti + i) u.y = fmaf(sm.P[ti + i][t + 1], sm.v[tc + 16 * j][t + 1], u.y);
+                        if (ro.reverse ? t >= ti + i && t < n : t <= ti + i) u.x = fmaf(sm.P[ti + i][t], sm.v[tc + 16 * j][t], u.x);
+                        if (ro.reverse ? t + 1 >= ti + i && t + 1 < n : t + 1 <= ti + i) u.y = fmaf(sm.P[ti + i][t + 1], sm.v[tc + 16 * j][t + 1], u.y);
                     }
                     y[i][j] = u.x + u.y;
                 }

@@ -244,6 +244,27 @@ def test_decays_from_none_to_all(sdm, dtype, dk, dv):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,dk,dv,T,log_decay", [("f32", 64, 64, 20, 3.0), ("f32", 36, 20, 52, 1.4), ("f32", 200, 64, 20, 3.0),
+                                                    ("bf16", 128, 128, 40, 1.5), ("bf16", 64, 64, 100, 0.7), ("bf16", 256, 136, 40, 1.5)])
+def test_growth_over_a_partial_chunk(sdm, dtype, dk, dv, T, log_decay):
+    """States that grow: the powers of the sequence's tokens fit float32, those of a whole chunk (32 or 64 tokens) need not."""
+    import torch
+    from dla_reference import dla, dla_grads, near
+    s = _inputs(2, 2, 1, T, dk, dv, dtype)
+    s["log_decay"] = torch.tensor([log_decay, -0.1], device="cuda")
+    n = torch.tensor([T, T // 2], dtype=torch.int32, device="cuda")
+    shape = sdm.DlaShape.make(2, 2, T, dk, dv, H_k=1, dtype=dtype)
+    y, state = run_forward(sdm, s, shape, n)
+    want_y, want_S = dla(s["q"], s["k"], s["v"], s["log_decay"], s["state"], 1.0, n)
+    grads = run_backward(sdm, s, shape, n)
+    want = dla_grads(*(s[x] for x in ("q", "k", "v", "log_decay", "state")), 1.0, s["dy"], s["dstate"], n)
+    for b in range(2):
+        for name, g, w in zip(("y", "state", "dq", "dk", "dv", "dstate0"), (y, state, *grads), (want_y, want_S, *want)):
+            assert g[b].isfinite().all(), (name, b)
+            near(g[b], w[b], f"{name} of sequence {b}")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,dk", [("f32", 64), ("bf16", 128), ("bf16", 256)])
 @pytest.mark.parametrize("name", ["q", "k", "v"])
 @pytest.mark.parametrize("value", [math.nan, math.inf])
