@@ -235,9 +235,10 @@ __global__ void __launch_bounds__(WT) k_dla_walk(const DlaWalk w) {
                     }
                     float2 u = make_float2(y[i][j], 0.f);    // in the same order
 #pragma unroll 1
-                    for (int t = 0; t < C; t += 2) {
-                        if (ro.reverse ? t >= ti + i && t < n : t <= ti + i) u.x = fmaf(sm.P[ti + i][t], sm.v[tc + 16 * j][t], u.x);
-                        if (ro.reverse ? t + 1 >= ti + i && t + 1 < n : t + 1 <= ti + i) u.y = fmaf(sm.P[ti + i][t + 1], sm.v[tc + 16 * j][t + 1], u.y);
+                    for (int t = 0; t < n; ++t) {
+                        if (ro.reverse ? t < ti + i : t > ti + i) continue;
+                        float& s = t & 1 ? u.y : u.x;
+                        s = fmaf(sm.P[ti + i][t], sm.v[tc + 16 * j][t], s);
                     }
                     y[i][j] = u.x + u.y;
                 }
