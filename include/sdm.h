@@ -317,10 +317,12 @@ sdm_status sdm_recur_backward_q(const sdm_shape* shape, const int32_t* idx_w, co
 
 /* Reads (host pointer `code`, synchronising on `stream`) and clears the device
  * status word of the current device: 0 = no fault; bit 0 = a slot index outside
- * [0, N) (or, of the gated delta rule, a length outside [0, T] or a slot not below n_slots) was skipped; bit 1 = a slot list given to the recurrence (forward, chunkwise
+ * [0, N) (or, of the gated delta rule and the decayed linear attention, a length outside [0, T] or a slot
+ * not below n_slots) was skipped; bit 1 = a slot list given to the recurrence (forward, chunkwise
  * or backward) was not strictly ascending; bit 2 = a bounded device wait gave up (the
- * tensor-core score kernel's mbarrier waits, or the writer/reader hand-over of the
- * recurrence): the kernel returned early and its results are undefined; bit 3 = a
+ * tensor-core kernels' mbarrier waits, the writer/reader hand-over of the
+ * recurrence, or the hand-over of a cut chain's state in sdm_dla_forward and sdm_dla_backward):
+ * the kernel returned early and its results are undefined; bit 3 = a
  * selection invariant failed (a candidate list not ordered by score; results
  * undefined).  Returns SDM_ERR_TIMEOUT when bit 2 was set, else SDM_ERR_DEVICE when the
  * word was non-zero, else SDM_OK; *code always receives the whole word. */
@@ -510,7 +512,8 @@ size_t sdm_dla_backward_workspace_bytes(const sdm_dla_shape* shape);
  * lengths: NULL, or [B] int32 on the device, as in sdm_gdn_forward: what q, k and v hold past a
  * sequence's length is never used, y is zero there and the state stays; a length outside [0, T] is
  * clamped and sets bit 0 of the device status word.  With T = 0 nothing is done.  An infinity or NaN in
- * a live token reaches its own and later outputs and the state; never an earlier token's.
+ * a live token reaches its own and later outputs and the state; never an earlier token's.  Bit 2 of the status word (a
+ * bounded wait ran out, which no input causes): y and the state are undefined, as are the gradients of sdm_dla_backward.
  * workspace: sdm_dla_workspace_bytes(shape), 256-byte aligned; calls that overlap must not share it. */
 sdm_status sdm_dla_forward(const sdm_dla_shape* shape, const void* q, const void* k, const void* v,
                            const float* log_decay, const int32_t* lengths, float* state, void* y,
@@ -532,6 +535,20 @@ sdm_status sdm_dla_backward(const sdm_dla_shape* shape, const void* q, const voi
                             const float* log_decay, const int32_t* lengths, const float* state0,
                             const void* dy, const float* dstate, void* dq, void* dk, void* dv, float* dstate0,
                             void* workspace, size_t workspace_bytes, sdm_stream_t stream);
+
+/* How a call of this shape runs (host only, launches nothing; for tests that must reach a given form, and for tuning).
+ * backward: 0 for sdm_dla_forward, else sdm_dla_backward.  Writes the first n (<= 4) of, in order: 1 on the tensor cores or
+ * 0; pieces that a sequence's tokens are cut into, and chunks a piece (64 tokens on the tensor cores, else 32); chains (of
+ * a sequence, a head and up to 128 columns of a state) that are cut once and hand their state over within the launch. */
+sdm_status sdm_dla_plan(const sdm_dla_shape* shape, int backward, int32_t* out, int n);
+
+/* Test hook for the bounded waits: sdm_dla_forward (same arguments and workspace) with the states of cut chains withheld and
+ * the wait for them limited to wait_polls (1 .. 2^24) polls of 0.1 us or more.  The waits run out, every CTA returns, and bit 2 of the
+ * device status word is set; y and the state of the chains that are cut are undefined, of the others as always.
+ * SDM_ERR_UNSUPPORTED where no chain of `shape` is cut (sdm_dla_plan). */
+sdm_status sdm_test_dla_wait_timeout(const sdm_dla_shape* shape, const void* q, const void* k, const void* v,
+                                     const float* log_decay, const int32_t* lengths, float* state, void* y, void* workspace,
+                                     size_t workspace_bytes, int32_t wait_polls, sdm_stream_t stream);
 
 /* ------------------------------------------------------------------------------------------
  * The norms around a block, with its gate, residual scale and residual, row by row:

@@ -15,6 +15,7 @@ from ._binding import (  # noqa: F401
     GdnShape, LinearShape, gdn_workspace_bytes, gdn_backward_workspace_bytes, gdn_forward, gdn_step, gdn_backward,
     linear_workspace_bytes, linear_backward_workspace_bytes, linear, linear_backward,
     DlaShape, dla_workspace_bytes, dla_backward_workspace_bytes, dla_forward, dla_step, dla_backward,
+    DLA_PLAN_FIELDS, dla_plan, test_dla_wait_timeout,
     BlockNormShape, block_norm, block_norm_backward_workspace_bytes, block_norm_backward,
     GradList, grad_workspace_bytes, grad_norm, grad_clip,
 )

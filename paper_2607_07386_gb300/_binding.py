@@ -222,12 +222,14 @@ def lib():
                 getattr(L, f).restype = ctypes.c_size_t
                 getattr(L, f).argtypes = args
             L.sdm_dla_forward.argtypes = [_DSP] + [_VP] * 8 + [_SZ, _VP]
+            L.sdm_dla_plan.argtypes = [_DSP, ctypes.c_int, ctypes.POINTER(ctypes.c_int32), ctypes.c_int]
+            L.sdm_test_dla_wait_timeout.argtypes = [_DSP] + [_VP] * 8 + [_SZ, ctypes.c_int32, _VP]
             L.sdm_dla_step.argtypes = [_DSP] + [_VP] * 5 + [ctypes.c_int32, _VP, _VP, _VP]
             L.sdm_dla_backward.argtypes = [_DSP] + [_VP] * 13 + [_SZ, _VP]
             L.sdm_block_norm.argtypes = [_BSP] + [_VP] * 9
             L.sdm_block_norm_backward.argtypes = [_BSP] + [_VP] * 15 + [_SZ, _VP]
             L.sdm_grad_norm.argtypes = L.sdm_grad_clip.argtypes = [ctypes.c_int64, _GTP, ctypes.c_float, _VP, _VP, _SZ, _VP]
-            for f in ("sdm_dla_forward", "sdm_dla_step", "sdm_dla_backward", "sdm_block_norm", "sdm_block_norm_backward",
+            for f in ("sdm_dla_forward", "sdm_dla_plan", "sdm_test_dla_wait_timeout", "sdm_dla_step", "sdm_dla_backward", "sdm_block_norm", "sdm_block_norm_backward",
                       "sdm_grad_norm", "sdm_grad_clip"):
                 getattr(L, f).restype = ctypes.c_int
             for f in ("sdm_gdn_forward", "sdm_gdn_step", "sdm_gdn_backward", "sdm_linear", "sdm_linear_backward"):
@@ -624,6 +626,23 @@ def dla_backward(shape: DlaShape, q, k, v, log_decay, state0, dy, dstate, dq, dk
     _check(lib().sdm_dla_backward(ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lengths),
                                   _ptr(state0), _ptr(dy), _ptr(dstate), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dstate0),
                                   _ptr(workspace), nb, _stream(stream)))
+
+
+DLA_PLAN_FIELDS = ("tensor_cores", "pieces", "chunks", "cuts")
+
+
+def dla_plan(shape: DlaShape, backward: bool = False) -> dict:
+    """sdm_dla_plan: how a call of `shape` runs (host only)."""
+    arr = (ctypes.c_int32 * len(DLA_PLAN_FIELDS))()
+    _check(lib().sdm_dla_plan(ctypes.byref(shape), int(backward), arr, len(DLA_PLAN_FIELDS)))
+    return {name: int(arr[i]) for i, name in enumerate(DLA_PLAN_FIELDS)}
+
+
+def test_dla_wait_timeout(shape: DlaShape, q, k, v, log_decay, state, y, workspace, wait_polls: int, lengths=None, stream=None):
+    """sdm_test_dla_wait_timeout: dla_forward with cut chains' states withheld and a short wait for them (the bounded waits
+    must run out and set status bit 2)."""
+    _check(lib().sdm_test_dla_wait_timeout(ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lengths), _ptr(state),
+                                           _ptr(y), _ptr(workspace), _nbytes(workspace) or 0, int(wait_polls), _stream(stream)))
 
 
 def block_norm(shape: BlockNormShape, x, y, h, z, gate=None, res_scale=None, gamma_post=None, gamma_pre=None, stream=None):

@@ -147,6 +147,33 @@ cudaError_t dla_run(int dtype, DlaLayout& L, const DlaCall* calls, char* ws, cud
     return e;
 }
 
+// cut_polls > 0: as a test, with cut chains' states withheld and that limit to the waits for them.
+sdm_status dla_forward(const char* who, const sdm_dla_shape* s, const void* q, const void* k, const void* v, const float* log_decay,
+                       const int32_t* lengths, float* state, void* y, void* workspace, size_t workspace_bytes, int32_t cut_polls, sdm_stream_t stream) {
+    const DlaSizes z = dla_sizes(s);
+    DlaLayout L = dla_layout(s, false);
+    const Buf bufs[] = {{"q", q, z.qk, 16, false, false}, {"k", k, z.qk, 16, false, false}, {"v", v, z.v, 16, false, false},
+                        {"log_decay", log_decay, static_cast<size_t>(s->H) * 4, 4, false, false},
+                        {"lengths", lengths, static_cast<size_t>(s->B) * 4, 4, true, false},
+                        {"state", state, z.state, 16, false, true}, {"y", y, z.v, 16, false, true},
+                        {"workspace", workspace, L.total, 16, true, true}};
+    SDM_TRY(check_bufs(who, bufs, 8));
+    SDM_TRY(check_ws(who, workspace, workspace_bytes, L.total));
+    SDM_TRY(sdm::api_status_word(&L.w.err));
+    if (s->T == 1 && lengths == nullptr) {
+        const sdm::DlaStep d{q, k, v, log_decay, nullptr, state, y, s->B, s->H, s->H_k, s->d_k, s->d_v, s->B, s->scale, L.w.err};
+        return done(sdm::launch_dla_step(s->dtype, d, reinterpret_cast<cudaStream_t>(stream)), who);
+    }
+    L.w.log_decay = log_decay;
+    L.w.lengths = lengths;
+    if (cut_polls > 0) {
+        L.w.cut_polls = cut_polls;
+        L.w.cut_hold = 1;
+    }
+    const DlaCall call{q, k, v, y, state, state};
+    return done(dla_run(s->dtype, L, &call, static_cast<char*>(workspace), reinterpret_cast<cudaStream_t>(stream)), who);
+}
+
 // ------------------------------------------------------------------ block norm
 sdm_status block_norm_check(const sdm_block_norm_shape* s) {
     if (!s) return fail(SDM_ERR_INVALID_ARG, "shape is NULL");
@@ -273,24 +300,27 @@ sdm_status sdm_dla_forward(const sdm_dla_shape* s, const void* q, const void* k,
                            const int32_t* lengths, float* state, void* y, void* workspace, size_t workspace_bytes, sdm_stream_t stream) {
     SDM_TRY(dla_check(s));
     if (static_cast<size_t>(s->B) * s->H * s->T == 0) return sdm::api_ok();
-    const DlaSizes z = dla_sizes(s);
-    DlaLayout L = dla_layout(s, false);
-    const Buf bufs[] = {{"q", q, z.qk, 16, false, false}, {"k", k, z.qk, 16, false, false}, {"v", v, z.v, 16, false, false},
-                        {"log_decay", log_decay, static_cast<size_t>(s->H) * 4, 4, false, false},
-                        {"lengths", lengths, static_cast<size_t>(s->B) * 4, 4, true, false},
-                        {"state", state, z.state, 16, false, true}, {"y", y, z.v, 16, false, true},
-                        {"workspace", workspace, L.total, 16, true, true}};
-    SDM_TRY(check_bufs("sdm_dla_forward", bufs, 8));
-    SDM_TRY(check_ws("sdm_dla_forward", workspace, workspace_bytes, L.total));
-    SDM_TRY(sdm::api_status_word(&L.w.err));
-    if (s->T == 1 && lengths == nullptr) {
-        const sdm::DlaStep d{q, k, v, log_decay, nullptr, state, y, s->B, s->H, s->H_k, s->d_k, s->d_v, s->B, s->scale, L.w.err};
-        return done(sdm::launch_dla_step(s->dtype, d, reinterpret_cast<cudaStream_t>(stream)), "sdm_dla_forward");
-    }
-    L.w.log_decay = log_decay;
-    L.w.lengths = lengths;
-    const DlaCall call{q, k, v, y, state, state};
-    return done(dla_run(s->dtype, L, &call, static_cast<char*>(workspace), reinterpret_cast<cudaStream_t>(stream)), "sdm_dla_forward");
+    return dla_forward("sdm_dla_forward", s, q, k, v, log_decay, lengths, state, y, workspace, workspace_bytes, 0, stream);
+}
+
+sdm_status sdm_dla_plan(const sdm_dla_shape* s, int backward, int32_t* out, int n) {
+    SDM_TRY(dla_check(s));
+    if (!out || n < 0 || n > 4) return fail(SDM_ERR_INVALID_ARG, "sdm_dla_plan: out must be non-NULL and n in [0, 4]");
+    const DlaLayout L = dla_layout(s, backward != 0);
+    const int32_t v[4] = {L.w.scan, L.w.segs, L.w.seg_chunks, L.w.span > 0 ? sdm::dla_scan_cuts(L.w) : 0};
+    for (int i = 0; i < n; ++i) out[i] = v[i];
+    return sdm::api_ok();
+}
+
+sdm_status sdm_test_dla_wait_timeout(const sdm_dla_shape* s, const void* q, const void* k, const void* v, const float* log_decay,
+                                     const int32_t* lengths, float* state, void* y, void* workspace, size_t workspace_bytes,
+                                     int32_t wait_polls, sdm_stream_t stream) {
+    const char* who = "sdm_test_dla_wait_timeout";
+    SDM_TRY(dla_check(s));
+    if (wait_polls < 1 || wait_polls > (1 << 24)) return fail(SDM_ERR_INVALID_ARG, "%s: wait_polls must be in [1, 2^24]", who);
+    const DlaLayout L = dla_layout(s, false);
+    if (L.w.span == 0 || sdm::dla_scan_cuts(L.w) == 0) return fail(SDM_ERR_UNSUPPORTED, "%s: no chain of this shape is cut", who);
+    return dla_forward(who, s, q, k, v, log_decay, lengths, state, y, workspace, workspace_bytes, wait_polls, stream);
 }
 
 sdm_status sdm_dla_step(const sdm_dla_shape* s, const void* q, const void* k, const void* v, const float* log_decay, const int32_t* slots,

@@ -44,6 +44,8 @@ struct DlaWalk {
     // Or the scan spreads more chains than SMs evenly over these: a list of all chains' chunks, one chain after the other, is cut
     // every `span` chunks (0: it is not).  A chain that is cut hands its state over in seg_state.
     int span;
+    int cut_polls;            // of the hand-over, before its wait gives up
+    int cut_hold;             // test hook: no state is handed over
     float* seg_state;
     int64_t seg_role[DLA_ROLES];      // where a role's sums start, in floats
 };
@@ -94,6 +96,7 @@ cudaError_t launch_dla(int dtype, DlaWalk& w, cudaStream_t stream);
 bool dla_scan_pays(int dtype, int T, int dk, int dv);
 void dla_scan_plan(DlaWalk& w);
 size_t dla_scan_cut_bytes();
+int dla_scan_cuts(const DlaWalk& w);              // chains that are cut
 cudaError_t launch_dla_scan(DlaWalk& w, cudaStream_t stream);
 // The states that the pieces start from, chunks of `chunk` tokens.
 cudaError_t launch_dla_prefix(const DlaWalk& w, int chunk, cudaStream_t stream);

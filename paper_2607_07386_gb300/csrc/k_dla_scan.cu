@@ -49,7 +49,6 @@ static_assert(SW * STATE_REGS + VW * V_REGS + (OW + PW) * REST_REGS <= (SW + VW 
 constexpr uint32_t S_COL = 0, D_COL = 128, V_COL = 192, P_COL = 288, O_COL = 352, I_COL = 416, T_COLS = 512;
 constexpr int CUT_LEAST = 4;                   // chunks of a piece
 constexpr int SPREAD_SAVES = 9;                // chunks
-constexpr int CUT_WAITS = 4 * 1000 * 1000;    // of 0.1 us
 constexpr int WP = 68;                         // floats of a row of W, so that rows start four banks apart
 
 template <int DA>
@@ -60,8 +59,8 @@ struct ScanTile {
 };
 // Barriers.  Completed by copies and MMAs: a stage's tile; P; D (per 64 rows of da); S's parts read; O, and with it I.  By
 // warps: the parts of P (and P taken out); of g v; of S; D taken out; O and I taken out; what lies past the length is zero.
-// By both: a stage is free.
-enum { B_FULL = 0, B_FREE = 4, B_P = 8, B_D, B_D1, B_SFREE, B_O, B_PS, B_V, B_S, B_DFREE, B_DFREE1, B_OFREE, B_ZERO, B_COUNT };
+// By both: a stage is free.  And every product of the walk.
+enum { B_FULL = 0, B_FREE = 4, B_P = 8, B_D, B_D1, B_SFREE, B_O, B_PS, B_V, B_S, B_DFREE, B_DFREE1, B_OFREE, B_ZERO, B_END, B_COUNT };
 struct ScanCtl {
     float W[C * WP];
     float add[2][C], inter[2][C];              // weights of a whole chunk and of the partial one
@@ -83,7 +82,8 @@ struct ScanMaps {
 
 // Chains that are cut, in ascending order: the first `at` chunks of the walk are one piece, the rest another.  The first pieces come
 // first, then the chains that are whole, then the rests, longest first.  A piece's place is drawn from a counter when it starts, so
-// that a rest never waits for a piece that has not started (and hardly ever at all: whole chains lie between).
+// that a rest never waits for a piece that has not started (and hardly ever at all: whole chains lie between).  Where it has waited
+// for w.cut_polls times about 0.1 us or more, it gives up, as every bounded wait: what it writes is undefined, and status bit 2 says so.
 struct ScanCuts {
     int n;
     int chain[SMS], at[SMS];
@@ -325,6 +325,11 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
                 }
                 __syncwarp();
             }
+            if (todo > 0) {                                  // whatever became of the waits, no product outlives the CTA
+                if (elect_one()) mma_commit(bar(B_END));
+                __syncwarp();
+                mbar_wait(bar(B_END), 0);
+            }
         } else if (lane == 0) {                              // copies
             const int hr = h / (w.H / ro.hr), hk = h / (w.H / ro.hk), hv = h / (w.H / ro.hv);
             int loaded = 0;
@@ -345,9 +350,8 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
                 tma_load_4d(t + L::V, &maps.v[role], col0, at, hv, b, fb);
                 tma_load_4d(t + L::V + 8192, &maps.v[role], col0 + 64, at, hv, b, fb);
             }
-            if (*dead)                                       // the copies in flight land before the CTA ends
-                for (int j = loaded > L::STAGES ? loaded - L::STAGES : 0; j < loaded; ++j)
-                    mbar_wait(bar(B_FULL + j % L::STAGES), (j / L::STAGES) & 1);
+            for (int j = loaded > L::STAGES ? loaded - L::STAGES : 0; j < loaded; ++j)     // nor does a copy
+                mbar_wait(bar(B_FULL + j % L::STAGES), (j / L::STAGES) & 1);
         }
     } else if (warp >= SW + VW) {                            // outputs: column `row`, all tokens
         regs_dec<REST_REGS>();
@@ -531,7 +535,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
             } else {                                         // what the chain's first piece left
                 if (lane == 0) {
                     unsigned ready = 0;
-                    for (int i = 0; i < CUT_WAITS && ready == 0; ++i) {
+                    for (int i = w.cut_polls; i > 0 && ready == 0; --i) {
                         asm volatile("ld.acquire.gpu.global.u32 %0, [%1];\n" : "=r"(ready) : "l"(&space->ready[cut]) : "memory");
                         if (ready == 0) __nanosleep(100);
                     }
@@ -597,7 +601,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
             }
             __threadfence();
             asm volatile("bar.sync 3, %0;\n" ::"n"(32 * SW) : "memory");
-            if (tid == 0) asm volatile("st.release.gpu.global.u32 [%0], 1;\n" ::"l"(&space->ready[cut]) : "memory");
+            if (tid == 0 && !w.cut_hold) asm volatile("st.release.gpu.global.u32 [%0], 1;\n" ::"l"(&space->ready[cut]) : "memory");
         }
         float* const out = SUMS ? pieces + (seg + 1) * per : ro.state_out != nullptr ? ro.state_out + chain * per : nullptr;
         if (out != nullptr && (SUMS || (seg == w.segs - 1 && to == INT_MAX))) write(out);
@@ -668,6 +672,7 @@ void dla_scan_plan(DlaWalk& w) {
     w.segs = static_cast<int>((chunks + w.seg_chunks - 1) / w.seg_chunks);
     const int64_t span = (ctas * chunks + SMS - 1) / SMS, rounds = (ctas + SMS - 1) / SMS;
     w.span = ctas > SMS && rounds * chunks - span >= SPREAD_SAVES + rounds / 2 ? static_cast<int>(span) : 0;
+    w.cut_polls = 4 * 1000 * 1000 + 32 * static_cast<int>(chunks);      // a first piece takes 2.1 us a chunk
 }
 size_t dla_scan_cut_bytes() { return sizeof(CutSpace); }
 
@@ -690,6 +695,8 @@ ScanCuts scan_cuts(const DlaWalk& w) {
 }
 
 }  // namespace
+
+int dla_scan_cuts(const DlaWalk& w) { return scan_cuts(w).n; }
 
 cudaError_t launch_dla_scan(DlaWalk& w, cudaStream_t stream) {
     ScanMaps m;

@@ -113,6 +113,19 @@ def test_empty_shapes_have_empty_workspaces(sdm, kw, dtype):
     sdm.dla_backward(shape, *[None] * 11, stream=0)
 
 
+def test_plan_and_wait_hook_refusals(sdm):
+    """sdm_dla_plan is host-only; the hook takes shapes with cut chains and limits from 1 on alone."""
+    cut, whole = _shape(sdm, B=10, H=16, H_k=16, T=1000, d_k=64, d_v=128), _shape(sdm)
+    assert sdm.dla_plan(cut)["cuts"] > 0 and sdm.dla_plan(whole)["cuts"] == 0
+    assert set(sdm.dla_plan(cut, backward=True)) == set(sdm.DLA_PLAN_FIELDS)
+    arr = (ctypes.c_int32 * 8)()
+    assert sdm.lib().sdm_dla_plan(ctypes.byref(cut), 0, arr, 5) == 1 and "[0, 4]" in sdm.last_error()
+    assert sdm.lib().sdm_dla_plan(ctypes.byref(_shape(sdm, T=-1)), 0, arr, 4) == 1
+    args = [A, 2 * A, 3 * A, 5 * A, None, 6 * A, 7 * A, 64 * A, 1 << 40]
+    for shape, polls, status, word in ((whole, 10, 2, "no chain"), (cut, 0, 1, "wait_polls"), (cut, (1 << 24) + 1, 1, "wait_polls")):
+        assert sdm.lib().sdm_test_dla_wait_timeout(ctypes.byref(shape), *args, polls, None) == status and word in sdm.last_error()
+
+
 # ------------------------------------------------------------------ parity
 def _inputs(B, H, Hk, T, dk, dv, dtype, token_major=False, seed=0, device="cuda"):
     import torch
@@ -458,6 +471,30 @@ def test_cut_chains_give_what_whole_ones_give(sdm):
         half = {n: x if n == "log_decay" else x[i:i + 5].contiguous() for n, x in s.items()}
         y5, state5 = run_forward(sdm, half, sdm.DlaShape.make(5, 16, 1000, 64, 128, dtype="bf16"))
         assert torch.equal(y[i:i + 5], y5) and torch.equal(state[i:i + 5], state5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lengths,polls", [(None, 1 << 12), (None, 1), ([0, 1000, 64, 65, 1, 999, 300, 1000, 512, 130], 1)])
+def test_a_withheld_state_ends_in_a_status(sdm, lengths, polls):
+    """Cut chains whose first piece hands nothing over: the wait runs out, every CTA returns, and the status word says so.  Whole
+    chains keep their results, and the next call runs as always."""
+    import torch
+    B, H, T, dk, dv = 10, 16, 1000, 64, 128
+    s = _inputs(B, H, H, T, dk, dv, "bf16")
+    shape = sdm.DlaShape.make(B, H, T, dk, dv, dtype="bf16")
+    cuts = sdm.dla_plan(shape)["cuts"]
+    n = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    want_y, want_S = run_forward(sdm, s, shape, n)
+    assert 0 < cuts < B * H and sdm.device_status() == 0
+    y, state = torch.zeros_like(want_y), s["state"].clone()
+    sdm.test_dla_wait_timeout(shape, s["q"], s["k"], s["v"], s["log_decay"], state, y, _ws(sdm.dla_workspace_bytes(shape)), polls, lengths=n)
+    torch.cuda.synchronize()
+    code = ctypes.c_int32(0)
+    assert sdm.lib().sdm_device_status(ctypes.byref(code), None) == 5 and code.value == 4
+    same = [torch.equal(y[b, h], want_y[b, h]) and torch.equal(state[b, h], want_S[b, h]) for b in range(B) for h in range(H)]
+    assert sum(same) >= B * H - cuts                         # a cut chain whose tokens end in its first piece may be right, too
+    again = run_forward(sdm, s, shape, n)
+    assert torch.equal(again[0], want_y) and torch.equal(again[1], want_S) and sdm.device_status() == 0
 
 
 @pytest.mark.gpu
