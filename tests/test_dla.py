@@ -473,6 +473,55 @@ def test_cut_chains_give_what_whole_ones_give(sdm):
         assert torch.equal(y[i:i + 5], y5) and torch.equal(state[i:i + 5], state5)
 
 
+# Chains that are cut, in the forward, the backward or both: B, H, Hk, T, dk, dv, dtype, layout, lengths, (forward, backward)
+CUT = [
+    (10, 16, 16, 1000, 64, 128, "bf16", "head_major", None, (True, True)),
+    # reversed walks that begin with a partial chunk, and pieces past the end of short sequences
+    (10, 16, 8, 1000, 64, 40, "bf16", "token_major", [1000, 0, 999, 64, 1, 300, 65, 512, 961, 130], (True, True)),
+    # the long sequence's rest starts while its first piece still runs
+    (10, 16, 8, 1000, 32, 32, "bf16", "head_major", [0] * 7 + [1000, 0, 0], (True, True)),
+    # a contraction in two pieces, two slices of the state, key heads of three value heads
+    (4, 15, 5, 1600, 128, 136, "bf16", "head_major", None, (False, True)),
+    (6, 16, 8, 1200, 136, 64, "bf16", "token_major", [1200, 1199, 0, 640, 63, 1111], (True, False)),
+    (8, 10, 10, 1400, 136, 72, "bf16", "head_major", None, (True, True)),
+]
+
+
+def test_what_is_cut(sdm):
+    """The shapes that stand for cut chains are cut by the rule, so that another constant there does not empty the tests."""
+    def cuts(B, H, Hk, T, dk, dv):
+        shape = sdm.DlaShape.make(B, H, T, dk, dv, H_k=Hk)
+        return tuple(sdm.dla_plan(shape, backward=b)["cuts"] > 0 for b in (False, True))
+
+    for case in CUT:
+        assert cuts(*case[:6]) == case[-1], case
+    assert cuts(10, 16, 16, 1000, 64, 128) == (True, True) and cuts(5, 16, 16, 1000, 64, 128) == (False, False)      # equal bit for bit, below
+    assert cuts(8, 16, 16, 4096, 128, 128) == (False, True)                                      # the 1.4B layer
+    for B, H, Hk, T, dk, dv in ((1, 1, 1, 3000, 64, 64), (3, 2, 1, 1100, 128, 128)):             # few chains, in pieces
+        assert sdm.dla_plan(sdm.DlaShape.make(B, H, T, dk, dv, H_k=Hk))["pieces"] > 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", CUT)
+def test_cut_chains_against_the_definition(sdm, case):
+    test_forward_and_backward(sdm, *case[:9])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lengths", [None, [1000, 0, 999, 64, 1, 300, 65, 512, 961, 130]])
+def test_cut_chains_have_the_gradients_of_whole_ones(sdm, lengths):
+    """The backward of ten sequences at once, whose chains are cut, and of five, whose chains are not: the same, bit for bit."""
+    import torch
+    s = _inputs(10, 16, 8, 1000, 64, 128, "bf16")
+    n = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    got = run_backward(sdm, s, sdm.DlaShape.make(10, 16, 1000, 64, 128, H_k=8), n)
+    for i in (0, 5):
+        half = {x: t if x == "log_decay" else t[i:i + 5].contiguous() for x, t in s.items()}
+        five = run_backward(sdm, half, sdm.DlaShape.make(5, 16, 1000, 64, 128, H_k=8), None if n is None else n[i:i + 5].contiguous())
+        for name, a, b in zip(("dq", "dk", "dv", "dstate0"), got, five):
+            assert torch.equal(a[i:i + 5], b), name
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("lengths,polls", [(None, 1 << 12), (None, 1), ([0, 1000, 64, 65, 1, 999, 300, 1000, 512, 130], 1)])
 def test_a_withheld_state_ends_in_a_status(sdm, lengths, polls):
