@@ -142,6 +142,53 @@ def test_many_tensors_and_repeats(sdm):  # noqa: F811
     assert abs(twice[0] - math.sqrt(2) * _norm([grads[5]])) <= 1e-6 * twice[0]
 
 
+def _list_sizes(filled, empty):
+    """`filled` sizes of up to three blocks' values, with empty tensors at the places given."""
+    sizes = [1 + (977 * i) % 20011 if i % 50 == 0 else 1 + (37 * i) % 700 for i in range(filled)]
+    for at in sorted(empty):
+        sizes.insert(at, 0)
+    return sizes
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("filled,empty", [(64, []), (65, []), (64, [0, 64, 65]), (960, []), (960, [960, 961, 962]), (961, []), (961, [960]),
+                                          (2000, [0, 960, 961, 1922, 2003]), (2881, [])])
+@pytest.mark.parametrize("kind", ["f32", "mixed"])
+def test_lists_at_and_past_a_launch(sdm, filled, empty, kind):  # noqa: F811
+    """A launch takes up to 64 or up to 960 tensors: lists of one, of several, and with empty tensors where one ends.  The
+    workspace is as long as asked for and no longer."""
+    import torch
+    sizes = _list_sizes(filled, empty)
+    f, b = torch.float32, torch.bfloat16
+    types = [f if kind == "f32" or i % 3 == 0 else b for i in range(len(sizes))]
+    grads = _flat(sizes, types, seed=filled)
+    kept = [g.clone() for g in grads]
+    outs = [torch.full_like(g, math.nan) for g in grads]
+    want = _norm([torch.cat([g.double() for g in grads])])
+    limit = want / 4
+    for out, call in ((None, "grad_norm"), (outs, "grad_clip"), (None, "grad_clip")):
+        lst = sdm.GradList.make(grads, out)
+        n = sdm.grad_workspace_bytes(lst)
+        ws = torch.full((n + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+        stats = torch.full((4,), -1.0, device="cuda")
+        getattr(sdm, call)(lst, limit, stats[:2], ws, workspace_nbytes=n)
+        assert (ws[n:] == 0xA5).all() and (stats[2:] == -1).all()
+        norm, factor = stats[:2].tolist()
+        assert abs(norm - want) <= 1e-6 * want and abs(factor - 0.25) <= 1e-6 * 0.25
+        if call == "grad_norm":
+            assert all(torch.equal(g, k) for g, k in zip(grads, kept))
+            first = stats.clone()
+            continue
+        assert torch.equal(stats, first)                     # whichever call, however often
+        for t, half in ((f, 2.0 ** -24), (b, 2.0 ** -8)):
+            if t not in types:
+                continue
+            o, g = (torch.cat([x for x, u in zip(xs, types) if u == t]).double() for xs in (grads if out is None else out, kept))
+            assert ((o - g * 0.25).abs() <= (half + 1e-6) * (g * 0.25).abs()).all()
+    with pytest.raises(sdm.SdmError, match="too small"):
+        sdm.grad_clip(lst, limit, stats[:2], ws, workspace_nbytes=n - 1)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("size", [1e38, 1e30, 1e-15, 1e-25, 1e-36])
 def test_whole_range_of_values(sdm, size):  # noqa: F811
