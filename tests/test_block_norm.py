@@ -280,3 +280,54 @@ def test_captured_beside_another_stream(sdm):  # noqa: F811
         calls(new, two)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(one[0] + one[1], two[0] + two[1]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gate_rows", [1, 4096])
+def test_rows_past_32_bits(sdm, gate_rows):  # noqa: F811
+    """More than 2^31 values an array: the last rows, the last gate and the vectors' gradients over all of them."""
+    import torch
+    from dla_reference import block_norm, near, rms_norm
+    D, eps, tail = 2048, 1e-5, 61
+    M = 2 ** 31 // D + 77
+    s = _inputs(M, D, "bf16", gate_rows, "gsop")
+    assert s["x"].numel() > 2 ** 31
+    vec = {n: s[n] for n in VECTORS}
+    shape = sdm.BlockNormShape.make(M, D, dtype="bf16", gate_rows=gate_rows, eps=eps)
+    h, z = (torch.full_like(s["x"], math.nan) for _ in range(2))
+    sdm.block_norm(shape, s["x"], s["y"], h, z, **vec)
+    out = {n: torch.full_like(s[n], math.nan) for n in VECTORS}
+    dx, dy = (torch.full_like(s["x"], math.nan) for _ in range(2))
+    ws = torch.empty(sdm.block_norm_backward_workspace_bytes(shape), dtype=torch.uint8, device="cuda")
+    sdm.block_norm_backward(shape, s["y"], h, s["dz"], s["dh"], dx, dy, **vec, **{"d" + n: out[n] for n in VECTORS}, workspace=ws)
+    first = M // gate_rows * gate_rows - gate_rows                                       # whole gates up to the end
+    rows = slice(first if gate_rows > 1 else M - tail, M)
+    gates = s["gate"][first // gate_rows:] if gate_rows > 1 else s["gate"][M - tail:]
+    live = {n: vec[n].double().requires_grad_(True) for n in VECTORS if n != "gate"}
+    gate, y = gates.double().requires_grad_(True), s["y"][rows].double().requires_grad_(True)
+    want_h, _ = block_norm(s["x"][rows], y, gate, live["res_scale"], live["gamma_post"], None, gate_rows, eps)
+    near(h[rows], want_h.detach(), "h")
+    stored = h[rows].double().requires_grad_(True)
+    want_z = rms_norm(stored, live["gamma_pre"], eps)
+    near(z[rows], want_z.detach(), "z")
+    (pre,) = torch.autograd.grad(want_z, stored, s["dz"][rows].double(), retain_graph=True)
+    want_dx = s["dh"][rows].double() + pre
+    near(dx[rows], want_dx, "dx")
+    want_dy, want_gate = torch.autograd.grad(want_h, (y, gate), want_dx)
+    near(dy[rows], want_dy, "dy")
+    near(out["gate"][-len(gates):], want_gate, "dgate")
+    del y, want_h, want_z, stored, pre, want_dx, want_dy, dx, dy, z, s["x"]
+    total = {n: torch.zeros(D, dtype=torch.float64, device="cuda") for n in live}
+    for a in range(0, M, 1 << 16):
+        b = min(M, a + (1 << 16))
+        hh, yy, dz, dh = (t[a:b].double() for t in (h, s["y"], s["dz"], s["dh"]))
+        rh, ry = ((t.square().mean(-1, keepdim=True) + eps).rsqrt() for t in (hh, yy))
+        dn = dz * vec["gamma_pre"].double()
+        g = (dh + rh * (dn - hh * rh * (dn * hh * rh).mean(-1, keepdim=True))) * yy * ry * s["gate"][torch.arange(a, b, device="cuda") // gate_rows].double()
+        total["gamma_pre"] += (dz * hh * rh).sum(0)
+        total["res_scale"] += (g * vec["gamma_post"].double()).sum(0)
+        total["gamma_post"] += (g * vec["res_scale"].double()).sum(0)
+    for n in live:
+        near(out[n], total[n], "d" + n)
+    del s, h, out, vec
+    torch.cuda.empty_cache()

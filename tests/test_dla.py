@@ -563,3 +563,67 @@ def test_offsets_past_32_bits(sdm):
     near(y, want_y)
     near(cache[n - 1:], want_S)
     assert not cache[:n - 1:97].any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,layout", [("bf16", "token_major"), ("bf16", "head_major"), ("f32", "token_major")])
+def test_long_sequences_past_32_bits(sdm, dtype, layout):
+    """A sequence of more than 2^31 values, key heads shared: what its first and its last tokens give, forwards and backwards.  Its
+    heads forget within 100 tokens (exp(-50) of a state is left), so that 300 tokens are all that these depend on."""
+    import torch
+    from dla_reference import dla, dla_grads, near
+    H, Hk, d, n, keep = 16, 8, 128, 300, 200
+    T, tm = 2 ** 31 // (H * d) + 77, layout == "token_major"
+    s = _inputs(1, H, Hk, T, d, d, dtype, tm)
+    assert s["v"].numel() > 2 ** 31
+    s["log_decay"] = -torch.linspace(0.5, 2.0, H, device="cuda")
+    shape = sdm.DlaShape.make(1, H, T, d, d, H_k=Hk, dtype=dtype, layout=layout)
+    y, state = run_forward(sdm, s, shape)
+    dq, dk, dv, dstate0 = run_backward(sdm, s, shape)
+    zero = torch.zeros_like(s["state"])
+    for last in (False, True):
+        def cut(x, m):
+            axis = 1 if tm else 2
+            return x.narrow(axis, x.shape[axis] - m if last else 0, m)
+
+        part = {x: cut(s[x], n).contiguous() for x in ("q", "k", "v", "dy")}
+        S0, dS = (zero, s["dstate"]) if last else (s["state"], zero)
+        want_y, want_S = dla(part["q"], part["k"], part["v"], s["log_decay"], S0, 1.0, None, tm)
+        near(cut(y, keep), cut(want_y, keep), f"y, last {last}")
+        if last:
+            near(state, want_S, "state")
+        want = dla_grads(part["q"], part["k"], part["v"], s["log_decay"], S0, 1.0, part["dy"], dS, None, tm)
+        for name, a, b in zip(("dq", "dk", "dv"), (dq, dk, dv), want):
+            near(cut(a, keep), cut(b, keep), f"{name}, last {last}")
+        if not last:
+            near(dstate0, want[3], "dstate0")
+    assert sdm.device_status() == 0
+    del s, y, state, dq, dk, dv
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+def test_sequences_past_32_bits(sdm):
+    """The second of two sequences begins past 2^31 values and has few tokens, the first none: what is past the lengths is zero."""
+    import torch
+    from dla_reference import dla, dla_grads, near
+    H, Hk, d, n = 16, 8, 128, 300
+    T = 2 ** 31 // (H * d) + 64
+    s = _inputs(2, H, Hk, T, d, d, "bf16", True)
+    lengths = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    shape = sdm.DlaShape.make(2, H, T, d, d, H_k=Hk, dtype="bf16", layout="token_major")
+    y, state = run_forward(sdm, s, shape, lengths)
+    grads = run_backward(sdm, s, shape, lengths)
+    part = {x: s[x][1:, :n].contiguous() for x in ("q", "k", "v", "dy")}
+    want_y, want_S = dla(part["q"], part["k"], part["v"], s["log_decay"], s["state"][1:], 1.0, None, True)
+    want = dla_grads(part["q"], part["k"], part["v"], s["log_decay"], s["state"][1:], 1.0, part["dy"], s["dstate"][1:], None, True)
+    near(y[1:, :n], want_y, "y")
+    near(state[1:], want_S, "state")
+    for name, a, b in zip(("dq", "dk", "dv"), grads, want):
+        near(a[1:, :n], b, name)
+        assert not a[0].any() and not a[1, n:].any(), name
+    near(grads[3][1:], want[3], "dstate0")
+    assert not y[0].any() and not y[1, n:].any()
+    assert torch.equal(state[0], s["state"][0]) and torch.equal(grads[3][0], s["dstate"][0])
+    del s, y, state, grads
+    torch.cuda.empty_cache()

@@ -256,3 +256,35 @@ def test_captured(sdm):  # noqa: F811
     assert abs(float(stats[0]) - want) <= 1e-6 * want
     for g, o in zip(grads, outs):
         assert ((o.double() - g.double() * (2 / want)).abs() <= ((2.0 ** -8 if o.dtype == torch.bfloat16 else 2.0 ** -24) + 1e-6) * (g.double() * (2 / want)).abs()).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", [None, "f32"])
+def test_a_tensor_past_32_bits(sdm, out):  # noqa: F811
+    """One gradient of more than 2^31 values, off 16 bytes, and a small one behind it; what lies after them stays."""
+    import torch
+    n = 2 ** 31 + 12345
+    g = torch.Generator(device="cuda").manual_seed(1)
+    buf = torch.empty(n + 64, dtype=torch.bfloat16, device="cuda")
+    for a in range(0, buf.numel(), 1 << 28):
+        part = buf[a:a + (1 << 28)]
+        part.copy_(torch.randn(part.numel(), generator=g, device="cuda"))
+    grads = [buf[3:3 + n], buf[3 + n:20 + n]]
+    kept = {a: buf[a:a + 4096].clone() for a in (0, 2 ** 31 - 2048, buf.numel() - 4096)}
+    want = math.sqrt(sum(float(buf[3:20 + n][a:a + (1 << 28)].double().square().sum()) for a in range(0, n + 17, 1 << 28)))
+    outs = None if out is None else [torch.full((x.numel(),), math.nan, device="cuda") for x in grads]
+    norm, factor = _run(sdm, grads, outs, want / 4)
+    assert abs(norm - want) <= 1e-6 * want and abs(factor - 0.25) <= 1e-6 * 0.25
+    half = 2.0 ** -8 if outs is None else 2.0 ** -24
+    for a, before in kept.items():
+        end = a + 4096
+        lo, hi = max(a, 3), min(end, 3 + n)
+        got = buf[lo:hi] if outs is None else outs[0][lo - 3:hi - 3]
+        x = before[lo - a:hi - a].double() * 0.25
+        assert ((got.double() - x).abs() <= (half + 1e-6) * x.abs()).all(), a
+        assert torch.equal(buf[a:lo], before[:lo - a]) and torch.equal(buf[20 + n:][:end - 20 - n], before[20 + n - a:] if end > 20 + n else before[:0])
+    last = buf[3 + n:20 + n] if outs is None else outs[1]
+    x = kept[buf.numel() - 4096][3 + n - (buf.numel() - 4096):][:17].double() * 0.25
+    assert ((last.double() - x).abs() <= (half + 1e-6) * x.abs()).all()
+    del buf, grads, outs, last, got
+    torch.cuda.empty_cache()
