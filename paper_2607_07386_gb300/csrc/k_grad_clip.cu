@@ -268,7 +268,7 @@ int64_t blocks_of(const sdm_grad_tensor& t) {
     const int64_t bytes = t.n * (t.dtype == SDM_F32 ? 4 : 2);
     return (bytes + BLOCK - 1) / BLOCK;
 }
-// The next launch's table; `i` goes past what it took.
+// The next launch's table; `i` goes past what it took.  All blocks fit an int: a list has up to 2^40 values in 2^24 tensors, 2^27 + 2^24 blocks.
 template <int N>
 void fill(GradTable<N>& t, int64_t n, const sdm_grad_tensor* list, int64_t& i) {
     t.count = 0;
@@ -277,7 +277,6 @@ void fill(GradTable<N>& t, int64_t n, const sdm_grad_tensor* list, int64_t& i) {
         const sdm_grad_tensor& g = list[i];
         const int64_t b = blocks_of(g);
         if (b == 0) continue;
-        if (blocks + b > INT32_MAX / 2) break;
         const bool half = g.dtype == SDM_BF16, out_half = g.out_dtype == SDM_BF16;
         // the pieces of src begin on 16 bytes; those of dst must begin on their own size
         const uintptr_t s = reinterpret_cast<uintptr_t>(g.grad), d = reinterpret_cast<uintptr_t>(g.out);
@@ -330,12 +329,11 @@ cudaError_t run(int64_t n, const sdm_grad_tensor* list, bool write, float max_no
 
 }  // namespace
 
-// A share is three sums in 64 bits; every launch has at most CTAS of them, and at least MANY tensors or 2^30 blocks but the last.
+// A share is three sums in 64 bits; a launch has at most CTAS of them, and no more than blocks.
 size_t grad_bytes(int64_t n, const sdm_grad_tensor* t) {
-    size_t shares = 0, blocks = 0;
+    size_t blocks = 0;
     for (int64_t i = 0; i < n; ++i) blocks += static_cast<size_t>(blocks_of(t[i]));
-    shares = (static_cast<size_t>(tensors_of(n, t)) + FEW - 1) / FEW + blocks / (1u << 29) + 1;
-    shares *= CTAS;
+    const size_t shares = (static_cast<size_t>(tensors_of(n, t)) + MANY - 1) / MANY * CTAS;
     return (blocks < shares ? blocks : shares) * 3 * 8;
 }
 
