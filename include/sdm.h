@@ -514,7 +514,7 @@ size_t sdm_dla_backward_workspace_bytes(const sdm_dla_shape* shape);
  * clamped and sets bit 0 of the device status word.  With T = 0 nothing is done.  An infinity or NaN in
  * a live token reaches its own and later outputs and the state; never an earlier token's.  Bit 2 of the status word (a
  * bounded wait ran out, which no input causes): y and the state are undefined, as are the gradients of sdm_dla_backward.
- * workspace: sdm_dla_workspace_bytes(shape), 256-byte aligned; calls that overlap must not share it. */
+ * workspace: sdm_dla_workspace_bytes(shape), 256-byte aligned; calls that overlap must not share it.  One token without lengths needs none. */
 sdm_status sdm_dla_forward(const sdm_dla_shape* shape, const void* q, const void* k, const void* v,
                            const float* log_decay, const int32_t* lengths, float* state, void* y,
                            void* workspace, size_t workspace_bytes, sdm_stream_t stream);

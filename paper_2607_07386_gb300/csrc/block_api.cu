@@ -152,15 +152,17 @@ sdm_status dla_forward(const char* who, const sdm_dla_shape* s, const void* q, c
                        const int32_t* lengths, float* state, void* y, void* workspace, size_t workspace_bytes, int32_t cut_polls, sdm_stream_t stream) {
     const DlaSizes z = dla_sizes(s);
     DlaLayout L = dla_layout(s, false);
+    const bool step = s->T == 1 && lengths == nullptr;       // on the kernel of sdm_dla_step, which takes no workspace
+    const size_t need = step ? 0 : L.total;
     const Buf bufs[] = {{"q", q, z.qk, 16, false, false}, {"k", k, z.qk, 16, false, false}, {"v", v, z.v, 16, false, false},
                         {"log_decay", log_decay, static_cast<size_t>(s->H) * 4, 4, false, false},
                         {"lengths", lengths, static_cast<size_t>(s->B) * 4, 4, true, false},
                         {"state", state, z.state, 16, false, true}, {"y", y, z.v, 16, false, true},
-                        {"workspace", workspace, L.total, 16, true, true}};
+                        {"workspace", workspace, need, 16, true, true}};
     SDM_TRY(check_bufs(who, bufs, 8));
-    SDM_TRY(check_ws(who, workspace, workspace_bytes, L.total));
+    SDM_TRY(check_ws(who, workspace, workspace_bytes, need));
     SDM_TRY(sdm::api_status_word(&L.w.err));
-    if (s->T == 1 && lengths == nullptr) {
+    if (step) {
         const sdm::DlaStep d{q, k, v, log_decay, nullptr, state, y, s->B, s->H, s->H_k, s->d_k, s->d_v, s->B, s->scale, L.w.err};
         return done(sdm::launch_dla_step(s->dtype, d, reinterpret_cast<cudaStream_t>(stream)), who);
     }

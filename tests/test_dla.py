@@ -349,6 +349,21 @@ def test_one_token_is_a_step(sdm, dtype, d):
 
 
 @pytest.mark.gpu
+def test_one_token_takes_no_workspace(sdm):
+    """Where a prompt of that shape would (a contraction in two pieces), one token without lengths does not, and with them does."""
+    import torch
+    s = _inputs(2, 4, 2, 1, 256, 64, "bf16")
+    shape = sdm.DlaShape.make(2, 4, 1, 256, 64, H_k=2, scale=0.7)
+    assert sdm.dla_workspace_bytes(shape) > 0
+    y, state = torch.empty_like(s["v"]), s["state"].clone()
+    sdm.dla_forward(shape, s["q"], s["k"], s["v"], s["log_decay"], state, y)
+    want_y, want_S = run_forward(sdm, s, shape)
+    assert torch.equal(y, want_y) and torch.equal(state, want_S)
+    with pytest.raises(sdm.SdmError, match="workspace is NULL"):
+        sdm.dla_forward(shape, s["q"], s["k"], s["v"], s["log_decay"], state, y, lengths=torch.ones(2, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_prefill_in_pieces_then_tokens(sdm, dtype):
     """A prompt in two calls and the rest token by token gives what one call gives, in whatever pieces."""
