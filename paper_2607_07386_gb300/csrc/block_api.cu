@@ -53,7 +53,7 @@ sdm::DlaWalk dla_walk(const sdm_dla_shape* s, const float* log_decay, const int3
 }
 
 // The roles of a call, the scan's with a wide contraction in two pieces, and where a workspace holds what: the pieces'
-// states, then the shares of the outputs that are sums (of value heads that share a key head, of the contraction's pieces).
+// states and decays, then the shares of the outputs that are sums (of value heads that share a key head, of the contraction's pieces).
 struct DlaCall {
     const void* r; const void* k; const void* v;
     void* out;
@@ -65,7 +65,7 @@ struct DlaLayout {
     sdm::DlaSums sums;
     int call[sdm::DLA_ROLES];     // the buffers that a role has, and the sum that it gives a share to (-1: none)
     int sum[sdm::DLA_ROLES];
-    size_t share[sdm::DLA_ROLES], total;
+    size_t share[sdm::DLA_ROLES], seg_pow, total;
 };
 DlaLayout dla_layout(const sdm_dla_shape* s, bool back) {
     DlaLayout L{};
@@ -122,13 +122,16 @@ DlaLayout dla_layout(const sdm_dla_shape* s, bool back) {
         L.w.seg_role[i] = q.x0 > 0 ? L.w.seg_role[i - 1] : static_cast<int64_t>(state);
         if (L.w.segs > 1 && q.x0 == 0) state += chains * L.w.segs * q.width * q.db;
     }
-    const size_t at = align256(L.w.span > 0 ? sdm::dla_scan_cut_bytes() : state * 4);
+    L.seg_pow = state * 4;                                   // a state is a multiple of 16 floats
+    const size_t pows = L.w.segs > 1 ? chains * L.w.roles * 3 * sizeof(float2) : 0;
+    const size_t at = align256(L.w.span > 0 ? sdm::dla_scan_cut_bytes() : L.seg_pow + pows);
     for (int i = 0; i < L.w.roles; ++i) L.share[i] = at + share[i] * 4;
     L.total = at + align256(floats * 4);
     return L;
 }
 cudaError_t dla_run(int dtype, DlaLayout& L, const DlaCall* calls, char* ws, cudaStream_t stream) {
     L.w.seg_state = reinterpret_cast<float*>(ws);
+    L.w.seg_pow = reinterpret_cast<float2*>(ws + L.seg_pow);
     for (int i = 0; i < L.w.roles; ++i) {
         sdm::DlaRole& r = L.w.role[i];
         const DlaCall& c = calls[L.call[i]];

@@ -39,8 +39,10 @@ struct DlaWalk {
     int slices[DLA_ROLES];    // of db, a CTA each
     // The tokens may be cut into `segs` pieces of `seg_chunks` chunks that run at once: a first launch copies the first
     // state and takes what each piece but the last adds to it into seg_state [role][B * H][segs][width * db], a small one turns
-    // that into the states that the pieces start from, and the walk proper takes them.
+    // that into the states that the pieces start from, and the walk proper takes them.  The decays over the pieces, in seg_pow
+    // [role][B * H][3]: a whole one, the first, the last that has tokens.
     int segs, seg_chunks;
+    float2* seg_pow;
     // Or the scan spreads more chains than SMs evenly over these: a list of all chains' chunks, one chain after the other, is cut
     // every `span` chunks (0: it is not).  A chain that is cut hands its state over in seg_state.
     int span;
@@ -62,6 +64,14 @@ __device__ __forceinline__ float2 dla_pow2(float ld, int n) {
     const double f = n == 0 ? 1.0 : exp(static_cast<double>(n) * static_cast<double>(ld));
     const float hi = static_cast<float>(f);
     return make_float2(hi, gdn_finite(hi) ? static_cast<float>(f - static_cast<double>(hi)) : 0.f);
+}
+// The decays over the pieces of a walk, in two parts (they are multiplied on once a piece); C tokens a chunk, which = 0, 1, 2.
+__device__ __forceinline__ void dla_piece_pow(const DlaWalk& w, int role, int64_t chain, float ld, int len, int C, int which) {
+    const int chunks = (len + C - 1) / C, s = which == 1 ? 0 : max(0, (chunks - 1) / w.seg_chunks);
+    const int s0 = min(s * w.seg_chunks, chunks), s1 = min(s0 + w.seg_chunks, chunks);
+    int n = (s1 - s0) * C;                                   // the walk's partial chunk is the sequence's last
+    if (s0 < s1 && (w.role[role].reverse ? s0 == 0 : s1 == chunks)) n -= chunks * C - len;
+    w.seg_pow[(role * static_cast<int64_t>(w.B) * w.H + chain) * 3 + which] = dla_pow2(ld, which == 0 ? w.seg_chunks * C : n);
 }
 __device__ __forceinline__ int dla_length(const DlaWalk& w, int b) {
     if (w.lengths == nullptr) return w.T;

@@ -189,6 +189,7 @@ __global__ void __launch_bounds__(ST, 1) k_dla_scan(const __grid_constant__ Scan
         ctl.lam[tid - 96][0] = f.x;
         ctl.lam[tid - 96][1] = f.y;
     }
+    if (SUMS && seg == 0 && col0 == 0 && tid >= 128 && tid < 131) dla_piece_pow(w, role, chain, ld, len, C, tid - 128);
     __syncthreads();
     if (tid < 2 * C) {
         const int k = tid / C, i = tid % C, n = k ? last_n : C;

@@ -436,6 +436,28 @@ def test_gradient_against_differences(sdm):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d,T", [("bf16", 128, 19456), ("bf16", 64, 9001), ("f32", 64, 22000), ("f32", 128, 6001)])
+@pytest.mark.parametrize("log_decay", [0.0, -1e-6, -1e-5, -1e-4])
+def test_long_memories_over_many_pieces(sdm, dtype, d, T, log_decay):
+    """One chain with a slow decay, its tokens in many pieces: each chunk's step of the state, a decay and an addition, is off by at most
+    2^-24 of it, and so are n of them in a row, of either sign, by 2^-24 sqrt(n)."""
+    import torch
+    s = _inputs(1, 1, 1, T, d, d, dtype)
+    s["log_decay"] = torch.tensor([log_decay], device="cuda")
+    shape = sdm.DlaShape.make(1, 1, T, d, d, dtype=dtype)
+    assert sdm.dla_plan(shape)["pieces"] > 10
+    _, state = run_forward(sdm, s, shape)
+    dstate0 = run_backward(sdm, s, shape)[3]
+    ld, at = s["log_decay"].double(), torch.arange(T, device="cuda")
+    q, k, v, dy = (s[x][0, 0].double() for x in ("q", "k", "v", "dy"))
+    want = torch.exp(ld * T) * s["state"][0, 0].double() + (torch.exp(ld * (T - 1 - at))[:, None] * k).T @ v
+    want0 = torch.exp(ld * T) * s["dstate"][0, 0].double() + (torch.exp(ld * (at + 1))[:, None] * q).T @ dy
+    limit = 2.0 ** -24 * math.sqrt(T / (64 if dtype == "bf16" else 32))
+    for name, a, b in (("state", state, want), ("dstate0", dstate0, want0)):
+        assert float((a[0, 0].double() - b).norm() / b.norm()) <= limit, name
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,B,H,d,T", [("f32", 1, 2, 64, 100), ("bf16", 1, 2, 128, 700), ("bf16", 10, 16, 64, 700)])
 def test_captured_and_on_another_stream(sdm, dtype, B, H, d, T):
     """A captured forward, backward and step replay with new inputs, while another stream runs the same calls."""
