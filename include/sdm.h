@@ -496,7 +496,8 @@ sdm_status sdm_linear_backward(const sdm_linear_shape* shape, const void* x, con
  * (-inf: lam = 0; above 0 the state grows); it is a setting of the model and has no gradient.
  * ------------------------------------------------------------------------------------------ */
 typedef struct {
-    int32_t B, H, H_k, T;     /* sequences, value heads, key heads (H a multiple of H_k), tokens */
+    int32_t B, H, H_k, T;     /* sequences, value heads, key heads (H a multiple of H_k), tokens: B and H at most 65535,
+                                 B H T at most 2^31 */
     int32_t d_k, d_v;         /* at most 256; times the element size multiples of 16 bytes */
     int32_t dtype;            /* sdm_dtype of q, k, v, y and of their gradients */
     int32_t layout;           /* SDM_HEAD_MAJOR or SDM_TOKEN_MAJOR, of q, k, v, y and their gradients */
@@ -558,7 +559,7 @@ sdm_status sdm_test_dla_wait_timeout(const sdm_dla_shape* shape, const void* q, 
  * next block takes.  Products are element by element; z is the norm of h as stored.
  * ------------------------------------------------------------------------------------------ */
 typedef struct {
-    int64_t M;                /* rows */
+    int64_t M;                /* rows, at most 2^31 */
     int64_t gate_rows;        /* rows that share a row of the gate: 1, or for example the tokens of a sequence */
     int32_t D;                /* row width, at most 16384; times the element size a multiple of 16 bytes */
     int32_t dtype;            /* sdm_dtype of x, y, gate, h, z and of their gradients */
@@ -599,7 +600,7 @@ typedef struct {
 } sdm_grad_tensor;
 
 /* Bytes of workspace for a list of n tensors (host memory; 0 if there is no element, or with
- * sdm_last_error set for an invalid list). */
+ * sdm_last_error set for an invalid list).  At most 2^24 tensors with 2^40 values in all. */
 size_t sdm_grad_workspace_bytes(int64_t n, const sdm_grad_tensor* tensors);
 
 /* stats: [2] float32 on the device, the norm and the factor min(1, max_norm / norm).  The norm of finite gradients is

@@ -8,9 +8,9 @@
 //   G = sum gate q over all:  dres_scale = gamma_post G,  dgamma_post = res_scale G.
 // So two column sums are all that the gradients of four vectors take.
 //
-// Bound by memory: everything is read once and written once, next rows on their way in shared memory (without: 125 and 211
-// us for rows of 2,048), the vectors in registers.  32,768 rows of 2,048 in bf16: forward 95 us, 5.6 TB/s, 0.83 of the copy bandwidth;
-// backward 152 us, 5.3 TB/s, 0.78, where the warps' issue slots are two thirds taken and the column sums' registers leave
+// Bound by memory: everything is read once and written once, next rows on their way in shared memory (without: 126 and 213
+// us for rows of 2,048), the vectors in registers.  32,768 rows of 2,048 in bf16: forward 99 us, 5.4 TB/s, 0.80 of the copy bandwidth;
+// backward 151 us, 5.3 TB/s, 0.78, where the warps' issue slots are two thirds taken and the column sums' registers leave
 // two CTAs an SM.  One row: 6 and 11 us, one launch and two.  Sums over a row: TPR threads a row, butterflies
 // within a warp, then the warps' shares through shared memory.
 #include "dla_internal.h"
@@ -109,7 +109,7 @@ __device__ __forceinline__ void row_sum(float (&s)[N], float (*sh)[16][8], int& 
     turn ^= 1;
 }
 
-// CTAs on an SM: of 256 threads three with 80 registers each (four: 98 to 100 us for rows of 2,048, three: 95 to 98), and
+// CTAs on an SM: of 256 threads three with 80 registers each (four are no faster: 99 to 100 us for rows of 2,048, three 99), and
 // for the gradients two with 128.
 constexpr int SMS = 152;
 __host__ __device__ constexpr int fore_ctas(int tpr) { return tpr > 256 ? 1 : 768 / cta(tpr); }
@@ -119,8 +119,8 @@ __host__ __device__ constexpr int back_ctas(int tpr) { return tpr > 256 ? 1 : 51
 template <class D, int TPR, int VE>
 struct Row {
     static constexpr int E = D::E, P = E / 2, V = VE / E, ROWS = cta(TPR) / TPR;
-    // The vectors' values of a thread stay in registers (8,192 rows of 8,192: 95 and 173 us, read again for each row 133 and 280);
-    // 32 of each are more than there are.
+    // The vectors' values of a thread stay in registers (8,192 rows of 8,192: 96 and 169 us, read again for each row 133 and 280).
+    // With 32 of each there are not enough registers, and they are read again; the gradients' sums spill all the same.
     static constexpr bool KEEP = VE <= 16;
 };
 // Rows on their way: each thread copies its own pieces of N arrays' next S rows into slots of its own in shared memory
@@ -584,13 +584,17 @@ NormCut norm_cut(int64_t M, int D, int tpr, bool shared) {
     return c;
 }
 
-// Threads a row and values a thread: eight values (16 make the registers of the gradients' sums: bf16 rows of 2,048 99 and 200 us forward
-// and backward, with eight 95 and 152) in up to 256 threads, as several CTAs of an SM hide each other's waits.  Then it is what
-// moves with two 16-byte pieces of an array a thread: 16 bf16 values (rows of 4,096: 102 and 156 us, 512 threads of eight 107 and 176) or
+// Threads a row and values a thread: eight values (16 make the registers of the gradients' sums: bf16 rows of 2,048 103 and 204 us forward
+// and backward, with eight 99 and 151) in up to 256 threads, as several CTAs of an SM hide each other's waits.  Then it is what
+// moves with two 16-byte pieces of an array a thread: 16 bf16 values (rows of 4,096: 102 and 152 us, 512 threads of eight 107 and 173) or
 // 512 threads of eight float32 values (98 and 152, 256 of 16 101 and 231).  Then 512 threads of 16 and 32.
 // A power of two leaves threads without work where the width is none.  bf16 gradients, 134 MB an array: rows of 768 by 96 threads
 // 146 us, by 128 180; 1,280 by 160 154, by 256 204; 1,536 by 192 156, by 256 190; 2,560 by 160 of 16 163, by 256 193.  Forward: 101 and
 // 94, 97 and 115, 101 and 101, 99 and 98 (with a gate a row 117 and 112), so there it is 160 threads of eight alone.
+// Wider rows leave one CTA of 512 threads an SM, and the gradients of 16 float32 and of 32 values spill (234 and 844 bytes in float32, 338
+// in bf16) and have one row on its way or none.  134 MB an array, forward and backward: float32 rows of 4,096 98 and 149 us, 5,120 98 and
+// 241, 8,192 95 and 233, 16,384 120 and 355; bf16 rows of 5,120 107 and 210, 6,144 93 and 188, 8,192 96 and 169, 10,240 155 and 387, 16,384 132
+// and 338.
 struct RowPlan {
     int tpr, ve;
 };

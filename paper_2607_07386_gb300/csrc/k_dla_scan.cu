@@ -19,9 +19,10 @@
 //
 // Bound by that chain: a chunk takes 1.9 us, 3,650 cycles, of which 2,050 are its 56 MMAs (32 cycles each with A in TMEM, 48
 // with A in shared memory) and most of the rest hand-overs, 250 cycles from a product's end to the warps that read it.
-// 8 x 16 heads of 128 x 4,096 tokens: forward 134 us, 0.6 of the copy bandwidth (537 MB of q, k, v and y are 79); backward,
-// three runs of this walk, 384 chains spread over the SMs, 370 us (405 in three rounds of whole chains).  Tried and no faster, forward: P by products of 64 rows and lanes moved by 16 (136 to 162
-// us), three warps that issue (137), the state's product first (140), waits that sleep (148).
+// 8 x 16 heads of 128 x 4,096 tokens: forward 135 us (64 chunks, and 13 us for the first and the last), 0.6 of the copy bandwidth (537
+// MB of q, k, v and y are 79); backward, three runs of this walk, 384 chains spread over the SMs, 377 us (405 in three rounds of whole
+// chains).  Tried and no faster, forward: P by products of 64 rows and lanes moved by 16 (136 to 162 us), three warps that issue (137), the
+// state's product first (140), waits that sleep (148).
 //
 // A value of v that is not finite must stay out of the outputs before its token, which share its products: v is zero in
 // them from that token on, its column's outputs from there are NaN, and so is the column of the state.
@@ -657,8 +658,9 @@ int64_t scan_ctas(const DlaWalk& w) {
 
 }  // namespace
 
-// With fewer CTAs than half of the SMs the tokens are cut, so that every SM has a piece, where that pays: a chunk takes 2.1 us
-// in the walk and about 1.1 in the walk for the sums, which with the joining launch costs 10 us more to begin with.
+// With fewer CTAs than half of the SMs the tokens are cut, so that every SM has a piece, where that pays: a chunk takes 1.9 us
+// in the walk and about 1.1 in the walk for the sums, which with the joining launch costs 10 us more to begin with.  The rule goes by T: a
+// piece past the end of a short sequence has nothing to do, and the longest sequence's pieces take as long as if all had its length.
 //
 // More CTAs than SMs are spread over these where the last round's time that this saves is more than its costs: about 6 us for the
 // cut chains' extra starts, and 1 us for every CTA's number.  Forward (backward), 10 x 16 heads of 128: 256 -> 154 us (532 -> 458)

@@ -7,9 +7,11 @@
 // the decay is above 1 for log_decay <= 0, so nothing can overflow however fast a head forgets.
 //
 // A CTA takes 32 columns of one state: the state lies in registers and, for the reads, in shared memory;
-// r, k and v of the next chunk are on their way while this one is computed.  Bound by the fp32 units' and shared memory's
-// latencies: three CTAs an SM hide each other's, and 256 threads were faster than 128 or 512.  4 x 8 heads of 64 x 1,024
-// tokens, forward: 91 us; the odd backward of 3 x 6 heads of 64 x 96, up to 333 tokens: 66 us, with float32 sums throughout.
+// r, k and v of the next chunk are on their way while this one is computed.  Every CTA of a chain takes the whole of P for itself: with
+// d_v = 128 four times.  Bound by the fp32 units' and shared memory's latencies, which two CTAs an SM hide of each other (128 registers
+// a thread to widths of 128; 252 at 256 in float32, and one CTA); 256 threads were faster than 128 or 512.  4 x 8 heads of 64 x 1,024
+// tokens, forward: 91 us; 8 x 16 heads of 128 x 1,024: 608, and 1,660 backward; the odd backward of 3 x 6 heads of 64 x 96, up to 333
+// tokens: 68 us, with float32 sums throughout.
 //
 // The single token reads and writes its state once, eight rows of four columns a thread, all its loads in flight together, and is bound by memory:
 // 256 sequences, 16 heads of 128 x 128 (537 MB): 84.5 us, 0.94 of the copy bandwidth; one sequence: 5.9 us, a launch.
@@ -453,9 +455,11 @@ void dla_plan(DlaWalk& w) {
         dla_scan_plan(w);
         return;
     }
-    // The tokens are cut until there are three CTAs for every SM, which hide each other's waits; a piece keeps at least three
+    // The tokens are cut until there are three CTAs for every SM, one more than run at once; a piece keeps at least three
     // chunks, for the pass over the pieces' sums costs half of a walk and a launch.  One head of 64, 2,048 tokens: 318 us whole,
-    // 41 cut; 4 x 8 heads, 1,024 tokens: 162 and 91.
+    // 41 cut; 4 x 8 heads, 1,024 tokens: 162 and 91.  Cut for one CTA an SM, for two and for three, forward (backward): 4 x 8 heads of 64 x
+    // 1,024 99 (197), 78 (197), 90 (203); 8 heads of 128 x 2,048 136 (363), 118 (284), 133 (302); 3 x 6 heads of 64 x 96 x 333 47
+    // (66), 46 (81), 46 (91), with the lengths of a ragged batch 47 (66), 43 (82), 43 (68).
     constexpr int64_t SMS = 152;
     int64_t ctas = 0;
     for (int i = 0; i < w.roles; ++i) ctas += (w.role[i].db + COLS - 1) / COLS;

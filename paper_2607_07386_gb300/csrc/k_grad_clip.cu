@@ -5,7 +5,7 @@
 // of 32 KB into one range a CTA, and the second walks every range backwards, so that what the first read last is still in L2.
 // The loads of a block are on their way while the one before is worked on.
 //
-// 1.14 GB: the norm in 175 us (6.5 TB/s), with the scaling 525 (0.96 of the copy bandwidth for three passes).
+// 1.15 GB: the norm in 181 us (6.4 TB/s), with the scaling 549 (0.93 of the copy bandwidth for three passes).
 //
 // The list goes to the kernels in their parameters: nothing is copied to the device first, and a captured launch holds its
 // list.  A CTA's sums go to the workspace and are joined in order (by every CTA of the second pass for itself), so the
