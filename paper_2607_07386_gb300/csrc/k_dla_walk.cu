@@ -10,7 +10,7 @@
 // r, k and v of the next chunk are on their way while this one is computed.  Every CTA of a chain takes the whole of P for itself: with
 // d_v = 128 four times.  Bound by the fp32 units' and shared memory's latencies, which two CTAs an SM hide of each other (128 registers
 // a thread to widths of 128; 252 at 256 in float32, and one CTA); 256 threads were faster than 128 or 512.  4 x 8 heads of 64 x 1,024
-// tokens, forward: 91 us; 8 x 16 heads of 128 x 1,024: 608, and 1,660 backward; the odd backward of 3 x 6 heads of 64 x 96, up to 333
+// tokens, forward: 91 us; 8 x 16 heads of 128 x 1,024: 601, and 1,656 backward; the odd backward of 3 x 6 heads of 64 x 96, up to 333
 // tokens: 68 us, with float32 sums throughout.
 //
 // The single token reads and writes its state once, eight rows of four columns a thread, all its loads in flight together, and is bound by memory:
@@ -238,10 +238,9 @@ __global__ void __launch_bounds__(WT) k_dla_walk(const DlaWalk w) {
                     }
                     float2 u = make_float2(y[i][j], 0.f);    // in the same order
 #pragma unroll 1
-                    for (int t = 0; t < n; ++t) {
-                        if (ro.reverse ? t < ti + i : t > ti + i) continue;
-                        float& s = t & 1 ? u.y : u.x;
-                        s = fmaf(sm.P[ti + i][t], sm.v[tc + 16 * j][t], s);
+                    for (int t = 0; t < n; t += 2) {
+                        if (ro.reverse ? t >= ti + i : t <= ti + i) u.x = fmaf(sm.P[ti + i][t], sm.v[tc + 16 * j][t], u.x);
+                        if (ro.reverse ? t + 1 >= ti + i && t + 1 < n : t + 1 <= ti + i) u.y = fmaf(sm.P[ti + i][t + 1], sm.v[tc + 16 * j][t + 1], u.y);
                     }
                     y[i][j] = u.x + u.y;
                 }
